@@ -504,6 +504,56 @@ int locmoe_moe_layer(const locmoe_shape_t *shape, const void *x, const int32_t *
                      const void *w_out, const locmoe_layer_buffers_t *bufs, void *out, void *stream);
 
 /*
+ * The norms around one block, fused with its gate and its residual (one pass over the rows).  The block's input is
+ * the normalised stream n, its output y (rows of the dispatched buffer, or token order), its gate the score R of the
+ * router.  Per token t, N(v) = v / sqrt(mean_j v_j^2 + eps):
+ *   v   = y[slot[t]], or y[t] with slot == NULL; 0 for a dropped token (slot < 0 or beyond the buffer) and for y == NULL
+ *   h'  = res_scale * h[t] + gate_w[t] * w_post * N(v)          (gate_w, w_post NULL: 1)
+ *   n   = w_pre * N(h')                                         (w_pre NULL: 1; from h' before it is rounded)
+ * so that one call ends a block and begins the next; y == NULL begins the first, n_out == NULL ends the last.
+ * Gating follows the norm: N undoes any factor on y, so y is passed as the experts give it.
+ * h, h_out, n_out [T][H] and y [T or D*E*C_alloc][H] of x_dtype; gate_w float[T]; w_post, w_pre float[H].  Sums in
+ * fp32 in a fixed order, outputs rounded once.  h_out may be h.  With slot == NULL C_alloc is not read.  Pointers are
+ * aligned to their elements; rows of whole 16-byte vectors (H % 8 == 0, 16-byte aligned arrays) take the fast kernel.
+ *
+ * Checkpoints (each pair NULL to skip): u8 = N(v), x8 = N(h') as [T][H] codes in E4M3 (8 bits, to nearest even),
+ * r_post, r_pre float[T] the reciprocal norms 1 / sqrt(mean + eps).  They are all the gradient needs of h' and y;
+ * a normalised element is at most sqrt(H), so H <= 200000 when they are asked for (448 is the format's largest).
+ */
+typedef struct {
+    const void *h; const void *y; const int32_t *slot; const float *gate_w; const float *w_post; const float *w_pre;
+    float res_scale; float eps;
+    void *h_out; void *n_out;                       /* one may be NULL                                */
+    uint8_t *u8; uint8_t *x8; float *r_post; float *r_pre;
+} locmoe_block_norm_t;
+int locmoe_block_norm(const locmoe_shape_t *shape, int32_t C_alloc, const locmoe_block_norm_t *b, void *stream);
+
+/*
+ * Its gradient.  dh_out, dn [T][H] are the gradients of h' and n (one may be NULL: zero); h_out and y as the forward
+ * call wrote / read them, or in their place the checkpoints x8, r_pre and u8, r_post (both sides in the same form).
+ * With x = N(h'), u = N(v), q and r the reciprocal norms:
+ *   D      = dh_out + q (dn w_pre - x mean(dn w_pre x))
+ *   dh     = res_scale * D                                       [T][H] of x_dtype, may be dh_out
+ *   dgate  = sum_j D w_post u                                    float[T]
+ *   dy     = r (gate_w w_post D - u gate_w dgate / H)            rows as y; with slot and inv (as locmoe_route wrote
+ *            them) rows with inv < 0 are zero-filled, without inv they are left alone
+ *   dw_post = sum_t gate_w D u,  dw_pre = sum_t dn x             float[H]
+ * Any output may be NULL.  Without dn, h_out / x8 are not read; without y / u8 the block has no branch (dy must be
+ * NULL).  dh_out, dn, dh, dy of x_dtype.  The sums over tokens have a fixed order: the results are deterministic.
+ * ws (only with dw_post or dw_pre): locmoe_block_norm_grad_bytes() bytes, 256-byte aligned.
+ */
+typedef struct {
+    const void *dh_out; const void *dn; const void *h_out; const void *y;
+    const uint8_t *u8; const uint8_t *x8; const float *r_post; const float *r_pre;
+    const int32_t *slot; const int32_t *inv; const float *gate_w; const float *w_post; const float *w_pre;
+    float res_scale; float eps;
+    void *dh; void *dy; float *dgate; float *dw_post; float *dw_pre;
+} locmoe_block_norm_grad_t;
+int locmoe_block_norm_grad_bytes(const locmoe_shape_t *shape, size_t *bytes);
+int locmoe_block_norm_grad(const locmoe_shape_t *shape, int32_t C_alloc, const locmoe_block_norm_grad_t *b, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/*
  * Host-side helpers of the capacity rule and the buffer layout: plain arithmetic
  * on host memory, nothing is launched.
  *

@@ -25,7 +25,7 @@ FLAG_DELTA_OVERRIDE, FLAG_MIN_SATURATED, FLAG_MIN_BINDS = 1, 2, 4
 EXPORTS = [
     "locmoe_workspace_bytes", "locmoe_gate", "locmoe_gate_ex", "locmoe_aux_loss_partial", "locmoe_capacity", "locmoe_capacity_noalloc", "locmoe_capacity_read", "locmoe_route", "locmoe_capacity_route", "locmoe_gate_route",
     "locmoe_conventional_capacity", "locmoe_batch_delta", "locmoe_dest_order",
-    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
+    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_block_norm", "locmoe_block_norm_grad_bytes", "locmoe_block_norm_grad", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
 ]
 
 
@@ -62,6 +62,19 @@ class LayerBuffers(C.Structure):
                                            "drop", "inv", "counts", "kept", "send_counts", "load", "locality",
                                            "status", "ws")] + [("ws_bytes", C.c_size_t)] + \
                [(n, C.c_void_p) for n in ("buf", "h1", "y")]
+
+
+class BlockNorm(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("h", "y", "slot", "gate_w", "w_post", "w_pre")] + \
+               [("res_scale", C.c_float), ("eps", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("h_out", "n_out", "u8", "x8", "r_post", "r_pre")]
+
+
+class BlockNormGrad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dh_out", "dn", "h_out", "y", "u8", "x8", "r_post", "r_pre", "slot", "inv", "gate_w",
+                                           "w_post", "w_pre")] + \
+               [("res_scale", C.c_float), ("eps", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("dh", "dy", "dgate", "dw_post", "dw_pre")]
 
 
 CAPACITY_BYTES = C.sizeof(Capacity)
@@ -105,6 +118,9 @@ def _load() -> C.CDLL:
     lib.locmoe_topk_select.argtypes = [C.POINTER(Shape), vp, vp, vp, i32, vp, vp, vp]
     lib.locmoe_topk_fold.argtypes = [C.POINTER(Shape), i32, vp, vp]
     lib.locmoe_combine_topk.argtypes = [C.POINTER(Shape), i32, vp, i32, i32, vp, vp, vp, vp]
+    lib.locmoe_block_norm.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNorm), vp]
+    lib.locmoe_block_norm_grad_bytes.argtypes = [C.POINTER(Shape), C.POINTER(C.c_size_t)]
+    lib.locmoe_block_norm_grad.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNormGrad), vp, C.c_size_t, vp]
     lib.locmoe_conventional_capacity.argtypes = [C.POINTER(Shape), C.POINTER(CapacityRule), C.POINTER(C.c_int32)]
     lib.locmoe_batch_delta.argtypes = [vp, i32, C.POINTER(C.c_double)]
     lib.locmoe_dest_order.argtypes = [C.POINTER(Shape), i32, i32]
@@ -472,6 +488,57 @@ def locmoe_moe_layer(shape: Shape, x, src_dev, eps, rule: CapacityRule, C_alloc,
     return _check("locmoe_moe_layer", _lib.locmoe_moe_layer(
         C.byref(shape), _ptr(x), _ptr(src_dev), _ptr(eps), C.byref(rule), int(C_alloc), int(F), _ptr(w_in), _ptr(w_out),
         C.byref(bufs), _ptr(out), _stream(stream)))
+
+
+def _fill(struct, dtypes, numels, tensors, scalars):
+    """Pointer block of one call: every given tensor is checked for dtype, size, device and density and stored."""
+    for name, t in tensors.items():
+        if t is not None:
+            _want(t, dtypes[name], numels[name], name)
+            setattr(struct, name, _ptr(t).value)
+    for name, v in scalars.items():
+        setattr(struct, name, float(v))
+    return struct
+
+
+def _norm_types(shape: Shape, C_alloc, slot):
+    dt = torch.float32 if shape.x_dtype == F32 else torch.bfloat16
+    TH, rows = shape.T * shape.H, shape.D * shape.E * int(C_alloc) if slot is not None else shape.T
+    dtypes, numels = {}, {}
+    for names, t, n in ((("h", "h_out", "n_out", "dh_out", "dn", "dh"), dt, TH), (("y", "dy"), dt, rows * shape.H),
+                        (("u8", "x8"), torch.float8_e4m3fn, TH), (("gate_w", "r_post", "r_pre", "dgate"), torch.float32, shape.T),
+                        (("w_post", "w_pre", "dw_post", "dw_pre"), torch.float32, shape.H), (("slot",), torch.int32, shape.T),
+                        (("inv",), torch.int32, rows)):
+        for k in names:
+            dtypes[k], numels[k] = t, n
+    return dtypes, numels
+
+
+def locmoe_block_norm(shape: Shape, C_alloc, h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6,
+                      h_out=None, n_out=None, u8=None, x8=None, r_post=None, r_pre=None, stream=None) -> int:
+    """Post-norm, gate, residual and the next pre-norm in one pass; any array that is not wanted is None."""
+    b = _fill(BlockNorm(), *_norm_types(shape, C_alloc, slot),
+              dict(h=h, y=y, slot=slot, gate_w=gate_w, w_post=w_post, w_pre=w_pre, h_out=h_out, n_out=n_out, u8=u8, x8=x8,
+                   r_post=r_post, r_pre=r_pre), dict(res_scale=res_scale, eps=eps))
+    return _check("locmoe_block_norm", _lib.locmoe_block_norm(C.byref(shape), int(C_alloc), C.byref(b), _stream(stream)))
+
+
+def locmoe_block_norm_grad_bytes(shape: Shape) -> int:
+    out = C.c_size_t(0)
+    _check("locmoe_block_norm_grad_bytes", _lib.locmoe_block_norm_grad_bytes(C.byref(shape), C.byref(out)))
+    return out.value
+
+
+def locmoe_block_norm_grad(shape: Shape, C_alloc, dh_out=None, dn=None, h_out=None, y=None, u8=None, x8=None, r_post=None, r_pre=None,
+                           slot=None, inv=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, dh=None, dy=None,
+                           dgate=None, dw_post=None, dw_pre=None, ws=None, stream=None) -> int:
+    """Gradient of locmoe_block_norm, from h_out and y or from the 8-bit checkpoints."""
+    b = _fill(BlockNormGrad(), *_norm_types(shape, C_alloc, slot),
+              dict(dh_out=dh_out, dn=dn, h_out=h_out, y=y, u8=u8, x8=x8, r_post=r_post, r_pre=r_pre, slot=slot, inv=inv,
+                   gate_w=gate_w, w_post=w_post, w_pre=w_pre, dh=dh, dy=dy, dgate=dgate, dw_post=dw_post, dw_pre=dw_pre),
+              dict(res_scale=res_scale, eps=eps))
+    return _check("locmoe_block_norm_grad", _lib.locmoe_block_norm_grad(
+        C.byref(shape), int(C_alloc), C.byref(b), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def conventional_capacity(T: int, D: int, E: int, capacity_factor: float) -> int:

@@ -1,0 +1,123 @@
+"""One MoE block around the router: the norms before and after it fused with its gate and residual, their gradient with
+activations kept in 8 bits, and the whole expert layer for a few tokens.
+
+The functions here allocate their outputs (and the workspace, from torch's allocator on the current stream) and call the
+entry points of ``binding``; all arithmetic runs in the CUDA library.  ``BlockNorm`` is the differentiable form.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding as B
+
+
+class Checkpoint(NamedTuple):
+    """What the gradient needs of the forward pass, in 8 bits: the normalised rows (E4M3) and their reciprocal norms.
+    ``u8`` / ``r_post`` are None where the block has no branch, ``x8`` / ``r_pre`` where it has no next norm."""
+    u8: Optional[torch.Tensor]
+    x8: Optional[torch.Tensor]
+    r_post: Optional[torch.Tensor]
+    r_pre: Optional[torch.Tensor]
+
+
+def _row_shape(like: torch.Tensor, y, slot) -> tuple:
+    """Shape struct and row stride for [T][H] tensors whose block output has ``y``'s rows."""
+    if like.dim() != 2:
+        raise ValueError("expected a [T][H] tensor, got %s" % (tuple(like.shape),))
+    T, H = like.shape
+    rows = T if slot is None else y.shape[0]
+    return B.Shape(T, H, 1, 1, 1, B.dtype_code(like.dtype), B.LAYOUT_SEND), rows
+
+
+def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, checkpoint=False,
+               want_h=True, want_n=True, stream=None):
+    """h' = res_scale * h + gate_w * w_post * N(y[slot]),  n = w_pre * N(h').
+
+    Returns ``(h_out, n, ckpt)``; ``h_out`` / ``n`` are None when not wanted, ``ckpt`` a ``Checkpoint`` or None.  Without
+    ``y`` the block has no branch (the norm before the first block; ``want_h`` = False leaves out the copy of h)."""
+    shape, rows = _row_shape(h, y, slot)
+    T, H, dev = shape.T, shape.H, h.device
+    if y is not None and y.shape[-1] != H:
+        raise ValueError("y: rows of %d expected, got %d" % (H, y.shape[-1]))
+    if T == 0:
+        z = lambda *s, dt=h.dtype: torch.empty(*s, dtype=dt, device=dev)
+        ck = Checkpoint(z(0, H, dt=torch.float8_e4m3fn) if y is not None else None, z(0, H, dt=torch.float8_e4m3fn) if want_n else None,
+                        z(0, dt=torch.float32) if y is not None else None, z(0, dt=torch.float32) if want_n else None)
+        return z(0, H) if want_h else None, z(0, H) if want_n else None, ck if checkpoint else None
+    h_out = torch.empty_like(h) if want_h else None
+    n = torch.empty_like(h) if want_n else None
+    u8 = x8 = r_post = r_pre = None
+    if checkpoint and y is not None:
+        u8, r_post = torch.empty(T, H, dtype=torch.float8_e4m3fn, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
+    if checkpoint and want_n:
+        x8, r_pre = torch.empty(T, H, dtype=torch.float8_e4m3fn, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
+    B.locmoe_block_norm(shape, rows, h, y, slot, gate_w, w_post, w_pre, res_scale, eps, h_out, n, u8, x8, r_post, r_pre, stream)
+    return h_out, n, Checkpoint(u8, x8, r_post, r_pre) if checkpoint else None
+
+
+def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpoint] = None, slot=None, inv=None, gate_w=None,
+                    w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, want_dh=True, want_dy=True, want_dgate=True,
+                    want_dw=True, stream=None):
+    """Gradient of ``block_norm`` from the gradients of h' and n (one may be None).
+
+    The activations are ``h_out`` and ``y`` or, in their place, ``checkpoint``.  Returns ``(dh, dy, dgate, dw_post, dw_pre)``,
+    each None when not wanted or not there.  With slots, ``dy`` has ``inv``'s rows, those without a token zero."""
+    like = dn if dn is not None else dh_out
+    ck = checkpoint
+    branch = (ck.u8 if ck is not None else y) is not None
+    if slot is not None and inv is None:
+        raise ValueError("inv: needed with slot (it says how many rows y has and which of them are empty)")
+    shape, rows = _row_shape(like, inv, slot if branch else None)
+    T, H, dev = shape.T, shape.H, like.device
+    f32 = dict(dtype=torch.float32, device=dev)
+    dh = torch.empty_like(like) if want_dh else None
+    dy = torch.empty(rows, H, dtype=like.dtype, device=dev) if want_dy and branch else None
+    dgate = torch.empty(T, **f32) if want_dgate and branch else None
+    dw_post = torch.empty(H, **f32) if want_dw and branch else None
+    dw_pre = torch.empty(H, **f32) if want_dw and dn is not None else None
+    if T == 0:
+        for t in (dy, dw_post, dw_pre):
+            if t is not None:
+                t.zero_()
+        return dh, dy, dgate, dw_post, dw_pre
+    ws = None
+    if dw_post is not None or dw_pre is not None:
+        ws = torch.empty(B.locmoe_block_norm_grad_bytes(shape), dtype=torch.uint8, device=dev)
+    acts = dict(u8=ck.u8, r_post=ck.r_post, x8=ck.x8 if dn is not None else None, r_pre=ck.r_pre if dn is not None else None) \
+        if ck is not None else dict(y=y, h_out=h_out if dn is not None else None)
+    B.locmoe_block_norm_grad(shape, rows, dh_out, dn, slot=slot if branch else None, inv=inv if branch and slot is not None else None,
+                             gate_w=gate_w, w_post=w_post, w_pre=w_pre, res_scale=res_scale, eps=eps, dh=dh, dy=dy, dgate=dgate,
+                             dw_post=dw_post, dw_pre=dw_pre, ws=ws, stream=stream, **acts)
+    return dh, dy, dgate, dw_post, dw_pre
+
+
+class BlockNorm(torch.autograd.Function):
+    """``BlockNorm.apply(h, y, gate_w, w_post, w_pre, slot, inv, res_scale, eps, checkpoint) -> (h_out, n)``, differentiable in
+    its first five arguments.  With ``checkpoint`` the activations kept for the gradient are the 8-bit ones."""
+
+    @staticmethod
+    def forward(ctx, h, y, gate_w, w_post, w_pre, slot=None, inv=None, res_scale=1.0, eps=1e-6, checkpoint=False):
+        h_out, n, ck = block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint)
+        ctx.consts = (res_scale, eps, ck is not None)
+        ctx.save_for_backward(gate_w, w_post, w_pre, slot, inv, *(ck if ck is not None else (y, h_out, None, None)))
+        ctx.set_materialize_grads(False)
+        return h_out, n
+
+    @staticmethod
+    def backward(ctx, dh_out, dn):
+        gate_w, w_post, w_pre, slot, inv, *acts = ctx.saved_tensors
+        res_scale, eps, packed = ctx.consts
+        if dh_out is None and dn is None:
+            return (None,) * 10
+        need = ctx.needs_input_grad
+        dense = lambda t: None if t is None else t.contiguous()
+        kw = dict(checkpoint=Checkpoint(*acts)) if packed else dict(y=acts[0], h_out=acts[1])
+        dh, dy, dgate, dw_post, dw_pre = block_norm_grad(
+            dense(dh_out), dense(dn), slot=slot, inv=inv, gate_w=gate_w, w_post=w_post, w_pre=w_pre, res_scale=res_scale, eps=eps,
+            want_dh=need[0], want_dy=need[1], want_dgate=need[2], want_dw=need[3] or need[4], **kw)
+        if need[4] and w_pre is not None and dw_pre is None:   # n was not used: its weight has no gradient
+            dw_pre = torch.zeros_like(w_pre)
+        return (dh, dy if need[1] else None, dgate if need[2] else None, dw_post if need[3] else None, dw_pre if need[4] else None,
+                None, None, None, None, None)

@@ -2,6 +2,8 @@
 #include <math.h>
 #include <stdlib.h>
 
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace locmoe {
@@ -403,6 +405,72 @@ int locmoe_moe_layer(const locmoe_shape_t* shape, const void* x, const int32_t* 
     rc = locmoe_combine(shape, C_alloc, ysrc, ydt, b->slot, b->gate_w, out, 0, stream);
     if (rc < 0) return rc;
     return warn | rc;
+}
+
+namespace {
+bool element_aligned(const void* p, int n) { return (uintptr_t)p % n == 0; }
+
+// Rows of the block output's array: the slot buffer's, or the tokens' own (no slots).
+long long norm_rows(const locmoe_shape_t* s, int32_t C_alloc, const int32_t* slot) { return slot ? buffer_rows(s, C_alloc) : s->T; }
+
+constexpr int32_t kMaxCheckpointH = 200000;   // sqrt(H) < 448, the largest E4M3 value
+}  // namespace
+
+int locmoe_block_norm(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe_block_norm_t* b, void* stream) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if (!b || !b->h || (!b->h_out && !b->n_out)) return LOCMOE_ERR_NULL;
+    if (!b->y && (b->slot || b->u8 || b->r_post)) return LOCMOE_ERR_NULL;
+    if (!b->u8 != !b->r_post || !b->x8 != !b->r_pre) return LOCMOE_ERR_NULL;
+    if (!(b->eps >= 0.0f) || b->res_scale != b->res_scale) return LOCMOE_ERR_SHAPE;
+    if ((b->u8 || b->x8) && shape->H > kMaxCheckpointH) return LOCMOE_ERR_SHAPE;
+    const long long rows = norm_rows(shape, C_alloc, b->slot);
+    if (rows < 0) return LOCMOE_ERR_SHAPE;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    for (const void* p : {b->h, b->y, (const void*)b->h_out, (const void*)b->n_out})
+        if (!element_aligned(p, esz)) return LOCMOE_ERR_ALIGN;
+    for (const void* p : {(const void*)b->slot, (const void*)b->gate_w, (const void*)b->w_post, (const void*)b->w_pre,
+                          (const void*)b->r_post, (const void*)b->r_pre})
+        if (!element_aligned(p, 4)) return LOCMOE_ERR_ALIGN;
+    return launch_block_norm(*shape, rows, *b, static_cast<cudaStream_t>(stream));
+}
+
+int locmoe_block_norm_grad_bytes(const locmoe_shape_t* shape, size_t* bytes) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if (!bytes) return LOCMOE_ERR_NULL;
+    *bytes = block_norm_grad_ws_bytes(*shape);
+    return LOCMOE_OK;
+}
+
+int locmoe_block_norm_grad(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe_block_norm_grad_t* b, void* ws,
+                           size_t ws_bytes, void* stream) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if (!b || (!b->dh_out && !b->dn)) return LOCMOE_ERR_NULL;
+    const bool ck = b->u8 || b->x8;
+    if (ck && (b->y || b->h_out)) return LOCMOE_ERR_DTYPE;          // one form of the activations at a time
+    if (!b->u8 != !b->r_post || !b->x8 != !b->r_pre) return LOCMOE_ERR_NULL;
+    if (b->dn && !b->h_out && !b->x8) return LOCMOE_ERR_NULL;
+    if (b->dw_pre && !b->dn) return LOCMOE_ERR_NULL;
+    const bool branch = b->y || b->u8;
+    if (!branch && (b->dy || b->dgate || b->dw_post || b->slot)) return LOCMOE_ERR_NULL;
+    if (b->inv && !b->slot) return LOCMOE_ERR_NULL;
+    if (!b->dh && !b->dy && !b->dgate && !b->dw_post && !b->dw_pre) return LOCMOE_ERR_NULL;
+    if (!(b->eps >= 0.0f) || b->res_scale != b->res_scale) return LOCMOE_ERR_SHAPE;
+    if (ck && shape->H > kMaxCheckpointH) return LOCMOE_ERR_SHAPE;
+    const long long rows = norm_rows(shape, C_alloc, b->slot);
+    if (rows < 0) return LOCMOE_ERR_SHAPE;
+    if (b->dw_post || b->dw_pre)
+        if (!ws || ws_bytes < block_norm_grad_ws_bytes(*shape) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    for (const void* p : {b->dh_out, b->dn, b->h_out, b->y, (const void*)b->dh, (const void*)b->dy})
+        if (!element_aligned(p, esz)) return LOCMOE_ERR_ALIGN;
+    for (const void* p : {(const void*)b->slot, (const void*)b->inv, (const void*)b->gate_w, (const void*)b->w_post, (const void*)b->w_pre,
+                          (const void*)b->r_post, (const void*)b->r_pre, (const void*)b->dgate, (const void*)b->dw_post,
+                          (const void*)b->dw_pre})
+        if (!element_aligned(p, 4)) return LOCMOE_ERR_ALIGN;
+    return launch_block_norm_grad(*shape, rows, *b, ws, static_cast<cudaStream_t>(stream));
 }
 
 int locmoe_conventional_capacity(const locmoe_shape_t* shape, const locmoe_capacity_rule_t* rule, int32_t* C_alloc) {

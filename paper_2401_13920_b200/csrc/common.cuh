@@ -124,6 +124,10 @@ int launch_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, const void* 
 int read_ffn_flags(int* out, cudaStream_t st);
 void plan_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, int kernels[2]);
 
+size_t block_norm_grad_ws_bytes(const locmoe_shape_t& s);
+int launch_block_norm(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_t& b, cudaStream_t st);
+int launch_block_norm_grad(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_grad_t& b, void* ws, cudaStream_t st);
+
 // Copies the device diagnostics word to host memory (synchronises the stream).
 int read_device_flags(int* out, cudaStream_t st);
 
