@@ -504,6 +504,27 @@ int locmoe_moe_layer(const locmoe_shape_t *shape, const void *x, const int32_t *
                      const void *w_out, const locmoe_layer_buffers_t *bufs, void *out, void *stream);
 
 /*
+ * A whole MoE layer for a few tokens, as decoding meets it: gate, the K best experts, their feed-forward networks
+ * and the gate-weighted sum, in two launches, with no capacity, no dropped token and no dispatch buffer.
+ *   G_i = ReLU(mean_i x_t + eps_i) as in locmoe_gate (eps == NULL: 0),  p = softmax(G),
+ *   choice c of a token = the c-th largest G_i, a tie going to the lower index,
+ *   out[t] = sum over c < K of p_c * W_out[e_c] . GeLU(W_in[e_c] . x_t)        (GeLU as in locmoe_expert_ffn)
+ * x, out [T][H] bf16; w_in [E][F][H], w_out [E][H][F] bf16; idx_k int32[K][T], w_k float[K][T] (the choices and their
+ * scores) are outputs too.  The GeLU's result is held to 16 bits (two bf16 parts), all sums are fp32 and added in a
+ * fixed order, out is rounded once.  flags: LOCMOE_FEW_UNWEIGHTED (K = 1 only) leaves the factor p_0 out, for a caller that applies it
+ * after a norm (locmoe_block_norm).  A token with an infinity or a NaN gets a valid choice and unspecified outputs and
+ * disturbs no other token.
+ * T <= LOCMOE_FEW_MAX_TOKENS, E <= 1024 (LOCMOE_ERR_TOO_LARGE), K <= min(8, E), F < 2^20, H and F multiples of 8,
+ * x, w_in, w_out 16-byte aligned.  ws: locmoe_moe_few_bytes() bytes, 256-byte aligned; its contents are undefined
+ * between calls.  The shape's node fields and layout are validated but do not matter.
+ */
+enum { LOCMOE_FEW_MAX_TOKENS = 128, LOCMOE_FEW_UNWEIGHTED = 1 };
+int locmoe_moe_few_bytes(const locmoe_shape_t *shape, int32_t K, int32_t F, size_t *bytes);
+int locmoe_moe_few(const locmoe_shape_t *shape, const void *x, const float *eps, int32_t K, int32_t F, const void *w_in,
+                   const void *w_out, int32_t flags, int32_t *idx_k, float *w_k, void *out, void *ws, size_t ws_bytes,
+                   void *stream);
+
+/*
  * The norms around one block, fused with its gate and its residual (one pass over the rows).  The block's input is
  * the normalised stream n, its output y (rows of the dispatched buffer, or token order), its gate the score R of the
  * router.  Per token t, N(v) = v / sqrt(mean_j v_j^2 + eps):

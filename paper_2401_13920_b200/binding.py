@@ -19,13 +19,14 @@ F32, BF16 = 0, 1
 LAYOUT_SEND, LAYOUT_RECV = 0, 1
 BOUND_BETA, BOUND_ERFC, BOUND_EXP = 0, 1, 2
 ROUTE_EARLY_INIT = 1
+FEW_MAX_TOKENS, FEW_UNWEIGHTED = 128, 1
 WARN_CLAMPED, WARN_BAD_SRC, WARN_BAD_IDX = 1, 2, 4
 FLAG_DELTA_OVERRIDE, FLAG_MIN_SATURATED, FLAG_MIN_BINDS = 1, 2, 4
 
 EXPORTS = [
     "locmoe_workspace_bytes", "locmoe_gate", "locmoe_gate_ex", "locmoe_aux_loss_partial", "locmoe_capacity", "locmoe_capacity_noalloc", "locmoe_capacity_read", "locmoe_route", "locmoe_capacity_route", "locmoe_gate_route",
     "locmoe_conventional_capacity", "locmoe_batch_delta", "locmoe_dest_order",
-    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_block_norm", "locmoe_block_norm_grad_bytes", "locmoe_block_norm_grad", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
+    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_moe_few_bytes", "locmoe_moe_few", "locmoe_block_norm", "locmoe_block_norm_grad_bytes", "locmoe_block_norm_grad", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
 ]
 
 
@@ -118,6 +119,8 @@ def _load() -> C.CDLL:
     lib.locmoe_topk_select.argtypes = [C.POINTER(Shape), vp, vp, vp, i32, vp, vp, vp]
     lib.locmoe_topk_fold.argtypes = [C.POINTER(Shape), i32, vp, vp]
     lib.locmoe_combine_topk.argtypes = [C.POINTER(Shape), i32, vp, i32, i32, vp, vp, vp, vp]
+    lib.locmoe_moe_few_bytes.argtypes = [C.POINTER(Shape), i32, i32, C.POINTER(C.c_size_t)]
+    lib.locmoe_moe_few.argtypes = [C.POINTER(Shape), vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, vp]
     lib.locmoe_block_norm.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNorm), vp]
     lib.locmoe_block_norm_grad_bytes.argtypes = [C.POINTER(Shape), C.POINTER(C.c_size_t)]
     lib.locmoe_block_norm_grad.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNormGrad), vp, C.c_size_t, vp]
@@ -488,6 +491,25 @@ def locmoe_moe_layer(shape: Shape, x, src_dev, eps, rule: CapacityRule, C_alloc,
     return _check("locmoe_moe_layer", _lib.locmoe_moe_layer(
         C.byref(shape), _ptr(x), _ptr(src_dev), _ptr(eps), C.byref(rule), int(C_alloc), int(F), _ptr(w_in), _ptr(w_out),
         C.byref(bufs), _ptr(out), _stream(stream)))
+
+
+def locmoe_moe_few_bytes(shape: Shape, K, F) -> int:
+    out = C.c_size_t(0)
+    _check("locmoe_moe_few_bytes", _lib.locmoe_moe_few_bytes(C.byref(shape), int(K), int(F), C.byref(out)))
+    return out.value
+
+
+def locmoe_moe_few(shape: Shape, x, K, F, w_in, w_out, idx_k, w_k, out, ws, eps=None, unweighted=False, stream=None) -> int:
+    """The whole layer for at most FEW_MAX_TOKENS tokens."""
+    bf = torch.bfloat16
+    for t, dt, n, name in ((x, bf, shape.T * shape.H, "x"), (w_in, bf, shape.E * F * shape.H, "w_in"), (w_out, bf, shape.E * F * shape.H, "w_out"),
+                           (idx_k, torch.int32, K * shape.T, "idx_k"), (w_k, torch.float32, K * shape.T, "w_k"), (out, bf, shape.T * shape.H, "out")):
+        _want(t, dt, n, name)
+    if eps is not None:
+        _want(eps, torch.float32, shape.E, "eps")
+    return _check("locmoe_moe_few", _lib.locmoe_moe_few(
+        C.byref(shape), _ptr(x), _ptr(eps), int(K), int(F), _ptr(w_in), _ptr(w_out), FEW_UNWEIGHTED if unweighted else 0, _ptr(idx_k),
+        _ptr(w_k), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def _fill(struct, dtypes, numels, tensors, scalars):

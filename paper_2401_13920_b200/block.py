@@ -31,6 +31,25 @@ def _row_shape(like: torch.Tensor, y, slot) -> tuple:
     return B.Shape(T, H, 1, 1, 1, B.dtype_code(like.dtype), B.LAYOUT_SEND), rows
 
 
+def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
+    """The whole MoE layer for a few tokens: x [T][H], w_in [E][F][H], w_out [E][H][F], all bf16, T <= 128.
+
+    Returns ``(out, idx, w)``: out [T][H], the K chosen experts and their scores, [K][T] each."""
+    if x.dim() != 2 or w_in.dim() != 3 or w_out.dim() != 3:
+        raise ValueError("expected x [T][H], w_in [E][F][H], w_out [E][H][F]")
+    (T, H), (E, F, _) = x.shape, w_in.shape
+    if w_in.shape[2] != H or w_out.shape != (E, H, F):
+        raise ValueError("x %s, w_in %s and w_out %s do not belong together" % (tuple(x.shape), tuple(w_in.shape), tuple(w_out.shape)))
+    out = torch.empty_like(x)
+    idx, w = torch.empty(K, T, dtype=torch.int32, device=x.device), torch.empty(K, T, dtype=torch.float32, device=x.device)
+    if T == 0:
+        return out, idx, w
+    shape = B.Shape(T, H, E, 1, 1, B.dtype_code(x.dtype), B.LAYOUT_SEND)
+    ws = torch.empty(B.locmoe_moe_few_bytes(shape, K, F), dtype=torch.uint8, device=x.device)
+    B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted, stream)
+    return out, idx, w
+
+
 def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, checkpoint=False,
                want_h=True, want_n=True, stream=None):
     """h' = res_scale * h + gate_w * w_post * N(y[slot]),  n = w_pre * N(h').

@@ -416,6 +416,40 @@ long long norm_rows(const locmoe_shape_t* s, int32_t C_alloc, const int32_t* slo
 constexpr int32_t kMaxCheckpointH = 200000;   // sqrt(H) < 448, the largest E4M3 value
 }  // namespace
 
+namespace {
+int check_few(const locmoe_shape_t* s, int32_t K, int32_t F) {
+    int rc = check_shape(s);
+    if (rc) return rc;
+    if (s->x_dtype != LOCMOE_BF16) return LOCMOE_ERR_DTYPE;
+    if (K < 1 || K > 8 || K > s->E || F < 8 || F % 8 != 0 || s->H % 8 != 0) return LOCMOE_ERR_SHAPE;
+    if (s->T > LOCMOE_FEW_MAX_TOKENS || s->E > 1024 || F >= (1 << 20) || s->H >= (1 << 20)) return LOCMOE_ERR_TOO_LARGE;
+    return LOCMOE_OK;
+}
+}  // namespace
+
+int locmoe_moe_few_bytes(const locmoe_shape_t* shape, int32_t K, int32_t F, size_t* bytes) {
+    int rc = check_few(shape, K, F);
+    if (rc) return rc;
+    if (!bytes) return LOCMOE_ERR_NULL;
+    *bytes = few_ws_bytes(*shape, F, K);
+    return LOCMOE_OK;
+}
+
+int locmoe_moe_few(const locmoe_shape_t* shape, const void* x, const float* eps, int32_t K, int32_t F, const void* w_in,
+                   const void* w_out, int32_t flags, int32_t* idx_k, float* w_k, void* out, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_few(shape, K, F);
+    if (rc) return rc;
+    if (!x || !w_in || !w_out || !idx_k || !w_k || !out) return LOCMOE_ERR_NULL;
+    if (flags & ~LOCMOE_FEW_UNWEIGHTED) return LOCMOE_ERR_DTYPE;
+    if ((flags & LOCMOE_FEW_UNWEIGHTED) && K != 1) return LOCMOE_ERR_SHAPE;
+    if ((uintptr_t)x % 16 || (uintptr_t)w_in % 16 || (uintptr_t)w_out % 16 || (uintptr_t)out % 2 || (uintptr_t)eps % 4 ||
+        (uintptr_t)idx_k % 4 || (uintptr_t)w_k % 4)
+        return LOCMOE_ERR_ALIGN;
+    if (!ws || ws_bytes < few_ws_bytes(*shape, F, K) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;
+    return launch_moe_few(*shape, x, eps, K, F, w_in, w_out, (flags & LOCMOE_FEW_UNWEIGHTED) ? 0 : 1, idx_k, w_k, out, ws,
+                          static_cast<cudaStream_t>(stream));
+}
+
 int locmoe_block_norm(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe_block_norm_t* b, void* stream) {
     int rc = check_shape(shape);
     if (rc) return rc;
@@ -546,7 +580,7 @@ const char* locmoe_status_string(int code) {
         case LOCMOE_ERR_ALIGN: return "pointer alignment";
         case LOCMOE_ERR_WORKSPACE: return "workspace missing, too small or misaligned";
         case LOCMOE_ERR_CUDA: return "a CUDA call failed";
-        case LOCMOE_ERR_TOO_LARGE: return "size exceeds the built-in scratch of the no-allocation entry point";
+        case LOCMOE_ERR_TOO_LARGE: return "size beyond what this entry point is built for";
         default: return code > 0 ? "warning bits set" : "unknown error";
     }
 }

@@ -124,6 +124,10 @@ int launch_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, const void* 
 int read_ffn_flags(int* out, cudaStream_t st);
 void plan_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, int kernels[2]);
 
+size_t few_ws_bytes(const locmoe_shape_t& s, int F, int K);
+int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int K, int F, const void* w_in, const void* w_out,
+                   int weighted, int32_t* idx_k, float* w_k, void* out, void* ws, cudaStream_t st);
+
 size_t block_norm_grad_ws_bytes(const locmoe_shape_t& s);
 int launch_block_norm(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_t& b, cudaStream_t st);
 int launch_block_norm_grad(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_grad_t& b, void* ws, cudaStream_t st);

@@ -1,0 +1,461 @@
+// A whole MoE layer for a few tokens (decoding), in two kernels: gate and first expert product, then second product
+// and the gate-weighted sum.
+//
+//   G_i = ReLU(mean_i x + eps_i),  p = softmax(G),  the K largest;   out_t = sum_c p_{t,c} W_out[e] GeLU(W_in[e] x_t)
+//
+// Bound by the weights of the experts that the tokens meet (4 F H bytes each), every one of which is read once.  So
+// the weights are what moves fast: every thread streams its own 16-byte pieces through a private ring of cp.async
+// slots, without barriers, across the borders of its tasks.  A task is a block of 8 * NB weight rows of one expert
+// (and, in the second product, one of S slices of the reduction); the CTA's warps take its steps of 32 k in turn.
+// The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
+// expert nothing is gained by larger matrix instructions.  The order of k inside a step is chosen so that a
+// thread's fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides).
+// The router is evaluated by every CTA for itself: a few tokens' rows out of L2 cost less than a launch of their own.
+#include "common.cuh"
+
+namespace locmoe {
+
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
+constexpr int kStepK = 32;
+constexpr uint32_t kNoRow = 0xffffffffu;
+
+struct FewArgs {
+    const uint16_t* x; const float* eps; const uint16_t* w_in; const uint16_t* w_out;
+    int32_t* idx_k; float* w_k; uint16_t* out;
+    uint16_t* g;        // [2][K * T][F] GeLU(W_in x) as the sum of two bf16 values: the rounded value and what rounding left
+    float* part;        // [S][K * T][H] slices of the second product
+    int32_t* arrived;   // [row blocks] tasks that have left their slice
+    int T, H, E, K, F, max_split, weighted;
+};
+
+struct Smem {   // offsets of the dynamic shared memory
+    int expert, sorted, score, act, first, chunk, ring, red, total;
+};
+__host__ __device__ constexpr int round16(int n) { return (n + 15) / 16 * 16; }
+template <int MT, int NB, int D>
+__host__ __device__ inline Smem layout(int TK, int E) {
+    Smem s{};
+    const int most = TK < E ? TK : E;
+    s.expert = 0;                                  // int16 [TK]  expert of assignment a = c * T + t
+    s.sorted = round16(2 * TK);                    // int16 [TK]  assignments by expert
+    s.score = s.sorted + round16(2 * TK);          // float [TK]
+    s.act = s.score + round16(4 * TK);             // int16 [most]      experts met
+    s.first = s.act + round16(2 * most);           // int16 [most + 1]  their first entry of `sorted`
+    s.chunk = s.first + round16(2 * most + 2);     // int16 [most + 1]  their first chunk of 16 * MT tokens
+    s.ring = s.chunk + round16(2 * most + 2);
+    // the router's scratch lies where ring and red are later: a strip of E floats per warp, the counters beside it
+    const int ring = D * NB * kThreads * 16, red = kWarps * 16 * MT * 8 * NB * 4;
+    s.red = s.ring + ring;
+    const int scratch = (kWarps + 2) * E * 4;
+    s.total = s.ring + (ring + red > scratch ? ring + red : scratch);
+    return s;
+}
+
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {   // zero-fills where !ok
+    const int n = ok ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Sum of `n` consecutive bf16 values from `p`, of which this lane takes every `of`-th piece from `sub` on.
+template <int EL>
+__device__ __forceinline__ float sum_pieces(const uint16_t* p, int n, int sub, int of) {
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll 4
+    for (int i = sub; i < n / EL; i += of) {
+        if constexpr (EL == 8) {
+            const uint4 w = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            s0 += (bf16_lo(w.x) + bf16_hi(w.x)) + (bf16_lo(w.y) + bf16_hi(w.y));
+            s1 += (bf16_lo(w.z) + bf16_hi(w.z)) + (bf16_lo(w.w) + bf16_hi(w.w));
+        } else if constexpr (EL == 2) {
+            const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+            s0 += bf16_lo(w); s1 += bf16_hi(w);
+        } else {
+            s0 += bf16_lo(__ldg(p + i));
+        }
+    }
+    return s0 + s1;
+}
+
+// Router for all tokens, one warp per token: fills expert[] and score[].
+__device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, float* score, float* strip_all) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = a.H / a.E;
+    float* G = strip_all + warp * a.E;
+    int lanes = 1;                                   // lanes that share one expert's group
+    while (lanes * 2 * a.E <= 32) lanes *= 2;
+    const int sub = lane % lanes;
+    const float inv_g = 1.0f / (float)g;
+    for (int t = warp; t < a.T; t += kWarps) {
+        const uint16_t* row = a.x + (size_t)t * a.H;
+        for (int i0 = 0; i0 < a.E; i0 += 32 / lanes) {
+            const int i = i0 + lane / lanes;
+            float s = 0.0f;
+            if (i < a.E) {
+                const uint16_t* p = row + (size_t)i * g;
+                s = g % 8 == 0 ? sum_pieces<8>(p, g, sub, lanes) : g % 2 == 0 ? sum_pieces<2>(p, g, sub, lanes) : sum_pieces<1>(p, g, sub, lanes);
+            }
+            for (int o = 1; o < lanes; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (i < a.E && sub == 0) G[i] = fmaxf(fmaf(s, inv_g, a.eps ? a.eps[i] : 0.0f), 0.0f);   // a NaN logit counts as 0
+        }
+        __syncwarp();
+        float top = 0.0f, z = 0.0f;
+        for (int c = 0; c < a.K; ++c) {
+            float best = -2.0f;
+            int bi = 0x7fffffff;
+            for (int i = lane; i < a.E; i += 32)
+                if (G[i] > best) { best = G[i]; bi = i; }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {       // the lower index wins a tie
+                const float ob = __shfl_xor_sync(0xffffffffu, best, o);
+                const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
+                if (ob > best || (ob == best && oi < bi)) { best = ob; bi = oi; }
+            }
+            if (c == 0) {
+                top = best;
+                for (int i = lane; i < a.E; i += 32) z += expf(G[i] - top);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            }
+            __syncwarp();
+            if (lane == 0) {
+                G[bi] = -1.0f;                       // below every logit: chosen
+                expert[c * a.T + t] = (int16_t)bi;
+                score[c * a.T + t] = expf(best - top) / z;
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// Position in the CTA's sequence of tasks: which weight rows and which steps this warp reads.
+struct Cursor {
+    int task, end, j;          // this CTA's tasks are [task, end); j: index of the expert in act[]
+    int e, row0, step, last, ch, s, rb;
+};
+
+template <int MT, int NB, int D, bool SECOND>
+__global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(const FewArgs a) {
+    extern __shared__ __align__(128) unsigned char sm[];
+    const int TK = a.T * a.K;
+    const Smem L = layout<MT, NB, D>(TK, a.E);
+    int16_t* expert = reinterpret_cast<int16_t*>(sm + L.expert);
+    int16_t* sorted = reinterpret_cast<int16_t*>(sm + L.sorted);
+    float* score = reinterpret_cast<float*>(sm + L.score);
+    int16_t* act = reinterpret_cast<int16_t*>(sm + L.act);
+    int16_t* first = reinterpret_cast<int16_t*>(sm + L.first);
+    int16_t* chunk = reinterpret_cast<int16_t*>(sm + L.chunk);
+    float* strips = reinterpret_cast<float*>(sm + L.ring);
+    int* count = reinterpret_cast<int*>(strips + kWarps * a.E);
+    int* place = count + a.E;
+    float* red = reinterpret_cast<float*>(sm + L.red);
+    __shared__ int n_act, flag;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
+    const int N = SECOND ? a.H : a.F, Kd = SECOND ? a.F : a.H;
+    const uint16_t* W = SECOND ? a.w_out : a.w_in;
+    const int RB = (N + 8 * NB - 1) / (8 * NB);
+
+    // With few assignments the second kernel evaluates the router again, so that it can fill its ring with weights
+    // while the first one is still running; with many it takes the first kernel's choices.
+    const bool early = SECOND && TK <= 8;
+    if (!SECOND) {
+        pdl_wait();
+        pdl_trigger();
+    }
+    if (!SECOND || early) {
+        few_router(a, expert, score, strips);
+    } else {
+        pdl_wait();
+        pdl_trigger();
+        for (int i = tid; i < TK; i += kThreads) { expert[i] = (int16_t)a.idx_k[i]; score[i] = a.w_k[i]; }
+    }
+    for (int i = tid; i < a.E; i += kThreads) count[i] = 0;
+    __syncthreads();
+    if (!SECOND && blockIdx.x == 0)
+        for (int i = tid; i < TK; i += kThreads) { a.idx_k[i] = expert[i]; a.w_k[i] = score[i]; }
+    if (!SECOND) {
+        const int blocks = (a.H + 7) / 8;
+        for (int i = blockIdx.x * kThreads + tid; i < blocks; i += gridDim.x * kThreads) a.arrived[i] = 0;
+    }
+    for (int i = tid; i < TK; i += kThreads) atomicAdd(&count[expert[i]], 1);
+    __syncthreads();
+    if (warp == 0) {
+        int na = 0, nf = 0, nc = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 32) {
+            const int e = e0 + lane, c = e < a.E ? count[e] : 0, ch = (c + 16 * MT - 1) / (16 * MT);
+            int sf = c, sc = ch;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int uf = __shfl_up_sync(0xffffffffu, sf, o), uc = __shfl_up_sync(0xffffffffu, sc, o);
+                if (lane >= o) { sf += uf; sc += uc; }
+            }
+            const unsigned met = __ballot_sync(0xffffffffu, c > 0);
+            if (e < a.E) place[e] = nf + sf - c;
+            if (c > 0) {
+                const int j = na + __popc(met & ((1u << lane) - 1u));
+                act[j] = (int16_t)e; first[j] = (int16_t)(nf + sf - c); chunk[j] = (int16_t)(nc + sc - ch);
+            }
+            na += __popc(met);
+            nf += __shfl_sync(0xffffffffu, sf, 31);
+            nc += __shfl_sync(0xffffffffu, sc, 31);
+        }
+        if (lane == 0) { n_act = na; first[na] = (int16_t)nf; chunk[na] = (int16_t)nc; }
+        __syncwarp();
+        // assignments sorted by expert, in ascending order within one: an expert's chunks may fall to different CTAs,
+        // which must agree on what is in them
+        for (int i0 = 0; i0 < TK; i0 += 32) {
+            const int i = i0 + lane;
+            const bool in = i < TK;
+            const unsigned have = __ballot_sync(0xffffffffu, in);
+            if (in) {
+                const int e = expert[i];
+                const unsigned same = __match_any_sync(have, e);
+                const int at = place[e] + __popc(same & ((1u << lane) - 1u));
+                sorted[at] = (int16_t)i;
+                __syncwarp(have);
+                if ((same >> lane) == 1u) place[e] = at + 1;   // the last of them
+            }
+            __syncwarp();
+        }
+    }
+    __syncthreads();   // the scratch is free: ring and red take its place
+
+    const int steps = (Kd + kStepK - 1) / kStepK, chunks = chunk[n_act];
+    int S = 1;         // slices of the reduction: enough tasks for an even load, at least two steps a warp
+    if (SECOND)
+        while (S < a.max_split && (long long)chunks * RB * S < 8ll * gridDim.x && steps >= 4 * kWarps * S) S *= 2;
+    const long long total = (long long)chunks * RB * S;
+    const int t0 = (int)(total * blockIdx.x / gridDim.x), t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
+
+    auto locate = [&](Cursor& c) {
+        while (c.task >= chunk[c.j + 1] * RB * S) ++c.j;
+        int r = c.task - chunk[c.j] * RB * S;
+        const int nch = chunk[c.j + 1] - chunk[c.j];
+        c.ch = r % nch; r /= nch;
+        c.rb = r % RB; c.s = r / RB;
+        c.e = act[c.j];
+        c.row0 = c.rb * 8 * NB;
+        c.step = (int)((long long)steps * c.s / S) + warp;
+        c.last = (int)((long long)steps * (c.s + 1) / S);
+    };
+    const uint32_t ring0 = smem_u32(sm + L.ring) + tid * 16;
+    Cursor in{};
+    in.task = t0; in.end = t1;
+    if (t0 < t1) {
+        locate(in);
+        while (in.step >= in.last && ++in.task < in.end) locate(in);
+    }
+    int in_slot = 0;
+    auto issue = [&]() {
+        if (in.task < in.end) {
+            const int k = in.step * kStepK + tq * 8;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int row = in.row0 + nb * 8 + gq;
+                const bool ok = row < N && k < Kd;
+                cp_async16(ring0 + (in_slot * NB + nb) * (kThreads * 16), ok ? W + ((size_t)in.e * N + row) * Kd + k : W, ok);
+            }
+            in.step += kWarps;
+            while (in.step >= in.last && ++in.task < in.end) locate(in);
+        }
+        cp_commit();
+        if (++in_slot == D) in_slot = 0;
+    };
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) issue();
+
+    if (early) {
+        pdl_wait();
+        pdl_trigger();
+    }
+    const uint16_t* A = SECOND ? a.g : a.x;
+    int slot = 0;
+    Cursor c{};
+    c.end = t1;
+    for (int task = t0; task < t1; ++task) {
+        c.task = task;
+        locate(c);
+        const int base = first[c.j] + c.ch * 16 * MT, m_here = min(16 * MT, first[c.j + 1] - base);
+        // The second product takes the intermediate as high + low part.  While its tokens fill no more than half of
+        // the tile's rows, the low parts are the other half; beyond that they take products of their own.
+        constexpr int half = 8 * MT;
+        const bool packed = SECOND && m_here <= half;
+        const int rows_used = packed ? half + m_here : m_here;
+        const uint32_t low = (uint32_t)TK * (uint32_t)Kd;
+        uint32_t off[2 * MT];   // element offset of the row in A; kNoRow: a row of zeros
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+            const int m = i * 8 + gq;
+            const bool lower = packed && i >= MT;
+            const int mm = lower ? m - half : m;
+            const int as = mm < m_here ? sorted[base + mm] : -1;
+            off[i] = as < 0 ? kNoRow : (uint32_t)(SECOND ? as : as % a.T) * (uint32_t)Kd + (lower ? low : 0u);
+        }
+        float acc[MT][NB][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+#pragma unroll 1
+        for (; c.step < c.last; c.step += kWarps) {
+            const int k = c.step * kStepK + tq * 8;
+            uint4 av[2 * MT];
+#pragma unroll
+            for (int i = 0; i < 2 * MT; ++i) {
+                av[i] = make_uint4(0, 0, 0, 0);
+                if (off[i] != kNoRow && k < Kd) av[i] = *reinterpret_cast<const uint4*>(A + off[i] + k);
+            }
+            cp_wait<D - 1>();
+            uint4 wv[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                wv[n] = *reinterpret_cast<const uint4*>(sm + L.ring + (size_t)((slot * NB + n) * kThreads + tid) * 16);
+            auto products = [&]() {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    if (m > 0 && m * 16 >= rows_used) break;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        mma16816(acc[m][n], av[2 * m].x, av[2 * m + 1].x, av[2 * m].y, av[2 * m + 1].y, wv[n].x, wv[n].y);
+                        mma16816(acc[m][n], av[2 * m].z, av[2 * m + 1].z, av[2 * m].w, av[2 * m + 1].w, wv[n].z, wv[n].w);
+                    }
+                }
+            };
+            products();
+            if (SECOND && !packed) {
+#pragma unroll
+                for (int i = 0; i < 2 * MT; ++i)
+                    if (off[i] != kNoRow && k < Kd) av[i] = *reinterpret_cast<const uint4*>(A + off[i] + low + k);
+                products();
+            }
+            issue();
+            if (++slot == D) slot = 0;
+        }
+        // the warps' shares of the sum, added in warp order
+        constexpr int C = 8 * NB;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float* r = red + ((warp * 16 * MT) + m * 16 + gq) * C + n * 8 + tq * 2;
+                *reinterpret_cast<float2*>(r) = make_float2(acc[m][n][0], acc[m][n][1]);
+                *reinterpret_cast<float2*>(r + 8 * C) = make_float2(acc[m][n][2], acc[m][n][3]);
+            }
+        __syncthreads();
+        const bool direct = SECOND && S == 1 && a.K == 1;
+        for (int o = tid; o < m_here * C; o += kThreads) {
+            const int m = o / C, r = o % C, row = c.row0 + r;
+            if (row >= N) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) v += red[(w * 16 * MT + m) * C + r];
+            if (packed) {
+                float lo = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) lo += red[(w * 16 * MT + half + m) * C + r];
+                v += lo;
+            }
+            const int as = sorted[base + m];
+            if (!SECOND) {
+                v = 0.5f * v * erfcf(-0.70710678118654752f * v);
+                const uint32_t hi = f32_to_bf16_bits(v);
+                a.g[(size_t)as * a.F + row] = (uint16_t)hi;
+                a.g[((size_t)TK + as) * a.F + row] = (uint16_t)f32_to_bf16_bits(v - bf16_lo(hi));
+            } else if (direct) {
+                a.out[(size_t)as * a.H + row] = (uint16_t)f32_to_bf16_bits(a.weighted ? v * score[as] : v);
+            } else {
+                a.part[((size_t)c.s * TK + as) * a.H + row] = v;
+            }
+        }
+        if (SECOND && !direct) __threadfence();
+        __syncthreads();
+        if (SECOND && !direct) {   // the last slice of these columns to arrive adds them all up, in a fixed order
+            if (tid == 0) {
+                __threadfence();
+                flag = atomicAdd(&a.arrived[c.rb], 1) == chunks * S - 1;
+            }
+            __syncthreads();
+            if (flag) {
+                __threadfence();
+                for (int o = tid; o < a.T * C; o += kThreads) {
+                    const int t = o / C, row = c.row0 + o % C;
+                    if (row >= N) continue;
+                    float v = 0.0f;
+                    for (int k = 0; k < a.K; ++k) {
+                        float y = 0.0f;
+                        for (int s = 0; s < S; ++s) y += __ldcg(&a.part[((size_t)s * TK + k * a.T + t) * a.H + row]);
+                        v = fmaf(a.weighted ? score[k * a.T + t] : 1.0f, y, v);
+                    }
+                    a.out[(size_t)t * a.H + row] = (uint16_t)f32_to_bf16_bits(v);
+                }
+            }
+        }
+    }
+    cp_wait<0>();
+}
+
+struct FewPlan { size_t off_g, off_part, off_arrived, total; int max_split; };
+FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
+    FewPlan p{};
+    const size_t TK = (size_t)s.T * K;
+    // slices only pay while there are few tasks, that is few assignments: at most 512 rows of partial sums for them
+    p.max_split = 1;
+    while (p.max_split < kMaxSplit && TK * p.max_split * 2 <= 512) p.max_split *= 2;
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    p.off_g = 0;
+    p.off_part = up(2 * TK * F * 2);
+    p.off_arrived = p.off_part + up(p.max_split * TK * s.H * 4);
+    p.total = p.off_arrived + up((size_t)(s.H + 7) / 8 * 4);
+    return p;
+}
+
+template <int MT, int NB, int D>
+int run_few(const FewArgs& a, cudaStream_t st) {
+    const Smem L = layout<MT, NB, D>(a.T * a.K, a.E);
+    static bool done_dev[64] = {false};   // the attribute is per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!done_dev[dev & 63]) {
+        const int most = layout<MT, NB, D>(kMaxTokens * kMaxK, kMaxExperts).total;
+        if (cudaFuncSetAttribute(moe_few_kernel<MT, NB, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+            cudaFuncSetAttribute(moe_few_kernel<MT, NB, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
+            cudaGetLastError();
+            return LOCMOE_ERR_CUDA;
+        }
+        done_dev[dev & 63] = true;
+    }
+    const dim3 grid(2 * sm_count());
+    const int rc = launch_pdl(moe_few_kernel<MT, NB, D, false>, grid, dim3(kThreads), L.total, st, a);
+    if (rc) return rc;
+    return launch_pdl(moe_few_kernel<MT, NB, D, true>, grid, dim3(kThreads), L.total, st, a);
+}
+
+}  // namespace
+
+size_t few_ws_bytes(const locmoe_shape_t& s, int F, int K) { return plan_few(s, F, K).total; }
+
+int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int K, int F, const void* w_in, const void* w_out,
+                   int weighted, int32_t* idx_k, float* w_k, void* out, void* ws, cudaStream_t st) {
+    const FewPlan p = plan_few(s, F, K);
+    unsigned char* base = static_cast<unsigned char*>(ws);
+    const FewArgs a{static_cast<const uint16_t*>(x), eps, static_cast<const uint16_t*>(w_in), static_cast<const uint16_t*>(w_out), idx_k,
+                    w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
+                    reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
+                    p.max_split, weighted};
+    if (s.T * K <= 8) return run_few<1, 1, 12>(a, st);
+    if (s.T <= 16) return run_few<1, 4, 4>(a, st);
+    return run_few<2, 4, 3>(a, st);
+}
+
+}  // namespace locmoe
