@@ -24,6 +24,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "tensor_map.cuh"
 
 namespace locmoe {
 
@@ -73,11 +74,6 @@ __device__ __forceinline__ void quiesce_after_abort(volatile int* abort_word) {
     }
 }
 
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
-                 : "memory");
-}
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
@@ -728,6 +724,8 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
+}  // namespace
+
 // K-major bf16 matrix [outer...][rows][K] with a box of box_rows x 64 elements, 128-byte swizzle.
 bool make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, uint32_t box_rows) {
     EncodeTiledFn fn = encode_fn();
@@ -740,6 +738,8 @@ bool make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 int launch_gemm(const void* A, const void* W, void* out, int out_f32, int gelu, int E, int M, int N, int K,
                 cudaStream_t st) {

@@ -4,14 +4,16 @@
 //   G_i = ReLU(mean_i x + eps_i),  p = softmax(G),  the K largest;   out_t = sum_c p_{t,c} W_out[e] GeLU(W_in[e] x_t)
 //
 // Bound by the weights of the experts that the tokens meet (4 F H bytes each), every one of which is read once.  So
-// the weights are what moves fast: every thread streams its own 16-byte pieces through a private ring of cp.async
-// slots, without barriers, across the borders of its tasks.  A task is a block of 8 * NB weight rows of one expert
-// (and, in the second product, one of S slices of the reduction); the CTA's warps take its steps of 32 k in turn.
-// The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
-// expert nothing is gained by larger matrix instructions.  The order of k inside a step is chosen so that a
-// thread's fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides).
+// the weights are what moves fast: every warp streams its own tiles of 8 * NB weight rows through a private ring of
+// TMA stages, without barriers between warps, across the borders of its tasks.  A task is a block of 8 * NB weight
+// rows of one expert (and, in the second product, one of S slices of the reduction); the stages of the CTA's tasks
+// are dealt to its warps in turn.  The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as
+// the 8 columns: at a few tokens an expert nothing is gained by larger matrix instructions.  The order of k inside a
+// stage is chosen so that a thread's fragments of both operands are 16 contiguous bytes of a row (the same
+// permutation on both sides), which the tiles' 128-byte swizzle gives without bank conflicts.
 // The router is evaluated by every CTA for itself: a few tokens' rows out of L2 cost less than a launch of their own.
 #include "common.cuh"
+#include "tensor_map.cuh"
 
 namespace locmoe {
 
@@ -19,7 +21,9 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
-constexpr int kStepK = 32;
+constexpr int kBoxK = 64;          // k of one TMA box: 128 bytes of a row
+
+__device__ int g_few_flags = 0;    // bit 0: a bounded wait gave up
 constexpr uint32_t kNoRow = 0xffffffffu;
 
 struct FewArgs {
@@ -31,35 +35,38 @@ struct FewArgs {
     int T, H, E, K, F, max_split, weighted;
 };
 
-struct Smem {   // offsets of the dynamic shared memory
-    int expert, sorted, score, act, first, chunk, ring, red, total;
+// A variant: MT tiles of 16 tokens, NB blocks of 8 weight rows, NBOX boxes of 64 k a stage, D stages a warp.
+template <int MT_, int NB_, int NBOX_, int D_>
+struct Variant {
+    static constexpr int MT = MT_, NB = NB_, NBOX = NBOX_, D = D_;
+    static constexpr int kBox = 8 * NB * 128, kStage = NBOX * kBox, kRing = kWarps * D * kStage;
+    static constexpr int kRed = kWarps * 16 * MT * 8 * NB;   // floats of one of the two strips
+    static constexpr int kStepK = NBOX * kBoxK;
+};
+
+struct Smem {   // offsets of the dynamic shared memory, from its first 1024-byte boundary on
+    int ring, red, bars, expert, sorted, score, act, first, chunk, total;
 };
 __host__ __device__ constexpr int round16(int n) { return (n + 15) / 16 * 16; }
-template <int MT, int NB, int D>
+template <class V>
 __host__ __device__ inline Smem layout(int TK, int E) {
     Smem s{};
     const int most = TK < E ? TK : E;
-    s.expert = 0;                                  // int16 [TK]  expert of assignment a = c * T + t
-    s.sorted = round16(2 * TK);                    // int16 [TK]  assignments by expert
-    s.score = s.sorted + round16(2 * TK);          // float [TK]
-    s.act = s.score + round16(4 * TK);             // int16 [most]      experts met
-    s.first = s.act + round16(2 * most);           // int16 [most + 1]  their first entry of `sorted`
-    s.chunk = s.first + round16(2 * most + 2);     // int16 [most + 1]  their first chunk of 16 * MT tokens
-    s.ring = s.chunk + round16(2 * most + 2);
     // the router's scratch lies where ring and red are later: a strip of E floats per warp, the counters beside it
-    const int ring = D * NB * kThreads * 16, red = kWarps * 16 * MT * 8 * NB * 4;
-    s.red = s.ring + ring;
-    const int scratch = (kWarps + 2) * E * 4;
-    s.total = s.ring + (ring + red > scratch ? ring + red : scratch);
+    const int scratch = (kWarps + 2) * E * 4, body = V::kRing + 2 * V::kRed * 4;
+    s.ring = 0;
+    s.red = V::kRing;
+    s.bars = scratch > body ? round16(scratch) : body;
+    s.expert = s.bars + round16(8 * kWarps * V::D);   // int16 [TK]  expert of assignment a = c * T + t
+    s.sorted = s.expert + round16(2 * TK);            // int16 [TK]  assignments by expert
+    s.score = s.sorted + round16(2 * TK);             // float [TK]
+    s.act = s.score + round16(4 * TK);                // int16 [most]      experts met
+    s.first = s.act + round16(2 * most);              // int16 [most + 1]  their first entry of `sorted`
+    s.chunk = s.first + round16(2 * most + 2);        // int16 [most + 1]  their first chunk of 16 * MT tokens
+    s.total = s.chunk + round16(2 * most + 2) + 1024 /* alignment slack */;
     return s;
 }
 
-template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {   // zero-fills where !ok
-    const int n = ok ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -136,17 +143,23 @@ __device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, fl
     }
 }
 
-// Position in the CTA's sequence of tasks: which weight rows and which steps this warp reads.
+// Position in the CTA's sequence of tasks: which weight rows and which stages this warp reads.
 struct Cursor {
-    int task, end, j;          // this CTA's tasks are [task, end); j: index of the expert in act[]
-    int e, row0, step, last, ch, s, rb;
+    int task, j;                    // j: index of the task's expert in act[]
+    int e, row0, ch, s, rb;
+    int step, last;                 // this warp's next stage of the task, the task's end
+    int turn;                       // stages of the CTA's earlier tasks, modulo the warps: whose turn the first one is
 };
 
-template <int MT, int NB, int D, bool SECOND>
-__global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(const FewArgs a) {
-    extern __shared__ __align__(128) unsigned char sm[];
+template <class V, bool SECOND>
+__global__ void __launch_bounds__(kThreads, V::NB == 1 ? 2 : 1)
+moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
+    constexpr int MT = V::MT, NB = V::NB, NBOX = V::NBOX, D = V::D;
+    extern __shared__ unsigned char raw[];
+    unsigned char* sm = reinterpret_cast<unsigned char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);   // the swizzle repeats every 1024 bytes
     const int TK = a.T * a.K;
-    const Smem L = layout<MT, NB, D>(TK, a.E);
+    const Smem L = layout<V>(TK, a.E);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + L.bars);
     int16_t* expert = reinterpret_cast<int16_t*>(sm + L.expert);
     int16_t* sorted = reinterpret_cast<int16_t*>(sm + L.sorted);
     float* score = reinterpret_cast<float*>(sm + L.score);
@@ -156,8 +169,9 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
     float* strips = reinterpret_cast<float*>(sm + L.ring);
     int* count = reinterpret_cast<int*>(strips + kWarps * a.E);
     int* place = count + a.E;
-    float* red = reinterpret_cast<float*>(sm + L.red);
+    float* red_all = reinterpret_cast<float*>(sm + L.red);
     __shared__ int n_act, flag;
+    __shared__ volatile int abort_word;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
     const int N = SECOND ? a.H : a.F, Kd = SECOND ? a.F : a.H;
@@ -167,6 +181,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
     // With few assignments the second kernel evaluates the router again, so that it can fill its ring with weights
     // while the first one is still running; with many it takes the first kernel's choices.
     const bool early = SECOND && TK <= 8;
+    if (tid < kWarps * D) mbar_init(&full[tid], 1);
+    if (tid == 0) { abort_word = 0; mbar_init_fence(); }
     if (!SECOND) {
         pdl_wait();
         pdl_trigger();
@@ -227,12 +243,13 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
             __syncwarp();
         }
     }
+    fence_async_smem();
     __syncthreads();   // the scratch is free: ring and red take its place
 
-    const int steps = (Kd + kStepK - 1) / kStepK, chunks = chunk[n_act];
-    int S = 1;         // slices of the reduction: enough tasks for an even load, at least two steps a warp
+    const int steps = (Kd + V::kStepK - 1) / V::kStepK, chunks = chunk[n_act];
+    int S = 1;         // slices of the reduction: enough tasks for an even load, at least four stages each
     if (SECOND)
-        while (S < a.max_split && (long long)chunks * RB * S < 8ll * gridDim.x && steps >= 4 * kWarps * S) S *= 2;
+        while (S < a.max_split && (long long)chunks * RB * S < 8ll * gridDim.x && steps >= 8 * S) S *= 2;
     const long long total = (long long)chunks * RB * S;
     const int t0 = (int)(total * blockIdx.x / gridDim.x), t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
 
@@ -240,34 +257,38 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
         while (c.task >= chunk[c.j + 1] * RB * S) ++c.j;
         int r = c.task - chunk[c.j] * RB * S;
         const int nch = chunk[c.j + 1] - chunk[c.j];
-        c.ch = r % nch; r /= nch;
-        c.rb = r % RB; c.s = r / RB;
+        if (nch > 1) { c.ch = r % nch; r /= nch; } else { c.ch = 0; }
+        if (S > 1) { c.rb = r % RB; c.s = r / RB; } else { c.rb = r; c.s = 0; }
         c.e = act[c.j];
         c.row0 = c.rb * 8 * NB;
-        c.step = (int)((long long)steps * c.s / S) + warp;
-        c.last = (int)((long long)steps * (c.s + 1) / S);
+        const int from = steps * c.s / S;
+        c.last = steps * (c.s + 1) / S;
+        c.step = from + ((warp - c.turn) & (kWarps - 1));
+        c.turn = (c.turn + c.last - from) & (kWarps - 1);
     };
-    const uint32_t ring0 = smem_u32(sm + L.ring) + tid * 16;
     Cursor in{};
-    in.task = t0; in.end = t1;
+    in.task = t0;
+    auto settle = [&]() {   // skips tasks in which it is never this warp's turn
+        while (in.step >= in.last && ++in.task < t1) locate(in);
+    };
     if (t0 < t1) {
         locate(in);
-        while (in.step >= in.last && ++in.task < in.end) locate(in);
+        settle();
     }
+    unsigned char* ring = sm + L.ring + warp * D * V::kStage;
     int in_slot = 0;
     auto issue = [&]() {
-        if (in.task < in.end) {
-            const int k = in.step * kStepK + tq * 8;
+        if (in.task < t1) {
+            if (lane == 0 && !abort_word) {
+                uint64_t* bar = &full[warp * D + in_slot];
+                mbar_expect_tx(bar, V::kStage);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int row = in.row0 + nb * 8 + gq;
-                const bool ok = row < N && k < Kd;
-                cp_async16(ring0 + (in_slot * NB + nb) * (kThreads * 16), ok ? W + ((size_t)in.e * N + row) * Kd + k : W, ok);
+                for (int b = 0; b < NBOX; ++b)   // beyond the matrix a box is filled with zeros
+                    tma_load_2d(ring + in_slot * V::kStage + b * V::kBox, &map, in.step * V::kStepK + b * kBoxK, in.e * N + in.row0, bar);
             }
             in.step += kWarps;
-            while (in.step >= in.last && ++in.task < in.end) locate(in);
+            settle();
         }
-        cp_commit();
         if (++in_slot == D) in_slot = 0;
     };
 #pragma unroll 1
@@ -278,9 +299,9 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
         pdl_trigger();
     }
     const uint16_t* A = SECOND ? a.g : a.x;
-    int slot = 0;
+    int slot = 0, strip = 0;
+    uint32_t phase = 0;
     Cursor c{};
-    c.end = t1;
     for (int task = t0; task < t1; ++task) {
         c.task = task;
         locate(c);
@@ -288,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
         // The second product takes the intermediate as high + low part.  While its tokens fill no more than half of
         // the tile's rows, the low parts are the other half; beyond that they take products of their own.
         constexpr int half = 8 * MT;
-        const bool packed = SECOND && m_here <= half;
+        const bool packed = SECOND && m_here <= half, two_pass = SECOND && !packed;
         const int rows_used = packed ? half + m_here : m_here;
         const uint32_t low = (uint32_t)TK * (uint32_t)Kd;
         uint32_t off[2 * MT];   // element offset of the row in A; kNoRow: a row of zeros
@@ -300,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
             const int as = mm < m_here ? sorted[base + mm] : -1;
             off[i] = as < 0 ? kNoRow : (uint32_t)(SECOND ? as : as % a.T) * (uint32_t)Kd + (lower ? low : 0u);
         }
+        constexpr int P = 2 * NBOX;   // 16-byte pieces of a row that one thread holds of a stage
         float acc[MT][NB][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -309,41 +331,64 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
                 for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
 #pragma unroll 1
         for (; c.step < c.last; c.step += kWarps) {
-            const int k = c.step * kStepK + tq * 8;
-            uint4 av[2 * MT];
+            const int k0 = c.step * V::kStepK + tq * 16;
+            uint4 av[P][2 * MT], al[SECOND && NB > 1 ? P : 1][2 * MT];
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) {
-                av[i] = make_uint4(0, 0, 0, 0);
-                if (off[i] != kNoRow && k < Kd) av[i] = *reinterpret_cast<const uint4*>(A + off[i] + k);
+            for (int p = 0; p < P; ++p) {
+                const int k = k0 + (p >> 1) * kBoxK + (p & 1) * 8;
+#pragma unroll
+                for (int i = 0; i < 2 * MT; ++i) {
+                    av[p][i] = make_uint4(0, 0, 0, 0);
+                    if (off[i] != kNoRow && k < Kd) av[p][i] = *reinterpret_cast<const uint4*>(A + off[i] + k);
+                }
             }
-            cp_wait<D - 1>();
-            uint4 wv[NB];
+            if constexpr (SECOND && NB > 1) {   // at most 8 assignments (NB = 1) are always packed
+                if (two_pass) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
-                wv[n] = *reinterpret_cast<const uint4*>(sm + L.ring + (size_t)((slot * NB + n) * kThreads + tid) * 16);
-            auto products = [&]() {
+                    for (int p = 0; p < P; ++p) {
+                        const int k = k0 + (p >> 1) * kBoxK + (p & 1) * 8;
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (m > 0 && m * 16 >= rows_used) break;
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        mma16816(acc[m][n], av[2 * m].x, av[2 * m + 1].x, av[2 * m].y, av[2 * m + 1].y, wv[n].x, wv[n].y);
-                        mma16816(acc[m][n], av[2 * m].z, av[2 * m + 1].z, av[2 * m].w, av[2 * m + 1].w, wv[n].z, wv[n].w);
+                        for (int i = 0; i < 2 * MT; ++i) {
+                            al[p][i] = make_uint4(0, 0, 0, 0);
+                            if (off[i] != kNoRow && k < Kd) al[p][i] = *reinterpret_cast<const uint4*>(A + off[i] + low + k);
+                        }
                     }
                 }
-            };
-            products();
-            if (SECOND && !packed) {
-#pragma unroll
-                for (int i = 0; i < 2 * MT; ++i)
-                    if (off[i] != kNoRow && k < Kd) av[i] = *reinterpret_cast<const uint4*>(A + off[i] + low + k);
-                products();
             }
+            if (!abort_word && !mbar_wait_bounded(&full[warp * D + slot], phase)) {
+                abort_word = 1;
+                atomicOr(&g_few_flags, 1);
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                uint4 wv[NB];
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    wv[n] = *reinterpret_cast<const uint4*>(ring + slot * V::kStage + (p >> 1) * V::kBox + (n * 8 + gq) * 128 +
+                                                            (((2 * tq + (p & 1)) ^ gq) * 16));
+                auto products = [&](const uint4 (&v)[2 * MT]) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        if (m > 0 && m * 16 >= rows_used) break;
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16816(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, wv[n].x, wv[n].y);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16816(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, wv[n].z, wv[n].w);
+                    }
+                };
+                products(av[p]);
+                if constexpr (SECOND && NB > 1) {
+                    if (two_pass) products(al[p]);
+                }
+            }
+            __syncwarp();   // the stage has been read by the whole warp
             issue();
-            if (++slot == D) slot = 0;
+            if (++slot == D) { slot = 0; phase ^= 1u; }
         }
         // the warps' shares of the sum, added in warp order
         constexpr int C = 8 * NB;
+        float* red = red_all + strip * V::kRed;
+        strip ^= 1;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -378,9 +423,9 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
                 a.part[((size_t)c.s * TK + as) * a.H + row] = v;
             }
         }
-        if (SECOND && !direct) __threadfence();
-        __syncthreads();
         if (SECOND && !direct) {   // the last slice of these columns to arrive adds them all up, in a fixed order
+            __threadfence();
+            __syncthreads();
             if (tid == 0) {
                 __threadfence();
                 flag = atomicAdd(&a.arrived[c.rb], 1) == chunks * S - 1;
@@ -402,7 +447,11 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 2) moe_few_kernel(cons
             }
         }
     }
-    cp_wait<0>();
+    // After a wait that was given up copies may still be on their way into this CTA's shared memory: it stays for a
+    // millisecond, hundreds of times their latency, before it leaves.
+    __syncthreads();
+    if (abort_word)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
 struct FewPlan { size_t off_g, off_part, off_arrived, total; int max_split; };
@@ -420,25 +469,28 @@ FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
     return p;
 }
 
-template <int MT, int NB, int D>
+template <class V>
 int run_few(const FewArgs& a, cudaStream_t st) {
-    const Smem L = layout<MT, NB, D>(a.T * a.K, a.E);
+    const Smem L = layout<V>(a.T * a.K, a.E);
     static bool done_dev[64] = {false};   // the attribute is per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!done_dev[dev & 63]) {
-        const int most = layout<MT, NB, D>(kMaxTokens * kMaxK, kMaxExperts).total;
-        if (cudaFuncSetAttribute(moe_few_kernel<MT, NB, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
-            cudaFuncSetAttribute(moe_few_kernel<MT, NB, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
+        const int most = layout<V>(kMaxTokens * kMaxK, kMaxExperts).total;
+        if (cudaFuncSetAttribute(moe_few_kernel<V, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+            cudaFuncSetAttribute(moe_few_kernel<V, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
             cudaGetLastError();
             return LOCMOE_ERR_CUDA;
         }
         done_dev[dev & 63] = true;
     }
-    const dim3 grid(2 * sm_count());
-    const int rc = launch_pdl(moe_few_kernel<MT, NB, D, false>, grid, dim3(kThreads), L.total, st, a);
+    CUtensorMap m1, m2;
+    const uint64_t d1[2] = {(uint64_t)a.H, (uint64_t)a.E * a.F}, d2[2] = {(uint64_t)a.F, (uint64_t)a.E * a.H};
+    if (!make_map(&m1, a.w_in, 2, d1, 8 * V::NB) || !make_map(&m2, a.w_out, 2, d2, 8 * V::NB)) return LOCMOE_ERR_CUDA;
+    const dim3 grid(sm_count());
+    const int rc = launch_pdl(moe_few_kernel<V, false>, grid, dim3(kThreads), L.total, st, m1, a);
     if (rc) return rc;
-    return launch_pdl(moe_few_kernel<MT, NB, D, true>, grid, dim3(kThreads), L.total, st, a);
+    return launch_pdl(moe_few_kernel<V, true>, grid, dim3(kThreads), L.total, st, m2, a);
 }
 
 }  // namespace
@@ -453,9 +505,18 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
                     w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
                     reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
                     p.max_split, weighted};
-    if (s.T * K <= 8) return run_few<1, 1, 12>(a, st);
-    if (s.T <= 16) return run_few<1, 4, 4>(a, st);
-    return run_few<2, 4, 3>(a, st);
+    if (s.T * K <= 8) return run_few<Variant<1, 1, 4, 3>>(a, st);
+    if (s.T <= 16) return run_few<Variant<1, 4, 1, 5>>(a, st);
+    return run_few<Variant<2, 4, 1, 4>>(a, st);
+}
+
+int read_few_flags(int* out, cudaStream_t st) {
+    if (cudaMemcpyFromSymbolAsync(out, g_few_flags, sizeof(int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    return LOCMOE_OK;
 }
 
 }  // namespace locmoe
