@@ -515,7 +515,7 @@ int locmoe_moe_layer(const locmoe_shape_t *shape, const void *x, const int32_t *
  * after a norm (locmoe_block_norm).  A token with an infinity or a NaN gets a valid choice and unspecified outputs and
  * disturbs no other token.
  * T <= LOCMOE_FEW_MAX_TOKENS, E <= 1024 (LOCMOE_ERR_TOO_LARGE), K <= min(8, E), F < 2^20, H and F multiples of 8,
- * x, w_in, w_out 16-byte aligned.  ws: locmoe_moe_few_bytes() bytes, 256-byte aligned; its contents are undefined
+ * x, w_in, w_out, out 16-byte aligned.  ws: locmoe_moe_few_bytes() bytes, 256-byte aligned; its contents are undefined
  * between calls.  The shape's node fields and layout are validated but do not matter.
  */
 enum { LOCMOE_FEW_MAX_TOKENS = 128, LOCMOE_FEW_UNWEIGHTED = 1 };

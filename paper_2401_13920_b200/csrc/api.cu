@@ -442,7 +442,7 @@ int locmoe_moe_few(const locmoe_shape_t* shape, const void* x, const float* eps,
     if (!x || !w_in || !w_out || !idx_k || !w_k || !out) return LOCMOE_ERR_NULL;
     if (flags & ~LOCMOE_FEW_UNWEIGHTED) return LOCMOE_ERR_DTYPE;
     if ((flags & LOCMOE_FEW_UNWEIGHTED) && K != 1) return LOCMOE_ERR_SHAPE;
-    if ((uintptr_t)x % 16 || (uintptr_t)w_in % 16 || (uintptr_t)w_out % 16 || (uintptr_t)out % 2 || (uintptr_t)eps % 4 ||
+    if ((uintptr_t)x % 16 || (uintptr_t)w_in % 16 || (uintptr_t)w_out % 16 || (uintptr_t)out % 16 || (uintptr_t)eps % 4 ||
         (uintptr_t)idx_k % 4 || (uintptr_t)w_k % 4)
         return LOCMOE_ERR_ALIGN;
     if (!ws || ws_bytes < few_ws_bytes(*shape, F, K) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;

@@ -5,12 +5,12 @@
 //
 // Bound by the weights of the experts that the tokens meet (4 F H bytes each), every one of which is read once.  So
 // the weights are what moves fast: every warp streams its own tiles of 8 * NB weight rows through a private ring of
-// TMA stages, without barriers between warps, across the borders of its tasks.  A task is a block of 8 * NB weight
-// rows of one expert (and, in the second product, one of S slices of the reduction); the stages of the CTA's tasks
-// are dealt to its warps in turn.  The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as
-// the 8 columns: at a few tokens an expert nothing is gained by larger matrix instructions.  The order of k inside a
-// stage is chosen so that a thread's fragments of both operands are 16 contiguous bytes of a row (the same
-// permutation on both sides), which the tiles' 128-byte swizzle gives without bank conflicts.
+// TMA stages.  A task is a block of 8 * NB weight rows of one expert (and, in the second product, one of S slices of
+// the reduction); a warp works on its tasks from the first byte to the result with no barrier but its own ring's.
+// The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
+// expert nothing is gained by larger matrix instructions.  The order of k inside a stage is chosen so that a
+// thread's fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides), which
+// the tiles' 128-byte swizzle gives without bank conflicts.
 // The router is evaluated by every CTA for itself: a few tokens' rows out of L2 cost less than a launch of their own.
 #include "common.cuh"
 #include "tensor_map.cuh"
@@ -19,7 +19,6 @@ namespace locmoe {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
 constexpr int kBoxK = 64;          // k of one TMA box: 128 bytes of a row
 
@@ -35,29 +34,28 @@ struct FewArgs {
     int T, H, E, K, F, max_split, weighted;
 };
 
-// A variant: MT tiles of 16 tokens, NB blocks of 8 weight rows, NBOX boxes of 64 k a stage, D stages a warp.
-template <int MT_, int NB_, int NBOX_, int D_>
+// A variant: W warps, MT tiles of 16 tokens, NB blocks of 8 weight rows, NBOX boxes of 64 k a stage, D stages a warp;
+// the tasks an SM should have at least for an even load, the CTAs for which an SM has room.
+template <int W_, int MT_, int NB_, int NBOX_, int D_, int TASKS_, int CTAS_>
 struct Variant {
-    static constexpr int MT = MT_, NB = NB_, NBOX = NBOX_, D = D_;
-    static constexpr int kBox = 8 * NB * 128, kStage = NBOX * kBox, kRing = kWarps * D * kStage;
-    static constexpr int kRed = kWarps * 16 * MT * 8 * NB;   // floats of one of the two strips
+    static constexpr int W = W_, MT = MT_, NB = NB_, NBOX = NBOX_, D = D_, kTasks = TASKS_, kCtas = CTAS_;
+    static constexpr int kThreads = 32 * W, kBox = 8 * NB * 128, kStage = NBOX * kBox, kRing = W * D * kStage;
     static constexpr int kStepK = NBOX * kBoxK;
 };
 
 struct Smem {   // offsets of the dynamic shared memory, from its first 1024-byte boundary on
-    int ring, red, bars, expert, sorted, score, act, first, chunk, total;
+    int ring, bars, expert, sorted, score, act, first, chunk, total;
 };
 __host__ __device__ constexpr int round16(int n) { return (n + 15) / 16 * 16; }
 template <class V>
 __host__ __device__ inline Smem layout(int TK, int E) {
     Smem s{};
     const int most = TK < E ? TK : E;
-    // the router's scratch lies where ring and red are later: a strip of E floats per warp, the counters beside it
-    const int scratch = (kWarps + 2) * E * 4, body = V::kRing + 2 * V::kRed * 4;
+    // the router's scratch lies where the ring is later: a strip of E floats per warp, the counters beside it
+    const int scratch = (V::W + 2) * E * 4;
     s.ring = 0;
-    s.red = V::kRing;
-    s.bars = scratch > body ? round16(scratch) : body;
-    s.expert = s.bars + round16(8 * kWarps * V::D);   // int16 [TK]  expert of assignment a = c * T + t
+    s.bars = scratch > V::kRing ? round16(scratch) : V::kRing;
+    s.expert = s.bars + round16(8 * V::W * V::D);   // int16 [TK]  expert of assignment a = c * T + t
     s.sorted = s.expert + round16(2 * TK);            // int16 [TK]  assignments by expert
     s.score = s.sorted + round16(2 * TK);             // float [TK]
     s.act = s.score + round16(4 * TK);                // int16 [most]      experts met
@@ -93,6 +91,7 @@ __device__ __forceinline__ float sum_pieces(const uint16_t* p, int n, int sub, i
 }
 
 // Router for all tokens, one warp per token: fills expert[] and score[].
+template <int W>
 __device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, float* score, float* strip_all) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = a.H / a.E;
@@ -101,7 +100,7 @@ __device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, fl
     while (lanes * 2 * a.E <= 32) lanes *= 2;
     const int sub = lane % lanes;
     const float inv_g = 1.0f / (float)g;
-    for (int t = warp; t < a.T; t += kWarps) {
+    for (int t = warp; t < a.T; t += W) {
         const uint16_t* row = a.x + (size_t)t * a.H;
         for (int i0 = 0; i0 < a.E; i0 += 32 / lanes) {
             const int i = i0 + lane / lanes;
@@ -143,18 +142,16 @@ __device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, fl
     }
 }
 
-// Position in the CTA's sequence of tasks: which weight rows and which stages this warp reads.
+// Position in a warp's sequence of tasks: which weight rows and which stages come next.
 struct Cursor {
     int task, j;                    // j: index of the task's expert in act[]
-    int e, row0, ch, s, rb;
-    int step, last;                 // this warp's next stage of the task, the task's end
-    int turn;                       // stages of the CTA's earlier tasks, modulo the warps: whose turn the first one is
+    int e, row0, ch, s, rb, step, last;
 };
 
 template <class V, bool SECOND>
-__global__ void __launch_bounds__(kThreads, V::NB == 1 ? 2 : 1)
+__global__ void __launch_bounds__(V::kThreads, V::kCtas)
 moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
-    constexpr int MT = V::MT, NB = V::NB, NBOX = V::NBOX, D = V::D;
+    constexpr int W = V::W, MT = V::MT, NB = V::NB, NBOX = V::NBOX, D = V::D, kThreads = V::kThreads;
     extern __shared__ unsigned char raw[];
     unsigned char* sm = reinterpret_cast<unsigned char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);   // the swizzle repeats every 1024 bytes
     const int TK = a.T * a.K;
@@ -167,28 +164,26 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
     int16_t* first = reinterpret_cast<int16_t*>(sm + L.first);
     int16_t* chunk = reinterpret_cast<int16_t*>(sm + L.chunk);
     float* strips = reinterpret_cast<float*>(sm + L.ring);
-    int* count = reinterpret_cast<int*>(strips + kWarps * a.E);
+    int* count = reinterpret_cast<int*>(strips + W * a.E);
     int* place = count + a.E;
-    float* red_all = reinterpret_cast<float*>(sm + L.red);
-    __shared__ int n_act, flag;
+    __shared__ int n_act;
     __shared__ volatile int abort_word;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
     const int N = SECOND ? a.H : a.F, Kd = SECOND ? a.F : a.H;
-    const uint16_t* W = SECOND ? a.w_out : a.w_in;
     const int RB = (N + 8 * NB - 1) / (8 * NB);
 
     // With few assignments the second kernel evaluates the router again, so that it can fill its ring with weights
     // while the first one is still running; with many it takes the first kernel's choices.
     const bool early = SECOND && TK <= 8;
-    if (tid < kWarps * D) mbar_init(&full[tid], 1);
+    if (tid < W * D) mbar_init(&full[tid], 1);
     if (tid == 0) { abort_word = 0; mbar_init_fence(); }
     if (!SECOND) {
         pdl_wait();
         pdl_trigger();
     }
     if (!SECOND || early) {
-        few_router(a, expert, score, strips);
+        few_router<W>(a, expert, score, strips);
     } else {
         pdl_wait();
         pdl_trigger();
@@ -244,14 +239,14 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
         }
     }
     fence_async_smem();
-    __syncthreads();   // the scratch is free: ring and red take its place
+    __syncthreads();   // the scratch is free: the ring takes its place
 
     const int steps = (Kd + V::kStepK - 1) / V::kStepK, chunks = chunk[n_act];
     int S = 1;         // slices of the reduction: enough tasks for an even load, at least four stages each
     if (SECOND)
-        while (S < a.max_split && (long long)chunks * RB * S < 8ll * gridDim.x && steps >= 8 * S) S *= 2;
+        while (S < a.max_split && (long long)chunks * RB * S < (long long)V::kTasks * gridDim.x && steps >= 8 * S) S *= 2;
     const long long total = (long long)chunks * RB * S;
-    const int t0 = (int)(total * blockIdx.x / gridDim.x), t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
+    const int t0 = (int)(total * blockIdx.x / gridDim.x) + warp, t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);   // every W-th of these
 
     auto locate = [&](Cursor& c) {
         while (c.task >= chunk[c.j + 1] * RB * S) ++c.j;
@@ -261,20 +256,12 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
         if (S > 1) { c.rb = r % RB; c.s = r / RB; } else { c.rb = r; c.s = 0; }
         c.e = act[c.j];
         c.row0 = c.rb * 8 * NB;
-        const int from = steps * c.s / S;
+        c.step = steps * c.s / S;
         c.last = steps * (c.s + 1) / S;
-        c.step = from + ((warp - c.turn) & (kWarps - 1));
-        c.turn = (c.turn + c.last - from) & (kWarps - 1);
     };
     Cursor in{};
     in.task = t0;
-    auto settle = [&]() {   // skips tasks in which it is never this warp's turn
-        while (in.step >= in.last && ++in.task < t1) locate(in);
-    };
-    if (t0 < t1) {
-        locate(in);
-        settle();
-    }
+    if (t0 < t1) locate(in);
     unsigned char* ring = sm + L.ring + warp * D * V::kStage;
     int in_slot = 0;
     auto issue = [&]() {
@@ -286,8 +273,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
                 for (int b = 0; b < NBOX; ++b)   // beyond the matrix a box is filled with zeros
                     tma_load_2d(ring + in_slot * V::kStage + b * V::kBox, &map, in.step * V::kStepK + b * kBoxK, in.e * N + in.row0, bar);
             }
-            in.step += kWarps;
-            settle();
+            if (++in.step == in.last && (in.task += W) < t1) locate(in);
         }
         if (++in_slot == D) in_slot = 0;
     };
@@ -299,10 +285,10 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
         pdl_trigger();
     }
     const uint16_t* A = SECOND ? a.g : a.x;
-    int slot = 0, strip = 0;
+    int slot = 0;
     uint32_t phase = 0;
     Cursor c{};
-    for (int task = t0; task < t1; ++task) {
+    for (int task = t0; task < t1; task += W) {
         c.task = task;
         locate(c);
         const int base = first[c.j] + c.ch * 16 * MT, m_here = min(16 * MT, first[c.j + 1] - base);
@@ -330,7 +316,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
 #pragma unroll 1
-        for (; c.step < c.last; c.step += kWarps) {
+        for (; c.step < c.last; ++c.step) {
             const int k0 = c.step * V::kStepK + tq * 16;
             uint4 av[P][2 * MT], al[SECOND && NB > 1 ? P : 1][2 * MT];
 #pragma unroll
@@ -385,65 +371,66 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
             issue();
             if (++slot == D) { slot = 0; phase ^= 1u; }
         }
-        // the warps' shares of the sum, added in warp order
-        constexpr int C = 8 * NB;
-        float* red = red_all + strip * V::kRed;
-        strip ^= 1;
+        // Results straight from the accumulators: thread (gq, tq) has weight rows 2 tq and 2 tq + 1 of each block and
+        // the tokens gq of each group of eight; the low parts' shares lie in the same thread.
+        const bool direct = SECOND && S == 1 && a.K == 1;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int i = 0; i < 2 * MT; ++i) {
+            const int m = i * 8 + gq;
+            if (m >= m_here) continue;
+            const int as = sorted[base + m];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                float* r = red + ((warp * 16 * MT) + m * 16 + gq) * C + n * 8 + tq * 2;
-                *reinterpret_cast<float2*>(r) = make_float2(acc[m][n][0], acc[m][n][1]);
-                *reinterpret_cast<float2*>(r + 8 * C) = make_float2(acc[m][n][2], acc[m][n][3]);
-            }
-        __syncthreads();
-        const bool direct = SECOND && S == 1 && a.K == 1;
-        for (int o = tid; o < m_here * C; o += kThreads) {
-            const int m = o / C, r = o % C, row = c.row0 + r;
-            if (row >= N) continue;
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) v += red[(w * 16 * MT + m) * C + r];
-            if (packed) {
-                float lo = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) lo += red[(w * 16 * MT + half + m) * C + r];
-                v += lo;
-            }
-            const int as = sorted[base + m];
-            if (!SECOND) {
-                v = 0.5f * v * erfcf(-0.70710678118654752f * v);
-                const uint32_t hi = f32_to_bf16_bits(v);
-                a.g[(size_t)as * a.F + row] = (uint16_t)hi;
-                a.g[((size_t)TK + as) * a.F + row] = (uint16_t)f32_to_bf16_bits(v - bf16_lo(hi));
-            } else if (direct) {
-                a.out[(size_t)as * a.H + row] = (uint16_t)f32_to_bf16_bits(a.weighted ? v * score[as] : v);
-            } else {
-                a.part[((size_t)c.s * TK + as) * a.H + row] = v;
+                const int row = c.row0 + n * 8 + tq * 2;
+                if (row >= N) continue;
+                float2 v = make_float2(acc[i >> 1][n][(i & 1) * 2], acc[i >> 1][n][(i & 1) * 2 + 1]);
+                if (packed && i < MT) {
+                    v.x += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2];
+                    v.y += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2 + 1];
+                }
+                if (!SECOND) {
+                    v.x = 0.5f * v.x * erfcf(-0.70710678118654752f * v.x);
+                    v.y = 0.5f * v.y * erfcf(-0.70710678118654752f * v.y);
+                    const uint32_t hi = cvt_bf16x2(v);
+                    uint16_t* g = a.g + (size_t)as * a.F + row;
+                    *reinterpret_cast<uint32_t*>(g) = hi;
+                    *reinterpret_cast<uint32_t*>(g + (size_t)TK * a.F) = cvt_bf16x2(make_float2(v.x - bf16_lo(hi), v.y - bf16_hi(hi)));
+                } else if (direct) {
+                    const float f = a.weighted ? score[as] : 1.0f;
+                    *reinterpret_cast<uint32_t*>(a.out + (size_t)as * a.H + row) = cvt_bf16x2(make_float2(v.x * f, v.y * f));
+                } else {
+                    *reinterpret_cast<float2*>(a.part + ((size_t)c.s * TK + as) * a.H + row) = v;
+                }
             }
         }
-        if (SECOND && !direct) {   // the last slice of these columns to arrive adds them all up, in a fixed order
+        if (SECOND && !direct) {   // the last task of these columns to arrive adds them all up, in a fixed order
             __threadfence();
-            __syncthreads();
-            if (tid == 0) {
+            __syncwarp();
+            int last = 0;
+            if (lane == 0) last = atomicAdd(&a.arrived[c.rb], 1) == chunks * S - 1;
+            if (__shfl_sync(0xffffffffu, last, 0)) {
                 __threadfence();
-                flag = atomicAdd(&a.arrived[c.rb], 1) == chunks * S - 1;
-            }
-            __syncthreads();
-            if (flag) {
-                __threadfence();
-                for (int o = tid; o < a.T * C; o += kThreads) {
-                    const int t = o / C, row = c.row0 + o % C;
-                    if (row >= N) continue;
-                    float v = 0.0f;
-                    for (int k = 0; k < a.K; ++k) {
-                        float y = 0.0f;
-                        for (int s = 0; s < S; ++s) y += __ldcg(&a.part[((size_t)s * TK + k * a.T + t) * a.H + row]);
-                        v = fmaf(a.weighted ? score[k * a.T + t] : 1.0f, y, v);
+                constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
+                const int row = c.row0 + (lane % Q) * 4;
+                if (row < N) {
+                    for (int t = lane / Q; t < a.T; t += 32 / Q) {
+                        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        for (int k = 0; k < a.K; ++k) {
+                            const float* p = a.part + ((size_t)k * a.T + t) * a.H + row;
+                            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+                            for (int s = 0; s < S; ++s) {
+                                const float4 z = __ldcg(reinterpret_cast<const float4*>(p + (size_t)s * TK * a.H));
+                                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                            }
+                            const float f = a.weighted ? score[k * a.T + t] : 1.0f;
+                            v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+                        }
+                        *reinterpret_cast<uint2*>(a.out + (size_t)t * a.H + row) =
+                            make_uint2(cvt_bf16x2(make_float2(v.x, v.y)), cvt_bf16x2(make_float2(v.z, v.w)));
                     }
-                    a.out[(size_t)t * a.H + row] = (uint16_t)f32_to_bf16_bits(v);
                 }
+                __syncwarp();
             }
         }
     }
@@ -488,9 +475,9 @@ int run_few(const FewArgs& a, cudaStream_t st) {
     const uint64_t d1[2] = {(uint64_t)a.H, (uint64_t)a.E * a.F}, d2[2] = {(uint64_t)a.F, (uint64_t)a.E * a.H};
     if (!make_map(&m1, a.w_in, 2, d1, 8 * V::NB) || !make_map(&m2, a.w_out, 2, d2, 8 * V::NB)) return LOCMOE_ERR_CUDA;
     const dim3 grid(sm_count());
-    const int rc = launch_pdl(moe_few_kernel<V, false>, grid, dim3(kThreads), L.total, st, m1, a);
+    const int rc = launch_pdl(moe_few_kernel<V, false>, grid, dim3(V::kThreads), L.total, st, m1, a);
     if (rc) return rc;
-    return launch_pdl(moe_few_kernel<V, true>, grid, dim3(kThreads), L.total, st, m2, a);
+    return launch_pdl(moe_few_kernel<V, true>, grid, dim3(V::kThreads), L.total, st, m2, a);
 }
 
 }  // namespace
@@ -505,9 +492,9 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
                     w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
                     reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
                     p.max_split, weighted};
-    if (s.T * K <= 8) return run_few<Variant<1, 1, 4, 3>>(a, st);
-    if (s.T <= 16) return run_few<Variant<1, 4, 1, 5>>(a, st);
-    return run_few<Variant<2, 4, 1, 4>>(a, st);
+    if (s.T * K <= 8) return run_few<Variant<16, 1, 1, 2, 3, 8, 2>>(a, st);
+    if (s.T <= 16) return run_few<Variant<12, 1, 2, 2, 4, 48, 1>>(a, st);
+    return run_few<Variant<12, 2, 4, 1, 4, 48, 1>>(a, st);
 }
 
 int read_few_flags(int* out, cudaStream_t st) {
