@@ -3,14 +3,16 @@
 //
 //   G_i = ReLU(mean_i x + eps_i),  p = softmax(G),  the K largest;   out_t = sum_c p_{t,c} W_out[e] GeLU(W_in[e] x_t)
 //
-// Bound by the weights of the experts that the tokens meet (4 F H bytes each), every one of which is read once.  So
-// the weights are what moves fast: every warp streams its own tiles of 8 * NB weight rows through a private ring of
-// TMA stages.  A task is a block of 8 * NB weight rows of one expert (and, in the second product, one of S slices of
-// the reduction); a warp works on its tasks from the first byte to the result with no barrier but its own ring's.
+// Bound by the weights of the experts that the tokens meet (4 F H bytes each), every one of which is read once.  A task
+// is a block of R weight rows of one expert (and, in the second product, one of S slices of the reduction); a CTA
+// streams its tasks' weights, without a pause between them, through one ring of stages: a producer warp fills a stage
+// with a TMA box of weights and the tokens' pieces of the same k (bulk copies, one a row), eight warps multiply.
+// The tokens travel with the weights because a load that a multiplying warp issues itself queues behind the ring's
+// own (4000 cycles at a full ring: 2.9 against 6.5 TB/s on a stream of rows of 10240).
 // The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
-// expert nothing is gained by larger matrix instructions.  The order of k inside a stage is chosen so that a
-// thread's fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides), which
-// the tiles' 128-byte swizzle gives without bank conflicts.
+// expert nothing is gained by larger matrix instructions.  The order of k inside a stage is chosen so that a thread's
+// fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides), which the weight
+// tiles' 128-byte swizzle and the token rows' pitch give without bank conflicts.
 // The router is evaluated by every CTA for itself: a few tokens' rows out of L2 cost less than a launch of their own.
 #include "common.cuh"
 #include "tensor_map.cuh"
@@ -20,10 +22,10 @@ namespace locmoe {
 namespace {
 
 constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
+constexpr int kMostSmem = 226 << 10;   // of the 227 KB that a CTA can have
 constexpr int kBoxK = 64;          // k of one TMA box: 128 bytes of a row
 
 __device__ int g_few_flags = 0;    // bit 0: a bounded wait gave up
-constexpr uint32_t kNoRow = 0xffffffffu;
 
 struct FewArgs {
     const uint16_t* x; const float* eps; const uint16_t* w_in; const uint16_t* w_out;
@@ -34,47 +36,67 @@ struct FewArgs {
     int T, H, E, K, F, max_split, weighted;
 };
 
-// A variant: W warps, MT tiles of 16 tokens, NB blocks of 8 weight rows, NBOX boxes of 64 k a stage, D stages a warp;
-// the tasks an SM should have at least for an even load, the CTAs for which an SM has room.
-template <int W_, int MT_, int NB_, int NBOX_, int D_, int TASKS_, int CTAS_>
+// A variant: GR groups, each with a ring, a producer warp and multiplying warps, WR along the weight rows and WK along
+// k; NB blocks of 8 weight rows a warp, BW boxes of 64 k a warp and stage, MT tiles of 16 tokens; the shared memory of
+// a CTA, how many an SM holds.  A group works on every GR-th task by itself, so that one group's sums and stores run
+// beside the others' products.
+constexpr int kMaxStages = 8;   // of a group's ring
+template <int GR_, int WR_, int WK_, int NB_, int BW_, int MT_, int SMEM_, int CTAS_>
 struct Variant {
-    static constexpr int W = W_, MT = MT_, NB = NB_, NBOX = NBOX_, D = D_, kTasks = TASKS_, kCtas = CTAS_;
-    static constexpr int kThreads = 32 * W, kBox = 8 * NB * 128, kStage = NBOX * kBox, kRing = W * D * kStage;
-    static constexpr int kStepK = NBOX * kBoxK;
+    static constexpr int GR = GR_, WR = WR_, WK = WK_, NB = NB_, BW = BW_, MT = MT_, kSmem = SMEM_, kCtas = CTAS_;
+    static constexpr int kMulWarps = WR * WK, kThreads = 32 * GR * (kMulWarps + 1);
+    static constexpr int kBoxes = WK * BW;
+    static constexpr int R = 8 * NB * WR, kStepK = kBoxK * kBoxes;      // weight rows of a task, k of a stage
+    static constexpr int kBox = R * 128, kWeights = kBoxes * kBox;      // bytes of one box and of a stage's weights
+    static constexpr int kPitch = kStepK * 2 + 16;                      // of a token's row: an odd number of 16-byte banks
+    static constexpr int kRed = WK > 1 ? WK * 16 * MT * R : 0;          // floats of a group's strip of partial sums
 };
 
 struct Smem {   // offsets of the dynamic shared memory, from its first 1024-byte boundary on
-    int ring, bars, expert, sorted, score, act, first, chunk, total;
+    int ring, red, full, empty, expert, sorted, score, act, first, chunk, total;
+    int stage, stages;   // bytes of a stage, stages of a group's ring
 };
-__host__ __device__ constexpr int round16(int n) { return (n + 15) / 16 * 16; }
+__host__ __device__ constexpr int round_up(int n, int to) { return (n + to - 1) / to * to; }
+// rows: token rows of a stage at most.  The ring takes what the rest leaves.
 template <class V>
-__host__ __device__ inline Smem layout(int TK, int E) {
+__host__ __device__ inline Smem layout(int TK, int E, int rows) {
     Smem s{};
-    const int most = TK < E ? TK : E;
-    // the router's scratch lies where the ring is later: a strip of E floats per warp, the counters beside it
-    const int scratch = (V::W + 2) * E * 4;
+    const int most = TK < E ? TK : E, red = V::GR * V::kRed * 4;
+    s.stage = round_up(V::kWeights + rows * V::kPitch, 1024);
+    const int tail = red + 16 * V::GR * kMaxStages + round_up(2 * TK, 16) * 2 + round_up(4 * TK, 16) + round_up(2 * most, 16) +
+                     2 * round_up(2 * most + 2, 16) + 1024 /* alignment slack */;
+    s.stages = (V::kSmem - tail) / s.stage / V::GR;
+    if (s.stages > kMaxStages) s.stages = kMaxStages;
+    // the logits (as many tokens' as fit) and then the counters (2 E ints) lie where the ring is later
     s.ring = 0;
-    s.bars = scratch > V::kRing ? round16(scratch) : V::kRing;
-    s.expert = s.bars + round16(8 * V::W * V::D);   // int16 [TK]  expert of assignment a = c * T + t
-    s.sorted = s.expert + round16(2 * TK);            // int16 [TK]  assignments by expert
-    s.score = s.sorted + round16(2 * TK);             // float [TK]
-    s.act = s.score + round16(4 * TK);                // int16 [most]      experts met
-    s.first = s.act + round16(2 * most);              // int16 [most + 1]  their first entry of `sorted`
-    s.chunk = s.first + round16(2 * most + 2);        // int16 [most + 1]  their first chunk of 16 * MT tokens
-    s.total = s.chunk + round16(2 * most + 2) + 1024 /* alignment slack */;
+    s.red = round_up(V::GR * s.stages * s.stage > 2 * E * 4 ? V::GR * s.stages * s.stage : 2 * E * 4, 16);
+    s.full = s.red + red;
+    s.empty = s.full + 8 * V::GR * kMaxStages;
+    s.expert = s.empty + 8 * V::GR * kMaxStages;              // int16 [TK]  expert of assignment a = c * T + t
+    s.sorted = s.expert + round_up(2 * TK, 16);       // int16 [TK]  assignments by expert
+    s.score = s.sorted + round_up(2 * TK, 16);        // float [TK]
+    s.act = s.score + round_up(4 * TK, 16);           // int16 [most]      experts met
+    s.first = s.act + round_up(2 * most, 16);         // int16 [most + 1]  their first entry of `sorted`
+    s.chunk = s.first + round_up(2 * most + 2, 16);   // int16 [most + 1]  their first chunk of 16 * MT tokens
+    s.total = s.chunk + round_up(2 * most + 2, 16) + 1024;
     return s;
 }
 
+__device__ __forceinline__ uint4 ld_shared(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Sum of `n` consecutive bf16 values from `p`, of which this lane takes every `of`-th piece from `sub` on.
+// Sum of `n` consecutive bf16 values from `p`, of which this lane takes every `of`-th piece of EL from `sub` on.
 template <int EL>
 __device__ __forceinline__ float sum_pieces(const uint16_t* p, int n, int sub, int of) {
     float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll 4
+#pragma unroll 10
     for (int i = sub; i < n / EL; i += of) {
         if constexpr (EL == 8) {
             const uint4 w = __ldg(reinterpret_cast<const uint4*>(p) + i);
@@ -90,106 +112,128 @@ __device__ __forceinline__ float sum_pieces(const uint16_t* p, int n, int sub, i
     return s0 + s1;
 }
 
-// Router for all tokens, one warp per token: fills expert[] and score[].
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// global -> shared bulk copy by shared-memory address (16-byte aligned, a multiple of 16 bytes)
+__device__ __forceinline__ void bulk_row(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// Bounded wait that also ends once another warp has given up.
+__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, volatile int* abort_word) {
+    for (uint32_t i = 0; i < (1u << 17); ++i) {   // about half a second
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 15u) == 15u && *abort_word) return false;
+    }
+    *abort_word = 1;
+    atomicOr(&g_few_flags, 1);
+    return false;
+}
+// Router for all tokens: fills expert[] and score[].  The CTA's threads share out the (token, expert) pairs of as many
+// tokens as the scratch holds logits for, several lanes a pair while there are threads for that; then a warp a token
+// takes the softmax and the K largest.
 template <int W>
-__device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, float* score, float* strip_all) {
+__device__ __forceinline__ void few_router(const FewArgs& a, int16_t* expert, float* score, float* logits, int floats) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int g = a.H / a.E;
-    float* G = strip_all + warp * a.E;
-    int lanes = 1;                                   // lanes that share one expert's group
-    while (lanes * 2 * a.E <= 32) lanes *= 2;
-    const int sub = lane % lanes;
+    const int g = a.H / a.E, el = g % 8 == 0 ? 8 : g % 2 == 0 ? 2 : 1;
     const float inv_g = 1.0f / (float)g;
-    for (int t = warp; t < a.T; t += W) {
-        const uint16_t* row = a.x + (size_t)t * a.H;
-        for (int i0 = 0; i0 < a.E; i0 += 32 / lanes) {
-            const int i = i0 + lane / lanes;
+    const int batch = min(a.T, floats / a.E);
+    for (int b0 = 0; b0 < a.T; b0 += batch) {
+        const int nt = min(batch, a.T - b0), pairs = nt * a.E;
+        int lanes = 1;
+        while (lanes < 32 && lanes * 2 * pairs <= 32 * W && lanes * 2 * el <= g) lanes *= 2;
+        const int sub = lane & (lanes - 1), per_round = 32 * W / lanes;
+        for (int p0 = 0; p0 < pairs; p0 += per_round) {   // a round is the same for all lanes: the sums are shuffled
+            const int p = p0 + threadIdx.x / lanes;
+            const int t = p / a.E, i = p - t * a.E;
             float s = 0.0f;
-            if (i < a.E) {
-                const uint16_t* p = row + (size_t)i * g;
-                s = g % 8 == 0 ? sum_pieces<8>(p, g, sub, lanes) : g % 2 == 0 ? sum_pieces<2>(p, g, sub, lanes) : sum_pieces<1>(p, g, sub, lanes);
+            if (p < pairs) {
+                const uint16_t* from = a.x + (size_t)(b0 + t) * a.H + (size_t)i * g;
+                s = el == 8 ? sum_pieces<8>(from, g, sub, lanes) : el == 2 ? sum_pieces<2>(from, g, sub, lanes) : sum_pieces<1>(from, g, sub, lanes);
             }
             for (int o = 1; o < lanes; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (i < a.E && sub == 0) G[i] = fmaxf(fmaf(s, inv_g, a.eps ? a.eps[i] : 0.0f), 0.0f);   // a NaN logit counts as 0
+            if (p < pairs && sub == 0) logits[p] = fmaxf(fmaf(s, inv_g, a.eps ? a.eps[i] : 0.0f), 0.0f);   // a NaN logit counts as 0
         }
-        __syncwarp();
-        float top = 0.0f, z = 0.0f;
-        for (int c = 0; c < a.K; ++c) {
-            float best = -2.0f;
-            int bi = 0x7fffffff;
-            for (int i = lane; i < a.E; i += 32)
-                if (G[i] > best) { best = G[i]; bi = i; }
+        __syncthreads();
+        for (int t = warp; t < nt; t += W) {
+            float* G = logits + t * a.E;
+            float top = 0.0f, z = 0.0f;
+            for (int c = 0; c < a.K; ++c) {
+                float best = -2.0f;
+                int bi = 0x7fffffff;
+                for (int i = lane; i < a.E; i += 32)
+                    if (G[i] > best) { best = G[i]; bi = i; }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {       // the lower index wins a tie
-                const float ob = __shfl_xor_sync(0xffffffffu, best, o);
-                const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
-                if (ob > best || (ob == best && oi < bi)) { best = ob; bi = oi; }
-            }
-            if (c == 0) {
-                top = best;
-                for (int i = lane; i < a.E; i += 32) z += expf(G[i] - top);
+                for (int o = 16; o > 0; o >>= 1) {       // the lower index wins a tie
+                    const float ob = __shfl_xor_sync(0xffffffffu, best, o);
+                    const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
+                    if (ob > best || (ob == best && oi < bi)) { best = ob; bi = oi; }
+                }
+                if (c == 0) {
+                    top = best;
+                    for (int i = lane; i < a.E; i += 32) z += expf(G[i] - top);
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+                    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    G[bi] = -1.0f;                       // below every logit: chosen
+                    expert[c * a.T + b0 + t] = (int16_t)bi;
+                    score[c * a.T + b0 + t] = expf(best - top) / z;
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            if (lane == 0) {
-                G[bi] = -1.0f;                       // below every logit: chosen
-                expert[c * a.T + t] = (int16_t)bi;
-                score[c * a.T + t] = expf(best - top) / z;
-            }
-            __syncwarp();
         }
+        __syncthreads();
     }
 }
 
-// Position in a warp's sequence of tasks: which weight rows and which stages come next.
-struct Cursor {
-    int task, j;                    // j: index of the task's expert in act[]
-    int e, row0, ch, s, rb, step, last;
-};
+struct Task { int row0, rb, s, base, m, step; };
 
 template <class V, bool SECOND>
 __global__ void __launch_bounds__(V::kThreads, V::kCtas)
 moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
-    constexpr int W = V::W, MT = V::MT, NB = V::NB, NBOX = V::NBOX, D = V::D, kThreads = V::kThreads;
+    constexpr int NB = V::NB, MT = V::MT, WK = V::WK, BW = V::BW, R = V::R, GR = V::GR, kThreads = V::kThreads;
     extern __shared__ unsigned char raw[];
     unsigned char* sm = reinterpret_cast<unsigned char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);   // the swizzle repeats every 1024 bytes
     const int TK = a.T * a.K;
-    const Smem L = layout<V>(TK, a.E);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + L.bars);
+    const Smem L = layout<V>(TK, a.E, min(a.T, 16 * MT) * (SECOND ? 2 : 1));
     int16_t* expert = reinterpret_cast<int16_t*>(sm + L.expert);
     int16_t* sorted = reinterpret_cast<int16_t*>(sm + L.sorted);
     float* score = reinterpret_cast<float*>(sm + L.score);
     int16_t* act = reinterpret_cast<int16_t*>(sm + L.act);
     int16_t* first = reinterpret_cast<int16_t*>(sm + L.first);
     int16_t* chunk = reinterpret_cast<int16_t*>(sm + L.chunk);
-    float* strips = reinterpret_cast<float*>(sm + L.ring);
-    int* count = reinterpret_cast<int*>(strips + W * a.E);
+    int* count = reinterpret_cast<int*>(sm + L.ring);
     int* place = count + a.E;
     __shared__ int n_act;
     __shared__ volatile int abort_word;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int N = SECOND ? a.H : a.F, Kd = SECOND ? a.F : a.H;
-    const int RB = (N + 8 * NB - 1) / (8 * NB);
+    const int RB = (N + R - 1) / R;
 
-    // With few assignments the second kernel evaluates the router again, so that it can fill its ring with weights
-    // while the first one is still running; with many it takes the first kernel's choices.
-    const bool early = SECOND && TK <= 8;
-    if (tid < W * D) mbar_init(&full[tid], 1);
-    if (tid == 0) { abort_word = 0; mbar_init_fence(); }
+    // Where both kernels fit an SM together the second one evaluates the router again, so that it can fill its ring with weights
+    // while the first one is still running; else it takes the first kernel's choices.
+    const bool early = SECOND && V::kCtas == 2;
+    if (tid < GR * L.stages) {
+        mbar_init(reinterpret_cast<uint64_t*>(sm + L.full) + tid, 1);
+        mbar_init(reinterpret_cast<uint64_t*>(sm + L.empty) + tid, V::kMulWarps);
+    }
+    if (tid == 0) abort_word = 0;
+    mbar_init_fence();
     if (!SECOND) {
         pdl_wait();
         pdl_trigger();
     }
     if (!SECOND || early) {
-        few_router<W>(a, expert, score, strips);
+        few_router<kThreads / 32>(a, expert, score, reinterpret_cast<float*>(sm + L.ring), L.red / 4);
     } else {
         pdl_wait();
         pdl_trigger();
         for (int i = tid; i < TK; i += kThreads) { expert[i] = (int16_t)a.idx_k[i]; score[i] = a.w_k[i]; }
     }
-    for (int i = tid; i < a.E; i += kThreads) count[i] = 0;
     __syncthreads();
     if (!SECOND && blockIdx.x == 0)
         for (int i = tid; i < TK; i += kThreads) { a.idx_k[i] = expert[i]; a.w_k[i] = score[i]; }
@@ -197,197 +241,236 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
         const int blocks = (a.H + 7) / 8;
         for (int i = blockIdx.x * kThreads + tid; i < blocks; i += gridDim.x * kThreads) a.arrived[i] = 0;
     }
-    for (int i = tid; i < TK; i += kThreads) atomicAdd(&count[expert[i]], 1);
-    __syncthreads();
-    if (warp == 0) {
-        int na = 0, nf = 0, nc = 0;
-        for (int e0 = 0; e0 < a.E; e0 += 32) {
-            const int e = e0 + lane, c = e < a.E ? count[e] : 0, ch = (c + 16 * MT - 1) / (16 * MT);
-            int sf = c, sc = ch;
+    // The assignments sorted by expert, in ascending order within one: an expert's chunks of 16 * MT tokens may fall to
+    // different CTAs, which must agree on what is in them.
+    if (TK <= 32) {   // one assignment a lane, one chunk an expert; every warp does it for itself and writes the same
+        const int e = lane < TK ? expert[lane] : 0x7fff;
+        const unsigned same = __match_any_sync(0xffffffffu, e), below = (1u << lane) - 1u;
+        const unsigned heads = __ballot_sync(0xffffffffu, lane < TK && (same & below) == 0);
+        int less = 0, j = 0;   // assignments and experts met with a lower expert index
+        for (int i = 0; i < TK; ++i) {
+            const int o = __shfl_sync(0xffffffffu, e, i);
+            less += o < e;
+            j += o < e && ((heads >> i) & 1u);
+        }
+        if (lane < TK) {
+            sorted[less + __popc(same & below)] = (int16_t)lane;
+            if ((same & below) == 0) { act[j] = (int16_t)e; first[j] = (int16_t)less; chunk[j] = (int16_t)j; }
+        }
+        if (lane == 0) { n_act = __popc(heads); first[n_act] = (int16_t)TK; chunk[n_act] = (int16_t)n_act; }
+        fence_async_smem();
+        __syncthreads();
+    } else {
+        for (int i = tid; i < a.E; i += kThreads) count[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < TK; i += kThreads) atomicAdd(&count[expert[i]], 1);
+        __syncthreads();
+        if (warp == 0) {
+            int na = 0, nf = 0, nc = 0;
+            for (int e0 = 0; e0 < a.E; e0 += 32) {
+                const int e = e0 + lane, c = e < a.E ? count[e] : 0, ch = (c + 16 * MT - 1) / (16 * MT);
+                int sf = c, sc = ch;
 #pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int uf = __shfl_up_sync(0xffffffffu, sf, o), uc = __shfl_up_sync(0xffffffffu, sc, o);
-                if (lane >= o) { sf += uf; sc += uc; }
+                for (int o = 1; o < 32; o *= 2) {
+                    const int uf = __shfl_up_sync(0xffffffffu, sf, o), uc = __shfl_up_sync(0xffffffffu, sc, o);
+                    if (lane >= o) { sf += uf; sc += uc; }
+                }
+                const unsigned met = __ballot_sync(0xffffffffu, c > 0);
+                if (e < a.E) place[e] = nf + sf - c;
+                if (c > 0) {
+                    const int j = na + __popc(met & ((1u << lane) - 1u));
+                    act[j] = (int16_t)e; first[j] = (int16_t)(nf + sf - c); chunk[j] = (int16_t)(nc + sc - ch);
+                }
+                na += __popc(met);
+                nf += __shfl_sync(0xffffffffu, sf, 31);
+                nc += __shfl_sync(0xffffffffu, sc, 31);
             }
-            const unsigned met = __ballot_sync(0xffffffffu, c > 0);
-            if (e < a.E) place[e] = nf + sf - c;
-            if (c > 0) {
-                const int j = na + __popc(met & ((1u << lane) - 1u));
-                act[j] = (int16_t)e; first[j] = (int16_t)(nf + sf - c); chunk[j] = (int16_t)(nc + sc - ch);
-            }
-            na += __popc(met);
-            nf += __shfl_sync(0xffffffffu, sf, 31);
-            nc += __shfl_sync(0xffffffffu, sc, 31);
-        }
-        if (lane == 0) { n_act = na; first[na] = (int16_t)nf; chunk[na] = (int16_t)nc; }
-        __syncwarp();
-        // assignments sorted by expert, in ascending order within one: an expert's chunks may fall to different CTAs,
-        // which must agree on what is in them
-        for (int i0 = 0; i0 < TK; i0 += 32) {
-            const int i = i0 + lane;
-            const bool in = i < TK;
-            const unsigned have = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const int e = expert[i];
-                const unsigned same = __match_any_sync(have, e);
-                const int at = place[e] + __popc(same & ((1u << lane) - 1u));
-                sorted[at] = (int16_t)i;
-                __syncwarp(have);
-                if ((same >> lane) == 1u) place[e] = at + 1;   // the last of them
-            }
+            if (lane == 0) { n_act = na; first[na] = (int16_t)nf; chunk[na] = (int16_t)nc; }
             __syncwarp();
+            for (int i0 = 0; i0 < TK; i0 += 32) {
+                const int i = i0 + lane;
+                const bool in = i < TK;
+                const unsigned have = __ballot_sync(0xffffffffu, in);
+                if (in) {
+                    const int e = expert[i];
+                    const unsigned same = __match_any_sync(have, e);
+                    const int at = place[e] + __popc(same & ((1u << lane) - 1u));
+                    sorted[at] = (int16_t)i;
+                    __syncwarp(have);
+                    if ((same >> lane) == 1u) place[e] = at + 1;   // the last of them
+                }
+                __syncwarp();
+            }
         }
+        fence_async_smem();
+        __syncthreads();   // the scratch is free: the ring takes its place
     }
-    fence_async_smem();
-    __syncthreads();   // the scratch is free: the ring takes its place
 
     const int steps = (Kd + V::kStepK - 1) / V::kStepK, chunks = chunk[n_act];
     int S = 1;         // slices of the reduction: enough tasks for an even load, at least four stages each
     if (SECOND)
-        while (S < a.max_split && (long long)chunks * RB * S < (long long)V::kTasks * gridDim.x && steps >= 8 * S) S *= 2;
+        while (S < a.max_split && (long long)chunks * RB * S < 8ll * gridDim.x && steps >= 8 * S) S *= 2;
+    const int stages = (steps + S - 1) / S;   // of a task; those beyond K are zeros
     const long long total = (long long)chunks * RB * S;
-    const int t0 = (int)(total * blockIdx.x / gridDim.x) + warp, t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);   // every W-th of these
+    const int t0 = (int)(total * blockIdx.x / gridDim.x), t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
 
-    auto locate = [&](Cursor& c) {
-        while (c.task >= chunk[c.j + 1] * RB * S) ++c.j;
-        int r = c.task - chunk[c.j] * RB * S;
-        const int nch = chunk[c.j + 1] - chunk[c.j];
-        if (nch > 1) { c.ch = r % nch; r /= nch; } else { c.ch = 0; }
-        if (S > 1) { c.rb = r % RB; c.s = r / RB; } else { c.rb = r; c.s = 0; }
-        c.e = act[c.j];
-        c.row0 = c.rb * 8 * NB;
-        c.step = steps * c.s / S;
-        c.last = steps * (c.s + 1) / S;
+    int j = 0;         // tasks come by expert, slice, row block and chunk: the chunks of a row block follow each other
+    auto locate = [&](int task) {
+        while (task >= chunk[j + 1] * RB * S) ++j;
+        int r = task - chunk[j] * RB * S, ch = 0;
+        const int nch = chunk[j + 1] - chunk[j];
+        Task t;
+        if (nch > 1) { ch = r % nch; r /= nch; }
+        t.rb = r; t.s = 0;
+        if (S > 1) { t.rb = r % RB; t.s = r / RB; }
+        t.row0 = t.rb * R;
+        t.base = first[j] + ch * 16 * MT;
+        t.m = min(16 * MT, first[j + 1] - t.base);
+        t.step = t.s * stages;
+        return t;
     };
-    Cursor in{};
-    in.task = t0;
-    if (t0 < t1) locate(in);
-    unsigned char* ring = sm + L.ring + warp * D * V::kStage;
-    int in_slot = 0;
-    auto issue = [&]() {
-        if (in.task < t1) {
-            if (lane == 0 && !abort_word) {
-                uint64_t* bar = &full[warp * D + in_slot];
-                mbar_expect_tx(bar, V::kStage);
-#pragma unroll
-                for (int b = 0; b < NBOX; ++b)   // beyond the matrix a box is filled with zeros
-                    tma_load_2d(ring + in_slot * V::kStage + b * V::kBox, &map, in.step * V::kStepK + b * kBoxK, in.e * N + in.row0, bar);
-            }
-            if (++in.step == in.last && (in.task += W) < t1) locate(in);
-        }
-        if (++in_slot == D) in_slot = 0;
-    };
-#pragma unroll 1
-    for (int d = 0; d < D; ++d) issue();
-
-    if (early) {
-        pdl_wait();
-        pdl_trigger();
-    }
-    const uint16_t* A = SECOND ? a.g : a.x;
+    const uint32_t low = (uint32_t)TK * (uint32_t)Kd;   // from an intermediate row to its low part
+    const int group = warp / (V::kMulWarps + 1), gw = warp - group * (V::kMulWarps + 1);
+    const uint32_t ring = smem_u32(sm + L.ring) + group * L.stages * L.stage;
+    const uint32_t full = smem_u32(sm + L.full) + group * L.stages * 8, empty = smem_u32(sm + L.empty) + group * L.stages * 8;
     int slot = 0;
     uint32_t phase = 0;
-    Cursor c{};
-    for (int task = t0; task < t1; task += W) {
-        c.task = task;
-        locate(c);
-        const int base = first[c.j] + c.ch * 16 * MT, m_here = min(16 * MT, first[c.j + 1] - base);
-        // The second product takes the intermediate as high + low part.  While its tokens fill no more than half of
-        // the tile's rows, the low parts are the other half; beyond that they take products of their own.
-        constexpr int half = 8 * MT;
-        const bool packed = SECOND && m_here <= half, two_pass = SECOND && !packed;
-        const int rows_used = packed ? half + m_here : m_here;
-        const uint32_t low = (uint32_t)TK * (uint32_t)Kd;
-        uint32_t off[2 * MT];   // element offset of the row in A; kNoRow: a row of zeros
+
+    if (gw == V::kMulWarps) {   // ---- producer: a lane a box of weights, a lane a token row ----
+        constexpr int kMine = (32 * MT + 31) / 32;   // token rows of a lane: at most 2 * 16 * MT in all
+        const uint16_t* A = SECOND ? a.g : a.x;
+        const uint16_t* src[kMine];
+        int w_row = 0, rows = 0;
+        auto enter = [&](const Task& t) {   // what stays the same over a task's stages
+            w_row = act[j] * N + t.row0;
+            rows = SECOND ? 2 * t.m : t.m;
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-            const int m = i * 8 + gq;
-            const bool lower = packed && i >= MT;
-            const int mm = lower ? m - half : m;
-            const int as = mm < m_here ? sorted[base + mm] : -1;
-            off[i] = as < 0 ? kNoRow : (uint32_t)(SECOND ? as : as % a.T) * (uint32_t)Kd + (lower ? low : 0u);
+            for (int q = 0; q < kMine; ++q) {
+                const int i = lane + 32 * q;
+                if (i < rows) {
+                    const bool lower = i >= t.m;
+                    const int as = sorted[t.base + (lower ? i - t.m : i)];
+                    src[q] = A + (size_t)(SECOND ? as : as % a.T) * Kd + (lower ? low : 0u) + t.step * V::kStepK;
+                }
+            }
+        };
+        auto weights = [&](int k, uint32_t dst, uint32_t bar) {
+            if (lane == 0) mbar_expect_tx(bar, V::kWeights + rows * 2 * max(0, min(V::kStepK, Kd - k)));
+            __syncwarp();
+            if (lane < V::kBoxes) tma_load_2d(dst + lane * V::kBox, &map, k + lane * kBoxK, w_row, bar);   // beyond the matrix: zeros
+        };
+        auto tokens = [&](int k, uint32_t dst, uint32_t bar) {
+#pragma unroll
+            for (int q = 0; q < kMine; ++q) {
+                const int i = lane + 32 * q;
+                if (i < rows && k < Kd) bulk_row(dst + V::kWeights + i * V::kPitch, src[q], 2 * min(V::kStepK, Kd - k), bar);
+                src[q] += V::kStepK;
+            }
+        };
+        int ahead = 0;   // stages whose weights have been asked for
+        if (early) {     // the weights of the whole ring, then the first kernel's results
+            for (int task = t0 + group; task < t1 && ahead < L.stages; task += GR) {
+                const Task t = locate(task);
+                w_row = act[j] * N + t.row0;
+                rows = 2 * t.m;
+                for (int i = 0; i < stages && ahead < L.stages; ++i, ++ahead)
+                    weights((t.step + i) * V::kStepK, ring + ahead * L.stage, full + ahead * 8);
+            }
+            pdl_wait();
+            pdl_trigger();
+            j = 0;
         }
-        constexpr int P = 2 * NBOX;   // 16-byte pieces of a row that one thread holds of a stage
-        float acc[MT][NB][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+        if (SECOND) asm volatile("fence.proxy.async;" ::: "memory");   // the first kernel's stores, read by copies here
+        bool alive = true;
+        for (int task = t0 + group; task < t1 && alive; task += GR) {
+            const Task t = locate(task);
+            enter(t);
+            int k = t.step * V::kStepK;
 #pragma unroll 1
-        for (; c.step < c.last; ++c.step) {
-            const int k0 = c.step * V::kStepK + tq * 16;
-            uint4 av[P][2 * MT], al[SECOND && NB > 1 ? P : 1][2 * MT];
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int k = k0 + (p >> 1) * kBoxK + (p & 1) * 8;
-#pragma unroll
-                for (int i = 0; i < 2 * MT; ++i) {
-                    av[p][i] = make_uint4(0, 0, 0, 0);
-                    if (off[i] != kNoRow && k < Kd) av[p][i] = *reinterpret_cast<const uint4*>(A + off[i] + k);
-                }
+            for (int i = 0; i < stages; ++i, k += V::kStepK) {
+                if (!wait_or_abort(empty + slot * 8, phase ^ 1u, &abort_word)) { alive = false; break; }
+                const uint32_t dst = ring + slot * L.stage, bar = full + slot * 8;
+                if (ahead > 0) --ahead;
+                else weights(k, dst, bar);
+                tokens(k, dst, bar);
+                if (++slot == L.stages) { slot = 0; phase ^= 1u; }
             }
-            if constexpr (SECOND && NB > 1) {   // at most 8 assignments (NB = 1) are always packed
-                if (two_pass) {
+        }
+    } else {                    // ---- the other warps of the group multiply ----
+        if (early) {
+            pdl_wait();
+            pdl_trigger();
+        }
+        const int gt = gw * 32 + lane, gq = lane >> 2, tq = lane & 3, wk = gw % WK, wr = gw / WK;
+        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(V::kMulWarps * 32) : "memory"); };
+        // this thread's bytes of a stage: weight row gq of each block, 16-byte pieces 2 tq and 2 tq + 1
+        const uint32_t wrow = wk * BW * V::kBox + (wr * 8 * NB + gq) * 128, even = wrow + ((2 * tq) ^ gq) * 16, odd = wrow + ((2 * tq + 1) ^ gq) * 16;
+        const bool direct = SECOND && S == 1 && a.K == 1;
+        bool alive = true;
+        for (int task = t0 + group; task < t1; task += GR) {
+            const Task t = locate(task);
+            // The second product takes the intermediate as high + low part.  While its tokens fill no more than half
+            // of the tile's rows, the low parts are the other half; beyond that they take products of their own.
+            constexpr int half = 8 * MT;
+            const bool packed = SECOND && t.m <= half, two_pass = SECOND && !packed;
+            const int rows_used = packed ? half + t.m : t.m;
+            // Rows of the tile beyond the tokens repeat a token: a row enters no other row's results.
+            uint32_t at[2 * MT];
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        const int k = k0 + (p >> 1) * kBoxK + (p & 1) * 8;
-#pragma unroll
-                        for (int i = 0; i < 2 * MT; ++i) {
-                            al[p][i] = make_uint4(0, 0, 0, 0);
-                            if (off[i] != kNoRow && k < Kd) al[p][i] = *reinterpret_cast<const uint4*>(A + off[i] + low + k);
-                        }
-                    }
-                }
+            for (int i = 0; i < 2 * MT; ++i) {
+                const bool lower = packed && i >= MT;
+                const int row = min((lower ? i - MT : i) * 8 + gq, t.m - 1) + (lower ? t.m : 0);
+                at[i] = V::kWeights + row * V::kPitch + wk * BW * 128 + tq * 32;
             }
-            if (!abort_word && !mbar_wait_bounded(&full[warp * D + slot], phase)) {
-                abort_word = 1;
-                atomicOr(&g_few_flags, 1);
-            }
+            float acc[MT][NB][4];
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                uint4 wv[NB];
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
-                    wv[n] = *reinterpret_cast<const uint4*>(ring + slot * V::kStage + (p >> 1) * V::kBox + (n * 8 + gq) * 128 +
-                                                            (((2 * tq + (p & 1)) ^ gq) * 16));
-                auto products = [&](const uint4 (&v)[2 * MT]) {
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        if (m > 0 && m * 16 >= rows_used) break;
+                    for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+            int left = Kd - t.step * V::kStepK - wk * BW * kBoxK - tq * 16;   // from this thread's first k to the end of the rows
+#pragma unroll 1
+            for (int i = 0; i < stages; ++i) {
+                if (alive) alive = wait_or_abort(full + slot * 8, phase, &abort_word);
+                const uint32_t stage = ring + slot * L.stage;
 #pragma unroll
-                        for (int n = 0; n < NB; ++n) mma16816(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, wv[n].x, wv[n].y);
+                for (int p = 0; p < 2 * BW; ++p) {
+                    uint4 wv[NB], av[2 * MT];
 #pragma unroll
-                        for (int n = 0; n < NB; ++n) mma16816(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, wv[n].z, wv[n].w);
+                    for (int n = 0; n < NB; ++n) wv[n] = ld_shared(stage + (p >> 1) * V::kBox + n * 1024 + ((p & 1) ? odd : even));
+                    auto tokens = [&](uint32_t more) {   // beyond K zeros: the weights' zeros alone would keep a NaN
+#pragma unroll
+                        for (int q = 0; q < 2 * MT; ++q) {
+                            av[q] = ld_shared(stage + at[q] + more + (p >> 1) * 128 + (p & 1) * 16);
+                            if ((p >> 1) * kBoxK + (p & 1) * 8 >= left) av[q] = make_uint4(0, 0, 0, 0);
+                        }
+                    };
+                    auto products = [&]() {
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            if (m > 0 && m * 16 >= rows_used) break;
+#pragma unroll
+                            for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].x, av[2 * m + 1].x, av[2 * m].y, av[2 * m + 1].y, wv[n].x, wv[n].y);
+#pragma unroll
+                            for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].z, av[2 * m + 1].z, av[2 * m].w, av[2 * m + 1].w, wv[n].z, wv[n].w);
+                        }
+                    };
+                    tokens(0);
+                    products();
+                    if (two_pass) {
+                        tokens(t.m * V::kPitch);
+                        products();
                     }
-                };
-                products(av[p]);
-                if constexpr (SECOND && NB > 1) {
-                    if (two_pass) products(al[p]);
                 }
+                __syncwarp();   // the stage has been read by the whole warp
+                if (lane == 0) mbar_arrive(empty + slot * 8);
+                left -= V::kStepK;
+                if (++slot == L.stages) { slot = 0; phase ^= 1u; }
             }
-            __syncwarp();   // the stage has been read by the whole warp
-            issue();
-            if (++slot == D) { slot = 0; phase ^= 1u; }
-        }
-        // Results straight from the accumulators: thread (gq, tq) has weight rows 2 tq and 2 tq + 1 of each block and
-        // the tokens gq of each group of eight; the low parts' shares lie in the same thread.
-        const bool direct = SECOND && S == 1 && a.K == 1;
-#pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-            const int m = i * 8 + gq;
-            if (m >= m_here) continue;
-            const int as = sorted[base + m];
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const int row = c.row0 + n * 8 + tq * 2;
-                if (row >= N) continue;
-                float2 v = make_float2(acc[i >> 1][n][(i & 1) * 2], acc[i >> 1][n][(i & 1) * 2 + 1]);
-                if (packed && i < MT) {
-                    v.x += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2];
-                    v.y += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2 + 1];
-                }
+            // A result pair: weight rows `row` and `row` + 1 of token m of the chunk.
+            auto emit = [&](int m, int row, float2 v) {
+                const int as = sorted[t.base + m];
                 if (!SECOND) {
                     v.x = 0.5f * v.x * erfcf(-0.70710678118654752f * v.x);
                     v.y = 0.5f * v.y * erfcf(-0.70710678118654752f * v.y);
@@ -399,38 +482,83 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a) {
                     const float f = a.weighted ? score[as] : 1.0f;
                     *reinterpret_cast<uint32_t*>(a.out + (size_t)as * a.H + row) = cvt_bf16x2(make_float2(v.x * f, v.y * f));
                 } else {
-                    *reinterpret_cast<float2*>(a.part + ((size_t)c.s * TK + as) * a.H + row) = v;
+                    *reinterpret_cast<float2*>(a.part + ((size_t)t.s * TK + as) * a.H + row) = v;
                 }
-            }
-        }
-        if (SECOND && !direct) {   // the last task of these columns to arrive adds them all up, in a fixed order
-            __threadfence();
-            __syncwarp();
-            int last = 0;
-            if (lane == 0) last = atomicAdd(&a.arrived[c.rb], 1) == chunks * S - 1;
-            if (__shfl_sync(0xffffffffu, last, 0)) {
-                __threadfence();
-                constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
-                const int row = c.row0 + (lane % Q) * 4;
-                if (row < N) {
-                    for (int t = lane / Q; t < a.T; t += 32 / Q) {
-                        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int k = 0; k < a.K; ++k) {
-                            const float* p = a.part + ((size_t)k * a.T + t) * a.H + row;
-                            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-                            for (int s = 0; s < S; ++s) {
-                                const float4 z = __ldcg(reinterpret_cast<const float4*>(p + (size_t)s * TK * a.H));
-                                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-                            }
-                            const float f = a.weighted ? score[k * a.T + t] : 1.0f;
-                            v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+            };
+            if constexpr (WK > 1) {   // the shares of the warps along k, added in warp order; then the low parts' rows
+                float* red = reinterpret_cast<float*>(sm + L.red) + group * V::kRed;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        float* r = red + ((wk * 16 * MT) + m * 16 + gq) * R + (wr * NB + n) * 8 + tq * 2;
+                        *reinterpret_cast<float2*>(r) = make_float2(acc[m][n][0], acc[m][n][1]);
+                        *reinterpret_cast<float2*>(r + 8 * R) = make_float2(acc[m][n][2], acc[m][n][3]);
+                    }
+                group_sync();
+                for (int o = gt; o < t.m * (R / 2); o += V::kMulWarps * 32) {
+                    const int m = o / (R / 2), r = o % (R / 2) * 2;
+                    if (t.row0 + r >= N) continue;
+                    float2 v = make_float2(0.0f, 0.0f), l = v;
+#pragma unroll
+                    for (int w = 0; w < WK; ++w) {
+                        const float2 z = *reinterpret_cast<const float2*>(red + (w * 16 * MT + m) * R + r);
+                        v.x += z.x; v.y += z.y;
+                        if (packed) {
+                            const float2 y = *reinterpret_cast<const float2*>(red + (w * 16 * MT + half + m) * R + r);
+                            l.x += y.x; l.y += y.y;
                         }
-                        *reinterpret_cast<uint2*>(a.out + (size_t)t * a.H + row) =
-                            make_uint2(cvt_bf16x2(make_float2(v.x, v.y)), cvt_bf16x2(make_float2(v.z, v.w)));
+                    }
+                    emit(m, t.row0 + r, make_float2(v.x + l.x, v.y + l.y));
+                }
+                group_sync();   // also: the strip may be written again
+            } else {          // thread (gq, tq) has the tokens gq of each eight and weight rows 2 tq, 2 tq + 1 of each block
+#pragma unroll
+                for (int i = 0; i < 2 * MT; ++i) {
+                    const int m = i * 8 + gq;
+                    if (m >= t.m) continue;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        const int row = t.row0 + (wr * NB + n) * 8 + tq * 2;
+                        if (row >= N) continue;
+                        float2 v = make_float2(acc[i >> 1][n][(i & 1) * 2], acc[i >> 1][n][(i & 1) * 2 + 1]);
+                        if (packed && i < MT) {
+                            v.x += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2];
+                            v.y += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2 + 1];
+                        }
+                        emit(m, row, v);
                     }
                 }
+            }
+            if (SECOND && !direct && wk == 0) {   // the last task to arrive at a warp's columns adds them all up, in a fixed order
+                __threadfence();
                 __syncwarp();
+                int last = 0;
+                if (lane == 0) last = atomicAdd(&a.arrived[t.rb * V::WR + wr], 1) == chunks * S - 1;
+                if (__shfl_sync(0xffffffffu, last, 0)) {
+                    __threadfence();
+                    constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
+                    const int row = t.row0 + wr * 8 * NB + (lane % Q) * 4;
+                    if (row < N) {
+                        for (int tok = lane / Q; tok < a.T; tok += 32 / Q) {
+                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            for (int k = 0; k < a.K; ++k) {
+                                const float* p = a.part + ((size_t)k * a.T + tok) * a.H + row;
+                                float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+                                for (int s = 0; s < S; ++s) {
+                                    const float4 z = __ldcg(reinterpret_cast<const float4*>(p + (size_t)s * TK * a.H));
+                                    y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                                }
+                                const float f = a.weighted ? score[k * a.T + tok] : 1.0f;
+                                v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+                            }
+                            *reinterpret_cast<uint2*>(a.out + (size_t)tok * a.H + row) =
+                                make_uint2(cvt_bf16x2(make_float2(v.x, v.y)), cvt_bf16x2(make_float2(v.z, v.w)));
+                        }
+                    }
+                    __syncwarp();
+                }
             }
         }
     }
@@ -458,26 +586,26 @@ FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
 
 template <class V>
 int run_few(const FewArgs& a, cudaStream_t st) {
-    const Smem L = layout<V>(a.T * a.K, a.E);
     static bool done_dev[64] = {false};   // the attribute is per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!done_dev[dev & 63]) {
-        const int most = layout<V>(kMaxTokens * kMaxK, kMaxExperts).total;
-        if (cudaFuncSetAttribute(moe_few_kernel<V, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
-            cudaFuncSetAttribute(moe_few_kernel<V, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
+        if (cudaFuncSetAttribute(moe_few_kernel<V, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(moe_few_kernel<V, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) {
             cudaGetLastError();
             return LOCMOE_ERR_CUDA;
         }
         done_dev[dev & 63] = true;
     }
+    const int rows = a.T < 16 * V::MT ? a.T : 16 * V::MT;
+    const Smem L1 = layout<V>(a.T * a.K, a.E, rows), L2 = layout<V>(a.T * a.K, a.E, 2 * rows);
     CUtensorMap m1, m2;
     const uint64_t d1[2] = {(uint64_t)a.H, (uint64_t)a.E * a.F}, d2[2] = {(uint64_t)a.F, (uint64_t)a.E * a.H};
-    if (!make_map(&m1, a.w_in, 2, d1, 8 * V::NB) || !make_map(&m2, a.w_out, 2, d2, 8 * V::NB)) return LOCMOE_ERR_CUDA;
+    if (!make_map(&m1, a.w_in, 2, d1, V::R) || !make_map(&m2, a.w_out, 2, d2, V::R)) return LOCMOE_ERR_CUDA;
     const dim3 grid(sm_count());
-    const int rc = launch_pdl(moe_few_kernel<V, false>, grid, dim3(V::kThreads), L.total, st, m1, a);
+    const int rc = launch_pdl(moe_few_kernel<V, false>, grid, dim3(V::kThreads), L1.total, st, m1, a);
     if (rc) return rc;
-    return launch_pdl(moe_few_kernel<V, true>, grid, dim3(V::kThreads), L.total, st, m2, a);
+    return launch_pdl(moe_few_kernel<V, true>, grid, dim3(V::kThreads), L2.total, st, m2, a);
 }
 
 }  // namespace
@@ -492,9 +620,10 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
                     w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
                     reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
                     p.max_split, weighted};
-    if (s.T * K <= 8) return run_few<Variant<16, 1, 1, 2, 3, 8, 2>>(a, st);
-    if (s.T <= 16) return run_few<Variant<12, 1, 2, 2, 4, 48, 1>>(a, st);
-    return run_few<Variant<12, 2, 4, 1, 4, 48, 1>>(a, st);
+    if (s.T * K <= 2) return run_few<Variant<2, 1, 4, 1, 2, 1, 100 << 10, 2>>(a, st);
+    if (s.T * K <= 8) return run_few<Variant<3, 1, 4, 2, 1, 1, 220 << 10, 1>>(a, st);
+    if (s.T <= 16) return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10, 1>>(a, st);
+    return run_few<Variant<3, 4, 1, 4, 1, 2, 220 << 10, 1>>(a, st);
 }
 
 int read_few_flags(int* out, cudaStream_t st) {
