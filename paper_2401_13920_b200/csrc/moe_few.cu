@@ -1,5 +1,5 @@
-// A whole MoE layer for a few tokens (decoding), in two kernels: the router, then both products of the experts and the
-// gate-weighted sum.
+// A whole MoE layer for a few tokens (decoding): the router and the first product of the experts, then the second
+// product and the gate-weighted sum.  Two launches up to 8 tokens; beyond that the router has one of its own.
 //
 //   G_i = ReLU(mean_i x + eps_i),  p = softmax(G),  the K largest;   out_t = sum_c p_{t,c} W_out[e] GeLU(W_in[e] x_t)
 //
@@ -9,8 +9,8 @@
 // tokens' pieces of the same k (bulk copies, one a row) without a pause between tasks; the other warps multiply.
 // The tokens travel with the weights because a load that a multiplying warp issues itself queues behind the ring's
 // own (4000 cycles at a full ring: 2.9 against 6.5 TB/s on a stream of rows of 10240).
-// Between the products all CTAs (one an SM, launched as a cooperative grid) count in; only the second product's token
-// rows wait for that, its weights are already on their way.
+// Both launches are programmatic: the CTAs of one take the SMs over as those of the one before leave them.  (One
+// cooperative kernel with a wait of the grid in between is no faster: its launch does not overlap anything.)
 // The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
 // expert nothing is gained by larger matrix instructions.  The order of k inside a stage is chosen so that a thread's
 // fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides), which the weight
@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
 constexpr int kMostSmem = 226 << 10;   // of the 227 KB that a CTA can have
+constexpr int kInlineTokens = 8;         // up to here every CTA routes all tokens itself
 constexpr int kBoxK = 64;          // k of one TMA box: 128 bytes of a row
 
 __device__ int g_few_flags = 0;    // bit 0: a bounded wait gave up
@@ -34,8 +35,7 @@ struct FewArgs {
     uint16_t* g;        // [2][K * T][F] GeLU(W_in x) as the sum of two bf16 values: the rounded value and what rounding left
     float* part;        // [S][K * T][H] slices of the second product
     int32_t* arrived;   // [H / 8] tasks of the second product that have left their slice, by column block
-    int32_t* done;      // [1] CTAs that have finished the first product
-    int T, H, E, K, F, max_split, weighted;
+    int T, H, E, K, F, max_split, weighted, inline_router;
 };
 
 // A variant: GR groups, each with a ring, a producer warp and multiplying warps, WR along the weight rows and WK along
@@ -119,12 +119,6 @@ __device__ __forceinline__ int add_acq_rel(int* p) {
     asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(p) : "memory");
     return old;
 }
-__device__ __forceinline__ int add_acq_rel_cta(int* p) {   // shared memory
-    int old;
-    asm volatile("atom.acq_rel.cta.shared.add.s32 %0, [%1], 1;" : "=r"(old) : "r"(smem_u32(p)) : "memory");
-    return old;
-}
-__device__ __forceinline__ void add_release(int* p) { asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -143,82 +137,81 @@ __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, vol
     atomicOr(&g_few_flags, 1);
     return false;
 }
-// Waits (bounded) until `target` CTAs have counted in.
-__device__ __forceinline__ bool wait_count(const int* p, int target, volatile int* abort_word) {
-    for (uint32_t i = 0; i < (1u << 20); ++i) {   // about a second
-        int v;
-        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-        if (v >= target) return true;
-        if ((i & 63u) == 63u && *abort_word) return false;
-        if (i > 64) __nanosleep(20);
-    }
-    *abort_word = 1;
-    atomicOr(&g_few_flags, 1);
-    return false;
-}
-
-// Router: a CTA a token.  Several lanes share an expert's group while there are threads for that; then a warp takes
-// the softmax and the K largest.  It also clears the counters of the kernel that follows.
-constexpr int kRouterThreads = 256;
-__global__ void __launch_bounds__(kRouterThreads) few_router_kernel(const FewArgs a) {
-    __shared__ float G[kMaxExperts];
-    pdl_wait();
-    pdl_trigger();
-    const int t = blockIdx.x, lane = threadIdx.x & 31;
-    for (int i = blockIdx.x * kRouterThreads + threadIdx.x; i < (a.H + 7) / 8; i += gridDim.x * kRouterThreads) a.arrived[i] = 0;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
-    const int g = a.H / a.E, el = g % 8 == 0 ? 8 : g % 2 == 0 ? 2 : 1;
+// Router for `nt` tokens from `b0` on, by a CTA of W warps; G: room for their logits.  The threads share out the (token,
+// expert) pairs, several lanes a pair while there are threads for that; then a warp a token takes the softmax and the
+// K largest and hands each choice to `put(c, t, expert, score)`.
+template <int W, typename Put>
+__device__ __forceinline__ void route_tokens(const FewArgs& a, int b0, int nt, float* logits, Put put) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = a.H / a.E, el = g % 8 == 0 ? 8 : g % 2 == 0 ? 2 : 1, pairs = nt * a.E;
     const float inv_g = 1.0f / (float)g;
     int lanes = 1;
-    while (lanes < 32 && lanes * 2 * a.E <= kRouterThreads && lanes * 2 * el <= g) lanes *= 2;
+    while (lanes < 32 && lanes * 2 * pairs <= 32 * W && lanes * 2 * el <= g) lanes *= 2;
     const int sub = lane & (lanes - 1);
-    for (int i0 = 0; i0 < a.E; i0 += kRouterThreads / lanes) {   // a round is the same for all lanes: the sums are shuffled
-        const int i = i0 + threadIdx.x / lanes;
+    for (int p0 = 0; p0 < pairs; p0 += 32 * W / lanes) {   // a round is the same for all lanes: the sums are shuffled
+        const int p = p0 + threadIdx.x / lanes;
+        const int t = p / a.E, i = p - t * a.E;
         float s = 0.0f;
-        if (i < a.E) {
-            const uint16_t* from = a.x + (size_t)t * a.H + (size_t)i * g;
+        if (p < pairs) {
+            const uint16_t* from = a.x + (size_t)(b0 + t) * a.H + (size_t)i * g;
             s = el == 8 ? sum_pieces<8>(from, g, sub, lanes) : el == 2 ? sum_pieces<2>(from, g, sub, lanes) : sum_pieces<1>(from, g, sub, lanes);
         }
         for (int o = 1; o < lanes; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (i < a.E && sub == 0) G[i] = fmaxf(fmaf(s, inv_g, a.eps ? a.eps[i] : 0.0f), 0.0f);   // a NaN logit counts as 0
+        if (p < pairs && sub == 0) logits[p] = fmaxf(fmaf(s, inv_g, a.eps ? a.eps[i] : 0.0f), 0.0f);   // a NaN logit counts as 0
     }
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    float top = 0.0f, z = 0.0f;
-    for (int c = 0; c < a.K; ++c) {
-        float best = -2.0f;
-        int bi = 0x7fffffff;
-        for (int i = lane; i < a.E; i += 32)
-            if (G[i] > best) { best = G[i]; bi = i; }
+    for (int t = warp; t < nt; t += W) {
+        float* G = logits + t * a.E;
+        float top = 0.0f, z = 0.0f;
+        for (int c = 0; c < a.K; ++c) {
+            float best = -2.0f;
+            int bi = 0x7fffffff;
+            for (int i = lane; i < a.E; i += 32)
+                if (G[i] > best) { best = G[i]; bi = i; }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {       // the lower index wins a tie
-            const float ob = __shfl_xor_sync(0xffffffffu, best, o);
-            const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
-            if (ob > best || (ob == best && oi < bi)) { best = ob; bi = oi; }
-        }
-        if (c == 0) {
-            top = best;
-            for (int i = lane; i < a.E; i += 32) z += expf(G[i] - top);
+            for (int o = 16; o > 0; o >>= 1) {       // the lower index wins a tie
+                const float ob = __shfl_xor_sync(0xffffffffu, best, o);
+                const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
+                if (ob > best || (ob == best && oi < bi)) { best = ob; bi = oi; }
+            }
+            if (c == 0) {
+                top = best;
+                for (int i = lane; i < a.E; i += 32) z += expf(G[i] - top);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+                for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            }
+            __syncwarp();
+            if (lane == 0) {
+                G[bi] = -1.0f;                       // below every logit: chosen
+                put(c, b0 + t, bi, expf(best - top) / z);
+            }
+            __syncwarp();
         }
-        __syncwarp();
-        if (lane == 0) {
-            G[bi] = -1.0f;                       // below every logit: chosen
-            a.idx_k[c * a.T + t] = bi;
-            a.w_k[c * a.T + t] = expf(best - top) / z;
-        }
-        __syncwarp();
     }
+}
+
+constexpr int kRouterThreads = 256;
+__global__ void __launch_bounds__(kRouterThreads) few_router_kernel(const FewArgs a) {   // a CTA a token
+    __shared__ float G[kMaxExperts];
+    pdl_wait();
+    pdl_trigger();
+    route_tokens<kRouterThreads / 32>(a, blockIdx.x, 1, G, [&](int c, int t, int e, float w) {
+        a.idx_k[c * a.T + t] = e;
+        a.w_k[c * a.T + t] = w;
+    });
 }
 
 // What one product is about: weight rows, reduction length, and how its tasks are cut.
 struct Product { int N, Kd, RB, S, stages, t0, t1; };
+__device__ __forceinline__ int token_of(int as, int T) {   // as mod T, for as < 8 T
+    while (as >= T) as -= T;
+    return as;
+}
 struct Task { int row0, rb, s, base, m, step; };
 
 template <class V>
 __global__ void __launch_bounds__(V::kThreads, 1)
-moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out, const FewArgs a) {
+moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a, const int second) {
     constexpr int NB = V::NB, MT = V::MT, WK = V::WK, BW = V::BW, R = V::R, GR = V::GR, kThreads = V::kThreads;
     extern __shared__ unsigned char raw[];
     unsigned char* sm = reinterpret_cast<unsigned char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);   // the swizzle repeats every 1024 bytes
@@ -232,7 +225,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
     int16_t* chunk = reinterpret_cast<int16_t*>(sm + L.chunk);
     int* count = reinterpret_cast<int*>(sm + L.ring);
     int* place = count + a.E;
-    __shared__ int n_act, groups_done;
+    __shared__ int n_act;
     __shared__ volatile int abort_word;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -240,15 +233,29 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
         mbar_init(reinterpret_cast<uint64_t*>(sm + L.full) + tid, 1);
         mbar_init(reinterpret_cast<uint64_t*>(sm + L.empty) + tid, V::kMulWarps);
     }
-    if (tid == 0) { abort_word = 0; groups_done = 0; }
+    if (tid == 0) abort_word = 0;
     mbar_init_fence();
+    if (tid == 0) prefetch_map(&map);
     pdl_wait();
     pdl_trigger();
+    if (!second) {
+        for (int i = blockIdx.x * kThreads + tid; i < (a.H + 7) / 8; i += gridDim.x * kThreads) a.arrived[i] = 0;
+    }
+    // A handful of tokens every CTA routes for itself: their rows out of L2 cost less than a launch of their own.
+    if (a.inline_router && !second) {
+        route_tokens<kThreads / 32>(a, 0, a.T, reinterpret_cast<float*>(sm + L.ring), [&](int c, int t, int e, float w) {
+            expert[c * a.T + t] = (int16_t)e;
+            score[c * a.T + t] = w;
+            if (blockIdx.x == 0) { a.idx_k[c * a.T + t] = e; a.w_k[c * a.T + t] = w; }
+        });
+    } else {
+        for (int i = tid; i < TK; i += kThreads) { expert[i] = (int16_t)a.idx_k[i]; score[i] = a.w_k[i]; }
+    }
+    __syncthreads();
     // The assignments sorted by expert, in ascending order within one: an expert's chunks of 16 * MT tokens may fall to
     // different CTAs, which must agree on what is in them.
     if (TK <= 32) {   // one assignment a lane, one chunk an expert; every warp does it for itself and writes the same
-        const int e = lane < TK ? a.idx_k[lane] : 0x7fff;
-        if (tid < TK) score[tid] = a.w_k[tid];
+        const int e = lane < TK ? expert[lane] : 0x7fff;
         const unsigned same = __match_any_sync(0xffffffffu, e), below = (1u << lane) - 1u;
         const unsigned heads = __ballot_sync(0xffffffffu, lane < TK && (same & below) == 0);
         int less = 0, j = 0;   // assignments and experts met with a lower expert index
@@ -265,7 +272,6 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
         fence_async_smem();
         __syncthreads();
     } else {
-        for (int i = tid; i < TK; i += kThreads) { expert[i] = (int16_t)a.idx_k[i]; score[i] = a.w_k[i]; }
         for (int i = tid; i < a.E; i += kThreads) count[i] = 0;
         __syncthreads();
         for (int i = tid; i < TK; i += kThreads) atomicAdd(&count[expert[i]], 1);
@@ -312,23 +318,21 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
     }
 
     const int chunks = chunk[n_act];
-    auto product = [&](bool second) {
-        Product p;
-        p.N = second ? a.H : a.F;
-        p.Kd = second ? a.F : a.H;
-        p.RB = (p.N + R - 1) / R;
-        const int steps = (p.Kd + V::kStepK - 1) / V::kStepK;
-        p.S = 1;            // slices of the reduction: enough tasks for an even load, at least four stages each
-        if (second)
-            while (p.S < a.max_split && chunks * p.RB * p.S < 8 * (int)gridDim.x && steps >= 8 * p.S) p.S *= 2;
-        p.stages = (steps + p.S - 1) / p.S;   // of a task; those beyond K are zeros
-        const long long total = (long long)chunks * p.RB * p.S;
-        p.t0 = (int)(total * blockIdx.x / gridDim.x);
-        p.t1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
-        return p;
-    };
+    Product p;
+    p.N = second ? a.H : a.F;
+    p.Kd = second ? a.F : a.H;
+    p.RB = (p.N + R - 1) / R;
+    const int steps = (p.Kd + V::kStepK - 1) / V::kStepK;
+    p.S = 1;                // slices of the reduction: enough tasks for an even load, at least four stages each
+    if (second)
+        while (p.S < a.max_split && chunks * p.RB * p.S < 8 * (int)gridDim.x && steps >= 8 * p.S) p.S *= 2;
+    p.stages = (steps + p.S - 1) / p.S;   // of a task; those beyond K are zeros
+    const int total = chunks * p.RB * p.S, share = total / (int)gridDim.x, more = total - share * (int)gridDim.x;
+    p.t0 = blockIdx.x * share + min((int)blockIdx.x, more);
+    p.t1 = p.t0 + share + ((int)blockIdx.x < more ? 1 : 0);
+
     int j = 0;              // tasks come by expert, slice, row block and chunk: the chunks of a row block follow each other
-    auto locate = [&](const Product& p, int task) {
+    auto locate = [&](int task) {
         while (task >= chunk[j + 1] * p.RB * p.S) ++j;
         int r = task - chunk[j] * p.RB * p.S, ch = 0;
         const int nch = chunk[j + 1] - chunk[j];
@@ -352,77 +356,41 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
         if (++slot == L.stages) { slot = 0; phase ^= 1u; }
     };
 
+    if (second) asm volatile("fence.proxy.async;" ::: "memory");   // the first product's stores, read by bulk copies here
     if (gw == V::kMulWarps) {   // ---- producer: a lane a box of weights, a lane a token row ----
         constexpr int kMine = (32 * MT + 31) / 32;   // token rows of a lane: at most 2 * 16 * MT in all
         const uint16_t* src[kMine];
         int w_row = 0, rows = 0;
-#pragma unroll 1
-        for (int ph = 0; ph < 2; ++ph) {
-            const bool second = ph != 0;
-            const Product p = product(second);
-            const CUtensorMap* map = second ? &map_out : &map_in;
-            const uint16_t* A = second ? a.g : a.x;
-            auto enter = [&](const Task& t) {   // what stays the same over a task's stages
-                w_row = act[j] * p.N + t.row0;
-                rows = second ? 2 * t.m : t.m;
+        auto enter = [&](const Task& t) {   // what stays the same over a task's stages
+            w_row = act[j] * p.N + t.row0;
+            rows = second ? 2 * t.m : t.m;
 #pragma unroll
-                for (int q = 0; q < kMine; ++q) {
-                    const int i = lane + 32 * q;
-                    if (i < rows) {
-                        const bool lower = i >= t.m;
-                        const int as = sorted[t.base + (lower ? i - t.m : i)];
-                        src[q] = A + (size_t)(second ? as + (lower ? TK : 0) : as % a.T) * p.Kd + t.step * V::kStepK;
-                    }
+            for (int q = 0; q < kMine; ++q) {
+                const int i = lane + 32 * q;
+                if (i < rows) {
+                    const bool lower = i >= t.m;
+                    const int as = sorted[t.base + (lower ? i - t.m : i)];
+                    src[q] = (second ? a.g + (size_t)(as + (lower ? TK : 0)) * p.Kd : a.x + (size_t)token_of(as, a.T) * p.Kd) + t.step * V::kStepK;
                 }
-            };
-            auto weights = [&](int k) {
-                const uint32_t dst = ring + slot * L.stage, bar = full + slot * 8;
-                if (lane == 0) mbar_expect_tx(bar, V::kWeights + rows * 2 * max(0, min(V::kStepK, p.Kd - k)));
+            }
+        };
+        for (int task = p.t0 + group; task < p.t1 && alive; task += GR) {
+            const Task t = locate(task);
+            enter(t);
+            int k = t.step * V::kStepK;
+#pragma unroll 1
+            for (int i = 0; i < p.stages; ++i, k += V::kStepK) {
+                if (!wait_or_abort(empty + slot * 8, phase ^ 1u, &abort_word)) { alive = false; break; }
+                const uint32_t dst = ring + slot * L.stage, bar = full + slot * 8, bytes = 2 * max(0, min(V::kStepK, p.Kd - k));
+                if (lane == 0) mbar_expect_tx(bar, V::kWeights + rows * bytes);
                 __syncwarp();
-                if (lane < V::kBoxes) tma_load_2d(dst + lane * V::kBox, map, k + lane * kBoxK, w_row, bar);   // beyond the matrix: zeros
-            };
-            auto tokens = [&](int k) {
-                const uint32_t dst = ring + slot * L.stage + V::kWeights, bar = full + slot * 8;
+                if (lane < V::kBoxes) tma_load_2d(dst + lane * V::kBox, &map, k + lane * kBoxK, w_row, bar);   // beyond the matrix: zeros
 #pragma unroll
                 for (int q = 0; q < kMine; ++q) {
-                    const int i = lane + 32 * q;
-                    if (i < rows && k < p.Kd) bulk_row(dst + i * V::kPitch, src[q], 2 * min(V::kStepK, p.Kd - k), bar);
+                    if (lane + 32 * q < rows && bytes) bulk_row(dst + V::kWeights + (lane + 32 * q) * V::kPitch, src[q], bytes, bar);
                     src[q] += V::kStepK;
                 }
-            };
-            int ahead = 0;   // stages whose weights have been asked for
-            j = 0;
-            if (second && alive) {   // a ring of weights, then the first product's results
-                const int slot0 = slot;
-                const uint32_t phase0 = phase;
-                for (int task = p.t0 + group; task < p.t1 && ahead < L.stages && alive; task += GR) {
-                    const Task t = locate(p, task);
-                    enter(t);
-                    for (int i = 0; i < p.stages && ahead < L.stages; ++i, ++ahead) {
-                        if (!wait_or_abort(empty + slot * 8, phase ^ 1u, &abort_word)) { alive = false; break; }
-                        weights((t.step + i) * V::kStepK);
-                        next_slot();
-                    }
-                }
-                slot = slot0; phase = phase0; j = 0;
-                if (alive && ahead > 0) alive = __shfl_sync(0xffffffffu, lane == 0 ? wait_count(a.done, (int)gridDim.x, &abort_word) : 1, 0);
-                asm volatile("fence.proxy.async;" ::: "memory");   // the first product's stores, read by copies from here on
-            }
-            for (int task = p.t0 + group; task < p.t1 && alive; task += GR) {
-                const Task t = locate(p, task);
-                enter(t);
-                int k = t.step * V::kStepK;
-#pragma unroll 1
-                for (int i = 0; i < p.stages; ++i, k += V::kStepK) {
-                    if (ahead > 0) {
-                        --ahead;
-                    } else {
-                        if (!wait_or_abort(empty + slot * 8, phase ^ 1u, &abort_word)) { alive = false; break; }
-                        weights(k);
-                    }
-                    tokens(k);
-                    next_slot();
-                }
+                next_slot();
             }
         }
     } else {                    // ---- the other warps of the group multiply ----
@@ -430,174 +398,164 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
         auto group_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(V::kMulWarps * 32) : "memory"); };
         // this thread's bytes of a stage: weight row gq of each block, 16-byte pieces 2 tq and 2 tq + 1
         const uint32_t wrow = wk * BW * V::kBox + (wr * 8 * NB + gq) * 128, even = wrow + ((2 * tq) ^ gq) * 16, odd = wrow + ((2 * tq + 1) ^ gq) * 16;
+        const bool direct = second && p.S == 1 && a.K == 1;
         int turn = 0;
-#pragma unroll 1
-        for (int ph = 0; ph < 2; ++ph) {
-            const bool second = ph != 0;
-            const Product p = product(second);
-            const bool direct = second && p.S == 1 && a.K == 1;
-            j = 0;
-            for (int task = p.t0 + group; task < p.t1; task += GR) {
-                const Task t = locate(p, task);
-                // The second product takes the intermediate as high + low part.  While its tokens fill no more than half
-                // of the tile's rows, the low parts are the other half; beyond that they take products of their own.
-                constexpr int half = 8 * MT;
-                const bool packed = second && t.m <= half, two_pass = second && !packed;
-                const int rows_used = packed ? half + t.m : t.m;
-                // Rows of the tile beyond the tokens repeat a token: a row enters no other row's results.
-                uint32_t at[2 * MT];
+        for (int task = p.t0 + group; task < p.t1; task += GR) {
+            const Task t = locate(task);
+            // The second product takes the intermediate as high + low part.  While its tokens fill no more than half
+            // of the tile's rows, the low parts are the other half; beyond that they take products of their own.
+            constexpr int half = 8 * MT;
+            const bool packed = second && t.m <= half, two_pass = second && !packed;
+            const int rows_used = packed ? half + t.m : t.m;
+            // Rows of the tile beyond the tokens repeat a token: a row enters no other row's results.
+            uint32_t at[2 * MT];
 #pragma unroll
-                for (int i = 0; i < 2 * MT; ++i) {
-                    const bool lower = packed && i >= MT;
-                    const int row = min((lower ? i - MT : i) * 8 + gq, t.m - 1) + (lower ? t.m : 0);
-                    at[i] = V::kWeights + row * V::kPitch + wk * BW * 128 + tq * 32;
+            for (int i = 0; i < 2 * MT; ++i) {
+                const bool lower = packed && i >= MT;
+                const int row = min((lower ? i - MT : i) * 8 + gq, t.m - 1) + (lower ? t.m : 0);
+                at[i] = V::kWeights + row * V::kPitch + wk * BW * 128 + tq * 32;
+            }
+            float acc[MT][NB][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+            int left = p.Kd - t.step * V::kStepK - wk * BW * kBoxK - tq * 16;   // from this thread's first k to the end of the rows
+#pragma unroll 1
+            for (int i = 0; i < p.stages; ++i) {
+                if (alive) alive = wait_or_abort(full + slot * 8, phase, &abort_word);
+                const uint32_t stage = ring + slot * L.stage;
+#pragma unroll
+                for (int c = 0; c < 2 * BW; ++c) {
+                    uint4 wv[NB], av[2 * MT];
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) wv[n] = ld_shared(stage + (c >> 1) * V::kBox + n * 1024 + ((c & 1) ? odd : even));
+                    auto tokens = [&](uint32_t more) {   // beyond K zeros: the weights' zeros alone would keep a NaN
+#pragma unroll
+                        for (int q = 0; q < 2 * MT; ++q) {
+                            av[q] = ld_shared(stage + at[q] + more + (c >> 1) * 128 + (c & 1) * 16);
+                            if ((c >> 1) * kBoxK + (c & 1) * 8 >= left) av[q] = make_uint4(0, 0, 0, 0);
+                        }
+                    };
+                    auto products = [&]() {
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            if (m > 0 && m * 16 >= rows_used) break;
+#pragma unroll
+                            for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].x, av[2 * m + 1].x, av[2 * m].y, av[2 * m + 1].y, wv[n].x, wv[n].y);
+#pragma unroll
+                            for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].z, av[2 * m + 1].z, av[2 * m].w, av[2 * m + 1].w, wv[n].z, wv[n].w);
+                        }
+                    };
+                    tokens(0);
+                    products();
+                    if (two_pass) {
+                        tokens(t.m * V::kPitch);
+                        products();
+                    }
                 }
-                float acc[MT][NB][4];
+                __syncwarp();   // the stage has been read by the whole warp
+                if (lane == 0) mbar_arrive(empty + slot * 8);
+                left -= V::kStepK;
+                next_slot();
+            }
+            // A result pair: weight rows `row` and `row` + 1 of token m of the chunk.
+            auto emit = [&](int m, int row, float2 v) {
+                const int as = sorted[t.base + m];
+                if (!second) {
+                    v.x = 0.5f * v.x * erfcf(-0.70710678118654752f * v.x);
+                    v.y = 0.5f * v.y * erfcf(-0.70710678118654752f * v.y);
+                    const uint32_t hi = cvt_bf16x2(v);
+                    uint16_t* g = a.g + (size_t)as * a.F + row;
+                    *reinterpret_cast<uint32_t*>(g) = hi;
+                    *reinterpret_cast<uint32_t*>(g + (size_t)TK * a.F) = cvt_bf16x2(make_float2(v.x - bf16_lo(hi), v.y - bf16_hi(hi)));
+                } else if (direct) {
+                    const float f = a.weighted ? score[as] : 1.0f;
+                    *reinterpret_cast<uint32_t*>(a.out + (size_t)as * a.H + row) = cvt_bf16x2(make_float2(v.x * f, v.y * f));
+                } else {
+                    *reinterpret_cast<float2*>(a.part + ((size_t)t.s * TK + as) * a.H + row) = v;
+                }
+            };
+            if constexpr (WK > 1) {   // the shares of the warps along k, added in warp order; then the low parts' rows
+                float* red = reinterpret_cast<float*>(sm + L.red) + group * V::kRed;
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int n = 0; n < NB; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
-                int left = p.Kd - t.step * V::kStepK - wk * BW * kBoxK - tq * 16;   // from this thread's first k to the end of the rows
-#pragma unroll 1
-                for (int i = 0; i < p.stages; ++i) {
-                    if (alive) alive = wait_or_abort(full + slot * 8, phase, &abort_word);
-                    const uint32_t stage = ring + slot * L.stage;
-#pragma unroll
-                    for (int c = 0; c < 2 * BW; ++c) {
-                        uint4 wv[NB], av[2 * MT];
-#pragma unroll
-                        for (int n = 0; n < NB; ++n) wv[n] = ld_shared(stage + (c >> 1) * V::kBox + n * 1024 + ((c & 1) ? odd : even));
-                        auto tokens = [&](uint32_t more) {   // beyond K zeros: the weights' zeros alone would keep a NaN
-#pragma unroll
-                            for (int q = 0; q < 2 * MT; ++q) {
-                                av[q] = ld_shared(stage + at[q] + more + (c >> 1) * 128 + (c & 1) * 16);
-                                if ((c >> 1) * kBoxK + (c & 1) * 8 >= left) av[q] = make_uint4(0, 0, 0, 0);
-                            }
-                        };
-                        auto products = [&]() {
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                if (m > 0 && m * 16 >= rows_used) break;
-#pragma unroll
-                                for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].x, av[2 * m + 1].x, av[2 * m].y, av[2 * m + 1].y, wv[n].x, wv[n].y);
-#pragma unroll
-                                for (int n = 0; n < NB; ++n) mma16816(acc[m][n], av[2 * m].z, av[2 * m + 1].z, av[2 * m].w, av[2 * m + 1].w, wv[n].z, wv[n].w);
-                            }
-                        };
-                        tokens(0);
-                        products();
-                        if (two_pass) {
-                            tokens(t.m * V::kPitch);
-                            products();
-                        }
+                    for (int n = 0; n < NB; ++n) {
+                        float* r = red + ((wk * 16 * MT) + m * 16 + gq) * R + (wr * NB + n) * 8 + tq * 2;
+                        *reinterpret_cast<float2*>(r) = make_float2(acc[m][n][0], acc[m][n][1]);
+                        *reinterpret_cast<float2*>(r + 8 * R) = make_float2(acc[m][n][2], acc[m][n][3]);
                     }
-                    __syncwarp();   // the stage has been read by the whole warp
-                    if (lane == 0) mbar_arrive(empty + slot * 8);
-                    left -= V::kStepK;
-                    next_slot();
-                }
-                // A result pair: weight rows `row` and `row` + 1 of token m of the chunk.
-                auto emit = [&](int m, int row, float2 v) {
-                    const int as = sorted[t.base + m];
-                    if (!second) {
-                        v.x = 0.5f * v.x * erfcf(-0.70710678118654752f * v.x);
-                        v.y = 0.5f * v.y * erfcf(-0.70710678118654752f * v.y);
-                        const uint32_t hi = cvt_bf16x2(v);
-                        uint16_t* g = a.g + (size_t)as * a.F + row;
-                        *reinterpret_cast<uint32_t*>(g) = hi;
-                        *reinterpret_cast<uint32_t*>(g + (size_t)TK * a.F) = cvt_bf16x2(make_float2(v.x - bf16_lo(hi), v.y - bf16_hi(hi)));
-                    } else if (direct) {
-                        const float f = a.weighted ? score[as] : 1.0f;
-                        *reinterpret_cast<uint32_t*>(a.out + (size_t)as * a.H + row) = cvt_bf16x2(make_float2(v.x * f, v.y * f));
-                    } else {
-                        *reinterpret_cast<float2*>(a.part + ((size_t)t.s * TK + as) * a.H + row) = v;
-                    }
-                };
-                if constexpr (WK > 1) {   // the shares of the warps along k, added in warp order; then the low parts' rows
-                    float* red = reinterpret_cast<float*>(sm + L.red) + group * V::kRed;
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int n = 0; n < NB; ++n) {
-                            float* r = red + ((wk * 16 * MT) + m * 16 + gq) * R + (wr * NB + n) * 8 + tq * 2;
-                            *reinterpret_cast<float2*>(r) = make_float2(acc[m][n][0], acc[m][n][1]);
-                            *reinterpret_cast<float2*>(r + 8 * R) = make_float2(acc[m][n][2], acc[m][n][3]);
-                        }
-                    group_sync();
-                    for (int o = gt; o < t.m * (R / 2); o += V::kMulWarps * 32) {
-                        const int m = o / (R / 2), r = o % (R / 2) * 2;
-                        if (t.row0 + r >= p.N) continue;
-                        float2 v = make_float2(0.0f, 0.0f), l = v;
-#pragma unroll
-                        for (int w = 0; w < WK; ++w) {
-                            const float2 z = *reinterpret_cast<const float2*>(red + (w * 16 * MT + m) * R + r);
-                            v.x += z.x; v.y += z.y;
-                            if (packed) {
-                                const float2 y = *reinterpret_cast<const float2*>(red + (w * 16 * MT + half + m) * R + r);
-                                l.x += y.x; l.y += y.y;
-                            }
-                        }
-                        emit(m, t.row0 + r, make_float2(v.x + l.x, v.y + l.y));
-                    }
-                    group_sync();   // also: the strip may be written again
-                } else {          // thread (gq, tq) has the tokens gq of each eight and weight rows 2 tq, 2 tq + 1 of each block
-#pragma unroll
-                    for (int i = 0; i < 2 * MT; ++i) {
-                        const int m = i * 8 + gq;
-                        if (m >= t.m) continue;
-#pragma unroll
-                        for (int n = 0; n < NB; ++n) {
-                            const int row = t.row0 + (wr * NB + n) * 8 + tq * 2;
-                            if (row >= p.N) continue;
-                            float2 v = make_float2(acc[i >> 1][n][(i & 1) * 2], acc[i >> 1][n][(i & 1) * 2 + 1]);
-                            if (packed && i < MT) {
-                                v.x += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2];
-                                v.y += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2 + 1];
-                            }
-                            emit(m, row, v);
-                        }
-                    }
-                }
-                // The last task to arrive at a warp's columns adds them all up, in a fixed order.  One lane's acquire-release
-                // addition orders the group's stores before it (they are behind a barrier) and the sums after it; the warps
-                // along k take turns, since it costs the one that does it a round trip to L2.
-                if (second && !direct && (WK == 1 || wk == turn)) {
-                    __syncwarp();
-                    int last = 0;
-                    if (lane == 0) last = add_acq_rel(&a.arrived[t.rb * V::WR + wr]) == chunks * p.S - 1;
-                    if (__shfl_sync(0xffffffffu, last, 0)) {
-                        constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
-                        const int row = t.row0 + wr * 8 * NB + (lane % Q) * 4;
-                        if (row < p.N) {
-                            for (int tok = lane / Q; tok < a.T; tok += 32 / Q) {
-                                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                                for (int k = 0; k < a.K; ++k) {
-                                    const float* from = a.part + ((size_t)k * a.T + tok) * a.H + row;
-                                    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-                                    for (int s = 0; s < p.S; ++s) {
-                                        const float4 z = __ldcg(reinterpret_cast<const float4*>(from + (size_t)s * TK * a.H));
-                                        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-                                    }
-                                    const float f = a.weighted ? score[k * a.T + tok] : 1.0f;
-                                    v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
-                                }
-                                *reinterpret_cast<uint2*>(a.out + (size_t)tok * a.H + row) =
-                                    make_uint2(cvt_bf16x2(make_float2(v.x, v.y)), cvt_bf16x2(make_float2(v.z, v.w)));
-                            }
-                        }
-                        __syncwarp();
-                    }
-                }
-                    turn = turn + 1 == WK ? 0 : turn + 1;
-                }
-            if (!second) {      // this group's part of the intermediate is there; the CTA's last group counts it in
                 group_sync();
-                if (gt == 0 && add_acq_rel_cta(&groups_done) == GR - 1) add_release(a.done);
+                for (int o = gt; o < t.m * (R / 2); o += V::kMulWarps * 32) {
+                    const int m = o / (R / 2), r = o % (R / 2) * 2;
+                    if (t.row0 + r >= p.N) continue;
+                    float2 v = make_float2(0.0f, 0.0f), l = v;
+#pragma unroll
+                    for (int w = 0; w < WK; ++w) {
+                        const float2 z = *reinterpret_cast<const float2*>(red + (w * 16 * MT + m) * R + r);
+                        v.x += z.x; v.y += z.y;
+                        if (packed) {
+                            const float2 y = *reinterpret_cast<const float2*>(red + (w * 16 * MT + half + m) * R + r);
+                            l.x += y.x; l.y += y.y;
+                        }
+                    }
+                    emit(m, t.row0 + r, make_float2(v.x + l.x, v.y + l.y));
+                }
+                group_sync();   // also: the strip may be written again
+            } else {          // thread (gq, tq) has the tokens gq of each eight and weight rows 2 tq, 2 tq + 1 of each block
+#pragma unroll
+                for (int i = 0; i < 2 * MT; ++i) {
+                    const int m = i * 8 + gq;
+                    if (m >= t.m) continue;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        const int row = t.row0 + (wr * NB + n) * 8 + tq * 2;
+                        if (row >= p.N) continue;
+                        float2 v = make_float2(acc[i >> 1][n][(i & 1) * 2], acc[i >> 1][n][(i & 1) * 2 + 1]);
+                        if (packed && i < MT) {
+                            v.x += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2];
+                            v.y += acc[(i + MT) >> 1][n][((i + MT) & 1) * 2 + 1];
+                        }
+                        emit(m, row, v);
+                    }
+                }
             }
-        }
+            // The last task to arrive at a warp's columns adds them all up, in a fixed order.  One lane's acquire-release
+            // addition orders the group's stores before it (they are behind a barrier) and the sums after it; the warps
+            // along k take turns, since it costs the one that does it a round trip to L2.
+            if (second && !direct && (WK == 1 || wk == turn)) {
+                __syncwarp();
+                int last = 0;
+                if (lane == 0) last = add_acq_rel(&a.arrived[t.rb * V::WR + wr]) == chunks * p.S - 1;
+                if (__shfl_sync(0xffffffffu, last, 0)) {
+                    constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
+                    const int row = t.row0 + wr * 8 * NB + (lane % Q) * 4;
+                    if (row < p.N) {
+                        for (int tok = lane / Q; tok < a.T; tok += 32 / Q) {
+                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            for (int k = 0; k < a.K; ++k) {
+                                const float* from = a.part + ((size_t)k * a.T + tok) * a.H + row;
+                                float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+                                for (int s = 0; s < p.S; ++s) {
+                                    const float4 z = __ldcg(reinterpret_cast<const float4*>(from + (size_t)s * TK * a.H));
+                                    y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                                }
+                                const float f = a.weighted ? score[k * a.T + tok] : 1.0f;
+                                v.x = fmaf(f, y.x, v.x); v.y = fmaf(f, y.y, v.y); v.z = fmaf(f, y.z, v.z); v.w = fmaf(f, y.w, v.w);
+                            }
+                            *reinterpret_cast<uint2*>(a.out + (size_t)tok * a.H + row) =
+                                make_uint2(cvt_bf16x2(make_float2(v.x, v.y)), cvt_bf16x2(make_float2(v.z, v.w)));
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+                turn = turn + 1 == WK ? 0 : turn + 1;
+            }
     }
     // After a wait that was given up copies may still be on their way into this CTA's shared memory: it stays for a
     // millisecond, hundreds of times their latency, before it leaves.
@@ -606,7 +564,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
-struct FewPlan { size_t off_g, off_part, off_arrived, off_done, total; int max_split; };
+struct FewPlan { size_t off_g, off_part, off_arrived, total; int max_split; };
 FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
     FewPlan p{};
     const size_t TK = (size_t)s.T * K;
@@ -617,8 +575,7 @@ FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
     p.off_g = 0;
     p.off_part = up(2 * TK * F * 2);
     p.off_arrived = p.off_part + up(p.max_split * TK * s.H * 4);
-    p.off_done = p.off_arrived + up((size_t)(s.H + 7) / 8 * 4);
-    p.total = p.off_done + 256;
+    p.total = p.off_arrived + up((size_t)(s.H + 7) / 8 * 4);
     return p;
 }
 
@@ -637,22 +594,12 @@ int run_few(const FewArgs& a, cudaStream_t st) {
     CUtensorMap m1, m2;
     const uint64_t d1[2] = {(uint64_t)a.H, (uint64_t)a.E * a.F}, d2[2] = {(uint64_t)a.F, (uint64_t)a.E * a.H};
     if (!make_map(&m1, a.w_in, 2, d1, V::R) || !make_map(&m2, a.w_out, 2, d2, V::R)) return LOCMOE_ERR_CUDA;
-    const int rc = launch_pdl(few_router_kernel, dim3(a.T), dim3(kRouterThreads), 0, st, a);
-    if (rc) return rc;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sm_count());
-    cfg.blockDim = dim3(V::kThreads);
-    cfg.dynamicSmemBytes = layout<V>(a.T * a.K, a.E, 2 * (a.T < 16 * V::MT ? a.T : 16 * V::MT)).total;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeCooperative;   // its CTAs wait for one another: all of them run at once or none
-    attr[0].val.cooperative = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, moe_few_kernel<V>, m1, m2, a) != cudaSuccess) { cudaGetLastError(); return LOCMOE_ERR_CUDA; }
-    return LOCMOE_OK;
+    int rc = LOCMOE_OK;
+    if (!a.inline_router && (rc = launch_pdl(few_router_kernel, dim3(a.T), dim3(kRouterThreads), 0, st, a))) return rc;
+    const dim3 grid(sm_count()), block(V::kThreads);
+    const int smem = layout<V>(a.T * a.K, a.E, 2 * (a.T < 16 * V::MT ? a.T : 16 * V::MT)).total;
+    if ((rc = launch_pdl(moe_few_kernel<V>, grid, block, smem, st, m1, a, 0))) return rc;
+    return launch_pdl(moe_few_kernel<V>, grid, block, smem, st, m2, a, 1);
 }
 
 }  // namespace
@@ -665,9 +612,8 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
     unsigned char* base = static_cast<unsigned char*>(ws);
     const FewArgs a{static_cast<const uint16_t*>(x), eps, static_cast<const uint16_t*>(w_in), static_cast<const uint16_t*>(w_out), idx_k,
                     w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
-                    reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived),
-                    reinterpret_cast<int32_t*>(base + p.off_done), s.T, s.H, s.E, K, F,
-                    p.max_split, weighted};
+                    reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
+                    p.max_split, weighted, s.T <= kInlineTokens};
     if (s.T * K <= 2) return run_few<Variant<5, 1, 4, 1, 1, 1, 220 << 10>>(a, st);
     if (s.T * K <= 8) return run_few<Variant<3, 1, 4, 2, 1, 1, 220 << 10>>(a, st);
     if (s.T <= 16) return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10>>(a, st);
