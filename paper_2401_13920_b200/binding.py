@@ -499,50 +499,37 @@ def locmoe_moe_few_bytes(shape: Shape, K, F) -> int:
     return out.value
 
 
+def _arg(t, dtype, numel, name):
+    """Device address of an argument (None for an absent one) after all checks; a plain int, which ctypes takes as it is."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < numel:
+        _want(t, dtype, numel, name)
+    if not (t.is_cuda and t.is_contiguous()):
+        _ptr(t)
+    return t.data_ptr()
+
+
 def locmoe_moe_few(shape: Shape, x, K, F, w_in, w_out, idx_k, w_k, out, ws, eps=None, unweighted=False, stream=None) -> int:
     """The whole layer for at most FEW_MAX_TOKENS tokens."""
-    bf = torch.bfloat16
-    for t, dt, n, name in ((x, bf, shape.T * shape.H, "x"), (w_in, bf, shape.E * F * shape.H, "w_in"), (w_out, bf, shape.E * F * shape.H, "w_out"),
-                           (idx_k, torch.int32, K * shape.T, "idx_k"), (w_k, torch.float32, K * shape.T, "w_k"), (out, bf, shape.T * shape.H, "out")):
-        _want(t, dt, n, name)
-    if eps is not None:
-        _want(eps, torch.float32, shape.E, "eps")
+    bf, f32, T, TH, n = torch.bfloat16, torch.float32, shape.T, shape.T * shape.H, shape.E * F * shape.H
     return _check("locmoe_moe_few", _lib.locmoe_moe_few(
-        C.byref(shape), _ptr(x), _ptr(eps), int(K), int(F), _ptr(w_in), _ptr(w_out), FEW_UNWEIGHTED if unweighted else 0, _ptr(idx_k),
-        _ptr(w_k), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
-
-
-def _fill(struct, dtypes, numels, tensors, scalars):
-    """Pointer block of one call: every given tensor is checked for dtype, size, device and density and stored."""
-    for name, t in tensors.items():
-        if t is not None:
-            _want(t, dtypes[name], numels[name], name)
-            setattr(struct, name, _ptr(t).value)
-    for name, v in scalars.items():
-        setattr(struct, name, float(v))
-    return struct
-
-
-def _norm_types(shape: Shape, C_alloc, slot):
-    dt = torch.float32 if shape.x_dtype == F32 else torch.bfloat16
-    TH, rows = shape.T * shape.H, shape.D * shape.E * int(C_alloc) if slot is not None else shape.T
-    dtypes, numels = {}, {}
-    for names, t, n in ((("h", "h_out", "n_out", "dh_out", "dn", "dh"), dt, TH), (("y", "dy"), dt, rows * shape.H),
-                        (("u8", "x8"), torch.float8_e4m3fn, TH), (("gate_w", "r_post", "r_pre", "dgate"), torch.float32, shape.T),
-                        (("w_post", "w_pre", "dw_post", "dw_pre"), torch.float32, shape.H), (("slot",), torch.int32, shape.T),
-                        (("inv",), torch.int32, rows)):
-        for k in names:
-            dtypes[k], numels[k] = t, n
-    return dtypes, numels
+        C.byref(shape), _arg(x, bf, TH, "x"), _arg(eps, f32, shape.E, "eps"), K, F, _arg(w_in, bf, n, "w_in"), _arg(w_out, bf, n, "w_out"),
+        FEW_UNWEIGHTED if unweighted else 0, _arg(idx_k, torch.int32, K * T, "idx_k"), _arg(w_k, f32, K * T, "w_k"), _arg(out, bf, TH, "out"),
+        _arg(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)))
 
 
 def locmoe_block_norm(shape: Shape, C_alloc, h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6,
                       h_out=None, n_out=None, u8=None, x8=None, r_post=None, r_pre=None, stream=None) -> int:
     """Post-norm, gate, residual and the next pre-norm in one pass; any array that is not wanted is None."""
-    b = _fill(BlockNorm(), *_norm_types(shape, C_alloc, slot),
-              dict(h=h, y=y, slot=slot, gate_w=gate_w, w_post=w_post, w_pre=w_pre, h_out=h_out, n_out=n_out, u8=u8, x8=x8,
-                   r_post=r_post, r_pre=r_pre), dict(res_scale=res_scale, eps=eps))
-    return _check("locmoe_block_norm", _lib.locmoe_block_norm(C.byref(shape), int(C_alloc), C.byref(b), _stream(stream)))
+    T, H = shape.T, shape.H
+    dt, f32, e4m3 = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.float8_e4m3fn
+    rows = T if slot is None else shape.D * shape.E * C_alloc
+    b = BlockNorm(_arg(h, dt, T * H, "h"), _arg(y, dt, rows * H, "y"), _arg(slot, torch.int32, T, "slot"), _arg(gate_w, f32, T, "gate_w"),
+                  _arg(w_post, f32, H, "w_post"), _arg(w_pre, f32, H, "w_pre"), res_scale, eps, _arg(h_out, dt, T * H, "h_out"),
+                  _arg(n_out, dt, T * H, "n_out"), _arg(u8, e4m3, T * H, "u8"), _arg(x8, e4m3, T * H, "x8"), _arg(r_post, f32, T, "r_post"),
+                  _arg(r_pre, f32, T, "r_pre"))
+    return _check("locmoe_block_norm", _lib.locmoe_block_norm(C.byref(shape), C_alloc, C.byref(b), _stream(stream)))
 
 
 def locmoe_block_norm_grad_bytes(shape: Shape) -> int:
@@ -555,12 +542,17 @@ def locmoe_block_norm_grad(shape: Shape, C_alloc, dh_out=None, dn=None, h_out=No
                            slot=None, inv=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, dh=None, dy=None,
                            dgate=None, dw_post=None, dw_pre=None, ws=None, stream=None) -> int:
     """Gradient of locmoe_block_norm, from h_out and y or from the 8-bit checkpoints."""
-    b = _fill(BlockNormGrad(), *_norm_types(shape, C_alloc, slot),
-              dict(dh_out=dh_out, dn=dn, h_out=h_out, y=y, u8=u8, x8=x8, r_post=r_post, r_pre=r_pre, slot=slot, inv=inv,
-                   gate_w=gate_w, w_post=w_post, w_pre=w_pre, dh=dh, dy=dy, dgate=dgate, dw_post=dw_post, dw_pre=dw_pre),
-              dict(res_scale=res_scale, eps=eps))
+    T, H = shape.T, shape.H
+    dt, f32, i32, e4m3 = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+    TH, rows = T * H, T if slot is None else shape.D * shape.E * C_alloc
+    b = BlockNormGrad(
+        _arg(dh_out, dt, TH, "dh_out"), _arg(dn, dt, TH, "dn"), _arg(h_out, dt, TH, "h_out"), _arg(y, dt, rows * H, "y"),
+        _arg(u8, e4m3, TH, "u8"), _arg(x8, e4m3, TH, "x8"), _arg(r_post, f32, T, "r_post"), _arg(r_pre, f32, T, "r_pre"),
+        _arg(slot, i32, T, "slot"), _arg(inv, i32, rows, "inv"), _arg(gate_w, f32, T, "gate_w"), _arg(w_post, f32, H, "w_post"),
+        _arg(w_pre, f32, H, "w_pre"), res_scale, eps, _arg(dh, dt, TH, "dh"), _arg(dy, dt, rows * H, "dy"), _arg(dgate, f32, T, "dgate"),
+        _arg(dw_post, f32, H, "dw_post"), _arg(dw_pre, f32, H, "dw_pre"))
     return _check("locmoe_block_norm_grad", _lib.locmoe_block_norm_grad(
-        C.byref(shape), int(C_alloc), C.byref(b), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+        C.byref(shape), C_alloc, C.byref(b), _arg(ws, torch.uint8, 0, "ws"), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def conventional_capacity(T: int, D: int, E: int, capacity_factor: float) -> int:

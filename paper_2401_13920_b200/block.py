@@ -6,6 +6,7 @@ entry points of ``binding``; all arithmetic runs in the CUDA library.  ``BlockNo
 """
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
@@ -22,13 +23,30 @@ class Checkpoint(NamedTuple):
     r_pre: Optional[torch.Tensor]
 
 
+# Shape structs are read by a call and never written: one for each shape met, and the workspace sizes that go with them.
+@lru_cache(maxsize=1024)
+def _shape(T: int, H: int, E: int, dtype: torch.dtype) -> B.Shape:
+    return B.Shape(T, H, E, 1, 1, B.dtype_code(dtype), B.LAYOUT_SEND)
+
+
+@lru_cache(maxsize=1024)
+def _few_plan(T: int, H: int, E: int, K: int, F: int, dtype: torch.dtype):
+    shape = _shape(T, H, E, dtype)
+    return shape, B.locmoe_moe_few_bytes(shape, K, F)
+
+
+@lru_cache(maxsize=1024)
+def _grad_bytes(T: int, H: int, dtype: torch.dtype, device: int) -> int:
+    return B.locmoe_block_norm_grad_bytes(_shape(T, H, 1, dtype))
+
+
 def _row_shape(like: torch.Tensor, y, slot) -> tuple:
     """Shape struct and row stride for [T][H] tensors whose block output has ``y``'s rows."""
     if like.dim() != 2:
         raise ValueError("expected a [T][H] tensor, got %s" % (tuple(like.shape),))
     T, H = like.shape
     rows = T if slot is None else y.shape[0]
-    return B.Shape(T, H, 1, 1, 1, B.dtype_code(like.dtype), B.LAYOUT_SEND), rows
+    return _shape(T, H, 1, like.dtype), rows
 
 
 def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
@@ -40,12 +58,13 @@ def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
     (T, H), (E, F, _) = x.shape, w_in.shape
     if w_in.shape[2] != H or w_out.shape != (E, H, F):
         raise ValueError("x %s, w_in %s and w_out %s do not belong together" % (tuple(x.shape), tuple(w_in.shape), tuple(w_out.shape)))
+    dev = x.device
     out = torch.empty_like(x)
-    idx, w = torch.empty(K, T, dtype=torch.int32, device=x.device), torch.empty(K, T, dtype=torch.float32, device=x.device)
+    idx, w = torch.empty((K, T), dtype=torch.int32, device=dev), torch.empty((K, T), dtype=torch.float32, device=dev)
     if T == 0:
         return out, idx, w
-    shape = B.Shape(T, H, E, 1, 1, B.dtype_code(x.dtype), B.LAYOUT_SEND)
-    ws = torch.empty(B.locmoe_moe_few_bytes(shape, K, F), dtype=torch.uint8, device=x.device)
+    shape, n = _few_plan(T, H, E, K, F, x.dtype)
+    ws = torch.empty((n,), dtype=torch.uint8, device=dev)
     B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted, stream)
     return out, idx, w
 
@@ -103,7 +122,7 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
         return dh, dy, dgate, dw_post, dw_pre
     ws = None
     if dw_post is not None or dw_pre is not None:
-        ws = torch.empty(B.locmoe_block_norm_grad_bytes(shape), dtype=torch.uint8, device=dev)
+        ws = torch.empty(_grad_bytes(T, H, like.dtype, torch.cuda.current_device()), dtype=torch.uint8, device=dev)
     acts = dict(u8=ck.u8, r_post=ck.r_post, x8=ck.x8 if dn is not None else None, r_pre=ck.r_pre if dn is not None else None) \
         if ck is not None else dict(y=y, h_out=h_out if dn is not None else None)
     B.locmoe_block_norm_grad(shape, rows, dh_out, dn, slot=slot if branch else None, inv=inv if branch and slot is not None else None,
