@@ -609,7 +609,8 @@ int locmoe_launch_counts(const locmoe_shape_t *shape, int32_t counts[5]);
 /* Device-side diagnostics of this library on the current device, copied to host
  * memory after waiting for the stream: bit 0 is set if a kernel gave up a
  * bounded wait for one of its own asynchronous copies (its output is then
- * incomplete); bit 1 the same for the expert-FFN kernels, bit 2 for those of locmoe_moe_few.  0 in normal operation.
+ * incomplete); bit 1 the same for the expert-FFN kernels, bit 2 for those of locmoe_moe_few, bit 3 for the
+ * block norms'.  0 in normal operation.
  * The paper has no counterpart. */
 int locmoe_device_flags(int32_t *flags_host, void *stream);
 

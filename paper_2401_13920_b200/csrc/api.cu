@@ -564,11 +564,12 @@ int locmoe_launch_counts(const locmoe_shape_t* shape, int32_t counts[5]) {
 
 int locmoe_device_flags(int32_t* flags_host, void* stream) {
     if (!flags_host) return LOCMOE_ERR_NULL;
-    int v = 0, f = 0, few = 0;
+    int v = 0, f = 0, few = 0, norm = 0;
     int rc = read_device_flags(&v, static_cast<cudaStream_t>(stream));
     if (rc == LOCMOE_OK) rc = read_ffn_flags(&f, static_cast<cudaStream_t>(stream));
     if (rc == LOCMOE_OK) rc = read_few_flags(&few, static_cast<cudaStream_t>(stream));
-    *flags_host = v | (f << 1) | (few << 2);
+    if (rc == LOCMOE_OK) rc = read_norm_flags(&norm, static_cast<cudaStream_t>(stream));
+    *flags_host = v | (f << 1) | (few << 2) | (norm << 3);
     return rc;
 }
 

@@ -6,8 +6,13 @@
 //              k  = sum_j D w_post u,   dR = k,   dv = r (R w_post D - u R k / H)
 //              dw_pre = sum_t dn x,     dw_post = sum_t R D u
 //
-// A row is worked on by a group of kWarp-multiple threads that keep it in registers between its two sums, so every
-// element is read and written once.  Sums are fp32 in a fixed order; outputs are rounded once.
+// Bound by memory: 8 bytes an element forward and 12 backward in bf16, 10 with checkpoints.  A row is worked on by a
+// group of kWarp-multiple threads that keep it in registers between its two sums, so every element is read and written
+// once.  The two sums of a row are two round trips through the group, during which a kernel that loads its rows itself
+// asks memory for nothing (65536 x 5120 in bf16: 699 us forward, 58 % of the copy bandwidth); so each group has a ring
+// of rows in shared memory that bulk copies fill D rows ahead, one thread asking for the row D on as soon as the first
+// sum's barrier shows that the group has taken a row out of its place.
+// Sums are fp32 in a fixed order; outputs are rounded once.
 // With checkpoints the forward also leaves u and x in E4M3: a normalised row has mean square <= 1 and so no element
 // above sqrt(H), which the format's 448 covers for every H the library takes here; r and q carry the scale.
 #include <cuda_fp8.h>
@@ -18,14 +23,14 @@ namespace locmoe {
 
 namespace {
 
-constexpr int kMaxGroups = 15;   // row groups of a CTA: one named barrier each (barrier 0 is the whole CTA's)
+constexpr int kMaxGroups = 15;      // row groups of a CTA: one named barrier each (barrier 0 is the whole CTA's)
 
 struct NormArgs {
     const void* h; const void* y; const int32_t* slot; const float* gate; const float* w_post; const float* w_pre;
     float res_scale, eps;
     void* h_out; void* n_out; uint8_t* u8; uint8_t* x8; float* r_post; float* r_pre;
     long long rows;
-    int T, H, tpr, groups;
+    int T, H, tpr, groups, depth;   // depth: rows of a group's ring
 };
 
 struct NormGradArgs {
@@ -35,7 +40,7 @@ struct NormGradArgs {
     float res_scale, eps;
     void* dh; void* dy; float* dgate; float* part_post; float* part_pre;   // parts: [grid][H]
     long long rows;
-    int T, H, tpr, groups;
+    int T, H, tpr, groups, depth;
 };
 
 // ---- one unit of a row: VEC = 8 elements by 16-byte accesses, VEC = 1 a single element ----
@@ -78,6 +83,47 @@ template <> struct Unit<float, 1> {
     static __device__ __forceinline__ void store(void* base, size_t at, const float* f) { static_cast<float*>(base)[at] = f[0]; }
 };
 
+// ---- the ring kernels work on pairs: two-wide fp32 instructions, four pairs a unit ----
+struct Unit8 { float2 p[4]; };
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+template <typename X>
+__device__ __forceinline__ Unit8 load_pairs(const unsigned char* at) {   // out of shared memory
+    Unit8 f;
+    if constexpr (sizeof(X) == 2) {
+        const uint4 w = *reinterpret_cast<const uint4*>(at);
+        f.p[0] = make_float2(bf16_lo(w.x), bf16_hi(w.x)); f.p[1] = make_float2(bf16_lo(w.y), bf16_hi(w.y));
+        f.p[2] = make_float2(bf16_lo(w.z), bf16_hi(w.z)); f.p[3] = make_float2(bf16_lo(w.w), bf16_hi(w.w));
+    } else {
+        const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 16);
+        f.p[0] = make_float2(a.x, a.y); f.p[1] = make_float2(a.z, a.w); f.p[2] = make_float2(b.x, b.y); f.p[3] = make_float2(b.z, b.w);
+    }
+    return f;
+}
+template <typename X>
+__device__ __forceinline__ void store_pairs(unsigned char* at, const Unit8& f) {
+    uint4* to = reinterpret_cast<uint4*>(at);
+    if constexpr (sizeof(X) == 2) {
+        st_stream(to, make_uint4(cvt_bf16x2(f.p[0]), cvt_bf16x2(f.p[1]), cvt_bf16x2(f.p[2]), cvt_bf16x2(f.p[3])));
+    } else {
+        st_stream(to, make_uint4(__float_as_uint(f.p[0].x), __float_as_uint(f.p[0].y), __float_as_uint(f.p[1].x), __float_as_uint(f.p[1].y)));
+        st_stream(to + 1, make_uint4(__float_as_uint(f.p[2].x), __float_as_uint(f.p[2].y), __float_as_uint(f.p[3].x), __float_as_uint(f.p[3].y)));
+    }
+}
+__device__ __forceinline__ void clear(Unit8& f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.p[j] = make_float2(0.0f, 0.0f);
+}
+__device__ __forceinline__ Unit8 load_weight_pairs(const float* w, int un) {   // a NULL weight is 1
+    Unit8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.p[i] = both(1.0f);
+    if (w) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(w) + 2 * un), b = __ldg(reinterpret_cast<const float4*>(w) + 2 * un + 1);
+        f.p[0] = make_float2(a.x, a.y); f.p[1] = make_float2(a.z, a.w); f.p[2] = make_float2(b.x, b.y); f.p[3] = make_float2(b.z, b.w);
+    }
+    return f;
+}
+
 template <int VEC>
 __device__ __forceinline__ void load_weight(const float* w, int at, float* f) {   // a NULL weight is 1
     if constexpr (VEC == 8) {
@@ -108,19 +154,35 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
     return __half22float2(__half2(h));
 }
+__device__ __forceinline__ void widen_e4m3(const uint2& w, float* f) {
+    const float2 a = e4m3x2_to_float2(w.x & 0xffffu), b = e4m3x2_to_float2(w.x >> 16);
+    const float2 c = e4m3x2_to_float2(w.y & 0xffffu), d = e4m3x2_to_float2(w.y >> 16);
+    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+}
 template <int VEC>
 __device__ __forceinline__ void load_e4m3(const uint8_t* base, size_t at, float* f) {
     if constexpr (VEC == 8) {
-        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(base + at));
-        const float2 a = e4m3x2_to_float2(w.x & 0xffffu), b = e4m3x2_to_float2(w.x >> 16);
-        const float2 c = e4m3x2_to_float2(w.y & 0xffffu), d = e4m3x2_to_float2(w.y >> 16);
-        f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+        widen_e4m3(__ldcs(reinterpret_cast<const uint2*>(base + at)), f);
     } else {
         f[0] = e4m3x2_to_float2(base[at]).x;
     }
 }
 
 constexpr int kRedFloats = 2 * 32 * 3;   // per group: two strips of 32 warps x up to 3 values
+__device__ __forceinline__ Unit8 load_codes(const unsigned char* at) {
+    const uint2 w = *reinterpret_cast<const uint2*>(at);
+    Unit8 f;
+    f.p[0] = e4m3x2_to_float2(w.x & 0xffffu); f.p[1] = e4m3x2_to_float2(w.x >> 16);
+    f.p[2] = e4m3x2_to_float2(w.y & 0xffffu); f.p[3] = e4m3x2_to_float2(w.y >> 16);
+    return f;
+}
+__device__ __forceinline__ void store_codes(uint8_t* at, const Unit8& f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __nv_cvt_float2_to_fp8x2(f.p[i], __NV_SATFINITE, __NV_E4M3);
+    *reinterpret_cast<uint2*>(at) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+}
+
 // Sum of N values over the threads of a row group, the same bits in every thread.  red: the group's own two
 // shared strips, used alternately, so that one barrier per sum is enough.
 template <int N>
@@ -137,14 +199,72 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* red, int& parity
 #pragma unroll
         for (int i = 0; i < N; ++i) strip[w * N + i] = v[i];
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
+    const int mine = threadIdx.x % kWarp;   // a partial a lane, added in the same tree by every warp
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.0f;
-    for (int k = 0; k < warps; ++k)
+    for (int i = 0; i < N; ++i) {
+        v[i] = mine < warps ? strip[mine * N + i] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += strip[k * N + i];
+        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
 }
 
-// NV > 0: the row stays in registers (NV units a thread).  NV == 0: any length; the row is read again after each sum.
+__device__ int g_norm_flags = 0;   // bit 0: a bounded wait for a row gave up
+
+// One group's ring: D places of `stage` bytes, a barrier each.
+struct RowRing {
+    unsigned char* base;
+    uint64_t* bars;
+    int stage, depth, place;
+    uint32_t phase;
+    bool dead;   // a wait (half a second) was given up: nothing is waited for any more
+    __device__ __forceinline__ unsigned char* wait() {   // the place whose row is next, once it is there
+        if (!dead && !mbar_wait_bounded(bars + place, phase, 1u << 17)) { dead = true; atomicOr(&g_norm_flags, 1); }
+        return base + (size_t)place * stage;
+    }
+    __device__ __forceinline__ void leave() {   // copies that were not waited for may still be on their way: hundreds of times their latency
+        if (dead)
+            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+    __device__ __forceinline__ void next() {
+        if (++place == depth) { place = 0; phase ^= 1u; }
+    }
+};
+// What a row needs besides its elements (s: its row of the block's output, -1: none); a group's table holds 64 rows of
+// them, by the row's number within the group.
+struct RowInfo { int s; float gate, q, r; };
+constexpr int kTable = 64;
+__device__ __forceinline__ int output_row(const int32_t* slot, bool branch, long long rows, int T, long long t) {
+    if (!branch || t >= T) return -1;
+    const long long s = slot ? (long long)slot[t] : t;
+    return s >= rows ? -1 : (int)s;
+}
+__device__ __forceinline__ RowInfo info_of(const NormArgs& a, long long t) {
+    return {output_row(a.slot, a.y != nullptr, a.rows, a.T, t), t < a.T && a.gate ? a.gate[t] : 1.0f, 0.0f, 0.0f};
+}
+template <bool CK>
+__device__ __forceinline__ RowInfo info_of(const NormGradArgs& a, bool branch, long long t) {
+    RowInfo f{output_row(a.slot, branch, a.rows, a.T, t), 1.0f, 0.0f, 0.0f};
+    if (t >= a.T) return f;
+    if (a.gate) f.gate = a.gate[t];
+    if constexpr (CK) {
+        if (a.dn) f.q = a.r_pre[t];
+        if (branch) f.r = a.r_post[t];
+    }
+    return f;
+}
+
+// Rings of all groups lie one after the other, then their barriers (16 bytes a place are kept, so that what follows is aligned).
+__device__ __forceinline__ RowRing ring_of(unsigned char* smem, int group, int groups, int depth, int stage) {
+    RowRing r{smem + (size_t)group * depth * stage, reinterpret_cast<uint64_t*>(smem + (size_t)groups * depth * stage) + group * depth, stage,
+              depth, 0, 0u, false};
+    for (int i = threadIdx.x; i < groups * depth; i += blockDim.x) mbar_init(reinterpret_cast<uint64_t*>(smem + (size_t)groups * depth * stage) + i, 1);
+    mbar_init_fence();
+    __syncthreads();
+    return r;
+}
+
+// Rows that bulk copies cannot move (or too long for a ring).  NV > 0: the row stays in registers (NV units a thread).
+// NV == 0: any length; the row is read again after each sum.
 template <typename X, int VEC, int NV>
 __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
@@ -157,11 +277,12 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
     const int units = a.H / VEC;
     const bool want_pre = a.n_out || a.x8 || a.r_pre;
     constexpr int R = (NV > 0 ? NV : 1) * VEC;
-    for (long long t = (long long)blockIdx.x * a.groups + group; t < a.T; t += (long long)gridDim.x * a.groups) {
-        long long s = !a.y ? -1 : a.slot ? (long long)a.slot[t] : t;
-        if (s >= a.rows) s = -1;   // no row of the buffer
+    const long long t_step = (long long)gridDim.x * a.groups;
+    for (long long t = (long long)blockIdx.x * a.groups + group; t < a.T; t += t_step) {
+        const RowInfo f = info_of(a, t);
+        const long long s = f.s;
         const size_t at_t = (size_t)t * a.H, at_s = s < 0 ? 0 : (size_t)s * a.H;
-        const float gate = a.gate ? a.gate[t] : 1.0f;
+        const float gate = f.gate;
         float v[R], h[R];
         float sum[1] = {0.0f};
         if constexpr (NV > 0) {
@@ -189,7 +310,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
             }
         }
         if (a.y) group_sum(sum, red, parity, group, tpr);
-        const float r = 1.0f / sqrtf(fmaf(sum[0], inv_h, a.eps));
+        const float r = rsqrtf(fmaf(sum[0], inv_h, a.eps));
         if (a.r_post && lane == 0) a.r_post[t] = r;
         const float gr = gate;
         // h' of unit `un` into h[], u into v[]
@@ -240,7 +361,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
         }
         if (want_pre) {
             group_sum(ss, red, parity, group, tpr);
-            const float q = 1.0f / sqrtf(fmaf(ss[0], inv_h, a.eps));
+            const float q = rsqrtf(fmaf(ss[0], inv_h, a.eps));
             if (a.r_pre && lane == 0) a.r_pre[t] = q;
             if constexpr (NV > 0) {
 #pragma unroll
@@ -263,11 +384,11 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
     }
 }
 
-// Gradient.  CK: normalised rows from E4M3 and their reciprocal norms, else h' and y as stored.
+// Its gradient.  CK: normalised rows from E4M3 and their reciprocal norms, else h' and y as stored.
 template <typename X, int VEC, int NV, bool CK>
 __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
-    extern __shared__ float cols[];   // [2][H]: the groups' column sums, joined in group order (NV > 0, several groups)
+    extern __shared__ float cols[];   // [2][H]: the groups' column sums, joined in group order at the end
     pdl_wait();
     pdl_trigger();
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
@@ -290,11 +411,13 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
                 if (mine_pre) mine_pre[un * VEC + j] = 0.0f;
             }
     }
-    for (long long t = (long long)blockIdx.x * a.groups + group; t < a.T; t += (long long)gridDim.x * a.groups) {
-        long long s = !branch ? -1 : a.slot ? (long long)a.slot[t] : t;
-        if (s >= a.rows) s = -1;   // no row of the buffer
+    const long long t_step = (long long)gridDim.x * a.groups;
+    for (long long t = (long long)blockIdx.x * a.groups + group; t < a.T; t += t_step) {
+        const RowInfo f = info_of<CK>(a, branch, t);
+        const long long s = f.s;
         const size_t at_t = (size_t)t * a.H, at_s = s < 0 ? 0 : (size_t)s * a.H;
-        const float gate = a.gate ? a.gate[t] : 1.0f;
+        const float gate = f.gate;
+        float q = f.q, r = f.r;
         float x[R], u[R], dn[R], D[R];
         // one unit of the four inputs; x / u are h' / v (or the normalised values with CK), missing ones zero
         auto load = [&](int un, float* xv, float* uv, float* nv, float* dv) {
@@ -333,13 +456,9 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
             for (int un = lane; un < units; un += tpr) { load(un, x, u, dn, D); gather(un, x, u, dn); }
         }
         group_sum(sum, red, parity, group, tpr);
-        float q, r;
-        if constexpr (CK) {
-            q = a.dn ? a.r_pre[t] : 0.0f;
-            r = branch ? a.r_post[t] : 0.0f;
-        } else {
-            q = 1.0f / sqrtf(fmaf(sum[0], inv_h, a.eps));
-            r = 1.0f / sqrtf(fmaf(sum[1], inv_h, a.eps));
+        if constexpr (!CK) {
+            q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+            r = rsqrtf(fmaf(sum[1], inv_h, a.eps));
         }
         const float xs = CK ? 1.0f : q, us = CK ? 1.0f : r;   // what turns x, u into normalised values
         const float c1 = sum[2] * xs * inv_h;
@@ -472,6 +591,301 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
     }
 }
 
+// ---- ring kernels: rows of whole 16-byte pieces, two units a thread ----
+constexpr int kFwdThreads = 640, kGradThreads = 384, kGradLongThreads = 512;   // of a CTA, which has an SM to itself
+
+// FULL: every thread has two units.  CKPT: checkpoints are left.
+template <typename X, bool FULL, bool CKPT>
+__global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const NormArgs a) {
+    __shared__ float red_all[kMaxGroups * kRedFloats];
+    extern __shared__ __align__(128) unsigned char ring_mem[];
+    pdl_wait();
+    pdl_trigger();
+    constexpr int UB = 8 * sizeof(X);   // bytes of a unit
+    const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
+    float* red = red_all + group * kRedFloats;
+    int parity = 0;
+    const float inv_h = 1.0f / (float)a.H;
+    const int units = a.H / 8;
+    const bool want_pre = a.n_out || (CKPT && a.x8);
+    const int t_first = (int)(blockIdx.x * a.groups + group), t_step = (int)(gridDim.x * a.groups);
+    const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X));
+    RowInfo* table = reinterpret_cast<RowInfo*>(ring_mem + (size_t)a.groups * a.depth * (2 * row_bytes + 16)) + group * kTable;
+    for (int i = lane; i < kTable; i += tpr) table[i] = info_of(a, t_first + (long long)i * t_step);
+    const bool have[2] = {FULL || lane < units, FULL || lane + tpr < units};
+    const uint32_t off[2] = {(uint32_t)(lane * UB), (uint32_t)((lane + tpr) * UB)};
+    Unit8 wp[2], wn[2];   // this thread's columns of the weights
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (have[i]) { wp[i] = load_weight_pairs(a.w_post, lane + i * tpr); wn[i] = load_weight_pairs(a.w_pre, lane + i * tpr); }
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)row_bytes);   // places of [h][y]; with a barrier of the CTA
+    auto ask = [&](long long t, int s, int place) {   // by one thread of the group
+        if (t >= a.T) return;
+        uint64_t* bar = ring.bars + place;
+        unsigned char* to = ring.base + (size_t)place * ring.stage;
+        mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
+        bulk_g2s(to, static_cast<const unsigned char*>(a.h) + t * row_bytes, row_bytes, bar);
+        if (s >= 0) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.y) + (size_t)s * row_bytes, row_bytes, bar);
+    };
+    if (lane == 0)
+        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d);
+    RowInfo soon{};
+    int n = 0;   // the row's number within the group
+    for (int t = t_first; t < a.T; t += t_step, ++n) {
+        const size_t row = (size_t)t * row_bytes;
+        const RowInfo f = table[n & (kTable - 1)];
+        if (lane < 32) {
+            if ((n & 31) == 0 && n > 0) soon = info_of(a, t + (32 + lane) * (long long)t_step);
+            if ((n & 31) == 16 && n > 32) table[(n + 16 + lane) & (kTable - 1)] = soon;
+        }
+        const unsigned char* place = ring.wait();
+        Unit8 h[2], v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (!FULL && !have[i]) { clear(h[i]); clear(v[i]); continue; }
+            h[i] = load_pairs<X>(place + off[i]);
+            v[i] = load_pairs<X>(place + row_bytes + off[i]);
+            if (f.s < 0) clear(v[i]);   // nothing came
+        }
+        float2 acc = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc = __ffma2_rn(v[i].p[j], v[i].p[j], acc);
+        float sum[1] = {acc.x + acc.y};
+        group_sum(sum, red, parity, group, tpr);
+        __syncwarp();
+        if (lane == 0) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place);   // the group has taken the row
+        ring.next();
+        const float r = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+        if (CKPT && a.r_post && lane == 0) a.r_post[t] = r;
+        const float2 g2 = both(f.gate), r2 = both(r), a2 = both(a.res_scale);
+        acc = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (have[i]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[i].p[j] = __fmul2_rn(v[i].p[j], r2);
+                    h[i].p[j] = __ffma2_rn(__fmul2_rn(g2, wp[i].p[j]), v[i].p[j], __fmul2_rn(a2, h[i].p[j]));
+                    acc = __ffma2_rn(h[i].p[j], h[i].p[j], acc);
+                }
+                if (a.h_out) store_pairs<X>(static_cast<unsigned char*>(a.h_out) + row + off[i], h[i]);
+                if (CKPT && a.u8) store_codes(a.u8 + (size_t)t * a.H + (lane + i * tpr) * 8, v[i]);
+            }
+        if (!want_pre) continue;
+        sum[0] = acc.x + acc.y;
+        group_sum(sum, red, parity, group, tpr);
+        const float q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+        if (CKPT && a.r_pre && lane == 0) a.r_pre[t] = q;
+        const float2 q2 = both(q);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (have[i]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[i].p[j] = __fmul2_rn(h[i].p[j], q2);
+                if (CKPT && a.x8) store_codes(a.x8 + (size_t)t * a.H + (lane + i * tpr) * 8, h[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[i].p[j] = __fmul2_rn(h[i].p[j], wn[i].p[j]);
+                if (a.n_out) store_pairs<X>(static_cast<unsigned char*>(a.n_out) + row + off[i], h[i]);
+            }
+    }
+    ring.leave();
+}
+
+// Gradient.  Written with the raw rows x', u' (x = xs x', u = us u'; codes: xs = us = 1):
+//   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    e = D w_post,  k = us sum(e u')
+//   dv = R r e - cu u',  cu = R r us k / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
+// MAXT: threads of the CTA at most; up to kGradThreads (rows of 6144) the weights fit into registers.  FULL: every thread
+// has two units.
+template <typename X, bool CK, int MAXT, bool FULL>
+__global__ void __launch_bounds__(MAXT) block_norm_grad_ring_kernel(const NormGradArgs a) {
+    constexpr bool kKept = MAXT == kGradThreads;
+    __shared__ float red_all[kMaxGroups * kRedFloats];
+    extern __shared__ __align__(128) unsigned char ring_mem[];
+    pdl_wait();
+    pdl_trigger();
+    const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
+    float* red = red_all + group * kRedFloats;
+    int parity = 0;
+    const float inv_h = 1.0f / (float)a.H;
+    const int units = a.H / 8;
+    const bool branch = CK ? a.u8 != nullptr : a.y != nullptr;
+    const bool need_k = branch && (a.dgate || a.dy);
+    constexpr int UB = 8 * sizeof(X), AB = CK ? 8 : UB;   // bytes of a unit of the rows and of the activations
+    const int t_first = (int)(blockIdx.x * a.groups + group), t_step = (int)(gridDim.x * a.groups);
+    const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X)), act_bytes = CK ? (uint32_t)a.H : row_bytes;
+    unsigned char* after = ring_mem + (size_t)a.groups * a.depth * (2 * (row_bytes + act_bytes) + 16);
+    RowInfo* table = reinterpret_cast<RowInfo*>(after) + group * kTable;
+    for (int i = lane; i < kTable; i += tpr) table[i] = info_of<CK>(a, branch, t_first + (long long)i * t_step);
+    const bool have[2] = {FULL || lane < units, FULL || lane + tpr < units};
+    const uint32_t off[2] = {(uint32_t)(lane * UB), (uint32_t)((lane + tpr) * UB)}, act[2] = {(uint32_t)(lane * AB), (uint32_t)((lane + tpr) * AB)};
+    Unit8 wp[2], wn[2];
+    float* w_shared = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H], where they are not kept
+    if constexpr (kKept) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (have[i]) { wp[i] = load_weight_pairs(a.w_post, lane + i * tpr); wn[i] = load_weight_pairs(a.w_pre, lane + i * tpr); }
+    } else {
+        for (int c = threadIdx.x; c < a.H; c += blockDim.x) {
+            w_shared[c] = a.w_post ? a.w_post[c] : 1.0f;
+            w_shared[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
+        }
+    }
+    auto weight = [&](bool post, int i) {
+        if constexpr (kKept) return post ? wp[i] : wn[i];
+        else return load_pairs<float>(reinterpret_cast<const unsigned char*>(w_shared + (post ? 0 : a.H) + (lane + i * tpr) * 8));
+    };
+    // places of [dh_out][dn][h_out or x8][y or u8]; with a barrier of the CTA
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_bytes + act_bytes));
+    auto ask = [&](long long t, int s, int place) {   // by one thread of the group
+        if (t >= a.T) return;
+        uint64_t* bar = ring.bars + place;
+        unsigned char* to = ring.base + (size_t)place * ring.stage;
+        mbar_expect_tx(bar, (a.dh_out ? row_bytes : 0u) + (a.dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
+        if (a.dh_out) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
+        if (a.dn) {
+            bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
+            bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
+        }
+        if (s >= 0)   // codes lie in token order, the block's output in slot order
+            bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
+    };
+    if (lane == 0)
+        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d);
+    Unit8 acc_post[2], acc_pre[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { acc_post[i].p[j] = both(0.0f); acc_pre[i].p[j] = both(0.0f); }
+    RowInfo soon{};
+    int n = 0;   // the row's number within the group
+    for (int t = t_first; t < a.T; t += t_step, ++n) {
+        const size_t row = (size_t)t * row_bytes;
+        const RowInfo f = table[n & (kTable - 1)];
+        if (lane < 32) {
+            if ((n & 31) == 0 && n > 0) soon = info_of<CK>(a, branch, t + (32 + lane) * (long long)t_step);
+            if ((n & 31) == 16 && n > 32) table[(n + 16 + lane) & (kTable - 1)] = soon;
+        }
+        const unsigned char* place = ring.wait();
+        Unit8 x[2], u[2], dn[2], D[2];
+        float2 sx = both(0.0f), su = both(0.0f), sg = both(0.0f);   // x'^2, u'^2, dn w_pre x'
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (!FULL && !have[i]) { clear(x[i]); clear(u[i]); clear(dn[i]); clear(D[i]); continue; }
+            D[i] = load_pairs<X>(place + off[i]);
+            dn[i] = load_pairs<X>(place + row_bytes + off[i]);
+            if constexpr (CK) {
+                x[i] = load_codes(place + 2 * row_bytes + act[i]);
+                u[i] = load_codes(place + 2 * row_bytes + act_bytes + act[i]);
+            } else {
+                x[i] = load_pairs<X>(place + 2 * row_bytes + act[i]);
+                u[i] = load_pairs<X>(place + 2 * row_bytes + act_bytes + act[i]);
+            }
+            if (!a.dh_out) clear(D[i]);   // nothing came
+            if (!a.dn) { clear(dn[i]); clear(x[i]); }
+            if (f.s < 0) clear(u[i]);
+            const Unit8 w = weight(false, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (!CK) sx = __ffma2_rn(x[i].p[j], x[i].p[j], sx);
+                if (!CK) su = __ffma2_rn(u[i].p[j], u[i].p[j], su);
+                sg = __ffma2_rn(__fmul2_rn(dn[i].p[j], w.p[j]), x[i].p[j], sg);
+            }
+        }
+        float q = f.q, r = f.r, xs = 1.0f, us = 1.0f, dot;
+        if constexpr (CK) {
+            float sum[1] = {sg.x + sg.y};
+            group_sum(sum, red, parity, group, tpr);
+            dot = sum[0];
+        } else {
+            float sum[3] = {sx.x + sx.y, su.x + su.y, sg.x + sg.y};
+            group_sum(sum, red, parity, group, tpr);
+            xs = q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+            us = r = rsqrtf(fmaf(sum[1], inv_h, a.eps));
+            dot = sum[2];
+        }
+        __syncwarp();
+        if (lane == 0) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place);   // the group has taken the row
+        ring.next();
+        const float2 q2 = both(q), cx = both(-q * xs * (dot * xs * inv_h));
+        float2 sk = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (have[i]) {
+                {
+                    const Unit8 w = weight(false, i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) D[i].p[j] = __ffma2_rn(cx, x[i].p[j], __ffma2_rn(q2, __fmul2_rn(dn[i].p[j], w.p[j]), D[i].p[j]));
+                }
+                if (need_k) {
+                    const Unit8 w = weight(true, i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sk = __ffma2_rn(__fmul2_rn(D[i].p[j], w.p[j]), u[i].p[j], sk);
+                }
+            }
+        float k[1] = {sk.x + sk.y};
+        if (need_k) group_sum(k, red, parity, group, tpr);
+        k[0] *= us;
+        if (a.dgate && lane == 0) a.dgate[t] = k[0];
+        const float rg = r * f.gate;
+        const float2 rg2 = both(rg), cu = both(-rg * us * (k[0] * inv_h)), gu = both(f.gate * us), xs2 = both(xs), a2 = both(a.res_scale);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (have[i]) {
+                Unit8 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc_post[i].p[j] = __ffma2_rn(gu, __fmul2_rn(D[i].p[j], u[i].p[j]), acc_post[i].p[j]);
+                    acc_pre[i].p[j] = __ffma2_rn(xs2, __fmul2_rn(dn[i].p[j], x[i].p[j]), acc_pre[i].p[j]);
+                }
+                if (a.dy && f.s >= 0) {
+                    const Unit8 w = weight(true, i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o.p[j] = __ffma2_rn(cu, u[i].p[j], __fmul2_rn(rg2, __fmul2_rn(D[i].p[j], w.p[j])));
+                    store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)f.s * row_bytes + off[i], o);
+                }
+                if (a.dh) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o.p[j] = __fmul2_rn(a2, D[i].p[j]);
+                    store_pairs<X>(static_cast<unsigned char*>(a.dh) + row + off[i], o);
+                }
+            }
+    }
+    ring.leave();
+    if (a.part_post || a.part_pre) {   // groups add their columns one after the other, where the ring was: a fixed order
+        float* cols = reinterpret_cast<float*>(ring_mem);   // [2][H]
+        __syncthreads();
+        for (int g = 0; g < a.groups; ++g) {
+            if (group == g)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (have[i])
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = (lane + i * tpr) * 8 + 2 * j;
+                            float2* post = reinterpret_cast<float2*>(cols + c);
+                            float2* pre = reinterpret_cast<float2*>(cols + a.H + c);
+                            float2 p = acc_post[i].p[j], m = acc_pre[i].p[j];
+                            if (g) { p = __fadd2_rn(p, *post); m = __fadd2_rn(m, *pre); }
+                            if (g + 1 < a.groups) { *post = p; *pre = m; }
+                            else {
+                                if (a.part_post) *reinterpret_cast<float2*>(a.part_post + (size_t)blockIdx.x * a.H + c) = p;
+                                if (a.part_pre) *reinterpret_cast<float2*>(a.part_pre + (size_t)blockIdx.x * a.H + c) = m;
+                            }
+                        }
+            __syncthreads();
+        }
+    }
+    if (a.dy && a.inv) {   // rows of the slot buffer that no token owns have a zero gradient
+        const Unit8 z{{both(0.0f), both(0.0f), both(0.0f), both(0.0f)}};
+        for (long long row = t_first; row < a.rows; row += t_step) {
+            if (a.inv[row] >= 0) continue;
+            for (int un = lane; un < units; un += tpr) store_pairs<X>(static_cast<unsigned char*>(a.dy) + row * row_bytes + un * UB, z);
+        }
+    }
+}
+
 // Column sums: the CTAs' rows of the workspace added in index order (fp32, 8 interleaved chains joined in order).
 constexpr int kColThreads = 256, kColChains = 8;
 __global__ void __launch_bounds__(kColThreads) block_norm_cols_kernel(const float* part_post, const float* part_pre, int parts, int H,
@@ -506,25 +920,58 @@ RowPlan plan_rows(int units, int nv, int threads) {
     return {tpr, groups};
 }
 
-constexpr int kGradCtasPerSm = 2;
+constexpr int kGradCtasPerSm = 2;       // at most: one row of column sums each
+constexpr int kRingSmem = 200 << 10;    // shared memory of an SM that rings may take
+constexpr int kRingMaxDepth = 4;
 
 bool aligned(const void* p, int n) { return (uintptr_t)p % n == 0; }
+
+// Rings of `groups` groups with `stage` bytes a row beside `extra` bytes: their depth, 0 if two rows do not fit; and the
+// shared memory of rings, barriers and tables.
+int ring_depth(int groups, int stage, int extra) {
+    int d = (kRingSmem - extra - groups * kTable * (int)sizeof(RowInfo)) / (groups * (stage + 16));
+    if (d > kRingMaxDepth) d = kRingMaxDepth;
+    return d < 2 ? 0 : d;
+}
+size_t ring_bytes(int groups, int depth, int stage) { return (size_t)groups * (depth * (stage + 16) + kTable * sizeof(RowInfo)); }
+template <typename K>
+bool allow_smem(K kernel, size_t bytes) {
+    if (bytes <= 32 << 10) return true;   // with the static strips within the 48 KB that need no leave
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess) return true;
+    cudaGetLastError();
+    return false;
+}
 
 template <typename X>
 int forward(NormArgs& a, cudaStream_t st) {
     const bool wide = a.H % 8 == 0 && aligned(a.h, 16) && aligned(a.y, 16) && aligned(a.h_out, 16) && aligned(a.n_out, 16) &&
                       aligned(a.w_post, 16) && aligned(a.w_pre, 16) && aligned(a.u8, 8) && aligned(a.x8, 8);
     const int units = wide ? a.H / 8 : a.H;
-    const int nv = wide ? (units <= 1024 * 2 ? 2 : 0) : (units <= 1024 * 8 ? 8 : 0);
+    auto launch = [&](auto kernel, const RowPlan& p, int ctas, size_t smem) {
+        a.tpr = p.tpr; a.groups = p.groups;
+        const int threads = p.tpr * p.groups;
+        long long grid = (a.T + p.groups - 1) / p.groups;
+        const long long most = (long long)sm_count() * ctas;
+        if (grid > most) grid = most;
+        if (!allow_smem(kernel, smem)) return (int)LOCMOE_ERR_CUDA;
+        return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
+    };
+    if (wide && units <= 2 * kFwdThreads) {
+        const RowPlan p = plan_rows(units, 2, kFwdThreads);
+        const int stage = 2 * a.H * (int)sizeof(X);
+        a.depth = ring_depth(p.groups, stage, 0);
+        const size_t smem = ring_bytes(p.groups, a.depth, stage);
+        if (a.depth) {
+            const bool full = units == 2 * p.tpr;
+            if (a.u8 || a.x8) return full ? launch(block_norm_ring_kernel<X, true, true>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, true>, p, 1, smem);
+            return full ? launch(block_norm_ring_kernel<X, true, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false>, p, 1, smem);
+        }
+    }
+    const int nv = wide ? 0 : (units <= 1024 * 8 ? 8 : 0);
     const RowPlan p = plan_rows(units, nv, 256);
-    a.tpr = p.tpr; a.groups = p.groups;
-    const int threads = p.tpr * p.groups;
-    long long grid = (a.T + p.groups - 1) / p.groups;
-    const long long most = (long long)sm_count() * (2048 / threads > 0 ? 2048 / threads : 1);
-    if (grid > most) grid = most;
-    auto run = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), 0, st, a); };
-    if (wide) return nv ? run(block_norm_kernel<X, 8, 2>) : run(block_norm_kernel<X, 8, 0>);
-    return nv ? run(block_norm_kernel<X, 1, 8>) : run(block_norm_kernel<X, 1, 0>);
+    const int ctas = 2048 / (p.tpr * p.groups) > 0 ? 2048 / (p.tpr * p.groups) : 1;
+    if (wide) return launch(block_norm_kernel<X, 8, 0>, p, ctas, 0);
+    return nv ? launch(block_norm_kernel<X, 1, 8>, p, ctas, 0) : launch(block_norm_kernel<X, 1, 0>, p, ctas, 0);
 }
 
 template <typename X, bool CK>
@@ -532,19 +979,42 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     const bool wide = a.H % 8 == 0 && aligned(a.dh_out, 16) && aligned(a.dn, 16) && aligned(a.h_out, 16) && aligned(a.y, 16) &&
                       aligned(a.x8, 8) && aligned(a.u8, 8) && aligned(a.w_post, 16) && aligned(a.w_pre, 16) && aligned(a.dh, 16) &&
                       aligned(a.dy, 16);
+    const bool bulk = wide && (!CK || (a.H % 16 == 0 && aligned(a.x8, 16) && aligned(a.u8, 16)));   // rows that bulk copies can move
     const int units = wide ? a.H / 8 : a.H;
-    const int nv = wide ? (units <= 512 ? 1 : 0) : (units <= 512 * 8 ? 8 : 0);
-    const RowPlan p = plan_rows(units, nv, 512);
-    a.tpr = p.tpr; a.groups = p.groups;
-    const int threads = p.tpr * p.groups;
-    long long grid = (a.T + p.groups - 1) / p.groups;
-    const long long most = (long long)sm_count() * kGradCtasPerSm;
-    if (grid > most) grid = most;
-    const size_t smem = nv && p.groups > 1 ? (size_t)a.H * 8 : 0;
-    auto run = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a); };
-    int rc;
-    if (wide) rc = nv ? run(block_norm_grad_kernel<X, 8, 1, CK>) : run(block_norm_grad_kernel<X, 8, 0, CK>);
-    else rc = nv ? run(block_norm_grad_kernel<X, 1, 8, CK>) : run(block_norm_grad_kernel<X, 1, 0, CK>);
+    long long grid = 0;
+    auto launch = [&](auto kernel, const RowPlan& p, int ctas, size_t smem) {
+        a.tpr = p.tpr; a.groups = p.groups;
+        const int threads = p.tpr * p.groups;
+        grid = (a.T + p.groups - 1) / p.groups;
+        const long long most = (long long)sm_count() * ctas;
+        if (grid > most) grid = most;
+        if (!allow_smem(kernel, smem)) return (int)LOCMOE_ERR_CUDA;
+        return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
+    };
+    int rc = LOCMOE_OK;
+    bool done = false;
+    if (bulk && units <= 2 * kGradLongThreads) {
+        const bool kept = units <= 2 * kGradThreads;
+        const RowPlan p = plan_rows(units, 2, kept ? kGradThreads : kGradLongThreads);
+        const int stage = 2 * a.H * ((int)sizeof(X) + (CK ? 1 : (int)sizeof(X))), extra = kept ? 0 : 8 * a.H;
+        a.depth = ring_depth(p.groups, stage, extra);
+        if (a.depth) {
+            const size_t smem = ring_bytes(p.groups, a.depth, stage) + extra;
+            const bool full = units == 2 * p.tpr;
+            if (!kept) rc = launch(block_norm_grad_ring_kernel<X, CK, kGradLongThreads, false>, p, 1, smem);
+            else rc = full ? launch(block_norm_grad_ring_kernel<X, CK, kGradThreads, true>, p, 1, smem)
+                           : launch(block_norm_grad_ring_kernel<X, CK, kGradThreads, false>, p, 1, smem);
+            done = true;
+        }
+    }
+    if (!done) {
+        const int nv = wide ? 0 : (units <= 512 * 8 ? 8 : 0);
+        const RowPlan p = plan_rows(units, nv, 512);
+        const size_t smem = nv && p.groups > 1 ? (size_t)a.H * 8 : 0;
+        if (wide) rc = launch(block_norm_grad_kernel<X, 8, 0, CK>, p, kGradCtasPerSm, smem);
+        else rc = nv ? launch(block_norm_grad_kernel<X, 1, 8, CK>, p, kGradCtasPerSm, smem)
+                     : launch(block_norm_grad_kernel<X, 1, 0, CK>, p, kGradCtasPerSm, smem);
+    }
     if (rc || (!dw_post && !dw_pre)) return rc;
     return launch_pdl(block_norm_cols_kernel, dim3((a.H + 31) / 32, 2), dim3(kColThreads), 0, st, a.part_post, a.part_pre, (int)grid,
                       a.H, dw_post, dw_pre);
@@ -560,7 +1030,7 @@ size_t block_norm_grad_ws_bytes(const locmoe_shape_t& s) {
 
 int launch_block_norm(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_t& b, cudaStream_t st) {
     NormArgs a{b.h, b.y, b.slot, b.gate_w, b.w_post, b.w_pre, b.res_scale, b.eps, b.h_out, b.n_out, b.u8, b.x8, b.r_post, b.r_pre,
-               rows, s.T, s.H, 0, 0};
+               rows, s.T, s.H, 0, 0, 0};
     return s.x_dtype == LOCMOE_F32 ? forward<float>(a, st) : forward<uint16_t>(a, st);
 }
 
@@ -568,11 +1038,20 @@ int launch_block_norm_grad(const locmoe_shape_t& s, long long rows, const locmoe
     float* part = static_cast<float*>(ws);
     NormGradArgs a{b.dh_out, b.dn, b.h_out, b.y, b.x8, b.u8, b.r_pre, b.r_post, b.slot, b.slot ? b.inv : nullptr, b.gate_w, b.w_post,
                    b.w_pre, b.res_scale, b.eps, b.dh, b.dy, b.dgate, b.dw_post ? part : nullptr,
-                   b.dw_pre ? part + (size_t)sm_count() * kGradCtasPerSm * s.H : nullptr, rows, s.T, s.H, 0, 0};
+                   b.dw_pre ? part + (size_t)sm_count() * kGradCtasPerSm * s.H : nullptr, rows, s.T, s.H, 0, 0, 0};
     const bool ck = b.x8 || b.u8;
     if (s.x_dtype == LOCMOE_F32)
         return ck ? backward<float, true>(a, b.dw_post, b.dw_pre, st) : backward<float, false>(a, b.dw_post, b.dw_pre, st);
     return ck ? backward<uint16_t, true>(a, b.dw_post, b.dw_pre, st) : backward<uint16_t, false>(a, b.dw_post, b.dw_pre, st);
+}
+
+int read_norm_flags(int* out, cudaStream_t st) {
+    if (cudaMemcpyFromSymbolAsync(out, g_norm_flags, sizeof(int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    return LOCMOE_OK;
 }
 
 }  // namespace locmoe

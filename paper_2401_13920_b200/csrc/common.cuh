@@ -124,6 +124,7 @@ int launch_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, const void* 
 int read_ffn_flags(int* out, cudaStream_t st);
 void plan_expert_ffn(const locmoe_shape_t& s, int64_t rows, int F, int kernels[2]);
 
+int read_norm_flags(int* out, cudaStream_t st);
 int read_few_flags(int* out, cudaStream_t st);
 size_t few_ws_bytes(const locmoe_shape_t& s, int F, int K);
 int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int K, int F, const void* w_in, const void* w_out,
