@@ -168,9 +168,23 @@ __device__ __forceinline__ void load_e4m3(const uint8_t* base, size_t at, float*
     }
 }
 
-constexpr int kRedFloats = 2 * 32 * 3;   // per group: two strips of 32 warps x up to 3 values
-__device__ __forceinline__ Unit8 load_codes(const unsigned char* at) {
-    const uint2 w = *reinterpret_cast<const uint2*>(at);
+constexpr int kRedFloats = 2 * 32 * 4;   // per group: two strips of up to 4 values x 32 warps
+// A unit of activations as it lies in memory: bf16, fp32 or codes.
+struct alignas(16) RawF32 { float4 a, b; };
+template <typename X, bool CK> struct RawUnit { using type = uint2; };
+template <> struct RawUnit<uint16_t, false> { using type = uint4; };
+template <> struct RawUnit<float, false> { using type = RawF32; };
+template <typename X>
+__device__ __forceinline__ Unit8 widen(const uint4& w) {
+    return {{make_float2(bf16_lo(w.x), bf16_hi(w.x)), make_float2(bf16_lo(w.y), bf16_hi(w.y)), make_float2(bf16_lo(w.z), bf16_hi(w.z)),
+             make_float2(bf16_lo(w.w), bf16_hi(w.w))}};
+}
+template <typename X>
+__device__ __forceinline__ Unit8 widen(const RawF32& w) {
+    return {{make_float2(w.a.x, w.a.y), make_float2(w.a.z, w.a.w), make_float2(w.b.x, w.b.y), make_float2(w.b.z, w.b.w)}};
+}
+template <typename X>
+__device__ __forceinline__ Unit8 widen(const uint2& w) {
     Unit8 f;
     f.p[0] = e4m3x2_to_float2(w.x & 0xffffu); f.p[1] = e4m3x2_to_float2(w.x >> 16);
     f.p[2] = e4m3x2_to_float2(w.y & 0xffffu); f.p[3] = e4m3x2_to_float2(w.y >> 16);
@@ -183,30 +197,56 @@ __device__ __forceinline__ void store_codes(uint8_t* at, const Unit8& f) {
     *reinterpret_cast<uint2*>(at) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
-// Sum of N values over the threads of a row group, the same bits in every thread.  red: the group's own two
-// shared strips, used alternately, so that one barrier per sum is enough.
-template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float* red, int& parity, int group, int tpr) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (tpr == kWarp) return;
-    const int warps = tpr / kWarp, w = (threadIdx.x % tpr) / kWarp;
-    float* strip = red + parity * (kRedFloats / 2);
-    parity ^= 1;
-    if (threadIdx.x % kWarp == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) strip[w * N + i] = v[i];
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
-    const int mine = threadIdx.x % kWarp;   // a partial a lane, added in the same tree by every warp
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = mine < warps ? strip[mine * N + i] : 0.0f;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+// Sums over the threads of a row group, the same bits in every thread.  Each warp adds up its lanes, the warps' partials
+// meet in one of two shared strips used alternately, so that one barrier per sum is enough.
+struct GroupSum {
+    float* strip;      // the next of the two
+    int other;         // from it to the other one, in floats
+    int barrier, tpr, warps, warp, lane;
+    __device__ __forceinline__ GroupSum(float* red, int group, int tpr_) {
+        strip = red; other = kRedFloats / 2; barrier = group + 1; tpr = tpr_; warps = tpr / kWarp;
+        warp = (threadIdx.x - group * tpr) / kWarp; lane = threadIdx.x % kWarp;
     }
-}
+    __device__ __forceinline__ void meet() { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(tpr) : "memory"); }
+    __device__ __forceinline__ void turn() { strip += other; other = -other; }
+    __device__ __forceinline__ float butterfly(float v, int from) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            if (o <= from) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    __device__ __forceinline__ float one(float v) {
+        v = butterfly(v, 16);
+        if (warps == 1) return v;
+        if (lane == 0) strip[warp] = v;
+        meet();
+        v = butterfly(lane < warps ? strip[lane] : 0.0f, 16);
+        turn();
+        return v;
+    }
+    // Three values with a third of the shuffles: lanes first trade values, so that each goes on with one; later a quarter
+    // of the lanes adds up each value's partials.
+    __device__ __forceinline__ void three(float& x, float& y, float& z) {
+        constexpr unsigned full = 0xffffffffu;
+        const bool upper = lane & 16, second = lane & 8;
+        const float a = (upper ? z : x) + __shfl_xor_sync(full, upper ? x : z, 16);
+        const float b = (upper ? 0.0f : y) + __shfl_xor_sync(full, upper ? y : 0.0f, 16);
+        float s = (second ? b : a) + __shfl_xor_sync(full, second ? a : b, 8);
+        s = butterfly(s, 4);   // lanes 0..7: x, 8..15: y, 16..23: z
+        if (warps > 1) {
+            if ((lane & 7) == 0) strip[(lane >> 3) * kWarp + warp] = s;
+            meet();
+            const float* p = strip + (lane >> 3) * kWarp;
+            s = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if ((lane & 7) + 8 * k < warps) s += p[(lane & 7) + 8 * k];
+            s = butterfly(s, 4);
+            turn();
+        }
+        x = __shfl_sync(full, s, 0); y = __shfl_sync(full, s, 8); z = __shfl_sync(full, s, 16);
+    }
+};
 
 __device__ int g_norm_flags = 0;   // bit 0: a bounded wait for a row gave up
 
@@ -231,7 +271,7 @@ struct RowRing {
 };
 // What a row needs besides its elements (s: its row of the block's output, -1: none); a group's table holds 64 rows of
 // them, by the row's number within the group.
-struct RowInfo { int s; float gate, q, r; };
+struct alignas(16) RowInfo { int s; float gate, q, r; };
 constexpr int kTable = 64;
 __device__ __forceinline__ int output_row(const int32_t* slot, bool branch, long long rows, int T, long long t) {
     if (!branch || t >= T) return -1;
@@ -271,8 +311,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
     pdl_wait();
     pdl_trigger();
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    float* red = red_all + group * kRedFloats;
-    int parity = 0;
+    GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
     const int units = a.H / VEC;
     const bool want_pre = a.n_out || a.x8 || a.r_pre;
@@ -309,7 +348,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
                 for (int j = 0; j < VEC; ++j) sum[0] = fmaf(v[j], v[j], sum[0]);
             }
         }
-        if (a.y) group_sum(sum, red, parity, group, tpr);
+        if (a.y) sum[0] = total.one(sum[0]);
         const float r = rsqrtf(fmaf(sum[0], inv_h, a.eps));
         if (a.r_post && lane == 0) a.r_post[t] = r;
         const float gr = gate;
@@ -360,7 +399,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
             }
         }
         if (want_pre) {
-            group_sum(ss, red, parity, group, tpr);
+            ss[0] = total.one(ss[0]);
             const float q = rsqrtf(fmaf(ss[0], inv_h, a.eps));
             if (a.r_pre && lane == 0) a.r_pre[t] = q;
             if constexpr (NV > 0) {
@@ -392,8 +431,7 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
     pdl_wait();
     pdl_trigger();
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    float* red = red_all + group * kRedFloats;
-    int parity = 0;
+    GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
     const int units = a.H / VEC;
     constexpr int R = (NV > 0 ? NV : 1) * VEC;
@@ -455,7 +493,7 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
         } else {
             for (int un = lane; un < units; un += tpr) { load(un, x, u, dn, D); gather(un, x, u, dn); }
         }
-        group_sum(sum, red, parity, group, tpr);
+        total.three(sum[0], sum[1], sum[2]);
         if constexpr (!CK) {
             q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
             r = rsqrtf(fmaf(sum[1], inv_h, a.eps));
@@ -502,7 +540,7 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
             }
         }
         if (need_k) {
-            group_sum(k, red, parity, group, tpr);
+            k[0] = total.one(k[0]);
             if (a.dgate && lane == 0) a.dgate[t] = k[0];
         } else if (a.dgate && lane == 0) {
             a.dgate[t] = 0.0f;
@@ -592,19 +630,18 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
 }
 
 // ---- ring kernels: rows of whole 16-byte pieces, two units a thread ----
-constexpr int kFwdThreads = 640, kGradThreads = 384, kGradLongThreads = 512;   // of a CTA, which has an SM to itself
+constexpr int kRingThreads = 640;   // of a CTA, which has an SM to itself: 102 registers a thread
 
 // FULL: every thread has two units.  CKPT: checkpoints are left.
 template <typename X, bool FULL, bool CKPT>
-__global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const NormArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
     pdl_wait();
     pdl_trigger();
     constexpr int UB = 8 * sizeof(X);   // bytes of a unit
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    float* red = red_all + group * kRedFloats;
-    int parity = 0;
+    GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
     const int units = a.H / 8;
     const bool want_pre = a.n_out || (CKPT && a.x8);
@@ -619,16 +656,19 @@ __global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const Norm
     for (int i = 0; i < 2; ++i)
         if (have[i]) { wp[i] = load_weight_pairs(a.w_post, lane + i * tpr); wn[i] = load_weight_pairs(a.w_pre, lane + i * tpr); }
     RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)row_bytes);   // places of [h][y]; with a barrier of the CTA
-    auto ask = [&](long long t, int s, int place) {   // by one thread of the group
+    // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
+    auto ask = [&](long long t, int s, int place, int from, int by) {
         if (t >= a.T) return;
         uint64_t* bar = ring.bars + place;
-        unsigned char* to = ring.base + (size_t)place * ring.stage;
-        mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
-        bulk_g2s(to, static_cast<const unsigned char*>(a.h) + t * row_bytes, row_bytes, bar);
-        if (s >= 0) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.y) + (size_t)s * row_bytes, row_bytes, bar);
+        unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
+        if (from == 0) mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
+        for (int k = from; k < 2; k += by)
+            if (k == 0) bulk_g2s(to, static_cast<const unsigned char*>(a.h) + t * row_bytes, row_bytes, bar);
+            else if (s >= 0) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.y) + (size_t)s * row_bytes, row_bytes, bar);
     };
+    const int asks = lane % kWarp ? 2 : lane / kWarp;   // from which array on this thread asks (2: none)
     if (lane == 0)
-        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d);
+        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d, 0, 1);
     RowInfo soon{};
     int n = 0;   // the row's number within the group
     for (int t = t_first; t < a.T; t += t_step, ++n) {
@@ -652,12 +692,11 @@ __global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const Norm
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc = __ffma2_rn(v[i].p[j], v[i].p[j], acc);
-        float sum[1] = {acc.x + acc.y};
-        group_sum(sum, red, parity, group, tpr);
+        float sum = total.one(acc.x + acc.y);
         __syncwarp();
-        if (lane == 0) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place);   // the group has taken the row
+        if (asks < 2) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place, asks, tpr / kWarp);   // the group has taken the row
         ring.next();
-        const float r = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+        const float r = rsqrtf(fmaf(sum, inv_h, a.eps));
         if (CKPT && a.r_post && lane == 0) a.r_post[t] = r;
         const float2 g2 = both(f.gate), r2 = both(r), a2 = both(a.res_scale);
         acc = both(0.0f);
@@ -674,9 +713,8 @@ __global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const Norm
                 if (CKPT && a.u8) store_codes(a.u8 + (size_t)t * a.H + (lane + i * tpr) * 8, v[i]);
             }
         if (!want_pre) continue;
-        sum[0] = acc.x + acc.y;
-        group_sum(sum, red, parity, group, tpr);
-        const float q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
+        sum = total.one(acc.x + acc.y);
+        const float q = rsqrtf(fmaf(sum, inv_h, a.eps));
         if (CKPT && a.r_pre && lane == 0) a.r_pre[t] = q;
         const float2 q2 = both(q);
 #pragma unroll
@@ -694,163 +732,174 @@ __global__ void __launch_bounds__(kFwdThreads) block_norm_ring_kernel(const Norm
 }
 
 // Gradient.  Written with the raw rows x', u' (x = xs x', u = us u'; codes: xs = us = 1):
-//   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    e = D w_post,  k = us sum(e u')
-//   dv = R r e - cu u',  cu = R r us k / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
-// MAXT: threads of the CTA at most; up to kGradThreads (rows of 6144) the weights fit into registers.  FULL: every thread
-// has two units.
-template <typename X, bool CK, int MAXT, bool FULL>
-__global__ void __launch_bounds__(MAXT) block_norm_grad_ring_kernel(const NormGradArgs a) {
-    constexpr bool kKept = MAXT == kGradThreads;
+//   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
+//   e = D w_post,  k = us sum(e u'),  dv = R r e - cu u',  cu = R r us k / H
+// Everything but dv is done between the two sums, so that only e and u' are held over the second one, and the weights lie
+// in shared memory.  That is for the registers: what spills comes back through an L1 that the rings leave little of,
+// behind the rings' copies (two units a thread with spills: 1380 us at 65536 x 5120 in bf16).
+// NV: units of a thread, one up to rows of 5120 (640 threads), else two (512 threads).  FULL: every thread has them all.
+// ALL: both upstream gradients, the branch, dh and dy are there.
+template <typename X, bool CK, int NV, bool FULL, bool ALL>
+__global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_ring_kernel(const NormGradArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
     pdl_wait();
     pdl_trigger();
+    constexpr int UB = 8 * sizeof(X), AB = CK ? 8 : UB;   // bytes of a unit of the rows and of the activations
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    float* red = red_all + group * kRedFloats;
-    int parity = 0;
+    GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
     const int units = a.H / 8;
-    const bool branch = CK ? a.u8 != nullptr : a.y != nullptr;
-    const bool need_k = branch && (a.dgate || a.dy);
-    constexpr int UB = 8 * sizeof(X), AB = CK ? 8 : UB;   // bytes of a unit of the rows and of the activations
+    const bool branch = ALL || (CK ? a.u8 != nullptr : a.y != nullptr);
+    const bool has_dn = ALL || a.dn, has_up = ALL || a.dh_out, has_dh = ALL || a.dh, has_dy = ALL || a.dy;
     const int t_first = (int)(blockIdx.x * a.groups + group), t_step = (int)(gridDim.x * a.groups);
     const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X)), act_bytes = CK ? (uint32_t)a.H : row_bytes;
     unsigned char* after = ring_mem + (size_t)a.groups * a.depth * (2 * (row_bytes + act_bytes) + 16);
     RowInfo* table = reinterpret_cast<RowInfo*>(after) + group * kTable;
+    float* weights = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H]: w_post, w_pre
     for (int i = lane; i < kTable; i += tpr) table[i] = info_of<CK>(a, branch, t_first + (long long)i * t_step);
-    const bool have[2] = {FULL || lane < units, FULL || lane + tpr < units};
-    const uint32_t off[2] = {(uint32_t)(lane * UB), (uint32_t)((lane + tpr) * UB)}, act[2] = {(uint32_t)(lane * AB), (uint32_t)((lane + tpr) * AB)};
-    Unit8 wp[2], wn[2];
-    float* w_shared = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H], where they are not kept
-    if constexpr (kKept) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (have[i]) { wp[i] = load_weight_pairs(a.w_post, lane + i * tpr); wn[i] = load_weight_pairs(a.w_pre, lane + i * tpr); }
-    } else {
-        for (int c = threadIdx.x; c < a.H; c += blockDim.x) {
-            w_shared[c] = a.w_post ? a.w_post[c] : 1.0f;
-            w_shared[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
-        }
+    for (int c = threadIdx.x; c < a.H; c += blockDim.x) {
+        weights[c] = a.w_post ? a.w_post[c] : 1.0f;
+        weights[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
     }
-    auto weight = [&](bool post, int i) {
-        if constexpr (kKept) return post ? wp[i] : wn[i];
-        else return load_pairs<float>(reinterpret_cast<const unsigned char*>(w_shared + (post ? 0 : a.H) + (lane + i * tpr) * 8));
-    };
     // places of [dh_out][dn][h_out or x8][y or u8]; with a barrier of the CTA
     RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_bytes + act_bytes));
-    auto ask = [&](long long t, int s, int place) {   // by one thread of the group
+    // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
+    auto ask = [&](long long t, int s, int place, int from, int by) {
         if (t >= a.T) return;
         uint64_t* bar = ring.bars + place;
-        unsigned char* to = ring.base + (size_t)place * ring.stage;
-        mbar_expect_tx(bar, (a.dh_out ? row_bytes : 0u) + (a.dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
-        if (a.dh_out) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
-        if (a.dn) {
-            bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
-            bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
-        }
-        if (s >= 0)   // codes lie in token order, the block's output in slot order
-            bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
+        unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
+        if (from == 0) mbar_expect_tx(bar, (a.dh_out ? row_bytes : 0u) + (a.dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
+        for (int k = from; k < 4; k += by)
+            if (k == 0) {
+                if (a.dh_out) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
+            } else if (k == 1) {
+                if (a.dn) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
+            } else if (k == 2) {
+                if (a.dn) bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
+            } else if (s >= 0) {   // codes lie in token order, the block's output in slot order
+                bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
+            }
     };
+    const int asks = lane % kWarp ? 4 : lane / kWarp;   // from which array on this thread asks (4 and more: none)
     if (lane == 0)
-        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d);
-    Unit8 acc_post[2], acc_pre[2];
+        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d, 0, 1);
+    // this thread's places in a row, in its activations, in the weights
+    bool have[NV];
+    uint32_t off[NV], act[NV];
+    const unsigned char* w_post[NV];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NV; ++i) {
+        const int un = lane + i * tpr;
+        have[i] = FULL || un < units;
+        off[i] = un * UB;
+        act[i] = 2 * row_bytes + un * AB;
+        w_post[i] = reinterpret_cast<const unsigned char*>(weights + un * 8);
+    }
+    const size_t to_pre = (size_t)a.H * 4;
+    using Raw = typename RawUnit<X, CK>::type;
+    auto activation = [&](const unsigned char* at) { return widen<X>(*reinterpret_cast<const Raw*>(at)); };
+    Unit8 acc_post[NV], acc_pre[NV];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { acc_post[i].p[j] = both(0.0f); acc_pre[i].p[j] = both(0.0f); }
+    for (int i = 0; i < NV; ++i) { clear(acc_post[i]); clear(acc_pre[i]); }
     RowInfo soon{};
+    unsigned char* dh_row = static_cast<unsigned char*>(a.dh) + (size_t)t_first * row_bytes;
+    const size_t dh_step = (size_t)t_step * row_bytes;
     int n = 0;   // the row's number within the group
     for (int t = t_first; t < a.T; t += t_step, ++n) {
-        const size_t row = (size_t)t * row_bytes;
         const RowInfo f = table[n & (kTable - 1)];
         if (lane < 32) {
             if ((n & 31) == 0 && n > 0) soon = info_of<CK>(a, branch, t + (32 + lane) * (long long)t_step);
             if ((n & 31) == 16 && n > 32) table[(n + 16 + lane) & (kTable - 1)] = soon;
         }
         const unsigned char* place = ring.wait();
-        Unit8 x[2], u[2], dn[2], D[2];
         float2 sx = both(0.0f), su = both(0.0f), sg = both(0.0f);   // x'^2, u'^2, dn w_pre x'
+        Unit8 x[NV], dx[NV], gp[NV];   // x', dn x', dn w_pre
+        Raw u[NV];                     // as they lie in memory
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (!FULL && !have[i]) { clear(x[i]); clear(u[i]); clear(dn[i]); clear(D[i]); continue; }
-            D[i] = load_pairs<X>(place + off[i]);
-            dn[i] = load_pairs<X>(place + row_bytes + off[i]);
-            if constexpr (CK) {
-                x[i] = load_codes(place + 2 * row_bytes + act[i]);
-                u[i] = load_codes(place + 2 * row_bytes + act_bytes + act[i]);
-            } else {
-                x[i] = load_pairs<X>(place + 2 * row_bytes + act[i]);
-                u[i] = load_pairs<X>(place + 2 * row_bytes + act_bytes + act[i]);
+        for (int i = 0; i < NV; ++i) {
+            if (!FULL && !have[i]) continue;
+            if (has_dn) {
+                x[i] = activation(place + act[i]);
+                const Unit8 dn = load_pairs<X>(place + row_bytes + off[i]), w = load_pairs<float>(w_post[i] + to_pre);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!CK) sx = __ffma2_rn(x[i].p[j], x[i].p[j], sx);
+                    dx[i].p[j] = __fmul2_rn(dn.p[j], x[i].p[j]);
+                    sg = __ffma2_rn(dx[i].p[j], w.p[j], sg);
+                    gp[i].p[j] = __fmul2_rn(dn.p[j], w.p[j]);
+                }
             }
-            if (!a.dh_out) clear(D[i]);   // nothing came
-            if (!a.dn) { clear(dn[i]); clear(x[i]); }
-            if (f.s < 0) clear(u[i]);
-            const Unit8 w = weight(false, i);
+            if (f.s >= 0) {
+                u[i] = *reinterpret_cast<const Raw*>(place + act[i] + act_bytes);
+                if (!CK) {
+                    const Unit8 v = widen<X>(u[i]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!CK) sx = __ffma2_rn(x[i].p[j], x[i].p[j], sx);
-                if (!CK) su = __ffma2_rn(u[i].p[j], u[i].p[j], su);
-                sg = __ffma2_rn(__fmul2_rn(dn[i].p[j], w.p[j]), x[i].p[j], sg);
+                    for (int j = 0; j < 4; ++j) su = __ffma2_rn(v.p[j], v.p[j], su);
+                }
             }
         }
         float q = f.q, r = f.r, xs = 1.0f, us = 1.0f, dot;
         if constexpr (CK) {
-            float sum[1] = {sg.x + sg.y};
-            group_sum(sum, red, parity, group, tpr);
-            dot = sum[0];
+            dot = total.one(sg.x + sg.y);
         } else {
-            float sum[3] = {sx.x + sx.y, su.x + su.y, sg.x + sg.y};
-            group_sum(sum, red, parity, group, tpr);
-            xs = q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
-            us = r = rsqrtf(fmaf(sum[1], inv_h, a.eps));
-            dot = sum[2];
+            float xx = sx.x + sx.y, uu = su.x + su.y;
+            dot = sg.x + sg.y;
+            total.three(xx, uu, dot);
+            xs = q = rsqrtf(fmaf(xx, inv_h, a.eps));
+            us = r = rsqrtf(fmaf(uu, inv_h, a.eps));
         }
-        __syncwarp();
-        if (lane == 0) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place);   // the group has taken the row
-        ring.next();
-        const float2 q2 = both(q), cx = both(-q * xs * (dot * xs * inv_h));
+        const float2 q2 = both(q), cx = both(-q * xs * (dot * xs * inv_h)), gu = both(f.gate * us), xs2 = both(xs), a2 = both(a.res_scale);
         float2 sk = both(0.0f);
+        Unit8 e[NV];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (have[i]) {
-                {
-                    const Unit8 w = weight(false, i);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) D[i].p[j] = __ffma2_rn(cx, x[i].p[j], __ffma2_rn(q2, __fmul2_rn(dn[i].p[j], w.p[j]), D[i].p[j]));
-                }
-                if (need_k) {
-                    const Unit8 w = weight(true, i);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sk = __ffma2_rn(__fmul2_rn(D[i].p[j], w.p[j]), u[i].p[j], sk);
-                }
-            }
-        float k[1] = {sk.x + sk.y};
-        if (need_k) group_sum(k, red, parity, group, tpr);
-        k[0] *= us;
-        if (a.dgate && lane == 0) a.dgate[t] = k[0];
-        const float rg = r * f.gate;
-        const float2 rg2 = both(rg), cu = both(-rg * us * (k[0] * inv_h)), gu = both(f.gate * us), xs2 = both(xs), a2 = both(a.res_scale);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (have[i]) {
-                Unit8 o;
+        for (int i = 0; i < NV; ++i) {
+            if (!FULL && !have[i]) continue;
+            Unit8 D;
+            clear(D);
+            if (has_up) D = load_pairs<X>(place + off[i]);
+            if (has_dn) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    acc_post[i].p[j] = __ffma2_rn(gu, __fmul2_rn(D[i].p[j], u[i].p[j]), acc_post[i].p[j]);
-                    acc_pre[i].p[j] = __ffma2_rn(xs2, __fmul2_rn(dn[i].p[j], x[i].p[j]), acc_pre[i].p[j]);
-                }
-                if (a.dy && f.s >= 0) {
-                    const Unit8 w = weight(true, i);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o.p[j] = __ffma2_rn(cu, u[i].p[j], __fmul2_rn(rg2, __fmul2_rn(D[i].p[j], w.p[j])));
-                    store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)f.s * row_bytes + off[i], o);
-                }
-                if (a.dh) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o.p[j] = __fmul2_rn(a2, D[i].p[j]);
-                    store_pairs<X>(static_cast<unsigned char*>(a.dh) + row + off[i], o);
+                    D.p[j] = __ffma2_rn(cx, x[i].p[j], __ffma2_rn(q2, gp[i].p[j], D.p[j]));
+                    acc_pre[i].p[j] = __ffma2_rn(xs2, dx[i].p[j], acc_pre[i].p[j]);
                 }
             }
+            if (f.s >= 0) {
+                const Unit8 v = widen<X>(u[i]), w = load_pairs<float>(w_post[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 du = __fmul2_rn(D.p[j], v.p[j]);
+                    acc_post[i].p[j] = __ffma2_rn(gu, du, acc_post[i].p[j]);
+                    sk = __ffma2_rn(du, w.p[j], sk);
+                    e[i].p[j] = __fmul2_rn(D.p[j], w.p[j]);
+                }
+            }
+            if (has_dh) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) D.p[j] = __fmul2_rn(a2, D.p[j]);
+                store_pairs<X>(dh_row + off[i], D);
+            }
+        }
+        dh_row += dh_step;
+        float k = total.one(sk.x + sk.y);
+        __syncwarp();
+        if (asks < 4) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place, asks, tpr / kWarp);   // the group is done with the row
+        ring.next();
+        k *= us;
+        if (lane == 0 && a.dgate) a.dgate[t] = k;
+        if (has_dy && f.s >= 0) {
+            const float rg = r * f.gate;
+            const float2 rg2 = both(rg), cu = both(-rg * us * (k * inv_h));
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (!FULL && !have[i]) continue;
+                const Unit8 v = widen<X>(u[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) e[i].p[j] = __ffma2_rn(cu, v.p[j], __fmul2_rn(rg2, e[i].p[j]));
+                store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)f.s * row_bytes + off[i], e[i]);
+            }
+        }
     }
     ring.leave();
     if (a.part_post || a.part_pre) {   // groups add their columns one after the other, where the ring was: a fixed order
@@ -859,7 +908,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_grad_ring_kernel(const NormGr
         for (int g = 0; g < a.groups; ++g) {
             if (group == g)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < NV; ++i)
                     if (have[i])
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -878,10 +927,15 @@ __global__ void __launch_bounds__(MAXT) block_norm_grad_ring_kernel(const NormGr
         }
     }
     if (a.dy && a.inv) {   // rows of the slot buffer that no token owns have a zero gradient
-        const Unit8 z{{both(0.0f), both(0.0f), both(0.0f), both(0.0f)}};
-        for (long long row = t_first; row < a.rows; row += t_step) {
-            if (a.inv[row] >= 0) continue;
-            for (int un = lane; un < units; un += tpr) store_pairs<X>(static_cast<unsigned char*>(a.dy) + row * row_bytes + un * UB, z);
+        Unit8 z;
+        clear(z);
+        const int l = threadIdx.x & 31;
+        for (long long row0 = (long long)t_first * 32; row0 < a.rows; row0 += (long long)t_step * 32) {   // every warp sees the same 32 rows
+            unsigned empty = __ballot_sync(0xffffffffu, row0 + l < a.rows && a.inv[row0 + l] < 0);
+            for (; empty; empty &= empty - 1) {
+                unsigned char* to = static_cast<unsigned char*>(a.dy) + (size_t)(row0 + __ffs(empty) - 1) * row_bytes;
+                for (int un = lane; un < units; un += tpr) store_pairs<X>(to + un * UB, z);
+            }
         }
     }
 }
@@ -921,7 +975,7 @@ RowPlan plan_rows(int units, int nv, int threads) {
 }
 
 constexpr int kGradCtasPerSm = 2;       // at most: one row of column sums each
-constexpr int kRingSmem = 200 << 10;    // shared memory of an SM that rings may take
+constexpr int kRingSmem = 210 << 10;    // shared memory of a CTA for rings and weights, beside the static strips
 constexpr int kRingMaxDepth = 4;
 
 bool aligned(const void* p, int n) { return (uintptr_t)p % n == 0; }
@@ -956,8 +1010,8 @@ int forward(NormArgs& a, cudaStream_t st) {
         if (!allow_smem(kernel, smem)) return (int)LOCMOE_ERR_CUDA;
         return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
     };
-    if (wide && units <= 2 * kFwdThreads) {
-        const RowPlan p = plan_rows(units, 2, kFwdThreads);
+    if (wide && units <= 2 * kRingThreads) {
+        const RowPlan p = plan_rows(units, 2, kRingThreads);
         const int stage = 2 * a.H * (int)sizeof(X);
         a.depth = ring_depth(p.groups, stage, 0);
         const size_t smem = ring_bytes(p.groups, a.depth, stage);
@@ -993,17 +1047,18 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     };
     int rc = LOCMOE_OK;
     bool done = false;
-    if (bulk && units <= 2 * kGradLongThreads) {
-        const bool kept = units <= 2 * kGradThreads;
-        const RowPlan p = plan_rows(units, 2, kept ? kGradThreads : kGradLongThreads);
-        const int stage = 2 * a.H * ((int)sizeof(X) + (CK ? 1 : (int)sizeof(X))), extra = kept ? 0 : 8 * a.H;
+    if (bulk && units <= 1024) {
+        const int nv = units <= kRingThreads ? 1 : 2;
+        const RowPlan p = plan_rows(units, nv, nv == 1 ? kRingThreads : 512);
+        const int stage = 2 * a.H * ((int)sizeof(X) + (CK ? 1 : (int)sizeof(X))), extra = 8 * a.H;
         a.depth = ring_depth(p.groups, stage, extra);
         if (a.depth) {
             const size_t smem = ring_bytes(p.groups, a.depth, stage) + extra;
-            const bool full = units == 2 * p.tpr;
-            if (!kept) rc = launch(block_norm_grad_ring_kernel<X, CK, kGradLongThreads, false>, p, 1, smem);
-            else rc = full ? launch(block_norm_grad_ring_kernel<X, CK, kGradThreads, true>, p, 1, smem)
-                           : launch(block_norm_grad_ring_kernel<X, CK, kGradThreads, false>, p, 1, smem);
+            const bool all = a.dh_out && a.dn && (CK ? (const void*)a.u8 : a.y) && a.dh && a.dy;
+            if (nv == 2) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false>, p, 1, smem);
+            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, false>, p, 1, smem);
+            else if (units == p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, true, true>, p, 1, smem);
+            else rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, true>, p, 1, smem);
             done = true;
         }
     }
