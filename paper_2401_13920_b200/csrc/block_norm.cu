@@ -246,6 +246,26 @@ struct GroupSum {
         }
         x = __shfl_sync(full, s, 0); y = __shfl_sync(full, s, 8); z = __shfl_sync(full, s, 16);
     }
+    __device__ __forceinline__ void four(float& x, float& y, float& z, float& w) {
+        constexpr unsigned full = 0xffffffffu;
+        const bool upper = lane & 16, second = lane & 8;
+        const float a = (upper ? z : x) + __shfl_xor_sync(full, upper ? x : z, 16);
+        const float b = (upper ? w : y) + __shfl_xor_sync(full, upper ? y : w, 16);
+        float s = (second ? b : a) + __shfl_xor_sync(full, second ? a : b, 8);
+        s = butterfly(s, 4);   // lanes 0..7: x, 8..15: y, 16..23: z, 24..31: w
+        if (warps > 1) {
+            float* p = strip + (lane >> 3) * kWarp;
+            if ((lane & 7) == 0) p[warp] = s;
+            meet();
+            s = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if ((lane & 7) + 8 * k < warps) s += p[(lane & 7) + 8 * k];
+            s = butterfly(s, 4);
+            turn();
+        }
+        x = __shfl_sync(full, s, 0); y = __shfl_sync(full, s, 8); z = __shfl_sync(full, s, 16); w = __shfl_sync(full, s, 24);
+    }
 };
 
 __device__ int g_norm_flags = 0;   // bit 0: a bounded wait for a row gave up
@@ -734,8 +754,9 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
 // Gradient.  Written with the raw rows x', u' (x = xs x', u = us u'; codes: xs = us = 1):
 //   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
 //   e = D w_post,  k = us sum(e u'),  dv = R r e - cu u',  cu = R r us k / H
-// Everything but dv is done between the two sums, so that only e and u' are held over the second one, and the weights lie
-// in shared memory.  That is for the registers: what spills comes back through an L1 that the rings leave little of,
+// A row's second sum (k) is taken together with the next row's first ones, so that a row costs one meeting of its group.
+// Everything but dv is done before it, so that only e and u' are held over it, and the weights lie in shared memory.  That
+// is for the registers: what spills comes back through an L1 that the rings leave little of,
 // behind the rings' copies (two units a thread with spills: 1380 us at 65536 x 5120 in bf16).
 // NV: units of a thread, one up to rows of 5120 (640 threads), else two (512 threads).  FULL: every thread has them all.
 // ALL: both upstream gradients, the branch, dh and dy are there.
@@ -802,56 +823,59 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
     Unit8 acc_post[NV], acc_pre[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) { clear(acc_post[i]); clear(acc_pre[i]); }
-    RowInfo soon{};
-    unsigned char* dh_row = static_cast<unsigned char*>(a.dh) + (size_t)t_first * row_bytes;
-    const size_t dh_step = (size_t)t_step * row_bytes;
-    int n = 0;   // the row's number within the group
-    for (int t = t_first; t < a.T; t += t_step, ++n) {
-        const RowInfo f = table[n & (kTable - 1)];
-        if (lane < 32) {
-            if ((n & 31) == 0 && n > 0) soon = info_of<CK>(a, branch, t + (32 + lane) * (long long)t_step);
-            if ((n & 31) == 16 && n > 32) table[(n + 16 + lane) & (kTable - 1)] = soon;
-        }
-        const unsigned char* place = ring.wait();
-        float2 sx = both(0.0f), su = both(0.0f), sg = both(0.0f);   // x'^2, u'^2, dn w_pre x'
-        Unit8 x[NV], dx[NV], gp[NV];   // x', dn x', dn w_pre
-        Raw u[NV];                     // as they lie in memory
+    Unit8 e[NV];                                       // D w_post
+    Raw u[NV], x[NV];                                  // u', x' and dn as they lie in memory: half the registers
+    typename RawUnit<X, false>::type dn[NV];
+    // A row's first sums: x'^2, u'^2, dn w_pre x'.
+    auto begin = [&](const unsigned char* place, int s, float& xx, float& uu, float& dot) {
+        float2 sx = both(0.0f), su = both(0.0f), sg = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (!FULL && !have[i]) continue;
             if (has_dn) {
-                x[i] = activation(place + act[i]);
-                const Unit8 dn = load_pairs<X>(place + row_bytes + off[i]), w = load_pairs<float>(w_post[i] + to_pre);
+                x[i] = *reinterpret_cast<const Raw*>(place + act[i]);
+                dn[i] = *reinterpret_cast<const typename RawUnit<X, false>::type*>(place + row_bytes + off[i]);
+                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = load_pairs<float>(w_post[i] + to_pre);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (!CK) sx = __ffma2_rn(x[i].p[j], x[i].p[j], sx);
-                    dx[i].p[j] = __fmul2_rn(dn.p[j], x[i].p[j]);
-                    sg = __ffma2_rn(dx[i].p[j], w.p[j], sg);
-                    gp[i].p[j] = __fmul2_rn(dn.p[j], w.p[j]);
+                    if (!CK) sx = __ffma2_rn(xv.p[j], xv.p[j], sx);
+                    sg = __ffma2_rn(__fmul2_rn(g.p[j], xv.p[j]), w.p[j], sg);
                 }
             }
-            if (f.s >= 0) {
-                u[i] = *reinterpret_cast<const Raw*>(place + act[i] + act_bytes);
-                if (!CK) {
-                    const Unit8 v = widen<X>(u[i]);
+            if (!CK && s >= 0) {
+                const Unit8 v = activation(place + act[i] + act_bytes);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) su = __ffma2_rn(v.p[j], v.p[j], su);
-                }
+                for (int j = 0; j < 4; ++j) su = __ffma2_rn(v.p[j], v.p[j], su);
             }
         }
-        float q = f.q, r = f.r, xs = 1.0f, us = 1.0f, dot;
-        if constexpr (CK) {
-            dot = total.one(sg.x + sg.y);
-        } else {
-            float xx = sx.x + sx.y, uu = su.x + su.y;
-            dot = sg.x + sg.y;
-            total.three(xx, uu, dot);
+        xx = sx.x + sx.y; uu = su.x + su.y; dot = sg.x + sg.y;
+    };
+    RowInfo soon{}, f{};
+    unsigned char* dh_row = static_cast<unsigned char*>(a.dh) + (size_t)t_first * row_bytes;
+    const size_t dh_step = (size_t)t_step * row_bytes;
+    const unsigned char* place = nullptr;
+    int at = 0;                        // the row's place
+    float xx = 0.0f, uu = 0.0f, dot = 0.0f;
+    if (t_first < a.T) {
+        f = table[0];
+        place = ring.wait();
+        ring.next();
+        begin(place, f.s, xx, uu, dot);
+        total.three(xx, uu, dot);
+    }
+    int n = 0;   // the row's number within the group
+    for (int t = t_first; t < a.T; t += t_step, ++n) {
+        if (lane < 32) {
+            if ((n & 31) == 0 && n > 0) soon = info_of<CK>(a, branch, t + (32 + lane) * (long long)t_step);
+            if ((n & 31) == 16 && n > 32) table[(n + 16 + lane) & (kTable - 1)] = soon;
+        }
+        float q = f.q, r = f.r, xs = 1.0f, us = 1.0f;
+        if constexpr (!CK) {
             xs = q = rsqrtf(fmaf(xx, inv_h, a.eps));
             us = r = rsqrtf(fmaf(uu, inv_h, a.eps));
         }
         const float2 q2 = both(q), cx = both(-q * xs * (dot * xs * inv_h)), gu = both(f.gate * us), xs2 = both(xs), a2 = both(a.res_scale);
         float2 sk = both(0.0f);
-        Unit8 e[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (!FULL && !have[i]) continue;
@@ -859,13 +883,15 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             clear(D);
             if (has_up) D = load_pairs<X>(place + off[i]);
             if (has_dn) {
+                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = load_pairs<float>(w_post[i] + to_pre);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    D.p[j] = __ffma2_rn(cx, x[i].p[j], __ffma2_rn(q2, gp[i].p[j], D.p[j]));
-                    acc_pre[i].p[j] = __ffma2_rn(xs2, dx[i].p[j], acc_pre[i].p[j]);
+                    D.p[j] = __ffma2_rn(cx, xv.p[j], __ffma2_rn(q2, __fmul2_rn(g.p[j], w.p[j]), D.p[j]));
+                    acc_pre[i].p[j] = __ffma2_rn(xs2, __fmul2_rn(g.p[j], xv.p[j]), acc_pre[i].p[j]);
                 }
             }
             if (f.s >= 0) {
+                u[i] = *reinterpret_cast<const Raw*>(place + act[i] + act_bytes);
                 const Unit8 v = widen<X>(u[i]), w = load_pairs<float>(w_post[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -882,14 +908,24 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             }
         }
         dh_row += dh_step;
-        float k = total.one(sk.x + sk.y);
+        // the next row's first sums beside this one's last
+        const RowInfo here = f;
+        const int was = at;
+        if (t + (long long)t_step < a.T) {
+            f = table[(n + 1) & (kTable - 1)];
+            at = ring.place;
+            place = ring.wait();
+            ring.next();
+            begin(place, f.s, xx, uu, dot);
+        }
+        float k = sk.x + sk.y;
+        total.four(k, xx, uu, dot);
         __syncwarp();
-        if (asks < 4) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place, asks, tpr / kWarp);   // the group is done with the row
-        ring.next();
+        if (asks < 4) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, was, asks, tpr / kWarp);   // the group is done with the row
         k *= us;
         if (lane == 0 && a.dgate) a.dgate[t] = k;
-        if (has_dy && f.s >= 0) {
-            const float rg = r * f.gate;
+        if (has_dy && here.s >= 0) {
+            const float rg = r * here.gate;
             const float2 rg2 = both(rg), cu = both(-rg * us * (k * inv_h));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -897,7 +933,7 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
                 const Unit8 v = widen<X>(u[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) e[i].p[j] = __ffma2_rn(cu, v.p[j], __fmul2_rn(rg2, e[i].p[j]));
-                store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)f.s * row_bytes + off[i], e[i]);
+                store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)here.s * row_bytes + off[i], e[i]);
             }
         }
     }
