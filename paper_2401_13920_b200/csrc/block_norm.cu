@@ -347,17 +347,18 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
         if constexpr (NV > 0) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int un = lane + i * tpr;
-                if (un < units) {
-                    Unit<X, VEC>::load(a.h, at_t + (size_t)un * VEC, h + i * VEC);
-                    if (s >= 0) Unit<X, VEC>::load(a.y, at_s + (size_t)un * VEC, v + i * VEC);
+                const int un = min(lane + i * tpr, units - 1);   // loads without branches: all of them in flight together
+                Unit<X, VEC>::load(a.h, at_t + (size_t)un * VEC, h + i * VEC);
+                if (a.y) Unit<X, VEC>::load(a.y, at_s + (size_t)un * VEC, v + i * VEC);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const bool none = lane + i * tpr >= units;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    if (none) h[i * VEC + j] = 0.0f;
+                    if (none || s < 0) v[i * VEC + j] = 0.0f;
                 }
-                if (un >= units || s < 0)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) v[i * VEC + j] = 0.0f;
-                if (un >= units)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) h[i * VEC + j] = 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < R; ++i) sum[0] = fmaf(v[i], v[i], sum[0]);
@@ -479,18 +480,23 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
         float x[R], u[R], dn[R], D[R];
         // one unit of the four inputs; x / u are h' / v (or the normalised values with CK), missing ones zero
         auto load = [&](int un, float* xv, float* uv, float* nv, float* dv) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) { xv[j] = 0.0f; uv[j] = 0.0f; nv[j] = 0.0f; dv[j] = 0.0f; }
-            if (un >= units) return;
-            if (a.dh_out) Unit<X, VEC>::load(a.dh_out, at_t + (size_t)un * VEC, dv);
+            const size_t c = (size_t)min(un, units - 1) * VEC;   // loads without branches: all of them in flight together
+            const bool none = un >= units;
+            if (a.dh_out) Unit<X, VEC>::load(a.dh_out, at_t + c, dv);
             if (a.dn) {
-                Unit<X, VEC>::load(a.dn, at_t + (size_t)un * VEC, nv);
-                if constexpr (CK) load_e4m3<VEC>(a.x8, at_t + (size_t)un * VEC, xv);
-                else Unit<X, VEC>::load(a.h_out, at_t + (size_t)un * VEC, xv);
+                Unit<X, VEC>::load(a.dn, at_t + c, nv);
+                if constexpr (CK) load_e4m3<VEC>(a.x8, at_t + c, xv);
+                else Unit<X, VEC>::load(a.h_out, at_t + c, xv);
             }
-            if (s >= 0) {
-                if constexpr (CK) load_e4m3<VEC>(a.u8, at_t + (size_t)un * VEC, uv);
-                else Unit<X, VEC>::load(a.y, at_s + (size_t)un * VEC, uv);
+            if (branch) {
+                if constexpr (CK) load_e4m3<VEC>(a.u8, at_t + c, uv);
+                else Unit<X, VEC>::load(a.y, at_s + c, uv);
+            }
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                if (none || !a.dh_out) dv[j] = 0.0f;
+                if (none || !a.dn) { nv[j] = 0.0f; xv[j] = 0.0f; }
+                if (none || s < 0) uv[j] = 0.0f;
             }
         };
         float sum[3] = {0.0f, 0.0f, 0.0f};   // x^2, u^2, dn w_pre x
@@ -1000,17 +1006,19 @@ __global__ void __launch_bounds__(kColThreads) block_norm_cols_kernel(const floa
 
 // Threads of a row group and the number of groups of a CTA for `units` units of which a thread keeps nv.
 struct RowPlan { int tpr, groups; };
-RowPlan plan_rows(int units, int nv, int threads) {
+RowPlan plan_rows(int units, int nv, int threads, int T) {
     int tpr = nv > 0 ? (units + nv - 1) / nv : threads;
     tpr = (tpr + kWarp - 1) / kWarp * kWarp;
     if (tpr > 1024) tpr = 1024;
     int groups = nv > 0 ? threads / tpr : 1;
     if (groups < 1) groups = 1;
     if (groups > kMaxGroups) groups = kMaxGroups;
+    const int share = (T + sm_count() - 1) / sm_count();   // few rows are spread over the SMs
+    if (groups > share) groups = share;
     return {tpr, groups};
 }
 
-constexpr int kGradCtasPerSm = 2;       // at most: one row of column sums each
+constexpr int kGradCtasPerSm = 1;       // one row of column sums each
 constexpr int kRingSmem = 210 << 10;    // shared memory of a CTA for rings and weights, beside the static strips
 constexpr int kRingMaxDepth = 4;
 
@@ -1047,7 +1055,7 @@ int forward(NormArgs& a, cudaStream_t st) {
         return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
     };
     if (wide && units <= 2 * kRingThreads) {
-        const RowPlan p = plan_rows(units, 2, kRingThreads);
+        const RowPlan p = plan_rows(units, 2, kRingThreads, a.T);
         const int stage = 2 * a.H * (int)sizeof(X);
         a.depth = ring_depth(p.groups, stage, 0);
         const size_t smem = ring_bytes(p.groups, a.depth, stage);
@@ -1058,7 +1066,7 @@ int forward(NormArgs& a, cudaStream_t st) {
         }
     }
     const int nv = wide ? 0 : (units <= 1024 * 8 ? 8 : 0);
-    const RowPlan p = plan_rows(units, nv, 256);
+    const RowPlan p = plan_rows(units, nv, 256, a.T);
     const int ctas = 2048 / (p.tpr * p.groups) > 0 ? 2048 / (p.tpr * p.groups) : 1;
     if (wide) return launch(block_norm_kernel<X, 8, 0>, p, ctas, 0);
     return nv ? launch(block_norm_kernel<X, 1, 8>, p, ctas, 0) : launch(block_norm_kernel<X, 1, 0>, p, ctas, 0);
@@ -1085,7 +1093,7 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     bool done = false;
     if (bulk && units <= 1024) {
         const int nv = units <= kRingThreads ? 1 : 2;
-        const RowPlan p = plan_rows(units, nv, nv == 1 ? kRingThreads : 512);
+        const RowPlan p = plan_rows(units, nv, nv == 1 ? kRingThreads : 512, a.T);
         const int stage = 2 * a.H * ((int)sizeof(X) + (CK ? 1 : (int)sizeof(X))), extra = 8 * a.H;
         a.depth = ring_depth(p.groups, stage, extra);
         if (a.depth) {
@@ -1100,7 +1108,7 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     }
     if (!done) {
         const int nv = wide ? 0 : (units <= 512 * 8 ? 8 : 0);
-        const RowPlan p = plan_rows(units, nv, 512);
+        const RowPlan p = plan_rows(units, nv, 512, a.T);
         const size_t smem = nv && p.groups > 1 ? (size_t)a.H * 8 : 0;
         if (wide) rc = launch(block_norm_grad_kernel<X, 8, 0, CK>, p, kGradCtasPerSm, smem);
         else rc = nv ? launch(block_norm_grad_kernel<X, 1, 8, CK>, p, kGradCtasPerSm, smem)
