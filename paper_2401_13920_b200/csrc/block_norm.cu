@@ -197,6 +197,88 @@ __device__ __forceinline__ void store_codes(uint8_t* at, const Unit8& f) {
     *reinterpret_cast<uint2*>(at) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
+// ---- rows whose length is no multiple of 16 bytes (ODD): bulk copies bring the 16-byte pieces that hold the row, which
+// then begins `mis` bytes into its place, and a unit is eight single elements, tpr apart, instead of eight in a row ----
+struct Piece { size_t from; uint32_t bytes, tail; };   // copy `bytes` from `from` on; then `tail` bytes by hand
+__device__ __forceinline__ Piece piece_of(size_t off, uint32_t len, size_t total) {   // of an array of `total` bytes, 16-byte aligned
+    const size_t end = off + len, whole = total & ~(size_t)15, from = off & ~(size_t)15;
+    size_t stop = (end + 15) & ~(size_t)15;
+    if (stop > whole) stop = whole;          // the array's last bytes: nothing beyond them is read
+    if (stop < from) stop = from;
+    return {from, (uint32_t)(stop - from), end > stop ? (uint32_t)(end - stop) : 0u};
+}
+__device__ __forceinline__ void tail_of(unsigned char* to, const unsigned char* base, const Piece& p) {
+    for (uint32_t i = 0; i < p.tail; ++i) to[p.bytes + i] = base[p.from + p.bytes + i];
+}
+template <typename X, bool CODE, bool ODD>
+__device__ __forceinline__ typename RawUnit<X, CODE>::type load_raw(const unsigned char* row, uint32_t off, int first, int step, int H) {
+    using Raw = typename RawUnit<X, CODE>::type;
+    if constexpr (!ODD) {
+        return *reinterpret_cast<const Raw*>(row + off);
+    } else if constexpr (CODE) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = first + j * step < H ? row[first + j * step] : 0u;
+        return make_uint2(w[0] | (w[1] << 8) | (w[2] << 16) | (w[3] << 24), w[4] | (w[5] << 8) | (w[6] << 16) | (w[7] << 24));
+    } else if constexpr (sizeof(X) == 2) {
+        const uint16_t* r = reinterpret_cast<const uint16_t*>(row);
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = first + j * step < H ? r[first + j * step] : 0u;
+        return make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+    } else {
+        const float* r = reinterpret_cast<const float*>(row);
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = first + j * step < H ? r[first + j * step] : 0.0f;
+        return {make_float4(w[0], w[1], w[2], w[3]), make_float4(w[4], w[5], w[6], w[7])};
+    }
+}
+template <typename X, bool ODD>
+__device__ __forceinline__ void store_unit(unsigned char* row, uint32_t off, int first, int step, int H, const Unit8& f) {
+    if constexpr (!ODD) {
+        store_pairs<X>(row + off, f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int a = first + 2 * j * step, b = a + step;
+            if constexpr (sizeof(X) == 2) {
+                const uint32_t w = cvt_bf16x2(f.p[j]);
+                if (a < H) reinterpret_cast<uint16_t*>(row)[a] = (uint16_t)w;
+                if (b < H) reinterpret_cast<uint16_t*>(row)[b] = (uint16_t)(w >> 16);
+            } else {
+                if (a < H) reinterpret_cast<float*>(row)[a] = f.p[j].x;
+                if (b < H) reinterpret_cast<float*>(row)[b] = f.p[j].y;
+            }
+        }
+    }
+}
+template <bool ODD>
+__device__ __forceinline__ void store_unit_codes(uint8_t* row, uint32_t off, int first, int step, int H, const Unit8& f) {
+    if constexpr (!ODD) {
+        store_codes(row + off, f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t w = __nv_cvt_float2_to_fp8x2(f.p[j], __NV_SATFINITE, __NV_E4M3);
+            const int a = first + 2 * j * step, b = a + step;
+            if (a < H) row[a] = (uint8_t)w;
+            if (b < H) row[b] = (uint8_t)(w >> 8);
+        }
+    }
+}
+template <bool ODD>
+__device__ __forceinline__ Unit8 weight_unit(const float* w, int un, int first, int step, int H) {   // from global memory; a NULL weight is 1
+    if constexpr (!ODD) {
+        return load_weight_pairs(w, un);
+    } else {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = !w ? 1.0f : first + j * step < H ? __ldg(w + first + j * step) : 0.0f;
+        return {{make_float2(f[0], f[1]), make_float2(f[2], f[3]), make_float2(f[4], f[5]), make_float2(f[6], f[7])}};
+    }
+}
+
 // Sums over the threads of a row group, the same bits in every thread.  Each warp adds up its lanes, the warps' partials
 // meet in one of two shared strips used alternately, so that one barrier per sum is enough.
 struct GroupSum {
@@ -658,8 +740,8 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
 // ---- ring kernels: rows of whole 16-byte pieces, two units a thread ----
 constexpr int kRingThreads = 640;   // of a CTA, which has an SM to itself: 102 registers a thread
 
-// FULL: every thread has two units.  CKPT: checkpoints are left.
-template <typename X, bool FULL, bool CKPT>
+// FULL: every thread has two units.  CKPT: checkpoints are left.  ODD: see above.
+template <typename X, bool FULL, bool CKPT, bool ODD>
 __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const NormArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
@@ -669,28 +751,48 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
     GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
-    const int units = a.H / 8;
+    const int units = (a.H + 7) / 8;
     const bool want_pre = a.n_out || (CKPT && a.x8);
     const int t_first = (int)(blockIdx.x * a.groups + group), t_step = (int)(gridDim.x * a.groups);
-    const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X));
-    RowInfo* table = reinterpret_cast<RowInfo*>(ring_mem + (size_t)a.groups * a.depth * (2 * row_bytes + 16)) + group * kTable;
+    const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X)), pitch = ODD ? (row_bytes + 30) / 16 * 16 : row_bytes;   // of an array in a place
+    RowInfo* table = reinterpret_cast<RowInfo*>(ring_mem + (size_t)a.groups * a.depth * (2 * pitch + 16)) + group * kTable;
     for (int i = lane; i < kTable; i += tpr) table[i] = info_of(a, t_first + (long long)i * t_step);
     const bool have[2] = {FULL || lane < units, FULL || lane + tpr < units};
     const uint32_t off[2] = {(uint32_t)(lane * UB), (uint32_t)((lane + tpr) * UB)};
+    const int first[2] = {lane, lane + 8 * tpr};   // ODD: this thread's elements are first + j * tpr
     Unit8 wp[2], wn[2];   // this thread's columns of the weights
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (have[i]) { wp[i] = load_weight_pairs(a.w_post, lane + i * tpr); wn[i] = load_weight_pairs(a.w_pre, lane + i * tpr); }
-    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)row_bytes);   // places of [h][y]; with a barrier of the CTA
+        if (ODD || have[i]) {
+            wp[i] = weight_unit<ODD>(a.w_post, lane + i * tpr, first[i], tpr, a.H);
+            wn[i] = weight_unit<ODD>(a.w_pre, lane + i * tpr, first[i], tpr, a.H);
+        }
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)pitch);   // places of [h][y]; with a barrier of the CTA
     // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
     auto ask = [&](long long t, int s, int place, int from, int by) {
         if (t >= a.T) return;
         uint64_t* bar = ring.bars + place;
         unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
-        if (from == 0) mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
-        for (int k = from; k < 2; k += by)
-            if (k == 0) bulk_g2s(to, static_cast<const unsigned char*>(a.h) + t * row_bytes, row_bytes, bar);
-            else if (s >= 0) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.y) + (size_t)s * row_bytes, row_bytes, bar);
+        const unsigned char *h = static_cast<const unsigned char*>(a.h), *y = static_cast<const unsigned char*>(a.y);
+        if constexpr (!ODD) {
+            if (from == 0) mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
+            for (int k = from; k < 2; k += by)
+                if (k == 0) bulk_g2s(to, h + t * row_bytes, row_bytes, bar);
+                else if (s >= 0) bulk_g2s(to + row_bytes, y + (size_t)s * row_bytes, row_bytes, bar);
+        } else {
+            const Piece ph = piece_of((size_t)t * row_bytes, row_bytes, (size_t)a.T * row_bytes);
+            Piece py{0, 0, 0};
+            if (s >= 0) py = piece_of((size_t)s * row_bytes, row_bytes, (size_t)a.rows * row_bytes);
+            if (from == 0) {
+                tail_of(to, h, ph);
+                tail_of(to + pitch, y, py);
+                mbar_expect_tx(bar, ph.bytes + py.bytes);
+            }
+            for (int k = from; k < 2; k += by) {
+                const Piece& p = k ? py : ph;
+                if (p.bytes) bulk_g2s(to + k * pitch, (k ? y : h) + p.from, p.bytes, bar);
+            }
+        }
     };
     const int asks = lane % kWarp ? 2 : lane / kWarp;   // from which array on this thread asks (2: none)
     if (lane == 0)
@@ -708,9 +810,9 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
         Unit8 h[2], v[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            if (!FULL && !have[i]) { clear(h[i]); clear(v[i]); continue; }
-            h[i] = load_pairs<X>(place + off[i]);
-            v[i] = load_pairs<X>(place + row_bytes + off[i]);
+            if (!FULL && !ODD && !have[i]) { clear(h[i]); clear(v[i]); continue; }
+            h[i] = widen<X>(load_raw<X, false, ODD>(place + (ODD ? (uint32_t)row & 15 : 0), off[i], first[i], tpr, a.H));
+            v[i] = widen<X>(load_raw<X, false, ODD>(place + pitch + (ODD ? (uint32_t)f.s * row_bytes & 15 : 0), off[i], first[i], tpr, a.H));
             if (f.s < 0) clear(v[i]);   // nothing came
         }
         float2 acc = both(0.0f);
@@ -728,15 +830,15 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
         acc = both(0.0f);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (have[i]) {
+            if (ODD || have[i]) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     v[i].p[j] = __fmul2_rn(v[i].p[j], r2);
                     h[i].p[j] = __ffma2_rn(__fmul2_rn(g2, wp[i].p[j]), v[i].p[j], __fmul2_rn(a2, h[i].p[j]));
                     acc = __ffma2_rn(h[i].p[j], h[i].p[j], acc);
                 }
-                if (a.h_out) store_pairs<X>(static_cast<unsigned char*>(a.h_out) + row + off[i], h[i]);
-                if (CKPT && a.u8) store_codes(a.u8 + (size_t)t * a.H + (lane + i * tpr) * 8, v[i]);
+                if (a.h_out) store_unit<X, ODD>(static_cast<unsigned char*>(a.h_out) + row, off[i], first[i], tpr, a.H, h[i]);
+                if (CKPT && a.u8) store_unit_codes<ODD>(a.u8 + (size_t)t * a.H, (lane + i * tpr) * 8, first[i], tpr, a.H, v[i]);
             }
         if (!want_pre) continue;
         sum = total.one(acc.x + acc.y);
@@ -745,13 +847,13 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
         const float2 q2 = both(q);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (have[i]) {
+            if (ODD || have[i]) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) h[i].p[j] = __fmul2_rn(h[i].p[j], q2);
-                if (CKPT && a.x8) store_codes(a.x8 + (size_t)t * a.H + (lane + i * tpr) * 8, h[i]);
+                if (CKPT && a.x8) store_unit_codes<ODD>(a.x8 + (size_t)t * a.H, (lane + i * tpr) * 8, first[i], tpr, a.H, h[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) h[i].p[j] = __fmul2_rn(h[i].p[j], wn[i].p[j]);
-                if (a.n_out) store_pairs<X>(static_cast<unsigned char*>(a.n_out) + row + off[i], h[i]);
+                if (a.n_out) store_unit<X, ODD>(static_cast<unsigned char*>(a.n_out) + row, off[i], first[i], tpr, a.H, h[i]);
             }
     }
     ring.leave();
@@ -765,8 +867,9 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
 // is for the registers: what spills comes back through an L1 that the rings leave little of,
 // behind the rings' copies (two units a thread with spills: 1380 us at 65536 x 5120 in bf16).
 // NV: units of a thread, one up to rows of 5120 (640 threads), else two (512 threads).  FULL: every thread has them all.
-// ALL: both upstream gradients, the branch, dh and dy are there.
-template <typename X, bool CK, int NV, bool FULL, bool ALL>
+// ALL: both upstream gradients, the branch, dh and dy are there.  ODD: see above (also rows of
+// codes that are no whole 16-byte pieces).
+template <typename X, bool CK, int NV, bool FULL, bool ALL, bool ODD>
 __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_ring_kernel(const NormGradArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
@@ -776,12 +879,14 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
     GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
-    const int units = a.H / 8;
+    const int units = (a.H + 7) / 8;
     const bool branch = ALL || (CK ? a.u8 != nullptr : a.y != nullptr);
     const bool has_dn = ALL || a.dn, has_up = ALL || a.dh_out, has_dh = ALL || a.dh, has_dy = ALL || a.dy;
     const int t_first = (int)(blockIdx.x * a.groups + group), t_step = (int)(gridDim.x * a.groups);
     const uint32_t row_bytes = (uint32_t)(a.H * sizeof(X)), act_bytes = CK ? (uint32_t)a.H : row_bytes;
-    unsigned char* after = ring_mem + (size_t)a.groups * a.depth * (2 * (row_bytes + act_bytes) + 16);
+    // of an array in a place
+    const uint32_t row_pitch = ODD ? (row_bytes + 30) / 16 * 16 : row_bytes, act_pitch = ODD ? (act_bytes + 30) / 16 * 16 : act_bytes;
+    unsigned char* after = ring_mem + (size_t)a.groups * a.depth * (2 * (row_pitch + act_pitch) + 16);
     RowInfo* table = reinterpret_cast<RowInfo*>(after) + group * kTable;
     float* weights = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H]: w_post, w_pre
     for (int i = lane; i < kTable; i += tpr) table[i] = info_of<CK>(a, branch, t_first + (long long)i * t_step);
@@ -790,23 +895,53 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
         weights[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
     }
     // places of [dh_out][dn][h_out or x8][y or u8]; with a barrier of the CTA
-    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_bytes + act_bytes));
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_pitch + act_pitch));
     // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
     auto ask = [&](long long t, int s, int place, int from, int by) {
         if (t >= a.T) return;
         uint64_t* bar = ring.bars + place;
         unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
-        if (from == 0) mbar_expect_tx(bar, (a.dh_out ? row_bytes : 0u) + (a.dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
-        for (int k = from; k < 4; k += by)
-            if (k == 0) {
-                if (a.dh_out) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
-            } else if (k == 1) {
-                if (a.dn) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
-            } else if (k == 2) {
-                if (a.dn) bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
-            } else if (s >= 0) {   // codes lie in token order, the block's output in slot order
-                bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
+        if constexpr (!ODD) {
+            if (from == 0) mbar_expect_tx(bar, (has_up ? row_bytes : 0u) + (has_dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
+            for (int k = from; k < 4; k += by)
+                if (k == 0) {
+                    if (has_up) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
+                } else if (k == 1) {
+                    if (has_dn) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
+                } else if (k == 2) {
+                    if (has_dn) bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
+                } else if (s >= 0) {   // codes lie in token order, the block's output in slot order
+                    bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
+                }
+            return;
+        }
+        const unsigned char* base[4] = {static_cast<const unsigned char*>(a.dh_out), static_cast<const unsigned char*>(a.dn),
+                                        CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out),
+                                        CK ? reinterpret_cast<const unsigned char*>(a.u8) : static_cast<const unsigned char*>(a.y)};
+        const bool wanted[4] = {a.dh_out != nullptr, a.dn != nullptr, a.dn != nullptr, s >= 0};
+        auto piece = [&](int k) -> Piece {
+            if (!wanted[k]) return {0, 0, 0};
+            const uint32_t len = k < 2 ? row_bytes : act_bytes;
+            const size_t at = (size_t)(k == 3 && !CK ? s : t) * len;
+            return piece_of(at, len, (size_t)(k == 3 && !CK ? a.rows : a.T) * len);
+        };
+        auto place_of = [&](int k) { return to + (k < 2 ? k * row_pitch : 2 * row_pitch + (k - 2) * act_pitch); };
+        if (from == 0) {
+            uint32_t bytes = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Piece p = piece(k);
+                bytes += p.bytes;
+                tail_of(place_of(k), base[k], p);
             }
+            mbar_expect_tx(bar, bytes);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k < from || (k - from) % by) continue;
+            const Piece p = piece(k);
+            if (p.bytes) bulk_g2s(place_of(k), base[k] + p.from, p.bytes, bar);
+        }
     };
     const int asks = lane % kWarp ? 4 : lane / kWarp;   // from which array on this thread asks (4 and more: none)
     if (lane == 0)
@@ -814,18 +949,31 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
     // this thread's places in a row, in its activations, in the weights
     bool have[NV];
     uint32_t off[NV], act[NV];
-    const unsigned char* w_post[NV];
+    int first[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int un = lane + i * tpr;
         have[i] = FULL || un < units;
         off[i] = un * UB;
-        act[i] = 2 * row_bytes + un * AB;
-        w_post[i] = reinterpret_cast<const unsigned char*>(weights + un * 8);
+        act[i] = un * AB;
+        first[i] = lane + 8 * i * tpr;   // ODD: this thread's elements are first + j * tpr
     }
-    const size_t to_pre = (size_t)a.H * 4;
+    auto weight = [&](bool post, int i) {
+        const float* w = weights + (post ? 0 : a.H);
+        if constexpr (ODD) return widen<float>(load_raw<float, false, true>(reinterpret_cast<const unsigned char*>(w), 0, first[i], tpr, a.H));
+        else return load_pairs<float>(reinterpret_cast<const unsigned char*>(w + (lane + i * tpr) * 8));
+    };
     using Raw = typename RawUnit<X, CK>::type;
-    auto activation = [&](const unsigned char* at) { return widen<X>(*reinterpret_cast<const Raw*>(at)); };
+    // row t's gradients (k = 0, 1), its activations from h_out / x8 and those from y / u8
+    auto raw_row = [&](const unsigned char* place, int t, int k, int i) {
+        return load_raw<X, false, ODD>(place + k * row_pitch + (ODD ? (uint32_t)t * row_bytes & 15 : 0), off[i], first[i], tpr, a.H);
+    };
+    auto raw_x = [&](const unsigned char* place, int t, int i) {
+        return load_raw<X, CK, ODD>(place + 2 * row_pitch + (ODD ? (uint32_t)t * act_bytes & 15 : 0), act[i], first[i], tpr, a.H);
+    };
+    auto raw_u = [&](const unsigned char* place, int t, int s, int i) {
+        return load_raw<X, CK, ODD>(place + 2 * row_pitch + act_pitch + (ODD ? (uint32_t)(CK ? t : s) * act_bytes & 15 : 0), act[i], first[i], tpr, a.H);
+    };
     Unit8 acc_post[NV], acc_pre[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) { clear(acc_post[i]); clear(acc_pre[i]); }
@@ -833,15 +981,15 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
     Raw u[NV], x[NV];                                  // u', x' and dn as they lie in memory: half the registers
     typename RawUnit<X, false>::type dn[NV];
     // A row's first sums: x'^2, u'^2, dn w_pre x'.
-    auto begin = [&](const unsigned char* place, int s, float& xx, float& uu, float& dot) {
+    auto begin = [&](const unsigned char* place, int t, int s, float& xx, float& uu, float& dot) {
         float2 sx = both(0.0f), su = both(0.0f), sg = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (!FULL && !have[i]) continue;
+            if (!FULL && !ODD && !have[i]) continue;
             if (has_dn) {
-                x[i] = *reinterpret_cast<const Raw*>(place + act[i]);
-                dn[i] = *reinterpret_cast<const typename RawUnit<X, false>::type*>(place + row_bytes + off[i]);
-                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = load_pairs<float>(w_post[i] + to_pre);
+                x[i] = raw_x(place, t, i);
+                dn[i] = raw_row(place, t, 1, i);
+                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = weight(false, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (!CK) sx = __ffma2_rn(xv.p[j], xv.p[j], sx);
@@ -849,7 +997,7 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
                 }
             }
             if (!CK && s >= 0) {
-                const Unit8 v = activation(place + act[i] + act_bytes);
+                const Unit8 v = widen<X>(raw_u(place, t, s, i));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) su = __ffma2_rn(v.p[j], v.p[j], su);
             }
@@ -866,7 +1014,7 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
         f = table[0];
         place = ring.wait();
         ring.next();
-        begin(place, f.s, xx, uu, dot);
+        begin(place, t_first, f.s, xx, uu, dot);
         total.three(xx, uu, dot);
     }
     int n = 0;   // the row's number within the group
@@ -884,12 +1032,12 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
         float2 sk = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (!FULL && !have[i]) continue;
+            if (!FULL && !ODD && !have[i]) continue;
             Unit8 D;
             clear(D);
-            if (has_up) D = load_pairs<X>(place + off[i]);
+            if (has_up) D = widen<X>(raw_row(place, t, 0, i));
             if (has_dn) {
-                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = load_pairs<float>(w_post[i] + to_pre);
+                const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = weight(false, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     D.p[j] = __ffma2_rn(cx, xv.p[j], __ffma2_rn(q2, __fmul2_rn(g.p[j], w.p[j]), D.p[j]));
@@ -897,8 +1045,8 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
                 }
             }
             if (f.s >= 0) {
-                u[i] = *reinterpret_cast<const Raw*>(place + act[i] + act_bytes);
-                const Unit8 v = widen<X>(u[i]), w = load_pairs<float>(w_post[i]);
+                u[i] = raw_u(place, t, f.s, i);
+                const Unit8 v = widen<X>(u[i]), w = weight(true, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 du = __fmul2_rn(D.p[j], v.p[j]);
@@ -910,7 +1058,7 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             if (has_dh) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) D.p[j] = __fmul2_rn(a2, D.p[j]);
-                store_pairs<X>(dh_row + off[i], D);
+                store_unit<X, ODD>(dh_row, off[i], first[i], tpr, a.H, D);
             }
         }
         dh_row += dh_step;
@@ -922,7 +1070,7 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             at = ring.place;
             place = ring.wait();
             ring.next();
-            begin(place, f.s, xx, uu, dot);
+            begin(place, t + t_step, f.s, xx, uu, dot);
         }
         float k = sk.x + sk.y;
         total.four(k, xx, uu, dot);
@@ -935,11 +1083,11 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             const float2 rg2 = both(rg), cu = both(-rg * us * (k * inv_h));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (!FULL && !have[i]) continue;
+                if (!FULL && !ODD && !have[i]) continue;
                 const Unit8 v = widen<X>(u[i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) e[i].p[j] = __ffma2_rn(cu, v.p[j], __fmul2_rn(rg2, e[i].p[j]));
-                store_pairs<X>(static_cast<unsigned char*>(a.dy) + (size_t)here.s * row_bytes + off[i], e[i]);
+                store_unit<X, ODD>(static_cast<unsigned char*>(a.dy) + (size_t)here.s * row_bytes, off[i], first[i], tpr, a.H, e[i]);
             }
         }
     }
@@ -951,20 +1099,18 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             if (group == g)
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (have[i])
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int c = (lane + i * tpr) * 8 + 2 * j;
-                            float2* post = reinterpret_cast<float2*>(cols + c);
-                            float2* pre = reinterpret_cast<float2*>(cols + a.H + c);
-                            float2 p = acc_post[i].p[j], m = acc_pre[i].p[j];
-                            if (g) { p = __fadd2_rn(p, *post); m = __fadd2_rn(m, *pre); }
-                            if (g + 1 < a.groups) { *post = p; *pre = m; }
-                            else {
-                                if (a.part_post) *reinterpret_cast<float2*>(a.part_post + (size_t)blockIdx.x * a.H + c) = p;
-                                if (a.part_pre) *reinterpret_cast<float2*>(a.part_pre + (size_t)blockIdx.x * a.H + c) = m;
-                            }
+                    for (int j = 0; j < 8; ++j) {
+                        const int c = ODD ? first[i] + j * tpr : (lane + i * tpr) * 8 + j;
+                        if (c >= a.H) continue;
+                        float p = j & 1 ? acc_post[i].p[j / 2].y : acc_post[i].p[j / 2].x, m = j & 1 ? acc_pre[i].p[j / 2].y : acc_pre[i].p[j / 2].x;
+                        if (g) { p += cols[c]; m += cols[a.H + c]; }
+                        if (g + 1 < a.groups) { cols[c] = p; cols[a.H + c] = m; }
+                        else {
+                            if (a.part_post) a.part_post[(size_t)blockIdx.x * a.H + c] = p;
+                            if (a.part_pre) a.part_pre[(size_t)blockIdx.x * a.H + c] = m;
                         }
+                    }
             __syncthreads();
         }
     }
@@ -976,7 +1122,8 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             unsigned empty = __ballot_sync(0xffffffffu, row0 + l < a.rows && a.inv[row0 + l] < 0);
             for (; empty; empty &= empty - 1) {
                 unsigned char* to = static_cast<unsigned char*>(a.dy) + (size_t)(row0 + __ffs(empty) - 1) * row_bytes;
-                for (int un = lane; un < units; un += tpr) store_pairs<X>(to + un * UB, z);
+                if constexpr (ODD) for (int c = lane; c < a.H; c += tpr) reinterpret_cast<X*>(to)[c] = 0;
+                else for (int un = lane; un < units; un += tpr) store_pairs<X>(to + un * UB, z);
             }
         }
     }
@@ -1032,6 +1179,7 @@ int ring_depth(int groups, int stage, int extra) {
     return d < 2 ? 0 : d;
 }
 size_t ring_bytes(int groups, int depth, int stage) { return (size_t)groups * (depth * (stage + 16) + kTable * sizeof(RowInfo)); }
+int round16(int n) { return (n + 15) / 16 * 16; }
 template <typename K>
 bool allow_smem(K kernel, size_t bytes) {
     if (bytes <= 32 << 10) return true;   // with the static strips within the 48 KB that need no leave
@@ -1042,8 +1190,10 @@ bool allow_smem(K kernel, size_t bytes) {
 
 template <typename X>
 int forward(NormArgs& a, cudaStream_t st) {
-    const bool wide = a.H % 8 == 0 && aligned(a.h, 16) && aligned(a.y, 16) && aligned(a.h_out, 16) && aligned(a.n_out, 16) &&
-                      aligned(a.w_post, 16) && aligned(a.w_pre, 16) && aligned(a.u8, 8) && aligned(a.x8, 8);
+    // bulk copies and vectors need arrays that begin at their boundaries; rows may begin anywhere
+    const bool based = aligned(a.h, 16) && aligned(a.y, 16) && aligned(a.h_out, 16) && aligned(a.n_out, 16) && aligned(a.w_post, 16) &&
+                       aligned(a.w_pre, 16) && aligned(a.u8, 8) && aligned(a.x8, 8);
+    const bool wide = based && a.H % 8 == 0;
     const int units = wide ? a.H / 8 : a.H;
     auto launch = [&](auto kernel, const RowPlan& p, int ctas, size_t smem) {
         a.tpr = p.tpr; a.groups = p.groups;
@@ -1054,15 +1204,17 @@ int forward(NormArgs& a, cudaStream_t st) {
         if (!allow_smem(kernel, smem)) return (int)LOCMOE_ERR_CUDA;
         return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
     };
-    if (wide && units <= 2 * kRingThreads) {
-        const RowPlan p = plan_rows(units, 2, kRingThreads, a.T);
-        const int stage = 2 * a.H * (int)sizeof(X);
+    if (based && a.H <= 16 * kRingThreads) {
+        const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X);
+        const RowPlan p = plan_rows(eights, 2, kRingThreads, a.T);
+        const int stage = 2 * (wide ? row : round16(row + 15));
         a.depth = ring_depth(p.groups, stage, 0);
         const size_t smem = ring_bytes(p.groups, a.depth, stage);
         if (a.depth) {
-            const bool full = units == 2 * p.tpr;
-            if (a.u8 || a.x8) return full ? launch(block_norm_ring_kernel<X, true, true>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, true>, p, 1, smem);
-            return full ? launch(block_norm_ring_kernel<X, true, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false>, p, 1, smem);
+            const bool full = eights == 2 * p.tpr, ck = a.u8 || a.x8;
+            if (!wide) return ck ? launch(block_norm_ring_kernel<X, false, true, true>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false, true>, p, 1, smem);
+            if (ck) return full ? launch(block_norm_ring_kernel<X, true, true, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, true, false>, p, 1, smem);
+            return full ? launch(block_norm_ring_kernel<X, true, false, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false, false>, p, 1, smem);
         }
     }
     const int nv = wide ? 0 : (units <= 1024 * 8 ? 8 : 0);
@@ -1074,10 +1226,9 @@ int forward(NormArgs& a, cudaStream_t st) {
 
 template <typename X, bool CK>
 int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
-    const bool wide = a.H % 8 == 0 && aligned(a.dh_out, 16) && aligned(a.dn, 16) && aligned(a.h_out, 16) && aligned(a.y, 16) &&
-                      aligned(a.x8, 8) && aligned(a.u8, 8) && aligned(a.w_post, 16) && aligned(a.w_pre, 16) && aligned(a.dh, 16) &&
-                      aligned(a.dy, 16);
-    const bool bulk = wide && (!CK || (a.H % 16 == 0 && aligned(a.x8, 16) && aligned(a.u8, 16)));   // rows that bulk copies can move
+    const bool based = aligned(a.dh_out, 16) && aligned(a.dn, 16) && aligned(a.h_out, 16) && aligned(a.y, 16) && aligned(a.x8, 16) &&
+                       aligned(a.u8, 16) && aligned(a.w_post, 16) && aligned(a.w_pre, 16) && aligned(a.dh, 16) && aligned(a.dy, 16);
+    const bool wide = based && a.H % 8 == 0;
     const int units = wide ? a.H / 8 : a.H;
     long long grid = 0;
     auto launch = [&](auto kernel, const RowPlan& p, int ctas, size_t smem) {
@@ -1091,18 +1242,22 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     };
     int rc = LOCMOE_OK;
     bool done = false;
-    if (bulk && units <= 1024) {
-        const int nv = units <= kRingThreads ? 1 : 2;
-        const RowPlan p = plan_rows(units, nv, nv == 1 ? kRingThreads : 512, a.T);
-        const int stage = 2 * a.H * ((int)sizeof(X) + (CK ? 1 : (int)sizeof(X))), extra = 8 * a.H;
+    if (based && a.H <= 8 * 1024) {
+        const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X), act = CK ? a.H : row;
+        const int nv = eights <= kRingThreads ? 1 : 2;
+        const RowPlan p = plan_rows(eights, nv, nv == 1 ? kRingThreads : 512, a.T);
+        const bool whole = wide && act % 16 == 0;   // all rows are whole 16-byte pieces
+        const int stage = whole ? 2 * (row + act) : 2 * (round16(row + 15) + round16(act + 15)), extra = 8 * a.H;
         a.depth = ring_depth(p.groups, stage, extra);
         if (a.depth) {
             const size_t smem = ring_bytes(p.groups, a.depth, stage) + extra;
             const bool all = a.dh_out && a.dn && (CK ? (const void*)a.u8 : a.y) && a.dh && a.dy;
-            if (nv == 2) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false>, p, 1, smem);
-            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, false>, p, 1, smem);
-            else if (units == p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, true, true>, p, 1, smem);
-            else rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, true>, p, 1, smem);
+            if (!whole) rc = nv == 2 ? launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, true>, p, 1, smem)
+                                    : launch(block_norm_grad_ring_kernel<X, CK, 1, false, false, true>, p, 1, smem);
+            else if (nv == 2) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false>, p, 1, smem);
+            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, false, false>, p, 1, smem);
+            else if (eights == p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, true, true, false>, p, 1, smem);
+            else rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, true, false>, p, 1, smem);
             done = true;
         }
     }

@@ -74,7 +74,8 @@ def _near_code(got, want):
 
 
 SHAPES = [(1, 8), (1, 1), (3, 64), (7, 256), (130, 520), (300, 1024), (17, 5120), (64, 2560), (5, 777), (33, 1001), (9, 4104), (3, 8191),
-          (4, 16384), (2, 16392), (2, 40000), (3, 9999), (1, 8193), (1000, 40), (2500, 96)]
+          (4, 16384), (2, 16392), (2, 40000), (3, 9999), (1, 8193), (1000, 40), (2500, 96), (700, 3), (301, 13), (400, 6), (2001, 77), (350, 5119), (160, 6001),
+          (90, 8184)]
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
