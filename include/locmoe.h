@@ -68,7 +68,7 @@ enum {
     LOCMOE_ERR_ALIGN = -4,     /* a pointer lacks the stated alignment                 */
     LOCMOE_ERR_WORKSPACE = -5, /* ws too small or misaligned                           */
     LOCMOE_ERR_CUDA = -6,      /* a CUDA call failed (launch error is cleared)         */
-    LOCMOE_ERR_TOO_LARGE = -7  /* size beyond what the entry point is built for       */
+    LOCMOE_ERR_TOO_LARGE = -7  /* size beyond the built-in scratch of a no-allocation call, or its limit */
 };
 enum {                         /* bits of the device status word                       */
     LOCMOE_WARN_CLAMPED = 1,   /* C_local > C_alloc: capacity clamped to C_alloc       */
