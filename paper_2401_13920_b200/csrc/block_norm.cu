@@ -859,6 +859,7 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
     ring.leave();
 }
 
+constexpr int kGradThreads = 384;
 // Gradient.  Written with the raw rows x', u' (x = xs x', u = us u'; codes: xs = us = 1):
 //   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
 //   e = D w_post,  k = us sum(e u'),  dv = R r e - cu u',  cu = R r us k / H
@@ -869,8 +870,8 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
 // NV: units of a thread, one up to rows of 5120 (640 threads), else two (512 threads).  FULL: every thread has them all.
 // ALL: both upstream gradients, the branch, dh and dy are there.  ODD: see above (also rows of
 // codes that are no whole 16-byte pieces).
-template <typename X, bool CK, int NV, bool FULL, bool ALL, bool ODD>
-__global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_ring_kernel(const NormGradArgs a) {
+template <typename X, bool CK, int NV, bool WREG, bool FULL, bool ALL, bool ODD>
+__global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_ring_kernel(const NormGradArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
     pdl_wait();
@@ -888,64 +889,49 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
     const uint32_t row_pitch = ODD ? (row_bytes + 30) / 16 * 16 : row_bytes, act_pitch = ODD ? (act_bytes + 30) / 16 * 16 : act_bytes;
     unsigned char* after = ring_mem + (size_t)a.groups * a.depth * (2 * (row_pitch + act_pitch) + 16);
     RowInfo* table = reinterpret_cast<RowInfo*>(after) + group * kTable;
-    float* weights = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H]: w_post, w_pre
+    float* weights = reinterpret_cast<float*>(after + a.groups * kTable * sizeof(RowInfo));   // [2][H]: w_post, w_pre (not WREG)
     for (int i = lane; i < kTable; i += tpr) table[i] = info_of<CK>(a, branch, t_first + (long long)i * t_step);
-    for (int c = threadIdx.x; c < a.H; c += blockDim.x) {
+    for (int c = threadIdx.x; c < a.H && !WREG; c += blockDim.x) {
         weights[c] = a.w_post ? a.w_post[c] : 1.0f;
         weights[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
     }
     // places of [dh_out][dn][h_out or x8][y or u8]; with a barrier of the CTA
     RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_pitch + act_pitch));
-    // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
-    auto ask = [&](long long t, int s, int place, int from, int by) {
-        if (t >= a.T) return;
+    // Row t, whose output row is s, into a place: by four lanes, one an array.
+    const unsigned char* from = nullptr;
+    uint32_t len = 0, at_place = 0;
+    if (lane < 4) {
+        from = lane == 0 ? static_cast<const unsigned char*>(a.dh_out) : lane == 1 ? static_cast<const unsigned char*>(a.dn) :
+               lane == 2 ? (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) :
+                           (CK ? reinterpret_cast<const unsigned char*>(a.u8) : static_cast<const unsigned char*>(a.y));
+        if (lane == 2 && !has_dn) from = nullptr;
+        len = lane < 2 ? row_bytes : act_bytes;
+        at_place = lane < 2 ? lane * row_pitch : 2 * row_pitch + (lane - 2) * act_pitch;
+    }
+    const uint32_t bytes_always = (has_up ? row_bytes : 0u) + (has_dn ? row_bytes + act_bytes : 0u);
+    auto ask = [&](long long t, int s, int place) {
         uint64_t* bar = ring.bars + place;
-        unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
+        unsigned char* to = ring.base + (uint32_t)(place * ring.stage) + at_place;
+        const bool wanted = from && (lane < 3 || s >= 0);
+        const size_t row = lane == 3 && !CK ? (size_t)s : (size_t)t;   // codes lie in token order, the block's output in slot order
         if constexpr (!ODD) {
-            if (from == 0) mbar_expect_tx(bar, (has_up ? row_bytes : 0u) + (has_dn ? row_bytes + act_bytes : 0u) + (s >= 0 ? act_bytes : 0u));
-            for (int k = from; k < 4; k += by)
-                if (k == 0) {
-                    if (has_up) bulk_g2s(to, static_cast<const unsigned char*>(a.dh_out) + t * row_bytes, row_bytes, bar);
-                } else if (k == 1) {
-                    if (has_dn) bulk_g2s(to + row_bytes, static_cast<const unsigned char*>(a.dn) + t * row_bytes, row_bytes, bar);
-                } else if (k == 2) {
-                    if (has_dn) bulk_g2s(to + 2 * row_bytes, (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) + t * act_bytes, act_bytes, bar);
-                } else if (s >= 0) {   // codes lie in token order, the block's output in slot order
-                    bulk_g2s(to + 2 * row_bytes + act_bytes, CK ? reinterpret_cast<const unsigned char*>(a.u8) + t * act_bytes : static_cast<const unsigned char*>(a.y) + (size_t)s * act_bytes, act_bytes, bar);
-                }
-            return;
-        }
-        const unsigned char* base[4] = {static_cast<const unsigned char*>(a.dh_out), static_cast<const unsigned char*>(a.dn),
-                                        CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out),
-                                        CK ? reinterpret_cast<const unsigned char*>(a.u8) : static_cast<const unsigned char*>(a.y)};
-        const bool wanted[4] = {a.dh_out != nullptr, a.dn != nullptr, a.dn != nullptr, s >= 0};
-        auto piece = [&](int k) -> Piece {
-            if (!wanted[k]) return {0, 0, 0};
-            const uint32_t len = k < 2 ? row_bytes : act_bytes;
-            const size_t at = (size_t)(k == 3 && !CK ? s : t) * len;
-            return piece_of(at, len, (size_t)(k == 3 && !CK ? a.rows : a.T) * len);
-        };
-        auto place_of = [&](int k) { return to + (k < 2 ? k * row_pitch : 2 * row_pitch + (k - 2) * act_pitch); };
-        if (from == 0) {
-            uint32_t bytes = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const Piece p = piece(k);
-                bytes += p.bytes;
-                tail_of(place_of(k), base[k], p);
-            }
-            mbar_expect_tx(bar, bytes);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k < from || (k - from) % by) continue;
-            const Piece p = piece(k);
-            if (p.bytes) bulk_g2s(place_of(k), base[k] + p.from, p.bytes, bar);
+            if (lane == 0) mbar_expect_tx(bar, bytes_always + (s >= 0 ? act_bytes : 0u));
+            if (wanted) bulk_g2s(to, from + row * len, len, bar);
+        } else {
+            Piece p{0, 0, 0};
+            if (wanted) p = piece_of(row * len, len, (size_t)(lane == 3 && !CK ? a.rows : a.T) * len);
+            tail_of(to, from, p);
+            uint32_t bytes = p.bytes;
+            bytes += __shfl_xor_sync(0xfu, bytes, 1);
+            bytes += __shfl_xor_sync(0xfu, bytes, 2);
+            __syncwarp(0xfu);   // the tails lie before the arrival
+            if (lane == 0) mbar_expect_tx(bar, bytes);
+            if (p.bytes) bulk_g2s(to, from + p.from, p.bytes, bar);
         }
     };
-    const int asks = lane % kWarp ? 4 : lane / kWarp;   // from which array on this thread asks (4 and more: none)
-    if (lane == 0)
-        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d, 0, 1);
+    if (lane < 4)
+        for (int d = 0; d < a.depth; ++d)
+            if (t_first + (long long)d * t_step < a.T) ask(t_first + (long long)d * t_step, table[d].s, d);
     // this thread's places in a row, in its activations, in the weights
     bool have[NV];
     uint32_t off[NV], act[NV];
@@ -958,9 +944,18 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
         act[i] = un * AB;
         first[i] = lane + 8 * i * tpr;   // ODD: this thread's elements are first + j * tpr
     }
+    Unit8 w_own[WREG ? 2 * NV : 1];
+    if constexpr (WREG)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (FULL || ODD || have[i]) {
+                w_own[i] = weight_unit<ODD>(a.w_post, lane + i * tpr, first[i], tpr, a.H);
+                w_own[NV + i] = weight_unit<ODD>(a.w_pre, lane + i * tpr, first[i], tpr, a.H);
+            }
     auto weight = [&](bool post, int i) {
         const float* w = weights + (post ? 0 : a.H);
-        if constexpr (ODD) return widen<float>(load_raw<float, false, true>(reinterpret_cast<const unsigned char*>(w), 0, first[i], tpr, a.H));
+        if constexpr (WREG) return w_own[post ? i : NV + i];
+        else if constexpr (ODD) return widen<float>(load_raw<float, false, true>(reinterpret_cast<const unsigned char*>(w), 0, first[i], tpr, a.H));
         else return load_pairs<float>(reinterpret_cast<const unsigned char*>(w + (lane + i * tpr) * 8));
     };
     using Raw = typename RawUnit<X, CK>::type;
@@ -1037,6 +1032,10 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
             clear(D);
             if (has_up) D = widen<X>(raw_row(place, t, 0, i));
             if (has_dn) {
+                if constexpr (sizeof(X) == 4) {   // too many registers to keep
+                    x[i] = raw_x(place, t, i);
+                    dn[i] = raw_row(place, t, 1, i);
+                }
                 const Unit8 xv = widen<X>(x[i]), g = widen<X>(dn[i]), w = weight(false, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -1075,7 +1074,8 @@ __global__ void __launch_bounds__(NV == 1 ? kRingThreads : 512) block_norm_grad_
         float k = sk.x + sk.y;
         total.four(k, xx, uu, dot);
         __syncwarp();
-        if (asks < 4) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, was, asks, tpr / kWarp);   // the group is done with the row
+        if (lane < 4 && t + (long long)a.depth * t_step < a.T)   // the group is done with the row
+            ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, was);
         k *= us;
         if (lane == 0 && a.dgate) a.dgate[t] = k;
         if (has_dy && here.s >= 0) {
@@ -1244,20 +1244,20 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     bool done = false;
     if (based && a.H <= 8 * 1024) {
         const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X), act = CK ? a.H : row;
-        const int nv = eights <= kRingThreads ? 1 : 2;
-        const RowPlan p = plan_rows(eights, nv, nv == 1 ? kRingThreads : 512, a.T);
+        const bool wreg = eights <= 2 * kGradThreads;
+        const RowPlan p = plan_rows(eights, 2, wreg ? kGradThreads : 512, a.T);
         const bool whole = wide && act % 16 == 0;   // all rows are whole 16-byte pieces
-        const int stage = whole ? 2 * (row + act) : 2 * (round16(row + 15) + round16(act + 15)), extra = 8 * a.H;
+        const int stage = whole ? 2 * (row + act) : 2 * (round16(row + 15) + round16(act + 15)), extra = wreg ? 0 : 8 * a.H;
         a.depth = ring_depth(p.groups, stage, extra);
         if (a.depth) {
             const size_t smem = ring_bytes(p.groups, a.depth, stage) + extra;
             const bool all = a.dh_out && a.dn && (CK ? (const void*)a.u8 : a.y) && a.dh && a.dy;
-            if (!whole) rc = nv == 2 ? launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, true>, p, 1, smem)
-                                    : launch(block_norm_grad_ring_kernel<X, CK, 1, false, false, true>, p, 1, smem);
-            else if (nv == 2) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false>, p, 1, smem);
-            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, false, false>, p, 1, smem);
-            else if (eights == p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 1, true, true, false>, p, 1, smem);
-            else rc = launch(block_norm_grad_ring_kernel<X, CK, 1, false, true, false>, p, 1, smem);
+            if (!whole) rc = wreg ? launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, false, true>, p, 1, smem)
+                                  : launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false, true>, p, 1, smem);
+            else if (!wreg) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false, false>, p, 1, smem);
+            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, false, false>, p, 1, smem);
+            else if (eights == 2 * p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, true, true, false>, p, 1, smem);
+            else rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, true, false>, p, 1, smem);
             done = true;
         }
     }
