@@ -396,10 +396,10 @@ __device__ __forceinline__ RowInfo info_of(const NormGradArgs& a, bool branch, l
 }
 
 // Rings of all groups lie one after the other, then their barriers (16 bytes a place are kept, so that what follows is aligned).
-__device__ __forceinline__ RowRing ring_of(unsigned char* smem, int group, int groups, int depth, int stage) {
+__device__ __forceinline__ RowRing ring_of(unsigned char* smem, int group, int groups, int depth, int stage, int askers) {
     RowRing r{smem + (size_t)group * depth * stage, reinterpret_cast<uint64_t*>(smem + (size_t)groups * depth * stage) + group * depth, stage,
               depth, 0, 0u, false};
-    for (int i = threadIdx.x; i < groups * depth; i += blockDim.x) mbar_init(reinterpret_cast<uint64_t*>(smem + (size_t)groups * depth * stage) + i, 1);
+    for (int i = threadIdx.x; i < groups * depth; i += blockDim.x) mbar_init(reinterpret_cast<uint64_t*>(smem + (size_t)groups * depth * stage) + i, askers);
     mbar_init_fence();
     __syncthreads();
     return r;
@@ -767,36 +767,27 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
             wp[i] = weight_unit<ODD>(a.w_post, lane + i * tpr, first[i], tpr, a.H);
             wn[i] = weight_unit<ODD>(a.w_pre, lane + i * tpr, first[i], tpr, a.H);
         }
-    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)pitch);   // places of [h][y]; with a barrier of the CTA
-    // Row t, whose output row is s, into a place: the arrays `from`, `from` + `by`, ... of it, by one thread.
-    auto ask = [&](long long t, int s, int place, int from, int by) {
-        if (t >= a.T) return;
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)pitch, 2);   // places of [h][y]; with a barrier of the CTA
+    // Row t, whose output row is s, into a place: h by the group's first thread, y by one of another warp where there is one.
+    const int asked = lane == 0 ? 0 : 1;
+    const bool asks = lane == 0 || lane == (tpr > kWarp ? kWarp : 1);
+    const unsigned char* from = static_cast<const unsigned char*>(asked ? a.y : a.h);
+    auto ask = [&](int t, int s, int place) {
         uint64_t* bar = ring.bars + place;
-        unsigned char* to = ring.base + (uint32_t)(place * ring.stage);
-        const unsigned char *h = static_cast<const unsigned char*>(a.h), *y = static_cast<const unsigned char*>(a.y);
-        if constexpr (!ODD) {
-            if (from == 0) mbar_expect_tx(bar, s >= 0 ? 2 * row_bytes : row_bytes);
-            for (int k = from; k < 2; k += by)
-                if (k == 0) bulk_g2s(to, h + t * row_bytes, row_bytes, bar);
-                else if (s >= 0) bulk_g2s(to + row_bytes, y + (size_t)s * row_bytes, row_bytes, bar);
-        } else {
-            const Piece ph = piece_of((size_t)t * row_bytes, row_bytes, (size_t)a.T * row_bytes);
-            Piece py{0, 0, 0};
-            if (s >= 0) py = piece_of((size_t)s * row_bytes, row_bytes, (size_t)a.rows * row_bytes);
-            if (from == 0) {
-                tail_of(to, h, ph);
-                tail_of(to + pitch, y, py);
-                mbar_expect_tx(bar, ph.bytes + py.bytes);
-            }
-            for (int k = from; k < 2; k += by) {
-                const Piece& p = k ? py : ph;
-                if (p.bytes) bulk_g2s(to + k * pitch, (k ? y : h) + p.from, p.bytes, bar);
-            }
+        unsigned char* to = ring.base + (uint32_t)(place * ring.stage) + asked * pitch;
+        const bool wanted = !asked || s >= 0;
+        const size_t off = (size_t)(uint32_t)(asked ? s : t) * row_bytes;
+        Piece p{off, wanted ? row_bytes : 0u, 0u};
+        if constexpr (ODD) {
+            if (wanted) p = piece_of(off, row_bytes, (size_t)(asked ? a.rows : a.T) * row_bytes);
+            tail_of(to, from, p);
         }
+        mbar_expect_tx(bar, p.bytes);
+        if (p.bytes) bulk_g2s(to, from + p.from, p.bytes, bar);
     };
-    const int asks = lane % kWarp ? 2 : lane / kWarp;   // from which array on this thread asks (2: none)
-    if (lane == 0)
-        for (int d = 0; d < a.depth; ++d) ask(t_first + (long long)d * t_step, table[d].s, d, 0, 1);
+    if (asks)
+        for (int d = 0; d < a.depth && t_first + (long long)d * t_step < a.T; ++d) ask(t_first + d * t_step, table[d].s, d);
+    const int ahead = a.depth * t_step, last_ask = a.T - ahead;
     RowInfo soon{};
     int n = 0;   // the row's number within the group
     for (int t = t_first; t < a.T; t += t_step, ++n) {
@@ -822,7 +813,7 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
             for (int j = 0; j < 4; ++j) acc = __ffma2_rn(v[i].p[j], v[i].p[j], acc);
         float sum = total.one(acc.x + acc.y);
         __syncwarp();
-        if (asks < 2) ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, ring.place, asks, tpr / kWarp);   // the group has taken the row
+        if (asks && t < last_ask) ask(t + ahead, table[(n + a.depth) & (kTable - 1)].s, ring.place);   // the group has taken the row
         ring.next();
         const float r = rsqrtf(fmaf(sum, inv_h, a.eps));
         if (CKPT && a.r_post && lane == 0) a.r_post[t] = r;
@@ -896,42 +887,37 @@ __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_rin
         weights[a.H + c] = a.w_pre ? a.w_pre[c] : 1.0f;
     }
     // places of [dh_out][dn][h_out or x8][y or u8]; with a barrier of the CTA
-    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_pitch + act_pitch));
-    // Row t, whose output row is s, into a place: by four lanes, one an array.
+    RowRing ring = ring_of(ring_mem, group, a.groups, a.depth, 2 * (int)(row_pitch + act_pitch), 4);
+    // Row t, whose output row is s, into a place: by four threads of different warps where there are four, one an array.
+    const int wide4 = tpr / kWarp, asked = (lane % kWarp) * wide4 + lane / kWarp;
+    const bool asks = lane % kWarp * wide4 < 4 && asked < 4;
     const unsigned char* from = nullptr;
     uint32_t len = 0, at_place = 0;
-    if (lane < 4) {
-        from = lane == 0 ? static_cast<const unsigned char*>(a.dh_out) : lane == 1 ? static_cast<const unsigned char*>(a.dn) :
-               lane == 2 ? (CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out)) :
-                           (CK ? reinterpret_cast<const unsigned char*>(a.u8) : static_cast<const unsigned char*>(a.y));
-        if (lane == 2 && !has_dn) from = nullptr;
-        len = lane < 2 ? row_bytes : act_bytes;
-        at_place = lane < 2 ? lane * row_pitch : 2 * row_pitch + (lane - 2) * act_pitch;
+    if (asks) {
+        if (asked == 0) from = static_cast<const unsigned char*>(a.dh_out);
+        else if (asked == 1) from = static_cast<const unsigned char*>(a.dn);
+        else if (asked == 2) from = !has_dn ? nullptr : CK ? reinterpret_cast<const unsigned char*>(a.x8) : static_cast<const unsigned char*>(a.h_out);
+        else from = CK ? reinterpret_cast<const unsigned char*>(a.u8) : static_cast<const unsigned char*>(a.y);
+        len = asked < 2 ? row_bytes : act_bytes;
+        at_place = asked < 2 ? asked * row_pitch : 2 * row_pitch + (asked - 2) * act_pitch;
     }
-    const uint32_t bytes_always = (has_up ? row_bytes : 0u) + (has_dn ? row_bytes + act_bytes : 0u);
-    auto ask = [&](long long t, int s, int place) {
+    const bool slots = asked == 3 && !CK;   // codes lie in token order, the block's output in slot order
+    auto ask = [&](int t, int s, int place) {
         uint64_t* bar = ring.bars + place;
         unsigned char* to = ring.base + (uint32_t)(place * ring.stage) + at_place;
-        const bool wanted = from && (lane < 3 || s >= 0);
-        const size_t row = lane == 3 && !CK ? (size_t)s : (size_t)t;   // codes lie in token order, the block's output in slot order
-        if constexpr (!ODD) {
-            if (lane == 0) mbar_expect_tx(bar, bytes_always + (s >= 0 ? act_bytes : 0u));
-            if (wanted) bulk_g2s(to, from + row * len, len, bar);
-        } else {
-            Piece p{0, 0, 0};
-            if (wanted) p = piece_of(row * len, len, (size_t)(lane == 3 && !CK ? a.rows : a.T) * len);
+        const bool wanted = from && (asked < 3 || s >= 0);
+        const size_t off = (size_t)(uint32_t)(slots ? s : t) * len;
+        Piece p{off, wanted ? len : 0u, 0u};
+        if constexpr (ODD) {
+            if (wanted) p = piece_of(off, len, (size_t)(slots ? a.rows : a.T) * len);
             tail_of(to, from, p);
-            uint32_t bytes = p.bytes;
-            bytes += __shfl_xor_sync(0xfu, bytes, 1);
-            bytes += __shfl_xor_sync(0xfu, bytes, 2);
-            __syncwarp(0xfu);   // the tails lie before the arrival
-            if (lane == 0) mbar_expect_tx(bar, bytes);
-            if (p.bytes) bulk_g2s(to, from + p.from, p.bytes, bar);
         }
+        mbar_expect_tx(bar, p.bytes);
+        if (p.bytes) bulk_g2s(to, from + p.from, p.bytes, bar);
     };
-    if (lane < 4)
-        for (int d = 0; d < a.depth; ++d)
-            if (t_first + (long long)d * t_step < a.T) ask(t_first + (long long)d * t_step, table[d].s, d);
+    if (asks)
+        for (int d = 0; d < a.depth && t_first + (long long)d * t_step < a.T; ++d) ask(t_first + d * t_step, table[d].s, d);
+    const int ahead = a.depth * t_step, last_ask = a.T - ahead;
     // this thread's places in a row, in its activations, in the weights
     bool have[NV];
     uint32_t off[NV], act[NV];
@@ -1074,8 +1060,7 @@ __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_rin
         float k = sk.x + sk.y;
         total.four(k, xx, uu, dot);
         __syncwarp();
-        if (lane < 4 && t + (long long)a.depth * t_step < a.T)   // the group is done with the row
-            ask(t + (long long)a.depth * t_step, table[(n + a.depth) & (kTable - 1)].s, was);
+        if (asks && t < last_ask) ask(t + ahead, table[(n + a.depth) & (kTable - 1)].s, was);   // the group is done with the row
         k *= us;
         if (lane == 0 && a.dgate) a.dgate[t] = k;
         if (has_dy && here.s >= 0) {
