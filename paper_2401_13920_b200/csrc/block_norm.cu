@@ -1077,26 +1077,37 @@ __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_rin
         }
     }
     ring.leave();
-    if (a.part_post || a.part_pre) {   // groups add their columns one after the other, where the ring was: a fixed order
-        float* cols = reinterpret_cast<float*>(ring_mem);   // [2][H]
+    if (a.part_post || a.part_pre) {   // the groups' columns meet where the rings were (8 H bytes a group fit there), added in group order
+        float* cols = reinterpret_cast<float*>(ring_mem);   // [groups][2][H]
         __syncthreads();
-        for (int g = 0; g < a.groups; ++g) {
-            if (group == g)
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            float* to = cols + (size_t)group * 2 * a.H;
+            if constexpr (ODD) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int c = ODD ? first[i] + j * tpr : (lane + i * tpr) * 8 + j;
-                        if (c >= a.H) continue;
-                        float p = j & 1 ? acc_post[i].p[j / 2].y : acc_post[i].p[j / 2].x, m = j & 1 ? acc_pre[i].p[j / 2].y : acc_pre[i].p[j / 2].x;
-                        if (g) { p += cols[c]; m += cols[a.H + c]; }
-                        if (g + 1 < a.groups) { cols[c] = p; cols[a.H + c] = m; }
-                        else {
-                            if (a.part_post) a.part_post[(size_t)blockIdx.x * a.H + c] = p;
-                            if (a.part_pre) a.part_pre[(size_t)blockIdx.x * a.H + c] = m;
-                        }
-                    }
-            __syncthreads();
+                for (int j = 0; j < 8; ++j) {
+                    const int c = first[i] + j * tpr;
+                    if (c >= a.H) continue;
+                    to[c] = j & 1 ? acc_post[i].p[j / 2].y : acc_post[i].p[j / 2].x;
+                    to[a.H + c] = j & 1 ? acc_pre[i].p[j / 2].y : acc_pre[i].p[j / 2].x;
+                }
+            } else if (FULL || have[i]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    reinterpret_cast<float2*>(to)[(lane + i * tpr) * 4 + j] = acc_post[i].p[j];
+                    reinterpret_cast<float2*>(to + a.H)[(lane + i * tpr) * 4 + j] = acc_pre[i].p[j];
+                }
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * a.H; c += blockDim.x) {
+            float v = cols[c];
+            for (int g = 1; g < a.groups; ++g) v += cols[(size_t)g * 2 * a.H + c];
+            if (c < a.H) {
+                if (a.part_post) a.part_post[(size_t)blockIdx.x * a.H + c] = v;
+            } else if (a.part_pre) {
+                a.part_pre[(size_t)blockIdx.x * a.H + c - a.H] = v;
+            }
         }
     }
     if (a.dy && a.inv) {   // rows of the slot buffer that no token owns have a zero gradient
@@ -1114,8 +1125,8 @@ __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_rin
     }
 }
 
-// Column sums: the CTAs' rows of the workspace added in index order (fp32, 8 interleaved chains joined in order).
-constexpr int kColThreads = 256, kColChains = 8;
+// Column sums: the CTAs' rows of the workspace added in index order (fp32, 16 interleaved chains joined in order).
+constexpr int kColThreads = 512, kColChains = 16;
 __global__ void __launch_bounds__(kColThreads) block_norm_cols_kernel(const float* part_post, const float* part_pre, int parts, int H,
                                                                       float* dw_post, float* dw_pre) {
     __shared__ float strip[kColChains][32];
@@ -1127,6 +1138,7 @@ __global__ void __launch_bounds__(kColThreads) block_norm_cols_kernel(const floa
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), chain = threadIdx.x >> 5;
     float s = 0.0f;
     if (c < H)
+#pragma unroll 10
         for (int p = chain; p < parts; p += kColChains) s += part[(size_t)p * H + c];
     strip[chain][threadIdx.x & 31] = s;
     __syncthreads();
