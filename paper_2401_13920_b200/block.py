@@ -10,8 +10,26 @@ from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
+from torch._C._dynamo.guards import _empty_strided_cuda   # 0.7 us a tensor; torch.empty takes 2.3, as much as a launch
 
 from . import binding as B
+
+
+def _rows(n: int, width: int, dtype: torch.dtype) -> torch.Tensor:
+    return _empty_strided_cuda((n, width), (width, 1), dtype)
+
+
+def _flat(n: int, dtype: torch.dtype) -> torch.Tensor:
+    return _empty_strided_cuda((n,), (1,), dtype)
+
+
+_F32 = torch.float32
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    """Outputs, workspace and launch belong to the current device: so must the inputs."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s: on %s, which is not the current CUDA device" % (name, t.device))
 
 
 class Checkpoint(NamedTuple):
@@ -46,7 +64,9 @@ def _row_shape(like: torch.Tensor, y, slot) -> tuple:
         raise ValueError("expected a [T][H] tensor, got %s" % (tuple(like.shape),))
     T, H = like.shape
     rows = T if slot is None else y.shape[0]
-    return _shape(T, H, 1, like.dtype), rows
+    shape = _shape(T, H, 1, like.dtype)
+    _here(like, "rows")
+    return shape, rows
 
 
 def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
@@ -58,13 +78,12 @@ def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
     (T, H), (E, F, _) = x.shape, w_in.shape
     if w_in.shape[2] != H or w_out.shape != (E, H, F):
         raise ValueError("x %s, w_in %s and w_out %s do not belong together" % (tuple(x.shape), tuple(w_in.shape), tuple(w_out.shape)))
-    dev = x.device
-    out = torch.empty_like(x)
-    idx, w = torch.empty((K, T), dtype=torch.int32, device=dev), torch.empty((K, T), dtype=torch.float32, device=dev)
+    _here(x, "x")
+    out, idx, w = _rows(T, H, x.dtype), _rows(K, T, torch.int32), _rows(K, T, _F32)
     if T == 0:
         return out, idx, w
     shape, n = _few_plan(T, H, E, K, F, x.dtype)
-    ws = torch.empty((n,), dtype=torch.uint8, device=dev)
+    ws = _flat(n, torch.uint8)
     B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted, stream)
     return out, idx, w
 
@@ -76,22 +95,18 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
     Returns ``(h_out, n, ckpt)``; ``h_out`` / ``n`` are None when not wanted, ``ckpt`` a ``Checkpoint`` or None.  Without
     ``y`` the block has no branch (the norm before the first block; ``want_h`` = False leaves out the copy of h)."""
     shape, rows = _row_shape(h, y, slot)
-    T, H, dev = shape.T, shape.H, h.device
+    T, H = shape.T, shape.H
     if y is not None and y.shape[-1] != H:
         raise ValueError("y: rows of %d expected, got %d" % (H, y.shape[-1]))
-    if T == 0:
-        z = lambda *s, dt=h.dtype: torch.empty(*s, dtype=dt, device=dev)
-        ck = Checkpoint(z(0, H, dt=torch.float8_e4m3fn) if y is not None else None, z(0, H, dt=torch.float8_e4m3fn) if want_n else None,
-                        z(0, dt=torch.float32) if y is not None else None, z(0, dt=torch.float32) if want_n else None)
-        return z(0, H) if want_h else None, z(0, H) if want_n else None, ck if checkpoint else None
-    h_out = torch.empty_like(h) if want_h else None
-    n = torch.empty_like(h) if want_n else None
+    h_out = _rows(T, H, h.dtype) if want_h else None
+    n = _rows(T, H, h.dtype) if want_n else None
     u8 = x8 = r_post = r_pre = None
     if checkpoint and y is not None:
-        u8, r_post = torch.empty(T, H, dtype=torch.float8_e4m3fn, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
+        u8, r_post = _rows(T, H, torch.float8_e4m3fn), _flat(T, _F32)
     if checkpoint and want_n:
-        x8, r_pre = torch.empty(T, H, dtype=torch.float8_e4m3fn, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
-    B.locmoe_block_norm(shape, rows, h, y, slot, gate_w, w_post, w_pre, res_scale, eps, h_out, n, u8, x8, r_post, r_pre, stream)
+        x8, r_pre = _rows(T, H, torch.float8_e4m3fn), _flat(T, _F32)
+    if T > 0:
+        B.locmoe_block_norm(shape, rows, h, y, slot, gate_w, w_post, w_pre, res_scale, eps, h_out, n, u8, x8, r_post, r_pre, stream)
     return h_out, n, Checkpoint(u8, x8, r_post, r_pre) if checkpoint else None
 
 
@@ -108,13 +123,12 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
     if slot is not None and inv is None:
         raise ValueError("inv: needed with slot (it says how many rows y has and which of them are empty)")
     shape, rows = _row_shape(like, inv, slot if branch else None)
-    T, H, dev = shape.T, shape.H, like.device
-    f32 = dict(dtype=torch.float32, device=dev)
-    dh = torch.empty_like(like) if want_dh else None
-    dy = torch.empty(rows, H, dtype=like.dtype, device=dev) if want_dy and branch else None
-    dgate = torch.empty(T, **f32) if want_dgate and branch else None
-    dw_post = torch.empty(H, **f32) if want_dw and branch else None
-    dw_pre = torch.empty(H, **f32) if want_dw and dn is not None else None
+    T, H = shape.T, shape.H
+    dh = _rows(T, H, like.dtype) if want_dh else None
+    dy = _rows(rows, H, like.dtype) if want_dy and branch else None
+    dgate = _flat(T, _F32) if want_dgate and branch else None
+    dw_post = _flat(H, _F32) if want_dw and branch else None
+    dw_pre = _flat(H, _F32) if want_dw and dn is not None else None
     if T == 0:
         for t in (dy, dw_post, dw_pre):
             if t is not None:
@@ -122,7 +136,7 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
         return dh, dy, dgate, dw_post, dw_pre
     ws = None
     if dw_post is not None or dw_pre is not None:
-        ws = torch.empty(_grad_bytes(T, H, like.dtype, torch.cuda.current_device()), dtype=torch.uint8, device=dev)
+        ws = _flat(_grad_bytes(T, H, like.dtype, torch.cuda.current_device()), torch.uint8)
     acts = dict(u8=ck.u8, r_post=ck.r_post, x8=ck.x8 if dn is not None else None, r_pre=ck.r_pre if dn is not None else None) \
         if ck is not None else dict(y=y, h_out=h_out if dn is not None else None)
     B.locmoe_block_norm_grad(shape, rows, dh_out, dn, slot=slot if branch else None, inv=inv if branch and slot is not None else None,
