@@ -24,7 +24,9 @@ namespace {
 
 constexpr int kMaxTokens = LOCMOE_FEW_MAX_TOKENS, kMaxExperts = 1024, kMaxK = 8, kMaxSplit = 8;
 constexpr int kMostSmem = 226 << 10;   // of the 227 KB that a CTA can have
-constexpr int kInlineTokens = 8;         // up to here every CTA routes all tokens itself
+// Up to here every CTA routes all tokens itself, beyond that a kernel of its own does (H = 2560, F = 10240, E = 32: one token
+// 35.2 us against 35.9, 8 tokens 129.2 / 131.6, 9 tokens 147.4 / 147.5, 16 tokens 220.5 / 217.2).
+constexpr int kInlineTokens = 8;
 constexpr int kBoxK = 64;          // k of one TMA box: 128 bytes of a row
 
 __device__ int g_few_flags = 0;    // bit 0: a bounded wait gave up
@@ -254,7 +256,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a, const i
     __syncthreads();
     // The assignments sorted by expert, in ascending order within one: an expert's chunks of 16 * MT tokens may fall to
     // different CTAs, which must agree on what is in them.
-    if (TK <= 32) {   // one assignment a lane, one chunk an expert; every warp does it for itself and writes the same
+    if (TK <= 32 && a.T <= 16 * MT) {   // one assignment a lane, one chunk an expert; every warp does it for itself and writes the same
         const int e = lane < TK ? expert[lane] : 0x7fff;
         const unsigned same = __match_any_sync(0xffffffffu, e), below = (1u << lane) - 1u;
         const unsigned heads = __ballot_sync(0xffffffffu, lane < TK && (same & below) == 0);
@@ -614,10 +616,18 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
                     w_k, static_cast<uint16_t*>(out), reinterpret_cast<uint16_t*>(base + p.off_g),
                     reinterpret_cast<float*>(base + p.off_part), reinterpret_cast<int32_t*>(base + p.off_arrived), s.T, s.H, s.E, K, F,
                     p.max_split, weighted, s.T <= kInlineTokens};
-    if (s.T * K <= 2) return run_few<Variant<5, 1, 4, 1, 1, 1, 220 << 10>>(a, st);
+    // Which variant: measured on H = 2560, F = 10240, E = 32 (us), beside H = 1024, F = 1024, E = 4 where it says so.
+    // - Up to 8 assignments a task of 16 weight rows, its reduction shared out over four warps: few tasks, so a short way
+    //   through each counts (T = 1, K = 1: 31.4; tasks of 64 rows 31.9, of 128 rows 40.5.  T = 4, K = 2: 133 / 141 / 142).
+    //   Beyond, each warp has rows of its own and no sums to meet for (T = 16, K = 1: 260 / 217 / 231).
+    // - Tiles of 32 tokens and 128 rows where experts with more than 16 tokens are common and the tasks are still many:
+    //   T = 128, K = 2 684 against 849 with tiles of 16 and 64 rows, whose second chunk of tokens takes the weights
+    //   through shared memory again; T = 64, K = 2 577 / 629.  With fewer tokens an expert (T = 64, K = 1: 495 / 470) or
+    //   fewer tasks (the small layer at T = 128, K = 2: 112 / 66) the smaller tiles win.
     if (s.T * K <= 8) return run_few<Variant<3, 1, 4, 2, 1, 1, 220 << 10>>(a, st);
-    if (s.T <= 16) return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10>>(a, st);
-    return run_few<Variant<3, 4, 1, 4, 1, 2, 220 << 10>>(a, st);
+    if (s.T > 16 && (long long)s.T * K >= 4ll * s.E && (long long)s.E * ((F + 127) / 128) >= 4 * sm_count())
+        return run_few<Variant<3, 4, 1, 4, 1, 2, 220 << 10>>(a, st);
+    return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10>>(a, st);
 }
 
 int read_few_flags(int* out, cudaStream_t st) {

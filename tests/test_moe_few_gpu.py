@@ -89,6 +89,15 @@ def test_all_tokens_on_one_expert(K, T, F, k):
     _check(got, _reference(x, w_in, w_out, k, eps))
 
 
+@pytest.mark.parametrize("T,F,k,one", [(17, 18952, 1, False), (17, 18952, 1, True), (40, 19000, 2, False), (128, 18944, 1, False), (128, 19000, 2, True)])
+def test_wide_layer_with_many_tokens_an_expert(K, T, F, k, one):
+    """The tiles of 32 tokens: one to four of them an expert, rows and k that end inside a tile."""
+    x, w_in, w_out, eps = _inputs(T, 264, F, 4, F, bias=True)
+    if one:
+        eps = torch.tensor([0.0, 0.0, 3.0, 0.0], device="cuda")
+    _check(K.moe_few(x, w_in, w_out, K=k, eps=eps), _reference(x, w_in, w_out, k, eps))
+
+
 def test_ties_go_to_the_lower_index(K):
     """Logits that the ReLU made 0 are equal: their experts are chosen in index order, with equal scores."""
     x, w_in, w_out, _ = _inputs(3, 128, 64, 8, 1)
