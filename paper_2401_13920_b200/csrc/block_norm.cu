@@ -10,8 +10,9 @@
 // group of kWarp-multiple threads that keep it in registers between its two sums, so every element is read and written
 // once.  The two sums of a row are two round trips through the group, during which a kernel that loads its rows itself
 // asks memory for nothing (65536 x 5120 in bf16: 699 us forward, 58 % of the copy bandwidth); so each group has a ring
-// of rows in shared memory that bulk copies fill D rows ahead, one thread asking for the row D on as soon as the first
-// sum's barrier shows that the group has taken a row out of its place.
+// of rows in shared memory that bulk copies fill D rows ahead, a thread asking for an array of the row D on as soon as a
+// sum's barrier shows that the group has taken a row out of its place (forward 418-435 us, 93-97 % of the copy bandwidth;
+// with checkpoints at 65536 x 2560 478 -> 278-285 us, 89-91 %).
 // Sums are fp32 in a fixed order; outputs are rounded once.
 // With checkpoints the forward also leaves u and x in E4M3: a normalised row has mean square <= 1 and so no element
 // above sqrt(H), which the format's 448 covers for every H the library takes here; r and q carry the scale.
@@ -737,7 +738,7 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
     }
 }
 
-// ---- ring kernels: rows of whole 16-byte pieces, two units a thread ----
+// ---- ring kernels: two units a thread ----
 constexpr int kRingThreads = 640;   // of a CTA, which has an SM to itself: 102 registers a thread
 
 // FULL: every thread has two units.  CKPT: checkpoints are left.  ODD: see above.
@@ -850,24 +851,28 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
     ring.leave();
 }
 
-constexpr int kGradThreads = 384;
 // Gradient.  Written with the raw rows x', u' (x = xs x', u = us u'; codes: xs = us = 1):
 //   D = dh' + q dn w_pre - cx x',  cx = q xs^2 sum(dn w_pre x') / H;    dw_post += (R us) D u',  dw_pre += xs dn x'
 //   e = D w_post,  k = us sum(e u'),  dv = R r e - cu u',  cu = R r us k / H
 // A row's second sum (k) is taken together with the next row's first ones, so that a row costs one meeting of its group.
-// Everything but dv is done before it, so that only e and u' are held over it, and the weights lie in shared memory.  That
-// is for the registers: what spills comes back through an L1 that the rings leave little of,
-// behind the rings' copies (two units a thread with spills: 1380 us at 65536 x 5120 in bf16).
-// NV: units of a thread, one up to rows of 5120 (640 threads), else two (512 threads).  FULL: every thread has them all.
-// ALL: both upstream gradients, the branch, dh and dy are there.  ODD: see above (also rows of
-// codes that are no whole 16-byte pieces).
-template <typename X, bool CK, int NV, bool WREG, bool FULL, bool ALL, bool ODD>
+// Everything but dv is done before it, so that only e and u' are held over it.
+// Bound by the instructions of a row and, at one group a CTA, by the length of the chain through its meeting (39 % of the
+// issue slots at 65536 x 5120).  Hence two units a thread (554 instructions a warp and row against 2 x 404 with one), the
+// weights' columns in registers (WREG; out of shared memory 887 us against 767), and each array of a row asked for by a
+// thread of another warp (by four lanes of one warp 789 us against 737).  Not taken: an mbarrier that warps pass later
+// than they arrive at it, with the work that needs no sum in between (860 us); widened rows kept over the meeting (1249
+// us: what spills comes back through an L1 that the rings leave little of).
+// Reached at 65536 x 5120 in bf16: 744-762 us (5.2-5.3 TB/s, 80-82 % of the copy bandwidth), from checkpoints 651-662.
+// FULL: every thread has two units.  ALL: both upstream gradients, the branch, dh and dy are there.  ODD: see above (also
+// rows of codes that are no whole 16-byte pieces).
+constexpr int kGradThreads = 384;   // 168 registers a thread; the weights of rows beyond 16 x 384 lie in shared memory, 512 threads
+template <typename X, bool CK, bool WREG, bool FULL, bool ALL, bool ODD>
 __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_ring_kernel(const NormGradArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
     pdl_wait();
     pdl_trigger();
-    constexpr int UB = 8 * sizeof(X), AB = CK ? 8 : UB;   // bytes of a unit of the rows and of the activations
+    constexpr int NV = 2, UB = 8 * sizeof(X), AB = CK ? 8 : UB;   // units of a thread; bytes of one of the rows and of the activations
     const int tpr = a.tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
     GroupSum total(red_all + group * kRedFloats, group, tpr);
     const float inv_h = 1.0f / (float)a.H;
@@ -1201,6 +1206,9 @@ int forward(NormArgs& a, cudaStream_t st) {
         if (!allow_smem(kernel, smem)) return (int)LOCMOE_ERR_CUDA;
         return launch_pdl(kernel, dim3((unsigned)grid), dim3(threads), smem, st, a);
     };
+    // The ring wherever a row has at most two units a thread (65536 x 5120 in bf16: 418 us against 699 by the kernel that
+    // loads its rows itself; gradient of 3001 x 777, rows that begin anywhere: 22 against 33); longer rows, and arrays that
+    // bulk copies cannot take, go through that kernel.
     if (based && a.H <= 16 * kRingThreads) {
         const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X);
         const RowPlan p = plan_rows(eights, 2, kRingThreads, a.T);
@@ -1239,9 +1247,10 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
     };
     int rc = LOCMOE_OK;
     bool done = false;
+    // as in the forward pass: the ring where a row has at most two units a thread
     if (based && a.H <= 8 * 1024) {
         const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X), act = CK ? a.H : row;
-        const bool wreg = eights <= 2 * kGradThreads;
+        const bool wreg = eights <= 2 * kGradThreads;   // (one unit a thread with 512 threads: 612 us against 640 at 65536 x 4096, but 531 / 375 at 2560)
         const RowPlan p = plan_rows(eights, 2, wreg ? kGradThreads : 512, a.T);
         const bool whole = wide && act % 16 == 0;   // all rows are whole 16-byte pieces
         const int stage = whole ? 2 * (row + act) : 2 * (round16(row + 15) + round16(act + 15)), extra = wreg ? 0 : 8 * a.H;
@@ -1249,12 +1258,12 @@ int backward(NormGradArgs& a, float* dw_post, float* dw_pre, cudaStream_t st) {
         if (a.depth) {
             const size_t smem = ring_bytes(p.groups, a.depth, stage) + extra;
             const bool all = a.dh_out && a.dn && (CK ? (const void*)a.u8 : a.y) && a.dh && a.dy;
-            if (!whole) rc = wreg ? launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, false, true>, p, 1, smem)
-                                  : launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false, true>, p, 1, smem);
-            else if (!wreg) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, false, false, false, false>, p, 1, smem);
-            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, false, false>, p, 1, smem);
-            else if (eights == 2 * p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, true, true, false>, p, 1, smem);
-            else rc = launch(block_norm_grad_ring_kernel<X, CK, 2, true, false, true, false>, p, 1, smem);
+            if (!whole) rc = wreg ? launch(block_norm_grad_ring_kernel<X, CK, true, false, false, true>, p, 1, smem)
+                                  : launch(block_norm_grad_ring_kernel<X, CK, false, false, false, true>, p, 1, smem);
+            else if (!wreg) rc = launch(block_norm_grad_ring_kernel<X, CK, false, false, false, false>, p, 1, smem);
+            else if (!all) rc = launch(block_norm_grad_ring_kernel<X, CK, true, false, false, false>, p, 1, smem);
+            else if (eights == 2 * p.tpr) rc = launch(block_norm_grad_ring_kernel<X, CK, true, true, true, false>, p, 1, smem);
+            else rc = launch(block_norm_grad_ring_kernel<X, CK, true, false, true, false>, p, 1, smem);
             done = true;
         }
     }
