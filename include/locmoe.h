@@ -505,7 +505,7 @@ int locmoe_moe_layer(const locmoe_shape_t *shape, const void *x, const int32_t *
 
 /*
  * A whole MoE layer for a few tokens, as decoding meets it: gate, the K best experts, their feed-forward networks
- * and the gate-weighted sum, in two launches, with no capacity, no dropped token and no dispatch buffer.
+ * and the gate-weighted sum, in two or three launches, with no capacity, no dropped token and no dispatch buffer.
  *   G_i = ReLU(mean_i x_t + eps_i) as in locmoe_gate (eps == NULL: 0),  p = softmax(G),
  *   choice c of a token = the c-th largest G_i, a tie going to the lower index,
  *   out[t] = sum over c < K of p_c * W_out[e_c] . GeLU(W_in[e_c] . x_t)        (GeLU as in locmoe_expert_ffn)

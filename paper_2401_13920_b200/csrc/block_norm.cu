@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a) {
             load_weight<VEC>(a.w_post, un * VEC, w);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                vv[j] *= r;
+                vv[j] *= s < 0 ? 0.0f : r;   // nothing stays 0 where eps is 0 and r infinite
                 hv[j] = fmaf(gr * w[j], vv[j], a.res_scale * hv[j]);
             }
         };
@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(512) block_norm_grad_kernel(const NormGradArgs
             q = rsqrtf(fmaf(sum[0], inv_h, a.eps));
             r = rsqrtf(fmaf(sum[1], inv_h, a.eps));
         }
-        const float xs = CK ? 1.0f : q, us = CK ? 1.0f : r;   // what turns x, u into normalised values
+        const float xs = CK ? 1.0f : q, us = CK ? 1.0f : s < 0 ? 0.0f : r;   // what turns x, u into normalised values (no row: r may be infinite)
         const float c1 = sum[2] * xs * inv_h;
         // D of one unit; x, u become normalised
         auto upstream = [&](int un, float* xv, float* uv, const float* nv, float* dv) {
@@ -818,7 +818,7 @@ __global__ void __launch_bounds__(kRingThreads) block_norm_ring_kernel(const Nor
         ring.next();
         const float r = rsqrtf(fmaf(sum, inv_h, a.eps));
         if (CKPT && a.r_post && lane == 0) a.r_post[t] = r;
-        const float2 g2 = both(f.gate), r2 = both(r), a2 = both(a.res_scale);
+        const float2 g2 = both(f.gate), r2 = both(f.s < 0 ? 0.0f : r), a2 = both(a.res_scale);   // nothing stays 0 where eps is 0 and r infinite
         acc = both(0.0f);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(WREG ? kGradThreads : 512) block_norm_grad_rin
         total.four(k, xx, uu, dot);
         __syncwarp();
         if (asks && t < last_ask) ask(t + ahead, table[(n + a.depth) & (kTable - 1)].s, was);   // the group is done with the row
-        k *= us;
+        k = here.s < 0 ? 0.0f : k * us;
         if (lane == 0 && a.dgate) a.dgate[t] = k;
         if (has_dy && here.s >= 0) {
             const float rg = r * here.gate;

@@ -218,6 +218,26 @@ def test_infinities_and_nan_stay_in_their_rows(K, H):
         assert torch.equal(ga[i][rest], gb[i][rest])
 
 
+@pytest.mark.parametrize("H,ck", [(64, False), (64, True), (777, False), (777, True), (10248, False), (10248, True), (10241, False)])
+def test_no_eps_keeps_dropped_tokens(K, H, ck):
+    """With eps = 0 a token without a row has an infinite reciprocal norm of nothing, which must stay nothing: the bits of
+    an eps that no row's mean square notices."""
+    s = _case(40, H, torch.float32, True, 5)
+    s["y"] += 0.01
+    s["h"] += 0.01
+    got = []
+    for eps in (0.0, 1e-30):
+        h_out, n, c = K.block_norm(s["h"], s["y"], s["slot"], s["gate_w"], s["w_post"], s["w_pre"], 0.5, eps, ck)
+        acts = dict(checkpoint=c) if ck else dict(h_out=h_out, y=s["y"])
+        grads = K.block_norm_grad(s["dh_out"], s["dn"], slot=s["slot"], inv=s["inv"], gate_w=s["gate_w"], w_post=s["w_post"],
+                                  w_pre=s["w_pre"], res_scale=0.5, eps=eps, **acts)
+        got.append([h_out, n, *grads] + ([c.u8.view(torch.uint8), c.x8.view(torch.uint8)] if ck else []))
+    assert (s["slot"] < 0).any()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+        assert not a.float().isnan().any()
+
+
 def test_unaligned_rows_in_place_and_repeatable(K):
     """Arrays at odd element offsets take the element-wise kernel; h_out may be h, dh may be dh_out; the bits repeat."""
     from paper_2401_13920_b200 import binding as B
