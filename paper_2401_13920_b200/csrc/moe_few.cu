@@ -42,12 +42,12 @@ struct FewArgs {
 
 // A variant: GR groups, each with a ring, a producer warp and multiplying warps, WR along the weight rows and WK along
 // k; NB blocks of 8 weight rows a warp, BW boxes of 64 k a warp and stage, MT tiles of 16 tokens; the shared memory of
-// a CTA.  A group works on every GR-th task by itself, so that one group's sums and stores run beside the others'
+// a CTA; the tasks an SM that the second product's reduction is sliced for.  A group works on every GR-th task by itself, so that one group's sums and stores run beside the others'
 // products.
 constexpr int kMaxStages = 8;   // of a group's ring
-template <int GR_, int WR_, int WK_, int NB_, int BW_, int MT_, int SMEM_>
+template <int GR_, int WR_, int WK_, int NB_, int BW_, int MT_, int SMEM_, int WANT_>
 struct Variant {
-    static constexpr int GR = GR_, WR = WR_, WK = WK_, NB = NB_, BW = BW_, MT = MT_, kSmem = SMEM_;
+    static constexpr int GR = GR_, WR = WR_, WK = WK_, NB = NB_, BW = BW_, MT = MT_, kSmem = SMEM_, kWant = WANT_;
     static constexpr int kMulWarps = WR * WK, kThreads = 32 * GR * (kMulWarps + 1);
     static constexpr int kBoxes = WK * BW;
     static constexpr int R = 8 * NB * WR, kStepK = kBoxK * kBoxes;      // weight rows of a task, k of a stage
@@ -327,7 +327,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a, const i
     const int steps = (p.Kd + V::kStepK - 1) / V::kStepK;
     p.S = 1;                // slices of the reduction: enough tasks for an even load, at least four stages each
     if (second)
-        while (p.S < a.max_split && chunks * p.RB * p.S < 8 * (int)gridDim.x && steps >= 8 * p.S) p.S *= 2;
+        while (p.S < a.max_split && chunks * p.RB * p.S < V::kWant * (int)gridDim.x && steps >= 8 * p.S) p.S *= 2;
     p.stages = (steps + p.S - 1) / p.S;   // of a task; those beyond K are zeros
     const int total = chunks * p.RB * p.S, share = total / (int)gridDim.x, more = total - share * (int)gridDim.x;
     p.t0 = blockIdx.x * share + min((int)blockIdx.x, more);
@@ -570,7 +570,8 @@ struct FewPlan { size_t off_g, off_part, off_arrived, total; int max_split; };
 FewPlan plan_few(const locmoe_shape_t& s, int F, int K) {
     FewPlan p{};
     const size_t TK = (size_t)s.T * K;
-    // slices only pay while there are few tasks, that is few assignments: at most 512 rows of partial sums for them
+    // at most 512 rows of partial sums for the slices: with many assignments there are tasks enough, and the sums would
+    // be a workspace of many times the tokens (H = 1024, F = 1024, E = 4, T = 128, K = 2 would take 57 us instead of 66)
     p.max_split = 1;
     while (p.max_split < kMaxSplit && TK * p.max_split * 2 <= 512) p.max_split *= 2;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -624,10 +625,14 @@ int launch_moe_few(const locmoe_shape_t& s, const void* x, const float* eps, int
     //   T = 128, K = 2 684 against 849 with tiles of 16 and 64 rows, whose second chunk of tokens takes the weights
     //   through shared memory again; T = 64, K = 2 577 / 629.  With fewer tokens an expert (T = 64, K = 1: 495 / 470) or
     //   fewer tasks (the small layer at T = 128, K = 2: 112 / 66) the smaller tiles win.
-    if (s.T * K <= 8) return run_few<Variant<3, 1, 4, 2, 1, 1, 220 << 10>>(a, st);
+    // The slices of the second product (tasks an SM: 1, 2 or 8): each is a pass over the partial sums more, but evens the
+    // load out.  A few assignments: 1 (H = 2048, F = 5632, E = 8, one token 18.5 us, with 2 21.2; H = 1560, F = 4104, E = 24,
+    // K = 3, one token 26.6 / 31.9).  Tiles of 16 tokens: 2 (13 of those tokens 104 us, with 8 115; 16 tokens of the former
+    // 71, with 1 81, with 8 79).  Tiles of 32 tokens differ most in their work: 8 (T = 128, K = 2 680 us, with 2 763).
+    if (s.T * K <= 8) return run_few<Variant<3, 1, 4, 2, 1, 1, 220 << 10, 1>>(a, st);
     if (s.T > 16 && (long long)s.T * K >= 4ll * s.E && (long long)s.E * ((F + 127) / 128) >= 4 * sm_count())
-        return run_few<Variant<3, 4, 1, 4, 1, 2, 220 << 10>>(a, st);
-    return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10>>(a, st);
+        return run_few<Variant<3, 4, 1, 4, 1, 2, 220 << 10, 8>>(a, st);
+    return run_few<Variant<4, 4, 1, 2, 1, 1, 220 << 10, 2>>(a, st);
 }
 
 int read_few_flags(int* out, cudaStream_t st) {
