@@ -743,11 +743,11 @@ constexpr int kRingThreads = 640;   // of a CTA, which has an SM to itself: 102 
 
 // ODD rows need more registers: fp32 rows without checkpoints do better with fewer threads that have them (32768 x 2561 211 us
 // against 263, x 4097 389 / 416), bf16 rows and checkpoints with more groups (2561 in bf16 248 / 233, 4097 490 / 358).
-template <typename X>
-__host__ __device__ constexpr int ring_threads(bool ckpt, bool odd) { return odd && !ckpt && sizeof(X) == 4 ? 512 : kRingThreads; }
-// FULL: every thread has two units.  CKPT: checkpoints are left.  ODD: see above.
-template <typename X, bool FULL, bool CKPT, bool ODD>
-__global__ void __launch_bounds__(ring_threads<X>(CKPT, ODD)) block_norm_ring_kernel(const NormArgs a) {
+constexpr int kOddThreads = 512;
+
+// FULL: every thread has two units.  CKPT: checkpoints are left.  ODD: see above.  TH: threads at most.
+template <typename X, bool FULL, bool CKPT, bool ODD, int TH = kRingThreads>
+__global__ void __launch_bounds__(TH) block_norm_ring_kernel(const NormArgs a) {
     __shared__ float red_all[kMaxGroups * kRedFloats];
     extern __shared__ __align__(128) unsigned char ring_mem[];
     pdl_wait();
@@ -1214,16 +1214,19 @@ int forward(NormArgs& a, cudaStream_t st) {
     // loads its rows itself; gradient of 3001 x 777, rows that begin anywhere: 22 against 33); longer rows, and arrays that
     // bulk copies cannot take, go through that kernel.
     const bool ck = a.u8 || a.x8;
-    const int most = ring_threads<X>(ck, !wide);
-    if (based && a.H <= 16 * most) {
+    if (based && a.H <= 16 * kRingThreads) {
         const int eights = (a.H + 7) / 8, row = a.H * (int)sizeof(X);
-        const RowPlan p = plan_rows(eights, 2, most, a.T);
+        const bool fewer = !wide && !ck && sizeof(X) == 4 && eights <= 2 * kOddThreads;
+        const RowPlan p = plan_rows(eights, 2, fewer ? kOddThreads : kRingThreads, a.T);
         const int stage = 2 * (wide ? row : round16(row + 15));
         a.depth = ring_depth(p.groups, stage, 0);
         const size_t smem = ring_bytes(p.groups, a.depth, stage);
         if (a.depth) {
             const bool full = eights == 2 * p.tpr;
-            if (!wide) return ck ? launch(block_norm_ring_kernel<X, false, true, true>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false, true>, p, 1, smem);
+            if (!wide && ck) return launch(block_norm_ring_kernel<X, false, true, true>, p, 1, smem);
+            if constexpr (sizeof(X) == 4)
+                if (fewer) return launch(block_norm_ring_kernel<X, false, false, true, kOddThreads>, p, 1, smem);
+            if (!wide) return launch(block_norm_ring_kernel<X, false, false, true>, p, 1, smem);
             if (ck) return full ? launch(block_norm_ring_kernel<X, true, true, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, true, false>, p, 1, smem);
             return full ? launch(block_norm_ring_kernel<X, true, false, false>, p, 1, smem) : launch(block_norm_ring_kernel<X, false, false, false>, p, 1, smem);
         }
