@@ -146,6 +146,13 @@ def test_gradient(K, T, H, dt, slots, ck):
         assert ((g.double() - w).abs() <= 4e-6 * z * max(1.0, (T / 8) ** 0.5)).all()
 
 
+@pytest.mark.parametrize("ck", [False, True])
+@pytest.mark.parametrize("T,H", [(5, 8192), (40, 8191), (200, 6664), (7, 6657), (3, 8200), (3, 8193)])
+def test_gradient_of_long_fp32_rows(K, T, H, ck):
+    """Rows of which two do not fit into shared memory."""
+    test_gradient(K, T, H, torch.float32, True, ck)
+
+
 def test_gradient_against_differences(K):
     """Central differences of the kernel's own fp32 forward pass, in random directions of each argument."""
     T, H = 24, 96
