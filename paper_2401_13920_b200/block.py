@@ -2,7 +2,9 @@
 activations kept in 8 bits, and the whole expert layer for a few tokens.
 
 The functions here allocate their outputs (and the workspace, from torch's allocator on the current stream) and call the
-entry points of ``binding``; all arithmetic runs in the CUDA library.  ``BlockNorm`` is the differentiable form.
+entry points of ``binding``; all arithmetic runs in the CUDA library.  With ``stream`` (a torch stream or a raw handle) the
+whole call, its allocations among them, is made under that stream, as by ``with torch.cuda.stream(stream)``: the inputs have
+to be ready there, and the outputs belong to it.  ``BlockNorm`` is the differentiable form.
 """
 from __future__ import annotations
 
@@ -30,6 +32,15 @@ def _here(t: torch.Tensor, name: str) -> None:
     """Outputs, workspace and launch belong to the current device: so must the inputs."""
     if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError("%s: on %s, which is not the current CUDA device" % (name, t.device))
+
+
+def _under(stream):
+    """Context of a call on `stream`.  Its memory has to come from that stream's pool: the workspace goes back to its pool
+    when the call returns, and only work of the same stream waits for the kernels that still use it."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        stream = torch.cuda.default_stream() if handle in (0, 1) else torch.cuda.ExternalStream(handle)   # 1: the legacy default
+    return torch.cuda.stream(stream)
 
 
 class Checkpoint(NamedTuple):
@@ -73,6 +84,9 @@ def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
     """The whole MoE layer for a few tokens: x [T][H], w_in [E][F][H], w_out [E][H][F], all bf16, T <= 128.
 
     Returns ``(out, idx, w)``: out [T][H], the K chosen experts and their scores, [K][T] each."""
+    if stream is not None:
+        with _under(stream):
+            return moe_few(x, w_in, w_out, K, eps, weighted)
     if x.dim() != 2 or w_in.dim() != 3 or w_out.dim() != 3:
         raise ValueError("expected x [T][H], w_in [E][F][H], w_out [E][H][F]")
     (T, H), (E, F, _) = x.shape, w_in.shape
@@ -84,7 +98,7 @@ def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
         return out, idx, w
     shape, n = _few_plan(T, H, E, K, F, x.dtype)
     ws = _flat(n, torch.uint8)
-    B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted, stream)
+    B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted)
     return out, idx, w
 
 
@@ -94,6 +108,9 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
 
     Returns ``(h_out, n, ckpt)``; ``h_out`` / ``n`` are None when not wanted, ``ckpt`` a ``Checkpoint`` or None.  Without
     ``y`` the block has no branch (the norm before the first block; ``want_h`` = False leaves out the copy of h)."""
+    if stream is not None:
+        with _under(stream):
+            return block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint, want_h, want_n)
     shape, rows = _row_shape(h, y, slot)
     T, H = shape.T, shape.H
     if y is not None and y.shape[-1] != H:
@@ -106,7 +123,7 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
     if checkpoint and want_n:
         x8, r_pre = _rows(T, H, torch.float8_e4m3fn), _flat(T, _F32)
     if T > 0:
-        B.locmoe_block_norm(shape, rows, h, y, slot, gate_w, w_post, w_pre, res_scale, eps, h_out, n, u8, x8, r_post, r_pre, stream)
+        B.locmoe_block_norm(shape, rows, h, y, slot, gate_w, w_post, w_pre, res_scale, eps, h_out, n, u8, x8, r_post, r_pre)
     return h_out, n, Checkpoint(u8, x8, r_post, r_pre) if checkpoint else None
 
 
@@ -117,6 +134,10 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
 
     The activations are ``h_out`` and ``y`` or, in their place, ``checkpoint``.  Returns ``(dh, dy, dgate, dw_post, dw_pre)``,
     each None when not wanted or not there.  With slots, ``dy`` has ``inv``'s rows, those without a token zero."""
+    if stream is not None:
+        with _under(stream):
+            return block_norm_grad(dh_out, dn, h_out, y, checkpoint, slot, inv, gate_w, w_post, w_pre, res_scale, eps, want_dh, want_dy,
+                                   want_dgate, want_dw)
     like = dn if dn is not None else dh_out
     ck = checkpoint
     branch = (ck.u8 if ck is not None else y) is not None
@@ -141,7 +162,7 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
         if ck is not None else dict(y=y, h_out=h_out if dn is not None else None)
     B.locmoe_block_norm_grad(shape, rows, dh_out, dn, slot=slot if branch else None, inv=inv if branch and slot is not None else None,
                              gate_w=gate_w, w_post=w_post, w_pre=w_pre, res_scale=res_scale, eps=eps, dh=dh, dy=dy, dgate=dgate,
-                             dw_post=dw_post, dw_pre=dw_pre, ws=ws, stream=stream, **acts)
+                             dw_post=dw_post, dw_pre=dw_pre, ws=ws, **acts)
     return dh, dy, dgate, dw_post, dw_pre
 
 

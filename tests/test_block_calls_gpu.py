@@ -1,0 +1,82 @@
+"""The calls around the block's kernels on the GPU: streams, memory, and what autograd makes of them."""
+import pytest
+import torch
+
+from tests.test_block_norm_gpu import EPS, _case
+from tests.test_moe_few_gpu import _inputs
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def K():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a CUDA device")
+    from paper_2401_13920_b200 import block
+    return block
+
+
+def _flat(out):
+    """The tensors of a result, checkpoints among them."""
+    parts = [p for o in out for p in (o if isinstance(o, tuple) else (o,))]
+    return [p.view(torch.uint8) if p.dtype is torch.float8_e4m3fn else p for p in parts if p is not None]
+
+
+def _calls(K):
+    x, w_in, w_out, eps = _inputs(12, 512, 1024, 8, 1, bias=True)
+    s = _case(300, 520, torch.bfloat16, True, 2)
+    kw = dict(slot=s["slot"], gate_w=s["gate_w"], w_post=s["w_post"], w_pre=s["w_pre"], res_scale=0.9, eps=EPS)
+    h_out, _, _ = K.block_norm(s["h"], s["y"], **kw)
+    return [lambda **a: K.moe_few(x, w_in, w_out, K=2, eps=eps, **a),
+            lambda **a: K.block_norm(s["h"], s["y"], checkpoint=True, **kw, **a),
+            lambda **a: K.block_norm_grad(s["dh_out"], s["dn"], h_out, s["y"], inv=s["inv"], **kw, **a)]
+
+
+@pytest.mark.parametrize("form", ["stream", "handle", "default", "zero"])
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_memory_belongs_to_the_given_stream(K, which, form):
+    """A call whose `stream` lags behind: what the current stream allocates and fills after the call must be none of the
+    memory that the call's kernels have still to use, its private workspace included."""
+    call = _calls(K)[which]
+    want = _flat(call())
+    torch.cuda.synchronize()
+    side, given = torch.cuda.Stream(), None
+    if form == "stream":
+        lag, here, given = side, torch.cuda.current_stream(), side
+    elif form == "handle":
+        lag, here, given = side, torch.cuda.current_stream(), side.cuda_stream
+    else:   # the call goes to the default stream from inside another one
+        lag, here, given = torch.cuda.default_stream(), side, torch.cuda.default_stream() if form == "default" else 0
+    with torch.cuda.stream(lag):
+        torch.cuda._sleep(20_000_000)          # about 10 ms: everything below is queued long before the kernels run
+    with torch.cuda.stream(here):
+        got = call(stream=given)
+        assert torch.cuda.current_stream() == here
+        held = []
+        for n in (1 << 10, 1 << 14, 1 << 17, 1 << 19, 1 << 21):      # bytes: sizes of the workspaces and the outputs, each pool of the allocator
+            for _ in range(12):
+                held.append(torch.full((n,), 0xff, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for a, b in zip(_flat(got), want):
+        assert torch.equal(a, b)
+    assert all(bool((t == 0xff).all()) for t in held)
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_outputs_on_another_stream_wait_for_no_one_elses_readers(K, which):
+    """Memory that the current stream has just released, with a reader of it still queued there, is not given to a call on
+    another stream."""
+    call = _calls(K)[which]
+    want = _flat(call())
+    shapes = [(t.shape, t.dtype) for t in want]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    old = [torch.zeros(*s, dtype=d, device="cuda") for s, d in shapes]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    copies = [t.clone() for t in old]          # reads that wait behind the sleep
+    del old
+    got = _flat(call(stream=side))
+    torch.cuda.synchronize()
+    assert not any(bool(c.any()) for c in copies)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
