@@ -499,36 +499,44 @@ def locmoe_moe_few_bytes(shape: Shape, K, F) -> int:
     return out.value
 
 
-def _arg(t, dtype, numel, name):
-    """Device address of an argument (None for an absent one) after all checks; a plain int, which ctypes takes as it is."""
+def _device():
+    """Index of the device that the calls below launch on; None before CUDA is in use (no tensor is on a device then)."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else None
+
+
+def _arg(t, dtype, numel, name, dev):
+    """Device address of an argument (None for an absent one) after all checks, that it is memory of device `dev` among
+    them; a plain int, which ctypes takes as it is."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() < numel:
         _want(t, dtype, numel, name)
-    if not (t.is_cuda and t.is_contiguous()):
+    if t.get_device() != dev or not t.is_contiguous():
+        if t.is_cuda and t.get_device() != dev:
+            raise ValueError("%s: on %s, which is not the current CUDA device" % (name, t.device))
         _ptr(t)
     return t.data_ptr()
 
 
 def locmoe_moe_few(shape: Shape, x, K, F, w_in, w_out, idx_k, w_k, out, ws, eps=None, unweighted=False, stream=None) -> int:
     """The whole layer for at most FEW_MAX_TOKENS tokens."""
-    bf, f32, T, TH, n = torch.bfloat16, torch.float32, shape.T, shape.T * shape.H, shape.E * F * shape.H
+    bf, f32, T, TH, n, dev = torch.bfloat16, torch.float32, shape.T, shape.T * shape.H, shape.E * F * shape.H, _device()
     return _check("locmoe_moe_few", _lib.locmoe_moe_few(
-        C.byref(shape), _arg(x, bf, TH, "x"), _arg(eps, f32, shape.E, "eps"), K, F, _arg(w_in, bf, n, "w_in"), _arg(w_out, bf, n, "w_out"),
-        FEW_UNWEIGHTED if unweighted else 0, _arg(idx_k, torch.int32, K * T, "idx_k"), _arg(w_k, f32, K * T, "w_k"), _arg(out, bf, TH, "out"),
-        _arg(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)))
+        C.byref(shape), _arg(x, bf, TH, "x", dev), _arg(eps, f32, shape.E, "eps", dev), K, F, _arg(w_in, bf, n, "w_in", dev), _arg(w_out, bf, n, "w_out", dev),
+        FEW_UNWEIGHTED if unweighted else 0, _arg(idx_k, torch.int32, K * T, "idx_k", dev), _arg(w_k, f32, K * T, "w_k", dev), _arg(out, bf, TH, "out", dev),
+        _arg(ws, torch.uint8, 0, "ws", dev), ws.numel(), _stream(stream)))
 
 
 def locmoe_block_norm(shape: Shape, C_alloc, h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6,
                       h_out=None, n_out=None, u8=None, x8=None, r_post=None, r_pre=None, stream=None) -> int:
     """Post-norm, gate, residual and the next pre-norm in one pass; any array that is not wanted is None."""
-    T, H = shape.T, shape.H
+    T, H, dev = shape.T, shape.H, _device()
     dt, f32, e4m3 = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.float8_e4m3fn
     rows = T if slot is None else shape.D * shape.E * C_alloc
-    b = BlockNorm(_arg(h, dt, T * H, "h"), _arg(y, dt, rows * H, "y"), _arg(slot, torch.int32, T, "slot"), _arg(gate_w, f32, T, "gate_w"),
-                  _arg(w_post, f32, H, "w_post"), _arg(w_pre, f32, H, "w_pre"), res_scale, eps, _arg(h_out, dt, T * H, "h_out"),
-                  _arg(n_out, dt, T * H, "n_out"), _arg(u8, e4m3, T * H, "u8"), _arg(x8, e4m3, T * H, "x8"), _arg(r_post, f32, T, "r_post"),
-                  _arg(r_pre, f32, T, "r_pre"))
+    b = BlockNorm(_arg(h, dt, T * H, "h", dev), _arg(y, dt, rows * H, "y", dev), _arg(slot, torch.int32, T, "slot", dev), _arg(gate_w, f32, T, "gate_w", dev),
+                  _arg(w_post, f32, H, "w_post", dev), _arg(w_pre, f32, H, "w_pre", dev), res_scale, eps, _arg(h_out, dt, T * H, "h_out", dev),
+                  _arg(n_out, dt, T * H, "n_out", dev), _arg(u8, e4m3, T * H, "u8", dev), _arg(x8, e4m3, T * H, "x8", dev), _arg(r_post, f32, T, "r_post", dev),
+                  _arg(r_pre, f32, T, "r_pre", dev))
     return _check("locmoe_block_norm", _lib.locmoe_block_norm(C.byref(shape), C_alloc, C.byref(b), _stream(stream)))
 
 
@@ -542,17 +550,17 @@ def locmoe_block_norm_grad(shape: Shape, C_alloc, dh_out=None, dn=None, h_out=No
                            slot=None, inv=None, gate_w=None, w_post=None, w_pre=None, res_scale=1.0, eps=1e-6, dh=None, dy=None,
                            dgate=None, dw_post=None, dw_pre=None, ws=None, stream=None) -> int:
     """Gradient of locmoe_block_norm, from h_out and y or from the 8-bit checkpoints."""
-    T, H = shape.T, shape.H
+    T, H, dev = shape.T, shape.H, _device()
     dt, f32, i32, e4m3 = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
     TH, rows = T * H, T if slot is None else shape.D * shape.E * C_alloc
     b = BlockNormGrad(
-        _arg(dh_out, dt, TH, "dh_out"), _arg(dn, dt, TH, "dn"), _arg(h_out, dt, TH, "h_out"), _arg(y, dt, rows * H, "y"),
-        _arg(u8, e4m3, TH, "u8"), _arg(x8, e4m3, TH, "x8"), _arg(r_post, f32, T, "r_post"), _arg(r_pre, f32, T, "r_pre"),
-        _arg(slot, i32, T, "slot"), _arg(inv, i32, rows, "inv"), _arg(gate_w, f32, T, "gate_w"), _arg(w_post, f32, H, "w_post"),
-        _arg(w_pre, f32, H, "w_pre"), res_scale, eps, _arg(dh, dt, TH, "dh"), _arg(dy, dt, rows * H, "dy"), _arg(dgate, f32, T, "dgate"),
-        _arg(dw_post, f32, H, "dw_post"), _arg(dw_pre, f32, H, "dw_pre"))
+        _arg(dh_out, dt, TH, "dh_out", dev), _arg(dn, dt, TH, "dn", dev), _arg(h_out, dt, TH, "h_out", dev), _arg(y, dt, rows * H, "y", dev),
+        _arg(u8, e4m3, TH, "u8", dev), _arg(x8, e4m3, TH, "x8", dev), _arg(r_post, f32, T, "r_post", dev), _arg(r_pre, f32, T, "r_pre", dev),
+        _arg(slot, i32, T, "slot", dev), _arg(inv, i32, rows, "inv", dev), _arg(gate_w, f32, T, "gate_w", dev), _arg(w_post, f32, H, "w_post", dev),
+        _arg(w_pre, f32, H, "w_pre", dev), res_scale, eps, _arg(dh, dt, TH, "dh", dev), _arg(dy, dt, rows * H, "dy", dev), _arg(dgate, f32, T, "dgate", dev),
+        _arg(dw_post, f32, H, "dw_post", dev), _arg(dw_pre, f32, H, "dw_pre", dev))
     return _check("locmoe_block_norm_grad", _lib.locmoe_block_norm_grad(
-        C.byref(shape), C_alloc, C.byref(b), _arg(ws, torch.uint8, 0, "ws"), 0 if ws is None else ws.numel(), _stream(stream)))
+        C.byref(shape), C_alloc, C.byref(b), _arg(ws, torch.uint8, 0, "ws", dev), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def conventional_capacity(T: int, D: int, E: int, capacity_factor: float) -> int:

@@ -1,0 +1,76 @@
+"""What the calls around the block's kernels refuse before anything is launched, and their ways around what a host may lack
+(no GPU needed: tensors are stand-ins, the library's entry points recorders)."""
+import pytest
+import torch
+
+BF, F32, I32, U8, E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
+
+
+class StandIn:
+    """A contiguous tensor as the checks see it, in the memory of device `index`."""
+    def __init__(self, numel, dtype, index=0):
+        self._n, self.dtype, self._i = numel, dtype, index
+        self.is_cuda, self.device = index >= 0, torch.device("cuda", index) if index >= 0 else torch.device("cpu")
+
+    numel = lambda self: self._n
+    get_device = lambda self: self._i
+    is_contiguous = lambda self: True
+    data_ptr = lambda self: 1 << 20
+
+
+@pytest.fixture
+def B(monkeypatch):
+    """The binding on a process whose current device is 0; entry points note that they were called and do nothing."""
+    from paper_2401_13920_b200 import binding
+
+    class Lib:
+        called = []
+        def __getattr__(self, name):
+            return lambda *a: self.called.append(name) or 0
+    lib = Lib()
+    lib.called = []
+    monkeypatch.setattr(binding, "_lib", lib)
+    monkeypatch.setattr(binding, "_device", lambda: 0)
+    monkeypatch.setattr(binding, "_stream", lambda s: None)
+    return binding
+
+
+T, H, F, E = 4, 64, 16, 8
+FEW = dict(x=(T * H, BF), w_in=(E * F * H, BF), w_out=(E * F * H, BF), idx_k=(2 * T, I32), w_k=(2 * T, F32), out=(T * H, BF),
+           ws=(1 << 20, U8), eps=(E, F32))
+NORM = dict(h=(T * H, BF), y=(T * H, BF), slot=(T, I32), gate_w=(T, F32), w_post=(H, F32), w_pre=(H, F32), h_out=(T * H, BF),
+            n_out=(T * H, BF), u8=(T * H, E4M3), x8=(T * H, E4M3), r_post=(T, F32), r_pre=(T, F32))
+GRAD = dict(dh_out=(T * H, BF), dn=(T * H, BF), h_out=(T * H, BF), y=(T * H, BF), u8=(T * H, E4M3), x8=(T * H, E4M3), r_post=(T, F32),
+            r_pre=(T, F32), slot=(T, I32), inv=(T, I32), gate_w=(T, F32), w_post=(H, F32), w_pre=(H, F32), dh=(T * H, BF),
+            dy=(T * H, BF), dgate=(T, F32), dw_post=(H, F32), dw_pre=(H, F32), ws=(1 << 20, U8))
+
+
+def _call(B, which, **over):
+    args = {k: StandIn(*v) for k, v in dict(few=FEW, norm=NORM, grad=GRAD)[which].items()}
+    args.update(over)
+    if which == "few":
+        return B.locmoe_moe_few(B.make_shape(T, H, E, 1, 1, B.BF16), K=2, F=F, **args)
+    shape = B.Shape(T, H, 1, 1, 1, B.BF16, 0)
+    return B.locmoe_block_norm(shape, T, **args) if which == "norm" else B.locmoe_block_norm_grad(shape, T, **args)
+
+
+@pytest.mark.parametrize("which,name", [(w, n) for w, d in (("few", FEW), ("norm", NORM), ("grad", GRAD)) for n in d])
+def test_every_tensor_has_to_be_on_the_current_device(B, which, name):
+    _call(B, which)
+    assert len(B._lib.called) == 1
+    spec = dict(few=FEW, norm=NORM, grad=GRAD)[which][name]
+    with pytest.raises(ValueError, match=name):
+        _call(B, which, **{name: StandIn(*spec, index=1)})
+    with pytest.raises(ValueError):
+        _call(B, which, **{name: StandIn(*spec, index=-1)})       # host memory
+    assert len(B._lib.called) == 1                                 # nothing was launched
+
+
+def test_no_tensor_is_on_a_device_before_cuda_is_in_use():
+    from paper_2401_13920_b200 import binding
+    if torch.cuda.is_initialized():
+        assert binding._device() == torch.cuda.current_device()
+    else:
+        assert binding._device() is None
+        with pytest.raises(ValueError):
+            binding._arg(torch.zeros(4), F32, 4, "x", binding._device())
