@@ -69,15 +69,19 @@ def _grad_bytes(T: int, H: int, dtype: torch.dtype, device: int) -> int:
     return B.locmoe_block_norm_grad_bytes(_shape(T, H, 1, dtype))
 
 
-def _row_shape(like: torch.Tensor, y, slot) -> tuple:
-    """Shape struct and row stride for [T][H] tensors whose block output has ``y``'s rows."""
+def _row_shape(like: torch.Tensor) -> B.Shape:
+    """Shape struct for [T][H] tensors like this one."""
     if like.dim() != 2:
         raise ValueError("expected a [T][H] tensor, got %s" % (tuple(like.shape),))
-    T, H = like.shape
-    rows = T if slot is None else y.shape[0]
-    shape = _shape(T, H, 1, like.dtype)
+    shape = _shape(like.shape[0], like.shape[1], 1, like.dtype)
     _here(like, "rows")
-    return shape, rows
+    return shape
+
+
+def _want_rows(t, rows: int, H: int, name: str) -> None:
+    """`t` (None: absent) is `rows` rows of H elements; how its other dimensions group them does not matter."""
+    if t is not None and (t.shape[-1:] != (H,) or t.numel() != rows * H):
+        raise ValueError("%s: expected %d rows of %d, got %s" % (name, rows, H, tuple(t.shape)))
 
 
 def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
@@ -106,15 +110,23 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
                want_h=True, want_n=True, stream=None):
     """h' = res_scale * h + gate_w * w_post * N(y[slot]),  n = w_pre * N(h').
 
+    ``h`` is [T][H]; ``y`` the T tokens' rows (any beyond them are not read) or, with ``slot``, all rows of the slot buffer,
+    also as [E][C][H] or [D][E][C][H].
     Returns ``(h_out, n, ckpt)``; ``h_out`` / ``n`` are None when not wanted, ``ckpt`` a ``Checkpoint`` or None.  Without
     ``y`` the block has no branch (the norm before the first block; ``want_h`` = False leaves out the copy of h)."""
     if stream is not None:
         with _under(stream):
             return block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint, want_h, want_n)
-    shape, rows = _row_shape(h, y, slot)
-    T, H = shape.T, shape.H
-    if y is not None and y.shape[-1] != H:
-        raise ValueError("y: rows of %d expected, got %d" % (H, y.shape[-1]))
+    if slot is not None and y is None:
+        raise ValueError("y: needed with slot")
+    shape = _row_shape(h)
+    T, H = h.shape
+    rows = T
+    if y is not None:
+        have = y.numel() // max(H, 1)
+        if slot is not None:
+            rows = have
+        _want_rows(y, have if slot is not None else max(have, T), H, "y")
     h_out = _rows(T, H, h.dtype) if want_h else None
     n = _rows(T, H, h.dtype) if want_n else None
     u8 = x8 = r_post = r_pre = None
@@ -133,18 +145,30 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
     """Gradient of ``block_norm`` from the gradients of h' and n (one may be None).
 
     The activations are ``h_out`` and ``y`` or, in their place, ``checkpoint``.  Returns ``(dh, dy, dgate, dw_post, dw_pre)``,
-    each None when not wanted or not there.  With slots, ``dy`` has ``inv``'s rows, those without a token zero."""
+    each None when not wanted or not there.  With slots, ``dy`` has ``inv``'s rows, those without a token zero.
+    All arrays of rows have exactly the rows that belong to them: T, or ``inv``'s for ``y`` with slots."""
     if stream is not None:
         with _under(stream):
             return block_norm_grad(dh_out, dn, h_out, y, checkpoint, slot, inv, gate_w, w_post, w_pre, res_scale, eps, want_dh, want_dy,
                                    want_dgate, want_dw)
     like = dn if dn is not None else dh_out
+    if like is None:
+        raise ValueError("dh_out, dn: one of them is needed")
     ck = checkpoint
     branch = (ck.u8 if ck is not None else y) is not None
     if slot is not None and inv is None:
         raise ValueError("inv: needed with slot (it says how many rows y has and which of them are empty)")
-    shape, rows = _row_shape(like, inv, slot if branch else None)
-    T, H = shape.T, shape.H
+    shape = _row_shape(like)
+    T, H = like.shape
+    rows = inv.numel() if branch and slot is not None else T
+    _want_rows(dh_out, T, H, "dh_out")
+    if ck is None:
+        _want_rows(y, rows, H, "y")
+        if dn is not None:
+            _want_rows(h_out, T, H, "h_out")
+    else:
+        _want_rows(ck.u8, T, H, "checkpoint.u8")
+        _want_rows(ck.x8, T, H, "checkpoint.x8")
     dh = _rows(T, H, like.dtype) if want_dh else None
     dy = _rows(rows, H, like.dtype) if want_dy and branch else None
     dgate = _flat(T, _F32) if want_dgate and branch else None
@@ -174,6 +198,7 @@ class BlockNorm(torch.autograd.Function):
     def forward(ctx, h, y, gate_w, w_post, w_pre, slot=None, inv=None, res_scale=1.0, eps=1e-6, checkpoint=False):
         h_out, n, ck = block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint)
         ctx.consts = (res_scale, eps, ck is not None)
+        ctx.y_shape = None if y is None else y.shape
         ctx.save_for_backward(gate_w, w_post, w_pre, slot, inv, *(ck if ck is not None else (y, h_out, None, None)))
         ctx.set_materialize_grads(False)
         return h_out, n
@@ -190,6 +215,10 @@ class BlockNorm(torch.autograd.Function):
         dh, dy, dgate, dw_post, dw_pre = block_norm_grad(
             dense(dh_out), dense(dn), slot=slot, inv=inv, gate_w=gate_w, w_post=w_post, w_pre=w_pre, res_scale=res_scale, eps=eps,
             want_dh=need[0], want_dy=need[1], want_dgate=need[2], want_dw=need[3] or need[4], **kw)
+        if dy is not None:
+            if dy.numel() != ctx.y_shape.numel():
+                raise ValueError("inv: %d rows, where y is %s" % (dy.shape[0], tuple(ctx.y_shape)))
+            dy = dy.view(ctx.y_shape)
         if need[4] and w_pre is not None and dw_pre is None:   # n was not used: its weight has no gradient
             dw_pre = torch.zeros_like(w_pre)
         return (dh, dy if need[1] else None, dgate if need[2] else None, dw_post if need[3] else None, dw_pre if need[4] else None,

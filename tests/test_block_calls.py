@@ -74,3 +74,78 @@ def test_no_tensor_is_on_a_device_before_cuda_is_in_use():
         assert binding._device() is None
         with pytest.raises(ValueError):
             binding._arg(torch.zeros(4), F32, 4, "x", binding._device())
+
+
+@pytest.fixture
+def K(B, monkeypatch):
+    """The allocating calls on host memory, up to the library's entry points: `K.passed` holds the last call's arguments."""
+    from paper_2401_13920_b200 import block
+
+    class Passed(dict):
+        pass
+    seen = Passed()
+
+    def norm(shape, C_alloc, *a, **kw):
+        seen.clear(); seen.update(rows=C_alloc, T=shape.T, H=shape.H, **kw)
+    monkeypatch.setattr(block, "_here", lambda t, name: None)
+    monkeypatch.setattr(block, "_rows", lambda n, w, dt: torch.zeros(n, w, dtype=dt))
+    monkeypatch.setattr(block, "_flat", lambda n, dt: torch.zeros(n, dtype=dt))
+    monkeypatch.setattr(block, "_grad_bytes", lambda *a: 64)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "locmoe_block_norm", norm)
+    monkeypatch.setattr(B, "locmoe_block_norm_grad", norm)
+    monkeypatch.setattr(block, "passed", seen, raising=False)
+    return block
+
+
+def _z(*shape, dt=BF):
+    return torch.zeros(*shape, dtype=dt)
+
+
+def test_a_buffer_by_expert_has_all_its_rows(K):
+    """Experts' outputs as [E][C][H] or [D][E][C][H]: every row can be named by a slot, not the first E or D alone."""
+    for y in (_z(24, 16), _z(3, 8, 16), _z(2, 3, 4, 16)):
+        K.block_norm(_z(5, 16), y, _z(5, dt=I32))
+        assert K.passed["rows"] == 24 and K.passed["T"] == 5
+        inv = _z(24, dt=I32)
+        _, dy, *_ = K.block_norm_grad(_z(5, 16), _z(5, 16), _z(5, 16), y, slot=_z(5, dt=I32), inv=inv)
+        assert K.passed["rows"] == 24 and dy.shape == (24, 16)
+    K.block_norm(_z(5, 16), _z(3, 16), _z(5, dt=I32))                  # fewer rows than tokens
+    assert K.passed["rows"] == 3
+    K.block_norm(_z(5, 16), _z(7, 16))                                  # without slots rows beyond the tokens' are not read
+    K.block_norm_grad(_z(6, 16), _z(6, 16), _z(2, 3, 16), _z(3, 2, 16))
+
+
+def test_rows_of_another_width_or_number_are_refused(K):
+    h, y, s, inv = _z(6, 16), _z(8, 16), _z(6, dt=I32), _z(8, dt=I32)
+    for bad in (_z(16, 8), _z(8, 32), _z(8, 16, 1), _z(128), _z(())):
+        with pytest.raises(ValueError, match="y: "):
+            K.block_norm(h, bad, s)
+        with pytest.raises(ValueError, match="y: "):
+            K.block_norm(h, bad)
+        with pytest.raises(ValueError, match="y: "):
+            K.block_norm_grad(h, h, h, bad, slot=s, inv=inv)
+    with pytest.raises(ValueError, match="y: "):
+        K.block_norm(h, _z(5, 16))                                      # a token without a row
+    with pytest.raises(ValueError, match="y: needed"):
+        K.block_norm(h, slot=s)
+    for rows in (7, 9):                                                 # not the rows that the slots name
+        with pytest.raises(ValueError, match="y: "):
+            K.block_norm_grad(h, h, h, _z(rows, 16), slot=s, inv=inv)
+    with pytest.raises(ValueError, match="y: "):
+        K.block_norm_grad(h, h, h, y)                                   # T rows without slots
+    for bad in (_z(3, 32), _z(12, 8), _z(7, 16), _z(5, 16), _z(96)):
+        with pytest.raises(ValueError, match="dh_out: "):
+            K.block_norm_grad(bad, h, h, y, slot=s, inv=inv)
+        with pytest.raises(ValueError, match="h_out: "):
+            K.block_norm_grad(h, h, bad, y, slot=s, inv=inv)
+        code, r = bad.to(E4M3), _z(6, dt=F32)
+        good = h.to(E4M3)
+        with pytest.raises(ValueError, match="u8: "):
+            K.block_norm_grad(h, h, checkpoint=K.Checkpoint(code, good, r, r), slot=s, inv=inv)
+        with pytest.raises(ValueError, match="x8: "):
+            K.block_norm_grad(h, h, checkpoint=K.Checkpoint(good, code, r, r), slot=s, inv=inv)
+    with pytest.raises(ValueError, match="one of them"):
+        K.block_norm_grad(None, None, h, h)
+    K.block_norm_grad(h, None, None, y, slot=s, inv=inv)                # h_out is not read without dn
+    K.block_norm_grad(h, h, h, y, slot=s, inv=inv)

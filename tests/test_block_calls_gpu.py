@@ -80,3 +80,26 @@ def test_outputs_on_another_stream_wait_for_no_one_elses_readers(K, which):
     torch.cuda.synchronize()
     assert not any(bool(c.any()) for c in copies)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("ck", [False, True])
+def test_rows_by_expert(K, ck):
+    """The slot buffer as [E][C][H], as a batched product leaves it: the same bits as its rows one after the other, and a
+    gradient of its shape."""
+    s = _case(100, 264, torch.bfloat16, True, 6, rows=140)
+    assert int(s["slot"].max()) >= 7
+    y3 = s["y"].view(7, 20, 264)
+    kw = dict(gate_w=s["gate_w"], w_post=s["w_post"], w_pre=s["w_pre"], res_scale=0.9, eps=EPS)
+    flat, cube = (K.block_norm(s["h"], y, s["slot"], checkpoint=ck, **kw) for y in (s["y"], y3))
+    assert all(torch.equal(a, b) for a, b in zip(_flat([o for o in flat if o is not None]), _flat([o for o in cube if o is not None])))
+    acts = lambda y: dict(checkpoint=flat[2]) if ck else dict(h_out=flat[0], y=y)
+    want = K.block_norm_grad(s["dh_out"], s["dn"], slot=s["slot"], inv=s["inv"], **acts(s["y"]), **kw)
+    got = K.block_norm_grad(s["dh_out"], s["dn"], slot=s["slot"], inv=s["inv"], **acts(y3), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    leaf = y3.clone().requires_grad_()
+    h_out, n = K.BlockNorm.apply(s["h"], leaf, s["gate_w"], s["w_post"], s["w_pre"], s["slot"], s["inv"], 0.9, EPS, ck)
+    grad, = torch.autograd.grad([h_out, n], [leaf], [s["dh_out"], s["dn"]])
+    assert grad.shape == (7, 20, 264) and torch.equal(grad.view(140, 264), want[1])
+    with pytest.raises(ValueError, match="inv"):
+        out = K.BlockNorm.apply(s["h"], leaf, s["gate_w"], s["w_post"], s["w_pre"], s["slot"], s["inv"][:120], 0.9, EPS, True)
+        torch.autograd.grad(out, [leaf], [s["dh_out"], s["dn"]])
