@@ -12,6 +12,7 @@ from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 from torch._C._dynamo.guards import _empty_strided_cuda   # 0.7 us a tensor; torch.empty takes 2.3, as much as a launch
 
 from . import binding as B
@@ -192,7 +193,8 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
 
 class BlockNorm(torch.autograd.Function):
     """``BlockNorm.apply(h, y, gate_w, w_post, w_pre, slot, inv, res_scale, eps, checkpoint) -> (h_out, n)``, differentiable in
-    its first five arguments.  With ``checkpoint`` the activations kept for the gradient are the 8-bit ones."""
+    its first five arguments, once: the gradient of a gradient is an error.  With ``checkpoint`` the activations kept for the
+    gradient are the 8-bit ones."""
 
     @staticmethod
     def forward(ctx, h, y, gate_w, w_post, w_pre, slot=None, inv=None, res_scale=1.0, eps=1e-6, checkpoint=False):
@@ -204,6 +206,7 @@ class BlockNorm(torch.autograd.Function):
         return h_out, n
 
     @staticmethod
+    @once_differentiable   # the kernels leave no graph: without it the results would pass as constants
     def backward(ctx, dh_out, dn):
         gate_w, w_post, w_pre, slot, inv, *acts = ctx.saved_tensors
         res_scale, eps, packed = ctx.consts

@@ -103,3 +103,18 @@ def test_rows_by_expert(K, ck):
     with pytest.raises(ValueError, match="inv"):
         out = K.BlockNorm.apply(s["h"], leaf, s["gate_w"], s["w_post"], s["w_pre"], s["slot"], s["inv"][:120], 0.9, EPS, True)
         torch.autograd.grad(out, [leaf], [s["dh_out"], s["dn"]])
+
+
+@pytest.mark.parametrize("ck", [False, True])
+def test_second_derivatives_are_an_error(K, ck):
+    """A penalty on a gradient would be taken for a constant: differentiating it raises instead."""
+    s = _case(20, 64, torch.float32, True, 7)
+    leaves = [s[k].clone().requires_grad_() for k in ("h", "y", "gate_w", "w_post", "w_pre")]
+    h_out, n = K.BlockNorm.apply(*leaves, s["slot"], s["inv"], 0.9, EPS, ck)
+    first = torch.autograd.grad([h_out.sum() + n.square().sum()], leaves, create_graph=True)
+    loss = n.sum() + sum(g.pow(2).sum() for g in first)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        loss.backward()
+    h_out, n = K.BlockNorm.apply(*leaves, s["slot"], s["inv"], 0.9, EPS, ck)     # the first ones are as they were
+    again = torch.autograd.grad([h_out.sum() + n.square().sum()], leaves)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
