@@ -53,14 +53,21 @@ class Checkpoint(NamedTuple):
     r_pre: Optional[torch.Tensor]
 
 
+def _count(*n: int) -> None:
+    if max(n) > 2 ** 31 - 1:   # the library's counts have 32 bits, and ctypes cuts longer ones off without a word
+        raise ValueError("a size of %d is too large" % max(n))
+
+
 # Shape structs are read by a call and never written: one for each shape met, and the workspace sizes that go with them.
 @lru_cache(maxsize=1024)
 def _shape(T: int, H: int, E: int, dtype: torch.dtype) -> B.Shape:
+    _count(T, H, E)
     return B.Shape(T, H, E, 1, 1, B.dtype_code(dtype), B.LAYOUT_SEND)
 
 
 @lru_cache(maxsize=1024)
 def _few_plan(T: int, H: int, E: int, K: int, F: int, dtype: torch.dtype):
+    _count(K, F)
     shape = _shape(T, H, E, dtype)
     return shape, B.locmoe_moe_few_bytes(shape, K, F)
 
@@ -98,10 +105,11 @@ def moe_few(x, w_in, w_out, K=1, eps=None, weighted=True, stream=None):
     if w_in.shape[2] != H or w_out.shape != (E, H, F):
         raise ValueError("x %s, w_in %s and w_out %s do not belong together" % (tuple(x.shape), tuple(w_in.shape), tuple(w_out.shape)))
     _here(x, "x")
+    if T > 0:
+        shape, n = _few_plan(T, H, E, K, F, x.dtype)
     out, idx, w = _rows(T, H, x.dtype), _rows(K, T, torch.int32), _rows(K, T, _F32)
     if T == 0:
         return out, idx, w
-    shape, n = _few_plan(T, H, E, K, F, x.dtype)
     ws = _flat(n, torch.uint8)
     B.locmoe_moe_few(shape, x, K, F, w_in, w_out, idx, w, out, ws, eps, not weighted)
     return out, idx, w
@@ -126,6 +134,7 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
     if y is not None:
         have = y.numel() // max(H, 1)
         if slot is not None:
+            _count(have)
             rows = have
         _want_rows(y, have if slot is not None else max(have, T), H, "y")
     h_out = _rows(T, H, h.dtype) if want_h else None
@@ -162,6 +171,7 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
     shape = _row_shape(like)
     T, H = like.shape
     rows = inv.numel() if branch and slot is not None else T
+    _count(rows)
     _want_rows(dh_out, T, H, "dh_out")
     if ck is None:
         _want_rows(y, rows, H, "y")

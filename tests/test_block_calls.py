@@ -149,3 +149,17 @@ def test_rows_of_another_width_or_number_are_refused(K):
         K.block_norm_grad(None, None, h, h)
     K.block_norm_grad(h, None, None, y, slot=s, inv=inv)                # h_out is not read without dn
     K.block_norm_grad(h, h, h, y, slot=s, inv=inv)
+
+
+def test_sizes_beyond_32_bits_are_refused(K):
+    one = lambda *s: torch.zeros(1, dtype=BF).expand(*s)               # sizes without the memory
+    with pytest.raises(ValueError, match="too large"):
+        K.block_norm(one(2 ** 32 + 5, 1))
+    with pytest.raises(ValueError, match="too large"):
+        K.block_norm(_z(5, 1), one(2 ** 32 + 5, 1), _z(5, dt=I32))
+    with pytest.raises(ValueError, match="too large"):
+        K.block_norm_grad(_z(5, 1), None, y=one(2 ** 32 + 5, 1), slot=_z(5, dt=I32), inv=torch.zeros(1, dtype=I32).expand(2 ** 32 + 5))
+    with pytest.raises(ValueError, match="too large"):
+        K.moe_few(one(2 ** 32 + 1, 8), one(1, 8, 8), one(1, 8, 8), K=0)
+    with pytest.raises(ValueError, match="too large"):
+        K.moe_few(one(1, 8), one(1, 2 ** 32 + 8, 8), one(1, 8, 2 ** 32 + 8))
