@@ -536,11 +536,13 @@ int locmoe_moe_few(const locmoe_shape_t *shape, const void *x, const float *eps,
  * h, h_out, n_out [T][H] and y [T or D*E*C_alloc][H] of x_dtype; gate_w float[T]; w_post, w_pre float[H].  Sums in
  * fp32 in a fixed order, outputs rounded once.  h_out may be h.  With slot == NULL C_alloc is not read.  Pointers are
  * aligned to their elements; rows of whole 16-byte vectors (H % 8 == 0, 16-byte aligned arrays) take the fast kernel.
+ * T, H <= LOCMOE_BLOCK_NORM_MAX (LOCMOE_ERR_TOO_LARGE), here and in the gradient.
  *
  * Checkpoints (each pair NULL to skip): u8 = N(v), x8 = N(h') as [T][H] codes in E4M3 (8 bits, to nearest even),
  * r_post, r_pre float[T] the reciprocal norms 1 / sqrt(mean + eps).  They are all the gradient needs of h' and y;
  * a normalised element is at most sqrt(H), so H <= 200000 when they are asked for (448 is the format's largest).
  */
+enum { LOCMOE_BLOCK_NORM_MAX = 0x7fffffff - 0xffff };
 typedef struct {
     const void *h; const void *y; const int32_t *slot; const float *gate_w; const float *w_post; const float *w_pre;
     float res_scale; float eps;

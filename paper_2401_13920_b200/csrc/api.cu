@@ -414,9 +414,14 @@ bool element_aligned(const void* p, int n) { return (uintptr_t)p % n == 0; }
 long long norm_rows(const locmoe_shape_t* s, int32_t C_alloc, const int32_t* slot) { return slot ? buffer_rows(s, C_alloc) : s->T; }
 
 constexpr int32_t kMaxCheckpointH = 200000;   // sqrt(H) < 448, the largest E4M3 value
-}  // namespace
 
-namespace {
+// Counts below the largest int by more than a grid's stride: the block norms' kernels step over them in ints.
+int check_norm_shape(const locmoe_shape_t* s) {
+    int rc = check_shape(s);
+    if (rc) return rc;
+    return s->T > LOCMOE_BLOCK_NORM_MAX || s->H > LOCMOE_BLOCK_NORM_MAX ? LOCMOE_ERR_TOO_LARGE : LOCMOE_OK;
+}
+
 int check_few(const locmoe_shape_t* s, int32_t K, int32_t F) {
     int rc = check_shape(s);
     if (rc) return rc;
@@ -451,7 +456,7 @@ int locmoe_moe_few(const locmoe_shape_t* shape, const void* x, const float* eps,
 }
 
 int locmoe_block_norm(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe_block_norm_t* b, void* stream) {
-    int rc = check_shape(shape);
+    int rc = check_norm_shape(shape);
     if (rc) return rc;
     if (!b || !b->h || (!b->h_out && !b->n_out)) return LOCMOE_ERR_NULL;
     if (!b->y && (b->slot || b->u8 || b->r_post)) return LOCMOE_ERR_NULL;
@@ -470,7 +475,7 @@ int locmoe_block_norm(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe
 }
 
 int locmoe_block_norm_grad_bytes(const locmoe_shape_t* shape, size_t* bytes) {
-    int rc = check_shape(shape);
+    int rc = check_norm_shape(shape);
     if (rc) return rc;
     if (!bytes) return LOCMOE_ERR_NULL;
     *bytes = block_norm_grad_ws_bytes(*shape);
@@ -479,7 +484,7 @@ int locmoe_block_norm_grad_bytes(const locmoe_shape_t* shape, size_t* bytes) {
 
 int locmoe_block_norm_grad(const locmoe_shape_t* shape, int32_t C_alloc, const locmoe_block_norm_grad_t* b, void* ws,
                            size_t ws_bytes, void* stream) {
-    int rc = check_shape(shape);
+    int rc = check_norm_shape(shape);
     if (rc) return rc;
     if (!b || (!b->dh_out && !b->dn)) return LOCMOE_ERR_NULL;
     const bool ck = b->u8 || b->x8;

@@ -163,3 +163,18 @@ def test_sizes_beyond_32_bits_are_refused(K):
         K.moe_few(one(2 ** 32 + 1, 8), one(1, 8, 8), one(1, 8, 8), K=0)
     with pytest.raises(ValueError, match="too large"):
         K.moe_few(one(1, 8), one(1, 2 ** 32 + 8, 8), one(1, 8, 2 ** 32 + 8))
+
+
+def test_counts_near_the_largest_int_are_refused():
+    """The kernels step over tokens and columns in ints: a count within a grid's stride of the largest one would wrap."""
+    import ctypes as C
+    from paper_2401_13920_b200 import binding as B
+    most, P = 0x7fffffff - 0xffff, 1 << 20
+    size = C.c_size_t()
+    for T, H, rc in ((most + 1, 1, -7), (0x7fffffff, 1, -7), (1, most + 1, -7), (1, 0x7fffffff, -7), (most, 1, -4), (1, most, -4)):
+        sh = B.Shape(T, H, 1, 1, 1, B.BF16, 0)
+        norm = B.BlockNorm(h=P + 1, h_out=P, eps=1e-6, res_scale=1.0)      # the last check: a misaligned array
+        grad = B.BlockNormGrad(dh_out=P + 1, dh=P, eps=1e-6, res_scale=1.0)
+        assert B._lib.locmoe_block_norm(C.byref(sh), 1, C.byref(norm), None) == rc
+        assert B._lib.locmoe_block_norm_grad(C.byref(sh), 1, C.byref(grad), None, 0, None) == rc
+        assert B._lib.locmoe_block_norm_grad_bytes(C.byref(sh), C.byref(size)) == (rc if rc == -7 else 0)
