@@ -532,7 +532,9 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a, const i
                 __syncwarp();
                 int last = 0;
                 if (lane == 0) last = add_acq_rel(&a.arrived[t.rb * V::WR + wr]) == chunks * p.S - 1;
-                if (__shfl_sync(0xffffffffu, last, 0)) {
+                last = __shfl_sync(0xffffffffu, last, 0);
+                __syncwarp();   // a shuffle orders no memory: what lane 0 has acquired, the other lanes read behind this
+                if (last) {
                     constexpr int Q = 2 * NB;   // lanes that share a token's 8 * NB columns
                     const int row = t.row0 + wr * 8 * NB + (lane % Q) * 4;
                     if (row < p.N) {

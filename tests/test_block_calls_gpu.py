@@ -118,3 +118,17 @@ def test_second_derivatives_are_an_error(K, ck):
     h_out, n = K.BlockNorm.apply(*leaves, s["slot"], s["inv"], 0.9, EPS, ck)     # the first ones are as they were
     again = torch.autograd.grad([h_out.sum() + n.square().sum()], leaves)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("T,H,F,E,k", [(3, 512, 8192, 4, 2), (16, 512, 4096, 8, 2), (128, 1024, 1024, 4, 2), (40, 264, 19000, 4, 2)])
+def test_slices_are_joined_behind_their_last_store(K, T, H, F, E, k):
+    """The last task to arrive adds up slices that other CTAs have stored: the bits of every repetition, with other inputs
+    (and so other slices in the same workspace) in between."""
+    x, w_in, w_out, eps = _inputs(T, H, F, E, 3, bias=True)
+    xs = [x, -x, x.flip(0)]
+    want = [K.moe_few(v, w_in, w_out, K=k, eps=eps)[0] for v in xs]
+    bad = torch.zeros(3, dtype=torch.int64, device="cuda")
+    for i in range(300):
+        out = K.moe_few(xs[i % 3], w_in, w_out, K=k, eps=eps)[0]
+        bad[i % 3] += (out != want[i % 3]).sum()
+    assert bad.tolist() == [0, 0, 0]
