@@ -171,9 +171,14 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr())
 
 
+# Handle of a device's current stream: torch.cuda.current_stream() builds a Stream object for it, 3 us a call.  The short way
+# has no public name, so a torch may lack it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream):
-    if stream is None:   # the raw handle: torch.cuda.current_stream() builds a Stream object for it, 3 us a call
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    if stream is None:
+        return C.c_void_p(_raw_stream(torch.cuda.current_device()))
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 

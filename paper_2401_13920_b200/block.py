@@ -13,9 +13,14 @@ from typing import NamedTuple, Optional
 
 import torch
 from torch.autograd.function import once_differentiable
-from torch._C._dynamo.guards import _empty_strided_cuda   # 0.7 us a tensor; torch.empty takes 2.3, as much as a launch
 
 from . import binding as B
+
+try:   # 0.7 us a tensor; torch.empty takes 2.3, as much as a launch
+    from torch._C._dynamo.guards import _empty_strided_cuda
+except ImportError:   # no public name: a torch may have moved it
+    def _empty_strided_cuda(size, stride, dtype):
+        return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
 
 
 def _rows(n: int, width: int, dtype: torch.dtype) -> torch.Tensor:

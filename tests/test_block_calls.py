@@ -178,3 +178,29 @@ def test_counts_near_the_largest_int_are_refused():
         assert B._lib.locmoe_block_norm(C.byref(sh), 1, C.byref(norm), None) == rc
         assert B._lib.locmoe_block_norm_grad(C.byref(sh), 1, C.byref(grad), None, 0, None) == rc
         assert B._lib.locmoe_block_norm_grad_bytes(C.byref(sh), C.byref(size)) == (rc if rc == -7 else 0)
+
+
+LOST = """
+import sys, types, torch
+sys.modules["torch._C._dynamo.guards"] = types.ModuleType("guards")       # as of a torch that has moved it
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    del torch._C._cuda_getCurrentRawStream
+from paper_2401_13920_b200 import binding, block
+made = []
+torch.empty_strided = lambda *a, **k: made.append((a, k)) or torch.zeros(1)
+block._rows(3, 5, torch.float32)
+assert made == [(((3, 5), (5, 1)), dict(dtype=torch.float32, device="cuda"))], made
+torch.cuda.current_device = lambda: 0
+torch.cuda.current_stream = lambda device=None: types.SimpleNamespace(cuda_stream=77)
+assert binding._stream(None).value == 77 and binding._stream(5).value == 5
+print("fine")
+"""
+
+
+def test_a_torch_without_the_short_ways():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    res = subprocess.run([sys.executable, "-c", LOST], cwd=root, capture_output=True, text=True)
+    assert res.returncode == 0 and "fine" in res.stdout, res.stderr
