@@ -195,6 +195,8 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
             if t is not None:
                 t.zero_()
         return dh, dy, dgate, dw_post, dw_pre
+    if dh is dy is dgate is dw_post is dw_pre is None:   # nothing is asked for that is there
+        return dh, dy, dgate, dw_post, dw_pre
     ws = None
     if dw_post is not None or dw_pre is not None:
         ws = _flat(_grad_bytes(T, H, like.dtype, torch.cuda.current_device()), torch.uint8)

@@ -93,7 +93,11 @@ def K(B, monkeypatch):
     monkeypatch.setattr(block, "_grad_bytes", lambda *a: 64)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(B, "locmoe_block_norm", norm)
-    monkeypatch.setattr(B, "locmoe_block_norm_grad", norm)
+
+    def grad(shape, C_alloc, *a, **kw):
+        assert any(kw[k] is not None for k in ("dh", "dy", "dgate", "dw_post", "dw_pre")), "the library refuses a call without outputs"
+        norm(shape, C_alloc, *a, **kw)
+    monkeypatch.setattr(B, "locmoe_block_norm_grad", grad)
     monkeypatch.setattr(block, "passed", seen, raising=False)
     return block
 
@@ -178,6 +182,21 @@ def test_counts_near_the_largest_int_are_refused():
         assert B._lib.locmoe_block_norm(C.byref(sh), 1, C.byref(norm), None) == rc
         assert B._lib.locmoe_block_norm_grad(C.byref(sh), 1, C.byref(grad), None, 0, None) == rc
         assert B._lib.locmoe_block_norm_grad_bytes(C.byref(sh), C.byref(size)) == (rc if rc == -7 else 0)
+
+
+def test_a_gradient_of_nothing_that_is_there(K):
+    """Weights that the loss does not reach have a gradient of zero or none, not an error."""
+    h, w = _z(6, 16), torch.ones(16, requires_grad=True)
+    h_out, n = K.BlockNorm.apply(h, None, None, None, w)
+    h_out.float().sum().backward()                                      # n, which alone has w in it, is not used
+    assert w.grad.shape == (16,) and not w.grad.any() and "dh" not in K.passed
+    gate = torch.ones(6, requires_grad=True)
+    h_out, n = K.BlockNorm.apply(h, None, gate, None, None)             # no branch that the gate would be applied to
+    n.float().sum().backward()
+    assert gate.grad is None or not gate.grad.any()
+    assert K.block_norm_grad(h, None, want_dh=False) == (None,) * 5
+    K.block_norm_grad(h, h, h, want_dh=False)                           # w_pre's alone
+    assert K.passed["dw_pre"].shape == (16,) and K.passed["dh"] is None
 
 
 LOST = """

@@ -132,3 +132,14 @@ def test_slices_are_joined_behind_their_last_store(K, T, H, F, E, k):
         out = K.moe_few(xs[i % 3], w_in, w_out, K=k, eps=eps)[0]
         bad[i % 3] += (out != want[i % 3]).sum()
     assert bad.tolist() == [0, 0, 0]
+
+
+def test_weight_of_a_norm_that_is_not_used(K):
+    """Only w_pre needs a gradient and n is not used: zeros, with or without a branch."""
+    s = _case(30, 72, torch.float32, False, 8)
+    for y in (None, s["y"]):
+        for ck in (False, True):
+            w = s["w_pre"].clone().requires_grad_()
+            h_out, n = K.BlockNorm.apply(s["h"], y, None, None, w, None, None, 1.0, EPS, ck)
+            h_out.sum().backward()
+            assert w.grad.shape == w.shape and not w.grad.any()
