@@ -83,14 +83,14 @@ def route(n, E, capacity_factor=1.25):
 
 def train_step(h, w_pre, w_in, w_out, w_post, w_next, target, checkpoint=True):
     """Loss and gradients of one block and the norm after it: ``loss = mean((n' - target)^2)``.  All weights require grad."""
-    none = dict(slot=None, inv=None, res_scale=1.0, eps=EPS, checkpoint=checkpoint)
-    _, n = block.BlockNorm.apply(h, None, None, None, w_pre, *none.values())
+    norm = dict(res_scale=1.0, eps=EPS, checkpoint=checkpoint, want_h=False)      # of h' nothing but its norm is used here
+    _, n = block.BlockNorm.apply(h, None, None, None, w_pre, None, None, *norm.values())
     with torch.no_grad():
         st = route(n.detach(), w_in.shape[0])
     E, rows = w_in.shape[0], st.rows
     x = torch.where((st.inv >= 0)[:, None], n[st.inv.clamp_min(0).long()], 0.0).reshape(E, rows // E, -1)
     y = torch.bmm(torch.nn.functional.gelu(torch.bmm(x, w_in.transpose(1, 2))), w_out.transpose(1, 2)).reshape(rows, -1)
-    _, n2 = block.BlockNorm.apply(h, y, st.gate_w, w_post, w_next, st.slot, st.inv, 1.0, EPS, checkpoint)
+    _, n2 = block.BlockNorm.apply(h, y, st.gate_w, w_post, w_next, st.slot, st.inv, *norm.values())
     loss = (n2.float() - target).square().mean()
     loss.backward()
     return loss.detach()

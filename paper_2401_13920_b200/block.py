@@ -209,18 +209,20 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
 
 
 class BlockNorm(torch.autograd.Function):
-    """``BlockNorm.apply(h, y, gate_w, w_post, w_pre, slot, inv, res_scale, eps, checkpoint) -> (h_out, n)``, differentiable in
-    its first five arguments, once: the gradient of a gradient is an error.  With ``checkpoint`` the activations kept for the
-    gradient are the 8-bit ones."""
+    """``BlockNorm.apply(h, y, gate_w, w_post, w_pre, slot, inv, res_scale, eps, checkpoint, want_h) -> (h_out, n)``,
+    differentiable in its first five arguments, once: the gradient of a gradient is an error.  With ``checkpoint`` the
+    activations kept for the gradient are the 8-bit ones.  Without ``want_h`` h_out is None (the norm before the first block,
+    whose h goes on as it is) and is formed only where the gradient needs it."""
 
     @staticmethod
-    def forward(ctx, h, y, gate_w, w_post, w_pre, slot=None, inv=None, res_scale=1.0, eps=1e-6, checkpoint=False):
-        h_out, n, ck = block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint)
+    def forward(ctx, h, y, gate_w, w_post, w_pre, slot=None, inv=None, res_scale=1.0, eps=1e-6, checkpoint=False, want_h=True):
+        same = y is None and res_scale == 1.0   # h' is h
+        h_out, n, ck = block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint, want_h or not (checkpoint or same))
         ctx.consts = (res_scale, eps, ck is not None)
         ctx.y_shape = None if y is None else y.shape
-        ctx.save_for_backward(gate_w, w_post, w_pre, slot, inv, *(ck if ck is not None else (y, h_out, None, None)))
+        ctx.save_for_backward(gate_w, w_post, w_pre, slot, inv, *(ck if ck is not None else (y, h if h_out is None else h_out, None, None)))
         ctx.set_materialize_grads(False)
-        return h_out, n
+        return h_out if want_h else None, n
 
     @staticmethod
     @once_differentiable   # the kernels leave no graph: without it the results would pass as constants
@@ -228,7 +230,7 @@ class BlockNorm(torch.autograd.Function):
         gate_w, w_post, w_pre, slot, inv, *acts = ctx.saved_tensors
         res_scale, eps, packed = ctx.consts
         if dh_out is None and dn is None:
-            return (None,) * 10
+            return (None,) * 11
         need = ctx.needs_input_grad
         dense = lambda t: None if t is None else t.contiguous()
         kw = dict(checkpoint=Checkpoint(*acts)) if packed else dict(y=acts[0], h_out=acts[1])
@@ -242,4 +244,4 @@ class BlockNorm(torch.autograd.Function):
         if need[4] and w_pre is not None and dw_pre is None:   # n was not used: its weight has no gradient
             dw_pre = torch.zeros_like(w_pre)
         return (dh, dy if need[1] else None, dgate if need[2] else None, dw_post if need[3] else None, dw_pre if need[4] else None,
-                None, None, None, None, None)
+                None, None, None, None, None, None)

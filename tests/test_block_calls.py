@@ -86,7 +86,7 @@ def K(B, monkeypatch):
     seen = Passed()
 
     def norm(shape, C_alloc, *a, **kw):
-        seen.clear(); seen.update(rows=C_alloc, T=shape.T, H=shape.H, **kw)
+        seen.clear(); seen.update(rows=C_alloc, T=shape.T, H=shape.H, wants_h=len(a) > 8 and a[8] is not None, **kw)
     monkeypatch.setattr(block, "_here", lambda t, name: None)
     monkeypatch.setattr(block, "_rows", lambda n, w, dt: torch.zeros(n, w, dtype=dt))
     monkeypatch.setattr(block, "_flat", lambda n, dt: torch.zeros(n, dtype=dt))
@@ -197,6 +197,17 @@ def test_a_gradient_of_nothing_that_is_there(K):
     assert K.block_norm_grad(h, None, want_dh=False) == (None,) * 5
     K.block_norm_grad(h, h, h, want_dh=False)                           # w_pre's alone
     assert K.passed["dw_pre"].shape == (16,) and K.passed["dh"] is None
+
+
+def test_a_stream_nobody_asks_for_is_not_written(K):
+    """h' of a norm without a branch is h itself: with want_h = False no copy of it is made."""
+    h = _z(6, 16).requires_grad_()
+    y = _z(6, 16)
+    for checkpoint in (False, True):
+        for branch, scale, formed in ((None, 1.0, False), (None, 0.5, not checkpoint), (y, 1.0, not checkpoint)):
+            h_out, n = K.BlockNorm.apply(h, branch, None, None, None, None, None, scale, 1e-6, checkpoint, False)
+            assert h_out is None and K.passed["wants_h"] == formed
+            assert K.BlockNorm.apply(h, branch, None, None, None, None, None, scale, 1e-6, checkpoint)[0] is not None
 
 
 LOST = """

@@ -143,3 +143,20 @@ def test_weight_of_a_norm_that_is_not_used(K):
             h_out, n = K.BlockNorm.apply(s["h"], y, None, None, w, None, None, 1.0, EPS, ck)
             h_out.sum().backward()
             assert w.grad.shape == w.shape and not w.grad.any()
+
+
+@pytest.mark.parametrize("ck", [False, True])
+@pytest.mark.parametrize("branch,scale", [(False, 1.0), (False, 0.5), (True, 1.0)])
+def test_gradients_without_the_stream(K, branch, scale, ck):
+    """BlockNorm without want_h: n and all gradients as with it."""
+    s = _case(60, 200, torch.bfloat16, True, 9)
+    got = []
+    for want_h in (True, False):
+        leaves = [s[k].clone().requires_grad_() for k in (("h", "y", "gate_w", "w_post", "w_pre") if branch else ("h", "w_pre"))]
+        h, w = leaves[0], leaves[-1]
+        y, gate, wp = leaves[1:4] if branch else (None,) * 3
+        sl = (s["slot"], s["inv"]) if branch else (None, None)
+        h_out, n = K.BlockNorm.apply(h, y, gate, wp, w, *sl, scale, EPS, ck, want_h)
+        assert (h_out is None) != want_h
+        got.append([n, *torch.autograd.grad([n], leaves, [s["dn"]])])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
