@@ -174,6 +174,7 @@ def _ptr(t):
 # Handle of a device's current stream: torch.cuda.current_stream() builds a Stream object for it, 3 us a call.  The short way
 # has no public name, so a torch may lack it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # the same, where CUDA is in use already
 
 
 def _stream(stream):
@@ -506,7 +507,7 @@ def locmoe_moe_few_bytes(shape: Shape, K, F) -> int:
 
 def _device():
     """Index of the device that the calls below launch on; None before CUDA is in use (no tensor is on a device then)."""
-    return torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    return _raw_device() if torch.cuda.is_initialized() else None
 
 
 def _arg(t, dtype, numel, name, dev):

@@ -35,8 +35,9 @@ _F32 = torch.float32
 
 
 def _here(t: torch.Tensor, name: str) -> None:
-    """Outputs, workspace and launch belong to the current device: so must the inputs."""
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    """Outputs, workspace and launch belong to the current device, so must the inputs.  The binding compares each tensor of a
+    launch with it; here are those of calls that launch nothing (no rows), and host memory, before anything is allocated."""
+    if not t.is_cuda or (t.numel() == 0 and t.get_device() != torch.cuda.current_device()):
         raise ValueError("%s: on %s, which is not the current CUDA device" % (name, t.device))
 
 
@@ -82,18 +83,19 @@ def _grad_bytes(T: int, H: int, dtype: torch.dtype, device: int) -> int:
     return B.locmoe_block_norm_grad_bytes(_shape(T, H, 1, dtype))
 
 
-def _row_shape(like: torch.Tensor) -> B.Shape:
-    """Shape struct for [T][H] tensors like this one."""
+def _row_shape(like: torch.Tensor) -> tuple:
+    """Shape struct, T and H for [T][H] tensors like this one."""
     if like.dim() != 2:
         raise ValueError("expected a [T][H] tensor, got %s" % (tuple(like.shape),))
-    shape = _shape(like.shape[0], like.shape[1], 1, like.dtype)
+    T, H = like.shape
+    shape = _shape(T, H, 1, like.dtype)
     _here(like, "rows")
-    return shape
+    return shape, T, H
 
 
 def _want_rows(t, rows: int, H: int, name: str) -> None:
     """`t` (None: absent) is `rows` rows of H elements; how its other dimensions group them does not matter."""
-    if t is not None and (t.shape[-1:] != (H,) or t.numel() != rows * H):
+    if t is not None and t.shape != (rows, H) and (t.shape[-1:] != (H,) or t.numel() != rows * H):
         raise ValueError("%s: expected %d rows of %d, got %s" % (name, rows, H, tuple(t.shape)))
 
 
@@ -133,15 +135,14 @@ def block_norm(h, y=None, slot=None, gate_w=None, w_post=None, w_pre=None, res_s
             return block_norm(h, y, slot, gate_w, w_post, w_pre, res_scale, eps, checkpoint, want_h, want_n)
     if slot is not None and y is None:
         raise ValueError("y: needed with slot")
-    shape = _row_shape(h)
-    T, H = h.shape
+    shape, T, H = _row_shape(h)
     rows = T
-    if y is not None:
+    if y is not None and (slot is not None or y.shape != h.shape):
         have = y.numel() // max(H, 1)
         if slot is not None:
-            _count(have)
             rows = have
-        _want_rows(y, have if slot is not None else max(have, T), H, "y")
+            _count(rows)
+        _want_rows(y, max(have, rows), H, "y")
     h_out = _rows(T, H, h.dtype) if want_h else None
     n = _rows(T, H, h.dtype) if want_n else None
     u8 = x8 = r_post = r_pre = None
@@ -173,10 +174,11 @@ def block_norm_grad(dh_out, dn, h_out=None, y=None, checkpoint: Optional[Checkpo
     branch = (ck.u8 if ck is not None else y) is not None
     if slot is not None and inv is None:
         raise ValueError("inv: needed with slot (it says how many rows y has and which of them are empty)")
-    shape = _row_shape(like)
-    T, H = like.shape
-    rows = inv.numel() if branch and slot is not None else T
-    _count(rows)
+    shape, T, H = _row_shape(like)
+    rows = T
+    if branch and slot is not None:
+        rows = inv.numel()
+        _count(rows)
     _want_rows(dh_out, T, H, "dh_out")
     if ck is None:
         _want_rows(y, rows, H, "y")

@@ -234,3 +234,29 @@ def test_a_torch_without_the_short_ways():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     res = subprocess.run([sys.executable, "-c", LOST], cwd=root, capture_output=True, text=True)
     assert res.returncode == 0 and "fine" in res.stdout, res.stderr
+
+
+def test_a_torch_without_the_short_way_to_its_device():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch
+del torch._C._cuda_getDevice
+from paper_2401_13920_b200 import binding
+assert binding._device() is None and binding._raw_device is torch.cuda.current_device
+print("fine")
+"""
+    res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert res.returncode == 0 and "fine" in res.stdout, res.stderr
+
+
+def test_tensors_without_rows_have_to_be_on_the_current_device_too(monkeypatch):
+    """A call without rows launches nothing, so the binding never sees its tensors."""
+    from paper_2401_13920_b200 import block
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    block._here(StandIn(0, BF, index=0), "x")
+    for t in (StandIn(0, BF, index=1), StandIn(0, BF, index=-1), StandIn(8, BF, index=-1)):
+        with pytest.raises(ValueError, match="x: on"):
+            block._here(t, "x")
