@@ -10,7 +10,8 @@
 // The tokens travel with the weights because a load that a multiplying warp issues itself queues behind the ring's
 // own (4000 cycles at a full ring: 2.9 against 6.5 TB/s on a stream of rows of 10240).
 // Both launches are programmatic: the CTAs of one take the SMs over as those of the one before leave them.  (One
-// cooperative kernel with a wait of the grid in between is no faster: its launch does not overlap anything.)
+// cooperative kernel with a wait of the grid in between, behind a router launch of its own, took 37 us for one token where
+// two launches with the router inside took 36; without the router launch it was not tried.)
 // The products run on mma.sync m16n8k16, tokens as the 16 rows and weight rows as the 8 columns: at a few tokens an
 // expert nothing is gained by larger matrix instructions.  The order of k inside a stage is chosen so that a thread's
 // fragments of both operands are 16 contiguous bytes of a row (the same permutation on both sides), which the weight
@@ -42,8 +43,8 @@ struct FewArgs {
 
 // A variant: GR groups, each with a ring, a producer warp and multiplying warps, WR along the weight rows and WK along
 // k; NB blocks of 8 weight rows a warp, BW boxes of 64 k a warp and stage, MT tiles of 16 tokens; the shared memory of
-// a CTA; the tasks an SM that the second product's reduction is sliced for.  A group works on every GR-th task by itself, so that one group's sums and stores run beside the others'
-// products.
+// a CTA; the tasks an SM that the second product's reduction is sliced for.  A group works on every GR-th task by itself,
+// so that one group's sums and stores run beside the others' products.
 constexpr int kMaxStages = 8;   // of a group's ring
 template <int GR_, int WR_, int WK_, int NB_, int BW_, int MT_, int SMEM_, int WANT_>
 struct Variant {
@@ -558,8 +559,8 @@ moe_few_kernel(const __grid_constant__ CUtensorMap map, const FewArgs a, const i
                     __syncwarp();
                 }
             }
-                turn = turn + 1 == WK ? 0 : turn + 1;
-            }
+            turn = turn + 1 == WK ? 0 : turn + 1;
+        }
     }
     // After a wait that was given up copies may still be on their way into this CTA's shared memory: it stays for a
     // millisecond, hundreds of times their latency, before it leaves.
