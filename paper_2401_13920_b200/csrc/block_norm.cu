@@ -11,8 +11,8 @@
 // once.  The two sums of a row are two round trips through the group, during which a kernel that loads its rows itself
 // asks memory for nothing (65536 x 5120 in bf16: 699 us forward, 58 % of the copy bandwidth); so each group has a ring
 // of rows in shared memory that bulk copies fill D rows ahead, a thread asking for an array of the row D on as soon as a
-// sum's barrier shows that the group has taken a row out of its place (forward 418-435 us, 93-97 % of the copy bandwidth;
-// with checkpoints at 65536 x 2560 478 -> 278-285 us, 89-91 %).
+// sum's barrier shows that the group has taken a row out of its place (forward 415-435 us, 92-97 % of the copy bandwidth;
+// with checkpoints at 65536 x 2560 478 -> 277-295 us, 86-91 %).
 // Sums are fp32 in a fixed order; outputs are rounded once.
 // With checkpoints the forward also leaves u and x in E4M3: a normalised row has mean square <= 1 and so no element
 // above sqrt(H), which the format's 448 covers for every H the library takes here; r and q carry the scale.
@@ -866,7 +866,7 @@ __global__ void __launch_bounds__(TH) block_norm_ring_kernel(const NormArgs a) {
 // thread of another warp (by four lanes of one warp 789 us against 737).  Not taken: an mbarrier that warps pass later
 // than they arrive at it, with the work that needs no sum in between (860 us); widened rows kept over the meeting (1249
 // us: what spills comes back through an L1 that the rings leave little of).
-// Reached at 65536 x 5120 in bf16: 744-762 us (5.2-5.3 TB/s, 80-82 % of the copy bandwidth), from checkpoints 651-662.
+// Reached at 65536 x 5120 in bf16: 714-762 us (5.2-5.6 TB/s, 80-85 % of the copy bandwidth), from checkpoints 651-662.
 // FULL: every thread has two units.  ALL: both upstream gradients, the branch, dh and dy are there.  ODD: see above (also
 // rows of codes that are no whole 16-byte pieces).
 constexpr int kGradThreads = 384;   // 168 registers a thread; the weights of rows beyond 16 x 384 lie in shared memory, 512 threads
