@@ -25,6 +25,7 @@
 
 #include "common.cuh"
 #include "tensor_map.cuh"
+#include "umma.cuh"
 
 namespace locmoe {
 
@@ -49,9 +50,6 @@ struct FfnArgs {
     int split_from;       // wide kernel: tiles from this index on are worked on as two half tiles (see there)
 };
 
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 // Bounded wait that also gives up as soon as another role has raised the abort word.
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_word) {
     for (uint32_t i = 0; i < (1u << 22); ++i) {
@@ -63,29 +61,6 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, vo
     return false;
 }
 
-// After a wait has been given up: asynchronous work this CTA started (bulk tensor loads that write its shared
-// memory and count on its barriers, tcgen05.commit arrivals) may still be in flight, and a CTA must not leave
-// while it is.  Nothing tells when the last of it has landed once the barriers' phases are out of step, so the
-// CTA simply stays for a millisecond -- hundreds of times the latency of any such operation -- before it goes on
-// to free its tensor memory.  Bounded, and only ever executed on the failure path.
-__device__ __forceinline__ void quiesce_after_abort(volatile int* abort_word) {
-    if (*abort_word) {
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-    }
-}
-
-__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-                 : "memory");
-}
-
-// Shared-memory matrix descriptor of a K-major bf16 tile with 128-byte swizzle: rows of 128 bytes, groups of
-// 8 rows 1024 bytes apart (stride byte offset), leading byte offset unused (1), descriptor version 1.
-__device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr) {
-    return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
-           (2ull << 61);
-}
 // Instruction descriptor: bf16 x bf16 -> fp32, both operands K-major, M = 128, N = 256.
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
 
@@ -94,58 +69,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t adesc, uint6
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(kIdesc), "r"(accumulate) : "memory");
-}
-// Arrives on the mbarrier once all MMAs issued so far by this thread have completed.
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// 32-byte store: one full sector per lane (rows of the output are far apart, so a warp store touches 32 sectors;
-// writing each of them whole avoids partial-sector writes in L2).  Needs a 32-byte aligned address.
-__device__ __forceinline__ void st_global_v8(void* p, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t a4,
-                                             uint32_t a5, uint32_t a6, uint32_t a7) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a0), "r"(a1), "r"(a2), "r"(a3),
-                 "r"(a4), "r"(a5), "r"(a6), "r"(a7) : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-// GeLU(v) = v * Phi(v) with Phi(v) = 1 - 0.5 erfc(v / sqrt 2).  erfc(x) = P(t) exp(-x^2), t = 1 / (1 + p x), for
-// x >= 0 by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (absolute error below 1.5e-7,
-// far under the bf16 rounding of the result); the negative side uses erfc(-x) = 2 - erfc(x) written so that a
-// small Phi is not formed by cancellation.  The reciprocal and the exponential are the hardware approximations
-// (rcp.approx, ex2.approx: a couple of ulps, far below the bf16 rounding of the result; 2.42 against 2.48 ms for the
-// first GEMM of the 65536 x 2560 x 10240 case).  About a third of the instructions of erff().
-// Two elements at a time with the two-wide fp32 instructions: the epilogue warps share their schedulers with
-// the TMA and MMA warps, so fewer epilogue instructions directly mean fewer bubbles in the MMA stream.
-__device__ __forceinline__ float rcp_approx(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float ex2_approx(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float2 gelu_erf2(float2 v) {
-    const float2 x = __fmul2_rn(make_float2(fabsf(v.x), fabsf(v.y)), make_float2(0.70710678118654752f, 0.70710678118654752f));
-    const float2 den = __ffma2_rn(make_float2(0.3275911f, 0.3275911f), x, make_float2(1.0f, 1.0f));
-    const float2 t = make_float2(rcp_approx(den.x), rcp_approx(den.y));
-    float2 poly = __ffma2_rn(make_float2(0.5307027145f, 0.5307027145f), t, make_float2(-0.7265760135f, -0.7265760135f));
-    poly = __ffma2_rn(poly, t, make_float2(0.7107068705f, 0.7107068705f));
-    poly = __ffma2_rn(poly, t, make_float2(-0.142248368f, -0.142248368f));
-    poly = __ffma2_rn(poly, t, make_float2(0.127414796f, 0.127414796f));
-    const float2 arg = __fmul2_rn(__fmul2_rn(x, x), make_float2(-1.4426950408889634f, -1.4426950408889634f));
-    const float2 ex = make_float2(ex2_approx(arg.x), ex2_approx(arg.y));
-    const float2 h = __fmul2_rn(__fmul2_rn(poly, t), ex);
-    const float2 om = __ffma2_rn(h, make_float2(-1.0f, -1.0f), make_float2(1.0f, 1.0f));
-    const float2 phi = make_float2(v.x < 0.0f ? h.x : om.x, v.y < 0.0f ? h.y : om.y);
-    return __fmul2_rn(v, phi);
 }
 // Stores 32 consecutive columns of one output row (converted to the output type); static indexing keeps v[] in
 // registers.
