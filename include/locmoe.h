@@ -577,6 +577,85 @@ int locmoe_block_norm_grad(const locmoe_shape_t *shape, int32_t C_alloc, const l
                            size_t ws_bytes, void *stream);
 
 /*
+ * Tokens sorted by expert, without a capacity (no token is dropped), and the way back; K choices a token (1 <= K <= 8).
+ * An assignment v = c * T + t is choice c of token t, idx_k int32[K][T] its expert; an index outside [0, E) is not
+ * routed (the tokens of a padding).  V = K * T.
+ *
+ * locmoe_sort: offsets int32[E + 1], slot int32[K][T], inv int32[V]:
+ *   expert e's rows are [offsets[e], offsets[e + 1]), its assignments in ascending v; slot[v] is the row of v (-1: not
+ *   routed), inv[row] the assignment of a row (-1 for rows from offsets[E] on).
+ * load (NULL to skip) int32[E]: tokens whose first choice is e, as locmoe_aux_loss takes them.  With x and xs (both or none;
+ * x [T][H], xs [V][H] of x_dtype) also the rows, xs[slot[c][t]] = x[t] bit for bit, zeros from offsets[E] on.
+ *
+ * locmoe_sort_grad: its gradient, dxs [V][H], dx [T][H] of x_dtype:
+ *   dx[t] = sum_c dxs[slot[c][t]]                                                      without x
+ * and with x [T][H] the gradient of the router (locmoe_gate, locmoe_topk_select) added:
+ *   dx[t][j] += dG_i / g,  i = j / g,  g = H / E,     dG_i = [G_i > 0] p_i (q_i - sum_j p_j q_j),
+ *   G_i = mean of group i of x[t] + eps_i (eps NULL: 0),  p = softmax(ReLU(G)),  q_i = dp_i + sum_c [idx_k[c][t] = i] dw[c][t]
+ * where dw float[K][T] is the gradient of the chosen scores w_k and dp float[E] that of any token's p_i, the same for all
+ * tokens (alpha n f_i / T for the balance loss); either may be NULL.  deps float[E] (NULL to skip) = sum_t dG, the gradient of
+ * eps.  dxs may be NULL with x.  The rows' sums of groups have to fit shared memory: rows up to 750 KB, or 48000 elements
+ * where a group is no whole number of 16 bytes (LOCMOE_ERR_TOO_LARGE); arrays that are not 16-byte aligned count as such
+ * (LOCMOE_ERR_ALIGN).  ws (only with deps): locmoe_sort_grad_bytes() bytes, 256-byte aligned.
+ *
+ * locmoe_unsort: out[t] = residual[t] + sum_c w_k[c][t] * y[slot[c][t]], y [V][H], out, residual (NULL: 0) [T][H] of x_dtype,
+ * w_k float[K][T] (NULL: 1); choices with slot < 0 have no term.  fp32, in the order of c, rounded once.  out may be residual.
+ *
+ * locmoe_unsort_grad: dout [T][H] gives dy[slot[c][t]] = w_k[c][t] * dout[t] (zeros from offsets[E] on) and
+ * dw[c][t] = <dout[t], y[slot[c][t]]> (0 where slot < 0), float[K][T]; dy or dw may be NULL, y only with dw NULL.
+ *
+ * E <= 1024 (LOCMOE_ERR_TOO_LARGE), V < 2^31.  H % E need only be 0 with the router's gradient.  The shape's node fields and
+ * layout are validated but do not matter.  Pointers aligned to their elements; rows of whole 16-byte vectors in 16-byte
+ * aligned arrays move fastest.  Row indices in slot outside [0, V) count as not routed.  All sums have a fixed order.
+ */
+int locmoe_sort(const locmoe_shape_t *shape, int32_t K, const int32_t *idx_k, const void *x, int32_t *offsets, int32_t *slot,
+                int32_t *inv, int32_t *load, void *xs, void *stream);
+typedef struct {
+    const void *dxs; const int32_t *slot; const void *x; const float *eps; const int32_t *idx_k; const float *dw; const float *dp;
+    void *dx; float *deps;
+} locmoe_sort_grad_t;
+int locmoe_sort_grad_bytes(const locmoe_shape_t *shape, size_t *bytes);
+int locmoe_sort_grad(const locmoe_shape_t *shape, int32_t K, const locmoe_sort_grad_t *g, void *ws, size_t ws_bytes, void *stream);
+int locmoe_unsort(const locmoe_shape_t *shape, int32_t K, const void *y, const int32_t *slot, const float *w_k,
+                  const void *residual, void *out, void *stream);
+int locmoe_unsort_grad(const locmoe_shape_t *shape, int32_t K, const void *dout, const void *y, const int32_t *offsets,
+                       const int32_t *slot, const float *w_k, void *dy, float *dw, void *stream);
+
+/*
+ * The experts' products on rows sorted by expert (locmoe_sort): shape->T rows of shape->H elements, of which expert e has
+ * [offsets[e], offsets[e + 1]), any number of them.  All matrices bf16, fp32 accumulation on the tensor cores (tcgen05):
+ *   z[r] = W_e x[r] + bias_e,   y[r] = act(z[r]) + residual[r]
+ * x [T][H], w [E][N][H], bias float[E][N] (NULL: 0), residual (NULL: 0), y, z (NULL to skip) [T][N]; y is formed from z before
+ * that is rounded.  Rows from offsets[E] on: zeros in y and z.  y may be residual.
+ * act: LOCMOE_ACT_NONE, _RELU, _GELU (erf form), _SILU.
+ *
+ * locmoe_expert_linear_grad: from dy [T][N], the gradient of z,
+ *   dx[r] = (W_e^T dy[r]) * act'(z[r])     [T][H], where z [T][H] (NULL: no factor) is what x = act(z) was made of: the
+ *                                          gradient goes through the activation before this product
+ *   dw_e = sum_r dy[r] x[r]^T              [E][N][H] of dw_dtype (zeros for an expert without rows)
+ *   db_e = sum_r dy[r]                     float[E][N]
+ * dx, dw, db may be NULL; w and z are read for dx, x for dw.  Rows from offsets[E] on: zeros in dx, not in dw and db.
+ *
+ * H and N multiples of 8, below 2^20; E <= 1024, T < 2^31 - 65536 (LOCMOE_ERR_TOO_LARGE); all arrays 16-byte aligned, offsets
+ * 4-byte.  Sums have a fixed order that depends on the offsets and the device: the same call gives the same bits.
+ * ws: locmoe_expert_linear_bytes() bytes (grad != 0 for the gradient), 256-byte aligned, undefined between calls.
+ */
+enum { LOCMOE_ACT_NONE = 0, LOCMOE_ACT_RELU = 1, LOCMOE_ACT_GELU = 2, LOCMOE_ACT_SILU = 3 };
+typedef struct {
+    const void *x; const void *w; const int32_t *offsets; const float *bias; const void *residual;
+    void *y; void *z; int32_t act;
+} locmoe_expert_linear_t;
+typedef struct {
+    const void *dy; const void *x; const void *w; const int32_t *offsets; const void *z;
+    void *dx; void *dw; float *db; int32_t act; int32_t dw_dtype;
+} locmoe_expert_linear_grad_t;
+int locmoe_expert_linear_bytes(const locmoe_shape_t *shape, int32_t N, int32_t grad, size_t *bytes);
+int locmoe_expert_linear(const locmoe_shape_t *shape, int32_t N, const locmoe_expert_linear_t *l, void *ws, size_t ws_bytes,
+                         void *stream);
+int locmoe_expert_linear_grad(const locmoe_shape_t *shape, int32_t N, const locmoe_expert_linear_grad_t *l, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/*
  * Host-side helpers of the capacity rule and the buffer layout: plain arithmetic
  * on host memory, nothing is launched.
  *
@@ -612,7 +691,7 @@ int locmoe_launch_counts(const locmoe_shape_t *shape, int32_t counts[5]);
  * memory after waiting for the stream: bit 0 is set if a kernel gave up a
  * bounded wait for one of its own asynchronous copies (its output is then
  * incomplete); bit 1 the same for the expert-FFN kernels, bit 2 for those of locmoe_moe_few, bit 3 for the
- * block norms'.  0 in normal operation.
+ * block norms', bit 4 for the experts' products on sorted rows.  0 in normal operation.
  * The paper has no counterpart. */
 int locmoe_device_flags(int32_t *flags_host, void *stream);
 

@@ -20,13 +20,15 @@ LAYOUT_SEND, LAYOUT_RECV = 0, 1
 BOUND_BETA, BOUND_ERFC, BOUND_EXP = 0, 1, 2
 ROUTE_EARLY_INIT = 1
 FEW_MAX_TOKENS, FEW_UNWEIGHTED = 128, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 WARN_CLAMPED, WARN_BAD_SRC, WARN_BAD_IDX = 1, 2, 4
 FLAG_DELTA_OVERRIDE, FLAG_MIN_SATURATED, FLAG_MIN_BINDS = 1, 2, 4
 
 EXPORTS = [
     "locmoe_workspace_bytes", "locmoe_gate", "locmoe_gate_ex", "locmoe_aux_loss_partial", "locmoe_capacity", "locmoe_capacity_noalloc", "locmoe_capacity_read", "locmoe_route", "locmoe_capacity_route", "locmoe_gate_route",
     "locmoe_conventional_capacity", "locmoe_batch_delta", "locmoe_dest_order",
-    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_moe_few_bytes", "locmoe_moe_few", "locmoe_block_norm", "locmoe_block_norm_grad_bytes", "locmoe_block_norm_grad", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
+    "locmoe_dispatch", "locmoe_combine", "locmoe_dispatch_peer", "locmoe_dispatch_peer_window", "locmoe_combine_peer", "locmoe_topk_select", "locmoe_topk_fold", "locmoe_combine_topk", "locmoe_expert_ffn", "locmoe_ffn_kernels", "locmoe_moe_layer", "locmoe_aux_loss", "locmoe_loc_loss", "locmoe_cos_hist", "locmoe_moe_few_bytes", "locmoe_moe_few", "locmoe_block_norm", "locmoe_block_norm_grad_bytes", "locmoe_block_norm_grad",
+    "locmoe_sort", "locmoe_sort_grad_bytes", "locmoe_sort_grad", "locmoe_unsort", "locmoe_unsort_grad", "locmoe_expert_linear_bytes", "locmoe_expert_linear", "locmoe_expert_linear_grad", "locmoe_launch_counts", "locmoe_device_flags", "locmoe_status_string",
 ]
 
 
@@ -78,6 +80,18 @@ class BlockNormGrad(C.Structure):
                [(n, C.c_void_p) for n in ("dh", "dy", "dgate", "dw_post", "dw_pre")]
 
 
+class SortGrad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dxs", "slot", "x", "eps", "idx_k", "dw", "dp", "dx", "deps")]
+
+
+class ExpertLinear(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "w", "offsets", "bias", "residual", "y", "z")] + [("act", C.c_int32)]
+
+
+class ExpertLinearGrad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dy", "x", "w", "offsets", "z", "dx", "dw", "db")] + [("act", C.c_int32), ("dw_dtype", C.c_int32)]
+
+
 CAPACITY_BYTES = C.sizeof(Capacity)
 
 
@@ -124,6 +138,14 @@ def _load() -> C.CDLL:
     lib.locmoe_block_norm.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNorm), vp]
     lib.locmoe_block_norm_grad_bytes.argtypes = [C.POINTER(Shape), C.POINTER(C.c_size_t)]
     lib.locmoe_block_norm_grad.argtypes = [C.POINTER(Shape), i32, C.POINTER(BlockNormGrad), vp, C.c_size_t, vp]
+    lib.locmoe_sort.argtypes = [C.POINTER(Shape), i32] + [vp] * 8
+    lib.locmoe_sort_grad_bytes.argtypes = [C.POINTER(Shape), C.POINTER(C.c_size_t)]
+    lib.locmoe_sort_grad.argtypes = [C.POINTER(Shape), i32, C.POINTER(SortGrad), vp, C.c_size_t, vp]
+    lib.locmoe_unsort.argtypes = [C.POINTER(Shape), i32] + [vp] * 6
+    lib.locmoe_unsort_grad.argtypes = [C.POINTER(Shape), i32] + [vp] * 8
+    lib.locmoe_expert_linear_bytes.argtypes = [C.POINTER(Shape), i32, i32, C.POINTER(C.c_size_t)]
+    lib.locmoe_expert_linear.argtypes = [C.POINTER(Shape), i32, C.POINTER(ExpertLinear), vp, C.c_size_t, vp]
+    lib.locmoe_expert_linear_grad.argtypes = [C.POINTER(Shape), i32, C.POINTER(ExpertLinearGrad), vp, C.c_size_t, vp]
     lib.locmoe_conventional_capacity.argtypes = [C.POINTER(Shape), C.POINTER(CapacityRule), C.POINTER(C.c_int32)]
     lib.locmoe_batch_delta.argtypes = [vp, i32, C.POINTER(C.c_double)]
     lib.locmoe_dest_order.argtypes = [C.POINTER(Shape), i32, i32]
@@ -567,6 +589,74 @@ def locmoe_block_norm_grad(shape: Shape, C_alloc, dh_out=None, dn=None, h_out=No
         _arg(dw_post, f32, H, "dw_post", dev), _arg(dw_pre, f32, H, "dw_pre", dev))
     return _check("locmoe_block_norm_grad", _lib.locmoe_block_norm_grad(
         C.byref(shape), C_alloc, C.byref(b), _arg(ws, torch.uint8, 0, "ws", dev), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def locmoe_sort(shape: Shape, K, idx_k, offsets, slot, inv, load=None, x=None, xs=None, stream=None) -> int:
+    """Order of the K * T assignments by expert and, with ``x``, the rows in it."""
+    dt, i32, V, dev = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.int32, K * shape.T, _device()
+    return _check("locmoe_sort", _lib.locmoe_sort(
+        C.byref(shape), K, _arg(idx_k, i32, V, "idx_k", dev), _arg(x, dt, shape.T * shape.H, "x", dev), _arg(offsets, i32, shape.E + 1, "offsets", dev),
+        _arg(slot, i32, V, "slot", dev), _arg(inv, i32, V, "inv", dev), _arg(load, i32, shape.E, "load", dev), _arg(xs, dt, V * shape.H, "xs", dev),
+        _stream(stream)))
+
+
+def locmoe_sort_grad_bytes(shape: Shape) -> int:
+    out = C.c_size_t(0)
+    _check("locmoe_sort_grad_bytes", _lib.locmoe_sort_grad_bytes(C.byref(shape), C.byref(out)))
+    return out.value
+
+
+def locmoe_sort_grad(shape: Shape, K, slot, dx, dxs=None, x=None, eps=None, idx_k=None, dw=None, dp=None, deps=None, ws=None, stream=None) -> int:
+    """Gradient of the sorted rows towards the tokens and, with ``x``, the router's."""
+    dt, f32, i32, T, V, dev = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.int32, shape.T, K * shape.T, _device()
+    g = SortGrad(_arg(dxs, dt, V * shape.H, "dxs", dev), _arg(slot, i32, V, "slot", dev), _arg(x, dt, T * shape.H, "x", dev), _arg(eps, f32, shape.E, "eps", dev),
+                 _arg(idx_k, i32, V, "idx_k", dev), _arg(dw, f32, V, "dw", dev), _arg(dp, f32, shape.E, "dp", dev), _arg(dx, dt, T * shape.H, "dx", dev),
+                 _arg(deps, f32, shape.E, "deps", dev))
+    return _check("locmoe_sort_grad", _lib.locmoe_sort_grad(C.byref(shape), K, C.byref(g), _arg(ws, torch.uint8, 0, "ws", dev),
+                                                            0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def locmoe_unsort(shape: Shape, K, y, slot, out, w_k=None, residual=None, stream=None) -> int:
+    """Weighted sum of each token's rows, back in token order."""
+    dt, T, V, dev = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, shape.T, K * shape.T, _device()
+    return _check("locmoe_unsort", _lib.locmoe_unsort(
+        C.byref(shape), K, _arg(y, dt, V * shape.H, "y", dev), _arg(slot, torch.int32, V, "slot", dev), _arg(w_k, torch.float32, V, "w_k", dev),
+        _arg(residual, dt, T * shape.H, "residual", dev), _arg(out, dt, T * shape.H, "out", dev), _stream(stream)))
+
+
+def locmoe_unsort_grad(shape: Shape, K, dout, offsets, slot, y=None, w_k=None, dy=None, dw=None, stream=None) -> int:
+    """Gradient of locmoe_unsort towards the rows and the weights."""
+    dt, f32, i32, T, V, dev = torch.float32 if shape.x_dtype == F32 else torch.bfloat16, torch.float32, torch.int32, shape.T, K * shape.T, _device()
+    return _check("locmoe_unsort_grad", _lib.locmoe_unsort_grad(
+        C.byref(shape), K, _arg(dout, dt, T * shape.H, "dout", dev), _arg(y, dt, V * shape.H, "y", dev), _arg(offsets, i32, shape.E + 1, "offsets", dev),
+        _arg(slot, i32, V, "slot", dev), _arg(w_k, f32, V, "w_k", dev), _arg(dy, dt, V * shape.H, "dy", dev), _arg(dw, f32, V, "dw", dev), _stream(stream)))
+
+
+def locmoe_expert_linear_bytes(shape: Shape, N, grad=False) -> int:
+    out = C.c_size_t(0)
+    _check("locmoe_expert_linear_bytes", _lib.locmoe_expert_linear_bytes(C.byref(shape), N, 1 if grad else 0, C.byref(out)))
+    return out.value
+
+
+def locmoe_expert_linear(shape: Shape, N, x, w, offsets, y, ws, bias=None, residual=None, z=None, act=ACT_NONE, stream=None) -> int:
+    """The experts' products on sorted rows with bias, activation and residual."""
+    bf, R, H, E, dev = torch.bfloat16, shape.T, shape.H, shape.E, _device()
+    l = ExpertLinear(_arg(x, bf, R * H, "x", dev), _arg(w, bf, E * N * H, "w", dev), _arg(offsets, torch.int32, E + 1, "offsets", dev),
+                     _arg(bias, torch.float32, E * N, "bias", dev), _arg(residual, bf, R * N, "residual", dev), _arg(y, bf, R * N, "y", dev),
+                     _arg(z, bf, R * N, "z", dev), act)
+    return _check("locmoe_expert_linear", _lib.locmoe_expert_linear(C.byref(shape), N, C.byref(l), _arg(ws, torch.uint8, 0, "ws", dev), ws.numel(),
+                                                                    _stream(stream)))
+
+
+def locmoe_expert_linear_grad(shape: Shape, N, dy, offsets, x=None, w=None, z=None, dx=None, dw=None, db=None, act=ACT_NONE, ws=None, stream=None) -> int:
+    """Gradient of locmoe_expert_linear's products towards the rows, the weights and the bias."""
+    bf, R, H, E, dev = torch.bfloat16, shape.T, shape.H, shape.E, _device()
+    dwt = bf if dw is None or dw.dtype is not torch.float32 else torch.float32
+    l = ExpertLinearGrad(_arg(dy, bf, R * N, "dy", dev), _arg(x, bf, R * H, "x", dev), _arg(w, bf, E * N * H, "w", dev),
+                         _arg(offsets, torch.int32, E + 1, "offsets", dev), _arg(z, bf, R * H, "z", dev), _arg(dx, bf, R * H, "dx", dev),
+                         _arg(dw, dwt, E * N * H, "dw", dev), _arg(db, torch.float32, E * N, "db", dev), act, F32 if dwt is torch.float32 else BF16)
+    return _check("locmoe_expert_linear_grad", _lib.locmoe_expert_linear_grad(
+        C.byref(shape), N, C.byref(l), _arg(ws, torch.uint8, 0, "ws", dev), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def conventional_capacity(T: int, D: int, E: int, capacity_factor: float) -> int:

@@ -512,6 +512,130 @@ int locmoe_block_norm_grad(const locmoe_shape_t* shape, int32_t C_alloc, const l
     return launch_block_norm_grad(*shape, rows, *b, ws, static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+// Calls on sorted tokens: H is a multiple of E only where the router's groups are meant.
+int check_sorted(const locmoe_shape_t* s, int32_t K, bool groups) {
+    if (!s) return LOCMOE_ERR_NULL;
+    locmoe_shape_t t = *s;
+    if (!groups && t.E > 0) t.H = t.H < 1 ? 0 : t.E;      // any H will do
+    const int rc = check_shape(&t);
+    if (rc) return rc;
+    if (K < 1 || K > 8) return LOCMOE_ERR_SHAPE;
+    if (s->E > 1024 || (long long)K * s->T > 0x7fffffffll) return LOCMOE_ERR_TOO_LARGE;
+    return LOCMOE_OK;
+}
+
+int check_linear(const locmoe_shape_t* s, int32_t N) {
+    const int rc = check_sorted(s, 1, false);
+    if (rc) return rc;
+    if (s->x_dtype != LOCMOE_BF16) return LOCMOE_ERR_DTYPE;
+    if (N < 8 || N % 8 != 0 || s->H % 8 != 0) return LOCMOE_ERR_SHAPE;
+    if (N >= (1 << 20) || s->H >= (1 << 20) || s->T >= 0x7fffffff - 65535) return LOCMOE_ERR_TOO_LARGE;
+    return LOCMOE_OK;
+}
+}  // namespace
+
+int locmoe_sort(const locmoe_shape_t* shape, int32_t K, const int32_t* idx_k, const void* x, int32_t* offsets, int32_t* slot,
+                int32_t* inv, int32_t* load, void* xs, void* stream) {
+    int rc = check_sorted(shape, K, false);
+    if (rc) return rc;
+    if (!idx_k || !offsets || !slot || !inv || !x != !xs) return LOCMOE_ERR_NULL;
+    for (const void* p : {(const void*)idx_k, (const void*)offsets, (const void*)slot, (const void*)inv, (const void*)load})
+        if (!element_aligned(p, 4)) return LOCMOE_ERR_ALIGN;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    if (!element_aligned(x, esz) || !element_aligned(xs, esz)) return LOCMOE_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    rc = launch_sort_plan(shape->T, K, shape->E, idx_k, offsets, slot, inv, load, st);
+    if (rc == LOCMOE_OK && x) rc = launch_sort_rows(*shape, K, x, offsets, slot, xs, st);
+    return rc;
+}
+
+int locmoe_sort_grad_bytes(const locmoe_shape_t* shape, size_t* bytes) {
+    int rc = check_sorted(shape, 1, true);
+    if (rc) return rc;
+    if (!bytes) return LOCMOE_ERR_NULL;
+    *bytes = sort_grad_ws_bytes(*shape);
+    return LOCMOE_OK;
+}
+
+int locmoe_sort_grad(const locmoe_shape_t* shape, int32_t K, const locmoe_sort_grad_t* g, void* ws, size_t ws_bytes, void* stream) {
+    if (!g) return LOCMOE_ERR_NULL;
+    int rc = check_sorted(shape, K, g->x != nullptr);
+    if (rc) return rc;
+    if (!g->slot || !g->dx || (!g->dxs && !g->x)) return LOCMOE_ERR_NULL;
+    if (!g->x && (g->eps || g->dw || g->dp || g->deps)) return LOCMOE_ERR_NULL;
+    if (g->dw && !g->idx_k) return LOCMOE_ERR_NULL;
+    if (g->x && !sort_grad_fits(*shape)) return LOCMOE_ERR_TOO_LARGE;
+    if (g->deps && (!ws || ws_bytes < sort_grad_ws_bytes(*shape) || (uintptr_t)ws % 256)) return LOCMOE_ERR_WORKSPACE;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    for (const void* p : {g->dxs, g->x, (const void*)g->dx})
+        if (!element_aligned(p, esz)) return LOCMOE_ERR_ALIGN;
+    for (const void* p : {(const void*)g->slot, (const void*)g->eps, (const void*)g->idx_k, (const void*)g->dw, (const void*)g->dp,
+                          (const void*)g->deps})
+        if (!element_aligned(p, 4)) return LOCMOE_ERR_ALIGN;
+    return launch_sort_grad(*shape, K, *g, ws, static_cast<cudaStream_t>(stream));
+}
+
+int locmoe_unsort(const locmoe_shape_t* shape, int32_t K, const void* y, const int32_t* slot, const float* w_k,
+                  const void* residual, void* out, void* stream) {
+    int rc = check_sorted(shape, K, false);
+    if (rc) return rc;
+    if (!y || !slot || !out) return LOCMOE_ERR_NULL;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    for (const void* p : {y, residual, (const void*)out})
+        if (!element_aligned(p, esz)) return LOCMOE_ERR_ALIGN;
+    if (!element_aligned(slot, 4) || !element_aligned(w_k, 4)) return LOCMOE_ERR_ALIGN;
+    return launch_unsort_rows(*shape, K, y, slot, w_k, residual, out, static_cast<cudaStream_t>(stream));
+}
+
+int locmoe_unsort_grad(const locmoe_shape_t* shape, int32_t K, const void* dout, const void* y, const int32_t* offsets,
+                       const int32_t* slot, const float* w_k, void* dy, float* dw, void* stream) {
+    int rc = check_sorted(shape, K, false);
+    if (rc) return rc;
+    if (!dout || !offsets || !slot || (!dy && !dw) || (dw && !y)) return LOCMOE_ERR_NULL;
+    const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
+    for (const void* p : {dout, y, (const void*)dy})
+        if (!element_aligned(p, esz)) return LOCMOE_ERR_ALIGN;
+    for (const void* p : {(const void*)offsets, (const void*)slot, (const void*)w_k, (const void*)dw})
+        if (!element_aligned(p, 4)) return LOCMOE_ERR_ALIGN;
+    return launch_unsort_grad(*shape, K, dout, y, offsets, slot, w_k, dy, dw, static_cast<cudaStream_t>(stream));
+}
+
+int locmoe_expert_linear_bytes(const locmoe_shape_t* shape, int32_t N, int32_t grad, size_t* bytes) {
+    int rc = check_linear(shape, N);
+    if (rc) return rc;
+    if (!bytes) return LOCMOE_ERR_NULL;
+    *bytes = expert_linear_ws_bytes(*shape, grad);
+    return LOCMOE_OK;
+}
+
+int locmoe_expert_linear(const locmoe_shape_t* shape, int32_t N, const locmoe_expert_linear_t* l, void* ws, size_t ws_bytes,
+                         void* stream) {
+    int rc = check_linear(shape, N);
+    if (rc) return rc;
+    if (!l || !l->x || !l->w || !l->offsets || !l->y) return LOCMOE_ERR_NULL;
+    if (l->act < LOCMOE_ACT_NONE || l->act > LOCMOE_ACT_SILU) return LOCMOE_ERR_DTYPE;
+    for (const void* p : {l->x, l->w, (const void*)l->bias, l->residual, (const void*)l->y, (const void*)l->z})
+        if (!element_aligned(p, 16)) return LOCMOE_ERR_ALIGN;
+    if (!element_aligned(l->offsets, 4)) return LOCMOE_ERR_ALIGN;
+    if (!ws || ws_bytes < expert_linear_ws_bytes(*shape, 0) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;
+    return launch_expert_linear(*shape, N, *l, ws, static_cast<cudaStream_t>(stream));
+}
+
+int locmoe_expert_linear_grad(const locmoe_shape_t* shape, int32_t N, const locmoe_expert_linear_grad_t* l, void* ws,
+                              size_t ws_bytes, void* stream) {
+    int rc = check_linear(shape, N);
+    if (rc) return rc;
+    if (!l || !l->dy || !l->offsets || (!l->dx && !l->dw && !l->db)) return LOCMOE_ERR_NULL;
+    if ((l->dx && !l->w) || (l->dw && !l->x)) return LOCMOE_ERR_NULL;
+    if (l->act < LOCMOE_ACT_NONE || l->act > LOCMOE_ACT_SILU || (l->dw_dtype != LOCMOE_F32 && l->dw_dtype != LOCMOE_BF16)) return LOCMOE_ERR_DTYPE;
+    for (const void* p : {l->dy, l->x, l->w, l->z, (const void*)l->dx, (const void*)l->dw, (const void*)l->db})
+        if (!element_aligned(p, 16)) return LOCMOE_ERR_ALIGN;
+    if (!element_aligned(l->offsets, 4)) return LOCMOE_ERR_ALIGN;
+    if ((l->dx || l->dw) && (!ws || ws_bytes < expert_linear_ws_bytes(*shape, 1) || (uintptr_t)ws % 256)) return LOCMOE_ERR_WORKSPACE;
+    return launch_expert_linear_grad(*shape, N, *l, ws, static_cast<cudaStream_t>(stream));
+}
+
 int locmoe_conventional_capacity(const locmoe_shape_t* shape, const locmoe_capacity_rule_t* rule, int32_t* C_alloc) {
     int rc = check_shape(shape);
     if (rc) return rc;
@@ -569,12 +693,13 @@ int locmoe_launch_counts(const locmoe_shape_t* shape, int32_t counts[5]) {
 
 int locmoe_device_flags(int32_t* flags_host, void* stream) {
     if (!flags_host) return LOCMOE_ERR_NULL;
-    int v = 0, f = 0, few = 0, norm = 0;
+    int v = 0, f = 0, few = 0, norm = 0, linear = 0;
     int rc = read_device_flags(&v, static_cast<cudaStream_t>(stream));
     if (rc == LOCMOE_OK) rc = read_ffn_flags(&f, static_cast<cudaStream_t>(stream));
     if (rc == LOCMOE_OK) rc = read_few_flags(&few, static_cast<cudaStream_t>(stream));
     if (rc == LOCMOE_OK) rc = read_norm_flags(&norm, static_cast<cudaStream_t>(stream));
-    *flags_host = v | (f << 1) | (few << 2) | (norm << 3);
+    if (rc == LOCMOE_OK) rc = read_linear_flags(&linear, static_cast<cudaStream_t>(stream));
+    *flags_host = v | (f << 1) | (few << 2) | (norm << 3) | (linear << 4);
     return rc;
 }
 

@@ -134,6 +134,20 @@ size_t block_norm_grad_ws_bytes(const locmoe_shape_t& s);
 int launch_block_norm(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_t& b, cudaStream_t st);
 int launch_block_norm_grad(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_grad_t& b, void* ws, cudaStream_t st);
 
+int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load, cudaStream_t st);
+int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st);
+int launch_unsort_rows(const locmoe_shape_t& s, int K, const void* y, const int32_t* slot, const float* w, const void* residual, void* out,
+                       cudaStream_t st);
+int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot,
+                       const float* w, void* dy, float* dw, cudaStream_t st);
+bool sort_grad_fits(const locmoe_shape_t& s);
+size_t sort_grad_ws_bytes(const locmoe_shape_t& s);
+int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g, void* ws, cudaStream_t st);
+size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad);
+int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_linear_t& l, void* ws, cudaStream_t st);
+int launch_expert_linear_grad(const locmoe_shape_t& s, int N, const locmoe_expert_linear_grad_t& l, void* ws, cudaStream_t st);
+int read_linear_flags(int* out, cudaStream_t st);
+
 // Copies the device diagnostics word to host memory (synchronises the stream).
 int read_device_flags(int* out, cudaStream_t st);
 

@@ -1,0 +1,605 @@
+// The experts' products on rows sorted by expert: group e is the rows [offsets[e], offsets[e + 1]), of any length.
+//   forward   y[r]  = act(x[r] W_e^T + b_e) + residual[r]            W_e [N][K]
+//   towards x dx[r] = (dy[r] W_e) * act'(z[r])                       W_e [K][N] here: the reduction runs over its rows
+//   weights   dW_e  = dy_e^T x_e,  db_e = sum of dy_e's rows         the reduction runs over the group's rows
+// One GEMM kernel on the tensor cores (tcgen05, bf16 operands, fp32 accumulators in TMEM) serves all three: 128 x 256 output
+// tiles, operands by TMA into a ring of four stages of 64 along the reduction, two accumulators so that a tile's epilogue runs
+// beside the next tile's products.  An operand whose rows run along the reduction is K-major, else MN-major: the same TMA
+// boxes of 64 elements x rows, the matrix descriptor says which way they lie, so nothing is transposed in memory.
+// Warp 0 loads, warp 1 issues the products, warps 2..9 drain the accumulators (a row a lane, half of the columns a warp).
+//
+// A group may begin and end inside a tile.  Forward and towards x that only means rows which are not stored; over the group's
+// rows (weights) the last block of the reduction holds rows of the next group, and those are overwritten with zeros in shared
+// memory, in both operands, since a zero in one does not undo an infinity in the other.
+//
+// Work is dealt by tiles (tile i to CTA i modulo the grid), neighbours in time sharing operands in L2, or, where the tiles do
+// not fill many waves, by equal runs of 64-blocks of the reduction, so that every SM gets the same share whatever the
+// groups are.  A tile that a run begins or ends in leaves fp32 sums in the workspace, which a second kernel adds in order.
+#include <cuda.h>
+#include <stdlib.h>
+
+#include "common.cuh"
+#include "tensor_map.cuh"
+#include "umma.cuh"
+
+namespace locmoe {
+
+namespace {
+
+constexpr int BM = 128, BN = 256, BK = 64, NSTAGE = 4, UMMA_K = 16;
+constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr uint32_t CHUNK_BYTES = 64 * BK * 2;       // 64 columns of an MN-major tile
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr uint32_t TMEM_COLS = 512;
+constexpr int kMaxE = 1024;
+constexpr size_t kSmem = 1024 /*alignment slack*/ + (size_t)NSTAGE * STAGE_BYTES + 256 /*barriers*/ + (kMaxE + 1) * sizeof(int);
+
+__device__ int g_linear_flags = 0;   // bit 0: a bounded wait gave up
+
+enum Kind { kForward = 0, kTowardsX = 1, kWeights = 2 };
+
+struct LinearArgs {
+    const int32_t* offsets;     // [E + 1]
+    void* out;                  // bf16 [R][N], or the weights' gradient [E][M][N], bf16 or fp32
+    void* z_out;                // bf16 [R][N] or nullptr
+    const float* bias;          // [E][N] or nullptr
+    const void* residual;       // bf16 [R][N] or nullptr
+    const void* z_in;           // bf16 [R][N]: multiply by act'(z_in); nullptr: no factor
+    float* part;                // [grid][2][part_rows][BN]
+    int act, out_f32;
+    int E, R, M, N, K;          // M: rows of a weight (weights only)
+    int n_tiles, a_rows;        // rows of one A box
+    int part_rows;
+    int grid, deal_waves;       // runs instead of tiles up to this many waves of tiles
+};
+
+__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_word) {
+    for (uint32_t i = 0; i < (1u << 22); ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 63u) == 63u && *abort_word) return false;
+    }
+    *abort_word = 1;
+    atomicOr(&g_linear_flags, 1);
+    return false;
+}
+
+// The same for a warp that stays together: all lanes get one answer.
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_word) {
+    return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_word));
+}
+
+// Group e's rows, whatever the offsets hold: inside [0, R) and not negative in number.
+struct Group { int lo, n; };
+__device__ __forceinline__ Group group_of(const int* offsets, int e, int R) {
+    const int lo = min(max(offsets[e], 0), R);
+    return {lo, max(min(offsets[e + 1], R) - lo, 0)};
+}
+
+// The list of work: the groups' tiles in order, a tile being `kb` blocks of the reduction.
+template <int KIND>
+struct Tiles {
+    const LinearArgs& a;
+    const int* offsets;
+    __device__ __forceinline__ int kblocks(const Group& g) const { return KIND == kWeights ? (g.n + BK - 1) / BK : (a.K + BK - 1) / BK; }
+    __device__ __forceinline__ int m_tiles(const Group& g) const { return KIND == kWeights ? (a.M + BM - 1) / BM : (g.n + BM - 1) / BM; }
+    __device__ __forceinline__ int tiles(const Group& g) const { return g.n > 0 ? m_tiles(g) * a.n_tiles : 0; }
+};
+
+struct Totals { long long tiles, units; };
+// Sums over the groups by one warp (all lanes get them).
+template <int KIND>
+__device__ __forceinline__ Totals totals(const LinearArgs& a, const int* offsets, int lane) {
+    const Tiles<KIND> t{a, offsets};
+    long long n = 0, u = 0;
+    for (int e = lane; e < a.E; e += 32) {
+        const Group g = group_of(offsets, e, a.R);
+        const long long k = t.tiles(g);
+        n += k;
+        u += k * t.kblocks(g);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        n += __shfl_xor_sync(0xffffffffu, n, o);
+        u += __shfl_xor_sync(0xffffffffu, u, o);
+    }
+    return {n, u};
+}
+
+// How the work is dealt; the same on every CTA and in the kernel that joins.  `runs` = 0: by tiles, else the number of runs.
+// A run has at least four blocks, so that its sums are worth their way through memory.
+__device__ __forceinline__ int deal(const LinearArgs& a, const Totals& s) {
+    if (s.tiles > (long long)a.deal_waves * a.grid || s.units == 0) return 0;
+    const long long r = s.units / 4;
+    return r < 1 ? 1 : r < a.grid ? (int)r : a.grid;
+}
+__device__ __forceinline__ long long run_begin(const Totals& s, int runs, int c) { return s.units * c / runs; }
+
+struct Item {
+    int e, lo, n;               // group, its first row, its rows
+    int mt, nt;                 // tile
+    int kb0, kb1, kb;           // blocks of this item, blocks of the tile
+};
+
+// Walks through one CTA's share.
+template <int KIND>
+struct Cursor {
+    const LinearArgs& a;
+    const int* offsets;
+    int runs;
+    long long at, end;          // tile (by tiles) or block (by runs)
+    int e;
+    long long base;             // first tile or block of group e
+    Group g;
+    int kb, per;                // blocks a tile, tiles of group e
+    __device__ __forceinline__ Cursor(const LinearArgs& a_, const int* off, const Totals& s, int runs_, int c) : a(a_), offsets(off), runs(runs_), e(-1), base(0) {
+        g = Group{0, 0};
+        kb = per = 0;
+        if (runs) { at = c < runs ? run_begin(s, runs, c) : 0; end = c < runs ? run_begin(s, runs, c + 1) : 0; }
+        else { at = c; end = s.tiles; }
+    }
+    __device__ __forceinline__ bool next(Item& it) {
+        if (at >= end) return false;
+        const Tiles<KIND> t{a, offsets};
+        while (true) {
+            const long long size = runs ? (long long)per * kb : per;
+            if (e >= 0 && at < base + size) break;
+            base += size;
+            if (++e >= a.E) return false;
+            g = group_of(offsets, e, a.R);
+            kb = t.kblocks(g);
+            per = t.tiles(g);
+        }
+        int tile;
+        it.kb = kb;
+        if (runs) {
+            const long long rel = at - base;
+            tile = (int)(rel / kb);
+            it.kb0 = (int)(rel - (long long)tile * kb);
+            const long long left = end - at;
+            it.kb1 = left < kb - it.kb0 ? it.kb0 + (int)left : kb;
+            at += it.kb1 - it.kb0;
+        } else {
+            tile = (int)(at - base);
+            it.kb0 = 0;
+            it.kb1 = kb;
+            at += a.grid;
+        }
+        it.e = e; it.lo = g.lo; it.n = g.n;
+        const int mts = t.m_tiles(g);
+        it.nt = tile / mts;             // tiles that share a weight tile are neighbours
+        it.mt = tile - it.nt * mts;
+        return true;
+    }
+};
+
+// Descriptor of an MN-major bf16 tile with 128-byte swizzle, as TMA boxes of 64 elements x 64 rows leave it: a row of 128
+// bytes is 64 elements at one step of the reduction, 8 steps are 1024 bytes (stride byte offset), the next 64 elements
+// follow a box later (leading byte offset).  16 steps further is 2048 bytes.
+__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr) {
+    return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | ((uint64_t)(CHUNK_BYTES >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+// bf16 x bf16 -> fp32, 128 x 256; bits 15 and 16: A, B are MN-major.
+__host__ __device__ constexpr uint32_t idesc(bool a_mn, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+}
+__device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(id), "r"(accumulate) : "memory");
+}
+
+// ---- epilogue arithmetic on pairs ----
+__device__ __forceinline__ float2 act2(float2 v, int act) {
+    if (act == LOCMOE_ACT_GELU) return gelu_erf2(v);
+    if (act == LOCMOE_ACT_SILU) return silu2(v);
+    if (act == LOCMOE_ACT_RELU) return make_float2(v.x < 0.0f ? 0.0f : v.x, v.y < 0.0f ? 0.0f : v.y);
+    return v;
+}
+__device__ __forceinline__ float2 slope2(float2 z, int act) {
+    if (act == LOCMOE_ACT_GELU) return gelu_erf_slope2(z);
+    if (act == LOCMOE_ACT_SILU) return silu_slope2(z);
+    return make_float2(z.x > 0.0f ? 1.0f : 0.0f, z.y > 0.0f ? 1.0f : 0.0f);    // ReLU
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
+
+// Eight sums of one row become outputs; `o` is the first's index in the [R][N] arrays, `col` its column.
+__device__ __forceinline__ void finish8(const LinearArgs& a, int e, size_t o, int col, float2 (&v)[4]) {
+    if (a.bias) {
+        const float4* b = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + col);
+        const float4 b0 = __ldg(b), b1 = __ldg(b + 1);
+        v[0].x += b0.x; v[0].y += b0.y; v[1].x += b0.z; v[1].y += b0.w;
+        v[2].x += b1.x; v[2].y += b1.y; v[3].x += b1.z; v[3].y += b1.w;
+    }
+    if (a.z_out)
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
+    if (a.z_in) {
+        const uint4 z = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.z_in) + o));
+        v[0] = __fmul2_rn(v[0], slope2(unpack2(z.x), a.act)); v[1] = __fmul2_rn(v[1], slope2(unpack2(z.y), a.act));
+        v[2] = __fmul2_rn(v[2], slope2(unpack2(z.z), a.act)); v[3] = __fmul2_rn(v[3], slope2(unpack2(z.w), a.act));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act2(v[i], a.act);
+    }
+    if (a.residual) {
+        const uint4 z = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.residual) + o));
+        const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = unpack2(w[i]); v[i].x += f.x; v[i].y += f.y; }
+    }
+}
+__device__ __forceinline__ void store8(const LinearArgs& a, size_t o, const float2 (&v)[4]) {
+    if (a.out_f32) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.out) + o);
+        p[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+        p[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + o) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
+    }
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(kThreads, 1)
+expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs a) {
+    constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
+    constexpr uint32_t kIdesc = idesc(A_MN, B_MN);
+    extern __shared__ unsigned char smraw[];
+    unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(base + (size_t)NSTAGE * STAGE_BYTES);
+    uint64_t* full = bars;                   // [NSTAGE] operands landed
+    uint64_t* empty = bars + NSTAGE;         // [NSTAGE] products that read the stage are done
+    uint64_t* acc_full = bars + 2 * NSTAGE;  // [2] accumulator complete
+    uint64_t* acc_empty = acc_full + 2;      // [2] accumulator drained
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+    volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    int* offsets = reinterpret_cast<int*>(base + (size_t)NSTAGE * STAGE_BYTES + 256);   // [E + 1]
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NSTAGE; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], kEpiWarps); }
+        *abort_word = 0;
+        mbar_init_fence();
+        prefetch_map(&tmA);
+        prefetch_map(&tmB);
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    pdl_trigger();
+    for (int i = threadIdx.x; i <= a.E; i += kThreads) offsets[i] = __ldg(a.offsets + i);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    const Totals sum = totals<KIND>(a, offsets, lane);
+    const int runs = deal(a, sum);
+    Cursor<KIND> cur(a, offsets, sum, runs, blockIdx.x);
+    Item it;
+
+    if (warp == 0) {
+        if (lane == 0) {  // ---- loads ----
+            int stage = 0; uint32_t phase = 0;
+            const uint32_t bytes = (A_MN ? A_BYTES : (uint32_t)a.a_rows * BK * 2) + B_BYTES;
+            bool ok = true;
+            while (ok && cur.next(it)) {
+                const int m0 = it.mt * BM, n0 = it.nt * BN;
+                for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                    if (!wait_or_abort(&empty[stage], phase ^ 1u, abort_word)) { ok = false; break; }
+                    unsigned char* sa = base + (size_t)stage * STAGE_BYTES;
+                    unsigned char* sb = sa + A_BYTES;
+                    mbar_expect_tx(&full[stage], bytes);
+                    if (A_MN) {
+#pragma unroll
+                        for (int c = 0; c < BM / 64; ++c) tma_load_2d(sa + c * CHUNK_BYTES, &tmA, m0 + 64 * c, it.lo + kb * BK, &full[stage]);
+                    } else {
+                        tma_load_2d(sa, &tmA, kb * BK, it.lo + m0, &full[stage]);
+                    }
+                    if (KIND == kForward) {
+                        tma_load_3d(sb, &tmB, kb * BK, n0, it.e, &full[stage]);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < BN / 64; ++c) {
+                            if (KIND == kWeights) tma_load_2d(sb + c * CHUNK_BYTES, &tmB, n0 + 64 * c, it.lo + kb * BK, &full[stage]);
+                            else tma_load_3d(sb + c * CHUNK_BYTES, &tmB, n0 + 64 * c, kb * BK, it.e, &full[stage]);
+                        }
+                    }
+                    if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
+                }
+            }
+            // tail: all asynchronous commits to this CTA's stage barriers have arrived before the CTA leaves
+            for (int i = 0; i < NSTAGE; ++i) {
+                if (!wait_or_abort(&empty[stage], phase ^ 1u, abort_word)) break;
+                if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {  // ---- products: the whole warp keeps step, lane 0 issues ----
+        int stage = 0; uint32_t phase = 0;
+        int acc = 0; uint32_t acc_phase = 0;
+        bool ok = true;
+        while (ok && cur.next(it)) {
+            if (!wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_word)) break;
+            tc_fence_after();
+            const uint32_t tmem_d = tmem_base + (uint32_t)acc * BN;
+            for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                if (!wait_warp(&full[stage], phase, abort_word)) { ok = false; break; }
+                unsigned char* pa = base + (size_t)stage * STAGE_BYTES;
+                const uint32_t sa = smem_u32(pa), sb = sa + A_BYTES;
+                int steps = BK / UMMA_K;
+                if (KIND == kWeights) {
+                    const int left = it.n - kb * BK;        // rows of the group in this block
+                    if (left < BK) {
+                        steps = (left + UMMA_K - 1) / UMMA_K;
+                        // rows [left, 16 * steps) belong to the next group: zeros.  A row is 128 bytes in each box, whatever
+                        // the swizzle, which moves bytes inside a row only.
+                        const int rows = steps * UMMA_K - left, per = rows * 8;
+                        for (int i = lane; i < (BM + BN) / 64 * per; i += 32) {
+                            const int c = i / per, r = i - c * per;
+                            *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
+                }
+                if (lane == 0) {
+                    tc_fence_after();
+                    for (int k = 0; k < steps; ++k) {
+                        const uint64_t da = A_MN ? umma_desc_mn(sa + k * 2048) : umma_desc_sw128(sa + k * UMMA_K * 2);
+                        const uint64_t db = B_MN ? umma_desc_mn(sb + k * 2048) : umma_desc_sw128(sb + k * UMMA_K * 2);
+                        umma_f16(tmem_d, da, db, kIdesc, (kb > it.kb0 || k > 0) ? 1u : 0u);
+                    }
+                    umma_commit(&empty[stage]);
+                }
+                __syncwarp();
+                if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
+            }
+            if (!ok) break;
+            if (lane == 0) umma_commit(&acc_full[acc]);
+            __syncwarp();
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    } else {  // ---- epilogue: TMEM lane quadrant = warp % 4, column half = (warp - 2) / 4 ----
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const int et = threadIdx.x - 64;
+        // what no tile covers: rows behind the last group, weights of experts without rows
+        if (KIND != kWeights) {
+            const long long kept = min(max(offsets[a.E], 0), a.R), per = a.N / 8, n = ((long long)a.R - kept) * per;
+            for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps)) {
+                const size_t o = (size_t)(kept * per + i) * 8;
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + o) = make_uint4(0, 0, 0, 0);
+                if (a.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(0, 0, 0, 0);
+            }
+        } else {
+            const float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+            const long long n = (long long)a.M * (a.N / 8);
+            for (int e = 0; e < a.E; ++e) {
+                if (group_of(offsets, e, a.R).n > 0) continue;
+                for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps))
+                    store8(a, (size_t)(e * n + i) * 8, z);
+            }
+        }
+        __syncwarp();
+        int acc = 0; uint32_t acc_phase = 0;
+        while (cur.next(it)) {
+            if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
+            tc_fence_after();
+            const int r_in = it.mt * BM + q * 32 + lane;
+            const bool row_ok = r_in < (KIND == kWeights ? a.M : it.n);
+            const bool whole = it.kb1 - it.kb0 == it.kb;
+            const size_t row = KIND == kWeights ? (size_t)it.e * a.M + r_in : (size_t)it.lo + r_in;
+            const int n0 = it.nt * BN;
+            float* part = nullptr;
+            if (!whole) part = a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + (q * 32 + lane)) * BN;
+#pragma unroll 1
+            for (int c = half * (BN / 64); c < (half + 1) * (BN / 64); ++c) {
+                __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
+                uint32_t r[32];
+                tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + c * 32), r);
+                if (!row_ok || n0 + c * 32 >= a.N) continue;
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) st_global_v8(part + c * 32 + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    const int col = n0 + c * 32 + i;
+                    if (col >= a.N) break;
+                    float2 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                    const size_t o = row * a.N + col;
+                    if (KIND != kWeights) finish8(a, it.e, o, col, v);
+                    store8(a, o, v);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&acc_empty[acc]);
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    quiesce_after_abort(abort_word);
+    __syncthreads();
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// Adds up the sums of the tiles that more than one run worked on, in the order of the runs, and finishes them.  CTA (x, y): the
+// tile in which run x ends, if it began in run x as well (so that each such tile has one owner), every gridDim.y-th piece.
+constexpr int kJoinThreads = 256, kJoinParts = 8;
+template <int KIND>
+__global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearArgs a) {
+    __shared__ int offsets[kMaxE + 1];
+    pdl_wait();
+    pdl_trigger();
+    for (int i = threadIdx.x; i <= a.E; i += kJoinThreads) offsets[i] = __ldg(a.offsets + i);
+    __syncthreads();
+    const Totals s = totals<KIND>(a, offsets, threadIdx.x & 31);
+    const int runs = deal(a, s), c0 = blockIdx.x;
+    if (c0 + 1 >= runs) return;
+    const long long cut = run_begin(s, runs, c0 + 1);       // the first block of the next run
+    const Tiles<KIND> t{a, offsets};
+    long long base = 0;
+    for (int e = 0; e < a.E; ++e) {
+        const Group g = group_of(offsets, e, a.R);
+        const int kb = t.kblocks(g), per = t.tiles(g);
+        const long long size = (long long)kb * per;
+        if (cut >= base + size) { base += size; continue; }
+        const int tile = (int)((cut - base) / kb);
+        const long long begin = base + (long long)tile * kb, end = begin + kb;
+        if (begin == cut || begin < run_begin(s, runs, c0)) return;     // the cut is between tiles, or an earlier run owns the tile
+        int c1 = c0 + 1;                                                // last run that worked on the tile
+        while (c1 + 1 < runs && run_begin(s, runs, c1 + 1) < end) ++c1;
+        const int mts = t.m_tiles(g), nt = tile / mts, mt = tile - nt * mts, n0 = nt * BN;
+        const int rows = min(BM, (KIND == kWeights ? a.M : g.n) - mt * BM), cols = min(BN, a.N - n0) / 8;
+        for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < rows * cols; i += gridDim.y * kJoinThreads) {
+            const int r = i / cols, col = (i - r * cols) * 8;
+            float2 v[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+            for (int c = c0; c <= c1; ++c) {
+                const float4* p = reinterpret_cast<const float4*>(a.part + (((size_t)c * 2 + (c == c0 ? 1 : 0)) * a.part_rows + r) * BN + col);
+                const float4 p0 = __ldcg(p), p1 = __ldcg(p + 1);
+                v[0].x += p0.x; v[0].y += p0.y; v[1].x += p0.z; v[1].y += p0.w;
+                v[2].x += p1.x; v[2].y += p1.y; v[3].x += p1.z; v[3].y += p1.w;
+            }
+            const size_t row = KIND == kWeights ? (size_t)e * a.M + mt * BM + r : (size_t)g.lo + mt * BM + r;
+            const size_t o = row * a.N + n0 + col;
+            if (KIND != kWeights) finish8(a, e, o, n0 + col, v);
+            store8(a, o, v);
+        }
+        return;
+    }
+}
+
+// db[e] = sum of the group's rows of dy, in a fixed order: a CTA takes 64 columns of one expert, a warp every eighth row.
+constexpr int kBiasThreads = 256;
+__global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const int32_t* __restrict__ offsets, const uint16_t* __restrict__ dy, int R, int N,
+                                                                        float* __restrict__ db) {
+    __shared__ float2 sm[kBiasThreads / 32][32];
+    pdl_wait();
+    pdl_trigger();
+    const int e = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Group g = group_of(offsets, e, R);
+    const int col = blockIdx.x * 64 + 2 * lane;             // N is a multiple of 8
+    float2 s = make_float2(0.0f, 0.0f);
+    if (col < N) {
+        const uint16_t* p = dy + (size_t)g.lo * N + col;
+        int r = warp;
+        for (; r + 24 < g.n; r += 32) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p + (size_t)(r + 8 * i) * N));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s.x += bf16_lo(w[i]); s.y += bf16_hi(w[i]); }
+        }
+        for (; r < g.n; r += 8) {
+            const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(p + (size_t)r * N));
+            s.x += bf16_lo(w); s.y += bf16_hi(w);
+        }
+    }
+    sm[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && col < N) {
+        for (int w = 1; w < kBiasThreads / 32; ++w) { s.x += sm[w][lane].x; s.y += sm[w][lane].y; }
+        *reinterpret_cast<float2*>(db + (size_t)e * N + col) = s;
+    }
+}
+
+// Up to this many waves of tiles the work is dealt by runs.
+constexpr int kDealWaves = 8;
+
+template <int KIND>
+int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cudaStream_t st) {
+    LinearArgs a = a0;
+    CUtensorMap tmA, tmB;
+    a.n_tiles = (a.N + BN - 1) / BN;
+    a.grid = sm_count();
+    a.deal_waves = kDealWaves;
+    a.part = static_cast<float*>(ws);
+    a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
+    a.a_rows = BM;
+    if (KIND == kWeights) {         // dy [R][M], x [R][N]
+        const uint64_t da[2] = {(uint64_t)a.M, (uint64_t)a.R}, db[2] = {(uint64_t)a.N, (uint64_t)a.R};
+        if (!make_map(&tmA, A, 2, da, BK) || !make_map(&tmB, B, 2, db, BK)) return LOCMOE_ERR_CUDA;
+    } else {
+        while (a.a_rows > 16 && a.a_rows / 2 >= a.R) a.a_rows /= 2;     // few rows: smaller boxes, the tile's other rows hold what they held
+        const uint64_t da[2] = {(uint64_t)a.K, (uint64_t)a.R};
+        const uint64_t db[3] = {(uint64_t)(KIND == kForward ? a.K : a.N), (uint64_t)(KIND == kForward ? a.N : a.K), (uint64_t)a.E};
+        if (!make_map(&tmA, A, 2, da, a.a_rows) || !make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK)) return LOCMOE_ERR_CUDA;
+    }
+    static bool attr_done_dev[64] = {false};   // the attribute is per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!attr_done_dev[dev & 63]) {
+        if (cudaFuncSetAttribute(expert_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return LOCMOE_ERR_CUDA;
+        }
+        attr_done_dev[dev & 63] = true;
+    }
+    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(kThreads), kSmem, st, tmA, tmB, a);
+    if (rc) return rc;
+    // without the join where the tiles are too many for runs whatever the groups are
+    const long long least = KIND == kWeights ? (long long)((a.M + BM - 1) / BM) * a.n_tiles : 0;
+    if (least <= (long long)a.deal_waves * a.grid) {
+        const int parts = (a.part_rows * (BN / 8) + kJoinThreads - 1) / kJoinThreads;
+        rc = launch_pdl(expert_join_kernel<KIND>, dim3(a.grid, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, st, a);
+    }
+    return rc ? rc : check_launch();
+}
+
+}  // namespace
+
+// Two tiles' sums a CTA.
+size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad) {
+    return (size_t)sm_count() * 2 * (grad || s.T > BM ? BM : s.T) * BN * sizeof(float);
+}
+
+int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_linear_t& l, void* ws, cudaStream_t st) {
+    LinearArgs a{};
+    a.offsets = l.offsets; a.out = l.y; a.z_out = l.z; a.bias = l.bias; a.residual = l.residual; a.act = l.act;
+    a.E = s.E; a.R = s.T; a.N = N; a.K = s.H;
+    return launch_gemm<kForward>(a, l.x, l.w, ws, st);
+}
+
+int launch_expert_linear_grad(const locmoe_shape_t& s, int N, const locmoe_expert_linear_grad_t& l, void* ws, cudaStream_t st) {
+    int rc = LOCMOE_OK;
+    if (l.dx) {
+        LinearArgs a{};
+        a.offsets = l.offsets; a.out = l.dx;
+        if (l.z && l.act != LOCMOE_ACT_NONE) { a.z_in = l.z; a.act = l.act; }
+        a.E = s.E; a.R = s.T; a.N = s.H; a.K = N;
+        rc = launch_gemm<kTowardsX>(a, l.dy, l.w, ws, st);
+        if (rc) return rc;
+    }
+    if (l.dw) {
+        LinearArgs a{};
+        a.offsets = l.offsets; a.out = l.dw; a.out_f32 = l.dw_dtype == LOCMOE_F32;
+        a.E = s.E; a.R = s.T; a.M = N; a.N = s.H;
+        rc = launch_gemm<kWeights>(a, l.dy, l.x, ws, st);
+        if (rc) return rc;
+    }
+    if (l.db) {
+        rc = launch_pdl(expert_bias_grad_kernel, dim3((N + 63) / 64, s.E), dim3(kBiasThreads), 0, st, l.offsets, static_cast<const uint16_t*>(l.dy), (int)s.T, N, l.db);
+        if (rc) return rc;
+    }
+    return check_launch();
+}
+
+int read_linear_flags(int* out, cudaStream_t st) {
+    if (cudaMemcpyFromSymbolAsync(out, g_linear_flags, sizeof(int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    return LOCMOE_OK;
+}
+
+}  // namespace locmoe

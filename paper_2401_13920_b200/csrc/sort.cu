@@ -1,0 +1,646 @@
+// Tokens sorted by expert and back, without a capacity: the order (stable, by expert), the rows in it, the weighted sum back
+// in token order, and the gradients of both, the router's among them.
+//
+// An assignment v = c * T + t is choice c of token t.  slot[v] is its row: the number of assignments with a lower expert plus
+// those of the same expert with a lower v; inv is the inverse.  All kernels but the first move rows and are bound by HBM:
+// a warp works on a token (or, with short rows, on several), reads each row it needs once with 16-byte streaming loads and
+// writes whole rows; rows that are no multiple of 16 bytes go element by element, more of them in flight.
+#include "common.cuh"
+
+namespace locmoe {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+// ---- the order: one cluster, counts in shared memory ----
+// A warp owns a contiguous run of assignments, a CTA the runs of its 32 warps, the cluster all of them.  Pass 1 counts each
+// warp's assignments by expert, without atomics: lanes with the same expert find each other by match, the lowest adds.
+// The counts become first rows by sums over experts, CTAs (through distributed shared memory) and warps; pass 2 hands out
+// the rows in order.  The index array is read twice, 131072 assignments by 8 CTAs in about 10 us.
+constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32, kPlanBatch = 8;
+constexpr int kPlanMaxCtas = 8;          // the portable cluster size
+
+__device__ __forceinline__ int ld_cluster(const int* p, int cta) {
+    uint32_t ra;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(smem_u32(p)), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ra) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* __restrict__ idx, int V, int T, int E, int32_t* __restrict__ offsets,
+                                                                 int32_t* __restrict__ slot, int32_t* __restrict__ inv, int32_t* __restrict__ load) {
+    extern __shared__ int sm[];
+    int* tot = sm;              // [E] assignments of this CTA
+    int* first = tot + E;       // [E] assignments of this CTA's first choices
+    int* scan = first + E;      // [32]
+    int* cnt = scan + 32;       // [32][E] by warp: counts, then next row
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nc = gridDim.x, rank = blockIdx.x;   // the grid is one cluster
+    for (int i = threadIdx.x; i < 2 * E + 32 + kPlanWarps * E; i += kPlanThreads) sm[i] = 0;
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    const long long per = (((long long)V + (long long)nc * kPlanWarps - 1) / (nc * kPlanWarps) + 31) & ~31ll;
+    const long long lo = min((long long)V, ((long long)rank * kPlanWarps + warp) * per), hi = min((long long)V, lo + per);
+    int* mine = cnt + warp * E;
+    for (long long b = lo; b < hi; b += 32 * kPlanBatch) {
+        int key[kPlanBatch];
+#pragma unroll
+        for (int i = 0; i < kPlanBatch; ++i) {
+            const long long v = b + 32 * i + lane;
+            key[i] = v < hi ? __ldg(idx + v) : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kPlanBatch; ++i) {
+            if (b + 32 * i >= hi) break;
+            const bool ok = key[i] >= 0 && key[i] < E;
+            const unsigned same = __match_any_sync(0xffffffffu, ok ? key[i] : -1);
+            if (ok && lane == __ffs(same) - 1) mine[key[i]] += __popc(same);
+            if (load && ok && b + 32 * i + lane < T) atomicAdd(first + key[i], 1);
+            __syncwarp();
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kPlanThreads) {
+        int sum = 0;
+        for (int w = 0; w < kPlanWarps; ++w) sum += cnt[w * E + e];
+        tot[e] = sum;
+    }
+    cluster_barrier();
+    const int e = threadIdx.x;     // E <= 1024
+    int before = 0, all = 0;
+    if (e < E) {
+        for (int r = 0; r < nc; ++r) {
+            const int n = ld_cluster(tot + e, r);
+            if (r < rank) before += n;
+            all += n;
+        }
+        if (load && rank == 0) {
+            int n = 0;
+            for (int r = 0; r < nc; ++r) n += ld_cluster(first + e, r);
+            load[e] = n;
+        }
+    }
+    int up = all;                  // inclusive sum over the experts
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int n = __shfl_up_sync(0xffffffffu, up, d);
+        if (lane >= d) up += n;
+    }
+    if (lane == 31) scan[warp] = up;
+    cluster_barrier();             // the other CTAs' counts have been read, and scan is complete
+    int lower = 0;
+    for (int w = 0; w < warp; ++w) lower += scan[w];
+    if (e < E) {
+        int row = lower + up - all;
+        if (rank == 0) {
+            offsets[e] = row;
+            if (e == E - 1) offsets[E] = row + all;
+        }
+        row += before;
+        for (int w = 0; w < kPlanWarps; ++w) {
+            const int n = cnt[w * E + e];
+            cnt[w * E + e] = row;
+            row += n;
+        }
+    }
+    int kept = 0;
+    for (int w = 0; w < kPlanWarps; ++w) kept += scan[w];
+    __syncthreads();
+    for (long long b = lo; b < hi; b += 32 * kPlanBatch) {
+        int key[kPlanBatch];
+#pragma unroll
+        for (int i = 0; i < kPlanBatch; ++i) {
+            const long long v = b + 32 * i + lane;
+            key[i] = v < hi ? __ldg(idx + v) : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kPlanBatch; ++i) {
+            const long long v = b + 32 * i + lane;
+            if (b + 32 * i >= hi) break;
+            const bool ok = key[i] >= 0 && key[i] < E;
+            const unsigned same = __match_any_sync(0xffffffffu, ok ? key[i] : -1);
+            const int row = ok ? mine[key[i]] + __popc(same & ((1u << lane) - 1u)) : -1;
+            __syncwarp();
+            if (ok && lane == __ffs(same) - 1) mine[key[i]] += __popc(same);
+            __syncwarp();
+            if (v < hi) slot[v] = row;
+            if (ok) inv[row] = (int)v;
+        }
+    }
+    for (long long r = (long long)kept + rank * kPlanThreads + threadIdx.x; r < V; r += (long long)nc * kPlanThreads) inv[r] = -1;
+}
+
+// ---- rows ----
+// A row in units: 16 bytes of elements, or one element where rows or arrays are not 16-byte aligned.
+template <int DT, bool VEC> struct Unit;
+template <> struct Unit<LOCMOE_BF16, true> {
+    static constexpr int N = 8, CH = 2;      // elements, units in flight a lane and row
+    typedef uint4 Raw;
+    static __device__ __forceinline__ Raw load(const void* p, long long i) { return ld_stream(static_cast<const uint4*>(p) + i); }
+    static __device__ __forceinline__ void widen(const Raw& r, float (&f)[N]) {
+        f[0] = bf16_lo(r.x); f[1] = bf16_hi(r.x); f[2] = bf16_lo(r.y); f[3] = bf16_hi(r.y);
+        f[4] = bf16_lo(r.z); f[5] = bf16_hi(r.z); f[6] = bf16_lo(r.w); f[7] = bf16_hi(r.w);
+    }
+    static __device__ __forceinline__ Raw narrow(const float (&f)[N]) {
+        return make_uint4(cvt_bf16x2(make_float2(f[0], f[1])), cvt_bf16x2(make_float2(f[2], f[3])), cvt_bf16x2(make_float2(f[4], f[5])),
+                          cvt_bf16x2(make_float2(f[6], f[7])));
+    }
+    static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { st_stream(static_cast<uint4*>(p) + i, r); }
+    static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
+};
+template <> struct Unit<LOCMOE_F32, true> {
+    static constexpr int N = 4, CH = 2;
+    typedef uint4 Raw;
+    static __device__ __forceinline__ Raw load(const void* p, long long i) { return ld_stream(static_cast<const uint4*>(p) + i); }
+    static __device__ __forceinline__ void widen(const Raw& r, float (&f)[N]) {
+        f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ Raw narrow(const float (&f)[N]) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { st_stream(static_cast<uint4*>(p) + i, r); }
+    static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
+};
+template <> struct Unit<LOCMOE_BF16, false> {
+    static constexpr int N = 1, CH = 8;
+    typedef uint16_t Raw;
+    static __device__ __forceinline__ Raw load(const void* p, long long i) { return __ldcs(static_cast<const unsigned short*>(p) + i); }
+    static __device__ __forceinline__ void widen(const Raw& r, float (&f)[N]) { f[0] = bf16_lo(r); }
+    static __device__ __forceinline__ Raw narrow(const float (&f)[N]) { return (Raw)cvt_bf16x2(make_float2(f[0], f[0])); }
+    static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { static_cast<uint16_t*>(p)[i] = r; }
+    static __device__ __forceinline__ Raw zero() { return 0; }
+};
+template <> struct Unit<LOCMOE_F32, false> {
+    static constexpr int N = 1, CH = 8;
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ Raw load(const void* p, long long i) { return __ldcs(static_cast<const unsigned int*>(p) + i); }
+    static __device__ __forceinline__ void widen(const Raw& r, float (&f)[N]) { f[0] = __uint_as_float(r); }
+    static __device__ __forceinline__ Raw narrow(const float (&f)[N]) { return __float_as_uint(f[0]); }
+    static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { static_cast<uint32_t*>(p)[i] = r; }
+    static __device__ __forceinline__ Raw zero() { return 0u; }
+};
+
+// What a row kernel works on.  `width` lanes (a power of two) share a token; a CTA owns `tpc` consecutive tokens.
+struct RowArgs {
+    int T, U, K, E;             // tokens, units a row, choices, experts
+    long long rows;             // K * T
+    int width, tpc;
+};
+
+// Rows [offsets[E], rows) hold no assignment: zeros.
+template <typename U>
+__device__ __forceinline__ void zero_tail(const RowArgs& a, const int32_t* __restrict__ offsets, void* __restrict__ out) {
+    const long long kept = max(0, __ldg(offsets + a.E));
+    const long long n = (a.rows - kept) * a.U;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads)
+        U::store(out, kept * a.U + i, U::zero());
+}
+
+// xs[slot[c][t]] = x[t]: a token's row is read once and written K times.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kThreads) sort_rows_kernel(const RowArgs a, const void* __restrict__ x, const int32_t* __restrict__ offsets,
+                                                             const int32_t* __restrict__ slot, void* __restrict__ xs) {
+    typedef Unit<DT, VEC> U;
+    constexpr int CH = 2 * U::CH;
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x % a.width, step = kThreads / a.width;
+    const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
+    for (long long t = lo + threadIdx.x / a.width; t < hi; t += step) {
+        bool any = false;
+        for (int c = 0; c < a.K; ++c) any |= __ldg(slot + (long long)c * a.T + t) >= 0;
+        if (!any) continue;
+        for (int u0 = lane; u0 < a.U; u0 += CH * a.width) {
+            typename U::Raw r[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+                if (u0 + i * a.width < a.U) r[i] = U::load(x, t * a.U + u0 + i * a.width);
+            for (int c = 0; c < a.K; ++c) {
+                const int s = __ldg(slot + (long long)c * a.T + t);
+                if (s < 0 || s >= a.rows) continue;
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+                    if (u0 + i * a.width < a.U) U::store(xs, (long long)s * a.U + u0 + i * a.width, r[i]);
+            }
+        }
+    }
+    zero_tail<U>(a, offsets, xs);
+}
+
+// out[t] = residual[t] + sum_c w[c][t] * y[slot[c][t]], choices without a row left out.
+template <int DT, bool VEC, int KM>
+__global__ void __launch_bounds__(kThreads) unsort_rows_kernel(const RowArgs a, const void* __restrict__ y, const int32_t* __restrict__ slot,
+                                                               const float* __restrict__ w, const void* __restrict__ residual, void* __restrict__ out) {
+    typedef Unit<DT, VEC> U;
+    constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x % a.width, step = kThreads / a.width;
+    const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
+    for (long long t = lo + threadIdx.x / a.width; t < hi; t += step) {
+        int s[KM];
+        float g[KM];
+#pragma unroll
+        for (int c = 0; c < KM; ++c) {
+            s[c] = c < a.K ? __ldg(slot + (long long)c * a.T + t) : -1;
+            g[c] = w && c < a.K ? __ldg(w + (long long)c * a.T + t) : 1.0f;
+            if (s[c] >= a.rows) s[c] = -1;
+        }
+        for (int u0 = lane; u0 < a.U; u0 += CH * a.width) {
+            typename U::Raw r[CH][KM], h[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int u = u0 + i * a.width;
+                if (u >= a.U) break;
+                if (residual) h[i] = U::load(residual, t * a.U + u);
+#pragma unroll
+                for (int c = 0; c < KM; ++c)
+                    if (s[c] >= 0) r[i][c] = U::load(y, (long long)s[c] * a.U + u);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int u = u0 + i * a.width;
+                if (u >= a.U) break;
+                float acc[U::N], v[U::N];
+                if (residual) U::widen(h[i], acc);
+                else {
+#pragma unroll
+                    for (int k = 0; k < U::N; ++k) acc[k] = 0.0f;
+                }
+#pragma unroll
+                for (int c = 0; c < KM; ++c) {
+                    if (s[c] < 0) continue;
+                    U::widen(r[i][c], v);
+#pragma unroll
+                    for (int k = 0; k < U::N; ++k) acc[k] = __fmaf_rn(g[c], v[k], acc[k]);
+                }
+                U::store(out, t * a.U + u, U::narrow(acc));
+            }
+        }
+    }
+}
+
+// dy[slot[c][t]] = w[c][t] * dout[t],  dw[c][t] = <dout[t], y[slot[c][t]]>; a token's dout is read once.
+template <int DT, bool VEC, int KM>
+__global__ void __launch_bounds__(kThreads) unsort_grad_kernel(const RowArgs a, const void* __restrict__ dout, const void* __restrict__ y,
+                                                               const int32_t* __restrict__ offsets, const int32_t* __restrict__ slot,
+                                                               const float* __restrict__ w, void* __restrict__ dy, float* __restrict__ dw) {
+    typedef Unit<DT, VEC> U;
+    constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x % a.width, step = kThreads / a.width;
+    const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
+    for (long long t0 = lo; t0 < hi; t0 += step) {          // whole warps stay together: the sums are shuffled
+        const long long t = t0 + threadIdx.x / a.width;
+        int s[KM];
+        float g[KM], dot[KM];
+        bool any = false;
+#pragma unroll
+        for (int c = 0; c < KM; ++c) {
+            s[c] = c < a.K && t < hi ? __ldg(slot + (long long)c * a.T + t) : -1;
+            if (s[c] >= a.rows) s[c] = -1;
+            g[c] = w && s[c] >= 0 ? __ldg(w + (long long)c * a.T + t) : 1.0f;
+            dot[c] = 0.0f;
+            any |= s[c] >= 0;
+        }
+        if (any) {
+            for (int u0 = lane; u0 < a.U; u0 += CH * a.width) {
+                typename U::Raw r[CH][KM], d[CH];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int u = u0 + i * a.width;
+                    if (u >= a.U) break;
+                    d[i] = U::load(dout, t * a.U + u);
+                    if (dw) {
+#pragma unroll
+                        for (int c = 0; c < KM; ++c)
+                            if (s[c] >= 0) r[i][c] = U::load(y, (long long)s[c] * a.U + u);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int u = u0 + i * a.width;
+                    if (u >= a.U) break;
+                    float f[U::N], v[U::N];
+                    U::widen(d[i], f);
+#pragma unroll
+                    for (int c = 0; c < KM; ++c) {
+                        if (s[c] < 0) continue;
+                        if (dw) {
+                            U::widen(r[i][c], v);
+#pragma unroll
+                            for (int k = 0; k < U::N; ++k) dot[c] = __fmaf_rn(f[k], v[k], dot[c]);
+                        }
+                        if (dy) {
+#pragma unroll
+                            for (int k = 0; k < U::N; ++k) v[k] = __fmul_rn(g[c], f[k]);
+                            U::store(dy, (long long)s[c] * a.U + u, U::narrow(v));
+                        }
+                    }
+                }
+            }
+        }
+        if (dw) {
+#pragma unroll
+            for (int c = 0; c < KM; ++c) {
+                for (int o = a.width >> 1; o; o >>= 1) dot[c] += __shfl_xor_sync(0xffffffffu, dot[c], o);
+                if (lane == 0 && t < hi && c < a.K) dw[(long long)c * a.T + t] = dot[c];
+            }
+        }
+    }
+    if (dy) zero_tail<U>(a, offsets, dy);
+}
+
+// Gradient of the sorted rows towards the tokens, the router's gradient added:
+//   dx[t][j] = sum_c dxs[slot[c][t]][j] + dG[t][j / g] / g,   dG_i = [G_i > 0] p_i (q_i - sum_j p_j q_j),
+//   G = group means of x[t] + eps, p = softmax(ReLU(G)), q_i = dp_i + sum_c [idx[c][t] = i] dw[c][t].
+// A warp works on a token and forms G, p and dG anew from the row, which costs the read of x; keeping p would cost E floats a
+// token instead but leave the sign of G open, which the ReLU needs.  Sums of whole units go through shared memory, where
+// the lanes add up the units of a group in order.  deps: each warp's sums in shared memory, the CTA's to `part`.
+struct RouterArgs {
+    const void* x; const float* eps; const int32_t* idx; const float* dw; const float* dp; float* part;
+    int g;                      // units a group
+    float inv_g;                // 1 / elements a group
+};
+
+template <int DT, bool VEC, int KM>
+__global__ void __launch_bounds__(kThreads) sort_grad_router_kernel(const RowArgs a, const RouterArgs b, const void* __restrict__ dxs,
+                                                                    const int32_t* __restrict__ slot, void* __restrict__ dx) {
+    typedef Unit<DT, VEC> U;
+    constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
+    extern __shared__ float smf[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5, E = a.E;
+    float* sums = smf + (size_t)warp * (a.U + 3 * E);      // [U] sums of the row's units
+    float* G = sums + a.U;                                  // [E] G, then dG / g
+    float* p = G + E;                                       // [E]
+    float* deps = p + E;                                    // [E] sums over this warp's tokens
+    for (int e = lane; e < E; e += 32) deps[e] = 0.0f;
+    pdl_wait();
+    pdl_trigger();
+    const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
+    for (long long t = lo + warp; t < hi; t += nw) {
+        int s[KM], id[KM];
+        float dw[KM];
+#pragma unroll
+        for (int c = 0; c < KM; ++c) {
+            const long long v = (long long)c * a.T + t;
+            s[c] = dxs && c < a.K ? __ldg(slot + v) : -1;
+            if (s[c] >= a.rows) s[c] = -1;
+            id[c] = c < a.K && b.dw ? __ldg(b.idx + v) : -1;
+            dw[c] = c < a.K && b.dw ? __ldg(b.dw + v) : 0.0f;
+        }
+        for (int u0 = lane; u0 < a.U; u0 += 2 * U::CH * 32) {
+            typename U::Raw r[2 * U::CH];
+#pragma unroll
+            for (int i = 0; i < 2 * U::CH; ++i)
+                if (u0 + 32 * i < a.U) r[i] = U::load(b.x, t * a.U + u0 + 32 * i);
+#pragma unroll
+            for (int i = 0; i < 2 * U::CH; ++i) {
+                if (u0 + 32 * i >= a.U) break;
+                float f[U::N];
+                U::widen(r[i], f);
+                float sum = f[0];
+#pragma unroll
+                for (int k = 1; k < U::N; ++k) sum += f[k];
+                sums[u0 + 32 * i] = sum;
+            }
+        }
+        __syncwarp();
+        float top = 0.0f;
+        for (int e = lane; e < E; e += 32) {
+            float sum = 0.0f;
+            for (int k = 0; k < b.g; ++k) sum += sums[e * b.g + k];
+            sum = sum * b.inv_g + (b.eps ? __ldg(b.eps + e) : 0.0f);
+            G[e] = sum;
+            top = fmaxf(top, sum);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        float z = 0.0f;
+        for (int e = lane; e < E; e += 32) {
+            const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top);    // a NaN stays one
+            p[e] = v;
+            z += v;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        const float rz = 1.0f / z;
+        float m = 0.0f;
+        for (int e = lane; e < E; e += 32) {
+            float q = b.dp ? __ldg(b.dp + e) : 0.0f;
+#pragma unroll
+            for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
+            const float v = p[e] * rz;
+            p[e] = G[e] <= 0.0f ? 0.0f : v;             // what leaves through the ReLU
+            m = __fmaf_rn(v, q, m);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+        for (int e = lane; e < E; e += 32) {
+            float q = b.dp ? __ldg(b.dp + e) : 0.0f;
+#pragma unroll
+            for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
+            const float d = p[e] * (q - m);
+            deps[e] += d;
+            G[e] = d * b.inv_g;
+        }
+        __syncwarp();
+        for (int u0 = lane; u0 < a.U; u0 += CH * 32) {
+            typename U::Raw r[CH][KM];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int u = u0 + 32 * i;
+                if (u >= a.U) break;
+#pragma unroll
+                for (int c = 0; c < KM; ++c)
+                    if (s[c] >= 0) r[i][c] = U::load(dxs, (long long)s[c] * a.U + u);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int u = u0 + 32 * i;
+                if (u >= a.U) break;
+                const float d = G[u / b.g];
+                float acc[U::N], v[U::N];
+#pragma unroll
+                for (int k = 0; k < U::N; ++k) acc[k] = d;
+#pragma unroll
+                for (int c = 0; c < KM; ++c) {
+                    if (s[c] < 0) continue;
+                    U::widen(r[i][c], v);
+#pragma unroll
+                    for (int k = 0; k < U::N; ++k) acc[k] += v[k];
+                }
+                U::store(dx, t * a.U + u, U::narrow(acc));
+            }
+        }
+        __syncwarp();
+    }
+    if (!b.part) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        float sum = 0.0f;
+        for (int w = 0; w < nw; ++w) sum += smf[(size_t)w * (a.U + 3 * E) + a.U + 2 * E + e];
+        b.part[(size_t)blockIdx.x * E + e] = sum;
+    }
+}
+
+// deps[e] = sum of the CTAs' sums, in a fixed order: 32 experts a CTA, the rows dealt to 8 warps.
+__global__ void __launch_bounds__(kThreads) deps_finish_kernel(const float* __restrict__ part, int n, int E, float* __restrict__ deps) {
+    __shared__ float sm[kWarps][32];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+    float sum = 0.0f;
+    if (e < E)
+        for (int r = warp; r < n; r += kWarps) sum += part[(size_t)r * E + e];
+    sm[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && e < E) {
+        for (int w = 1; w < kWarps; ++w) sum += sm[w][lane];
+        deps[e] = sum;
+    }
+}
+
+bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }   // an absent array is
+
+// Tokens a CTA and lanes a token of a row kernel.
+RowArgs row_args(const locmoe_shape_t& s, int K, int U, int* grid) {
+    RowArgs a{s.T, U, K, s.E, (long long)K * s.T, 32, 1};
+    while (a.width > 1 && a.width / 2 >= U) a.width /= 2;
+    const long long step = kThreads / a.width;
+    const long long want = (s.T + step - 1) / step, cap = 1024ll * sm_count();     // many short CTAs, in ascending token order
+    const long long g = want < cap ? want : cap;
+    a.tpc = (int)((s.T + g - 1) / g);
+    a.tpc = (int)((a.tpc + step - 1) / step * step);
+    *grid = (int)((s.T + a.tpc - 1) / a.tpc);
+    return a;
+}
+
+constexpr size_t kRouterSmem = 200 * 1024;
+size_t router_warp_bytes(int U, int E) { return ((size_t)U + 3 * (size_t)E) * sizeof(float); }
+// Whether a row's groups are whole 16-byte units.
+bool router_vec(const locmoe_shape_t& s, bool aligned) {
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
+    return aligned && (s.H / s.E) % n == 0;
+}
+int router_grid_cap() { return 8 * sm_count(); }
+
+#define LOCMOE_BY_UNIT(DTYPE, VEC, F, ...)                                             \
+    ((DTYPE) == LOCMOE_F32 ? ((VEC) ? F<LOCMOE_F32, true>(__VA_ARGS__) : F<LOCMOE_F32, false>(__VA_ARGS__)) \
+                           : ((VEC) ? F<LOCMOE_BF16, true>(__VA_ARGS__) : F<LOCMOE_BF16, false>(__VA_ARGS__)))
+
+template <int DT, bool VEC>
+int sort_rows_dt(int grid, const RowArgs& a, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st) {
+    return launch_pdl(sort_rows_kernel<DT, VEC>, dim3(grid), dim3(kThreads), 0, st, a, x, offsets, slot, xs);
+}
+template <int DT, bool VEC>
+int unsort_rows_dt(int grid, const RowArgs& a, const void* y, const int32_t* slot, const float* w, const void* residual, void* out, cudaStream_t st) {
+    auto* k = a.K == 1 ? unsort_rows_kernel<DT, VEC, 1> : a.K == 2 ? unsort_rows_kernel<DT, VEC, 2>
+            : a.K <= 4 ? unsort_rows_kernel<DT, VEC, 4> : unsort_rows_kernel<DT, VEC, 8>;
+    return launch_pdl(k, dim3(grid), dim3(kThreads), 0, st, a, y, slot, w, residual, out);
+}
+template <int DT, bool VEC>
+int unsort_grad_dt(int grid, const RowArgs& a, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot, const float* w,
+                   void* dy, float* dw, cudaStream_t st) {
+    auto* k = a.K == 1 ? unsort_grad_kernel<DT, VEC, 1> : a.K == 2 ? unsort_grad_kernel<DT, VEC, 2>
+            : a.K <= 4 ? unsort_grad_kernel<DT, VEC, 4> : unsort_grad_kernel<DT, VEC, 8>;
+    return launch_pdl(k, dim3(grid), dim3(kThreads), 0, st, a, dout, y, offsets, slot, w, dy, dw);
+}
+template <int DT, bool VEC>
+int sort_grad_router_dt(int grid, int warps, size_t smem, const RowArgs& a, const RouterArgs& b, const void* dxs, const int32_t* slot, void* dx,
+                        cudaStream_t st) {
+    auto* k = a.K == 1 ? sort_grad_router_kernel<DT, VEC, 1> : a.K == 2 ? sort_grad_router_kernel<DT, VEC, 2>
+            : a.K <= 4 ? sort_grad_router_kernel<DT, VEC, 4> : sort_grad_router_kernel<DT, VEC, 8>;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRouterSmem) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    return launch_pdl(k, dim3(grid), dim3(32 * warps), smem, st, a, b, dxs, slot, dx);
+}
+
+}  // namespace
+
+int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load, cudaStream_t st) {
+    const long long V = (long long)K * T;
+    const size_t smem = ((size_t)(kPlanWarps + 2) * E + 32) * sizeof(int);
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(sort_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    cudaLaunchConfig_t cfg = {};
+    const int nc = V <= 8192 ? 1 : kPlanMaxCtas;
+    cfg.gridDim = dim3(nc); cfg.blockDim = dim3(kPlanThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = nc; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, sort_plan_kernel, idx, (int)V, T, E, offsets, slot, inv, load) != cudaSuccess) {
+        cudaGetLastError();
+        return LOCMOE_ERR_CUDA;
+    }
+    return check_launch();
+}
+
+int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st) {
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
+    const bool vec = s.H % n == 0 && aligned16(x) && aligned16(xs);
+    int grid;
+    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_rows_dt, grid, a, x, offsets, slot, xs, st);
+    return rc ? rc : check_launch();
+}
+
+int launch_unsort_rows(const locmoe_shape_t& s, int K, const void* y, const int32_t* slot, const float* w, const void* residual, void* out,
+                       cudaStream_t st) {
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
+    const bool vec = s.H % n == 0 && aligned16(y) && aligned16(residual) && aligned16(out);
+    int grid;
+    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, unsort_rows_dt, grid, a, y, slot, w, residual, out, st);
+    return rc ? rc : check_launch();
+}
+
+int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot,
+                       const float* w, void* dy, float* dw, cudaStream_t st) {
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
+    const bool vec = s.H % n == 0 && aligned16(dout) && aligned16(y) && aligned16(dy);
+    int grid;
+    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, unsort_grad_dt, grid, a, dout, y, offsets, slot, w, dy, dw, st);
+    return rc ? rc : check_launch();
+}
+
+// A row's unit sums have to fit the shared memory of a CTA, whichever way its arrays are aligned.
+bool sort_grad_fits(const locmoe_shape_t& s) { return router_warp_bytes(router_vec(s, true) ? s.H / (s.x_dtype == LOCMOE_F32 ? 4 : 8) : s.H, s.E) <= kRouterSmem; }
+size_t sort_grad_ws_bytes(const locmoe_shape_t& s) { return ((size_t)router_grid_cap() * s.E * sizeof(float) + 255) & ~(size_t)255; }
+
+int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g, void* ws, cudaStream_t st) {
+    if (!g.x) return launch_unsort_rows(s, K, g.dxs, g.slot, nullptr, nullptr, g.dx, st);
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
+    const bool vec = router_vec(s, aligned16(g.x) && aligned16(g.dxs) && aligned16(g.dx));
+    const int U = vec ? s.H / n : s.H;
+    const size_t per = router_warp_bytes(U, s.E);
+    if (per > kRouterSmem) return LOCMOE_ERR_ALIGN;      // arrays that are not 16-byte aligned take more room
+    int warps = (int)(kRouterSmem / per);
+    if (warps > kWarps) warps = kWarps;
+    RowArgs a{s.T, U, K, s.E, (long long)K * s.T, 32, 1};
+    long long grid = ((long long)s.T + warps - 1) / warps;
+    if (grid > router_grid_cap()) grid = router_grid_cap();
+    a.tpc = (int)((s.T + grid - 1) / grid);
+    grid = (s.T + a.tpc - 1) / a.tpc;
+    const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, U / s.E, 1.0f / (float)(s.H / s.E)};
+    int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_grad_router_dt, (int)grid, warps, per * warps, a, b, g.dxs, g.slot, g.dx, st);
+    if (rc == LOCMOE_OK && g.deps)
+        rc = launch_pdl(deps_finish_kernel, dim3((s.E + 31) / 32), dim3(kThreads), 0, st, (const float*)ws, (int)grid, s.E, g.deps);
+    return rc ? rc : check_launch();
+}
+
+}  // namespace locmoe
