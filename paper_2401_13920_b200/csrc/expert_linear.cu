@@ -49,6 +49,7 @@ struct LinearArgs {
     int act, out_f32;
     int E, R, M, N, K;          // M: rows of a weight (weights only)
     int n_tiles, a_rows;        // rows of one A box
+    int a_chunks, b_chunks;     // 1: one load brings an MN-major tile, else one for each 64 columns
     int part_rows;
     int grid, deal_waves;       // runs instead of tiles up to this many waves of tiles
 };
@@ -191,59 +192,97 @@ __device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64
 }
 
 // ---- epilogue arithmetic on pairs ----
-__device__ __forceinline__ float2 act2(float2 v, int act) {
-    if (act == LOCMOE_ACT_GELU) return gelu_erf2(v);
-    if (act == LOCMOE_ACT_SILU) return silu2(v);
-    if (act == LOCMOE_ACT_RELU) return make_float2(v.x < 0.0f ? 0.0f : v.x, v.y < 0.0f ? 0.0f : v.y);
-    return v;
-}
-__device__ __forceinline__ float2 slope2(float2 z, int act) {
-    if (act == LOCMOE_ACT_GELU) return gelu_erf_slope2(z);
-    if (act == LOCMOE_ACT_SILU) return silu_slope2(z);
-    return make_float2(z.x > 0.0f ? 1.0f : 0.0f, z.y > 0.0f ? 1.0f : 0.0f);    // ReLU
-}
 __device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
 
-// Eight sums of one row become outputs; `o` is the first's index in the [R][N] arrays, `col` its column.
-__device__ __forceinline__ void finish8(const LinearArgs& a, int e, size_t o, int col, float2 (&v)[4]) {
-    if (a.bias) {
-        const float4* b = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + col);
-        const float4 b0 = __ldg(b), b1 = __ldg(b + 1);
-        v[0].x += b0.x; v[0].y += b0.y; v[1].x += b0.z; v[1].y += b0.w;
-        v[2].x += b1.x; v[2].y += b1.y; v[3].x += b1.z; v[3].y += b1.w;
+// W sums of one row become outputs, W = 8 or 16 columns from `col` on; `o` is the first's index in the [R][N] arrays.  The arrays'
+// values (`extra`: z_in or residual) are loaded by the caller, long before the sums are there.  16 columns are 32 bytes of
+// bf16, a whole sector: rows are far apart, and a lane that stores half a sector at a time costs the L2 a merge (forward
+// product of 65536 x 2560 x 10240 with GeLU and z: 3.85 against 3.09 ms, the gradient through the GeLU 5.0 against 3.3 ms).
+template <int W>
+__device__ __forceinline__ void st_bf16(void* base, size_t o, const float2 (&v)[W / 2]) {
+    uint16_t* p = static_cast<uint16_t*>(base) + o;
+    if (W == 16)
+        st_global_v8(p, cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]), cvt_bf16x2(v[W / 2 - 4]), cvt_bf16x2(v[W / 2 - 3]),
+                     cvt_bf16x2(v[W / 2 - 2]), cvt_bf16x2(v[W / 2 - 1]));
+    else
+        *reinterpret_cast<uint4*>(p) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
+}
+template <int W>
+__device__ __forceinline__ void ld_bf16(const void* base, size_t o, uint32_t* r) {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + o;
+    if (W == 16)
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
+    else
+        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+}
+template <int KIND, int W>
+__device__ __forceinline__ void finish(const LinearArgs& a, int e, size_t o, int col, float2 (&v)[W / 2], const uint32_t* extra) {
+    if (KIND == kForward) {
+        if (a.bias) {
+            const float4* b = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + col);
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const float4 f = __ldg(b + i);
+                v[2 * i] = __fadd2_rn(v[2 * i], make_float2(f.x, f.y));
+                v[2 * i + 1] = __fadd2_rn(v[2 * i + 1], make_float2(f.z, f.w));
+            }
+        }
+        if (a.z_out) st_bf16<W>(a.z_out, o, v);
+        if (a.act == LOCMOE_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = gelu_erf2(v[i]);
+        } else if (a.act == LOCMOE_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = silu2(v[i]);
+        } else if (a.act == LOCMOE_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = make_float2(v[i].x < 0.0f ? 0.0f : v[i].x, v[i].y < 0.0f ? 0.0f : v[i].y);
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = __fadd2_rn(v[i], unpack2(extra[i]));
+        }
+    } else if (KIND == kTowardsX) {
+        if (a.act == LOCMOE_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = __fmul2_rn(v[i], gelu_erf_slope2(unpack2(extra[i])));
+        } else if (a.act == LOCMOE_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) v[i] = __fmul2_rn(v[i], silu_slope2(unpack2(extra[i])));
+        } else if (a.act == LOCMOE_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) {
+                const float2 z = unpack2(extra[i]);
+                v[i] = make_float2(z.x > 0.0f ? v[i].x : 0.0f, z.y > 0.0f ? v[i].y : 0.0f);
+            }
+        }
     }
-    if (a.z_out)
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
-    if (a.z_in) {
-        const uint4 z = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.z_in) + o));
-        v[0] = __fmul2_rn(v[0], slope2(unpack2(z.x), a.act)); v[1] = __fmul2_rn(v[1], slope2(unpack2(z.y), a.act));
-        v[2] = __fmul2_rn(v[2], slope2(unpack2(z.z), a.act)); v[3] = __fmul2_rn(v[3], slope2(unpack2(z.w), a.act));
+    if (KIND == kWeights && a.out_f32) {
+        float* p = static_cast<float*>(a.out) + o;
+        if (W == 16) {      // rows begin on 64 bytes
+#pragma unroll
+            for (int i = 0; i < W / 2; i += 4)
+                st_global_v8(p + 2 * i, __float_as_uint(v[i].x), __float_as_uint(v[i].y), __float_as_uint(v[i + 1].x), __float_as_uint(v[i + 1].y),
+                             __float_as_uint(v[i + 2].x), __float_as_uint(v[i + 2].y), __float_as_uint(v[i + 3].x), __float_as_uint(v[i + 3].y));
+        } else {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+        }
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act2(v[i], a.act);
-    }
-    if (a.residual) {
-        const uint4 z = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.residual) + o));
-        const uint32_t w[4] = {z.x, z.y, z.z, z.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 f = unpack2(w[i]); v[i].x += f.x; v[i].y += f.y; }
+        st_bf16<W>(a.out, o, v);
     }
 }
-__device__ __forceinline__ void store8(const LinearArgs& a, size_t o, const float2 (&v)[4]) {
-    if (a.out_f32) {
-        float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.out) + o);
-        p[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-        p[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
-    } else {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + o) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
-    }
-}
+// The array read along with the sums, if there is one.
+template <int KIND>
+__device__ __forceinline__ const void* extra_array(const LinearArgs& a) { return KIND == kForward ? a.residual : KIND == kTowardsX ? a.z_in : nullptr; }
 
 template <int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs a) {
     constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
     constexpr uint32_t kIdesc = idesc(A_MN, B_MN);
+    constexpr uint64_t kStepA = (A_MN ? 2048 : UMMA_K * 2) >> 4, kStepB = (B_MN ? 2048 : UMMA_K * 2) >> 4;   // 16 steps of the reduction
     extern __shared__ unsigned char smraw[];
     unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
     uint64_t* bars = reinterpret_cast<uint64_t*>(base + (size_t)NSTAGE * STAGE_BYTES);
@@ -292,7 +331,9 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     unsigned char* sa = base + (size_t)stage * STAGE_BYTES;
                     unsigned char* sb = sa + A_BYTES;
                     mbar_expect_tx(&full[stage], bytes);
-                    if (A_MN) {
+                    if (A_MN && a.a_chunks) {
+                        tma_load_4d(sa, &tmA, 0, it.lo + kb * BK, m0 / 64, 0, &full[stage]);
+                    } else if (A_MN) {
 #pragma unroll
                         for (int c = 0; c < BM / 64; ++c) tma_load_2d(sa + c * CHUNK_BYTES, &tmA, m0 + 64 * c, it.lo + kb * BK, &full[stage]);
                     } else {
@@ -300,6 +341,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     }
                     if (KIND == kForward) {
                         tma_load_3d(sb, &tmB, kb * BK, n0, it.e, &full[stage]);
+                    } else if (a.b_chunks) {
+                        tma_load_4d(sb, &tmB, 0, KIND == kWeights ? it.lo + kb * BK : kb * BK, n0 / 64, KIND == kWeights ? 0 : it.e, &full[stage]);
                     } else {
 #pragma unroll
                         for (int c = 0; c < BN / 64; ++c) {
@@ -316,7 +359,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
             }
         }
-    } else if (warp == 1) {  // ---- products: the whole warp keeps step, lane 0 issues ----
+    } else if (warp == 1) {  // ---- products: lane 0 issues them alone but for a group's last block, which the warp prepares ----
         int stage = 0; uint32_t phase = 0;
         int acc = 0; uint32_t acc_phase = 0;
         bool ok = true;
@@ -324,39 +367,49 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (!wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_word)) break;
             tc_fence_after();
             const uint32_t tmem_d = tmem_base + (uint32_t)acc * BN;
-            for (int kb = it.kb0; kb < it.kb1; ++kb) {
+            const int left = KIND == kWeights ? it.n - (it.kb1 - 1) * BK : BK;      // rows of the group in the last block
+            const int plain = it.kb1 - it.kb0 - (left < BK ? 1 : 0);                // blocks that are products and nothing else
+            if (lane == 0) {
+                int s = stage; uint32_t ph = phase;
+                for (int i = 0; i < plain; ++i) {
+                    if (!wait_or_abort(&full[s], ph, abort_word)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(base) + (uint32_t)s * STAGE_BYTES;
+                    const uint64_t da = A_MN ? umma_desc_mn(sa) : umma_desc_sw128(sa), db = B_MN ? umma_desc_mn(sa + A_BYTES) : umma_desc_sw128(sa + A_BYTES);
+#pragma unroll
+                    for (int k = 0; k < BK / UMMA_K; ++k)
+                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (i > 0 || k > 0) ? 1u : 0u);
+                    umma_commit(&empty[s]);
+                    if (++s == NSTAGE) { s = 0; ph ^= 1u; }
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            phase ^= (uint32_t)((stage + plain) / NSTAGE) & 1u;
+            stage = (stage + plain) % NSTAGE;
+            if (left < BK) {
                 if (!wait_warp(&full[stage], phase, abort_word)) { ok = false; break; }
                 unsigned char* pa = base + (size_t)stage * STAGE_BYTES;
-                const uint32_t sa = smem_u32(pa), sb = sa + A_BYTES;
-                int steps = BK / UMMA_K;
-                if (KIND == kWeights) {
-                    const int left = it.n - kb * BK;        // rows of the group in this block
-                    if (left < BK) {
-                        steps = (left + UMMA_K - 1) / UMMA_K;
-                        // rows [left, 16 * steps) belong to the next group: zeros.  A row is 128 bytes in each box, whatever
-                        // the swizzle, which moves bytes inside a row only.
-                        const int rows = steps * UMMA_K - left, per = rows * 8;
-                        for (int i = lane; i < (BM + BN) / 64 * per; i += 32) {
-                            const int c = i / per, r = i - c * per;
-                            *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                    }
+                const int steps = (left + UMMA_K - 1) / UMMA_K;
+                // rows [left, 16 * steps) belong to the next group: zeros.  A row is 128 bytes in each box, whatever the swizzle,
+                // which moves bytes inside a row only.
+                const int rows = steps * UMMA_K - left, per = rows * 8;
+                for (int i = lane; i < (BM + BN) / 64 * per; i += 32) {
+                    const int c = i / per, r = i - c * per;
+                    *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
                 }
+                fence_async_smem();
+                __syncwarp();
                 if (lane == 0) {
                     tc_fence_after();
-                    for (int k = 0; k < steps; ++k) {
-                        const uint64_t da = A_MN ? umma_desc_mn(sa + k * 2048) : umma_desc_sw128(sa + k * UMMA_K * 2);
-                        const uint64_t db = B_MN ? umma_desc_mn(sb + k * 2048) : umma_desc_sw128(sb + k * UMMA_K * 2);
-                        umma_f16(tmem_d, da, db, kIdesc, (kb > it.kb0 || k > 0) ? 1u : 0u);
-                    }
+                    const uint64_t da = umma_desc_mn(smem_u32(pa)), db = umma_desc_mn(smem_u32(pa) + A_BYTES);
+                    for (int k = 0; k < steps; ++k)
+                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (plain > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[stage]);
                 }
                 __syncwarp();
                 if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
             }
-            if (!ok) break;
             if (lane == 0) umma_commit(&acc_full[acc]);
             __syncwarp();
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -373,15 +426,19 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (a.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(0, 0, 0, 0);
             }
         } else {
-            const float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
             const long long n = (long long)a.M * (a.N / 8);
             for (int e = 0; e < a.E; ++e) {
                 if (group_of(offsets, e, a.R).n > 0) continue;
                 for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps))
-                    store8(a, (size_t)(e * n + i) * 8, z);
+                    {
+                    float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+                    finish<KIND, 8>(a, e, (size_t)(e * n + i) * 8, 0, z, nullptr);
+                }
             }
         }
         __syncwarp();
+        const void* with = extra_array<KIND>(a);
+        const bool wide_ok = a.N % 16 == 0 && (((uintptr_t)a.out | (uintptr_t)a.z_out | (uintptr_t)with) % 32) == 0;
         int acc = 0; uint32_t acc_phase = 0;
         while (cur.next(it)) {
             if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
@@ -393,27 +450,38 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const int n0 = it.nt * BN;
             float* part = nullptr;
             if (!whole) part = a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + (q * 32 + lane)) * BN;
+            const size_t o0 = row * a.N + n0;
 #pragma unroll 1
             for (int c = half * (BN / 64); c < (half + 1) * (BN / 64); ++c) {
+                const int cols = a.N - n0 - c * 32;      // columns from here to the row's end
+                const bool full32 = wide_ok && cols >= 32;
+                uint32_t extra[16];
+                if (row_ok && whole && full32 && with) { ld_bf16<16>(with, o0 + c * 32, extra); ld_bf16<16>(with, o0 + c * 32 + 16, extra + 8); }
                 __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
                 uint32_t r[32];
                 tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + c * 32), r);
-                if (!row_ok || n0 + c * 32 >= a.N) continue;
+                if (!row_ok || cols <= 0) continue;
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) st_global_v8(part + c * 32 + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
-                    continue;
-                }
+                } else if (full32) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    const int col = n0 + c * 32 + i;
-                    if (col >= a.N) break;
-                    float2 v[4];
+                    for (int i = 0; i < 32; i += 16) {
+                        float2 v[8];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                    const size_t o = row * a.N + col;
-                    if (KIND != kWeights) finish8(a, it.e, o, col, v);
-                    store8(a, o, v);
+                        for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                        finish<KIND, 16>(a, it.e, o0 + c * 32 + i, n0 + c * 32 + i, v, extra + i / 2);
+                    }
+                } else {    // the row's end, or rows that do not begin on 32 bytes
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        if (i >= cols) break;
+                        float2 v[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                        if (with) ld_bf16<8>(with, o0 + c * 32 + i, extra);
+                        finish<KIND, 8>(a, it.e, o0 + c * 32 + i, n0 + c * 32 + i, v, extra);
+                    }
                 }
             }
             tc_fence_before();
@@ -471,8 +539,9 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
             }
             const size_t row = KIND == kWeights ? (size_t)e * a.M + mt * BM + r : (size_t)g.lo + mt * BM + r;
             const size_t o = row * a.N + n0 + col;
-            if (KIND != kWeights) finish8(a, e, o, n0 + col, v);
-            store8(a, o, v);
+            uint32_t extra[4];
+            if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra);
+            finish<KIND, 8>(a, e, o, n0 + col, v, extra);
         }
         return;
     }
@@ -525,14 +594,18 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     a.part = static_cast<float*>(ws);
     a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
     a.a_rows = BM;
+    a.b_chunks = KIND != kForward && a.N % 64 == 0;
     if (KIND == kWeights) {         // dy [R][M], x [R][N]
         const uint64_t da[2] = {(uint64_t)a.M, (uint64_t)a.R}, db[2] = {(uint64_t)a.N, (uint64_t)a.R};
-        if (!make_map(&tmA, A, 2, da, BK) || !make_map(&tmB, B, 2, db, BK)) return LOCMOE_ERR_CUDA;
+        a.a_chunks = a.M % 64 == 0;
+        if (!(a.a_chunks ? make_map_chunks(&tmA, A, a.M, a.R, 1, BK, BM / 64) : make_map(&tmA, A, 2, da, BK))) return LOCMOE_ERR_CUDA;
+        if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.R, 1, BK, BN / 64) : make_map(&tmB, B, 2, db, BK))) return LOCMOE_ERR_CUDA;
     } else {
         while (a.a_rows > 16 && a.a_rows / 2 >= a.R) a.a_rows /= 2;     // few rows: smaller boxes, the tile's other rows hold what they held
         const uint64_t da[2] = {(uint64_t)a.K, (uint64_t)a.R};
         const uint64_t db[3] = {(uint64_t)(KIND == kForward ? a.K : a.N), (uint64_t)(KIND == kForward ? a.N : a.K), (uint64_t)a.E};
-        if (!make_map(&tmA, A, 2, da, a.a_rows) || !make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK)) return LOCMOE_ERR_CUDA;
+        if (!make_map(&tmA, A, 2, da, a.a_rows)) return LOCMOE_ERR_CUDA;
+        if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.K, a.E, BK, BN / 64) : make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK))) return LOCMOE_ERR_CUDA;
     }
     static bool attr_done_dev[64] = {false};   // the attribute is per device
     int dev = 0;

@@ -662,6 +662,20 @@ bool make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same memory as [outer][cols / 64][rows][64], cols a multiple of 64, with a box of `chunks` x box_rows x 64 elements: one
+// load brings the boxes of 64 columns that make up an MN-major tile.
+bool make_map_chunks(CUtensorMap* map, const void* ptr, uint64_t cols, uint64_t rows, uint64_t outer, uint32_t box_rows, uint32_t chunks) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t gdim[4] = {(cuuint64_t)BK, rows, cols / BK, outer};
+    cuuint64_t gstr[3] = {cols * 2, (cuuint64_t)BK * 2, cols * rows * 2};
+    cuuint32_t box[4] = {(cuuint32_t)BK, box_rows, chunks, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), gdim, gstr, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 int launch_gemm(const void* A, const void* W, void* out, int out_f32, int gelu, int E, int M, int N, int K,

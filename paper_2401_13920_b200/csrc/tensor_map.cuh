@@ -9,6 +9,8 @@ namespace locmoe {
 
 // K-major bf16 matrix [outer...][rows][K] with a box of box_rows x 64 elements, 128-byte swizzle; false on failure.
 bool make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, uint32_t box_rows);
+// Row-major bf16 [outer][rows][cols], cols a multiple of 64, as [outer][cols / 64][rows][64] with a box of chunks x box_rows x 64.
+bool make_map_chunks(CUtensorMap* map, const void* ptr, uint64_t cols, uint64_t rows, uint64_t outer, uint32_t box_rows, uint32_t chunks);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
