@@ -545,6 +545,7 @@ int locmoe_sort(const locmoe_shape_t* shape, int32_t K, const int32_t* idx_k, co
     const int esz = shape->x_dtype == LOCMOE_F32 ? 4 : 2;
     if (!element_aligned(x, esz) || !element_aligned(xs, esz)) return LOCMOE_ERR_ALIGN;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (x && sort_is_few(shape->T, K)) return launch_sort_few(*shape, K, idx_k, x, offsets, slot, inv, load, xs, st);
     rc = launch_sort_plan(shape->T, K, shape->E, idx_k, offsets, slot, inv, load, st);
     if (rc == LOCMOE_OK && x) rc = launch_sort_rows(*shape, K, x, offsets, slot, xs, st);
     return rc;

@@ -26,13 +26,17 @@ namespace locmoe {
 
 namespace {
 
-constexpr int BM = 128, BN = 256, BK = 64, NSTAGE = 4, UMMA_K = 16;
-constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int BM = 128, BN = 256, BK = 64, UMMA_K = 16;
+constexpr int kMaxStages = 6;                       // four of whole tiles, six where the rows are few
+constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
 constexpr uint32_t CHUNK_BYTES = 64 * BK * 2;       // 64 columns of an MN-major tile
-constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kEpiWarps = 8, kSumWarps = 4;         // the latter only where the weights' gradient comes with the bias's
+constexpr int kThreads = 64 + 32 * kEpiWarps, kWeightsThreads = kThreads + 32 * kSumWarps;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int kMaxE = 1024;
-constexpr size_t kSmem = 1024 /*alignment slack*/ + (size_t)NSTAGE * STAGE_BYTES + 256 /*barriers*/ + (kMaxE + 1) * sizeof(int);
+constexpr size_t kRing = 6 * (size_t)(16 * BK * 2 + B_BYTES);     // 204 KB, a little more than four whole stages
+constexpr size_t kSmem = 1024 /*alignment slack*/ + kRing + 256 /*barriers*/ + (kMaxE + 1) * sizeof(int);
+static_assert(4 * (A_BYTES + B_BYTES) <= kRing && kSmem <= 227 * 1024, "the ring fits");
 
 __device__ int g_linear_flags = 0;   // bit 0: a bounded wait gave up
 
@@ -46,9 +50,12 @@ struct LinearArgs {
     const void* residual;       // bf16 [R][N] or nullptr
     const void* z_in;           // bf16 [R][N]: multiply by act'(z_in); nullptr: no factor
     float* part;                // [grid][2][part_rows][BN]
+    float* db;                  // weights only: [E][M] or nullptr
+    float* db_part;             // [grid][2][BM]
     int act, out_f32;
     int E, R, M, N, K;          // M: rows of a weight (weights only)
     int n_tiles, a_rows;        // rows of one A box
+    int stages;                 // of the ring
     int a_chunks, b_chunks;     // 1: one load brings an MN-major tile, else one for each 64 columns
     int part_rows;
     int grid, deal_waves;       // runs instead of tiles up to this many waves of tiles
@@ -113,7 +120,16 @@ __device__ __forceinline__ int deal(const LinearArgs& a, const Totals& s) {
     const long long r = s.units / 4;
     return r < 1 ? 1 : r < a.grid ? (int)r : a.grid;
 }
-__device__ __forceinline__ long long run_begin(const Totals& s, int runs, int c) { return s.units * c / runs; }
+// Where run c begins: `each` blocks a run, one more in the first `more`.
+struct Runs {
+    int n;
+    long long each;
+    int more;
+    __device__ __forceinline__ Runs(const Totals& s, int runs) : n(runs), each(0), more(0) {
+        if (runs) { each = s.units / runs; more = (int)(s.units - each * runs); }
+    }
+    __device__ __forceinline__ long long begin(int c) const { return each * c + min(c, more); }
+};
 
 struct Item {
     int e, lo, n;               // group, its first row, its rows
@@ -132,10 +148,10 @@ struct Cursor {
     long long base;             // first tile or block of group e
     Group g;
     int kb, per;                // blocks a tile, tiles of group e
-    __device__ __forceinline__ Cursor(const LinearArgs& a_, const int* off, const Totals& s, int runs_, int c) : a(a_), offsets(off), runs(runs_), e(-1), base(0) {
+    __device__ __forceinline__ Cursor(const LinearArgs& a_, const int* off, const Totals& s, const Runs& r, int c) : a(a_), offsets(off), runs(r.n), e(-1), base(0) {
         g = Group{0, 0};
         kb = per = 0;
-        if (runs) { at = c < runs ? run_begin(s, runs, c) : 0; end = c < runs ? run_begin(s, runs, c + 1) : 0; }
+        if (runs) { at = c < runs ? r.begin(c) : 0; end = c < runs ? r.begin(c + 1) : 0; }
         else { at = c; end = s.tiles; }
     }
     __device__ __forceinline__ bool next(Item& it) {
@@ -278,26 +294,29 @@ template <int KIND>
 __device__ __forceinline__ const void* extra_array(const LinearArgs& a) { return KIND == kForward ? a.residual : KIND == kTowardsX ? a.z_in : nullptr; }
 
 template <int KIND>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(KIND == kWeights ? kWeightsThreads : kThreads, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs a) {
     constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
     constexpr uint32_t kIdesc = idesc(A_MN, B_MN);
     constexpr uint64_t kStepA = (A_MN ? 2048 : UMMA_K * 2) >> 4, kStepB = (B_MN ? 2048 : UMMA_K * 2) >> 4;   // 16 steps of the reduction
     extern __shared__ unsigned char smraw[];
     unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(base + (size_t)NSTAGE * STAGE_BYTES);
-    uint64_t* full = bars;                   // [NSTAGE] operands landed
-    uint64_t* empty = bars + NSTAGE;         // [NSTAGE] products that read the stage are done
-    uint64_t* acc_full = bars + 2 * NSTAGE;  // [2] accumulator complete
+    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing);
+    uint64_t* full = bars;                   // [stages] operands landed
+    uint64_t* empty = bars + kMaxStages;     // [stages] products (and column sums) that read the stage are done
+    uint64_t* acc_full = bars + 2 * kMaxStages;  // [2] accumulator complete
     uint64_t* acc_empty = acc_full + 2;      // [2] accumulator drained
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    int* offsets = reinterpret_cast<int*>(base + (size_t)NSTAGE * STAGE_BYTES + 256);   // [E + 1]
+    int* offsets = reinterpret_cast<int*>(base + kRing + 256);   // [E + 1]
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int NSTAGE = a.stages;
+    const uint32_t a_bytes = (uint32_t)a.a_rows * BK * 2, STAGE_BYTES = a_bytes + B_BYTES;   // products read on beyond a short A: into B, for rows of no account
+    const bool with_db = KIND == kWeights && a.db;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < NSTAGE; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], kEpiWarps); }
+        for (int s = 0; s < NSTAGE; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], with_db ? 1 + kSumWarps : 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], with_db ? kEpiWarps + kSumWarps : kEpiWarps); }
         *abort_word = 0;
         mbar_init_fence();
         prefetch_map(&tmA);
@@ -309,28 +328,26 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
     pdl_wait();
     pdl_trigger();
-    for (int i = threadIdx.x; i <= a.E; i += kThreads) offsets[i] = __ldg(a.offsets + i);
+    for (int i = threadIdx.x; i <= a.E; i += blockDim.x) offsets[i] = __ldg(a.offsets + i);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     const Totals sum = totals<KIND>(a, offsets, lane);
-    const int runs = deal(a, sum);
-    Cursor<KIND> cur(a, offsets, sum, runs, blockIdx.x);
+    Cursor<KIND> cur(a, offsets, sum, Runs(sum, deal(a, sum)), blockIdx.x);
     Item it;
 
     if (warp == 0) {
         if (lane == 0) {  // ---- loads ----
             int stage = 0; uint32_t phase = 0;
-            const uint32_t bytes = (A_MN ? A_BYTES : (uint32_t)a.a_rows * BK * 2) + B_BYTES;
             bool ok = true;
             while (ok && cur.next(it)) {
                 const int m0 = it.mt * BM, n0 = it.nt * BN;
                 for (int kb = it.kb0; kb < it.kb1; ++kb) {
                     if (!wait_or_abort(&empty[stage], phase ^ 1u, abort_word)) { ok = false; break; }
                     unsigned char* sa = base + (size_t)stage * STAGE_BYTES;
-                    unsigned char* sb = sa + A_BYTES;
-                    mbar_expect_tx(&full[stage], bytes);
+                    unsigned char* sb = sa + a_bytes;
+                    mbar_expect_tx(&full[stage], STAGE_BYTES);
                     if (A_MN && a.a_chunks) {
                         tma_load_4d(sa, &tmA, 0, it.lo + kb * BK, m0 / 64, 0, &full[stage]);
                     } else if (A_MN) {
@@ -375,11 +392,12 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     if (!wait_or_abort(&full[s], ph, abort_word)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t sa = smem_u32(base) + (uint32_t)s * STAGE_BYTES;
-                    const uint64_t da = A_MN ? umma_desc_mn(sa) : umma_desc_sw128(sa), db = B_MN ? umma_desc_mn(sa + A_BYTES) : umma_desc_sw128(sa + A_BYTES);
+                    const uint64_t da = A_MN ? umma_desc_mn(sa) : umma_desc_sw128(sa), db = B_MN ? umma_desc_mn(sa + a_bytes) : umma_desc_sw128(sa + a_bytes);
 #pragma unroll
                     for (int k = 0; k < BK / UMMA_K; ++k)
                         umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (i > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[s]);
+                    if (with_db && it.nt != 0) mbar_arrive_n(&empty[s], kSumWarps);    // nobody else reads this stage
                     if (++s == NSTAGE) { s = 0; ph ^= 1u; }
                 }
             }
@@ -402,10 +420,11 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 __syncwarp();
                 if (lane == 0) {
                     tc_fence_after();
-                    const uint64_t da = umma_desc_mn(smem_u32(pa)), db = umma_desc_mn(smem_u32(pa) + A_BYTES);
+                    const uint64_t da = umma_desc_mn(smem_u32(pa)), db = umma_desc_mn(smem_u32(pa) + a_bytes);
                     for (int k = 0; k < steps; ++k)
                         umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (plain > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[stage]);
+                    if (with_db && it.nt != 0) mbar_arrive_n(&empty[stage], kSumWarps);
                 }
                 __syncwarp();
                 if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
@@ -413,6 +432,60 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (lane == 0) umma_commit(&acc_full[acc]);
             __syncwarp();
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    } else if (KIND == kWeights && warp >= 2 + kEpiWarps) {
+        // ---- column sums of dy, from the A tiles of the first column of output tiles: a warp 32 columns, a lane 8 of them in
+        // every eighth row.  Four lanes' units of 16 bytes in rows r and r + 4 fill the banks once, swizzled as they are.
+        // Each tile's accumulator is waited for and released like the epilogue does, so that these warps never fall a phase behind.
+        if (with_db) {
+            const int w = warp - 2 - kEpiWarps, o = w * 4 + (lane & 3), r0 = ((lane >> 2) & 1) * 4 + (lane >> 3);
+            const uint32_t at = (uint32_t)(o >> 3) * CHUNK_BYTES + (uint32_t)(((o & 7) ^ r0) << 4) + (uint32_t)r0 * 128;
+            int stage = 0; uint32_t phase = 0;
+            int acc = 0; uint32_t acc_phase = 0;
+            bool ok = true;
+            while (ok && cur.next(it)) {
+                const int n = it.kb1 - it.kb0;
+                if (it.nt == 0) {
+                    float2 v[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+                    for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                        if (!wait_warp(&full[stage], phase, abort_word)) { ok = false; break; }
+                        const unsigned char* p = base + (size_t)stage * STAGE_BYTES + at;
+                        const int left = it.n - kb * BK;
+#pragma unroll
+                        for (int i = 0; i < BK / 8; ++i) {
+                            if (r0 + 8 * i >= left) break;
+                            const uint4 q = *reinterpret_cast<const uint4*>(p + i * 1024);
+                            v[0] = __fadd2_rn(v[0], unpack2(q.x)); v[1] = __fadd2_rn(v[1], unpack2(q.y));
+                            v[2] = __fadd2_rn(v[2], unpack2(q.z)); v[3] = __fadd2_rn(v[3], unpack2(q.w));
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&empty[stage]);
+                        if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, d);
+                            v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, d);
+                        }
+                    }
+                    const int col = it.mt * BM + o * 8;
+                    float* out = n == it.kb ? (col < a.M ? a.db + (size_t)it.e * a.M + col : nullptr)
+                                            : a.db_part + ((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * BM + o * 8;
+                    if (lane < 4 && out) {
+                        reinterpret_cast<float4*>(out)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+                        reinterpret_cast<float4*>(out)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+                    }
+                } else {
+                    phase ^= (uint32_t)((stage + n) / NSTAGE) & 1u;
+                    stage = (stage + n) % NSTAGE;
+                }
+                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
+                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
         }
     } else {  // ---- epilogue: TMEM lane quadrant = warp % 4, column half = (warp - 2) / 4 ----
         const int q = warp & 3, half = (warp - 2) >> 2;
@@ -429,6 +502,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const long long n = (long long)a.M * (a.N / 8);
             for (int e = 0; e < a.E; ++e) {
                 if (group_of(offsets, e, a.R).n > 0) continue;
+                if (a.db && e % (int)gridDim.x == (int)blockIdx.x)
+                    for (int i = et; i < a.M; i += 32 * kEpiWarps) a.db[(size_t)e * a.M + i] = 0.0f;
                 for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps))
                     {
                     float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
@@ -503,6 +578,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // Adds up the sums of the tiles that more than one run worked on, in the order of the runs, and finishes them.  CTA (x, y): the
 // tile in which run x ends, if it began in run x as well (so that each such tile has one owner), every gridDim.y-th piece.
 constexpr int kJoinThreads = 256, kJoinParts = 8;
+static_assert(kJoinThreads >= BM, "a thread for each row of a tile");
 template <int KIND>
 __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearArgs a) {
     __shared__ int offsets[kMaxE + 1];
@@ -511,9 +587,10 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
     for (int i = threadIdx.x; i <= a.E; i += kJoinThreads) offsets[i] = __ldg(a.offsets + i);
     __syncthreads();
     const Totals s = totals<KIND>(a, offsets, threadIdx.x & 31);
-    const int runs = deal(a, s), c0 = blockIdx.x;
-    if (c0 + 1 >= runs) return;
-    const long long cut = run_begin(s, runs, c0 + 1);       // the first block of the next run
+    const Runs runs(s, deal(a, s));
+    const int c0 = blockIdx.x;
+    if (c0 + 1 >= runs.n) return;
+    const long long cut = runs.begin(c0 + 1);               // the first block of the next run
     const Tiles<KIND> t{a, offsets};
     long long base = 0;
     for (int e = 0; e < a.E; ++e) {
@@ -523,31 +600,53 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
         if (cut >= base + size) { base += size; continue; }
         const int tile = (int)((cut - base) / kb);
         const long long begin = base + (long long)tile * kb, end = begin + kb;
-        if (begin == cut || begin < run_begin(s, runs, c0)) return;     // the cut is between tiles, or an earlier run owns the tile
+        if (begin == cut || begin < runs.begin(c0)) return;             // the cut is between tiles, or an earlier run owns the tile
         int c1 = c0 + 1;                                                // last run that worked on the tile
-        while (c1 + 1 < runs && run_begin(s, runs, c1 + 1) < end) ++c1;
+        while (c1 + 1 < runs.n && runs.begin(c1 + 1) < end) ++c1;
         const int mts = t.m_tiles(g), nt = tile / mts, mt = tile - nt * mts, n0 = nt * BN;
         const int rows = min(BM, (KIND == kWeights ? a.M : g.n) - mt * BM), cols = min(BN, a.N - n0) / 8;
+        if (KIND == kWeights && a.db && nt == 0 && blockIdx.y == 0) {
+            const int i = threadIdx.x;
+            if (i < rows) {
+                float sum = __ldcg(a.db_part + ((size_t)c0 * 2 + 1) * BM + i);
+                for (int c = c0 + 1; c <= c1; ++c) sum += __ldcg(a.db_part + (size_t)c * 2 * BM + i);
+                a.db[(size_t)e * a.M + mt * BM + i] = sum;
+            }
+        }
+        const size_t step = (size_t)2 * a.part_rows * BN;               // from a run's sums to the next one's
         for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < rows * cols; i += gridDim.y * kJoinThreads) {
             const int r = i / cols, col = (i - r * cols) * 8;
-            float2 v[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
-            for (int c = c0; c <= c1; ++c) {
-                const float4* p = reinterpret_cast<const float4*>(a.part + (((size_t)c * 2 + (c == c0 ? 1 : 0)) * a.part_rows + r) * BN + col);
-                const float4 p0 = __ldcg(p), p1 = __ldcg(p + 1);
-                v[0].x += p0.x; v[0].y += p0.y; v[1].x += p0.z; v[1].y += p0.w;
-                v[2].x += p1.x; v[2].y += p1.y; v[3].x += p1.z; v[3].y += p1.w;
-            }
             const size_t row = KIND == kWeights ? (size_t)e * a.M + mt * BM + r : (size_t)g.lo + mt * BM + r;
             const size_t o = row * a.N + n0 + col;
             uint32_t extra[4];
             if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra);
+            // the first run's part is its second slot's, the others' their first
+            const float* p = a.part + (((size_t)c0 * 2 + 1) * a.part_rows + r) * BN + col;
+            const float4 f0 = __ldcg(reinterpret_cast<const float4*>(p)), f1 = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+            float2 v[4] = {{f0.x, f0.y}, {f0.z, f0.w}, {f1.x, f1.y}, {f1.z, f1.w}};
+            p = a.part + (((size_t)c0 * 2 + 2) * a.part_rows + r) * BN + col;
+            for (int c = c0 + 1; c <= c1; c += 4, p += 4 * step) {      // four runs' sums in flight
+                float4 q[4][2];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (c + k > c1) break;
+                    q[k][0] = __ldcg(reinterpret_cast<const float4*>(p + k * step));
+                    q[k][1] = __ldcg(reinterpret_cast<const float4*>(p + k * step) + 1);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (c + k > c1) break;
+                    v[0].x += q[k][0].x; v[0].y += q[k][0].y; v[1].x += q[k][0].z; v[1].y += q[k][0].w;
+                    v[2].x += q[k][1].x; v[2].y += q[k][1].y; v[3].x += q[k][1].z; v[3].y += q[k][1].w;
+                }
+            }
             finish<KIND, 8>(a, e, o, n0 + col, v, extra);
         }
         return;
     }
 }
 
-// db[e] = sum of the group's rows of dy, in a fixed order: a CTA takes 64 columns of one expert, a warp every eighth row.
+// db without dw: db[e] = sum of the group's rows of dy, in a fixed order: a CTA takes 64 columns of one expert, a warp every eighth row.
 constexpr int kBiasThreads = 256;
 __global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const int32_t* __restrict__ offsets, const uint16_t* __restrict__ dy, int R, int N,
                                                                         float* __restrict__ db) {
@@ -593,6 +692,7 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     a.deal_waves = kDealWaves;
     a.part = static_cast<float*>(ws);
     a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
+    a.db_part = a.part + (size_t)a.grid * 2 * BM * BN;      // behind whole tiles
     a.a_rows = BM;
     a.b_chunks = KIND != kForward && a.N % 64 == 0;
     if (KIND == kWeights) {         // dy [R][M], x [R][N]
@@ -607,6 +707,8 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         if (!make_map(&tmA, A, 2, da, a.a_rows)) return LOCMOE_ERR_CUDA;
         if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.K, a.E, BK, BN / 64) : make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK))) return LOCMOE_ERR_CUDA;
     }
+    a.stages = (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
+    if (a.stages > kMaxStages) a.stages = kMaxStages;
     static bool attr_done_dev[64] = {false};   // the attribute is per device
     int dev = 0;
     cudaGetDevice(&dev);
@@ -617,7 +719,7 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         }
         attr_done_dev[dev & 63] = true;
     }
-    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(kThreads), kSmem, st, tmA, tmB, a);
+    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, a);
     if (rc) return rc;
     // without the join where the tiles are too many for runs whatever the groups are
     const long long least = KIND == kWeights ? (long long)((a.M + BM - 1) / BM) * a.n_tiles : 0;
@@ -632,7 +734,8 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
 
 // Two tiles' sums a CTA.
 size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad) {
-    return (size_t)sm_count() * 2 * (grad || s.T > BM ? BM : s.T) * BN * sizeof(float);
+    const size_t rows = grad || s.T > BM ? BM : s.T, sums = rows * BN + (grad ? BM : 0);
+    return ((size_t)sm_count() * 2 * sums * sizeof(float) + 255) & ~(size_t)255;
 }
 
 int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_linear_t& l, void* ws, cudaStream_t st) {
@@ -654,12 +757,12 @@ int launch_expert_linear_grad(const locmoe_shape_t& s, int N, const locmoe_exper
     }
     if (l.dw) {
         LinearArgs a{};
-        a.offsets = l.offsets; a.out = l.dw; a.out_f32 = l.dw_dtype == LOCMOE_F32;
+        a.offsets = l.offsets; a.out = l.dw; a.out_f32 = l.dw_dtype == LOCMOE_F32; a.db = l.db;
         a.E = s.E; a.R = s.T; a.M = N; a.N = s.H;
         rc = launch_gemm<kWeights>(a, l.dy, l.x, ws, st);
         if (rc) return rc;
     }
-    if (l.db) {
+    if (l.db && !l.dw) {
         rc = launch_pdl(expert_bias_grad_kernel, dim3((N + 63) / 64, s.E), dim3(kBiasThreads), 0, st, l.offsets, static_cast<const uint16_t*>(l.dy), (int)s.T, N, l.db);
         if (rc) return rc;
     }

@@ -185,6 +185,58 @@ template <> struct Unit<LOCMOE_F32, false> {
     static __device__ __forceinline__ Raw zero() { return 0u; }
 };
 
+// Order and rows of a few assignments in one launch: CTA v finds the row of assignment v by counting the assignments that come
+// before it, and copies the token there; the assignments that are not routed take the rows behind the last group, in
+// order, as rows of zeros.  The CTAs after those count for the offsets.  V^2 reads of the index array out of L2 and L1: up to
+// kFewMax assignments that is less than the second launch it saves (8 tokens x 2 choices: ... against ... us).
+constexpr int kFewThreads = 128, kFewMax = 512;
+template <typename R>
+__global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const int32_t* __restrict__ idx, int V, int T, int E, const R* __restrict__ x, int U,
+                                                               int32_t* __restrict__ offsets, int32_t* __restrict__ slot, int32_t* __restrict__ inv,
+                                                               int32_t* __restrict__ load, R* __restrict__ xs) {
+    pdl_wait();
+    pdl_trigger();
+    if ((int)blockIdx.x >= V) {
+        const int e = ((int)blockIdx.x - V) * kFewThreads + threadIdx.x;
+        if (e > E) return;
+        int below = 0, first = 0;
+        for (int u = 0; u < V; ++u) {
+            const int k = __ldg(idx + u);
+            below += k >= 0 && k < e;
+            first += u < T && k == e;
+        }
+        offsets[e] = below;
+        if (load && e < E) load[e] = first;
+        return;
+    }
+    const int v = blockIdx.x, key = __ldg(idx + v), t = v % T;
+    const bool ok = key >= 0 && key < E;
+    constexpr int CH = sizeof(R) == 16 ? 4 : 8;
+    R r[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (ok && (int)threadIdx.x + i * kFewThreads < U) r[i] = x[(size_t)t * U + threadIdx.x + i * kFewThreads];
+    int row = 0;
+    for (int u = threadIdx.x; u - (int)threadIdx.x < V; u += kFewThreads) {
+        const int k = u < V ? __ldg(idx + u) : -1;
+        const bool routed = k >= 0 && k < E;
+        row += __syncthreads_count(u < V && (ok ? routed && (k < key || (k == key && u < v)) : routed || u < v));
+    }
+    if (threadIdx.x == 0) {
+        slot[v] = ok ? row : -1;
+        inv[row] = ok ? v : -1;
+    }
+    for (int u0 = threadIdx.x; u0 < U; u0 += CH * kFewThreads) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int u = u0 + i * kFewThreads;
+            if (u >= U) break;
+            if (u0 != (int)threadIdx.x && ok) r[i] = x[(size_t)t * U + u];
+            xs[(size_t)row * U + u] = ok ? r[i] : R{};
+        }
+    }
+}
+
 // What a row kernel works on.  `width` lanes (a power of two) share a token; a CTA owns `tpc` consecutive tokens.
 struct RowArgs {
     int T, U, K, E;             // tokens, units a row, choices, experts
@@ -490,21 +542,28 @@ __global__ void __launch_bounds__(kThreads) sort_grad_router_kernel(const RowArg
     }
 }
 
-// deps[e] = sum of the CTAs' sums, in a fixed order: 32 experts a CTA, the rows dealt to 8 warps.
-__global__ void __launch_bounds__(kThreads) deps_finish_kernel(const float* __restrict__ part, int n, int E, float* __restrict__ deps) {
-    __shared__ float sm[kWarps][32];
+// deps[e] = sum of the CTAs' sums, in a fixed order: 32 experts a CTA, the rows dealt to 32 warps, eight loads in flight.
+constexpr int kFinishThreads = 1024;
+__global__ void __launch_bounds__(kFinishThreads) deps_finish_kernel(const float* __restrict__ part, int n, int E, float* __restrict__ deps) {
+    __shared__ float sm[32][33];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (e < E)
-        for (int r = warp; r < n; r += kWarps) sum += part[(size_t)r * E + e];
+        for (int r = warp; r < n; r += 32 * 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = r + 32 * i < n ? __ldcg(part + (size_t)(r + 32 * i) * E + e) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
     sm[warp][lane] = sum;
     __syncthreads();
-    if (warp == 0 && e < E) {
-        for (int w = 1; w < kWarps; ++w) sum += sm[w][lane];
-        deps[e] = sum;
-    }
+    sum = sm[lane][warp];           // expert `warp` of the CTA's 32
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0 && blockIdx.x * 32 + warp < E) deps[blockIdx.x * 32 + warp] = sum;
 }
 
 bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }   // an absent array is
@@ -589,6 +648,24 @@ int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, 
     return check_launch();
 }
 
+// Whether locmoe_sort is one launch.
+bool sort_is_few(int T, int K) { return (long long)K * T <= kFewMax; }
+
+int launch_sort_few(const locmoe_shape_t& s, int K, const int32_t* idx, const void* x, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load,
+                    void* xs, cudaStream_t st) {
+    const int V = K * s.T, esz = s.x_dtype == LOCMOE_F32 ? 4 : 2;
+    const long long bytes = (long long)s.H * esz;
+    const dim3 grid(V + (s.E + kFewThreads) / kFewThreads), block(kFewThreads);      // E + 1 offsets
+    int rc;
+    if (bytes % 16 == 0 && aligned16(x) && aligned16(xs))
+        rc = launch_pdl(sort_few_kernel<uint4>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint4*)x, (int)(bytes / 16), offsets, slot, inv, load, (uint4*)xs);
+    else if (esz == 4)
+        rc = launch_pdl(sort_few_kernel<uint32_t>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint32_t*)x, (int)s.H, offsets, slot, inv, load, (uint32_t*)xs);
+    else
+        rc = launch_pdl(sort_few_kernel<uint16_t>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint16_t*)x, (int)s.H, offsets, slot, inv, load, (uint16_t*)xs);
+    return rc ? rc : check_launch();
+}
+
 int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st) {
     const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
     const bool vec = s.H % n == 0 && aligned16(x) && aligned16(xs);
@@ -639,7 +716,7 @@ int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g
     const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, U / s.E, 1.0f / (float)(s.H / s.E)};
     int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_grad_router_dt, (int)grid, warps, per * warps, a, b, g.dxs, g.slot, g.dx, st);
     if (rc == LOCMOE_OK && g.deps)
-        rc = launch_pdl(deps_finish_kernel, dim3((s.E + 31) / 32), dim3(kThreads), 0, st, (const float*)ws, (int)grid, s.E, g.deps);
+        rc = launch_pdl(deps_finish_kernel, dim3((s.E + 31) / 32), dim3(kFinishThreads), 0, st, (const float*)ws, (int)grid, s.E, g.deps);
     return rc ? rc : check_launch();
 }
 

@@ -12,6 +12,9 @@ namespace locmoe {
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive_n(uint64_t* bar, uint32_t n) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
 // After a wait has been given up: asynchronous work this CTA started (bulk tensor loads that write its shared
 // memory and count on its barriers, tcgen05.commit arrivals) may still be in flight, and a CTA must not leave
 // while it is.  Nothing tells when the last of it has landed once the barriers' phases are out of step, so the
