@@ -40,6 +40,12 @@ static_assert(4 * (A_BYTES + B_BYTES) <= kRing && kSmem <= 227 * 1024, "the ring
 
 __device__ int g_linear_flags = 0;   // bit 0: a bounded wait gave up
 
+// A tile whose first blocks are run c's last ones, left to the kernel that joins: written by CTA c, rows = 0 if there is none.
+struct __align__(16) Split {
+    int e, row, rows, nt;       // expert, the tile's first row in the output, its rows, its column
+    int last, pad[3];           // last run that worked on it
+};
+
 enum Kind { kForward = 0, kTowardsX = 1, kWeights = 2 };
 
 struct LinearArgs {
@@ -52,6 +58,7 @@ struct LinearArgs {
     float* part;                // [grid][2][part_rows][BN]
     float* db;                  // weights only: [E][M] or nullptr
     float* db_part;             // [grid][2][BM]
+    Split* split;               // [grid]
     int act, out_f32;
     int E, R, M, N, K;          // M: rows of a weight (weights only)
     int n_tiles, a_rows;        // rows of one A box
@@ -135,6 +142,7 @@ struct Item {
     int e, lo, n;               // group, its first row, its rows
     int mt, nt;                 // tile
     int kb0, kb1, kb;           // blocks of this item, blocks of the tile
+    long long begin;            // by runs: the tile's first block
 };
 
 // Walks through one CTA's share.
@@ -171,7 +179,8 @@ struct Cursor {
         if (runs) {
             const long long rel = at - base;
             tile = (int)(rel / kb);
-            it.kb0 = (int)(rel - (long long)tile * kb);
+            it.begin = base + (long long)tile * kb;
+            it.kb0 = (int)(at - it.begin);
             const long long left = end - at;
             it.kb1 = left < kb - it.kb0 ? it.kb0 + (int)left : kb;
             at += it.kb1 - it.kb0;
@@ -334,7 +343,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     const Totals sum = totals<KIND>(a, offsets, lane);
-    Cursor<KIND> cur(a, offsets, sum, Runs(sum, deal(a, sum)), blockIdx.x);
+    const Runs runs(sum, deal(a, sum));
+    Cursor<KIND> cur(a, offsets, sum, runs, blockIdx.x);
     Item it;
 
     if (warp == 0) {
@@ -514,8 +524,17 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         __syncwarp();
         const void* with = extra_array<KIND>(a);
         const bool wide_ok = a.N % 16 == 0 && (((uintptr_t)a.out | (uintptr_t)a.z_out | (uintptr_t)with) % 32) == 0;
+        Split split{};
         int acc = 0; uint32_t acc_phase = 0;
         while (cur.next(it)) {
+            if (runs.n && it.kb0 == 0 && it.kb1 < it.kb) {
+                split.e = it.e;
+                split.row = it.mt * BM + (KIND == kWeights ? 0 : it.lo);
+                split.rows = min(BM, (KIND == kWeights ? a.M : it.n) - it.mt * BM);
+                split.nt = it.nt;
+                split.last = blockIdx.x + 1;
+                while (split.last + 1 < runs.n && runs.begin(split.last + 1) < it.begin + it.kb) ++split.last;
+            }
             if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
             tc_fence_after();
             const int r_in = it.mt * BM + q * 32 + lane;
@@ -564,6 +583,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (lane == 0) mbar_arrive(&acc_empty[acc]);
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
+        if (et == 0 && a.split) a.split[blockIdx.x] = split;
     }
     tc_fence_before();
     __syncthreads();
@@ -575,74 +595,55 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
 }
 
-// Adds up the sums of the tiles that more than one run worked on, in the order of the runs, and finishes them.  CTA (x, y): the
-// tile in which run x ends, if it began in run x as well (so that each such tile has one owner), every gridDim.y-th piece.
+// Adds up the sums of the tiles that more than one run worked on, in the order of the runs, and finishes them.  CTA (x, y): run
+// x's split tile, every gridDim.y-th piece.  What tile that is the GEMM has written down; finding it anew cost every warp
+// here a few thousand cycles (200 rows of 1600 x 4096, 23 experts: 15 against ... us).
 constexpr int kJoinThreads = 256, kJoinParts = 8;
 static_assert(kJoinThreads >= BM, "a thread for each row of a tile");
 template <int KIND>
 __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearArgs a) {
-    __shared__ int offsets[kMaxE + 1];
     pdl_wait();
     pdl_trigger();
-    for (int i = threadIdx.x; i <= a.E; i += kJoinThreads) offsets[i] = __ldg(a.offsets + i);
-    __syncthreads();
-    const Totals s = totals<KIND>(a, offsets, threadIdx.x & 31);
-    const Runs runs(s, deal(a, s));
     const int c0 = blockIdx.x;
-    if (c0 + 1 >= runs.n) return;
-    const long long cut = runs.begin(c0 + 1);               // the first block of the next run
-    const Tiles<KIND> t{a, offsets};
-    long long base = 0;
-    for (int e = 0; e < a.E; ++e) {
-        const Group g = group_of(offsets, e, a.R);
-        const int kb = t.kblocks(g), per = t.tiles(g);
-        const long long size = (long long)kb * per;
-        if (cut >= base + size) { base += size; continue; }
-        const int tile = (int)((cut - base) / kb);
-        const long long begin = base + (long long)tile * kb, end = begin + kb;
-        if (begin == cut || begin < runs.begin(c0)) return;             // the cut is between tiles, or an earlier run owns the tile
-        int c1 = c0 + 1;                                                // last run that worked on the tile
-        while (c1 + 1 < runs.n && runs.begin(c1 + 1) < end) ++c1;
-        const int mts = t.m_tiles(g), nt = tile / mts, mt = tile - nt * mts, n0 = nt * BN;
-        const int rows = min(BM, (KIND == kWeights ? a.M : g.n) - mt * BM), cols = min(BN, a.N - n0) / 8;
-        if (KIND == kWeights && a.db && nt == 0 && blockIdx.y == 0) {
-            const int i = threadIdx.x;
-            if (i < rows) {
-                float sum = __ldcg(a.db_part + ((size_t)c0 * 2 + 1) * BM + i);
-                for (int c = c0 + 1; c <= c1; ++c) sum += __ldcg(a.db_part + (size_t)c * 2 * BM + i);
-                a.db[(size_t)e * a.M + mt * BM + i] = sum;
+    const int4 s0 = __ldcg(reinterpret_cast<const int4*>(a.split + c0));
+    const int last = __ldcg(&a.split[c0].last);
+    const int e = s0.x, rows = s0.z, n0 = s0.w * BN;
+    if (rows == 0) return;
+    const size_t row0 = KIND == kWeights ? (size_t)e * a.M + s0.y : (size_t)s0.y;
+    const int cols = min(BN, a.N - n0) / 8;
+    if (KIND == kWeights && a.db && n0 == 0 && blockIdx.y == 0 && (int)threadIdx.x < rows) {
+        const int i = threadIdx.x;
+        float sum = __ldcg(a.db_part + ((size_t)c0 * 2 + 1) * BM + i);
+        for (int c = c0 + 1; c <= last; ++c) sum += __ldcg(a.db_part + (size_t)c * 2 * BM + i);
+        a.db[row0 + i] = sum;
+    }
+    const size_t step = (size_t)2 * a.part_rows * BN;               // from a run's sums to the next one's
+    for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < rows * cols; i += gridDim.y * kJoinThreads) {
+        const int r = i / cols, col = (i - r * cols) * 8;
+        const size_t o = (row0 + r) * a.N + n0 + col;
+        uint32_t extra[4];
+        if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra);
+        // the first run's part is its second slot's, the others' their first
+        const float* p = a.part + (((size_t)c0 * 2 + 1) * a.part_rows + r) * BN + col;
+        const float4 f0 = __ldcg(reinterpret_cast<const float4*>(p)), f1 = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+        float2 v[4] = {{f0.x, f0.y}, {f0.z, f0.w}, {f1.x, f1.y}, {f1.z, f1.w}};
+        p = a.part + (((size_t)c0 * 2 + 2) * a.part_rows + r) * BN + col;
+        for (int c = c0 + 1; c <= last; c += 4, p += 4 * step) {    // four runs' sums in flight
+            float4 q[4][2];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (c + k > last) break;
+                q[k][0] = __ldcg(reinterpret_cast<const float4*>(p + k * step));
+                q[k][1] = __ldcg(reinterpret_cast<const float4*>(p + k * step) + 1);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (c + k > last) break;
+                v[0].x += q[k][0].x; v[0].y += q[k][0].y; v[1].x += q[k][0].z; v[1].y += q[k][0].w;
+                v[2].x += q[k][1].x; v[2].y += q[k][1].y; v[3].x += q[k][1].z; v[3].y += q[k][1].w;
             }
         }
-        const size_t step = (size_t)2 * a.part_rows * BN;               // from a run's sums to the next one's
-        for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < rows * cols; i += gridDim.y * kJoinThreads) {
-            const int r = i / cols, col = (i - r * cols) * 8;
-            const size_t row = KIND == kWeights ? (size_t)e * a.M + mt * BM + r : (size_t)g.lo + mt * BM + r;
-            const size_t o = row * a.N + n0 + col;
-            uint32_t extra[4];
-            if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra);
-            // the first run's part is its second slot's, the others' their first
-            const float* p = a.part + (((size_t)c0 * 2 + 1) * a.part_rows + r) * BN + col;
-            const float4 f0 = __ldcg(reinterpret_cast<const float4*>(p)), f1 = __ldcg(reinterpret_cast<const float4*>(p) + 1);
-            float2 v[4] = {{f0.x, f0.y}, {f0.z, f0.w}, {f1.x, f1.y}, {f1.z, f1.w}};
-            p = a.part + (((size_t)c0 * 2 + 2) * a.part_rows + r) * BN + col;
-            for (int c = c0 + 1; c <= c1; c += 4, p += 4 * step) {      // four runs' sums in flight
-                float4 q[4][2];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (c + k > c1) break;
-                    q[k][0] = __ldcg(reinterpret_cast<const float4*>(p + k * step));
-                    q[k][1] = __ldcg(reinterpret_cast<const float4*>(p + k * step) + 1);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (c + k > c1) break;
-                    v[0].x += q[k][0].x; v[0].y += q[k][0].y; v[1].x += q[k][0].z; v[1].y += q[k][0].w;
-                    v[2].x += q[k][1].x; v[2].y += q[k][1].y; v[3].x += q[k][1].z; v[3].y += q[k][1].w;
-                }
-            }
-            finish<KIND, 8>(a, e, o, n0 + col, v, extra);
-        }
-        return;
+        finish<KIND, 8>(a, e, o, n0 + col, v, extra);
     }
 }
 
@@ -692,7 +693,7 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     a.deal_waves = kDealWaves;
     a.part = static_cast<float*>(ws);
     a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
-    a.db_part = a.part + (size_t)a.grid * 2 * BM * BN;      // behind whole tiles
+    a.db_part = a.part + (size_t)a.grid * 2 * a.part_rows * BN;
     a.a_rows = BM;
     a.b_chunks = KIND != kForward && a.N % 64 == 0;
     if (KIND == kWeights) {         // dy [R][M], x [R][N]
@@ -719,11 +720,13 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         }
         attr_done_dev[dev & 63] = true;
     }
+    // no join where the tiles are too many for runs whatever the groups are
+    const long long least = KIND == kWeights ? (long long)((a.M + BM - 1) / BM) * a.n_tiles : 0;
+    const bool join = least <= (long long)a.deal_waves * a.grid;
+    a.split = join ? reinterpret_cast<Split*>(a.db_part + (KIND == kWeights ? (size_t)a.grid * 2 * BM : 0)) : nullptr;
     int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, a);
     if (rc) return rc;
-    // without the join where the tiles are too many for runs whatever the groups are
-    const long long least = KIND == kWeights ? (long long)((a.M + BM - 1) / BM) * a.n_tiles : 0;
-    if (least <= (long long)a.deal_waves * a.grid) {
+    if (join) {
         const int parts = (a.part_rows * (BN / 8) + kJoinThreads - 1) / kJoinThreads;
         rc = launch_pdl(expert_join_kernel<KIND>, dim3(a.grid, parts < kJoinParts ? parts : kJoinParts), dim3(kJoinThreads), 0, st, a);
     }
@@ -732,10 +735,10 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
 
 }  // namespace
 
-// Two tiles' sums a CTA.
+// Two tiles' sums a CTA, and what its split tile is.
 size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad) {
     const size_t rows = grad || s.T > BM ? BM : s.T, sums = rows * BN + (grad ? BM : 0);
-    return ((size_t)sm_count() * 2 * sums * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)sm_count() * (2 * sums * sizeof(float) + sizeof(Split)) + 255) & ~(size_t)255;
 }
 
 int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_linear_t& l, void* ws, cudaStream_t st) {
