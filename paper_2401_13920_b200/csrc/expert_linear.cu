@@ -35,7 +35,8 @@ constexpr int kThreads = 64 + 32 * kEpiWarps, kWeightsThreads = kThreads + 32 * 
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int kMaxE = 1024;
 constexpr size_t kRing = 6 * (size_t)(16 * BK * 2 + B_BYTES);     // 204 KB, a little more than four whole stages
-constexpr size_t kSmem = 1024 /*alignment slack*/ + kRing + 256 /*barriers*/ + (kMaxE + 1) * sizeof(int);
+constexpr size_t kOffsetBytes = (kMaxE + 4) * sizeof(int), kBiasBytes = kEpiWarps * (BN / 2) * sizeof(float);
+constexpr size_t kSmem = 1024 /*alignment slack*/ + kRing + 256 /*barriers*/ + kOffsetBytes + kBiasBytes;
 static_assert(4 * (A_BYTES + B_BYTES) <= kRing && kSmem <= 227 * 1024, "the ring fits");
 
 __device__ int g_linear_flags = 0;   // bit 0: a bounded wait gave up
@@ -219,41 +220,47 @@ __device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64
 // ---- epilogue arithmetic on pairs ----
 __device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
 
-// W sums of one row become outputs, W = 8 or 16 columns from `col` on; `o` is the first's index in the [R][N] arrays.  The arrays'
-// values (`extra`: z_in or residual) are loaded by the caller, long before the sums are there.  16 columns are 32 bytes of
-// bf16, a whole sector: rows are far apart, and a lane that stores half a sector at a time costs the L2 a merge (forward
-// product of 65536 x 2560 x 10240 with GeLU and z: 3.85 against 3.09 ms, the gradient through the GeLU 5.0 against 3.3 ms).
+// W sums of one row become outputs, W = 8 or 16 columns from `col` on; `o` is the first's index in the [R][N] arrays, `extra` what
+// is read along (z_in or residual), `b` the bias, both loaded by the caller, long before the sums are there.  16 columns
+// are 32 bytes of bf16, a whole sector: rows are far apart, and a lane that stores half a sector at a time costs the L2 a
+// merge (first product of 65536 x 2560 x 10240 with GeLU and z: 3.85 against 3.09 ms, the gradient through the GeLU 5.0
+// against 3.3 ms).  `wide`: rows begin on 32 bytes; else the same in pieces of 16.
 template <int W>
-__device__ __forceinline__ void st_bf16(void* base, size_t o, const float2 (&v)[W / 2]) {
+__device__ __forceinline__ void st_bf16(void* base, size_t o, const float2 (&v)[W / 2], bool wide) {
     uint16_t* p = static_cast<uint16_t*>(base) + o;
-    if (W == 16)
-        st_global_v8(p, cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]), cvt_bf16x2(v[W / 2 - 4]), cvt_bf16x2(v[W / 2 - 3]),
-                     cvt_bf16x2(v[W / 2 - 2]), cvt_bf16x2(v[W / 2 - 1]));
-    else
-        *reinterpret_cast<uint4*>(p) = make_uint4(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]), cvt_bf16x2(v[2]), cvt_bf16x2(v[3]));
+    uint32_t r[W / 2];
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) r[i] = cvt_bf16x2(v[i]);
+    if (W == 16 && wide) {
+        st_global_v8(p, r[0], r[1], r[2], r[3], r[W / 2 - 4], r[W / 2 - 3], r[W / 2 - 2], r[W / 2 - 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 8; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+    }
 }
 template <int W>
-__device__ __forceinline__ void ld_bf16(const void* base, size_t o, uint32_t* r) {
+__device__ __forceinline__ void ld_bf16(const void* base, size_t o, uint32_t* r, bool wide) {
     const uint16_t* p = static_cast<const uint16_t*>(base) + o;
-    if (W == 16)
+    if (W == 16 && wide) {
         asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
-    else
-        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 8; ++i)
+            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[4 * i]), "=r"(r[4 * i + 1]), "=r"(r[4 * i + 2]), "=r"(r[4 * i + 3]) : "l"(p + 8 * i) : "memory");
+    }
 }
 template <int KIND, int W>
-__device__ __forceinline__ void finish(const LinearArgs& a, int e, size_t o, int col, float2 (&v)[W / 2], const uint32_t* extra) {
+__device__ __forceinline__ void finish(const LinearArgs& a, size_t o, float2 (&v)[W / 2], const float4* b, const uint32_t* extra, bool wide) {
     if (KIND == kForward) {
         if (a.bias) {
-            const float4* b = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + col);
 #pragma unroll
             for (int i = 0; i < W / 4; ++i) {
-                const float4 f = __ldg(b + i);
-                v[2 * i] = __fadd2_rn(v[2 * i], make_float2(f.x, f.y));
-                v[2 * i + 1] = __fadd2_rn(v[2 * i + 1], make_float2(f.z, f.w));
+                v[2 * i] = __fadd2_rn(v[2 * i], make_float2(b[i].x, b[i].y));
+                v[2 * i + 1] = __fadd2_rn(v[2 * i + 1], make_float2(b[i].z, b[i].w));
             }
         }
-        if (a.z_out) st_bf16<W>(a.z_out, o, v);
+        if (a.z_out) st_bf16<W>(a.z_out, o, v, wide);
         if (a.act == LOCMOE_ACT_GELU) {
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) v[i] = gelu_erf2(v[i]);
@@ -285,17 +292,17 @@ __device__ __forceinline__ void finish(const LinearArgs& a, int e, size_t o, int
     }
     if (KIND == kWeights && a.out_f32) {
         float* p = static_cast<float*>(a.out) + o;
-        if (W == 16) {      // rows begin on 64 bytes
 #pragma unroll
-            for (int i = 0; i < W / 2; i += 4)
+        for (int i = 0; i < W / 2; i += 4)      // rows of whole 32 bytes, N being a multiple of 8, but perhaps not on one
+            if (wide)
                 st_global_v8(p + 2 * i, __float_as_uint(v[i].x), __float_as_uint(v[i].y), __float_as_uint(v[i + 1].x), __float_as_uint(v[i + 1].y),
                              __float_as_uint(v[i + 2].x), __float_as_uint(v[i + 2].y), __float_as_uint(v[i + 3].x), __float_as_uint(v[i + 3].y));
-        } else {
-#pragma unroll
-            for (int i = 0; i < W / 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
-        }
+            else {
+                reinterpret_cast<float4*>(p + 2 * i)[0] = make_float4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
+                reinterpret_cast<float4*>(p + 2 * i)[1] = make_float4(v[i + 2].x, v[i + 2].y, v[i + 3].x, v[i + 3].y);
+            }
     } else {
-        st_bf16<W>(a.out, o, v);
+        st_bf16<W>(a.out, o, v, wide);
     }
 }
 // The array read along with the sums, if there is one.
@@ -415,7 +422,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (!ok) break;
             phase ^= (uint32_t)((stage + plain) / NSTAGE) & 1u;
             stage = (stage + plain) % NSTAGE;
-            if (left < BK) {
+            if constexpr (KIND == kWeights) if (left < BK) {
                 if (!wait_warp(&full[stage], phase, abort_word)) { ok = false; break; }
                 unsigned char* pa = base + (size_t)stage * STAGE_BYTES;
                 const int steps = (left + UMMA_K - 1) / UMMA_K;
@@ -517,13 +524,14 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps))
                     {
                     float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
-                    finish<KIND, 8>(a, e, (size_t)(e * n + i) * 8, 0, z, nullptr);
+                    finish<KIND, 8>(a, (size_t)(e * n + i) * 8, z, nullptr, nullptr, false);
                 }
             }
         }
         __syncwarp();
         const void* with = extra_array<KIND>(a);
-        const bool wide_ok = a.N % 16 == 0 && (((uintptr_t)a.out | (uintptr_t)a.z_out | (uintptr_t)with) % 32) == 0;
+        const bool wide = a.N % 16 == 0 && (((uintptr_t)a.out | (uintptr_t)a.z_out | (uintptr_t)with) % 32) == 0;
+        float* bias = reinterpret_cast<float*>(base + kRing + 256 + kOffsetBytes) + (warp - 2) * (BN / 2);   // this warp's columns
         Split split{};
         int acc = 0; uint32_t acc_phase = 0;
         while (cur.next(it)) {
@@ -535,22 +543,35 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 split.last = blockIdx.x + 1;
                 while (split.last + 1 < runs.n && runs.begin(split.last + 1) < it.begin + it.kb) ++split.last;
             }
-            if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
-            tc_fence_after();
             const int r_in = it.mt * BM + q * 32 + lane;
             const bool row_ok = r_in < (KIND == kWeights ? a.M : it.n);
             const bool whole = it.kb1 - it.kb0 == it.kb;
             const size_t row = KIND == kWeights ? (size_t)it.e * a.M + r_in : (size_t)it.lo + r_in;
             const int n0 = it.nt * BN;
+            const size_t o0 = row * a.N + n0;
             float* part = nullptr;
             if (!whole) part = a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + (q * 32 + lane)) * BN;
-            const size_t o0 = row * a.N + n0;
+            // the bias and the array read along come ahead: the former through shared memory, the latter a block ahead, the first
+            // block's before the sums are there (1000 rows of 1560 x 4104 with both: loads one after the other were 9 us a tile)
+            if (KIND == kForward && a.bias && whole) {
+                const int col = n0 + half * (BN / 2) + 4 * lane;
+                if (col < a.N) *reinterpret_cast<float4*>(bias + 4 * lane) = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)it.e * a.N + col));
+                __syncwarp();
+            }
+            uint32_t next[16];
+            auto fetch = [&](int c) {
+                if (row_ok && whole && with && a.N - n0 - c * 32 >= 32) { ld_bf16<16>(with, o0 + c * 32, next, wide); ld_bf16<16>(with, o0 + c * 32 + 16, next + 8, wide); }
+            };
+            fetch(half * (BN / 64));
+            if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
+            tc_fence_after();
 #pragma unroll 1
             for (int c = half * (BN / 64); c < (half + 1) * (BN / 64); ++c) {
                 const int cols = a.N - n0 - c * 32;      // columns from here to the row's end
-                const bool full32 = wide_ok && cols >= 32;
                 uint32_t extra[16];
-                if (row_ok && whole && full32 && with) { ld_bf16<16>(with, o0 + c * 32, extra); ld_bf16<16>(with, o0 + c * 32 + 16, extra + 8); }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) extra[i] = next[i];
+                if (c + 1 < (half + 1) * (BN / 64)) fetch(c + 1);
                 __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
                 uint32_t r[32];
                 tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + c * 32), r);
@@ -558,23 +579,33 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) st_global_v8(part + c * 32 + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
-                } else if (full32) {
+                } else if (cols >= 32) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 16) {
                         float2 v[8];
+                        float4 b[4];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                        finish<KIND, 16>(a, it.e, o0 + c * 32 + i, n0 + c * 32 + i, v, extra + i / 2);
+                        if (KIND == kForward && a.bias) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) b[k] = reinterpret_cast<const float4*>(bias + (c & 3) * 32 + i)[k];
+                        }
+                        finish<KIND, 16>(a, o0 + c * 32 + i, v, b, extra + i / 2, wide);
                     }
-                } else {    // the row's end, or rows that do not begin on 32 bytes
+                } else {    // the row's end
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
                         if (i >= cols) break;
                         float2 v[4];
+                        float4 b[2];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                        if (with) ld_bf16<8>(with, o0 + c * 32 + i, extra);
-                        finish<KIND, 8>(a, it.e, o0 + c * 32 + i, n0 + c * 32 + i, v, extra);
+                        if (KIND == kForward && a.bias) {
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) b[k] = reinterpret_cast<const float4*>(bias + (c & 3) * 32 + i)[k];
+                        }
+                        if (with) ld_bf16<8>(with, o0 + c * 32 + i, extra, false);
+                        finish<KIND, 8>(a, o0 + c * 32 + i, v, b, extra, false);
                     }
                 }
             }
@@ -622,7 +653,12 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
         const int r = i / cols, col = (i - r * cols) * 8;
         const size_t o = (row0 + r) * a.N + n0 + col;
         uint32_t extra[4];
-        if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra);
+        if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra, false);
+        float4 b[2];
+        if (KIND == kForward && a.bias) {
+            const float4* q = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + n0 + col);
+            b[0] = __ldg(q); b[1] = __ldg(q + 1);
+        }
         // the first run's part is its second slot's, the others' their first
         const float* p = a.part + (((size_t)c0 * 2 + 1) * a.part_rows + r) * BN + col;
         const float4 f0 = __ldcg(reinterpret_cast<const float4*>(p)), f1 = __ldcg(reinterpret_cast<const float4*>(p) + 1);
@@ -643,7 +679,7 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
                 v[2].x += q[k][1].x; v[2].y += q[k][1].y; v[3].x += q[k][1].z; v[3].y += q[k][1].w;
             }
         }
-        finish<KIND, 8>(a, e, o, n0 + col, v, extra);
+        finish<KIND, 8>(a, o, v, b, extra, false);
     }
 }
 
