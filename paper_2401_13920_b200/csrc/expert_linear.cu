@@ -12,9 +12,9 @@
 // rows (weights) the last block of the reduction holds rows of the next group, and those are overwritten with zeros in shared
 // memory, in both operands, since a zero in one does not undo an infinity in the other.
 //
-// Work is dealt by tiles (tile i to CTA i modulo the grid), neighbours in time sharing operands in L2, or, where the tiles do
-// not fill many waves, by equal runs of 64-blocks of the reduction, so that every SM gets the same share whatever the
-// groups are.  A tile that a run begins or ends in leaves fp32 sums in the workspace, which a second kernel adds in order.
+// Work is dealt by tiles (tile i to CTA i modulo the grid), neighbours in time sharing operands in L2, and what is left after the
+// last full wave in equal runs of 64-blocks of the reduction, so that every SM gets the same share whatever the groups are.
+// A tile that a run begins or ends in leaves fp32 sums in the workspace, which a second kernel adds in order.
 #include <cuda.h>
 #include <stdlib.h>
 
@@ -27,17 +27,28 @@ namespace locmoe {
 namespace {
 
 constexpr int BM = 128, BN = 256, BK = 64, UMMA_K = 16;
-constexpr int kMaxStages = 6;                       // four of whole tiles, six where the rows are few
 constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
 constexpr uint32_t CHUNK_BYTES = 64 * BK * 2;       // 64 columns of an MN-major tile
-constexpr int kEpiWarps = 8, kSumWarps = 4;         // the latter only where the weights' gradient comes with the bias's
-constexpr int kThreads = 64 + 32 * kEpiWarps, kWeightsThreads = kThreads + 32 * kSumWarps;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int kMaxE = 1024;
-constexpr size_t kRing = 6 * (size_t)(16 * BK * 2 + B_BYTES);     // 204 KB, a little more than four whole stages
-constexpr size_t kOffsetBytes = (kMaxE + 4) * sizeof(int), kBiasBytes = kEpiWarps * (BN / 2) * sizeof(float);
+
+enum Kind { kForward = 0, kTowardsX = 1, kWeights = 2 };
+
+// Warps after the two that load and issue: the epilogue's (sixteen of them on 16 columns a step were 10 % slower throughout), and
+// those of the column sums.
+constexpr int kEpiWarps = 8, kEpiThreads = 32 * kEpiWarps;
+constexpr int kSumWarps = 4;                        // only where the weights' gradient comes with the bias's
+constexpr int kThreads = 64 + kEpiThreads, kWeightsThreads = kThreads + 32 * kSumWarps;
+
+// Shared memory: the ring (four whole stages; more of them where the rows are few and A short), or three stages and two boxes a
+// warp (weights' gradients of short groups); then the barriers, the offsets, a tile's bias.
+constexpr uint32_t kBoxBytes = 32 * 128;            // 32 rows of 128 bytes on their way out
+constexpr int kMaxStages = 6, kBoxStages = 3;
+constexpr size_t kRing = kBoxStages * (size_t)(A_BYTES + B_BYTES) + 2 * kEpiWarps * kBoxBytes;
+static_assert(kRing >= 4 * (size_t)(A_BYTES + B_BYTES) && kRing >= 6 * (size_t)(16 * BK * 2 + B_BYTES), "the rings fit");
+constexpr size_t kOffsetBytes = (kMaxE + 4) * sizeof(int), kBiasBytes = BN * 4 * sizeof(float);
 constexpr size_t kSmem = 1024 /*alignment slack*/ + kRing + 256 /*barriers*/ + kOffsetBytes + kBiasBytes;
-static_assert(4 * (A_BYTES + B_BYTES) <= kRing && kSmem <= 227 * 1024, "the ring fits");
+static_assert(kSmem <= 227 * 1024, "all of it fits");
 
 __device__ int g_linear_flags = 0;   // bit 0: a bounded wait gave up
 
@@ -46,8 +57,6 @@ struct __align__(16) Split {
     int e, row, rows, nt;       // expert, the tile's first row in the output, its rows, its column
     int last, pad[3];           // last run that worked on it
 };
-
-enum Kind { kForward = 0, kTowardsX = 1, kWeights = 2 };
 
 struct LinearArgs {
     const int32_t* offsets;     // [E + 1]
@@ -64,9 +73,10 @@ struct LinearArgs {
     int E, R, M, N, K;          // M: rows of a weight (weights only)
     int n_tiles, a_rows;        // rows of one A box
     int stages;                 // of the ring
+    int boxes;                  // weights: rows leave as boxes
     int a_chunks, b_chunks;     // 1: one load brings an MN-major tile, else one for each 64 columns
     int part_rows;
-    int grid, deal_waves;       // runs instead of tiles up to this many waves of tiles
+    int grid;
 };
 
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_word) {
@@ -101,100 +111,136 @@ struct Tiles {
     __device__ __forceinline__ int tiles(const Group& g) const { return g.n > 0 ? m_tiles(g) * a.n_tiles : 0; }
 };
 
-struct Totals { long long tiles, units; };
-// Sums over the groups by one warp (all lanes get them).
-template <int KIND>
-__device__ __forceinline__ Totals totals(const LinearArgs& a, const int* offsets, int lane) {
-    const Tiles<KIND> t{a, offsets};
-    long long n = 0, u = 0;
-    for (int e = lane; e < a.E; e += 32) {
-        const Group g = group_of(offsets, e, a.R);
-        const long long k = t.tiles(g);
-        n += k;
-        u += k * t.kblocks(g);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        n += __shfl_xor_sync(0xffffffffu, n, o);
-        u += __shfl_xor_sync(0xffffffffu, u, o);
-    }
-    return {n, u};
-}
-
-// How the work is dealt; the same on every CTA and in the kernel that joins.  `runs` = 0: by tiles, else the number of runs.
-// A run has at least four blocks, so that its sums are worth their way through memory.
-__device__ __forceinline__ int deal(const LinearArgs& a, const Totals& s) {
-    if (s.tiles > (long long)a.deal_waves * a.grid || s.units == 0) return 0;
-    const long long r = s.units / 4;
-    return r < 1 ? 1 : r < a.grid ? (int)r : a.grid;
-}
-// Where run c begins: `each` blocks a run, one more in the first `more`.
-struct Runs {
-    int n;
-    long long each;
+// How the work is dealt, the same on every CTA.  Tiles below `whole` go to the CTAs one by one; what they leave, less than a tile
+// for every CTA, is cut into `runs` equal runs of blocks, or dealt like the others (whole = all tiles) where that is no slower.
+struct Deal {
+    int tiles, whole, runs;
+    long long each;             // run c begins at each * c + min(c, more) of the rest's blocks
     int more;
-    __device__ __forceinline__ Runs(const Totals& s, int runs) : n(runs), each(0), more(0) {
-        if (runs) { each = s.units / runs; more = (int)(s.units - each * runs); }
-    }
     __device__ __forceinline__ long long begin(int c) const { return each * c + min(c, more); }
 };
+
+__device__ __forceinline__ long long sum_warp(long long v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// By one warp (all lanes get it).  Splitting the rest saves the part of a wave in which SMs would stand idle: kb blocks times the
+// share of idle SMs, at 0.27 us a block where the tensor cores are the limit, up to 0.73 us where each weight tile is used by
+// one tile of rows and comes out of HBM at 148 x 32 KB a step.  It costs the join's launch, 3 us, and the sums' way through
+// memory, 0.07 us for each row of a tile (1981 rows of 304 x 1024 with every tile split 28 against 19 us whole; 2 rows of
+// 10240 x 2560, 20 tiles in all, 27 us split).
+template <int KIND>
+__device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, int lane) {
+    const Tiles<KIND> t{a, offsets};
+    long long n = 0, rows = 0, rowtiles = 0, groups = 0;
+    for (int e = lane; e < a.E; e += 32) {
+        const Group g = group_of(offsets, e, a.R);
+        n += t.tiles(g);
+        rows += g.n;
+        if (g.n > 0) { rowtiles += t.m_tiles(g); ++groups; }
+    }
+    Deal d{(int)sum_warp(n), 0, 0, 0, 0};
+    d.whole = d.tiles;
+    const int rest = d.tiles % a.grid;
+    if (rest == 0 || !a.split) return d;
+    // blocks of the last `rest` tiles
+    long long units = 0;
+    if (KIND == kWeights) {
+        int before = 0;                                         // tiles of the groups passed
+        for (int e0 = 0; e0 < a.E; e0 += 32) {
+            const Group g = e0 + lane < a.E ? group_of(offsets, e0 + lane, a.R) : Group{0, 0};
+            const unsigned busy = __ballot_sync(0xffffffffu, g.n > 0);
+            const int per = t.m_tiles(g) * a.n_tiles, first = before + per * __popc(busy & ((1u << lane) - 1u));
+            if (g.n > 0) units += (long long)max(0, min(per, first + per - (d.tiles - rest))) * t.kblocks(g);
+            before += per * __popc(busy);
+        }
+        units = sum_warp(units);
+    } else {
+        units = (long long)rest * ((a.K + BK - 1) / BK);
+    }
+    rows = sum_warp(rows); rowtiles = sum_warp(rowtiles); groups = sum_warp(groups);
+    const float kb = (float)units / (float)rest, idle = 1.0f - (float)rest / (float)a.grid;
+    const float block = KIND == kWeights ? 0.27f : fmaxf(0.27f, 0.73f * (float)groups / (float)rowtiles);
+    const float tile_rows = KIND == kWeights ? (float)BM : (float)rows / (float)rowtiles;
+    if (kb * idle * block < 3.0f + 0.07f * tile_rows) return d;
+    const long long r = units / 4;                              // a run has at least four blocks
+    d.whole = d.tiles - rest;
+    d.runs = r < 1 ? 1 : r < a.grid ? (int)r : a.grid;
+    d.each = units / d.runs;
+    d.more = (int)(units - d.each * d.runs);
+    return d;
+}
+// The host's side of that rule: whether any offsets could lead to a split.
+template <int KIND>
+bool may_split(const LinearArgs& a) {
+    const float kb = (float)(((KIND == kWeights ? a.R : a.K) + BK - 1) / BK);
+    return KIND == kWeights ? kb * 0.27f >= 3.0f + 0.07f * BM : kb * 0.73f >= 3.0f;
+}
 
 struct Item {
     int e, lo, n;               // group, its first row, its rows
     int mt, nt;                 // tile
     int kb0, kb1, kb;           // blocks of this item, blocks of the tile
-    long long begin;            // by runs: the tile's first block
+    long long begin;            // in a run: the tile's first block among the rest's
 };
 
-// Walks through one CTA's share.
+// Walks through one CTA's share: its tiles, then its run.
 template <int KIND>
 struct Cursor {
     const LinearArgs& a;
     const int* offsets;
-    int runs;
-    long long at, end;          // tile (by tiles) or block (by runs)
-    int e;
-    long long base;             // first tile or block of group e
+    const Deal& d;
+    int tile, e, base;          // next tile; group; the group's first tile
+    long long at, end, ubase;   // next block and end of the run; blocks of the rest before group e
     Group g;
     int kb, per;                // blocks a tile, tiles of group e
-    __device__ __forceinline__ Cursor(const LinearArgs& a_, const int* off, const Totals& s, const Runs& r, int c) : a(a_), offsets(off), runs(r.n), e(-1), base(0) {
+    __device__ __forceinline__ Cursor(const LinearArgs& a_, const int* off, const Deal& d_, int c) : a(a_), offsets(off), d(d_), tile(c), e(-1), base(0), ubase(0) {
         g = Group{0, 0};
         kb = per = 0;
-        if (runs) { at = c < runs ? r.begin(c) : 0; end = c < runs ? r.begin(c + 1) : 0; }
-        else { at = c; end = s.tiles; }
+        at = c < d.runs ? d.begin(c) : 0;
+        end = c < d.runs ? d.begin(c + 1) : 0;
+    }
+    __device__ __forceinline__ int rest() const { return max(0, min(per, base + per - d.whole)); }     // tiles of group e in runs
+    __device__ __forceinline__ bool step() {
+        ubase += (long long)rest() * kb;
+        base += per;
+        if (++e >= a.E) return false;
+        const Tiles<KIND> t{a, offsets};
+        g = group_of(offsets, e, a.R);
+        kb = t.kblocks(g);
+        per = t.tiles(g);
+        return true;
     }
     __device__ __forceinline__ bool next(Item& it) {
-        if (at >= end) return false;
-        const Tiles<KIND> t{a, offsets};
-        while (true) {
-            const long long size = runs ? (long long)per * kb : per;
-            if (e >= 0 && at < base + size) break;
-            base += size;
-            if (++e >= a.E) return false;
-            g = group_of(offsets, e, a.R);
-            kb = t.kblocks(g);
-            per = t.tiles(g);
-        }
-        int tile;
-        it.kb = kb;
-        if (runs) {
-            const long long rel = at - base;
-            tile = (int)(rel / kb);
-            it.begin = base + (long long)tile * kb;
+        int in;                 // tile inside the group
+        if (tile < d.whole) {
+            while (e < 0 || tile >= base + per)
+                if (!step()) return false;
+            in = tile - base;
+            it.kb0 = 0;
+            it.kb1 = kb;
+            tile += a.grid;
+        } else if (at < end) {
+            while (e < 0 || at >= ubase + (long long)rest() * kb)
+                if (!step()) return false;
+            const long long rel = at - ubase;
+            const int j = (rel >> 32) == 0 ? (int)((uint32_t)rel / (uint32_t)kb) : (int)(rel / kb);
+            in = per - rest() + j;
+            it.begin = ubase + (long long)j * kb;
             it.kb0 = (int)(at - it.begin);
             const long long left = end - at;
             it.kb1 = left < kb - it.kb0 ? it.kb0 + (int)left : kb;
             at += it.kb1 - it.kb0;
         } else {
-            tile = (int)(at - base);
-            it.kb0 = 0;
-            it.kb1 = kb;
-            at += a.grid;
+            return false;
         }
+        it.kb = kb;
         it.e = e; it.lo = g.lo; it.n = g.n;
-        const int mts = t.m_tiles(g);
-        it.nt = tile / mts;             // tiles that share a weight tile are neighbours
-        it.mt = tile - it.nt * mts;
+        const int mts = Tiles<KIND>{a, offsets}.m_tiles(g);
+        it.nt = in / mts;               // tiles that share a weight tile are neighbours
+        it.mt = in - it.nt * mts;
         return true;
     }
 };
@@ -206,9 +252,10 @@ __device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr) {
     return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | ((uint64_t)(CHUNK_BYTES >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
            (2ull << 61);
 }
-// bf16 x bf16 -> fp32, 128 x 256; bits 15 and 16: A, B are MN-major.
-__host__ __device__ constexpr uint32_t idesc(bool a_mn, bool b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+// bf16 x bf16 -> fp32, 128 x up to 256 columns; bits 15 and 16: A, B are MN-major.
+__device__ __forceinline__ uint32_t idesc(bool a_mn, bool b_mn, int cols) {
+    const uint32_t n = cols < BN ? (uint32_t)(cols + 15) / 16 * 16 : BN;     // no products beyond the row's end
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
 }
 __device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t id, uint32_t accumulate) {
     asm volatile(
@@ -220,13 +267,11 @@ __device__ __forceinline__ void umma_f16(uint32_t tmem_d, uint64_t adesc, uint64
 // ---- epilogue arithmetic on pairs ----
 __device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
 
-// W sums of one row become outputs, W = 8 or 16 columns from `col` on; `o` is the first's index in the [R][N] arrays, `extra` what
-// is read along (z_in or residual), `b` the bias, both loaded by the caller, long before the sums are there.  16 columns
-// are 32 bytes of bf16, a whole sector: rows are far apart, and a lane that stores half a sector at a time costs the L2 a
-// merge (first product of 65536 x 2560 x 10240 with GeLU and z: 3.85 against 3.09 ms, the gradient through the GeLU 5.0
-// against 3.3 ms).  `wide`: rows begin on 32 bytes; else the same in pieces of 16.
+// 8 or 16 columns of a row, by the lane that has them.  Rows are far apart, so that a lane's 32 bytes are a sector of their own:
+// stored whole they cost the L2 no merge (first product of 65536 x 2560 x 10240 with GeLU and z 3.85 ms with 16 bytes a
+// store, 3.09 with 32).  `wide`: rows begin on 32 bytes.
 template <int W>
-__device__ __forceinline__ void st_bf16(void* base, size_t o, const float2 (&v)[W / 2], bool wide) {
+__device__ __forceinline__ void st_row(void* base, size_t o, const float2 (&v)[W / 2], bool wide) {
     uint16_t* p = static_cast<uint16_t*>(base) + o;
     uint32_t r[W / 2];
 #pragma unroll
@@ -239,7 +284,7 @@ __device__ __forceinline__ void st_bf16(void* base, size_t o, const float2 (&v)[
     }
 }
 template <int W>
-__device__ __forceinline__ void ld_bf16(const void* base, size_t o, uint32_t* r, bool wide) {
+__device__ __forceinline__ void ld_row(const void* base, size_t o, uint32_t* r, bool wide) {
     const uint16_t* p = static_cast<const uint16_t*>(base) + o;
     if (W == 16 && wide) {
         asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -250,17 +295,10 @@ __device__ __forceinline__ void ld_bf16(const void* base, size_t o, uint32_t* r,
             asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[4 * i]), "=r"(r[4 * i + 1]), "=r"(r[4 * i + 2]), "=r"(r[4 * i + 3]) : "l"(p + 8 * i) : "memory");
     }
 }
+// What comes after z: the activation and the residual, or the slope of the activation before the product.
 template <int KIND, int W>
-__device__ __forceinline__ void finish(const LinearArgs& a, size_t o, float2 (&v)[W / 2], const float4* b, const uint32_t* extra, bool wide) {
+__device__ __forceinline__ void arithmetic(const LinearArgs& a, float2 (&v)[W / 2], const uint32_t* extra) {
     if (KIND == kForward) {
-        if (a.bias) {
-#pragma unroll
-            for (int i = 0; i < W / 4; ++i) {
-                v[2 * i] = __fadd2_rn(v[2 * i], make_float2(b[i].x, b[i].y));
-                v[2 * i + 1] = __fadd2_rn(v[2 * i + 1], make_float2(b[i].z, b[i].w));
-            }
-        }
-        if (a.z_out) st_bf16<W>(a.z_out, o, v, wide);
         if (a.act == LOCMOE_ACT_GELU) {
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) v[i] = gelu_erf2(v[i]);
@@ -290,20 +328,59 @@ __device__ __forceinline__ void finish(const LinearArgs& a, size_t o, float2 (&v
             }
         }
     }
-    if (KIND == kWeights && a.out_f32) {
-        float* p = static_cast<float*>(a.out) + o;
+}
+template <int W>
+__device__ __forceinline__ void add_bias(float2 (&v)[W / 2], const float4* b) {
 #pragma unroll
-        for (int i = 0; i < W / 2; i += 4)      // rows of whole 32 bytes, N being a multiple of 8, but perhaps not on one
-            if (wide)
-                st_global_v8(p + 2 * i, __float_as_uint(v[i].x), __float_as_uint(v[i].y), __float_as_uint(v[i + 1].x), __float_as_uint(v[i + 1].y),
-                             __float_as_uint(v[i + 2].x), __float_as_uint(v[i + 2].y), __float_as_uint(v[i + 3].x), __float_as_uint(v[i + 3].y));
-            else {
-                reinterpret_cast<float4*>(p + 2 * i)[0] = make_float4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
-                reinterpret_cast<float4*>(p + 2 * i)[1] = make_float4(v[i + 2].x, v[i + 2].y, v[i + 3].x, v[i + 3].y);
-            }
-    } else {
-        st_bf16<W>(a.out, o, v, wide);
+    for (int i = 0; i < W / 4; ++i) {
+        v[2 * i] = __fadd2_rn(v[2 * i], make_float2(b[i].x, b[i].y));
+        v[2 * i + 1] = __fadd2_rn(v[2 * i + 1], make_float2(b[i].z, b[i].w));
     }
+}
+// W sums of one row on their whole way; `o` is the first's index in the output, `b` the bias, `extra` what is read along.
+template <int KIND, int W>
+__device__ __forceinline__ void finish(const LinearArgs& a, size_t o, float2 (&v)[W / 2], const float4* b, const uint32_t* extra, bool wide) {
+    if (KIND == kForward && a.bias) add_bias<W>(v, b);
+    if (KIND == kForward && a.z_out) st_row<W>(a.z_out, o, v, wide);
+    arithmetic<KIND, W>(a, v, extra);
+    if (KIND == kWeights && a.out_f32) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.out) + o);
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) p[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+    } else {
+        st_row<W>(a.out, o, v, wide);
+    }
+}
+// 32 columns of a weight's gradient by the lane that has the row, `cols` of them before the row's end.
+__device__ __forceinline__ void store_weights32(const LinearArgs& a, size_t o, int cols, const uint32_t (&r)[32], bool wide) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+        if (i >= cols) break;
+        if (a.out_f32) {
+            float* p = static_cast<float*>(a.out) + o + i;
+            if (wide) {
+                st_global_v8(p, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+            } else {
+                reinterpret_cast<uint4*>(p)[0] = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+                reinterpret_cast<uint4*>(p)[1] = make_uint4(r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+            }
+        } else if (wide && i % 16 == 0 && i + 16 <= cols) {
+            float2 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[(i & 16) + 2 * k]), __uint_as_float(r[(i & 16) + 2 * k + 1]));
+            st_row<16>(a.out, o + i, v, true);
+        } else if (!wide || i % 16 == 0) {
+            float2 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+            st_row<8>(a.out, o + i, v, false);
+        }
+    }
+}
+// A 16-byte piece of a lane's row in a box of 32 rows x 128 bytes on its way out, where the map's swizzle wants it (eight lanes fill
+// the banks once).
+__device__ __forceinline__ void put_piece(unsigned char* box, int lane, int i, const uint4& r) {
+    *reinterpret_cast<uint4*>(box + lane * 128 + ((i ^ (lane & 7)) << 4)) = r;
 }
 // The array read along with the sums, if there is one.
 template <int KIND>
@@ -311,9 +388,9 @@ __device__ __forceinline__ const void* extra_array(const LinearArgs& a) { return
 
 template <int KIND>
 __global__ void __launch_bounds__(KIND == kWeights ? kWeightsThreads : kThreads, 1)
-expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs a) {
+expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
+                   const LinearArgs a) {
     constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
-    constexpr uint32_t kIdesc = idesc(A_MN, B_MN);
     constexpr uint64_t kStepA = (A_MN ? 2048 : UMMA_K * 2) >> 4, kStepB = (B_MN ? 2048 : UMMA_K * 2) >> 4;   // 16 steps of the reduction
     extern __shared__ unsigned char smraw[];
     unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
@@ -349,9 +426,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    const Totals sum = totals<KIND>(a, offsets, lane);
-    const Runs runs(sum, deal(a, sum));
-    Cursor<KIND> cur(a, offsets, sum, runs, blockIdx.x);
+    const Deal runs = deal<KIND>(a, offsets, lane);
+    Cursor<KIND> cur(a, offsets, runs, blockIdx.x);
     Item it;
 
     if (warp == 0) {
@@ -400,7 +476,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         while (ok && cur.next(it)) {
             if (!wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_word)) break;
             tc_fence_after();
-            const uint32_t tmem_d = tmem_base + (uint32_t)acc * BN;
+            const uint32_t tmem_d = tmem_base + (uint32_t)acc * BN, id = idesc(A_MN, B_MN, a.N - it.nt * BN);
             const int left = KIND == kWeights ? it.n - (it.kb1 - 1) * BK : BK;      // rows of the group in the last block
             const int plain = it.kb1 - it.kb0 - (left < BK ? 1 : 0);                // blocks that are products and nothing else
             if (lane == 0) {
@@ -412,7 +488,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     const uint64_t da = A_MN ? umma_desc_mn(sa) : umma_desc_sw128(sa), db = B_MN ? umma_desc_mn(sa + a_bytes) : umma_desc_sw128(sa + a_bytes);
 #pragma unroll
                     for (int k = 0; k < BK / UMMA_K; ++k)
-                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (i > 0 || k > 0) ? 1u : 0u);
+                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, id, (i > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[s]);
                     if (with_db && it.nt != 0) mbar_arrive_n(&empty[s], kSumWarps);    // nobody else reads this stage
                     if (++s == NSTAGE) { s = 0; ph ^= 1u; }
@@ -439,7 +515,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     tc_fence_after();
                     const uint64_t da = umma_desc_mn(smem_u32(pa)), db = umma_desc_mn(smem_u32(pa) + a_bytes);
                     for (int k = 0; k < steps; ++k)
-                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, kIdesc, (plain > 0 || k > 0) ? 1u : 0u);
+                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, id, (plain > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[stage]);
                     if (with_db && it.nt != 0) mbar_arrive_n(&empty[stage], kSumWarps);
                 }
@@ -504,13 +580,14 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    } else {  // ---- epilogue: TMEM lane quadrant = warp % 4, column half = (warp - 2) / 4 ----
-        const int q = warp & 3, half = (warp - 2) >> 2;
+    } else {  // ---- epilogue: TMEM lane quadrant = warp % 4, the columns dealt to the warps of a quadrant ----
+        constexpr int kCols = BN * 4 / kEpiWarps, kBlock = 32;       // columns of one warp, of a step
+        const int q = warp & 3, part0 = ((warp - 2) >> 2) * kCols;
         const int et = threadIdx.x - 64;
         // what no tile covers: rows behind the last group, weights of experts without rows
         if (KIND != kWeights) {
             const long long kept = min(max(offsets[a.E], 0), a.R), per = a.N / 8, n = ((long long)a.R - kept) * per;
-            for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps)) {
+            for (long long i = (long long)blockIdx.x * kEpiThreads + et; i < n; i += (long long)gridDim.x * kEpiThreads) {
                 const size_t o = (size_t)(kept * per + i) * 8;
                 *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + o) = make_uint4(0, 0, 0, 0);
                 if (a.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(0, 0, 0, 0);
@@ -520,92 +597,137 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             for (int e = 0; e < a.E; ++e) {
                 if (group_of(offsets, e, a.R).n > 0) continue;
                 if (a.db && e % (int)gridDim.x == (int)blockIdx.x)
-                    for (int i = et; i < a.M; i += 32 * kEpiWarps) a.db[(size_t)e * a.M + i] = 0.0f;
-                for (long long i = (long long)blockIdx.x * (32 * kEpiWarps) + et; i < n; i += (long long)gridDim.x * (32 * kEpiWarps))
-                    {
+                    for (int i = et; i < a.M; i += kEpiThreads) a.db[(size_t)e * a.M + i] = 0.0f;
+                for (long long i = (long long)blockIdx.x * kEpiThreads + et; i < n; i += (long long)gridDim.x * kEpiThreads) {
                     float2 z[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
                     finish<KIND, 8>(a, (size_t)(e * n + i) * 8, z, nullptr, nullptr, false);
                 }
             }
         }
+        if (et == 0 && a.split) a.split[blockIdx.x].rows = 0;
         __syncwarp();
         const void* with = extra_array<KIND>(a);
         const bool wide = a.N % 16 == 0 && (((uintptr_t)a.out | (uintptr_t)a.z_out | (uintptr_t)with) % 32) == 0;
-        float* bias = reinterpret_cast<float*>(base + kRing + 256 + kOffsetBytes) + (warp - 2) * (BN / 2);   // this warp's columns
-        Split split{};
+        float* bias = reinterpret_cast<float*>(base + kRing + 256 + kOffsetBytes) + (warp - 2) * kCols;      // of this warp's columns
+        unsigned char* boxes = base + (size_t)kBoxStages * (A_BYTES + B_BYTES) + (size_t)(warp - 2) * 2 * kBoxBytes;
+        int turn = 0;
         int acc = 0; uint32_t acc_phase = 0;
         while (cur.next(it)) {
-            if (runs.n && it.kb0 == 0 && it.kb1 < it.kb) {
-                split.e = it.e;
-                split.row = it.mt * BM + (KIND == kWeights ? 0 : it.lo);
-                split.rows = min(BM, (KIND == kWeights ? a.M : it.n) - it.mt * BM);
-                split.nt = it.nt;
-                split.last = blockIdx.x + 1;
-                while (split.last + 1 < runs.n && runs.begin(split.last + 1) < it.begin + it.kb) ++split.last;
+            if (it.kb0 == 0 && it.kb1 < it.kb && et == 0) {
+                int last = blockIdx.x + 1;
+                while (last + 1 < runs.runs && runs.begin(last + 1) < it.begin + it.kb) ++last;
+                Split split{it.e, it.mt * BM + (KIND == kWeights ? 0 : it.lo), min(BM, (KIND == kWeights ? a.M : it.n) - it.mt * BM), it.nt, last};
+                a.split[blockIdx.x] = split;
             }
-            const int r_in = it.mt * BM + q * 32 + lane;
-            const bool row_ok = r_in < (KIND == kWeights ? a.M : it.n);
-            const bool whole = it.kb1 - it.kb0 == it.kb;
-            const size_t row = KIND == kWeights ? (size_t)it.e * a.M + r_in : (size_t)it.lo + r_in;
-            const int n0 = it.nt * BN;
-            const size_t o0 = row * a.N + n0;
-            float* part = nullptr;
-            if (!whole) part = a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + (q * 32 + lane)) * BN;
-            // the bias and the array read along come ahead: the former through shared memory, the latter a block ahead, the first
-            // block's before the sums are there (1000 rows of 1560 x 4104 with both: loads one after the other were 9 us a tile)
-            if (KIND == kForward && a.bias && whole) {
-                const int col = n0 + half * (BN / 2) + 4 * lane;
-                if (col < a.N) *reinterpret_cast<float4*>(bias + 4 * lane) = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)it.e * a.N + col));
-                __syncwarp();
-            }
-            uint32_t next[16];
-            auto fetch = [&](int c) {
-                if (row_ok && whole && with && a.N - n0 - c * 32 >= 32) { ld_bf16<16>(with, o0 + c * 32, next, wide); ld_bf16<16>(with, o0 + c * 32 + 16, next + 8, wide); }
-            };
-            fetch(half * (BN / 64));
-            if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
-            tc_fence_after();
+            __syncwarp();
+            const int m0 = it.mt * BM + q * 32, n0 = it.nt * BN + part0;      // the warp's first row and column
+            const int all = KIND == kWeights ? a.M : it.n;
+            const bool row_ok = m0 + lane < all, whole = it.kb1 - it.kb0 == it.kb;
+            const size_t o0 = ((size_t)(KIND == kWeights ? 0 : it.lo) + m0 + lane) * a.N + n0;      // rows' outputs only
+            float* part = whole ? nullptr : a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + q * 32 + lane) * BN + part0;
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part0);
+            if constexpr (KIND == kWeights) {
+                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
+                tc_fence_after();
+                const int step = a.out_f32 ? 32 : 64;       // columns of a box
 #pragma unroll 1
-            for (int c = half * (BN / 64); c < (half + 1) * (BN / 64); ++c) {
-                const int cols = a.N - n0 - c * 32;      // columns from here to the row's end
-                uint32_t extra[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) extra[i] = next[i];
-                if (c + 1 < (half + 1) * (BN / 64)) fetch(c + 1);
-                __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
-                uint32_t r[32];
-                tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + c * 32), r);
-                if (!row_ok || cols <= 0) continue;
-                if (!whole) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8) st_global_v8(part + c * 32 + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
-                } else if (cols >= 32) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 16) {
-                        float2 v[8];
-                        float4 b[4];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                        if (KIND == kForward && a.bias) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) b[k] = reinterpret_cast<const float4*>(bias + (c & 3) * 32 + i)[k];
-                        }
-                        finish<KIND, 16>(a, o0 + c * 32 + i, v, b, extra + i / 2, wide);
+                for (int c = 0; c < kCols; c += step) {
+                    if (m0 >= all || n0 + c >= a.N) break;                  // all lanes alike
+                    unsigned char* box = boxes + turn * kBoxBytes;
+                    if (whole && a.boxes) {
+                        if (lane == 0) bulk_wait_read<1>();                 // the box before the last one has left
+                        __syncwarp();
                     }
-                } else {    // the row's end
+#pragma unroll 1
+                    for (int h = 0; h < step; h += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(taddr + c + h, r);
+                        if (!whole) {
+                            if (row_ok) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        if (i >= cols) break;
-                        float2 v[4];
-                        float4 b[2];
+                                for (int i = 0; i < 32; i += 8) st_global_v8(part + c + h + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                            }
+                            __syncwarp();
+                        } else if (!a.boxes) {
+                            if (row_ok) store_weights32(a, ((size_t)it.e * a.M + m0 + lane) * a.N + n0 + c + h, a.N - n0 - c - h, r, wide);
+                            __syncwarp();
+                        } else if (a.out_f32) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                            for (int i = 0; i < 8; ++i) put_piece(box, lane, i, make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t p[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) p[k] = cvt_bf16x2(make_float2(__uint_as_float(r[8 * i + 2 * k]), __uint_as_float(r[8 * i + 2 * k + 1])));
+                                put_piece(box, lane, h / 8 + i, make_uint4(p[0], p[1], p[2], p[3]));
+                            }
+                        }
+                    }
+                    if (whole && a.boxes) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {                    // what lies beyond the weights' rows and columns is left out
+                            tma_store_3d(&tmOut, box, n0 + c, m0, it.e);
+                            bulk_commit();
+                        }
+                        turn ^= 1;
+                    }
+                }
+            } else {
+                // the bias and the array read along come ahead: the former through shared memory, the latter a block ahead, the
+                // first block's before the sums are there (1000 rows of 1560 x 4104 with both: loads one after the other were
+                // 9 us a tile)
+                if (KIND == kForward && a.bias && whole) {
+                    if (4 * lane < kCols && n0 + 4 * lane < a.N)
+                        *reinterpret_cast<float4*>(bias + 4 * lane) = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)it.e * a.N + n0) + lane);
+                    __syncwarp();
+                }
+                uint32_t next[kBlock / 2];
+                auto fetch = [&](int c) {
+                    if (!row_ok || !whole || !with) return;
+#pragma unroll
+                    for (int i = 0; i < kBlock; i += 16) {
+                        if (n0 + c + i + 16 <= a.N) ld_row<16>(with, o0 + c + i, next + i / 2, wide);
+                        else if (n0 + c + i < a.N) ld_row<8>(with, o0 + c + i, next + i / 2, false);
+                    }
+                };
+                fetch(0);
+                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += kBlock) {
+                    uint32_t extra[kBlock / 2];
+#pragma unroll
+                    for (int i = 0; i < kBlock / 2; ++i) extra[i] = next[i];
+                    if (c + kBlock < kCols) fetch(c + kBlock);
+                    __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
+                    uint32_t r[kBlock];
+                    tmem_ld(taddr + c, r);
+                    if (!row_ok || n0 + c >= a.N) continue;
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < kBlock; i += 8) st_global_v8(part + c + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                        continue;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBlock; i += 16) {
+                        float4 b[4];
                         if (KIND == kForward && a.bias) {
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) b[k] = reinterpret_cast<const float4*>(bias + (c & 3) * 32 + i)[k];
+                            for (int k = 0; k < 4; ++k) b[k] = reinterpret_cast<const float4*>(bias + c + i)[k];
                         }
-                        if (with) ld_bf16<8>(with, o0 + c * 32 + i, extra, false);
-                        finish<KIND, 8>(a, o0 + c * 32 + i, v, b, extra, false);
+                        if (n0 + c + i + 16 <= a.N) {
+                            float2 v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                            finish<KIND, 16>(a, o0 + c + i, v, b, extra + i / 2, wide);
+                        } else if (n0 + c + i < a.N) {      // the row's last eight
+                            float2 v[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                            finish<KIND, 8>(a, o0 + c + i, v, b, extra + i / 2, false);
+                        }
                     }
                 }
             }
@@ -614,7 +736,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (lane == 0) mbar_arrive(&acc_empty[acc]);
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
-        if (et == 0 && a.split) a.split[blockIdx.x] = split;
+        if (KIND == kWeights && lane == 0) bulk_wait_all<0>();      // the last boxes are where they belong
     }
     tc_fence_before();
     __syncthreads();
@@ -628,7 +750,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
 // Adds up the sums of the tiles that more than one run worked on, in the order of the runs, and finishes them.  CTA (x, y): run
 // x's split tile, every gridDim.y-th piece.  What tile that is the GEMM has written down; finding it anew cost every warp
-// here a few thousand cycles (200 rows of 1600 x 4096, 23 experts: 15 against ... us).
+// here a few thousand cycles (200 rows of 1600 x 4096, 23 experts: 15 against 4 us).
 constexpr int kJoinThreads = 256, kJoinParts = 8;
 static_assert(kJoinThreads >= BM, "a thread for each row of a tile");
 template <int KIND>
@@ -653,7 +775,7 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
         const int r = i / cols, col = (i - r * cols) * 8;
         const size_t o = (row0 + r) * a.N + n0 + col;
         uint32_t extra[4];
-        if (extra_array<KIND>(a)) ld_bf16<8>(extra_array<KIND>(a), o, extra, false);
+        if (extra_array<KIND>(a)) ld_row<8>(extra_array<KIND>(a), o, extra, false);
         float4 b[2];
         if (KIND == kForward && a.bias) {
             const float4* q = reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + n0 + col);
@@ -717,16 +839,18 @@ __global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const in
     }
 }
 
-// Up to this many waves of tiles the work is dealt by runs.
-constexpr int kDealWaves = 8;
+// Weights' gradients: up to this many rows an expert on average a tile is stores more than products, and its rows leave as boxes of
+// 128 bytes a row by TMA; a lane's stores of its own row are 32 bytes each, half sectors where rows do not begin on 32 (72
+// rows of 12 experts, weights of 5440 x 8984: 686 against 340 us).  The boxes take the fourth stage of the ring, which long
+// reductions need (65536 rows of 10240 x 2560: 64 % of the tensor cores' cycles with three stages, 80 % with four).
+constexpr int kBoxRows = 512;
 
 template <int KIND>
 int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cudaStream_t st) {
     LinearArgs a = a0;
-    CUtensorMap tmA, tmB;
+    CUtensorMap tmA, tmB, tmOut;
     a.n_tiles = (a.N + BN - 1) / BN;
     a.grid = sm_count();
-    a.deal_waves = kDealWaves;
     a.part = static_cast<float*>(ws);
     a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
     a.db_part = a.part + (size_t)a.grid * 2 * a.part_rows * BN;
@@ -744,7 +868,10 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         if (!make_map(&tmA, A, 2, da, a.a_rows)) return LOCMOE_ERR_CUDA;
         if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.K, a.E, BK, BN / 64) : make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK))) return LOCMOE_ERR_CUDA;
     }
-    a.stages = (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
+    if (KIND != kWeights) tmOut = tmA;          // not used
+    else if (!make_store_map(&tmOut, a.out, a.out_f32, a.N, a.M, a.E)) return LOCMOE_ERR_CUDA;
+    a.boxes = KIND == kWeights && (long long)a.R < (long long)kBoxRows * a.E;
+    a.stages = a.boxes ? kBoxStages : KIND == kWeights ? 4 : (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     static bool attr_done_dev[64] = {false};   // the attribute is per device
     int dev = 0;
@@ -756,11 +883,9 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         }
         attr_done_dev[dev & 63] = true;
     }
-    // no join where the tiles are too many for runs whatever the groups are
-    const long long least = KIND == kWeights ? (long long)((a.M + BM - 1) / BM) * a.n_tiles : 0;
-    const bool join = least <= (long long)a.deal_waves * a.grid;
+    const bool join = may_split<KIND>(a);
     a.split = join ? reinterpret_cast<Split*>(a.db_part + (KIND == kWeights ? (size_t)a.grid * 2 * BM : 0)) : nullptr;
-    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, a);
+    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, tmOut, a);
     if (rc) return rc;
     if (join) {
         const int parts = (a.part_rows * (BN / 8) + kJoinThreads - 1) / kJoinThreads;

@@ -676,6 +676,19 @@ bool make_map_chunks(CUtensorMap* map, const void* ptr, uint64_t cols, uint64_t 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_store_map(CUtensorMap* map, void* ptr, bool f32, uint64_t cols, uint64_t rows, uint64_t outer) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t es = f32 ? 4 : 2;
+    cuuint64_t gdim[3] = {cols, rows, outer};
+    cuuint64_t gstr[2] = {cols * es, cols * rows * es};
+    cuuint32_t box[3] = {(cuuint32_t)(128 / es), 32, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, ptr, gdim, gstr, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 int launch_gemm(const void* A, const void* W, void* out, int out_f32, int gelu, int E, int M, int N, int K,

@@ -188,7 +188,8 @@ template <> struct Unit<LOCMOE_F32, false> {
 // Order and rows of a few assignments in one launch: CTA v finds the row of assignment v by counting the assignments that come
 // before it, and copies the token there; the assignments that are not routed take the rows behind the last group, in
 // order, as rows of zeros.  The CTAs after those count for the offsets.  V^2 reads of the index array out of L2 and L1: up to
-// kFewMax assignments that is less than the second launch it saves (8 tokens x 2 choices: ... against ... us).
+// kFewMax assignments that is less than the second launch it saves (8 tokens x 2 choices: 12.9 against 15.6 us
+// a call).
 constexpr int kFewThreads = 128, kFewMax = 512;
 template <typename R>
 __global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const int32_t* __restrict__ idx, int V, int T, int E, const R* __restrict__ x, int U,

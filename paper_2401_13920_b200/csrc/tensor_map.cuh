@@ -11,6 +11,8 @@ namespace locmoe {
 bool make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, uint32_t box_rows);
 // Row-major bf16 [outer][rows][cols], cols a multiple of 64, as [outer][cols / 64][rows][64] with a box of chunks x box_rows x 64.
 bool make_map_chunks(CUtensorMap* map, const void* ptr, uint64_t cols, uint64_t rows, uint64_t outer, uint32_t box_rows, uint32_t chunks);
+// Row-major [outer][rows][cols] for stores, a box of 32 rows x 128 bytes, 128-byte swizzle.
+bool make_store_map(CUtensorMap* map, void* ptr, bool f32, uint64_t cols, uint64_t rows, uint64_t outer);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
