@@ -413,115 +413,154 @@ __global__ void __launch_bounds__(kThreads) unsort_grad_kernel(const RowArgs a, 
 // Gradient of the sorted rows towards the tokens, the router's gradient added:
 //   dx[t][j] = sum_c dxs[slot[c][t]][j] + dG[t][j / g] / g,   dG_i = [G_i > 0] p_i (q_i - sum_j p_j q_j),
 //   G = group means of x[t] + eps, p = softmax(ReLU(G)), q_i = dp_i + sum_c [idx[c][t] = i] dw[c][t].
-// A warp works on a token and forms G, p and dG anew from the row, which costs the read of x; keeping p would cost E floats a
-// token instead but leave the sign of G open, which the ReLU needs.  Sums of whole units go through shared memory, where
-// the lanes add up the units of a group in order.  deps: each warp's sums in shared memory, the CTA's to `part`.
+// G, p and dG are formed anew from the row, which costs the read of x; keeping p would cost E floats a token instead but leave
+// the sign of G open, which the ReLU needs.  A team of 1 to 8 warps works on a token: the sums of the row's units go through
+// shared memory, where a few lanes each add up a group's; a unit that two groups meet in (MIXED) leaves two sums.  The
+// softmax is every warp's, to save barriers.  deps: the team's sums in shared memory, then the CTA's in `part`.  One warp a token is best where there are many tokens and their sums leave room for them
+// (65536 x 5120: 331 us, 566 with eight), more where a row is long or the tokens few (10737 rows of 5912 floats in 4
+// groups: 708 us with one, 197 with eight; 4 rows of 3216 20.7 against 5.9 us).
 struct RouterArgs {
     const void* x; const float* eps; const int32_t* idx; const float* dw; const float* dp; float* part;
-    int g;                      // units a group
-    float inv_g;                // 1 / elements a group
+    int g;                      // elements a group
+    float inv_g;
+    int warps;                  // of a team: 1, 2, 4, 8
+    int lanes;                  // that share a group's sum, a power of two up to 32
+    size_t floats;              // of shared memory a team
 };
 
-template <int DT, bool VEC, int KM>
-__global__ void __launch_bounds__(kThreads) sort_grad_router_kernel(const RowArgs a, const RouterArgs b, const void* __restrict__ dxs,
+template <int DT, bool VEC, bool MIXED, int KM>
+__global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const RowArgs a, const RouterArgs b, const void* __restrict__ dxs,
                                                                     const int32_t* __restrict__ slot, void* __restrict__ dx) {
     typedef Unit<DT, VEC> U;
-    constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
+    // units in flight a lane and row: registers for four CTAs an SM, which spills cost more than loads in flight gain
+    constexpr int CH = VEC ? (KM <= 2 ? 2 : 1) : KM <= 2 ? 8 / KM : 16 / KM, XCH = VEC ? 4 : 8;
     extern __shared__ float smf[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5, E = a.E;
-    float* sums = smf + (size_t)warp * (a.U + 3 * E);      // [U] sums of the row's units
-    float* G = sums + a.U;                                  // [E] G, then dG / g
-    float* p = G + E;                                       // [E]
-    float* deps = p + E;                                    // [E] sums over this warp's tokens
-    for (int e = lane; e < E; e += 32) deps[e] = 0.0f;
+    const int nt = 32 * b.warps, team = threadIdx.x / nt, teams = kThreads / nt, tid = threadIdx.x - team * nt, lane = tid & 31, E = a.E;
+    auto meet = [&] {               // the team's warps
+        if (nt == 32) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(nt) : "memory");
+    };
+    float* lo = smf + team * b.floats;                            // [U] sum of a unit's elements in the group of its first
+    float* hi = lo + a.U;                       // [U] and of the others (MIXED)
+    float* G = hi + (MIXED ? a.U : 0);          // [E]
+    float* dG = G + E;                          // [E] dG / g
+    float* deps = dG + E;                       // [E] sums over this team's tokens
+    for (int e = tid; e < E; e += nt) deps[e] = 0.0f;
     pdl_wait();
     pdl_trigger();
-    const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
-    for (long long t = lo + warp; t < hi; t += nw) {
-        int s[KM], id[KM];
+    const long long first = (long long)blockIdx.x * a.tpc, last = min((long long)a.T, first + a.tpc);
+    for (long long t = first + team; t < last; t += teams) {
+        int s[KM];
+#pragma unroll
+        for (int c = 0; c < KM; ++c) {
+            s[c] = dxs && c < a.K ? __ldg(slot + (long long)c * a.T + t) : -1;
+            if (s[c] >= a.rows) s[c] = -1;
+        }
+        for (int u0 = tid; u0 < a.U; u0 += XCH * nt) {
+            typename U::Raw r[XCH];
+#pragma unroll
+            for (int i = 0; i < XCH; ++i)
+                if (u0 + nt * i < a.U) r[i] = U::load(b.x, t * a.U + u0 + nt * i);
+#pragma unroll
+            for (int i = 0; i < XCH; ++i) {
+                const int u = u0 + nt * i;
+                if (u >= a.U) break;
+                float f[U::N];
+                U::widen(r[i], f);
+                if (MIXED) {
+                    const int left = b.g - (int)((unsigned)(u * U::N) % (unsigned)b.g);     // elements to the group's end
+                    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < U::N; ++k) {
+                        if (k < left) s0 += f[k];
+                        else s1 += f[k];
+                    }
+                    lo[u] = s0;
+                    hi[u] = s1;
+                } else {
+                    float sum = f[0];
+#pragma unroll
+                    for (int k = 1; k < U::N; ++k) sum += f[k];
+                    lo[u] = sum;
+                }
+            }
+        }
+        meet();
+        {
+            const int j = tid & (b.lanes - 1), per = nt / b.lanes;
+            for (int e0 = 0; e0 < E; e0 += per) {
+                const int e = e0 + tid / b.lanes;
+                float sum = 0.0f;
+                if (e < E) {
+                    const int begin = e * b.g, end = begin + b.g - 1;      // first and last element
+                    const int ub = begin / U::N, ue = end / U::N;
+                    for (int u = ub + j; u <= ue; u += b.lanes) sum += MIXED && u == ub && begin % U::N != 0 ? hi[u] : lo[u];
+                }
+                for (int o = b.lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (e < E && j == 0) G[e] = sum * b.inv_g + (b.eps ? __ldg(b.eps + e) : 0.0f);
+            }
+        }
+        int id[KM];
         float dw[KM];
 #pragma unroll
         for (int c = 0; c < KM; ++c) {
-            const long long v = (long long)c * a.T + t;
-            s[c] = dxs && c < a.K ? __ldg(slot + v) : -1;
-            if (s[c] >= a.rows) s[c] = -1;
-            id[c] = c < a.K && b.dw ? __ldg(b.idx + v) : -1;
-            dw[c] = c < a.K && b.dw ? __ldg(b.dw + v) : 0.0f;
+            id[c] = c < a.K && b.dw ? __ldg(b.idx + (long long)c * a.T + t) : -1;
+            dw[c] = c < a.K && b.dw ? __ldg(b.dw + (long long)c * a.T + t) : 0.0f;
         }
-        for (int u0 = lane; u0 < a.U; u0 += 2 * U::CH * 32) {
-            typename U::Raw r[2 * U::CH];
-#pragma unroll
-            for (int i = 0; i < 2 * U::CH; ++i)
-                if (u0 + 32 * i < a.U) r[i] = U::load(b.x, t * a.U + u0 + 32 * i);
-#pragma unroll
-            for (int i = 0; i < 2 * U::CH; ++i) {
-                if (u0 + 32 * i >= a.U) break;
-                float f[U::N];
-                U::widen(r[i], f);
-                float sum = f[0];
-#pragma unroll
-                for (int k = 1; k < U::N; ++k) sum += f[k];
-                sums[u0 + 32 * i] = sum;
-            }
-        }
-        __syncwarp();
-        float top = 0.0f;
-        for (int e = lane; e < E; e += 32) {
-            float sum = 0.0f;
-            for (int k = 0; k < b.g; ++k) sum += sums[e * b.g + k];
-            sum = sum * b.inv_g + (b.eps ? __ldg(b.eps + e) : 0.0f);
-            G[e] = sum;
-            top = fmaxf(top, sum);
-        }
+        meet();
+        float top = 0.0f, z = 0.0f, m = 0.0f;
+        for (int e = lane; e < E; e += 32) top = fmaxf(top, G[e]);
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        float z = 0.0f;
         for (int e = lane; e < E; e += 32) {
-            const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top);    // a NaN stays one
-            p[e] = v;
-            z += v;
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        const float rz = 1.0f / z;
-        float m = 0.0f;
-        for (int e = lane; e < E; e += 32) {
+            const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top);        // a NaN stays one
             float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
             for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
-            const float v = p[e] * rz;
-            p[e] = G[e] <= 0.0f ? 0.0f : v;             // what leaves through the ReLU
+            z += v;
             m = __fmaf_rn(v, q, m);
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
-        for (int e = lane; e < E; e += 32) {
-            float q = b.dp ? __ldg(b.dp + e) : 0.0f;
+        for (int o = 16; o; o >>= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); m += __shfl_xor_sync(0xffffffffu, m, o); }
+        const float rz = 1.0f / z;
+        m *= rz;
+        if (tid < 32) {
+            for (int e = lane; e < E; e += 32) {
+                float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
-            for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
-            const float d = p[e] * (q - m);
-            deps[e] += d;
-            G[e] = d * b.inv_g;
+                for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
+                const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top) * rz;
+                const float d = G[e] <= 0.0f ? 0.0f * v : v * (q - m);      // what leaves through the ReLU
+                deps[e] += d;
+                dG[e] = d * b.inv_g;
+            }
         }
-        __syncwarp();
-        for (int u0 = lane; u0 < a.U; u0 += CH * 32) {
+        meet();
+        for (int u0 = tid; u0 < a.U; u0 += CH * nt) {
             typename U::Raw r[CH][KM];
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int u = u0 + 32 * i;
-                if (u >= a.U) break;
 #pragma unroll
-                for (int c = 0; c < KM; ++c)
-                    if (s[c] >= 0) r[i][c] = U::load(dxs, (long long)s[c] * a.U + u);
+                for (int c = 0; c < KM; ++c) {
+                    if (u0 + nt * i < a.U && s[c] >= 0) r[i][c] = U::load(dxs, (long long)s[c] * a.U + u0 + nt * i);
+                }
             }
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int u = u0 + 32 * i;
+                const int u = u0 + nt * i;
                 if (u >= a.U) break;
-                const float d = G[u / b.g];
+                const int e = (int)((unsigned)(u * U::N) / (unsigned)b.g);
                 float acc[U::N], v[U::N];
+                const float d = dG[e];
+                if (MIXED) {
+                    const int left = (e + 1) * b.g - u * U::N;
+                    const float d1 = left < U::N ? dG[e + 1] : 0.0f;
 #pragma unroll
-                for (int k = 0; k < U::N; ++k) acc[k] = d;
+                    for (int k = 0; k < U::N; ++k) acc[k] = k < left ? d : d1;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < U::N; ++k) acc[k] = d;
+                }
 #pragma unroll
                 for (int c = 0; c < KM; ++c) {
                     if (s[c] < 0) continue;
@@ -532,13 +571,12 @@ __global__ void __launch_bounds__(kThreads) sort_grad_router_kernel(const RowArg
                 U::store(dx, t * a.U + u, U::narrow(acc));
             }
         }
-        __syncwarp();
     }
     if (!b.part) return;
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+    for (int e = threadIdx.x; e < E; e += kThreads) {
         float sum = 0.0f;
-        for (int w = 0; w < nw; ++w) sum += smf[(size_t)w * (a.U + 3 * E) + a.U + 2 * E + e];
+        for (int w = 0; w < teams; ++w) sum += smf[w * b.floats + (deps - lo) + e];
         b.part[(size_t)blockIdx.x * E + e] = sum;
     }
 }
@@ -583,13 +621,19 @@ RowArgs row_args(const locmoe_shape_t& s, int K, int U, int* grid) {
 }
 
 constexpr size_t kRouterSmem = 200 * 1024;
-size_t router_warp_bytes(int U, int E) { return ((size_t)U + 3 * (size_t)E) * sizeof(float); }
-// Whether a row's groups are whole 16-byte units.
-bool router_vec(const locmoe_shape_t& s, bool aligned) {
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
-    return aligned && (s.H / s.E) % n == 0;
+// How a row is cut for the router's gradient: units of 16 bytes where a unit meets two groups at most, whole in one (or MIXED), else
+// elements.
+struct RouterPlan { bool vec, mixed; int U; size_t smem; };
+RouterPlan router_plan(const locmoe_shape_t& s, bool aligned) {
+    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8, g = s.H / s.E;
+    RouterPlan p;
+    p.vec = aligned && s.H % n == 0 && g >= n;
+    p.mixed = p.vec && g % n != 0;
+    p.U = p.vec ? s.H / n : s.H;
+    p.smem = ((size_t)p.U * (p.mixed ? 2 : 1) + 3 * (size_t)s.E) * sizeof(float);
+    return p;
 }
-int router_grid_cap() { return 8 * sm_count(); }
+int router_grid_cap() { return 4 * sm_count(); }        // what is resident
 
 #define LOCMOE_BY_UNIT(DTYPE, VEC, F, ...)                                             \
     ((DTYPE) == LOCMOE_F32 ? ((VEC) ? F<LOCMOE_F32, true>(__VA_ARGS__) : F<LOCMOE_F32, false>(__VA_ARGS__)) \
@@ -613,15 +657,19 @@ int unsort_grad_dt(int grid, const RowArgs& a, const void* dout, const void* y, 
     return launch_pdl(k, dim3(grid), dim3(kThreads), 0, st, a, dout, y, offsets, slot, w, dy, dw);
 }
 template <int DT, bool VEC>
-int sort_grad_router_dt(int grid, int warps, size_t smem, const RowArgs& a, const RouterArgs& b, const void* dxs, const int32_t* slot, void* dx,
+int sort_grad_router_dt(int grid, const RouterPlan& p, const RowArgs& a, const RouterArgs& b, const void* dxs, const int32_t* slot, void* dx,
                         cudaStream_t st) {
-    auto* k = a.K == 1 ? sort_grad_router_kernel<DT, VEC, 1> : a.K == 2 ? sort_grad_router_kernel<DT, VEC, 2>
-            : a.K <= 4 ? sort_grad_router_kernel<DT, VEC, 4> : sort_grad_router_kernel<DT, VEC, 8>;
+#define LOCMOE_BY_CHOICES(MIXED)                                                                                              \
+    (a.K == 1 ? sort_grad_router_kernel<DT, VEC, MIXED, 1> : a.K == 2 ? sort_grad_router_kernel<DT, VEC, MIXED, 2>             \
+     : a.K <= 4 ? sort_grad_router_kernel<DT, VEC, MIXED, 4> : sort_grad_router_kernel<DT, VEC, MIXED, 8>)
+    auto* k = VEC && p.mixed ? LOCMOE_BY_CHOICES(VEC) : LOCMOE_BY_CHOICES(false);
+#undef LOCMOE_BY_CHOICES
+    const size_t smem = p.smem * (kWarps / b.warps);
     if (smem > 48 * 1024 && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRouterSmem) != cudaSuccess) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;
     }
-    return launch_pdl(k, dim3(grid), dim3(32 * warps), smem, st, a, b, dxs, slot, dx);
+    return launch_pdl(k, dim3(grid), dim3(kThreads), smem, st, a, b, dxs, slot, dx);
 }
 
 }  // namespace
@@ -696,26 +744,28 @@ int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const v
     return rc ? rc : check_launch();
 }
 
-// A row's unit sums have to fit the shared memory of a CTA, whichever way its arrays are aligned.
-bool sort_grad_fits(const locmoe_shape_t& s) { return router_warp_bytes(router_vec(s, true) ? s.H / (s.x_dtype == LOCMOE_F32 ? 4 : 8) : s.H, s.E) <= kRouterSmem; }
+// A row's sums have to fit the shared memory of a CTA.
+bool sort_grad_fits(const locmoe_shape_t& s) { return router_plan(s, true).smem <= kRouterSmem; }
 size_t sort_grad_ws_bytes(const locmoe_shape_t& s) { return ((size_t)router_grid_cap() * s.E * sizeof(float) + 255) & ~(size_t)255; }
 
 int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g, void* ws, cudaStream_t st) {
     if (!g.x) return launch_unsort_rows(s, K, g.dxs, g.slot, nullptr, nullptr, g.dx, st);
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
-    const bool vec = router_vec(s, aligned16(g.x) && aligned16(g.dxs) && aligned16(g.dx));
-    const int U = vec ? s.H / n : s.H;
-    const size_t per = router_warp_bytes(U, s.E);
-    if (per > kRouterSmem) return LOCMOE_ERR_ALIGN;      // arrays that are not 16-byte aligned take more room
-    int warps = (int)(kRouterSmem / per);
-    if (warps > kWarps) warps = kWarps;
-    RowArgs a{s.T, U, K, s.E, (long long)K * s.T, 32, 1};
-    long long grid = ((long long)s.T + warps - 1) / warps;
+    const RouterPlan p = router_plan(s, aligned16(g.x) && aligned16(g.dxs) && aligned16(g.dx));
+    if (p.smem > kRouterSmem) return LOCMOE_ERR_ALIGN;      // arrays that are not 16-byte aligned take more room
+    // warps a token: so many that four CTAs' sums fit an SM, and while all tokens are still at work at once
+    int warps = 1;
+    while (warps < kWarps && ((kWarps / warps) * p.smem > 50 * 1024 || 2ll * warps * s.T <= (long long)router_grid_cap() * kWarps)) warps *= 2;
+    int lanes = 32;
+    while (lanes > 1 && (long long)lanes * s.E > 32 * warps) lanes /= 2;
+    const int teams = kWarps / warps;
+    RowArgs a{s.T, p.U, K, s.E, (long long)K * s.T, 32, 1};
+    long long grid = ((long long)s.T + teams - 1) / teams;
     if (grid > router_grid_cap()) grid = router_grid_cap();
     a.tpc = (int)((s.T + grid - 1) / grid);
     grid = (s.T + a.tpc - 1) / a.tpc;
-    const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, U / s.E, 1.0f / (float)(s.H / s.E)};
-    int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_grad_router_dt, (int)grid, warps, per * warps, a, b, g.dxs, g.slot, g.dx, st);
+    const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, s.H / s.E, 1.0f / (float)(s.H / s.E), warps, lanes,
+                       p.smem / sizeof(float)};
+    int rc = LOCMOE_BY_UNIT(s.x_dtype, p.vec, sort_grad_router_dt, (int)grid, p, a, b, g.dxs, g.slot, g.dx, st);
     if (rc == LOCMOE_OK && g.deps)
         rc = launch_pdl(deps_finish_kernel, dim3((s.E + 31) / 32), dim3(kFinishThreads), 0, st, (const float*)ws, (int)grid, s.E, g.deps);
     return rc ? rc : check_launch();

@@ -78,7 +78,7 @@ def test_refusals_of_the_calls_on_sorted_tokens(B):
     assert _sort_grad(B, x=None) == -1                                         # what belongs to the router needs the tokens
     assert _sort_grad(B, x=None, eps=None, dw=None, dp=None, deps=None, dxs=None) == -1
     assert _sort_grad(B, _shape(B, H=60)) == -2                                # groups of H / E
-    assert _sort_grad(B, _shape(B, H=52 * 1001, E=52)) == -7                   # 1001 is no whole number of 16 bytes
+    assert _sort_grad(B, _shape(B, H=52 * 1001, E=52)) == -7                   # 52052 elements, no whole number of 16 bytes
     assert _sort_grad(B, ws=None) == _sort_grad(B, ws=P + 16) == -5
     assert _sort_grad(B, ws_bytes=B.locmoe_sort_grad_bytes(_shape(B)) - 1) == -5
     for name in ("dxs", "slot", "x", "eps", "idx_k", "dw", "dp", "dx", "deps"):
