@@ -546,8 +546,8 @@ int locmoe_sort(const locmoe_shape_t* shape, int32_t K, const int32_t* idx_k, co
     if (!element_aligned(x, esz) || !element_aligned(xs, esz)) return LOCMOE_ERR_ALIGN;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (x && sort_is_few(shape->T, K)) return launch_sort_few(*shape, K, idx_k, x, offsets, slot, inv, load, xs, st);
-    rc = launch_sort_plan(shape->T, K, shape->E, idx_k, offsets, slot, inv, load, st);
-    if (rc == LOCMOE_OK && x) rc = launch_sort_rows(*shape, K, x, offsets, slot, xs, st);
+    rc = launch_sort_plan(shape->T, K, shape->E, idx_k, offsets, slot, inv, x ? 0 : 1, load, st);
+    if (rc == LOCMOE_OK && x) rc = launch_sort_rows(*shape, K, x, offsets, slot, inv, xs, st);
     return rc;
 }
 

@@ -134,11 +134,11 @@ size_t block_norm_grad_ws_bytes(const locmoe_shape_t& s);
 int launch_block_norm(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_t& b, cudaStream_t st);
 int launch_block_norm_grad(const locmoe_shape_t& s, long long rows, const locmoe_block_norm_grad_t& b, void* ws, cudaStream_t st);
 
-int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load, cudaStream_t st);
+int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int with_inv, int32_t* load, cudaStream_t st);
 bool sort_is_few(int T, int K);
 int launch_sort_few(const locmoe_shape_t& s, int K, const int32_t* idx, const void* x, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load,
                     void* xs, cudaStream_t st);
-int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st);
+int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, int32_t* inv, void* xs, cudaStream_t st);
 int launch_unsort_rows(const locmoe_shape_t& s, int K, const void* y, const int32_t* slot, const float* w, const void* residual, void* out,
                        cudaStream_t st);
 int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot,

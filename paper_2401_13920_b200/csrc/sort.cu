@@ -14,12 +14,13 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // ---- the order: one cluster, counts in shared memory ----
-// A warp owns a contiguous run of assignments, a CTA the runs of its 32 warps, the cluster all of them.  Pass 1 counts each
-// warp's assignments by expert, without atomics: lanes with the same expert find each other by match, the lowest adds.
-// The counts become first rows by sums over experts, CTAs (through distributed shared memory) and warps; pass 2 hands out
-// the rows in order.  The index array is read twice, 131072 assignments by 8 CTAs in about 10 us.
+// A warp owns a contiguous run of assignments, a CTA the runs of its 32 warps, the cluster all of them.  Pass 1 ranks each
+// assignment among its warp's of the same expert and counts them, without atomics: lanes with the same expert find each
+// other by a ballot a bit, the lowest adds.  The counts become first rows by sums over experts, CTAs (through distributed
+// shared memory) and warps; pass 2 adds them to the ranks.  131072 assignments by 16 CTAs in 13 us (28 with 8 and match.any, of
+// which an SM does one in 60 cycles, in both passes).
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32, kPlanBatch = 8;
-constexpr int kPlanMaxCtas = 8;          // the portable cluster size
+constexpr int kPlanRun = 1024;           // assignments a CTA before another is taken, up to 16 (8 where the device has no more)
 
 __device__ __forceinline__ int ld_cluster(const int* p, int cta) {
     uint32_t ra;
@@ -32,8 +33,23 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Lanes that hold the same key of BITS bits.
+template <int BITS>
+__device__ __forceinline__ unsigned same_key(int key) {
+    unsigned same = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < BITS; ++i) {
+        const bool on = (key >> i) & 1;
+        const unsigned b = __ballot_sync(0xffffffffu, on);
+        same &= on ? b : ~b;
+    }
+    return same;
+}
+
+template <int BITS>
 __global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* __restrict__ idx, int V, int T, int E, int32_t* __restrict__ offsets,
-                                                                 int32_t* __restrict__ slot, int32_t* __restrict__ inv, int32_t* __restrict__ load) {
+                                                                 int32_t* __restrict__ slot, int32_t* __restrict__ inv, int with_inv,
+                                                                 int32_t* __restrict__ load) {
     extern __shared__ int sm[];
     int* tot = sm;              // [E] assignments of this CTA
     int* first = tot + E;       // [E] assignments of this CTA's first choices
@@ -56,17 +72,22 @@ __global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* 
         }
 #pragma unroll
         for (int i = 0; i < kPlanBatch; ++i) {
+            const long long v = b + 32 * i + lane;
             if (b + 32 * i >= hi) break;
             const bool ok = key[i] >= 0 && key[i] < E;
-            const unsigned same = __match_any_sync(0xffffffffu, ok ? key[i] : -1);
-            if (ok && lane == __ffs(same) - 1) mine[key[i]] += __popc(same);
-            if (load && ok && b + 32 * i + lane < T) atomicAdd(first + key[i], 1);
+            const unsigned same = same_key<BITS>(ok ? key[i] : E), below = same & ((1u << lane) - 1u);
+            const int before = ok ? mine[key[i]] : 0;
+            __syncwarp();
+            if (ok && below == 0) mine[key[i]] = before + __popc(same);
+            if (load && ok && v < T) atomicAdd(first + key[i], 1);
+            if (v < hi) slot[v] = before + __popc(below);       // among this warp's
             __syncwarp();
         }
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += kPlanThreads) {
         int sum = 0;
+#pragma unroll 16
         for (int w = 0; w < kPlanWarps; ++w) sum += cnt[w * E + e];
         tot[e] = sum;
     }
@@ -93,8 +114,13 @@ __global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* 
     }
     if (lane == 31) scan[warp] = up;
     cluster_barrier();             // the other CTAs' counts have been read, and scan is complete
-    int lower = 0;
-    for (int w = 0; w < warp; ++w) lower += scan[w];
+    int lower = 0, kept = 0;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) {
+        const int n = scan[w];
+        if (w < warp) lower += n;
+        kept += n;
+    }
     if (e < E) {
         int row = lower + up - all;
         if (rank == 0) {
@@ -102,34 +128,29 @@ __global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* 
             if (e == E - 1) offsets[E] = row + all;
         }
         row += before;
+#pragma unroll 8
         for (int w = 0; w < kPlanWarps; ++w) {
             const int n = cnt[w * E + e];
             cnt[w * E + e] = row;
             row += n;
         }
     }
-    int kept = 0;
-    for (int w = 0; w < kPlanWarps; ++w) kept += scan[w];
     __syncthreads();
     for (long long b = lo; b < hi; b += 32 * kPlanBatch) {
-        int key[kPlanBatch];
+        int key[kPlanBatch], row[kPlanBatch];
 #pragma unroll
         for (int i = 0; i < kPlanBatch; ++i) {
             const long long v = b + 32 * i + lane;
             key[i] = v < hi ? __ldg(idx + v) : -1;
+            row[i] = v < hi ? slot[v] : 0;
         }
 #pragma unroll
         for (int i = 0; i < kPlanBatch; ++i) {
             const long long v = b + 32 * i + lane;
-            if (b + 32 * i >= hi) break;
             const bool ok = key[i] >= 0 && key[i] < E;
-            const unsigned same = __match_any_sync(0xffffffffu, ok ? key[i] : -1);
-            const int row = ok ? mine[key[i]] + __popc(same & ((1u << lane) - 1u)) : -1;
-            __syncwarp();
-            if (ok && lane == __ffs(same) - 1) mine[key[i]] += __popc(same);
-            __syncwarp();
-            if (v < hi) slot[v] = row;
-            if (ok) inv[row] = (int)v;
+            row[i] = ok ? row[i] + mine[key[i]] : -1;
+            if (v < hi) slot[v] = row[i];
+            if (ok && with_inv) inv[row[i]] = (int)v;
         }
     }
     for (long long r = (long long)kept + rank * kPlanThreads + threadIdx.x; r < V; r += (long long)nc * kPlanThreads) inv[r] = -1;
@@ -254,10 +275,10 @@ __device__ __forceinline__ void zero_tail(const RowArgs& a, const int32_t* __res
         U::store(out, kept * a.U + i, U::zero());
 }
 
-// xs[slot[c][t]] = x[t]: a token's row is read once and written K times.
+// xs[slot[c][t]] = x[t]: a token's row is read once and written K times; inv along with it.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kThreads) sort_rows_kernel(const RowArgs a, const void* __restrict__ x, const int32_t* __restrict__ offsets,
-                                                             const int32_t* __restrict__ slot, void* __restrict__ xs) {
+                                                             const int32_t* __restrict__ slot, int32_t* __restrict__ inv, void* __restrict__ xs) {
     typedef Unit<DT, VEC> U;
     constexpr int CH = 2 * U::CH;
     pdl_wait();
@@ -276,6 +297,7 @@ __global__ void __launch_bounds__(kThreads) sort_rows_kernel(const RowArgs a, co
             for (int c = 0; c < a.K; ++c) {
                 const int s = __ldg(slot + (long long)c * a.T + t);
                 if (s < 0 || s >= a.rows) continue;
+                if (u0 == 0) inv[s] = (int)((long long)c * a.T + t);
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
                     if (u0 + i * a.width < a.U) U::store(xs, (long long)s * a.U + u0 + i * a.width, r[i]);
@@ -640,8 +662,8 @@ int router_grid_cap() { return 4 * sm_count(); }        // what is resident
                            : ((VEC) ? F<LOCMOE_BF16, true>(__VA_ARGS__) : F<LOCMOE_BF16, false>(__VA_ARGS__)))
 
 template <int DT, bool VEC>
-int sort_rows_dt(int grid, const RowArgs& a, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st) {
-    return launch_pdl(sort_rows_kernel<DT, VEC>, dim3(grid), dim3(kThreads), 0, st, a, x, offsets, slot, xs);
+int sort_rows_dt(int grid, const RowArgs& a, const void* x, const int32_t* offsets, const int32_t* slot, int32_t* inv, void* xs, cudaStream_t st) {
+    return launch_pdl(sort_rows_kernel<DT, VEC>, dim3(grid), dim3(kThreads), 0, st, a, x, offsets, slot, inv, xs);
 }
 template <int DT, bool VEC>
 int unsort_rows_dt(int grid, const RowArgs& a, const void* y, const int32_t* slot, const float* w, const void* residual, void* out, cudaStream_t st) {
@@ -674,15 +696,19 @@ int sort_grad_router_dt(int grid, const RouterPlan& p, const RowArgs& a, const R
 
 }  // namespace
 
-int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int32_t* load, cudaStream_t st) {
+// `with_inv` = 0: the rows' kernel, which follows, writes inv's part with assignments.
+int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int with_inv, int32_t* load, cudaStream_t st) {
     const long long V = (long long)K * T;
     const size_t smem = ((size_t)(kPlanWarps + 2) * E + 32) * sizeof(int);
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(sort_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    auto* kernel = E < 16 ? sort_plan_kernel<4> : E < 64 ? sort_plan_kernel<6> : E < 256 ? sort_plan_kernel<8> : sort_plan_kernel<11>;    // keys 0 to E
+    if ((smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) ||
+        (V > 8ll * kPlanRun && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;
     }
     cudaLaunchConfig_t cfg = {};
-    const int nc = V <= 8192 ? 1 : kPlanMaxCtas;
+    int nc = 1;
+    while (nc < 16 && V > (long long)nc * kPlanRun) nc *= 2;
     cfg.gridDim = dim3(nc); cfg.blockDim = dim3(kPlanThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -690,7 +716,14 @@ int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, 
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, sort_plan_kernel, idx, (int)V, T, E, offsets, slot, inv, load) != cudaSuccess) {
+    int fit = 1;
+    if (nc == 16 && (cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess || fit < 1)) {
+        cudaGetLastError();
+        nc = 8;
+        cfg.gridDim = dim3(nc);
+        attr[0].val.clusterDim.x = nc;
+    }
+    if (cudaLaunchKernelEx(&cfg, kernel, idx, (int)V, T, E, offsets, slot, inv, with_inv, load) != cudaSuccess) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;
     }
@@ -715,12 +748,12 @@ int launch_sort_few(const locmoe_shape_t& s, int K, const int32_t* idx, const vo
     return rc ? rc : check_launch();
 }
 
-int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, void* xs, cudaStream_t st) {
+int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, int32_t* inv, void* xs, cudaStream_t st) {
     const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
     const bool vec = s.H % n == 0 && aligned16(x) && aligned16(xs);
     int grid;
     const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
-    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_rows_dt, grid, a, x, offsets, slot, xs, st);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_rows_dt, grid, a, x, offsets, slot, inv, xs, st);
     return rc ? rc : check_launch();
 }
 
