@@ -6,6 +6,8 @@
   out of the slot buffer, so that the gate-weighted combine costs no pass of its own.
 * ``train_step``: gradients of one block with the activations of the norms kept in 8 bits (``BlockNorm``); the experts are
   plain torch products here, and the router's choices and scores are taken as they are.
+* ``train_step_dropless``: the same with every token kept, two experts each, the router trained as well: tokens sorted by
+  expert, products on ragged groups, and all gradients through ``experts.moe_layer``.
 
     python examples/moe_block.py        # on a B200: both forms of the stack against each other, then training steps
 """
@@ -20,6 +22,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2401_13920_b200 import binding as B  # noqa: E402
 from paper_2401_13920_b200 import block  # noqa: E402
+from paper_2401_13920_b200 import experts  # noqa: E402
 
 EPS = 1e-6
 
@@ -96,6 +99,17 @@ def train_step(h, w_pre, w_in, w_out, w_post, w_next, target, checkpoint=True):
     return loss.detach()
 
 
+def train_step_dropless(h, w_pre, w_in, w_out, w_post, w_next, target, K=2, alpha=0.01):
+    """``train_step`` without a capacity: loss = mean((n' - target)^2) + the balance loss.  The scores are applied to the experts'
+    rows (``moe_layer``), so that their gradient trains the router; the norm after the block has no gate of its own."""
+    _, n = block.BlockNorm.apply(h, None, None, None, w_pre, None, None, 1.0, EPS, True, False)
+    y, aux = experts.moe_layer(n, w_in, w_out, K, alpha=alpha)
+    _, n2 = block.BlockNorm.apply(h, y, None, w_post, w_next, None, None, 1.0, EPS, True, False)
+    loss = (n2.float() - target).square().mean() + aux
+    loss.backward()
+    return loss.detach()
+
+
 def main():
     H, F, E = 2560, 10240, 32
     layers = make_layers(2, H, F, E)
@@ -117,14 +131,15 @@ def main():
     h = torch.randn(T, H, device="cuda").to(torch.bfloat16)
     target = torch.randn(T, H, device="cuda")
     params = [l.w_pre, l.w_in, l.w_out, l.w_post, torch.ones(H, device="cuda")]
-    params = [p.clone().requires_grad_() for p in params]
-    for step in range(5):
-        loss = train_step(h, *params, target)
-        with torch.no_grad():
-            for p in params:
-                p -= 0.5 * p.grad.to(p.dtype)
-                p.grad = None
-        print("  training step %d with 8-bit checkpoints: loss %.5f" % (step, float(loss)))
+    for name, run in (("with 8-bit checkpoints", train_step), ("without a capacity, two experts a token", train_step_dropless)):
+        leaves = [p.clone().requires_grad_() for p in params]
+        for step in range(5):
+            loss = run(h, *leaves, target)
+            with torch.no_grad():
+                for p in leaves:
+                    p -= 0.5 * p.grad.to(p.dtype)
+                    p.grad = None
+            print("  training step %d %s: loss %.5f" % (step, name, float(loss)))
 
 
 if __name__ == "__main__":
