@@ -111,6 +111,8 @@ struct Tiles {
     __device__ __forceinline__ int tiles(const Group& g) const { return g.n > 0 ? m_tiles(g) * a.n_tiles : 0; }
 };
 
+constexpr float kWeightsBlock = 0.4f, kJoinUs = 3.0f, kRowUs = 0.05f;     // us, see deal()
+
 // How the work is dealt, the same on every CTA.  Tiles below `whole` go to the CTAs one by one; what they leave, less than a tile
 // for every CTA, is cut into `runs` equal runs of blocks, or dealt like the others (whole = all tiles) where that is no slower.
 struct Deal {
@@ -126,11 +128,12 @@ __device__ __forceinline__ long long sum_warp(long long v) {
     return v;
 }
 
-// By one warp (all lanes get it).  Splitting the rest saves the part of a wave in which SMs would stand idle: kb blocks times the
-// share of idle SMs, at 0.27 us a block where the tensor cores are the limit, up to 0.73 us where each weight tile is used by
-// one tile of rows and comes out of HBM at 148 x 32 KB a step.  It costs the join's launch, 3 us, and the sums' way through
-// memory, 0.07 us for each row of a tile (1981 rows of 304 x 1024 with every tile split 28 against 19 us whole; 2 rows of
-// 10240 x 2560, 20 tiles in all, 27 us split).
+// By one warp (all lanes get it).  Splitting the rest saves what its longest tile takes beyond an equal share, at 0.27 us a block
+// where the tensor cores are the limit, 0.4 where a few SMs stream the rows of long groups (weights), and up to 0.73 where
+// each weight tile is used by one tile of rows and comes out of HBM at 148 x 32 KB a step.  It costs the join's launch, 3 us,
+// and the sums' way through memory, 0.05 us for each row of a tile (1981 rows of 304 x 1024 with every tile split 28 against
+// 19 us whole; 2 rows of 10240 x 2560, 20 tiles in all, 27 us split; weights' gradient of 10749 rows in 4 groups, 400 x 160,
+// 16 tiles, 52 us whole, 32 split).
 template <int KIND>
 __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, int lane) {
     const Tiles<KIND> t{a, offsets};
@@ -146,25 +149,29 @@ __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, in
     const int rest = d.tiles % a.grid;
     if (rest == 0 || !a.split) return d;
     // blocks of the last `rest` tiles
-    long long units = 0;
+    long long units = 0, longest = (a.K + BK - 1) / BK;
     if (KIND == kWeights) {
+        longest = 0;
         int before = 0;                                         // tiles of the groups passed
         for (int e0 = 0; e0 < a.E; e0 += 32) {
             const Group g = e0 + lane < a.E ? group_of(offsets, e0 + lane, a.R) : Group{0, 0};
             const unsigned busy = __ballot_sync(0xffffffffu, g.n > 0);
             const int per = t.m_tiles(g) * a.n_tiles, first = before + per * __popc(busy & ((1u << lane) - 1u));
-            if (g.n > 0) units += (long long)max(0, min(per, first + per - (d.tiles - rest))) * t.kblocks(g);
+            const int in = g.n > 0 ? max(0, min(per, first + per - (d.tiles - rest))) : 0;
+            units += (long long)in * t.kblocks(g);
+            if (in > 0) longest = max(longest, (long long)t.kblocks(g));
             before += per * __popc(busy);
         }
         units = sum_warp(units);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
     } else {
         units = (long long)rest * ((a.K + BK - 1) / BK);
     }
     rows = sum_warp(rows); rowtiles = sum_warp(rowtiles); groups = sum_warp(groups);
-    const float kb = (float)units / (float)rest, idle = 1.0f - (float)rest / (float)a.grid;
-    const float block = KIND == kWeights ? 0.27f : fmaxf(0.27f, 0.73f * (float)groups / (float)rowtiles);
+    const float block = KIND == kWeights ? kWeightsBlock : fmaxf(0.27f, 0.73f * (float)groups / (float)rowtiles);
     const float tile_rows = KIND == kWeights ? (float)BM : (float)rows / (float)rowtiles;
-    if (kb * idle * block < 3.0f + 0.07f * tile_rows) return d;
+    if (((float)longest - (float)units / (float)a.grid) * block < kJoinUs + kRowUs * tile_rows) return d;
     const long long r = units / 4;                              // a run has at least four blocks
     d.whole = d.tiles - rest;
     d.runs = r < 1 ? 1 : r < a.grid ? (int)r : a.grid;
@@ -176,7 +183,7 @@ __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, in
 template <int KIND>
 bool may_split(const LinearArgs& a) {
     const float kb = (float)(((KIND == kWeights ? a.R : a.K) + BK - 1) / BK);
-    return KIND == kWeights ? kb * 0.27f >= 3.0f + 0.07f * BM : kb * 0.73f >= 3.0f;
+    return KIND == kWeights ? kb * kWeightsBlock >= kJoinUs + kRowUs * BM : kb * 0.73f >= kJoinUs;
 }
 
 struct Item {

@@ -5,6 +5,8 @@
 // those of the same expert with a lower v; inv is the inverse.  All kernels but the first move rows and are bound by HBM:
 // a warp works on a token (or, with short rows, on several), reads each row it needs once with 16-byte streaming loads and
 // writes whole rows; rows that are no multiple of 16 bytes go element by element, more of them in flight.
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace locmoe {
@@ -157,9 +159,10 @@ __global__ void __launch_bounds__(kPlanThreads) sort_plan_kernel(const int32_t* 
 }
 
 // ---- rows ----
-// A row in units: 16 bytes of elements, or one element where rows or arrays are not 16-byte aligned.
-template <int DT, bool VEC> struct Unit;
-template <> struct Unit<LOCMOE_BF16, true> {
+// A row in units: 16 bytes of elements (WIDE), where rows or arrays do not allow that two bf16 (PAIR), else one element (ONE).
+enum { ONE = 0, PAIR = 1, WIDE = 2 };
+template <int DT, int CLS> struct Unit;
+template <> struct Unit<LOCMOE_BF16, WIDE> {
     static constexpr int N = 8, CH = 2;      // elements, units in flight a lane and row
     typedef uint4 Raw;
     static __device__ __forceinline__ Raw load(const void* p, long long i) { return ld_stream(static_cast<const uint4*>(p) + i); }
@@ -174,7 +177,7 @@ template <> struct Unit<LOCMOE_BF16, true> {
     static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { st_stream(static_cast<uint4*>(p) + i, r); }
     static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
 };
-template <> struct Unit<LOCMOE_F32, true> {
+template <> struct Unit<LOCMOE_F32, WIDE> {
     static constexpr int N = 4, CH = 2;
     typedef uint4 Raw;
     static __device__ __forceinline__ Raw load(const void* p, long long i) { return ld_stream(static_cast<const uint4*>(p) + i); }
@@ -187,7 +190,7 @@ template <> struct Unit<LOCMOE_F32, true> {
     static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { st_stream(static_cast<uint4*>(p) + i, r); }
     static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
 };
-template <> struct Unit<LOCMOE_BF16, false> {
+template <> struct Unit<LOCMOE_BF16, ONE> {
     static constexpr int N = 1, CH = 8;
     typedef uint16_t Raw;
     static __device__ __forceinline__ Raw load(const void* p, long long i) { return __ldcs(static_cast<const unsigned short*>(p) + i); }
@@ -196,7 +199,16 @@ template <> struct Unit<LOCMOE_BF16, false> {
     static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { static_cast<uint16_t*>(p)[i] = r; }
     static __device__ __forceinline__ Raw zero() { return 0; }
 };
-template <> struct Unit<LOCMOE_F32, false> {
+template <> struct Unit<LOCMOE_BF16, PAIR> {
+    static constexpr int N = 2, CH = 8;
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ Raw load(const void* p, long long i) { return __ldcs(static_cast<const unsigned int*>(p) + i); }
+    static __device__ __forceinline__ void widen(const Raw& r, float (&f)[N]) { f[0] = bf16_lo(r); f[1] = bf16_hi(r); }
+    static __device__ __forceinline__ Raw narrow(const float (&f)[N]) { return cvt_bf16x2(make_float2(f[0], f[1])); }
+    static __device__ __forceinline__ void store(void* p, long long i, const Raw& r) { static_cast<uint32_t*>(p)[i] = r; }
+    static __device__ __forceinline__ Raw zero() { return 0u; }
+};
+template <> struct Unit<LOCMOE_F32, ONE> {
     static constexpr int N = 1, CH = 8;
     typedef uint32_t Raw;
     static __device__ __forceinline__ Raw load(const void* p, long long i) { return __ldcs(static_cast<const unsigned int*>(p) + i); }
@@ -209,26 +221,31 @@ template <> struct Unit<LOCMOE_F32, false> {
 // Order and rows of a few assignments in one launch: CTA v finds the row of assignment v by counting the assignments that come
 // before it, and copies the token there; the assignments that are not routed take the rows behind the last group, in
 // order, as rows of zeros.  The CTAs after those count for the offsets.  V^2 reads of the index array out of L2 and L1: up to
-// kFewMax assignments that is less than the second launch it saves (8 tokens x 2 choices: 12.9 against 15.6 us
-// a call).
-constexpr int kFewThreads = 128, kFewMax = 512;
+// kFewMax assignments that is less than two launches (8 tokens x 2 choices 12.9 against 15.6 us a call, 2048 assignments with
+// their rows 7.7 against 9.7 us on the device, 4096 already 14.7 against 9.4).
+constexpr int kFewThreads = 128, kFewMax = 2048;
 template <typename R>
 __global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const int32_t* __restrict__ idx, int V, int T, int E, const R* __restrict__ x, int U,
                                                                int32_t* __restrict__ offsets, int32_t* __restrict__ slot, int32_t* __restrict__ inv,
                                                                int32_t* __restrict__ load, R* __restrict__ xs) {
     pdl_wait();
     pdl_trigger();
-    if ((int)blockIdx.x >= V) {
-        const int e = ((int)blockIdx.x - V) * kFewThreads + threadIdx.x;
+    if ((int)blockIdx.x >= V) {             // a warp an offset
+        const int e = ((int)blockIdx.x - V) * (kFewThreads / 32) + (threadIdx.x >> 5);
         if (e > E) return;
         int below = 0, first = 0;
-        for (int u = 0; u < V; ++u) {
+#pragma unroll 4
+        for (int u = threadIdx.x & 31; u < V; u += 32) {
             const int k = __ldg(idx + u);
             below += k >= 0 && k < e;
             first += u < T && k == e;
         }
-        offsets[e] = below;
-        if (load && e < E) load[e] = first;
+        below = __reduce_add_sync(0xffffffffu, below);
+        first = __reduce_add_sync(0xffffffffu, first);
+        if ((threadIdx.x & 31) == 0) {
+            offsets[e] = below;
+            if (load && e < E) load[e] = first;
+        }
         return;
     }
     const int v = blockIdx.x, key = __ldg(idx + v), t = v % T;
@@ -239,11 +256,17 @@ __global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const int32_t* __
     for (int i = 0; i < CH; ++i)
         if (ok && (int)threadIdx.x + i * kFewThreads < U) r[i] = x[(size_t)t * U + threadIdx.x + i * kFewThreads];
     int row = 0;
-    for (int u = threadIdx.x; u - (int)threadIdx.x < V; u += kFewThreads) {
-        const int k = u < V ? __ldg(idx + u) : -1;
+#pragma unroll 4
+    for (int u = threadIdx.x; u < V; u += kFewThreads) {
+        const int k = __ldg(idx + u);
         const bool routed = k >= 0 && k < E;
-        row += __syncthreads_count(u < V && (ok ? routed && (k < key || (k == key && u < v)) : routed || u < v));
+        row += ok ? routed && (k < key || (k == key && u < v)) : routed || u < v;
     }
+    row = __reduce_add_sync(0xffffffffu, row);
+    __shared__ int part[kFewThreads / 32];
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = row;
+    __syncthreads();
+    row = part[0] + part[1] + part[2] + part[3];
     if (threadIdx.x == 0) {
         slot[v] = ok ? row : -1;
         inv[row] = ok ? v : -1;
@@ -259,7 +282,7 @@ __global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const int32_t* __
     }
 }
 
-// What a row kernel works on.  `width` lanes (a power of two) share a token; a CTA owns `tpc` consecutive tokens.
+// What a row kernel works on.  `width` threads (a power of two, up to a CTA) share a token; a CTA owns `tpc` consecutive tokens.
 struct RowArgs {
     int T, U, K, E;             // tokens, units a row, choices, experts
     long long rows;             // K * T
@@ -276,10 +299,10 @@ __device__ __forceinline__ void zero_tail(const RowArgs& a, const int32_t* __res
 }
 
 // xs[slot[c][t]] = x[t]: a token's row is read once and written K times; inv along with it.
-template <int DT, bool VEC>
+template <int DT, int CLS>
 __global__ void __launch_bounds__(kThreads) sort_rows_kernel(const RowArgs a, const void* __restrict__ x, const int32_t* __restrict__ offsets,
                                                              const int32_t* __restrict__ slot, int32_t* __restrict__ inv, void* __restrict__ xs) {
-    typedef Unit<DT, VEC> U;
+    typedef Unit<DT, CLS> U;
     constexpr int CH = 2 * U::CH;
     pdl_wait();
     pdl_trigger();
@@ -308,10 +331,10 @@ __global__ void __launch_bounds__(kThreads) sort_rows_kernel(const RowArgs a, co
 }
 
 // out[t] = residual[t] + sum_c w[c][t] * y[slot[c][t]], choices without a row left out.
-template <int DT, bool VEC, int KM>
+template <int DT, int CLS, int KM>
 __global__ void __launch_bounds__(kThreads) unsort_rows_kernel(const RowArgs a, const void* __restrict__ y, const int32_t* __restrict__ slot,
                                                                const float* __restrict__ w, const void* __restrict__ residual, void* __restrict__ out) {
-    typedef Unit<DT, VEC> U;
+    typedef Unit<DT, CLS> U;
     constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
     pdl_wait();
     pdl_trigger();
@@ -361,17 +384,18 @@ __global__ void __launch_bounds__(kThreads) unsort_rows_kernel(const RowArgs a, 
 }
 
 // dy[slot[c][t]] = w[c][t] * dout[t],  dw[c][t] = <dout[t], y[slot[c][t]]>; a token's dout is read once.
-template <int DT, bool VEC, int KM>
+template <int DT, int CLS, int KM>
 __global__ void __launch_bounds__(kThreads) unsort_grad_kernel(const RowArgs a, const void* __restrict__ dout, const void* __restrict__ y,
                                                                const int32_t* __restrict__ offsets, const int32_t* __restrict__ slot,
                                                                const float* __restrict__ w, void* __restrict__ dy, float* __restrict__ dw) {
-    typedef Unit<DT, VEC> U;
+    __shared__ float sums[kWarps][KM];
+    typedef Unit<DT, CLS> U;
     constexpr int CH = KM <= 2 ? U::CH : U::CH / 2;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x % a.width, step = kThreads / a.width;
     const long long lo = (long long)blockIdx.x * a.tpc, hi = min((long long)a.T, lo + a.tpc);
-    for (long long t0 = lo; t0 < hi; t0 += step) {          // whole warps stay together: the sums are shuffled
+    for (long long t0 = lo; t0 < hi; t0 += step) {          // the CTA stays together: the sums are shuffled and shared
         const long long t = t0 + threadIdx.x / a.width;
         int s[KM];
         float g[KM], dot[KM];
@@ -423,10 +447,25 @@ __global__ void __launch_bounds__(kThreads) unsort_grad_kernel(const RowArgs a, 
         }
         if (dw) {
 #pragma unroll
-            for (int c = 0; c < KM; ++c) {
-                for (int o = a.width >> 1; o; o >>= 1) dot[c] += __shfl_xor_sync(0xffffffffu, dot[c], o);
-                if (lane == 0 && t < hi && c < a.K) dw[(long long)c * a.T + t] = dot[c];
+            for (int c = 0; c < KM; ++c)
+                for (int o = min(a.width, 32) >> 1; o; o >>= 1) dot[c] += __shfl_xor_sync(0xffffffffu, dot[c], o);
+            if (a.width > 32) {             // several warps a token: their sums in order
+                if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+                    for (int c = 0; c < KM; ++c) sums[threadIdx.x >> 5][c] = dot[c];
+                }
+                __syncthreads();
+                if (lane == 0) {
+                    for (int w = 1; w < a.width / 32; ++w) {
+#pragma unroll
+                        for (int c = 0; c < KM; ++c) dot[c] += sums[(threadIdx.x >> 5) + w][c];
+                    }
+                }
+                __syncthreads();
             }
+#pragma unroll
+            for (int c = 0; c < KM; ++c)
+                if (lane == 0 && t < hi && c < a.K) dw[(long long)c * a.T + t] = dot[c];
         }
     }
     if (dy) zero_tail<U>(a, offsets, dy);
@@ -450,12 +489,12 @@ struct RouterArgs {
     size_t floats;              // of shared memory a team
 };
 
-template <int DT, bool VEC, bool MIXED, int KM>
+template <int DT, int CLS, bool MIXED, int KM>
 __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const RowArgs a, const RouterArgs b, const void* __restrict__ dxs,
                                                                     const int32_t* __restrict__ slot, void* __restrict__ dx) {
-    typedef Unit<DT, VEC> U;
+    typedef Unit<DT, CLS> U;
     // units in flight a lane and row: registers for four CTAs an SM, which spills cost more than loads in flight gain
-    constexpr int CH = VEC ? (KM <= 2 ? 2 : 1) : KM <= 2 ? 8 / KM : 16 / KM, XCH = VEC ? 4 : 8;
+    constexpr int CH = CLS == WIDE ? (KM <= 2 ? 2 : 1) : KM <= 2 ? 8 / KM : 16 / KM, XCH = CLS == WIDE ? 4 : 8;
     extern __shared__ float smf[];
     const int nt = 32 * b.warps, team = threadIdx.x / nt, teams = kThreads / nt, tid = threadIdx.x - team * nt, lane = tid & 31, E = a.E;
     auto meet = [&] {               // the team's warps
@@ -627,12 +666,12 @@ __global__ void __launch_bounds__(kFinishThreads) deps_finish_kernel(const float
     if (lane == 0 && blockIdx.x * 32 + warp < E) deps[blockIdx.x * 32 + warp] = sum;
 }
 
-bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }   // an absent array is
-
-// Tokens a CTA and lanes a token of a row kernel.
+// Tokens a CTA and threads a token of a row kernel.
 RowArgs row_args(const locmoe_shape_t& s, int K, int U, int* grid) {
     RowArgs a{s.T, U, K, s.E, (long long)K * s.T, 32, 1};
     while (a.width > 1 && a.width / 2 >= U) a.width /= 2;
+    // few tokens with long rows: more threads a token (48 tokens of 7928, three choices, their gradient 19.6 against 5.3 us)
+    while (a.width >= 32 && a.width < kThreads && a.width < U && 2ll * s.T * a.width <= 1024ll * sm_count()) a.width *= 2;
     const long long step = kThreads / a.width;
     const long long want = (s.T + step - 1) / step, cap = 1024ll * sm_count();     // many short CTAs, in ascending token order
     const long long g = want < cap ? want : cap;
@@ -642,49 +681,59 @@ RowArgs row_args(const locmoe_shape_t& s, int K, int U, int* grid) {
     return a;
 }
 
+// The widest unit that rows of H elements in these arrays (absent ones are no obstacle) are made of.
+int unit_of(const locmoe_shape_t& s, std::initializer_list<const void*> arrays) {
+    const int esz = s.x_dtype == LOCMOE_F32 ? 4 : 2;
+    uintptr_t any = (uintptr_t)s.H * esz;
+    for (const void* p : arrays) any |= (uintptr_t)p;
+    return any % 16 == 0 ? WIDE : esz == 2 && any % 4 == 0 ? PAIR : ONE;
+}
+int unit_elements(const locmoe_shape_t& s, int cls) { return cls == WIDE ? (s.x_dtype == LOCMOE_F32 ? 4 : 8) : cls == PAIR ? 2 : 1; }
+
 constexpr size_t kRouterSmem = 200 * 1024;
-// How a row is cut for the router's gradient: units of 16 bytes where a unit meets two groups at most, whole in one (or MIXED), else
-// elements.
-struct RouterPlan { bool vec, mixed; int U; size_t smem; };
-RouterPlan router_plan(const locmoe_shape_t& s, bool aligned) {
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8, g = s.H / s.E;
+// How a row is cut for the router's gradient: units that meet two groups at most, whole in one or of 16 bytes (MIXED).
+struct RouterPlan { int cls; bool mixed; int U; size_t smem; };
+RouterPlan router_plan(const locmoe_shape_t& s, int cls) {
+    const int g = s.H / s.E;
     RouterPlan p;
-    p.vec = aligned && s.H % n == 0 && g >= n;
-    p.mixed = p.vec && g % n != 0;
-    p.U = p.vec ? s.H / n : s.H;
+    p.cls = cls == WIDE && g < unit_elements(s, WIDE) ? PAIR : cls;
+    if (p.cls == PAIR && (s.x_dtype == LOCMOE_F32 || g % 2 != 0)) p.cls = ONE;
+    p.mixed = p.cls == WIDE && g % unit_elements(s, WIDE) != 0;
+    p.U = s.H / unit_elements(s, p.cls);
     p.smem = ((size_t)p.U * (p.mixed ? 2 : 1) + 3 * (size_t)s.E) * sizeof(float);
     return p;
 }
 int router_grid_cap() { return 4 * sm_count(); }        // what is resident
 
-#define LOCMOE_BY_UNIT(DTYPE, VEC, F, ...)                                             \
-    ((DTYPE) == LOCMOE_F32 ? ((VEC) ? F<LOCMOE_F32, true>(__VA_ARGS__) : F<LOCMOE_F32, false>(__VA_ARGS__)) \
-                           : ((VEC) ? F<LOCMOE_BF16, true>(__VA_ARGS__) : F<LOCMOE_BF16, false>(__VA_ARGS__)))
+#define LOCMOE_BY_UNIT(DTYPE, CLS, F, ...)                                                       \
+    ((DTYPE) == LOCMOE_F32 ? ((CLS) == WIDE ? F<LOCMOE_F32, WIDE>(__VA_ARGS__) : F<LOCMOE_F32, ONE>(__VA_ARGS__)) \
+     : (CLS) == WIDE ? F<LOCMOE_BF16, WIDE>(__VA_ARGS__)                                         \
+     : (CLS) == PAIR ? F<LOCMOE_BF16, PAIR>(__VA_ARGS__) : F<LOCMOE_BF16, ONE>(__VA_ARGS__))
 
-template <int DT, bool VEC>
+template <int DT, int CLS>
 int sort_rows_dt(int grid, const RowArgs& a, const void* x, const int32_t* offsets, const int32_t* slot, int32_t* inv, void* xs, cudaStream_t st) {
-    return launch_pdl(sort_rows_kernel<DT, VEC>, dim3(grid), dim3(kThreads), 0, st, a, x, offsets, slot, inv, xs);
+    return launch_pdl(sort_rows_kernel<DT, CLS>, dim3(grid), dim3(kThreads), 0, st, a, x, offsets, slot, inv, xs);
 }
-template <int DT, bool VEC>
+template <int DT, int CLS>
 int unsort_rows_dt(int grid, const RowArgs& a, const void* y, const int32_t* slot, const float* w, const void* residual, void* out, cudaStream_t st) {
-    auto* k = a.K == 1 ? unsort_rows_kernel<DT, VEC, 1> : a.K == 2 ? unsort_rows_kernel<DT, VEC, 2>
-            : a.K <= 4 ? unsort_rows_kernel<DT, VEC, 4> : unsort_rows_kernel<DT, VEC, 8>;
+    auto* k = a.K == 1 ? unsort_rows_kernel<DT, CLS, 1> : a.K == 2 ? unsort_rows_kernel<DT, CLS, 2>
+            : a.K <= 4 ? unsort_rows_kernel<DT, CLS, 4> : unsort_rows_kernel<DT, CLS, 8>;
     return launch_pdl(k, dim3(grid), dim3(kThreads), 0, st, a, y, slot, w, residual, out);
 }
-template <int DT, bool VEC>
+template <int DT, int CLS>
 int unsort_grad_dt(int grid, const RowArgs& a, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot, const float* w,
                    void* dy, float* dw, cudaStream_t st) {
-    auto* k = a.K == 1 ? unsort_grad_kernel<DT, VEC, 1> : a.K == 2 ? unsort_grad_kernel<DT, VEC, 2>
-            : a.K <= 4 ? unsort_grad_kernel<DT, VEC, 4> : unsort_grad_kernel<DT, VEC, 8>;
+    auto* k = a.K == 1 ? unsort_grad_kernel<DT, CLS, 1> : a.K == 2 ? unsort_grad_kernel<DT, CLS, 2>
+            : a.K <= 4 ? unsort_grad_kernel<DT, CLS, 4> : unsort_grad_kernel<DT, CLS, 8>;
     return launch_pdl(k, dim3(grid), dim3(kThreads), 0, st, a, dout, y, offsets, slot, w, dy, dw);
 }
-template <int DT, bool VEC>
+template <int DT, int CLS>
 int sort_grad_router_dt(int grid, const RouterPlan& p, const RowArgs& a, const RouterArgs& b, const void* dxs, const int32_t* slot, void* dx,
                         cudaStream_t st) {
 #define LOCMOE_BY_CHOICES(MIXED)                                                                                              \
-    (a.K == 1 ? sort_grad_router_kernel<DT, VEC, MIXED, 1> : a.K == 2 ? sort_grad_router_kernel<DT, VEC, MIXED, 2>             \
-     : a.K <= 4 ? sort_grad_router_kernel<DT, VEC, MIXED, 4> : sort_grad_router_kernel<DT, VEC, MIXED, 8>)
-    auto* k = VEC && p.mixed ? LOCMOE_BY_CHOICES(VEC) : LOCMOE_BY_CHOICES(false);
+    (a.K == 1 ? sort_grad_router_kernel<DT, CLS, MIXED, 1> : a.K == 2 ? sort_grad_router_kernel<DT, CLS, MIXED, 2>             \
+     : a.K <= 4 ? sort_grad_router_kernel<DT, CLS, MIXED, 4> : sort_grad_router_kernel<DT, CLS, MIXED, 8>)
+    auto* k = CLS == WIDE && p.mixed ? LOCMOE_BY_CHOICES(CLS == WIDE) : LOCMOE_BY_CHOICES(false);
 #undef LOCMOE_BY_CHOICES
     const size_t smem = p.smem * (kWarps / b.warps);
     if (smem > 48 * 1024 && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRouterSmem) != cudaSuccess) {
@@ -737,53 +786,51 @@ int launch_sort_few(const locmoe_shape_t& s, int K, const int32_t* idx, const vo
                     void* xs, cudaStream_t st) {
     const int V = K * s.T, esz = s.x_dtype == LOCMOE_F32 ? 4 : 2;
     const long long bytes = (long long)s.H * esz;
-    const dim3 grid(V + (s.E + kFewThreads) / kFewThreads), block(kFewThreads);      // E + 1 offsets
+    const dim3 grid(V + (s.E + kFewThreads / 32) / (kFewThreads / 32)), block(kFewThreads);      // E + 1 offsets
     int rc;
-    if (bytes % 16 == 0 && aligned16(x) && aligned16(xs))
+    const int cls = unit_of(s, {x, xs});
+    if (cls == WIDE)
         rc = launch_pdl(sort_few_kernel<uint4>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint4*)x, (int)(bytes / 16), offsets, slot, inv, load, (uint4*)xs);
-    else if (esz == 4)
-        rc = launch_pdl(sort_few_kernel<uint32_t>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint32_t*)x, (int)s.H, offsets, slot, inv, load, (uint32_t*)xs);
+    else if (cls == PAIR || esz == 4)
+        rc = launch_pdl(sort_few_kernel<uint32_t>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint32_t*)x, (int)(bytes / 4), offsets, slot, inv, load, (uint32_t*)xs);
     else
         rc = launch_pdl(sort_few_kernel<uint16_t>, grid, block, 0, st, idx, V, (int)s.T, (int)s.E, (const uint16_t*)x, (int)s.H, offsets, slot, inv, load, (uint16_t*)xs);
     return rc ? rc : check_launch();
 }
 
 int launch_sort_rows(const locmoe_shape_t& s, int K, const void* x, const int32_t* offsets, const int32_t* slot, int32_t* inv, void* xs, cudaStream_t st) {
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
-    const bool vec = s.H % n == 0 && aligned16(x) && aligned16(xs);
+    const int cls = unit_of(s, {x, xs});
     int grid;
-    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
-    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, sort_rows_dt, grid, a, x, offsets, slot, inv, xs, st);
+    const RowArgs a = row_args(s, K, s.H / unit_elements(s, cls), &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, cls, sort_rows_dt, grid, a, x, offsets, slot, inv, xs, st);
     return rc ? rc : check_launch();
 }
 
 int launch_unsort_rows(const locmoe_shape_t& s, int K, const void* y, const int32_t* slot, const float* w, const void* residual, void* out,
                        cudaStream_t st) {
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
-    const bool vec = s.H % n == 0 && aligned16(y) && aligned16(residual) && aligned16(out);
+    const int cls = unit_of(s, {y, residual, out});
     int grid;
-    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
-    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, unsort_rows_dt, grid, a, y, slot, w, residual, out, st);
+    const RowArgs a = row_args(s, K, s.H / unit_elements(s, cls), &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, cls, unsort_rows_dt, grid, a, y, slot, w, residual, out, st);
     return rc ? rc : check_launch();
 }
 
 int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const void* y, const int32_t* offsets, const int32_t* slot,
                        const float* w, void* dy, float* dw, cudaStream_t st) {
-    const int n = s.x_dtype == LOCMOE_F32 ? 4 : 8;
-    const bool vec = s.H % n == 0 && aligned16(dout) && aligned16(y) && aligned16(dy);
+    const int cls = unit_of(s, {dout, y, dy});
     int grid;
-    const RowArgs a = row_args(s, K, vec ? s.H / n : s.H, &grid);
-    const int rc = LOCMOE_BY_UNIT(s.x_dtype, vec, unsort_grad_dt, grid, a, dout, y, offsets, slot, w, dy, dw, st);
+    const RowArgs a = row_args(s, K, s.H / unit_elements(s, cls), &grid);
+    const int rc = LOCMOE_BY_UNIT(s.x_dtype, cls, unsort_grad_dt, grid, a, dout, y, offsets, slot, w, dy, dw, st);
     return rc ? rc : check_launch();
 }
 
 // A row's sums have to fit the shared memory of a CTA.
-bool sort_grad_fits(const locmoe_shape_t& s) { return router_plan(s, true).smem <= kRouterSmem; }
+bool sort_grad_fits(const locmoe_shape_t& s) { return router_plan(s, unit_of(s, {})).smem <= kRouterSmem; }
 size_t sort_grad_ws_bytes(const locmoe_shape_t& s) { return ((size_t)router_grid_cap() * s.E * sizeof(float) + 255) & ~(size_t)255; }
 
 int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g, void* ws, cudaStream_t st) {
     if (!g.x) return launch_unsort_rows(s, K, g.dxs, g.slot, nullptr, nullptr, g.dx, st);
-    const RouterPlan p = router_plan(s, aligned16(g.x) && aligned16(g.dxs) && aligned16(g.dx));
+    const RouterPlan p = router_plan(s, unit_of(s, {g.x, g.dxs, g.dx}));
     if (p.smem > kRouterSmem) return LOCMOE_ERR_ALIGN;      // arrays that are not 16-byte aligned take more room
     // warps a token: so many that four CTAs' sums fit an SM, and while all tokens are still at work at once
     int warps = 1;
@@ -798,7 +845,7 @@ int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g
     grid = (s.T + a.tpc - 1) / a.tpc;
     const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, s.H / s.E, 1.0f / (float)(s.H / s.E), warps, lanes,
                        p.smem / sizeof(float)};
-    int rc = LOCMOE_BY_UNIT(s.x_dtype, p.vec, sort_grad_router_dt, (int)grid, p, a, b, g.dxs, g.slot, g.dx, st);
+    int rc = LOCMOE_BY_UNIT(s.x_dtype, p.cls, sort_grad_router_dt, (int)grid, p, a, b, g.dxs, g.slot, g.dx, st);
     if (rc == LOCMOE_OK && g.deps)
         rc = launch_pdl(deps_finish_kernel, dim3((s.E + 31) / 32), dim3(kFinishThreads), 0, st, (const float*)ws, (int)grid, s.E, g.deps);
     return rc ? rc : check_launch();

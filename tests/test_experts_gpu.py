@@ -91,7 +91,7 @@ def test_order(X, B, T, K, E, kind):
 
 
 SHAPES = [(1, 1, 8, 1, "any"), (3, 8, 5, 4, "bad"), (5, 2, 2560, 4, "any"), (17, 3, 777, 7, "bad"), (300, 2, 96, 8, "any"), (64, 1, 64, 3, "none"),
-          (1000, 4, 264, 16, "bad"), (4099, 2, 40, 8, "any"), (129, 1, 1234, 2, "one")]
+          (1000, 4, 264, 16, "bad"), (4099, 2, 40, 8, "any"), (129, 1, 1234, 2, "one"), (2, 5, 9000, 3, "any"), (700, 3, 96, 8, "bad")]
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
@@ -159,7 +159,8 @@ def router64(x, idx, dw, eps, dp):
 
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("T,K,H,E,kind", [(1, 1, 8, 1, "any"), (9, 2, 2560, 32, "any"), (33, 3, 777, 21, "bad"), (65, 1, 5120, 64, "any"), (50, 8, 1024, 1024, "any"),
-                                          (700, 2, 1000, 4, "bad"), (2500, 4, 128, 32, "none"), (40, 1, 12288, 3, "any")])
+                                          (700, 2, 1000, 4, "bad"), (2500, 4, 128, 32, "none"), (40, 1, 12288, 3, "any"), (31, 3, 1236, 6, "bad"),
+                                          (6000, 2, 96, 24, "any")])
 def test_router_gradient(X, B, T, K, H, E, kind, dt):
     g = gen(T * 3 + H)
     idx = choices(g, T, K, E, kind)
