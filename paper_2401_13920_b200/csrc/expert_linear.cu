@@ -245,9 +245,14 @@ struct Cursor {
         }
         it.kb = kb;
         it.e = e; it.lo = g.lo; it.n = g.n;
-        const int mts = Tiles<KIND>{a, offsets}.m_tiles(g);
-        it.nt = in / mts;               // tiles that share a weight tile are neighbours
-        it.mt = in - it.nt * mts;
+        if (KIND == kWeights && a.boxes) {      // whole rows of the gradient are written at a time
+            it.mt = in / a.n_tiles;
+            it.nt = in - it.mt * a.n_tiles;
+        } else {                        // tiles that share a weight tile are neighbours
+            const int mts = Tiles<KIND>{a, offsets}.m_tiles(g);
+            it.nt = in / mts;
+            it.mt = in - it.nt * mts;
+        }
         return true;
     }
 };
@@ -395,7 +400,7 @@ __device__ __forceinline__ const void* extra_array(const LinearArgs& a) { return
 
 template <int KIND>
 __global__ void __launch_bounds__(KIND == kWeights ? kWeightsThreads : kThreads, 1)
-expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
+expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOther,
                    const LinearArgs a) {
     constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
     constexpr uint64_t kStepA = (A_MN ? 2048 : UMMA_K * 2) >> 4, kStepB = (B_MN ? 2048 : UMMA_K * 2) >> 4;   // 16 steps of the reduction
@@ -421,6 +426,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         mbar_init_fence();
         prefetch_map(&tmA);
         prefetch_map(&tmB);
+        prefetch_map(&tmOther);
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
@@ -443,16 +449,22 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             bool ok = true;
             while (ok && cur.next(it)) {
                 const int m0 = it.mt * BM, n0 = it.nt * BN;
+                // a group's last rows come in boxes of 32: what lies behind them is another group's, and would be read for nothing
+                // (1000 rows of 1560 x 4104 over 24 experts 76 against 65 us)
+                const int few = A_MN || a.a_rows < BM || it.n - m0 > BM - 32 ? 0 : (it.n - m0 + 31) / 32;
+                const uint32_t bytes = few ? (uint32_t)few * 32 * BK * 2 + B_BYTES : STAGE_BYTES;
                 for (int kb = it.kb0; kb < it.kb1; ++kb) {
                     if (!wait_or_abort(&empty[stage], phase ^ 1u, abort_word)) { ok = false; break; }
                     unsigned char* sa = base + (size_t)stage * STAGE_BYTES;
                     unsigned char* sb = sa + a_bytes;
-                    mbar_expect_tx(&full[stage], STAGE_BYTES);
+                    mbar_expect_tx(&full[stage], bytes);
                     if (A_MN && a.a_chunks) {
                         tma_load_4d(sa, &tmA, 0, it.lo + kb * BK, m0 / 64, 0, &full[stage]);
                     } else if (A_MN) {
 #pragma unroll
                         for (int c = 0; c < BM / 64; ++c) tma_load_2d(sa + c * CHUNK_BYTES, &tmA, m0 + 64 * c, it.lo + kb * BK, &full[stage]);
+                    } else if (few) {
+                        for (int i = 0; i < few; ++i) tma_load_2d(sa + i * (32 * BK * 2), &tmOther, kb * BK, it.lo + m0 + 32 * i, &full[stage]);
                     } else {
                         tma_load_2d(sa, &tmA, kb * BK, it.lo + m0, &full[stage]);
                     }
@@ -511,10 +523,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 const int steps = (left + UMMA_K - 1) / UMMA_K;
                 // rows [left, 16 * steps) belong to the next group: zeros.  A row is 128 bytes in each box, whatever the swizzle,
                 // which moves bytes inside a row only.
-                const int rows = steps * UMMA_K - left, per = rows * 8;
-                for (int i = lane; i < (BM + BN) / 64 * per; i += 32) {
-                    const int c = i / per, r = i - c * per;
-                    *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+                for (int r = left + (lane >> 3); r < steps * UMMA_K; r += 4) {
+#pragma unroll
+                    for (int c = 0; c < (BM + BN) / 64; ++c)
+                        *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -675,7 +687,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) {                    // what lies beyond the weights' rows and columns is left out
-                            tma_store_3d(&tmOut, box, n0 + c, m0, it.e);
+                            tma_store_3d(&tmOther, box, n0 + c, m0, it.e);
                             bulk_commit();
                         }
                         turn ^= 1;
@@ -848,14 +860,14 @@ __global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const in
 
 // Weights' gradients: up to this many rows an expert on average a tile is stores more than products, and its rows leave as boxes of
 // 128 bytes a row by TMA; a lane's stores of its own row are 32 bytes each, half sectors where rows do not begin on 32 (72
-// rows of 12 experts, weights of 5440 x 8984: 686 against 340 us).  The boxes take the fourth stage of the ring, which long
+// rows of 12 experts, weights of 5440 x 8984: 686 against 324 us).  The boxes take the fourth stage of the ring, which long
 // reductions need (65536 rows of 10240 x 2560: 64 % of the tensor cores' cycles with three stages, 80 % with four).
 constexpr int kBoxRows = 512;
 
 template <int KIND>
 int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cudaStream_t st) {
     LinearArgs a = a0;
-    CUtensorMap tmA, tmB, tmOut;
+    CUtensorMap tmA, tmB, tmOther;
     a.n_tiles = (a.N + BN - 1) / BN;
     a.grid = sm_count();
     a.part = static_cast<float*>(ws);
@@ -875,8 +887,9 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
         if (!make_map(&tmA, A, 2, da, a.a_rows)) return LOCMOE_ERR_CUDA;
         if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.K, a.E, BK, BN / 64) : make_map(&tmB, B, 3, db, KIND == kForward ? BN : BK))) return LOCMOE_ERR_CUDA;
     }
-    if (KIND != kWeights) tmOut = tmA;          // not used
-    else if (!make_store_map(&tmOut, a.out, a.out_f32, a.N, a.M, a.E)) return LOCMOE_ERR_CUDA;
+    // the weights' gradient on its way out, or A in boxes of 32 rows
+    const uint64_t dims[2] = {(uint64_t)a.K, (uint64_t)a.R};
+    if (!(KIND == kWeights ? make_store_map(&tmOther, a.out, a.out_f32, a.N, a.M, a.E) : make_map(&tmOther, A, 2, dims, 32))) return LOCMOE_ERR_CUDA;
     a.boxes = KIND == kWeights && (long long)a.R < (long long)kBoxRows * a.E;
     a.stages = a.boxes ? kBoxStages : KIND == kWeights ? 4 : (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
@@ -892,7 +905,7 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     }
     const bool join = may_split<KIND>(a);
     a.split = join ? reinterpret_cast<Split*>(a.db_part + (KIND == kWeights ? (size_t)a.grid * 2 * BM : 0)) : nullptr;
-    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, tmOut, a);
+    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, tmOther, a);
     if (rc) return rc;
     if (join) {
         const int parts = (a.part_rows * (BN / 8) + kJoinThreads - 1) / kJoinThreads;
