@@ -623,10 +623,11 @@ int locmoe_unsort_grad(const locmoe_shape_t *shape, int32_t K, const void *dout,
 
 /*
  * The experts' products on rows sorted by expert (locmoe_sort): shape->T rows of shape->H elements, of which expert e has
- * [offsets[e], offsets[e + 1]), any number of them.  All matrices bf16, fp32 accumulation on the tensor cores (tcgen05):
+ * [offsets[e], offsets[e + 1]), any number of them; a slice of the offsets gives a part of the experts.  All matrices bf16, fp32
+ * accumulation on the tensor cores (tcgen05):
  *   z[r] = W_e x[r] + bias_e,   y[r] = act(z[r]) + residual[r]
  * x [T][H], w [E][N][H], bias float[E][N] (NULL: 0), residual (NULL: 0), y, z (NULL to skip) [T][N]; y is formed from z before
- * that is rounded.  Rows from offsets[E] on: zeros in y and z.  y may be residual.
+ * that is rounded.  Rows before offsets[0] and from offsets[E] on: zeros in y and z.  y may be residual.
  * act: LOCMOE_ACT_NONE, _RELU, _GELU (erf form), _SILU.
  *
  * locmoe_expert_linear_grad: from dy [T][N], the gradient of z,
@@ -634,7 +635,7 @@ int locmoe_unsort_grad(const locmoe_shape_t *shape, int32_t K, const void *dout,
  *                                          gradient goes through the activation before this product
  *   dw_e = sum_r dy[r] x[r]^T              [E][N][H] of dw_dtype (zeros for an expert without rows)
  *   db_e = sum_r dy[r]                     float[E][N]
- * dx, dw, db may be NULL; w and z are read for dx, x for dw.  Rows from offsets[E] on: zeros in dx, not in dw and db.
+ * dx, dw, db may be NULL; w and z are read for dx, x for dw.  Rows of no group: zeros in dx, no part of dw and db.
  *
  * H and N multiples of 8, below 2^20; E <= 1024, T < 2^31 - 65536 (LOCMOE_ERR_TOO_LARGE); all arrays 16-byte aligned, offsets
  * 4-byte.  Sums have a fixed order that depends on the offsets and the device: the same call gives the same bits.

@@ -603,11 +603,12 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         constexpr int kCols = BN * 4 / kEpiWarps, kBlock = 32;       // columns of one warp, of a step
         const int q = warp & 3, part0 = ((warp - 2) >> 2) * kCols;
         const int et = threadIdx.x - 64;
-        // what no tile covers: rows behind the last group, weights of experts without rows
+        // what no tile covers: rows before the first group and behind the last, weights of experts without rows
         if (KIND != kWeights) {
-            const long long kept = min(max(offsets[a.E], 0), a.R), per = a.N / 8, n = ((long long)a.R - kept) * per;
+            const int first = min(max(offsets[0], 0), a.R), kept = max(min(offsets[a.E], a.R), first);
+            const long long per = a.N / 8, before = first * per, n = before + ((long long)a.R - kept) * per;
             for (long long i = (long long)blockIdx.x * kEpiThreads + et; i < n; i += (long long)gridDim.x * kEpiThreads) {
-                const size_t o = (size_t)(kept * per + i) * 8;
+                const size_t o = (size_t)(i < before ? i : i - before + kept * per) * 8;
                 *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + o) = make_uint4(0, 0, 0, 0);
                 if (a.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint4(0, 0, 0, 0);
             }

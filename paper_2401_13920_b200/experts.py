@@ -64,6 +64,12 @@ def _slots(order: Order, T: int) -> int:
     return s[0]
 
 
+def _on_current(t, name: str) -> None:
+    """For the router's calls, whose binding does not compare devices."""
+    if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        raise ValueError("%s: on %s, which is not the current CUDA device" % (name, t.device))
+
+
 def _want_shape(t, shape: tuple, name: str) -> None:
     if t is not None and t.shape != shape:
         raise ValueError("%s: expected %s, got %s" % (name, shape, tuple(t.shape)))
@@ -195,7 +201,8 @@ def expert_linear(x, w, offsets, bias=None, act=None, residual=None, want_z=Fals
     """y = act(z) + residual, z[r] = w[e] x[r] + bias[e] for the rows [offsets[e], offsets[e + 1]) of every expert e.
 
     x [R][IN], w [E][OUT][IN], residual [R][OUT] bf16, bias [E][OUT] fp32; act one of none, relu, gelu, silu.  Returns ``(y, z)``,
-    z (bf16, for the gradient) None without ``want_z``; rows behind the last group are zero in both."""
+    z (bf16, for the gradient) None without ``want_z``; rows of no group (behind the last, or before the first where offsets is a
+    slice for a part of the experts) are zero in both."""
     if stream is not None:
         with _under(stream):
             return expert_linear(x, w, offsets, bias, act, residual, want_z)
@@ -217,8 +224,8 @@ def expert_linear_grad(dy, x, w, offsets, z=None, act=None, want_dx=True, want_d
     """Gradient of the products from dy [R][OUT], the gradient of z: ``(dx, dw, db)``, each None when not wanted.
 
     With ``z`` [R][IN], what the rows x = act(z) were made of, dx is the gradient of that z: it has gone through the activation
-    before this product.  dw [E][OUT][IN] is in ``dw_dtype`` (bf16 or fp32, by default w's), db [E][OUT] in fp32.  Rows behind
-    the last group: zeros in dx, no part of dw and db.  x may be None without ``want_dw``."""
+    before this product.  dw [E][OUT][IN] is in ``dw_dtype`` (bf16 or fp32, by default w's), db [E][OUT] in fp32.  Rows of
+    no group: zeros in dx, no part of dw and db.  x may be None without ``want_dw``."""
     if stream is not None:
         with _under(stream):
             return expert_linear_grad(dy, x, w, offsets, z, act, want_dx, want_dw, want_db, dw_dtype)
@@ -267,7 +274,9 @@ class RouteSort(torch.autograd.Function):
         T, H = _matrix(x, "x")
         if not 1 <= K <= min(8, E):
             raise ValueError("K: expected 1 to %d, got %d" % (min(8, E), K))
-        _here(x, "x")
+        _on_current(x, "x")
+        _on_current(eps, "eps")
+        _want_shape(eps, (E,), "eps")
         ctx.set_materialize_grads(False)
         idx_k, w_k, aux, f = _rows(K, T, _I32), _rows(K, T, _F32), None, None
         if T > 0:

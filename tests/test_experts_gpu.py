@@ -354,6 +354,34 @@ def test_offsets_that_make_no_sense_touch_nothing_else(X, B):
     assert B.locmoe_device_flags() == 0
 
 
+@pytest.mark.parametrize("counts,lo,hi", [([70, 3, 130, 0, 9], 1, 3), ([5, 0, 300, 20], 2, 3), ([40, 50, 60], 1, 1)])
+def test_a_part_of_the_experts(X, B, counts, lo, hi):
+    """A slice of the offsets with its experts' weights: their rows as in the whole, zeros in all others."""
+    g = gen(7)
+    offsets, R = ragged(counts, 2)
+    E, a, b = hi - lo + 1, int(offsets[lo]), int(offsets[hi + 1])
+    part = offsets[lo:hi + 2]
+    x, w, dy, bias = randn(g, R, 200, dtype=BF), randn(g, E, 264, 200, dtype=BF), randn(g, R, 264, dtype=BF), randn(g, E, 264)
+    for t in (x, dy):
+        t[:a], t[b:] = float("nan"), float("inf")
+    y, z = X.expert_linear(x, w, part, bias, "silu", want_z=True)
+    dx, dw, db = X.expert_linear_grad(dy, x, w, part, want_db=True, dw_dtype=F32)
+    own = part - a
+    y1, z1 = X.expert_linear(x[a:b].clone(), w, own, bias, "silu", want_z=True)
+    dx1, dw1, db1 = X.expert_linear_grad(dy[a:b].clone(), x[a:b].clone(), w, own, want_db=True, dw_dtype=F32)
+    # the same sums, in another order at most: (terms + 3) 2^-24 of the sum of the magnitudes for each, the slope of SiLU 1.1; and
+    # bf16's rounding of each.  A row's sum of magnitudes is below its norms' product.
+    for got, want, left, terms in ((y, y1, x, 200), (z, z1, x, 200), (dx, dx1, dy, 264)):
+        norm = left[a:b].float().norm(dim=1, keepdim=True) * w.float().norm(dim=2 if left is x else 1).max() + bias.abs().max()
+        assert ((got[a:b].float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 2 * 1.13 * (terms + 3) * 2.0 ** -24 * norm).all()
+        assert not got[:a].any() and not got[b:].any()
+    magnitudes = [(dy[s:t].float().abs(), x[s:t].float().abs()) for s, t in zip(part[:-1].tolist(), part[1:].tolist())]
+    tol = 2 * (max(counts) + 3) * 2.0 ** -24
+    assert ((dw - dw1).abs() <= tol * torch.stack([d.t() @ v for d, v in magnitudes])).all()
+    assert ((db - db1).abs() <= tol * torch.stack([d.sum(0) for d, _ in magnitudes])).all()
+    assert B.locmoe_device_flags() == 0
+
+
 def test_residual_may_be_the_output(X, B):
     g = gen(2)
     offsets, R = ragged([4, 0, 200, 3])
@@ -430,6 +458,20 @@ def test_parts_that_need_no_gradient_get_none(X):
         y = X.Unsort.apply(x, None, None, *X.RouteSort.apply(x.detach(), None, 4, 1, 0.0)[4:])
         d = torch.autograd.grad(y.float().sum(), x, create_graph=True)[0]
         torch.autograd.grad(d.float().sum(), x)
+
+
+def test_tensors_of_another_device_are_refused(X, monkeypatch):
+    g = gen(4)
+    p = layer_inputs(g, 20, 64, 72, 4, 1)
+    args = (p["x"], p["w_in"], p["w_out"], 2)
+    for bad in (dict(eps=p["eps"].cpu()), dict(eps=torch.zeros(5, device="cuda"))):
+        with pytest.raises(ValueError):
+            X.moe_layer(*args, **bad)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)            # as if the tensors were on a device that is not current
+    with pytest.raises(ValueError, match="not the current"):
+        X.moe_layer(*args)
+    with pytest.raises(ValueError, match="not the current"):
+        X.RouteSort.apply(p["x"], None, 4, 1, 0.0)
 
 
 def test_nothing_to_do(X):
