@@ -264,6 +264,23 @@ def _dense(t):
     return None if t is None else t.contiguous()
 
 
+# A leaf's gradient is added up on the stream that the node for it was made on, and the node lives as long as any graph that
+# reached it.  If that was the default stream, which no capture can take in, a captured backward pass through it spoils the
+# capture and can end the process.  So the forward passes note the stream at each node (the first one stays: later graphs
+# share the node), and a captured backward pass refuses such a node before any gradient is sent there.
+def _note_stream(ctx) -> None:
+    for node, _ in ctx.next_functions:
+        if node is not None and type(node).__name__ == "AccumulateGrad":
+            node.metadata.setdefault("locmoe_stream", B._raw_stream(torch.cuda.current_device()))
+
+
+def _check_capture(ctx) -> None:
+    if torch.cuda.is_current_stream_capturing() and any(node is not None and node.metadata.get("locmoe_stream", 1) == 0
+                                                        for node, _ in ctx.next_functions):
+        raise RuntimeError("a captured backward pass: a graph of the same leaves that was built on the default stream is still "
+                           "alive; drop its outputs first, or build it on another stream")
+
+
 class RouteSort(torch.autograd.Function):
     """``RouteSort.apply(x, eps, E, K, alpha) -> (xs, w_k, aux, idx_k, offsets, slot, inv)``: the router and the tokens in the
     order of its choices.  Differentiable in x and eps, once; aux is the load-balance loss alpha * E * sum f_i P_i (None with
@@ -277,6 +294,7 @@ class RouteSort(torch.autograd.Function):
         _on_current(x, "x")
         _on_current(eps, "eps")
         _want_shape(eps, (E,), "eps")
+        _note_stream(ctx)
         ctx.set_materialize_grads(False)
         idx_k, w_k, aux, f = _rows(K, T, _I32), _rows(K, T, _F32), None, None
         if T > 0:
@@ -301,6 +319,7 @@ class RouteSort(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dxs, dw, daux, *_):
+        _check_capture(ctx)
         x, eps, idx_k, offsets, slot, inv, f = ctx.saved_tensors
         if dxs is None and dw is None and daux is None:
             return (None,) * 5
@@ -322,6 +341,7 @@ class ExpertFFN(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, xs, w_in, w_out, b_in, b_out, offsets, act="gelu"):
+        _note_stream(ctx)
         a, z = expert_linear(xs, w_in, offsets, b_in, act, want_z=_act(act) != B.ACT_NONE)
         y, _ = expert_linear(a, w_out, offsets, b_out)
         ctx.act = act
@@ -331,6 +351,7 @@ class ExpertFFN(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
+        _check_capture(ctx)
         xs, w_in, w_out, b_in, b_out, offsets, a, z = ctx.saved_tensors
         need = ctx.needs_input_grad
         dy = dy.contiguous()
@@ -349,12 +370,14 @@ class Unsort(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, y, w_k, residual, offsets, slot, inv):
+        _note_stream(ctx)
         ctx.save_for_backward(y, w_k, offsets, slot, inv)
         return unsort_rows(y, Order(offsets, slot, inv), w_k, residual)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
+        _check_capture(ctx)
         y, w_k, offsets, slot, inv = ctx.saved_tensors
         need = ctx.needs_input_grad
         dy = dw = None
@@ -367,7 +390,10 @@ def moe_layer(x, w_in, w_out, K=1, b_in=None, b_out=None, eps=None, act="gelu", 
     """The MoE layer without a capacity: out[t] = residual[t] + sum over the K best experts of score * FFN_e(x[t]).
 
     x [T][H], w_in [E][F][H], w_out [E][H][F] bf16; b_in [E][F], b_out [E][H] and eps [E] (the router's bias) fp32, or None.
-    Returns ``(out, aux)``, aux the load-balance loss with alpha > 0, else None.  Differentiable in all tensors."""
+    Returns ``(out, aux)``, aux the load-balance loss with alpha > 0, else None.  Differentiable in all tensors.
+
+    Forward and backward can be captured into a CUDA graph; no graph of the same leaves that was built on the default stream
+    may then be alive (the backward pass refuses it)."""
     xs, w_k, aux, _, offsets, slot, inv = RouteSort.apply(x, eps, w_in.shape[0], K, alpha)
     y = ExpertFFN.apply(xs, w_in, w_out, b_in, b_out, offsets, act)
     return Unsort.apply(y, w_k, residual, offsets, slot, inv), aux

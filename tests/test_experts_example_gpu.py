@@ -1,5 +1,6 @@
 """The example's dropless training step, and a whole step captured into a graph, against autograd in 64 bits."""
 import os
+import subprocess
 import sys
 
 import pytest
@@ -103,6 +104,45 @@ def test_a_captured_training_step(X):
         (o.float().square().sum() + aux).backward()
         for a, b in zip(got, [o.detach()] + [t.grad for t in fresh]):
             assert torch.equal(a, b)
+
+
+CHILD = """
+import torch
+from paper_2401_13920_b200 import experts
+BF = torch.bfloat16
+x = torch.randn(40, 64, device="cuda").to(BF).requires_grad_()
+w_in, w_out = (torch.randn(4, *s, device="cuda").to(BF).requires_grad_() for s in ((72, 64), (64, 72)))
+leaves = (x, w_in, w_out)
+def run():
+    return experts.moe_layer(*leaves, 2, residual=x if RESIDUAL else None)[0].float().square().sum()
+s = torch.cuda.Stream()
+with torch.cuda.stream(s):
+    run().backward()
+torch.cuda.synchronize()
+for live in (True, False):
+    for t in leaves:
+        t.grad = None
+    eager = run() if live else None
+    graph = torch.cuda.CUDAGraph()
+    try:
+        with torch.cuda.graph(graph):
+            run().backward()
+        print("captured")
+        graph.replay()
+        for t, g in zip(leaves, torch.autograd.grad(run(), leaves)):
+            assert torch.equal(t.grad, g)
+    except RuntimeError as e:
+        print("refused" if "a captured backward pass" in str(e) else e)
+    torch.cuda.synchronize()
+"""
+
+
+@pytest.mark.parametrize("residual", [False, True])
+def test_a_captured_backward_pass_refuses_a_graph_on_the_default_stream(residual):
+    """In a process of its own, which has to live on and capture the step once the other graph is gone."""
+    done = subprocess.run([sys.executable, "-c", CHILD.replace("RESIDUAL", str(residual))], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+    assert done.stdout.split() == ["refused", "captured"], done.stdout
 
 
 def test_example_main_runs(X, capsys):
