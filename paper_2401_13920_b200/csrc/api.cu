@@ -606,7 +606,7 @@ int locmoe_expert_linear_bytes(const locmoe_shape_t* shape, int32_t N, int32_t g
     int rc = check_linear(shape, N);
     if (rc) return rc;
     if (!bytes) return LOCMOE_ERR_NULL;
-    *bytes = expert_linear_ws_bytes(*shape, grad);
+    *bytes = expert_linear_ws_bytes(*shape, N, grad);
     return LOCMOE_OK;
 }
 
@@ -619,7 +619,7 @@ int locmoe_expert_linear(const locmoe_shape_t* shape, int32_t N, const locmoe_ex
     for (const void* p : {l->x, l->w, (const void*)l->bias, l->residual, (const void*)l->y, (const void*)l->z})
         if (!element_aligned(p, 16)) return LOCMOE_ERR_ALIGN;
     if (!element_aligned(l->offsets, 4)) return LOCMOE_ERR_ALIGN;
-    if (!ws || ws_bytes < expert_linear_ws_bytes(*shape, 0) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;
+    if (!ws || ws_bytes < expert_linear_ws_bytes(*shape, N, 0) || (uintptr_t)ws % 256) return LOCMOE_ERR_WORKSPACE;
     return launch_expert_linear(*shape, N, *l, ws, static_cast<cudaStream_t>(stream));
 }
 
@@ -633,7 +633,7 @@ int locmoe_expert_linear_grad(const locmoe_shape_t* shape, int32_t N, const locm
     for (const void* p : {l->dy, l->x, l->w, l->z, (const void*)l->dx, (const void*)l->dw, (const void*)l->db})
         if (!element_aligned(p, 16)) return LOCMOE_ERR_ALIGN;
     if (!element_aligned(l->offsets, 4)) return LOCMOE_ERR_ALIGN;
-    if ((l->dx || l->dw) && (!ws || ws_bytes < expert_linear_ws_bytes(*shape, 1) || (uintptr_t)ws % 256)) return LOCMOE_ERR_WORKSPACE;
+    if ((l->dx || l->dw) && (!ws || ws_bytes < expert_linear_ws_bytes(*shape, N, 1) || (uintptr_t)ws % 256)) return LOCMOE_ERR_WORKSPACE;
     return launch_expert_linear_grad(*shape, N, *l, ws, static_cast<cudaStream_t>(stream));
 }
 

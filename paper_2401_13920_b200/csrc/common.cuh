@@ -146,7 +146,7 @@ int launch_unsort_grad(const locmoe_shape_t& s, int K, const void* dout, const v
 bool sort_grad_fits(const locmoe_shape_t& s);
 size_t sort_grad_ws_bytes(const locmoe_shape_t& s);
 int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g, void* ws, cudaStream_t st);
-size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad);
+size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int N, int grad);
 int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_linear_t& l, void* ws, cudaStream_t st);
 int launch_expert_linear_grad(const locmoe_shape_t& s, int N, const locmoe_expert_linear_grad_t& l, void* ws, cudaStream_t st);
 int read_linear_flags(int* out, cudaStream_t st);

@@ -4,7 +4,7 @@
 //   weights   dW_e  = dy_e^T x_e,  db_e = sum of dy_e's rows         the reduction runs over the group's rows
 // One GEMM kernel on the tensor cores (tcgen05, bf16 operands, fp32 accumulators in TMEM) serves all three: 128 x 256 output
 // tiles, operands by TMA into a ring of four stages of 64 along the reduction, two accumulators so that a tile's epilogue runs
-// beside the next tile's products.  An operand whose rows run along the reduction is K-major, else MN-major: the same TMA
+// beside the next tile's products; or tiles of 256 x 256, an accumulator for each half, where loads are the limit.  An operand whose rows run along the reduction is K-major, else MN-major: the same TMA
 // boxes of 64 elements x rows, the matrix descriptor says which way they lie, so nothing is transposed in memory.
 // Warp 0 loads, warp 1 issues the products, warps 2..9 drain the accumulators (a row a lane, half of the columns a warp).
 //
@@ -67,10 +67,11 @@ struct LinearArgs {
     const void* z_in;           // bf16 [R][N]: multiply by act'(z_in); nullptr: no factor
     float* part;                // [grid][2][part_rows][BN]
     float* db;                  // weights only: [E][M] or nullptr
-    float* db_part;             // [grid][2][BM]
+    float* db_part;             // [grid][2][unit]
     Split* split;               // [grid]
     int act, out_f32;
     int E, R, M, N, K;          // M: rows of a weight (weights only)
+    int unit;                   // rows of a tile: BM, or 2 BM with an accumulator for each half
     int n_tiles, a_rows;        // rows of one A box
     int stages;                 // of the ring
     int boxes;                  // weights: rows leave as boxes
@@ -102,12 +103,13 @@ __device__ __forceinline__ Group group_of(const int* offsets, int e, int R) {
 }
 
 // The list of work: the groups' tiles in order, a tile being `kb` blocks of the reduction.
-template <int KIND>
+template <int KIND, int HALVES>
 struct Tiles {
+    static constexpr int UNIT = HALVES * BM;
     const LinearArgs& a;
     const int* offsets;
     __device__ __forceinline__ int kblocks(const Group& g) const { return KIND == kWeights ? (g.n + BK - 1) / BK : (a.K + BK - 1) / BK; }
-    __device__ __forceinline__ int m_tiles(const Group& g) const { return KIND == kWeights ? (a.M + BM - 1) / BM : (g.n + BM - 1) / BM; }
+    __device__ __forceinline__ int m_tiles(const Group& g) const { return ((KIND == kWeights ? a.M : g.n) + UNIT - 1) / UNIT; }
     __device__ __forceinline__ int tiles(const Group& g) const { return g.n > 0 ? m_tiles(g) * a.n_tiles : 0; }
 };
 
@@ -134,9 +136,9 @@ __device__ __forceinline__ long long sum_warp(long long v) {
 // and the sums' way through memory, 0.05 us for each row of a tile (1981 rows of 304 x 1024 with every tile split 28 against
 // 19 us whole; 2 rows of 10240 x 2560, 20 tiles in all, 27 us split; weights' gradient of 10749 rows in 4 groups, 400 x 160,
 // 16 tiles, 52 us whole, 32 split).
-template <int KIND>
+template <int KIND, int HALVES>
 __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, int lane) {
-    const Tiles<KIND> t{a, offsets};
+    const Tiles<KIND, HALVES> t{a, offsets};
     long long n = 0, rows = 0, rowtiles = 0, groups = 0;
     for (int e = lane; e < a.E; e += 32) {
         const Group g = group_of(offsets, e, a.R);
@@ -169,8 +171,8 @@ __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, in
         units = (long long)rest * ((a.K + BK - 1) / BK);
     }
     rows = sum_warp(rows); rowtiles = sum_warp(rowtiles); groups = sum_warp(groups);
-    const float block = KIND == kWeights ? kWeightsBlock : fmaxf(0.27f, 0.73f * (float)groups / (float)rowtiles);
-    const float tile_rows = KIND == kWeights ? (float)BM : (float)rows / (float)rowtiles;
+    const float block = (float)HALVES * (KIND == kWeights ? kWeightsBlock : fmaxf(0.27f, 0.73f * (float)groups / (float)rowtiles));
+    const float tile_rows = KIND == kWeights ? (float)(HALVES * BM) : (float)rows / (float)rowtiles;
     if (((float)longest - (float)units / (float)a.grid) * block < kJoinUs + kRowUs * tile_rows) return d;
     const long long r = units / 4;                              // a run has at least four blocks
     d.whole = d.tiles - rest;
@@ -183,7 +185,7 @@ __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, in
 template <int KIND>
 bool may_split(const LinearArgs& a) {
     const float kb = (float)(((KIND == kWeights ? a.R : a.K) + BK - 1) / BK);
-    return KIND == kWeights ? kb * kWeightsBlock >= kJoinUs + kRowUs * BM : kb * 0.73f >= kJoinUs;
+    return KIND == kWeights ? kb * (float)(a.unit / BM) * kWeightsBlock >= kJoinUs + kRowUs * (float)a.unit : kb * (float)(a.unit / BM) * 0.73f >= kJoinUs;
 }
 
 struct Item {
@@ -193,8 +195,14 @@ struct Item {
     long long begin;            // in a run: the tile's first block among the rest's
 };
 
+// Halves of a tile that hold rows.
+template <int KIND, int HALVES>
+__device__ __forceinline__ int halves_of(const LinearArgs& a, const Item& it) {
+    return HALVES == 2 && (KIND == kWeights ? a.M : it.n) - it.mt * HALVES * BM > BM ? 2 : 1;
+}
+
 // Walks through one CTA's share: its tiles, then its run.
-template <int KIND>
+template <int KIND, int HALVES>
 struct Cursor {
     const LinearArgs& a;
     const int* offsets;
@@ -214,7 +222,7 @@ struct Cursor {
         ubase += (long long)rest() * kb;
         base += per;
         if (++e >= a.E) return false;
-        const Tiles<KIND> t{a, offsets};
+        const Tiles<KIND, HALVES> t{a, offsets};
         g = group_of(offsets, e, a.R);
         kb = t.kblocks(g);
         per = t.tiles(g);
@@ -249,7 +257,7 @@ struct Cursor {
             it.mt = in / a.n_tiles;
             it.nt = in - it.mt * a.n_tiles;
         } else {                        // tiles that share a weight tile are neighbours
-            const int mts = Tiles<KIND>{a, offsets}.m_tiles(g);
+            const int mts = Tiles<KIND, HALVES>{a, offsets}.m_tiles(g);
             it.nt = in / mts;
             it.mt = in - it.nt * mts;
         }
@@ -398,10 +406,12 @@ __device__ __forceinline__ void put_piece(unsigned char* box, int lane, int i, c
 template <int KIND>
 __device__ __forceinline__ const void* extra_array(const LinearArgs& a) { return KIND == kForward ? a.residual : KIND == kTowardsX ? a.z_in : nullptr; }
 
-template <int KIND>
+// HALVES: of a tile, 128 rows each with an accumulator.
+template <int KIND, int HALVES>
 __global__ void __launch_bounds__(KIND == kWeights ? kWeightsThreads : kThreads, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOther,
                    const LinearArgs a) {
+    constexpr int UNIT = HALVES * BM;
     constexpr bool A_MN = KIND == kWeights, B_MN = KIND != kForward;
     constexpr uint64_t kStepA = (A_MN ? 2048 : UMMA_K * 2) >> 4, kStepB = (B_MN ? 2048 : UMMA_K * 2) >> 4;   // 16 steps of the reduction
     extern __shared__ unsigned char smraw[];
@@ -439,8 +449,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    const Deal runs = deal<KIND>(a, offsets, lane);
-    Cursor<KIND> cur(a, offsets, runs, blockIdx.x);
+    const Deal runs = deal<KIND, HALVES>(a, offsets, lane);
+    Cursor<KIND, HALVES> cur(a, offsets, runs, blockIdx.x);
     Item it;
 
     if (warp == 0) {
@@ -448,10 +458,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             int stage = 0; uint32_t phase = 0;
             bool ok = true;
             while (ok && cur.next(it)) {
-                const int m0 = it.mt * BM, n0 = it.nt * BN;
+                const int m0 = it.mt * UNIT, n0 = it.nt * BN;
                 // a group's last rows come in boxes of 32: what lies behind them is another group's, and would be read for nothing
                 // (1000 rows of 1560 x 4104 over 24 experts 76 against 65 us)
-                const int few = A_MN || a.a_rows < BM || it.n - m0 > BM - 32 ? 0 : (it.n - m0 + 31) / 32;
+                const int few = A_MN || a.a_rows < BM || it.n - m0 > UNIT - 32 ? 0 : (it.n - m0 + 31) / 32;
                 const uint32_t bytes = few ? (uint32_t)few * 32 * BK * 2 + B_BYTES : STAGE_BYTES;
                 for (int kb = it.kb0; kb < it.kb1; ++kb) {
                     if (!wait_or_abort(&empty[stage], phase ^ 1u, abort_word)) { ok = false; break; }
@@ -462,7 +472,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                         tma_load_4d(sa, &tmA, 0, it.lo + kb * BK, m0 / 64, 0, &full[stage]);
                     } else if (A_MN) {
 #pragma unroll
-                        for (int c = 0; c < BM / 64; ++c) tma_load_2d(sa + c * CHUNK_BYTES, &tmA, m0 + 64 * c, it.lo + kb * BK, &full[stage]);
+                        for (int c = 0; c < UNIT / 64; ++c) tma_load_2d(sa + c * CHUNK_BYTES, &tmA, m0 + 64 * c, it.lo + kb * BK, &full[stage]);
                     } else if (few) {
                         for (int i = 0; i < few; ++i) tma_load_2d(sa + i * (32 * BK * 2), &tmOther, kb * BK, it.lo + m0 + 32 * i, &full[stage]);
                     } else {
@@ -493,9 +503,11 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         int acc = 0; uint32_t acc_phase = 0;
         bool ok = true;
         while (ok && cur.next(it)) {
+            const int halves = halves_of<KIND, HALVES>(a, it);
             if (!wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_word)) break;
+            if (halves == 2 && !wait_warp(&acc_empty[acc ^ 1], acc == 0 ? acc_phase ^ 1u : acc_phase, abort_word)) break;
             tc_fence_after();
-            const uint32_t tmem_d = tmem_base + (uint32_t)acc * BN, id = idesc(A_MN, B_MN, a.N - it.nt * BN);
+            const uint32_t id = idesc(A_MN, B_MN, a.N - it.nt * BN);
             const int left = KIND == kWeights ? it.n - (it.kb1 - 1) * BK : BK;      // rows of the group in the last block
             const int plain = it.kb1 - it.kb0 - (left < BK ? 1 : 0);                // blocks that are products and nothing else
             if (lane == 0) {
@@ -505,9 +517,11 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     tc_fence_after();
                     const uint32_t sa = smem_u32(base) + (uint32_t)s * STAGE_BYTES;
                     const uint64_t da = A_MN ? umma_desc_mn(sa) : umma_desc_sw128(sa), db = B_MN ? umma_desc_mn(sa + a_bytes) : umma_desc_sw128(sa + a_bytes);
+                    for (int h = 0; h < halves; ++h) {
 #pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k)
-                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, id, (i > 0 || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < BK / UMMA_K; ++k)
+                            umma_f16(tmem_base + (uint32_t)((acc ^ h) * BN), da + h * (A_BYTES >> 4) + k * kStepA, db + k * kStepB, id, (i > 0 || k > 0) ? 1u : 0u);
+                    }
                     umma_commit(&empty[s]);
                     if (with_db && it.nt != 0) mbar_arrive_n(&empty[s], kSumWarps);    // nobody else reads this stage
                     if (++s == NSTAGE) { s = 0; ph ^= 1u; }
@@ -524,8 +538,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 // rows [left, 16 * steps) belong to the next group: zeros.  A row is 128 bytes in each box, whatever the swizzle,
                 // which moves bytes inside a row only.
                 for (int r = left + (lane >> 3); r < steps * UMMA_K; r += 4) {
-#pragma unroll
-                    for (int c = 0; c < (BM + BN) / 64; ++c)
+                    for (int c = 0; c < (int)(STAGE_BYTES / CHUNK_BYTES); ++c)
                         *reinterpret_cast<uint4*>(pa + c * CHUNK_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async_smem();
@@ -533,17 +546,20 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (lane == 0) {
                     tc_fence_after();
                     const uint64_t da = umma_desc_mn(smem_u32(pa)), db = umma_desc_mn(smem_u32(pa) + a_bytes);
-                    for (int k = 0; k < steps; ++k)
-                        umma_f16(tmem_d, da + k * kStepA, db + k * kStepB, id, (plain > 0 || k > 0) ? 1u : 0u);
+                    for (int h = 0; h < halves; ++h)
+                        for (int k = 0; k < steps; ++k)
+                            umma_f16(tmem_base + (uint32_t)((acc ^ h) * BN), da + h * (A_BYTES >> 4) + k * kStepA, db + k * kStepB, id, (plain > 0 || k > 0) ? 1u : 0u);
                     umma_commit(&empty[stage]);
                     if (with_db && it.nt != 0) mbar_arrive_n(&empty[stage], kSumWarps);
                 }
                 __syncwarp();
                 if (++stage == NSTAGE) { stage = 0; phase ^= 1u; }
             }
-            if (lane == 0) umma_commit(&acc_full[acc]);
+            for (int h = 0; h < halves; ++h) {
+                if (lane == 0) umma_commit(&acc_full[acc]);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
             __syncwarp();
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
     } else if (KIND == kWeights && warp >= 2 + kEpiWarps) {
         // ---- column sums of dy, from the A tiles of the first column of output tiles: a warp 32 columns, a lane 8 of them in
@@ -557,18 +573,23 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             bool ok = true;
             while (ok && cur.next(it)) {
                 const int n = it.kb1 - it.kb0;
+                const int halves = halves_of<KIND, HALVES>(a, it);
                 if (it.nt == 0) {
-                    float2 v[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+                    float2 v[HALVES][4] = {};
                     for (int kb = it.kb0; kb < it.kb1; ++kb) {
                         if (!wait_warp(&full[stage], phase, abort_word)) { ok = false; break; }
                         const unsigned char* p = base + (size_t)stage * STAGE_BYTES + at;
                         const int left = it.n - kb * BK;
 #pragma unroll
-                        for (int i = 0; i < BK / 8; ++i) {
-                            if (r0 + 8 * i >= left) break;
-                            const uint4 q = *reinterpret_cast<const uint4*>(p + i * 1024);
-                            v[0] = __fadd2_rn(v[0], unpack2(q.x)); v[1] = __fadd2_rn(v[1], unpack2(q.y));
-                            v[2] = __fadd2_rn(v[2], unpack2(q.z)); v[3] = __fadd2_rn(v[3], unpack2(q.w));
+                        for (int h = 0; h < HALVES; ++h) {
+                            if (h == halves) break;
+#pragma unroll
+                            for (int i = 0; i < BK / 8; ++i) {
+                                if (r0 + 8 * i >= left) break;
+                                const uint4 q = *reinterpret_cast<const uint4*>(p + h * A_BYTES + i * 1024);
+                                v[h][0] = __fadd2_rn(v[h][0], unpack2(q.x)); v[h][1] = __fadd2_rn(v[h][1], unpack2(q.y));
+                                v[h][2] = __fadd2_rn(v[h][2], unpack2(q.z)); v[h][3] = __fadd2_rn(v[h][3], unpack2(q.w));
+                            }
                         }
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&empty[stage]);
@@ -576,27 +597,32 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     }
                     if (!ok) break;
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) {
+                    for (int h = 0; h < HALVES; ++h) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, d);
-                            v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, d);
+                        for (int d = 4; d < 32; d <<= 1) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                v[h][i].x += __shfl_xor_sync(0xffffffffu, v[h][i].x, d);
+                                v[h][i].y += __shfl_xor_sync(0xffffffffu, v[h][i].y, d);
+                            }
                         }
-                    }
-                    const int col = it.mt * BM + o * 8;
-                    float* out = n == it.kb ? (col < a.M ? a.db + (size_t)it.e * a.M + col : nullptr)
-                                            : a.db_part + ((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * BM + o * 8;
-                    if (lane < 4 && out) {
-                        reinterpret_cast<float4*>(out)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-                        reinterpret_cast<float4*>(out)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+                        const int in = h * BM + o * 8, col = it.mt * UNIT + in;
+                        float* out = n == it.kb ? (col < a.M ? a.db + (size_t)it.e * a.M + col : nullptr)
+                                                : a.db_part + ((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * UNIT + in;
+                        if (lane < 4 && h < halves && out) {
+                            reinterpret_cast<float4*>(out)[0] = make_float4(v[h][0].x, v[h][0].y, v[h][1].x, v[h][1].y);
+                            reinterpret_cast<float4*>(out)[1] = make_float4(v[h][2].x, v[h][2].y, v[h][3].x, v[h][3].y);
+                        }
                     }
                 } else {
                     phase ^= (uint32_t)((stage + n) / NSTAGE) & 1u;
                     stage = (stage + n) % NSTAGE;
                 }
-                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
-                if (lane == 0) mbar_arrive(&acc_empty[acc]);
-                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                for (int h = 0; ok && h < halves; ++h) {
+                    ok = wait_warp(&acc_full[acc], acc_phase, abort_word);
+                    if (ok && lane == 0) mbar_arrive(&acc_empty[acc]);
+                    if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                }
             }
         }
     } else {  // ---- epilogue: TMEM lane quadrant = warp % 4, the columns dealt to the warps of a quadrant ----
@@ -632,129 +658,134 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         unsigned char* boxes = base + (size_t)kBoxStages * (A_BYTES + B_BYTES) + (size_t)(warp - 2) * 2 * kBoxBytes;
         int turn = 0;
         int acc = 0; uint32_t acc_phase = 0;
-        while (cur.next(it)) {
+        bool ok = true;
+        while (ok && cur.next(it)) {
             if (it.kb0 == 0 && it.kb1 < it.kb && et == 0) {
                 int last = blockIdx.x + 1;
                 while (last + 1 < runs.runs && runs.begin(last + 1) < it.begin + it.kb) ++last;
-                Split split{it.e, it.mt * BM + (KIND == kWeights ? 0 : it.lo), min(BM, (KIND == kWeights ? a.M : it.n) - it.mt * BM), it.nt, last};
+                Split split{it.e, it.mt * UNIT + (KIND == kWeights ? 0 : it.lo), min(UNIT, (KIND == kWeights ? a.M : it.n) - it.mt * UNIT), it.nt, last};
                 a.split[blockIdx.x] = split;
             }
             __syncwarp();
-            const int m0 = it.mt * BM + q * 32, n0 = it.nt * BN + part0;      // the warp's first row and column
-            const int all = KIND == kWeights ? a.M : it.n;
-            const bool row_ok = m0 + lane < all, whole = it.kb1 - it.kb0 == it.kb;
-            const size_t o0 = ((size_t)(KIND == kWeights ? 0 : it.lo) + m0 + lane) * a.N + n0;      // rows' outputs only
-            float* part = whole ? nullptr : a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + q * 32 + lane) * BN + part0;
-            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part0);
-            if constexpr (KIND == kWeights) {
-                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
-                tc_fence_after();
-                const int step = a.out_f32 ? 32 : 64;       // columns of a box
+            const int halves = halves_of<KIND, HALVES>(a, it);
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += step) {
-                    if (m0 >= all || n0 + c >= a.N) break;                  // all lanes alike
-                    unsigned char* box = boxes + turn * kBoxBytes;
-                    if (whole && a.boxes) {
-                        if (lane == 0) bulk_wait_read<1>();                 // the box before the last one has left
+            for (int h = 0; h < halves; ++h) {
+                const int m0 = it.mt * UNIT + h * BM + q * 32, n0 = it.nt * BN + part0;      // the warp's first row and column
+                const int all = KIND == kWeights ? a.M : it.n;
+                const bool row_ok = m0 + lane < all, whole = it.kb1 - it.kb0 == it.kb;
+                const size_t o0 = ((size_t)(KIND == kWeights ? 0 : it.lo) + m0 + lane) * a.N + n0;      // rows' outputs only
+                float* part = whole ? nullptr : a.part + (((size_t)blockIdx.x * 2 + (it.kb0 == 0 ? 1 : 0)) * a.part_rows + h * BM + q * 32 + lane) * BN + part0;
+                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part0);
+                if constexpr (KIND == kWeights) {
+                    if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) { ok = false; break; }
+                    tc_fence_after();
+                    const int step = a.out_f32 ? 32 : 64;       // columns of a box
+#pragma unroll 1
+                    for (int c = 0; c < kCols; c += step) {
+                        if (m0 >= all || n0 + c >= a.N) break;                  // all lanes alike
+                        unsigned char* box = boxes + turn * kBoxBytes;
+                        if (whole && a.boxes) {
+                            if (lane == 0) bulk_wait_read<1>();                 // the box before the last one has left
+                            __syncwarp();
+                        }
+#pragma unroll 1
+                        for (int d = 0; d < step; d += 32) {
+                            uint32_t r[32];
+                            tmem_ld32(taddr + c + d, r);
+                            if (!whole) {
+                                if (row_ok) {
+#pragma unroll
+                                    for (int i = 0; i < 32; i += 8) st_global_v8(part + c + d + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                                }
+                                __syncwarp();
+                            } else if (!a.boxes) {
+                                if (row_ok) store_weights32(a, ((size_t)it.e * a.M + m0 + lane) * a.N + n0 + c + d, a.N - n0 - c - d, r, wide);
+                                __syncwarp();
+                            } else if (a.out_f32) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) put_piece(box, lane, i, make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    uint32_t p[4];
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) p[k] = cvt_bf16x2(make_float2(__uint_as_float(r[8 * i + 2 * k]), __uint_as_float(r[8 * i + 2 * k + 1])));
+                                    put_piece(box, lane, d / 8 + i, make_uint4(p[0], p[1], p[2], p[3]));
+                                }
+                            }
+                        }
+                        if (whole && a.boxes) {
+                            fence_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {                    // what lies beyond the weights' rows and columns is left out
+                                tma_store_3d(&tmOther, box, n0 + c, m0, it.e);
+                                bulk_commit();
+                            }
+                            turn ^= 1;
+                        }
+                    }
+                } else {
+                    // the bias and the array read along come ahead: the former through shared memory, the latter a block ahead, the
+                    // first block's before the sums are there (1000 rows of 1560 x 4104 with both: loads one after the other were
+                    // 9 us a tile)
+                    if (KIND == kForward && a.bias && whole) {
+                        if (4 * lane < kCols && n0 + 4 * lane < a.N)
+                            *reinterpret_cast<float4*>(bias + 4 * lane) = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)it.e * a.N + n0) + lane);
                         __syncwarp();
                     }
+                    uint32_t next[kBlock / 2];
+                    auto fetch = [&](int c) {
+                        if (!row_ok || !whole || !with) return;
+#pragma unroll
+                        for (int i = 0; i < kBlock; i += 16) {
+                            if (n0 + c + i + 16 <= a.N) ld_row<16>(with, o0 + c + i, next + i / 2, wide);
+                            else if (n0 + c + i < a.N) ld_row<8>(with, o0 + c + i, next + i / 2, false);
+                        }
+                    };
+                    fetch(0);
+                    if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) { ok = false; break; }
+                    tc_fence_after();
 #pragma unroll 1
-                    for (int h = 0; h < step; h += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(taddr + c + h, r);
+                    for (int c = 0; c < kCols; c += kBlock) {
+                        uint32_t extra[kBlock / 2];
+#pragma unroll
+                        for (int i = 0; i < kBlock / 2; ++i) extra[i] = next[i];
+                        if (c + kBlock < kCols) fetch(c + kBlock);
+                        __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
+                        uint32_t r[kBlock];
+                        tmem_ld(taddr + c, r);
+                        if (!row_ok || n0 + c >= a.N) continue;
                         if (!whole) {
-                            if (row_ok) {
 #pragma unroll
-                                for (int i = 0; i < 32; i += 8) st_global_v8(part + c + h + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                            for (int i = 0; i < kBlock; i += 8) st_global_v8(part + c + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
+                            continue;
+                        }
+#pragma unroll
+                        for (int i = 0; i < kBlock; i += 16) {
+                            float4 b[4];
+                            if (KIND == kForward && a.bias) {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) b[k] = reinterpret_cast<const float4*>(bias + c + i)[k];
                             }
-                            __syncwarp();
-                        } else if (!a.boxes) {
-                            if (row_ok) store_weights32(a, ((size_t)it.e * a.M + m0 + lane) * a.N + n0 + c + h, a.N - n0 - c - h, r, wide);
-                            __syncwarp();
-                        } else if (a.out_f32) {
+                            if (n0 + c + i + 16 <= a.N) {
+                                float2 v[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) put_piece(box, lane, i, make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]));
-                        } else {
+                                for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                                finish<KIND, 16>(a, o0 + c + i, v, b, extra + i / 2, wide);
+                            } else if (n0 + c + i < a.N) {      // the row's last eight
+                                float2 v[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t p[4];
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) p[k] = cvt_bf16x2(make_float2(__uint_as_float(r[8 * i + 2 * k]), __uint_as_float(r[8 * i + 2 * k + 1])));
-                                put_piece(box, lane, h / 8 + i, make_uint4(p[0], p[1], p[2], p[3]));
+                                for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
+                                finish<KIND, 8>(a, o0 + c + i, v, b, extra + i / 2, false);
                             }
                         }
                     }
-                    if (whole && a.boxes) {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {                    // what lies beyond the weights' rows and columns is left out
-                            tma_store_3d(&tmOther, box, n0 + c, m0, it.e);
-                            bulk_commit();
-                        }
-                        turn ^= 1;
-                    }
                 }
-            } else {
-                // the bias and the array read along come ahead: the former through shared memory, the latter a block ahead, the
-                // first block's before the sums are there (1000 rows of 1560 x 4104 with both: loads one after the other were
-                // 9 us a tile)
-                if (KIND == kForward && a.bias && whole) {
-                    if (4 * lane < kCols && n0 + 4 * lane < a.N)
-                        *reinterpret_cast<float4*>(bias + 4 * lane) = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)it.e * a.N + n0) + lane);
-                    __syncwarp();
-                }
-                uint32_t next[kBlock / 2];
-                auto fetch = [&](int c) {
-                    if (!row_ok || !whole || !with) return;
-#pragma unroll
-                    for (int i = 0; i < kBlock; i += 16) {
-                        if (n0 + c + i + 16 <= a.N) ld_row<16>(with, o0 + c + i, next + i / 2, wide);
-                        else if (n0 + c + i < a.N) ld_row<8>(with, o0 + c + i, next + i / 2, false);
-                    }
-                };
-                fetch(0);
-                if (!wait_warp(&acc_full[acc], acc_phase, abort_word)) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < kCols; c += kBlock) {
-                    uint32_t extra[kBlock / 2];
-#pragma unroll
-                    for (int i = 0; i < kBlock / 2; ++i) extra[i] = next[i];
-                    if (c + kBlock < kCols) fetch(c + kBlock);
-                    __syncwarp();  // tcgen05.ld is warp-collective: reconverge after the masked stores
-                    uint32_t r[kBlock];
-                    tmem_ld(taddr + c, r);
-                    if (!row_ok || n0 + c >= a.N) continue;
-                    if (!whole) {
-#pragma unroll
-                        for (int i = 0; i < kBlock; i += 8) st_global_v8(part + c + i, r[i], r[i + 1], r[i + 2], r[i + 3], r[i + 4], r[i + 5], r[i + 6], r[i + 7]);
-                        continue;
-                    }
-#pragma unroll
-                    for (int i = 0; i < kBlock; i += 16) {
-                        float4 b[4];
-                        if (KIND == kForward && a.bias) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) b[k] = reinterpret_cast<const float4*>(bias + c + i)[k];
-                        }
-                        if (n0 + c + i + 16 <= a.N) {
-                            float2 v[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                            finish<KIND, 16>(a, o0 + c + i, v, b, extra + i / 2, wide);
-                        } else if (n0 + c + i < a.N) {      // the row's last eight
-                            float2 v[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(r[i + 2 * k]), __uint_as_float(r[i + 2 * k + 1]));
-                            finish<KIND, 8>(a, o0 + c + i, v, b, extra + i / 2, false);
-                        }
-                    }
-                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty[acc]);
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
         if (KIND == kWeights && lane == 0) bulk_wait_all<0>();      // the last boxes are where they belong
     }
@@ -772,7 +803,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // x's split tile, every gridDim.y-th piece.  What tile that is the GEMM has written down; finding it anew cost every warp
 // here a few thousand cycles (200 rows of 1600 x 4096, 23 experts: 15 against 4 us).
 constexpr int kJoinThreads = 256, kJoinParts = 8;
-static_assert(kJoinThreads >= BM, "a thread for each row of a tile");
+static_assert(kJoinThreads >= 2 * BM, "a thread for each row of a tile");
 template <int KIND>
 __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearArgs a) {
     pdl_wait();
@@ -786,8 +817,8 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
     const int cols = min(BN, a.N - n0) / 8;
     if (KIND == kWeights && a.db && n0 == 0 && blockIdx.y == 0 && (int)threadIdx.x < rows) {
         const int i = threadIdx.x;
-        float sum = __ldcg(a.db_part + ((size_t)c0 * 2 + 1) * BM + i);
-        for (int c = c0 + 1; c <= last; ++c) sum += __ldcg(a.db_part + (size_t)c * 2 * BM + i);
+        float sum = __ldcg(a.db_part + ((size_t)c0 * 2 + 1) * a.unit + i);
+        for (int c = c0 + 1; c <= last; ++c) sum += __ldcg(a.db_part + (size_t)c * 2 * a.unit + i);
         a.db[row0 + i] = sum;
     }
     const size_t step = (size_t)2 * a.part_rows * BN;               // from a run's sums to the next one's
@@ -865,6 +896,24 @@ __global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const in
 // reductions need (65536 rows of 10240 x 2560: 64 % of the tensor cores' cycles with three stages, 80 % with four).
 constexpr int kBoxRows = 512;
 
+// Rows of a tile.  256 rows share each weight tile's load: 32 instead of 48 KB for 128 x 256 x 64 products come through the SM's
+// port to the L2, which has 64 bytes a cycle: 0.40 us for 48 KB where the products take 0.27, and 0.65 us where rows do not
+// begin on sectors of 32 bytes.  But both accumulators belong to one tile then, and its epilogue stands alone.  That pays
+// where rows are off the sectors, groups and reductions are long and the tiles last for some waves (18083 rows in 16 experts,
+// 3544 x 3520: 535 against 456 us forward, 493 against 436 towards x, 575 against 448 for the weights, whose tiles are
+// split more dearly: 12332 rows in 8 experts, 2528 x 1784, 3.8 waves, 123 against 166); with whole sectors only for weights'
+// gradients of very many tiles (65536 rows in 32 experts, 2560 x 10240: 3225 against 2957 us; 20893 rows in 8, 2944 x 4672,
+// 12 waves: 495 against 549), and not for products with few rows or an epilogue that costs more (65536 rows forward with
+// GeLU and z: 3137 against 3696).
+constexpr int kTallRows = 1024, kTallK = 1536;
+int rows_of_tile(Kind kind, long long R, int E, int M, int N, int K) {
+    const long long tiles = (kind == kWeights ? (long long)E * ((M + 2 * BM - 1) / (2 * BM)) : R / (2 * BM)) * ((N + BN - 1) / BN);
+    const bool off = kind == kWeights ? (M | N) % 16 != 0 : K % 16 != 0 || (kind == kTowardsX && N % 16 != 0);
+    const bool tall = R >= (long long)kTallRows * E && (kind == kWeights ? tiles >= (off ? 8ll : 32ll) * sm_count()
+                                                                         : off && K >= kTallK && tiles >= 3ll * sm_count());
+    return tall ? 2 * BM : BM;
+}
+
 template <int KIND>
 int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cudaStream_t st) {
     LinearArgs a = a0;
@@ -872,14 +921,15 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     a.n_tiles = (a.N + BN - 1) / BN;
     a.grid = sm_count();
     a.part = static_cast<float*>(ws);
-    a.part_rows = KIND == kWeights ? BM : min(a.R, BM);
+    a.unit = rows_of_tile((Kind)KIND, a.R, a.E, a.M, a.N, a.K);
+    a.part_rows = KIND == kWeights ? a.unit : min(a.R, a.unit);
     a.db_part = a.part + (size_t)a.grid * 2 * a.part_rows * BN;
-    a.a_rows = BM;
+    a.a_rows = a.unit;
     a.b_chunks = KIND != kForward && a.N % 64 == 0;
     if (KIND == kWeights) {         // dy [R][M], x [R][N]
         const uint64_t da[2] = {(uint64_t)a.M, (uint64_t)a.R}, db[2] = {(uint64_t)a.N, (uint64_t)a.R};
         a.a_chunks = a.M % 64 == 0;
-        if (!(a.a_chunks ? make_map_chunks(&tmA, A, a.M, a.R, 1, BK, BM / 64) : make_map(&tmA, A, 2, da, BK))) return LOCMOE_ERR_CUDA;
+        if (!(a.a_chunks ? make_map_chunks(&tmA, A, a.M, a.R, 1, BK, a.unit / 64) : make_map(&tmA, A, 2, da, BK))) return LOCMOE_ERR_CUDA;
         if (!(a.b_chunks ? make_map_chunks(&tmB, B, a.N, a.R, 1, BK, BN / 64) : make_map(&tmB, B, 2, db, BK))) return LOCMOE_ERR_CUDA;
     } else {
         while (a.a_rows > 16 && a.a_rows / 2 >= a.R) a.a_rows /= 2;     // few rows: smaller boxes, the tile's other rows hold what they held
@@ -891,22 +941,24 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
     // the weights' gradient on its way out, or A in boxes of 32 rows
     const uint64_t dims[2] = {(uint64_t)a.K, (uint64_t)a.R};
     if (!(KIND == kWeights ? make_store_map(&tmOther, a.out, a.out_f32, a.N, a.M, a.E) : make_map(&tmOther, A, 2, dims, 32))) return LOCMOE_ERR_CUDA;
-    a.boxes = KIND == kWeights && (long long)a.R < (long long)kBoxRows * a.E;
-    a.stages = a.boxes ? kBoxStages : KIND == kWeights ? 4 : (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
+    a.boxes = KIND == kWeights && a.unit == BM && (long long)a.R < (long long)kBoxRows * a.E;
+    a.stages = a.boxes ? kBoxStages : (int)(kRing / ((size_t)a.a_rows * BK * 2 + B_BYTES));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    static bool attr_done_dev[64] = {false};   // the attribute is per device
+    auto* kernel = a.unit > BM ? expert_gemm_kernel<KIND, 2> : expert_gemm_kernel<KIND, 1>;
+    static bool attr_done_dev[2][64] = {};     // the attribute is per device
     int dev = 0;
     cudaGetDevice(&dev);
-    if (!attr_done_dev[dev & 63]) {
-        if (cudaFuncSetAttribute(expert_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) {
+    bool& attr_done = attr_done_dev[a.unit > BM][dev & 63];
+    if (!attr_done) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) {
             cudaGetLastError();
             return LOCMOE_ERR_CUDA;
         }
-        attr_done_dev[dev & 63] = true;
+        attr_done = true;
     }
     const bool join = may_split<KIND>(a);
-    a.split = join ? reinterpret_cast<Split*>(a.db_part + (KIND == kWeights ? (size_t)a.grid * 2 * BM : 0)) : nullptr;
-    int rc = launch_pdl(expert_gemm_kernel<KIND>, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, tmOther, a);
+    a.split = join ? reinterpret_cast<Split*>(a.db_part + (KIND == kWeights ? (size_t)a.grid * 2 * a.unit : 0)) : nullptr;
+    int rc = launch_pdl(kernel, dim3(a.grid), dim3(KIND == kWeights && a.db ? kWeightsThreads : kThreads), kSmem, st, tmA, tmB, tmOther, a);
     if (rc) return rc;
     if (join) {
         const int parts = (a.part_rows * (BN / 8) + kJoinThreads - 1) / kJoinThreads;
@@ -918,8 +970,9 @@ int launch_gemm(const LinearArgs& a0, const void* A, const void* B, void* ws, cu
 }  // namespace
 
 // Two tiles' sums a CTA, and what its split tile is.
-size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int grad) {
-    const size_t rows = grad || s.T > BM ? BM : s.T, sums = rows * BN + (grad ? BM : 0);
+size_t expert_linear_ws_bytes(const locmoe_shape_t& s, int N, int grad) {
+    const int unit = grad ? max(rows_of_tile(kTowardsX, s.T, s.E, 0, s.H, N), rows_of_tile(kWeights, s.T, s.E, N, s.H, 0)) : rows_of_tile(kForward, s.T, s.E, 0, N, s.H);
+    const size_t rows = grad || s.T > unit ? unit : s.T, sums = rows * BN + (grad ? unit : 0);
     return ((size_t)sm_count() * (2 * sums * sizeof(float) + sizeof(Split)) + 255) & ~(size_t)255;
 }
 

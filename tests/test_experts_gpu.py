@@ -341,6 +341,36 @@ def test_long_groups_and_every_way_of_dealing_the_work(X, B):
     assert B.locmoe_device_flags() == 0
 
 
+@pytest.mark.parametrize("counts,lost,IN,OUT", [([2300], 0, 9208, 8200), ([4000, 129, 0, 1, 9000, 257, 5300], 11, 1544, 6600), ([9000, 0, 11001], 300, 1544, 2856)])
+def test_many_tiles_of_long_groups(X, B, counts, lost, IN, OUT):
+    """Sizes at which a tile has two accumulators: groups that end in either half, the same sums again, a bias's gradient of both."""
+    offsets, R = ragged(counts, lost)
+    E, g, o = len(counts), gen(R), offsets.tolist()
+    x, w, dy = randn(g, R, IN, dtype=BF), randn(g, E, OUT, IN, dtype=BF, std=IN ** -0.5), randn(g, R, OUT, dtype=BF)
+    bias, zin = randn(g, E, OUT), randn(g, R, IN, dtype=BF)
+    for t in (x, dy, zin):
+        t[o[-1]:] = float("nan")
+    y, z = X.expert_linear(x, w, offsets, bias, "relu", want_z=True)
+    dx, dw, db = X.expert_linear_grad(dy, x, w, offsets, zin, "relu", want_db=True)
+    again = X.expert_linear_grad(dy, x, w, offsets, zin, "relu", want_db=True)
+    assert all(torch.equal(a, b) for a, b in zip((y, z, dx, dw, db), (*X.expert_linear(x, w, offsets, bias, "relu", want_z=True), *again)))
+    for t in (y, z, dx):
+        assert not t[o[-1]:].any()
+    for e in range(E):
+        s = slice(o[e], o[e + 1])
+        xe, we, de = x[s].double(), w[e].double(), dy[s].double()
+        v = xe @ we.t() + bias[e].double()
+        f = (zin[s] > 0).double()
+        vsize = xe.abs() @ we.abs().t() + bias[e].double().abs()
+        for got, want, size, n, half in ((z[s], v, vsize, IN, 2.0 ** -8), (y[s], v.clamp_min(0), vsize, IN, 2.0 ** -8),
+                                         (dx[s], de @ we * f, de.abs() @ we.abs(), OUT, 2.0 ** -8),
+                                         (dw[e], de.t() @ xe, de.abs().t() @ xe.abs(), counts[e], 2.0 ** -8),
+                                         (db[e], de.sum(0), de.abs().sum(0), counts[e], 2.0 ** -24)):
+            assert ((got.double() - want).abs() <= half * want.abs() + (n + 3) * 2.0 ** -24 * (1 + half) * size).all()
+        del xe, we, de, v, f, vsize, got, want, size
+    assert B.locmoe_device_flags() == 0
+
+
 def test_offsets_that_make_no_sense_touch_nothing_else(X, B):
     """Offsets that descend or leave the rows: unspecified rows, and no access beyond the arrays."""
     g = gen(1)
