@@ -384,6 +384,18 @@ def test_offsets_that_make_no_sense_touch_nothing_else(X, B):
     assert B.locmoe_device_flags() == 0
 
 
+@pytest.mark.parametrize("counts,lost", GROUPS + [([3000, 0, 1, 700], 9)])
+@pytest.mark.parametrize("OUT", [8, 72, 520])
+def test_the_gradient_of_the_bias_alone(X, counts, lost, OUT):
+    offsets, R = ragged(counts, lost)
+    dy, w = randn(gen(OUT), R, OUT, dtype=BF), torch.zeros(len(counts), OUT, 8, dtype=BF, device="cuda")
+    dy[int(offsets[-1]):] = float("nan")
+    dx, dw, db = X.expert_linear_grad(dy, None, w, offsets, want_dx=False, want_dw=False, want_db=True)
+    assert dx is None and dw is None
+    for e, d in enumerate(dy[:int(offsets[-1])].double().split(counts)):
+        assert ((db[e].double() - d.sum(0)).abs() <= counts[e] * 2.0 ** -24 * d.abs().sum(0)).all()
+
+
 @pytest.mark.parametrize("counts,lo,hi", [([70, 3, 130, 0, 9], 1, 3), ([5, 0, 300, 20], 2, 3), ([40, 50, 60], 1, 1)])
 def test_a_part_of_the_experts(X, B, counts, lo, hi):
     """A slice of the offsets with its experts' weights: their rows as in the whole, zeros in all others."""
