@@ -856,6 +856,120 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
     }
 }
 
+// Forward for a few rows, single tokens' most of all: nothing but the weights to read, and no tile to fill.  A task is four columns of
+// an expert with rows; its CTA's threads share the reduction, 16 bytes of each of the four weight rows at a time, twice in
+// flight, and two rows of x share them.  The sums of the lanes, then of the warps, in a fixed order.  Weights in a ring in
+// shared memory, asynchronously and on into the next task's, were slower (two rows, 2560 x 10240: 26 against 23 us).
+constexpr int kFewRows = 8, kFewThreads = 256, kFewWarps = 24;      // kFewWarps: of an SM
+constexpr int kFewCols = 4, kFewShare = 2;                          // columns and rows of a task
+// Four rows (of one expert 20 us either way at 2560 x 10240, of four 41 against 35, two of two 26 against 20, one 19 against 12;
+// 16 experts of 3936 x 288 12 against 5), eight where the weights are so small that the tiles' fixed times count (64 of
+// 1024 x 1024, eight rows of as many 12 against 6 us, of one expert 9 against 10; 2560 x 10240 20 against 49).
+constexpr int kFewWeight = 1 << 21;
+template <int ROWS>
+__device__ __forceinline__ void few_sums(int K, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w, float* sums) {
+    constexpr int DEPTH = ROWS == 1 ? 2 : 1;                        // registers for kFewWarps
+    float2 v[ROWS][kFewCols] = {};
+    const int step = blockDim.x * 8;
+#pragma unroll 1
+    for (int k = threadIdx.x * 8; k < K; k += DEPTH * step) {
+        uint4 q[DEPTH][kFewCols];
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+#pragma unroll
+            for (int c = 0; c < kFewCols; ++c)
+                if (i == 0 || k + step < K) q[i][c] = ld_stream(reinterpret_cast<const uint4*>(w + (size_t)c * K + k + i * step));
+        }
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            if (i == 1 && k + step >= K) break;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const uint4 p = __ldg(reinterpret_cast<const uint4*>(x + (size_t)r * K + k + i * step));
+                const float2 x0 = unpack2(p.x), x1 = unpack2(p.y), x2 = unpack2(p.z), x3 = unpack2(p.w);
+#pragma unroll
+                for (int c = 0; c < kFewCols; ++c) {
+                    v[r][c] = __ffma2_rn(unpack2(q[i][c].x), x0, v[r][c]);
+                    v[r][c] = __ffma2_rn(unpack2(q[i][c].y), x1, v[r][c]);
+                    v[r][c] = __ffma2_rn(unpack2(q[i][c].z), x2, v[r][c]);
+                    v[r][c] = __ffma2_rn(unpack2(q[i][c].w), x3, v[r][c]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int c = 0; c < kFewCols; ++c) {
+            float f = v[r][c].x + v[r][c].y;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) f += __shfl_xor_sync(0xffffffffu, f, d);
+            if ((threadIdx.x & 31) == 0) sums[((threadIdx.x >> 5) * kFewShare + r) * kFewCols + c] = f;
+        }
+    }
+}
+__global__ void __launch_bounds__(kFewThreads, kFewWarps * 32 / kFewThreads) expert_few_kernel(const LinearArgs a, const uint16_t* __restrict__ x,
+                                                                                              const uint16_t* __restrict__ w) {
+    __shared__ __align__(16) float sums[2][kFewThreads / 32 * kFewShare * kFewCols];
+    __shared__ int busy[kFewRows][3], n_busy;       // experts with rows: expert, first row, rows
+    pdl_wait();
+    pdl_trigger();
+    if (threadIdx.x < 32) {
+        int n = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 32) {
+            const int e = e0 + (int)threadIdx.x;
+            const Group g = e < a.E ? group_of(a.offsets, e, a.R) : Group{0, 0};
+            const unsigned has = __ballot_sync(0xffffffffu, g.n > 0);
+            const int at = n + __popc(has & ((1u << threadIdx.x) - 1u));
+            if (g.n > 0 && at < kFewRows) { busy[at][0] = e; busy[at][1] = g.lo; busy[at][2] = g.n; }
+            n += __popc(has);
+        }
+        if (threadIdx.x == 0) n_busy = min(n, kFewRows);       // more only where the offsets descend
+    }
+    const int first = min(max(__ldg(a.offsets), 0), a.R), kept = max(min(__ldg(a.offsets + a.E), a.R), first);
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.R * (a.N / 8); i += gridDim.x * blockDim.x) {
+        const int r = i / (a.N / 8);
+        if (r >= first && r < kept) continue;
+        reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
+        if (a.z_out) reinterpret_cast<uint4*>(a.z_out)[i] = make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    const int per = a.N / kFewCols;
+    int turn = 0;
+    for (int t = blockIdx.x; t < n_busy * per; t += gridDim.x) {
+        const int g = t / per, n0 = (t - g * per) * kFewCols, e = busy[g][0];
+        for (int r0 = 0; r0 < busy[g][2]; r0 += kFewShare, turn ^= 1) {
+            const int rows = min(kFewShare, busy[g][2] - r0), row = busy[g][1] + r0;
+            const uint16_t* xr = x + (size_t)row * a.K;
+            const uint16_t* wr = w + ((size_t)e * a.N + n0) * a.K;
+            if (rows == 1) few_sums<1>(a.K, xr, wr, sums[turn]);
+            else few_sums<2>(a.K, xr, wr, sums[turn]);
+            __syncthreads();        // the other half of sums is written next
+            if ((int)threadIdx.x < rows) {
+                const size_t o = (size_t)(row + threadIdx.x) * a.N + n0;
+                float2 v[2] = {};
+                for (int i = 0; i < (int)blockDim.x / 32; ++i) {
+                    const float4 f = *reinterpret_cast<const float4*>(&sums[turn][(i * kFewShare + threadIdx.x) * kFewCols]);
+                    v[0] = __fadd2_rn(v[0], make_float2(f.x, f.y));
+                    v[1] = __fadd2_rn(v[1], make_float2(f.z, f.w));
+                }
+                if (a.bias) {
+                    const float4 b = __ldg(reinterpret_cast<const float4*>(a.bias + (size_t)e * a.N + n0));
+                    add_bias<4>(v, &b);
+                }
+                if (a.z_out) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.z_out) + o) = make_uint2(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]));
+                uint32_t extra[2];
+                if (a.residual) {
+                    const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.residual) + o);
+                    extra[0] = h.x; extra[1] = h.y;
+                }
+                arithmetic<kForward, 4>(a, v, extra);
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o) = make_uint2(cvt_bf16x2(v[0]), cvt_bf16x2(v[1]));
+            }
+        }
+    }
+}
+
 // db without dw: db[e] = sum of the group's rows of dy, in a fixed order: a CTA takes 64 columns of one expert, eight lanes a row of
 // them, all its warps the group's rows (15818 rows in 4 experts, 192 columns: 98 us with eight warps and 4 bytes a lane, 16 so).
 constexpr int kBiasThreads = 1024, kBiasFew = 256, kBiasLong = 192;     // most, those for groups of fewer rows than that
@@ -996,6 +1110,20 @@ int launch_expert_linear(const locmoe_shape_t& s, int N, const locmoe_expert_lin
     LinearArgs a{};
     a.offsets = l.offsets; a.out = l.y; a.z_out = l.z; a.bias = l.bias; a.residual = l.residual; a.act = l.act;
     a.E = s.E; a.R = s.T; a.N = N; a.K = s.H;
+    if (s.T <= (s.H <= kFewWeight / N ? kFewRows : kFewRows / 2)) {
+        // warps a task: the fewest turns of all, each as long as a warp's part of the reduction
+        const long long tasks = (long long)s.T * (N / kFewCols), warps = (long long)kFewWarps * sm_count();
+        int best = 1;
+        double cost = 1e30;
+        for (int n = 1; n * 32 <= kFewThreads && (n == 1 || n * 32 <= s.H / 8); n *= 2) {
+            const double c = (double)((tasks * n + warps - 1) / warps) * ((s.H / 8 + 32 * n - 1) / (32 * n) + 1);
+            if (c <= cost) { cost = c; best = n; }
+        }
+        const long long resident = warps / best;
+        const int rc = launch_pdl(expert_few_kernel, dim3((unsigned)(tasks < resident ? tasks : resident)), dim3(32 * best), 0, st, a,
+                                  static_cast<const uint16_t*>(l.x), static_cast<const uint16_t*>(l.w));
+        return rc ? rc : check_launch();
+    }
     return launch_gemm<kForward>(a, l.x, l.w, ws, st);
 }
 

@@ -384,6 +384,48 @@ def test_offsets_that_make_no_sense_touch_nothing_else(X, B):
     assert B.locmoe_device_flags() == 0
 
 
+FEW = [([1], 0), ([0, 1, 0, 0, 1], 0), ([2, 1], 1), ([4], 0), ([0, 3, 0, 1], 0), ([1] * 8, 0), ([8], 0), ([5, 0, 2], 1), ([0] * 40 + [1, 1] + [0] * 40, 0), ([0, 0], 3)]
+
+
+@pytest.mark.parametrize("counts,lost", FEW)
+@pytest.mark.parametrize("IN,OUT", [(8, 8), (264, 72), (1000, 1544), (10240, 24), (2056, 4104)])
+def test_a_few_rows(X, B, counts, lost, IN, OUT):
+    """Single tokens and a few more, with all that may come with the product."""
+    offsets, R = ragged(counts, lost)
+    E, g, kept = len(counts), gen(R + IN), sum(counts)
+    x, w = randn(g, R, IN, dtype=BF), randn(g, E, OUT, IN, dtype=BF, std=IN ** -0.5)
+    bias, res = randn(g, E, OUT), randn(g, R, OUT, dtype=BF)
+    x[kept:] = float("nan")
+    e_of = torch.repeat_interleave(torch.arange(E), torch.tensor(counts)).cuda()
+    v = torch.bmm(w[e_of].double(), x[:kept].double()[:, :, None])[:, :, 0]
+    size = torch.bmm(w[e_of].double().abs(), x[:kept].double().abs()[:, :, None])[:, :, 0]
+    for act, bi, r, want_z in (("none", None, None, False), ("gelu", bias, None, True), ("silu", bias, res, True), ("relu", None, res, False)):
+        u = v if bi is None else v + bi[e_of].double()
+        off = (IN + 3) * 2.0 ** -24 * (size if bi is None else size + bi[e_of].double().abs())
+        y, z = X.expert_linear(x, w, offsets, bi, act, r, want_z)
+        want, tol = ACT64[act](u), 1.13 * off + 2e-6 * u.abs()              # slopes and approximations as above
+        if r is not None:
+            want = want + r[:kept].double()
+            tol = tol + 2.0 ** -24 * want.abs()
+        assert ((y[:kept].double() - want).abs() <= 2.0 ** -8 * want.abs() + (1 + 2.0 ** -8) * tol).all() and not y[kept:].any()
+        assert (z is not None) == want_z
+        if want_z:
+            assert ((z[:kept].double() - u).abs() <= 2.0 ** -8 * u.abs() + (1 + 2.0 ** -8) * off).all() and not z[kept:].any()
+    assert B.locmoe_device_flags() == 0
+
+
+def test_a_few_rows_and_offsets_of_all_kinds(X):
+    """A slice of the offsets: zeros before and behind.  Offsets that make no sense: no access beyond the arrays."""
+    g = gen(5)
+    x, w = randn(g, 7, 136, dtype=BF), randn(g, 3, 40, 136, dtype=BF)
+    y, z = X.expert_linear(x, w, torch.tensor([0, 2, 3, 3, 5, 7], dtype=I32, device="cuda")[1:5], act="gelu", want_z=True)
+    for t in (y, z):
+        assert not t[:2].any() and not t[5:].any() and t[2:5].any(1).all()
+    for o in ([0, 90, -20, 2 ** 31 - 1], [7, 0, 7, 0], [-5, -2 ** 31, 3, 1], [2 ** 31 - 1] * 4):
+        X.expert_linear(x, w, torch.tensor(o, dtype=I32, device="cuda"), act="gelu", want_z=True)
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("counts,lost", GROUPS + [([3000, 0, 1, 700], 9)])
 @pytest.mark.parametrize("OUT", [8, 72, 520])
 def test_the_gradient_of_the_bias_alone(X, counts, lost, OUT):
