@@ -15,8 +15,9 @@
 // Work is dealt by tiles (tile i to CTA i modulo the grid), neighbours in time sharing operands in L2, and what is left after the
 // last full wave in equal runs of 64-blocks of the reduction, so that every SM gets the same share whatever the groups are.
 // A tile that a run begins or ends in leaves fp32 sums in the workspace, which a second kernel adds in order.
+//
+// A few rows, and the bias's gradient alone, have kernels without tiles.
 #include <cuda.h>
-#include <stdlib.h>
 
 #include "common.cuh"
 #include "tensor_map.cuh"
@@ -134,7 +135,7 @@ __device__ __forceinline__ long long sum_warp(long long v) {
 // where the tensor cores are the limit, 0.4 where a few SMs stream the rows of long groups (weights), and up to 0.73 where
 // each weight tile is used by one tile of rows and comes out of HBM at 148 x 32 KB a step.  It costs the join's launch, 3 us,
 // and the sums' way through memory, 0.05 us for each row of a tile (1981 rows of 304 x 1024 with every tile split 28 against
-// 19 us whole; 2 rows of 10240 x 2560, 20 tiles in all, 27 us split; weights' gradient of 10749 rows in 4 groups, 400 x 160,
+// 19 us whole; 8 rows of one expert, 10240 x 2560, 10 tiles in all, 20 us split; weights' gradient of 10749 rows in 4 groups, 400 x 160,
 // 16 tiles, 52 us whole, 32 split).
 template <int KIND, int HALVES>
 __device__ __forceinline__ Deal deal(const LinearArgs& a, const int* offsets, int lane) {
