@@ -475,17 +475,19 @@ __global__ void __launch_bounds__(kThreads) unsort_grad_kernel(const RowArgs a, 
 //   dx[t][j] = sum_c dxs[slot[c][t]][j] + dG[t][j / g] / g,   dG_i = [G_i > 0] p_i (q_i - sum_j p_j q_j),
 //   G = group means of x[t] + eps, p = softmax(ReLU(G)), q_i = dp_i + sum_c [idx[c][t] = i] dw[c][t].
 // G, p and dG are formed anew from the row, which costs the read of x; keeping p would cost E floats a token instead but leave
-// the sign of G open, which the ReLU needs.  A team of 1 to 8 warps works on a token: the sums of the row's units go through
-// shared memory, where a few lanes each add up a group's; a unit that two groups meet in (MIXED) leaves two sums.  The
-// softmax is every warp's, to save barriers.  deps: the team's sums in shared memory, then the CTA's in `part`.  One warp a token is best where there are many tokens and their sums leave room for them
-// (65536 x 5120: 331 us, 566 with eight), more where a row is long or the tokens few (10737 rows of 5912 floats in 4
-// groups: 708 us with one, 197 with eight; 4 rows of 3216 20.7 against 5.9 us).
+// the sign of G open, which the ReLU needs.  A team of 8 lanes or 1 to 8 warps works on a token: the sums of the row's units go
+// through shared memory, where a few lanes each add up a group's; a unit that two groups meet in (MIXED) leaves two sums.  The
+// softmax is every warp's, to save barriers.  deps: the team's sums in shared memory, then the CTA's in `part`.  One warp a
+// token is best where there are many tokens and their sums leave room for them (65536 x 5120: 331 us, 566 with eight), more
+// where a row is long or the tokens few (10737 rows of 5912 floats in 4 groups: 708 us with one, 197 with eight; 4 rows of 3216
+// 20.7 against 5.9 us), eight lanes where rows are short and a token is latencies (29585 rows of 72 floats 28 us with a warp,
+// 12 so; 65536 x 256 in 32 groups 58 against 33; 3751 x 168 10.4 against 12.5).
 struct RouterArgs {
     const void* x; const float* eps; const int32_t* idx; const float* dw; const float* dp; float* part;
     int g;                      // elements a group
     unsigned rcp_g;             // floor((2^32 - 1) / g)
     float inv_g;
-    int warps;                  // of a team: 1, 2, 4, 8
+    int team;                   // threads: 8, or 1, 2, 4, 8 warps
     int lanes;                  // that share a group's sum, a power of two up to 32
     size_t floats;              // of shared memory a team
 };
@@ -496,16 +498,17 @@ __device__ __forceinline__ int group_at(const RouterArgs& b, int n) {
     return n - e * b.g >= b.g ? e + 1 : e;
 }
 
-template <int DT, int CLS, bool MIXED, int KM>
+// W: lanes of a warp that work on one token, 32 (and more warps with them) or 8.
+template <int DT, int CLS, bool MIXED, int KM, int W>
 __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const RowArgs a, const RouterArgs b, const void* __restrict__ dxs,
                                                                     const int32_t* __restrict__ slot, void* __restrict__ dx) {
     typedef Unit<DT, CLS> U;
     // units in flight a lane and row: registers for four CTAs an SM, which spills cost more than loads in flight gain
     constexpr int CH = CLS == WIDE ? (KM <= 2 ? 2 : 1) : KM <= 2 ? 8 / KM : 16 / KM, XCH = CLS == WIDE ? 4 : 8;
     extern __shared__ float smf[];
-    const int nt = 32 * b.warps, team = threadIdx.x / nt, teams = kThreads / nt, tid = threadIdx.x - team * nt, lane = tid & 31, E = a.E;
-    auto meet = [&] {               // the team's warps
-        if (nt == 32) __syncwarp();
+    const int nt = W < 32 ? W : b.team, team = threadIdx.x / nt, teams = kThreads / nt, tid = threadIdx.x - team * nt, lane = tid & 31, E = a.E;
+    auto meet = [&] {               // the team, or the teams of a warp
+        if (W < 32 || nt == 32) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(nt) : "memory");
     };
     float* lo = smf + team * b.floats;                            // [U] sum of a unit's elements in the group of its first
@@ -517,14 +520,18 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
     pdl_wait();
     pdl_trigger();
     const long long first = (long long)blockIdx.x * a.tpc, last = min((long long)a.T, first + a.tpc);
-    for (long long t = first + team; t < last; t += teams) {
+    for (long long t0 = first; t0 < last; t0 += teams) {
+        const long long t = t0 + team;
+        const bool on = W == 32 || t < last;    // the teams of a warp stay together
+        if (W == 32 && t >= last) break;
+        const int units = on ? a.U : 0;
         int s[KM];
 #pragma unroll
         for (int c = 0; c < KM; ++c) {
-            s[c] = dxs && c < a.K ? __ldg(slot + (long long)c * a.T + t) : -1;
+            s[c] = on && dxs && c < a.K ? __ldg(slot + (long long)c * a.T + t) : -1;
             if (s[c] >= a.rows) s[c] = -1;
         }
-        for (int u0 = tid; u0 < a.U; u0 += XCH * nt) {
+        for (int u0 = tid; u0 < units; u0 += XCH * nt) {
             typename U::Raw r[XCH];
 #pragma unroll
             for (int i = 0; i < XCH; ++i)
@@ -572,15 +579,15 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
         float dw[KM];
 #pragma unroll
         for (int c = 0; c < KM; ++c) {
-            id[c] = c < a.K && b.dw ? __ldg(b.idx + (long long)c * a.T + t) : -1;
-            dw[c] = c < a.K && b.dw ? __ldg(b.dw + (long long)c * a.T + t) : 0.0f;
+            id[c] = on && c < a.K && b.dw ? __ldg(b.idx + (long long)c * a.T + t) : -1;
+            dw[c] = on && c < a.K && b.dw ? __ldg(b.dw + (long long)c * a.T + t) : 0.0f;
         }
         meet();
         float top = 0.0f, z = 0.0f, m = 0.0f;
-        for (int e = lane; e < E; e += 32) top = fmaxf(top, G[e]);
+        for (int e = lane; e < E; e += W) top = fmaxf(top, G[e]);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        for (int e = lane; e < E; e += 32) {
+        for (int o = W / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int e = lane; e < E; e += W) {
             const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top);        // a NaN stays one
             float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
@@ -589,11 +596,11 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
             m = __fmaf_rn(v, q, m);
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); m += __shfl_xor_sync(0xffffffffu, m, o); }
+        for (int o = W / 2; o; o >>= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); m += __shfl_xor_sync(0xffffffffu, m, o); }
         const float rz = 1.0f / z;
         m *= rz;
-        if (tid < 32) {
-            for (int e = lane; e < E; e += 32) {
+        if (on && tid < 32) {
+            for (int e = lane; e < E; e += W) {
                 float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
                 for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
@@ -604,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
             }
         }
         meet();
-        for (int u0 = tid; u0 < a.U; u0 += CH * nt) {
+        for (int u0 = tid; u0 < units; u0 += CH * nt) {
             typename U::Raw r[CH][KM];
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
@@ -697,6 +704,7 @@ int unit_of(const locmoe_shape_t& s, std::initializer_list<const void*> arrays) 
 }
 int unit_elements(const locmoe_shape_t& s, int cls) { return cls == WIDE ? (s.x_dtype == LOCMOE_F32 ? 4 : 8) : cls == PAIR ? 2 : 1; }
 
+constexpr int kLanes = 8;                // that share a token whose row is short
 constexpr size_t kRouterSmem = 200 * 1024;
 // How a row is cut for the router's gradient: units that meet two groups at most, whole in one or of 16 bytes (MIXED).
 struct RouterPlan { int cls; bool mixed; int U; size_t smem; };
@@ -737,12 +745,14 @@ int unsort_grad_dt(int grid, const RowArgs& a, const void* dout, const void* y, 
 template <int DT, int CLS>
 int sort_grad_router_dt(int grid, const RouterPlan& p, const RowArgs& a, const RouterArgs& b, const void* dxs, const int32_t* slot, void* dx,
                         cudaStream_t st) {
-#define LOCMOE_BY_CHOICES(MIXED)                                                                                              \
-    (a.K == 1 ? sort_grad_router_kernel<DT, CLS, MIXED, 1> : a.K == 2 ? sort_grad_router_kernel<DT, CLS, MIXED, 2>             \
-     : a.K <= 4 ? sort_grad_router_kernel<DT, CLS, MIXED, 4> : sort_grad_router_kernel<DT, CLS, MIXED, 8>)
-    auto* k = CLS == WIDE && p.mixed ? LOCMOE_BY_CHOICES(CLS == WIDE) : LOCMOE_BY_CHOICES(false);
+#define LOCMOE_BY_CHOICES(MIXED, W)                                                                                                 \
+    (a.K == 1 ? sort_grad_router_kernel<DT, CLS, MIXED, 1, W> : a.K == 2 ? sort_grad_router_kernel<DT, CLS, MIXED, 2, W>             \
+     : a.K <= 4 ? sort_grad_router_kernel<DT, CLS, MIXED, 4, W> : sort_grad_router_kernel<DT, CLS, MIXED, 8, W>)
+#define LOCMOE_BY_TEAM(MIXED) (b.team < 32 ? LOCMOE_BY_CHOICES(MIXED, kLanes) : LOCMOE_BY_CHOICES(MIXED, 32))
+    auto* k = CLS == WIDE && p.mixed ? LOCMOE_BY_TEAM(CLS == WIDE) : LOCMOE_BY_TEAM(false);
+#undef LOCMOE_BY_TEAM
 #undef LOCMOE_BY_CHOICES
-    const size_t smem = p.smem * (kWarps / b.warps);
+    const size_t smem = p.smem * (kThreads / b.team);
     if (smem > 48 * 1024 && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRouterSmem) != cudaSuccess) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;
@@ -840,17 +850,21 @@ int launch_sort_grad(const locmoe_shape_t& s, int K, const locmoe_sort_grad_t& g
     const RouterPlan p = router_plan(s, unit_of(s, {g.x, g.dxs, g.dx}));
     if (p.smem > kRouterSmem) return LOCMOE_ERR_ALIGN;      // arrays that are not 16-byte aligned take more room
     // warps a token: so many that four CTAs' sums fit an SM, and while all tokens are still at work at once
-    int warps = 1;
-    while (warps < kWarps && ((kWarps / warps) * p.smem > 50 * 1024 || 2ll * warps * s.T <= (long long)router_grid_cap() * kWarps)) warps *= 2;
-    int lanes = 32;
-    while (lanes > 1 && (long long)lanes * s.E > 32 * warps) lanes /= 2;
-    const int teams = kWarps / warps;
+    int team = 32;
+    while (team < kThreads && ((kThreads / team) * p.smem > 50 * 1024 || 2ll * team * s.T <= (long long)router_grid_cap() * kThreads)) team *= 2;
+    // eight lanes a token: short rows, and a third of the lanes that fit at work at least
+    if (team == 32 && p.U <= (p.cls == WIDE ? 12 : 24) * kLanes && 3ll * kLanes * s.T >= (long long)router_grid_cap() * kThreads &&
+        (kThreads / kLanes) * p.smem <= 50 * 1024)
+        team = kLanes;
+    int lanes = min(team, 32);
+    while (lanes > 1 && (long long)lanes * s.E > team) lanes /= 2;
+    const int teams = kThreads / team;
     RowArgs a{s.T, p.U, K, s.E, (long long)K * s.T, 32, 1};
     long long grid = ((long long)s.T + teams - 1) / teams;
     if (grid > router_grid_cap()) grid = router_grid_cap();
     a.tpc = (int)((s.T + grid - 1) / grid);
     grid = (s.T + a.tpc - 1) / a.tpc;
-    const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, s.H / s.E, 0xffffffffu / (unsigned)(s.H / s.E), 1.0f / (float)(s.H / s.E), warps, lanes,
+    const RouterArgs b{g.x, g.eps, g.idx_k, g.dw, g.dp, g.deps ? static_cast<float*>(ws) : nullptr, s.H / s.E, 0xffffffffu / (unsigned)(s.H / s.E), 1.0f / (float)(s.H / s.E), team, lanes,
                        p.smem / sizeof(float)};
     int rc = LOCMOE_BY_UNIT(s.x_dtype, p.cls, sort_grad_router_dt, (int)grid, p, a, b, g.dxs, g.slot, g.dx, st);
     if (rc == LOCMOE_OK && g.deps)

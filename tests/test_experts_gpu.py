@@ -160,7 +160,8 @@ def router64(x, idx, dw, eps, dp):
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("T,K,H,E,kind", [(1, 1, 8, 1, "any"), (9, 2, 2560, 32, "any"), (33, 3, 777, 21, "bad"), (65, 1, 5120, 64, "any"), (50, 8, 1024, 1024, "any"),
                                           (700, 2, 1000, 4, "bad"), (2500, 4, 128, 32, "none"), (40, 1, 12288, 3, "any"), (31, 3, 1236, 6, "bad"),
-                                          (6000, 2, 96, 24, "any")])
+                                          (6000, 2, 96, 24, "any"), (7001, 1, 72, 8, "any"), (6500, 2, 256, 64, "bad"), (9000, 3, 189, 21, "any"),
+                                          (6400, 4, 256, 32, "none"), (6350, 8, 100, 10, "bad"), (6321, 1, 768, 3, "any")])
 def test_router_gradient(X, B, T, K, H, E, kind, dt):
     g = gen(T * 3 + H)
     idx = choices(g, T, K, E, kind)
