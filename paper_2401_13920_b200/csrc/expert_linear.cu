@@ -863,6 +863,7 @@ __global__ void __launch_bounds__(kJoinThreads) expert_join_kernel(const LinearA
 // shared memory, asynchronously and on into the next task's, were slower (two rows, 2560 x 10240: 26 against 23 us).
 constexpr int kFewRows = 8, kFewThreads = 256, kFewWarps = 24;      // kFewWarps: of an SM
 constexpr int kFewCols = 4, kFewShare = 2;                          // columns and rows of a task
+constexpr int kScan = 8;                                            // offsets a lane in flight (a row of 1024 experts, 256 x 256: 3.8 us, 6.3 with one)
 // Four rows (of one expert 20 us either way at 2560 x 10240, of four 41 against 35, two of two 26 against 20, one 19 against 12;
 // 16 experts of 3936 x 288 12 against 5), eight where the weights are so small that the tiles' fixed times count (64 of
 // 1024 x 1024, eight rows of as many 12 against 6 us, of one expert 9 against 10; 2560 x 10240 20 against 49).
@@ -917,13 +918,22 @@ __global__ void __launch_bounds__(kFewThreads, kFewWarps * 32 / kFewThreads) exp
     pdl_trigger();
     if (threadIdx.x < 32) {
         int n = 0;
-        for (int e0 = 0; e0 < a.E; e0 += 32) {
-            const int e = e0 + (int)threadIdx.x;
-            const Group g = e < a.E ? group_of(a.offsets, e, a.R) : Group{0, 0};
-            const unsigned has = __ballot_sync(0xffffffffu, g.n > 0);
-            const int at = n + __popc(has & ((1u << threadIdx.x) - 1u));
-            if (g.n > 0 && at < kFewRows) { busy[at][0] = e; busy[at][1] = g.lo; busy[at][2] = g.n; }
-            n += __popc(has);
+        for (int e0 = 0; e0 < a.E; e0 += 32 * kScan) {
+            int off[kScan][2];
+#pragma unroll
+            for (int i = 0; i < kScan; ++i) {
+                const int e = e0 + 32 * i + (int)threadIdx.x;
+                off[i][0] = e < a.E ? __ldg(a.offsets + e) : 0;
+                off[i][1] = e < a.E ? __ldg(a.offsets + e + 1) : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < kScan; ++i) {
+                const Group g = group_of(off[i], 0, a.R);
+                const unsigned has = __ballot_sync(0xffffffffu, g.n > 0);
+                const int at = n + __popc(has & ((1u << threadIdx.x) - 1u));
+                if (g.n > 0 && at < kFewRows) { busy[at][0] = e0 + 32 * i + (int)threadIdx.x; busy[at][1] = g.lo; busy[at][2] = g.n; }
+                n += __popc(has);
+            }
         }
         if (threadIdx.x == 0) n_busy = min(n, kFewRows);       // more only where the offsets descend
     }
