@@ -23,6 +23,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 // which an SM does one in 60 cycles, in both passes).
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32, kPlanBatch = 8;
 constexpr int kPlanRun = 1024;           // assignments a CTA before another is taken, up to 16 (8 where the device has no more)
+constexpr size_t plan_smem(int E) { return ((size_t)(kPlanWarps + 2) * E + 32) * sizeof(int); }
 
 __device__ __forceinline__ int ld_cluster(const int* p, int cta) {
     uint32_t ra;
@@ -765,9 +766,10 @@ int sort_grad_router_dt(int grid, const RouterPlan& p, const RowArgs& a, const R
 // `with_inv` = 0: the rows' kernel, which follows, writes inv's part with assignments.
 int launch_sort_plan(int T, int K, int E, const int32_t* idx, int32_t* offsets, int32_t* slot, int32_t* inv, int with_inv, int32_t* load, cudaStream_t st) {
     const long long V = (long long)K * T;
-    const size_t smem = ((size_t)(kPlanWarps + 2) * E + 32) * sizeof(int);
+    const size_t smem = plan_smem(E);
     auto* kernel = E < 16 ? sort_plan_kernel<4> : E < 64 ? sort_plan_kernel<6> : E < 256 ? sort_plan_kernel<8> : sort_plan_kernel<11>;    // keys 0 to E
-    if ((smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) ||
+    // always the most that any call needs: the limit is the kernel's, and another host thread's smaller one would refuse this launch
+    if ((smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_smem(1024)) != cudaSuccess) ||
         (V > 8ll * kPlanRun && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;

@@ -1,0 +1,73 @@
+"""Calls of the sorted-token operators and the layer made of them at the edges of what their documentation allows: no tokens, host
+threads, captures, default types, and that nothing but the outputs is written."""
+import ctypes as C
+import os
+import subprocess
+import sys
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BF, F32, I32, U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+@pytest.fixture(scope="module")
+def X():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a CUDA device")
+    from paper_2401_13920_b200 import experts
+    return experts
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2401_13920_b200 import binding
+    return binding
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def at_once(calls, n=4000):
+    """Straight calls of the library from a host thread each, which leave the interpreter's lock: {key: the codes they returned}."""
+    codes = {k: set() for k in calls}
+
+    def loop(k):
+        f, args = calls[k]
+        for _ in range(n):
+            codes[k].add(f(*args))
+    threads = [threading.Thread(target=loop, args=(k,)) for k in calls]
+    torch.cuda.synchronize()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    return codes
+
+
+# What one thread asks of a kernel must not be taken away, between its check and its launch, by the smaller request of another.
+
+def test_host_threads_order_by_different_numbers_of_experts(X, B):
+    T, calls, kept = 64, {}, {}
+    for E in (400, 600, 800, 1024):
+        s = torch.cuda.Stream()
+        idx = torch.randint(0, E, (1, T), generator=gen(E), device="cuda", dtype=I32)
+        out = [torch.full((m,), -7, dtype=I32, device="cuda") for m in (E + 1, T, T)]
+        shape = B.Shape(T, 1024, E, 1, 1, B.BF16, 0)
+        kept[E] = (shape, idx, out, s)
+        calls[E] = B._lib.locmoe_sort, (C.byref(shape), 1, idx.data_ptr(), None, *(t.data_ptr() for t in out), None, None, s.cuda_stream)
+    codes = at_once(calls)
+    assert all(c == {0} for c in codes.values()), codes
+    for E, (_, idx, (offsets, slot, inv), _) in kept.items():
+        order = torch.sort(idx[0], stable=True).indices
+        assert torch.equal(inv, order.to(I32)) and torch.equal(slot[order.long()], torch.arange(T, device="cuda", dtype=I32))
+        assert torch.equal(offsets[1:].long(), torch.bincount(idx[0].long(), minlength=E).cumsum(0))
