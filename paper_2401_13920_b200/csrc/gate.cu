@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(256) gate_scalar_kernel(const GateArgs a) {
 
 int gcd_int(int a, int b) { while (b) { int t = a % b; a = b; b = t; } return a; }
 
+constexpr size_t kMostSmem = 200 * 1024;    // of a CTA
 thread_local int g_last_grid = 0;   // grid of the launch just queued by this thread's call (rows of p_part); set by launch_persistent
 
 template <typename K>
@@ -483,10 +484,11 @@ int launch_persistent(K kernel, const GateArgs& a, int max_warps, cudaStream_t s
     size_t smem = 0;
     for (; wpb >= 1; wpb >>= 1) {
         smem = ((size_t)wpb * (a.warp_floats + a.pacc_floats) + a.tab_ints) * sizeof(float);
-        if (smem <= 200 * 1024) break;
+        if (smem <= kMostSmem) break;
     }
     if (wpb < 1) return LOCMOE_ERR_SHAPE;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    // always the most: the limit is the kernel's, and another host thread's smaller one would refuse this launch
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem) != cudaSuccess) {
         cudaGetLastError();
         return LOCMOE_ERR_CUDA;
     }

@@ -71,3 +71,18 @@ def test_host_threads_order_by_different_numbers_of_experts(X, B):
         order = torch.sort(idx[0], stable=True).indices
         assert torch.equal(inv, order.to(I32)) and torch.equal(slot[order.long()], torch.arange(T, device="cuda", dtype=I32))
         assert torch.equal(offsets[1:].long(), torch.bincount(idx[0].long(), minlength=E).cumsum(0))
+
+
+def test_host_threads_run_the_router_on_rows_of_different_lengths(B):
+    T, calls, kept = 32, {}, {}
+    for H, E in ((16384, 512), (8192, 512), (4096, 128), (1024, 8)):
+        s, x = torch.cuda.Stream(), randn(gen(H), T, H, dtype=BF)
+        out = [torch.empty(T, dtype=t, device="cuda") for t in (I32, F32, F32)]
+        shape, opts = B.Shape(T, H, E, 1, 1, B.BF16, 0), B.GateOpts(None, None, None, None, 0)
+        B.locmoe_gate_ex(shape, x, *out)
+        kept[H] = (shape, opts, s, x, out, [t.clone() for t in out])
+        calls[H] = B._lib.locmoe_gate_ex, (C.byref(shape), x.data_ptr(), C.byref(opts), *(t.data_ptr() for t in out), s.cuda_stream)
+    codes = at_once(calls)
+    assert all(c == {0} for c in codes.values()), codes
+    for *_, out, want in kept.values():
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
