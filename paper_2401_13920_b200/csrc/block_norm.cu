@@ -1189,7 +1189,8 @@ int round16(int n) { return (n + 15) / 16 * 16; }
 template <typename K>
 bool allow_smem(K kernel, size_t bytes) {
     if (bytes <= 32 << 10) return true;   // with the static strips within the 48 KB that need no leave
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess) return true;
+    // always the most: the limit is the kernel's, and another host thread's smaller one would refuse this launch
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem) == cudaSuccess) return true;
     cudaGetLastError();
     return false;
 }

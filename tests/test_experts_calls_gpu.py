@@ -86,3 +86,20 @@ def test_host_threads_run_the_router_on_rows_of_different_lengths(B):
     assert all(c == {0} for c in codes.values()), codes
     for *_, out, want in kept.values():
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_host_threads_run_the_norms_on_rows_of_different_lengths(B):
+    T, calls, kept = 64, {}, {}
+    for H in (512, 1024, 2048, 4096):
+        s, h, dn = torch.cuda.Stream(), randn(gen(H), T, H), randn(gen(H + 1), T, H)
+        n, dh, w = torch.empty_like(h), torch.empty_like(h), torch.ones(H, device="cuda")
+        shape = B.Shape(T, H, 1, 1, 1, B.F32, 0)
+        f = B.BlockNorm(h=h.data_ptr(), w_pre=w.data_ptr(), n_out=n.data_ptr(), res_scale=1.0, eps=1e-6)
+        kept[H] = (shape, s, h, dn, n, dh, w, f)
+        calls[H] = B._lib.locmoe_block_norm, (C.byref(shape), T, C.byref(f), s.cuda_stream)
+    codes = at_once(calls)
+    assert all(c == {0} for c in codes.values()), codes
+    for _, _, h, _, n, *_ in kept.values():
+        want = h.double() * (h.double().square().mean(1, keepdim=True) + 1e-6).rsqrt()
+        # the sum of the squares, its root and the products: some steps of fp32
+        assert ((n.double() - want).abs() <= (h.shape[1] + 8) * 2.0 ** -24 * want.abs()).all()
