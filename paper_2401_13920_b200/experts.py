@@ -323,8 +323,10 @@ class RouteSort(torch.autograd.Function):
         x, eps, idx_k, offsets, slot, inv, f = ctx.saved_tensors
         if dxs is None and dw is None and daux is None:
             return (None,) * 5
+        if x.shape[0] == 0:
+            return torch.zeros_like(x), torch.zeros_like(eps) if ctx.needs_input_grad[1] else None, None, None, None
         dp = None
-        if daux is not None and x.shape[0] > 0:
+        if daux is not None:
             dp = f * (daux * (ctx.alpha * f.numel() / x.shape[0]))
         router = dw is not None or dp is not None
         dx, deps = sort_rows_grad(_dense(dxs), Order(offsets, slot, inv), x if router else None, idx_k, _dense(dw), eps if router else None, dp,

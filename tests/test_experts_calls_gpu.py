@@ -36,6 +36,18 @@ def randn(g, *shape, dtype=F32):
     return torch.randn(*shape, generator=g, device="cuda").to(dtype)
 
 
+@pytest.mark.parametrize("K", [1, 2])
+def test_the_balance_loss_of_no_tokens(X, K):
+    """Every output of the router may be the only one that a loss uses, also where there are no tokens."""
+    for use in (0, 1, 2):
+        x = torch.zeros(0, 64, dtype=BF, device="cuda", requires_grad=True)
+        eps = torch.zeros(4, device="cuda", requires_grad=True)
+        out = X.RouteSort.apply(x, eps, 4, K, 0.1)
+        out[use].float().sum().backward()
+        assert x.grad.shape == (0, 64) and x.grad.dtype == BF
+        assert use == 0 and eps.grad is None or eps.grad.tolist() == [0.0] * 4
+
+
 def at_once(calls, n=4000):
     """Straight calls of the library from a host thread each, which leave the interpreter's lock: {key: the codes they returned}."""
     codes = {k: set() for k in calls}
