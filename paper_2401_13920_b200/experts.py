@@ -239,7 +239,8 @@ def expert_linear_grad(dy, x, w, offsets, z=None, act=None, want_dx=True, want_d
         raise ValueError("act: needed with z")
     _want_shape(x, (R, H), "x")
     _want_shape(z, (R, H), "z")
-    dw_dtype = _BF if dw_dtype is None else dw_dtype
+    if dw_dtype is None:
+        dw_dtype = w.dtype if want_dw else _BF
     if dw_dtype not in (_BF, _F32):
         raise TypeError("dw_dtype: expected bfloat16 or float32, got %s" % (dw_dtype,))
     _here(dy, "dy")

@@ -48,6 +48,18 @@ def test_the_balance_loss_of_no_tokens(X, K):
         assert use == 0 and eps.grad is None or eps.grad.tolist() == [0.0] * 4
 
 
+def test_the_weights_gradient_has_the_weights_type(X):
+    g = gen(1)
+    offsets = torch.tensor([0, 3, 3, 7], dtype=I32, device="cuda")
+    x, dy, w = randn(g, 7, 16, dtype=BF), randn(g, 7, 24, dtype=BF), randn(g, 3, 24, 16)
+    for rows in (7, 0):
+        o = offsets if rows else torch.zeros_like(offsets)
+        for wt in (F32, BF):
+            _, dw, _ = X.expert_linear_grad(dy[:rows], x[:rows], w.to(wt), o, want_dx=False)
+            _, same, _ = X.expert_linear_grad(dy[:rows], x[:rows], w.to(BF), o, want_dx=False, dw_dtype=wt)
+            assert dw.dtype == wt and torch.equal(dw, same)
+
+
 def at_once(calls, n=4000):
     """Straight calls of the library from a host thread each, which leave the interpreter's lock: {key: the codes they returned}."""
     codes = {k: set() for k in calls}
