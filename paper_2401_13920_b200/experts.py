@@ -265,21 +265,59 @@ def _dense(t):
     return None if t is None else t.contiguous()
 
 
-# A leaf's gradient is added up on the stream that the node for it was made on, and the node lives as long as any graph that
-# reached it.  If that was the default stream, which no capture can take in, a captured backward pass through it spoils the
-# capture and can end the process.  So the forward passes note the stream at each node (the first one stays: later graphs
-# share the node), and a captured backward pass refuses such a node before any gradient is sent there.
-def _note_stream(ctx) -> None:
-    for node, _ in ctx.next_functions:
-        if node is not None and type(node).__name__ == "AccumulateGrad":
-            node.metadata.setdefault("locmoe_stream", B._raw_stream(torch.cuda.current_device()))
+# A leaf's gradient is added up on the stream that the node for it was made on, by whichever operator came first, and the node
+# lives as long as any graph that reached it.  If that was the default stream, which no capture can take in, a captured backward
+# pass through it spoils the capture and can end the process.  So a captured backward pass asks each node for its stream and
+# refuses before any gradient is sent there.  The node says it to a hook of its leaf only: a pass that sends it nothing reaches
+# the hook on that stream, and ends there, before anything is launched or waited for.
+class _Found(Exception):
+    pass
+
+
+class _Nothing(torch.autograd.Function):
+    """A number of the host's that depends on a tensor and gives it no gradient."""
+
+    @staticmethod
+    def forward(ctx, t):
+        return torch.zeros(())
+
+    @staticmethod
+    def backward(ctx, g):
+        return None
+
+
+def _leaf_stream(leaf) -> int:
+    """The stream (a raw handle, 0: the default stream) that gradients of this leaf are added up on."""
+    if not leaf.requires_grad:      # any more: its node cannot be asked
+        return 0
+    found = []
+
+    def hook(_):
+        found.append(B._raw_stream(leaf.get_device()))
+        raise _Found
+    with torch.enable_grad():
+        out = _Nothing.apply(leaf)
+    others = dict(leaf._backward_hooks or {})                   # are for gradients
+    if others:
+        leaf._backward_hooks.clear()
+    handle = leaf.register_hook(hook)
+    try:
+        out.backward()
+    except _Found:
+        pass
+    finally:
+        handle.remove()
+        leaf._backward_hooks.update(others)
+    return found[0]
 
 
 def _check_capture(ctx) -> None:
-    if torch.cuda.is_current_stream_capturing() and any(node is not None and node.metadata.get("locmoe_stream", 1) == 0
-                                                        for node, _ in ctx.next_functions):
-        raise RuntimeError("a captured backward pass: a graph of the same leaves that was built on the default stream is still "
-                           "alive; drop its outputs first, or build it on another stream")
+    if not torch.cuda.is_current_stream_capturing():
+        return
+    for node, _ in ctx.next_functions:
+        if node is not None and type(node).__name__ == "AccumulateGrad" and _leaf_stream(node.variable) == 0:
+            raise RuntimeError("a captured backward pass: a graph of the same leaves that was built on the default stream is still "
+                               "alive; drop its outputs first, or build it on another stream")
 
 
 class RouteSort(torch.autograd.Function):
@@ -295,7 +333,6 @@ class RouteSort(torch.autograd.Function):
         _on_current(x, "x")
         _on_current(eps, "eps")
         _want_shape(eps, (E,), "eps")
-        _note_stream(ctx)
         ctx.set_materialize_grads(False)
         idx_k, w_k, aux, f = _rows(K, T, _I32), _rows(K, T, _F32), None, None
         if T > 0:
@@ -344,7 +381,6 @@ class ExpertFFN(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, xs, w_in, w_out, b_in, b_out, offsets, act="gelu"):
-        _note_stream(ctx)
         a, z = expert_linear(xs, w_in, offsets, b_in, act, want_z=_act(act) != B.ACT_NONE)
         y, _ = expert_linear(a, w_out, offsets, b_out)
         ctx.act = act
@@ -373,7 +409,6 @@ class Unsort(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, y, w_k, residual, offsets, slot, inv):
-        _note_stream(ctx)
         ctx.save_for_backward(y, w_k, offsets, slot, inv)
         return unsort_rows(y, Order(offsets, slot, inv), w_k, residual)
 
@@ -395,8 +430,8 @@ def moe_layer(x, w_in, w_out, K=1, b_in=None, b_out=None, eps=None, act="gelu", 
     x [T][H], w_in [E][F][H], w_out [E][H][F] bf16; b_in [E][F], b_out [E][H] and eps [E] (the router's bias) fp32, or None.
     Returns ``(out, aux)``, aux the load-balance loss with alpha > 0, else None.  Differentiable in all tensors.
 
-    Forward and backward can be captured into a CUDA graph; no graph of the same leaves that was built on the default stream
-    may then be alive (the backward pass refuses it)."""
+    Forward and backward can be captured into a CUDA graph; no graph of the same leaves that was built on the default stream, by
+    whatever operator, may then be alive (the backward pass refuses leaves of its own inputs that are held so)."""
     xs, w_k, aux, _, offsets, slot, inv = RouteSort.apply(x, eps, w_in.shape[0], K, alpha)
     y = ExpertFFN.apply(xs, w_in, w_out, b_in, b_out, offsets, act)
     return Unsort.apply(y, w_k, residual, offsets, slot, inv), aux

@@ -127,3 +127,70 @@ def test_host_threads_run_the_norms_on_rows_of_different_lengths(B):
         want = h.double() * (h.double().square().mean(1, keepdim=True) + 1e-6).rsqrt()
         # the sum of the squares, its root and the products: some steps of fp32
         assert ((n.double() - want).abs() <= (h.shape[1] + 8) * 2.0 ** -24 * want.abs()).all()
+
+
+CHILD = """
+import torch
+from paper_2401_13920_b200 import experts
+BF = torch.bfloat16
+t = dict(x=torch.randn(40, 64, device="cuda").to(BF), w_in=torch.randn(4, 72, 64, device="cuda").to(BF), w_out=torch.randn(4, 64, 72, device="cuda").to(BF),
+         residual=torch.randn(40, 64, device="cuda").to(BF))
+leaf = t[LEAF].requires_grad_()
+side = torch.cuda.Stream()
+side.wait_stream(torch.cuda.current_stream())
+def run():
+    return experts.moe_layer(t["x"], t["w_in"], t["w_out"], 2, residual=t["residual"])[0].float().square().sum()
+def under(stream, f):
+    with torch.cuda.stream(stream):
+        return f()
+def capture():
+    leaf.grad = None
+    graph = torch.cuda.CUDAGraph()
+    try:
+        with torch.cuda.graph(graph):
+            run().backward()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, leaf.grad = leaf.grad, None
+        assert torch.equal(got, torch.autograd.grad(run(), leaf)[0])
+        print("captured")
+    except RuntimeError as e:
+        print("refused" if "a captured backward pass" in str(e) else e)
+    torch.cuda.synchronize()
+default = torch.cuda.default_stream()
+under(side, lambda: run().backward())                   # a pass before any capture
+torch.cuda.synchronize()
+other, layer = (default, side) if FIRST == "default" else (side, default)
+kept = under(other, lambda: leaf * 1.0)                 # the leaf's node belongs to another operator's stream ...
+graph = under(layer, run)                               # ... and the layer sees it on one that says otherwise
+torch.cuda.synchronize()
+capture()
+del kept, graph
+capture()
+"""
+
+
+@pytest.mark.parametrize("leaf", ["x", "w_in", "w_out", "residual"])
+@pytest.mark.parametrize("first,want", [("default", "refused"), ("side", "captured")])
+def test_a_captured_backward_pass_knows_where_a_leafs_node_was_made(leaf, first, want):
+    """In a process of its own, which has to live on."""
+    code = CHILD.replace("LEAF", repr(leaf)).replace("FIRST", repr(first))
+    done = subprocess.run([sys.executable, "-W", "ignore", "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+    assert done.stdout.split() == [want, "captured"], done.stdout
+
+
+def test_asking_for_a_leafs_stream_leaves_the_leaf_alone(X):
+    """Its own hooks are for gradients: not called, and kept in their order; no gradient appears."""
+    calls = []
+    x = torch.ones(4, device="cuda", requires_grad=True)
+    for f in (3.0, 5.0):
+        x.register_hook(lambda g, f=f: calls.append(f) or g + f * len(calls))
+    side = torch.cuda.Stream()
+    for stream, handle in ((torch.cuda.default_stream(), 0), (side, side.cuda_stream)):
+        with torch.cuda.stream(stream):
+            kept = x * 2.0
+        assert X._leaf_stream(x) == handle and not calls and x.grad is None
+        del kept
+    (x * 2.0).sum().backward()
+    assert calls == [3.0, 5.0] and x.grad.tolist() == [2.0 + 3.0 + 10.0] * 4
