@@ -594,8 +594,8 @@ int locmoe_block_norm_grad(const locmoe_shape_t *shape, int32_t C_alloc, const l
  *   G_i = mean of group i of x[t] + eps_i (eps NULL: 0),  p = softmax(ReLU(G)),  q_i = dp_i + sum_c [idx_k[c][t] = i] dw[c][t]
  * where dw float[K][T] is the gradient of the chosen scores w_k and dp float[E] that of any token's p_i, the same for all
  * tokens (alpha n f_i / T for the balance loss); either may be NULL.  deps float[E] (NULL to skip) = sum_t dG, the gradient of
- * eps.  dxs may be NULL with x.  The rows' sums of groups have to fit shared memory: rows up to 375 KB, or 48000 elements
- * where rows are no whole number of 16 bytes or groups are shorter (LOCMOE_ERR_TOO_LARGE); arrays that are not 16-byte
+ * eps.  A G_i that is NaN counts as 0, as in the forward pass.  dxs may be NULL with x.  The rows' sums of groups have to fit
+ * shared memory: rows up to 375 KB, or 48000 elements where rows are no whole number of 16 bytes or groups are shorter (LOCMOE_ERR_TOO_LARGE); arrays that are not 16-byte
  * aligned count as such (LOCMOE_ERR_ALIGN).  ws (only with deps): locmoe_sort_grad_bytes() bytes, 256-byte aligned.
  *
  * locmoe_unsort: out[t] = residual[t] + sum_c w_k[c][t] * y[slot[c][t]], y [V][H], out, residual (NULL: 0) [T][H] of x_dtype,

@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
 #pragma unroll
         for (int o = W / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         for (int e = lane; e < E; e += W) {
-            const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top);        // a NaN stays one
+            const float v = expf(fmaxf(G[e], 0.0f) - top);                  // a mean that is NaN counts as 0, as in the forward pass
             float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
             for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
@@ -605,8 +605,8 @@ __global__ void __launch_bounds__(kThreads, 4) sort_grad_router_kernel(const Row
                 float q = b.dp ? __ldg(b.dp + e) : 0.0f;
 #pragma unroll
                 for (int c = 0; c < KM; ++c) q += id[c] == e ? dw[c] : 0.0f;
-                const float v = expf((G[e] < 0.0f ? 0.0f : G[e]) - top) * rz;
-                const float d = G[e] <= 0.0f ? 0.0f * v : v * (q - m);      // what leaves through the ReLU
+                const float v = expf(fmaxf(G[e], 0.0f) - top) * rz;
+                const float d = G[e] > 0.0f ? v * (q - m) : 0.0f * v;       // what leaves through the ReLU
                 deps[e] += d;
                 dG[e] = d * b.inv_g;
             }

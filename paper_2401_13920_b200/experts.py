@@ -104,7 +104,7 @@ def sort_rows_grad(dxs, order: Order, x=None, idx_k=None, dw=None, eps=None, dp=
 
     With the tokens x [T][H] the router's own gradient is added: ``dw`` [K][T] is the gradient of the chosen scores (with
     ``idx_k``), ``dp`` [E] that of every token's probabilities, ``eps`` [E] the bias the router ran with; deps [E] is then the
-    gradient of eps, else None.  dxs may be None with x."""
+    gradient of eps, else None.  A group mean that is NaN counts as 0, as in the forward pass.  dxs may be None with x."""
     if stream is not None:
         with _under(stream):
             return sort_rows_grad(dxs, order, x, idx_k, dw, eps, dp, want_deps)
