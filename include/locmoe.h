@@ -595,8 +595,9 @@ int locmoe_block_norm_grad(const locmoe_shape_t *shape, int32_t C_alloc, const l
  * where dw float[K][T] is the gradient of the chosen scores w_k and dp float[E] that of any token's p_i, the same for all
  * tokens (alpha n f_i / T for the balance loss); either may be NULL.  deps float[E] (NULL to skip) = sum_t dG, the gradient of
  * eps.  A G_i that is NaN counts as 0, as in the forward pass.  dxs may be NULL with x.  The rows' sums of groups have to fit
- * shared memory: rows up to 375 KB, or 48000 elements where rows are no whole number of 16 bytes or groups are shorter (LOCMOE_ERR_TOO_LARGE); arrays that are not 16-byte
- * aligned count as such (LOCMOE_ERR_ALIGN).  ws (only with deps): locmoe_sort_grad_bytes() bytes, 256-byte aligned.
+ * shared memory: rows up to 375 KB, or 48000 elements where rows are no whole number of 16 bytes or groups are shorter
+ * (LOCMOE_ERR_TOO_LARGE); arrays that are not 16-byte aligned count as such (LOCMOE_ERR_ALIGN).  ws (only with deps):
+ * locmoe_sort_grad_bytes() bytes, 256-byte aligned.
  *
  * locmoe_unsort: out[t] = residual[t] + sum_c w_k[c][t] * y[slot[c][t]], y [V][H], out, residual (NULL: 0) [T][H] of x_dtype,
  * w_k float[K][T] (NULL: 1); choices with slot < 0 have no term.  fp32, in the order of c, rounded once.  out may be residual.
@@ -604,9 +605,9 @@ int locmoe_block_norm_grad(const locmoe_shape_t *shape, int32_t C_alloc, const l
  * locmoe_unsort_grad: dout [T][H] gives dy[slot[c][t]] = w_k[c][t] * dout[t] (zeros from offsets[E] on) and
  * dw[c][t] = <dout[t], y[slot[c][t]]> (0 where slot < 0), float[K][T]; dy or dw may be NULL, y only with dw NULL.
  *
- * E <= 1024 (LOCMOE_ERR_TOO_LARGE), V < 2^31.  H % E need only be 0 with the router's gradient.  The shape's node fields and
- * layout are validated but do not matter.  Pointers aligned to their elements; rows of whole 16-byte vectors in 16-byte
- * aligned arrays move fastest.  Row indices in slot outside [0, V) count as not routed.  All sums have a fixed order.
+ * E <= 1024, V < 2^31, H < 2^31 - 65535 (LOCMOE_ERR_TOO_LARGE).  H % E need only be 0 with the router's gradient.  The shape's
+ * node fields and layout are validated but do not matter.  Pointers aligned to their elements; rows of whole 16-byte vectors in
+ * 16-byte aligned arrays move fastest.  Row indices in slot outside [0, V) count as not routed.  All sums have a fixed order.
  */
 int locmoe_sort(const locmoe_shape_t *shape, int32_t K, const int32_t *idx_k, const void *x, int32_t *offsets, int32_t *slot,
                 int32_t *inv, int32_t *load, void *xs, void *stream);

@@ -521,7 +521,8 @@ int check_sorted(const locmoe_shape_t* s, int32_t K, bool groups) {
     const int rc = check_shape(&t);
     if (rc) return rc;
     if (K < 1 || K > 8) return LOCMOE_ERR_SHAPE;
-    if (s->E > 1024 || (long long)K * s->T > 0x7fffffffll) return LOCMOE_ERR_TOO_LARGE;
+    // the kernels' int counters of a row's units go on by a CTA's step beyond its end
+    if (s->E > 1024 || (long long)K * s->T > 0x7fffffffll || s->H > 0x7fffffff - 65535) return LOCMOE_ERR_TOO_LARGE;
     return LOCMOE_OK;
 }
 
