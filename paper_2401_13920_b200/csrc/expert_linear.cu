@@ -322,7 +322,7 @@ __device__ __forceinline__ void arithmetic(const LinearArgs& a, float2 (&v)[W / 
     if (KIND == kForward) {
         if (a.act == LOCMOE_ACT_GELU) {
 #pragma unroll
-            for (int i = 0; i < W / 2; ++i) v[i] = gelu_erf2(v[i]);
+            for (int i = 0; i < W / 2; ++i) v[i] = gelu2(v[i]);
         } else if (a.act == LOCMOE_ACT_SILU) {
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) v[i] = silu2(v[i]);
@@ -337,7 +337,7 @@ __device__ __forceinline__ void arithmetic(const LinearArgs& a, float2 (&v)[W / 
     } else if (KIND == kTowardsX) {
         if (a.act == LOCMOE_ACT_GELU) {
 #pragma unroll
-            for (int i = 0; i < W / 2; ++i) v[i] = __fmul2_rn(v[i], gelu_erf_slope2(unpack2(extra[i])));
+            for (int i = 0; i < W / 2; ++i) v[i] = __fmul2_rn(v[i], gelu_slope2(unpack2(extra[i])));
         } else if (a.act == LOCMOE_ACT_SILU) {
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) v[i] = __fmul2_rn(v[i], silu_slope2(unpack2(extra[i])));

@@ -88,8 +88,8 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) { tme
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld32(taddr, r); }
 
 // GeLU(v) = v * Phi(v) with Phi(v) = 1 - 0.5 erfc(v / sqrt 2).  erfc(x) = P(t) exp(-x^2), t = 1 / (1 + p x), for
-// x >= 0 by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (absolute error below 1.5e-7,
-// far under the bf16 rounding of the result); the negative side uses erfc(-x) = 2 - erfc(x) written so that a
+// x >= 0 by the five-term rational approximation of Abramowitz & Stegun 7.1.26 (absolute error below 1.5e-7, which is
+// less than the bf16 rounding of the result for v > -5); the negative side uses erfc(-x) = 2 - erfc(x) written so that a
 // small Phi is not formed by cancellation.  The reciprocal and the exponential are the hardware approximations
 // (rcp.approx, ex2.approx: a couple of ulps, far below the bf16 rounding of the result; 2.42 against 2.48 ms for the
 // first GEMM of the 65536 x 2560 x 10240 case).  About a third of the instructions of erff().
@@ -112,20 +112,35 @@ __device__ __forceinline__ float2 gelu_erf2(float2 v) {
     const float2 phi = make_float2(v.x < 0.0f ? h.x : om.x, v.y < 0.0f ? h.y : om.y);
     return __fmul2_rn(v, phi);
 }
-// Its slope Phi(z) + z phi(z), phi(z) = exp(-z^2 / 2) / sqrt(2 pi): the exponential of erfc serves both terms.
-__device__ __forceinline__ float2 gelu_erf_slope2(float2 z) {
-    const float2 x = __fmul2_rn(make_float2(fabsf(z.x), fabsf(z.y)), make_float2(0.70710678118654752f, 0.70710678118654752f));
-    const float2 den = __ffma2_rn(make_float2(0.3275911f, 0.3275911f), x, make_float2(1.0f, 1.0f));
+// The same for the products on sorted rows, with the digits kept far below zero: that formula's error is an absolute one, and
+// Phi(-6) = 1e-9 comes out 0.7 % off, more than a rounding to bf16.  Here erfc(x) / 2 = t P(t) exp(-x^2), t = 1 / (1 + 0.33 x), P a
+// polynomial of degree 7 fitted to the relative error for x up to 9.6 (weighted least squares, 8e-8), where the exponential leaves
+// the normal numbers; what remains is the rounding of the exponential's argument.  `ex`: exp(-v^2 / 2).
+__device__ __forceinline__ float2 normal_cdf2(float2 v, float2& ex) {
+    const float2 x = __fmul2_rn(make_float2(fabsf(v.x), fabsf(v.y)), make_float2(0.70710678118654752f, 0.70710678118654752f));
+    const float2 den = __ffma2_rn(make_float2(0.33f, 0.33f), x, make_float2(1.0f, 1.0f));
     const float2 t = make_float2(rcp_approx(den.x), rcp_approx(den.y));
-    float2 poly = __ffma2_rn(make_float2(0.5307027145f, 0.5307027145f), t, make_float2(-0.7265760135f, -0.7265760135f));
-    poly = __ffma2_rn(poly, t, make_float2(0.7107068705f, 0.7107068705f));
-    poly = __ffma2_rn(poly, t, make_float2(-0.142248368f, -0.142248368f));
-    poly = __ffma2_rn(poly, t, make_float2(0.127414796f, 0.127414796f));
+    float2 poly = __ffma2_rn(make_float2(-0.067964375f, -0.067964375f), t, make_float2(0.23134398f, 0.23134398f));
+    poly = __ffma2_rn(poly, t, make_float2(-0.17771928f, -0.17771928f));
+    poly = __ffma2_rn(poly, t, make_float2(0.20627064f, 0.20627064f));
+    poly = __ffma2_rn(poly, t, make_float2(0.022505404f, 0.022505404f));
+    poly = __ffma2_rn(poly, t, make_float2(0.100961894f, 0.100961894f));
+    poly = __ffma2_rn(poly, t, make_float2(0.09141863f, 0.09141863f));
+    poly = __ffma2_rn(poly, t, make_float2(0.093183056f, 0.093183056f));
     const float2 arg = __fmul2_rn(__fmul2_rn(x, x), make_float2(-1.4426950408889634f, -1.4426950408889634f));
-    const float2 ex = make_float2(ex2_approx(arg.x), ex2_approx(arg.y));
+    ex = make_float2(ex2_approx(arg.x), ex2_approx(arg.y));
     const float2 h = __fmul2_rn(__fmul2_rn(poly, t), ex);
     const float2 om = __ffma2_rn(h, make_float2(-1.0f, -1.0f), make_float2(1.0f, 1.0f));
-    const float2 phi = make_float2(z.x < 0.0f ? h.x : om.x, z.y < 0.0f ? h.y : om.y);
+    return make_float2(v.x < 0.0f ? h.x : om.x, v.y < 0.0f ? h.y : om.y);
+}
+__device__ __forceinline__ float2 gelu2(float2 v) {
+    float2 ex;
+    return __fmul2_rn(v, normal_cdf2(v, ex));
+}
+// Its slope Phi(z) + z phi(z), phi(z) = exp(-z^2 / 2) / sqrt(2 pi): the exponential of erfc serves both terms.
+__device__ __forceinline__ float2 gelu_slope2(float2 z) {
+    float2 ex;
+    const float2 phi = normal_cdf2(z, ex);
     return __ffma2_rn(__fmul2_rn(z, make_float2(0.39894228040143268f, 0.39894228040143268f)), ex, phi);
 }
 
