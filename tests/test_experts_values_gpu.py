@@ -27,6 +27,46 @@ def randn(g, *shape, dtype=F32, std=1.0):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,H,E,K", [(2, 64, 4, 1), (50, 64, 8, 2), (301, 120, 5, 3), (2000, 512, 32, 1)])
+def test_the_balance_loss_and_its_gradient_alone(X, T, H, E, K, dt):
+    """weight * alpha * E * sum_i f_i P_i against 64 bits, f of the kernel's own first choices, some experts liked more; and that a
+    loss with any of its factors lost or its sign turned would be seen."""
+    g, alpha, weight = gen(T), 0.07, 2.5
+    n = H // E
+    like = (torch.linspace(0.0, 1.0, E, device="cuda") + 0.1)[None, :, None]
+    x = (randn(g, T, E, n) + like).reshape(T, H).to(dt).requires_grad_()
+    eps = randn(g, E, std=0.05).requires_grad_()
+    _, _, aux, idx, *_ = X.RouteSort.apply(x, eps, E, K, alpha)
+    (weight * aux).backward()
+    f = torch.bincount(idx[0].long(), minlength=E).double() / T
+    G = x.detach().double().view(T, E, n).mean(2) + eps.detach().double()
+    p = torch.softmax(G.clamp_min(0.0), 1)
+    want = alpha * E * float((f * p.mean(0)).sum())
+    # the loss: sums of T and E terms in fp32, the exponentials a few steps
+    assert abs(float(aux.detach()) - want) <= (T + E + 16) * 2.0 ** -24 * want + 1e-5 * want
+    q = weight * alpha * E / T * f                              # gradient of every token's p
+    m = (p * q).sum(1, keepdim=True)
+    dG = torch.where(G > 0, p * (q - m), 0.0)
+    # as in the router's other test: G is off by `off`, p by 2 off, the exponential, the sum and the division; q by 8 roundings
+    off = (n + 3) * 2.0 ** -24 * (x.detach().double().abs().view(T, E, n).mean(2) + eps.detach().double().abs())
+    clear = G.abs() > off
+    assert clear.double().mean() > 0.99
+    rel = 2 * off.amax(1, keepdim=True) + (E + 8) * 2.0 ** -24
+    tol = p * (q + m) * (2 * rel + (E + 13) * 2.0 ** -24)
+    spread = lambda a: (a / n)[:, :, None].expand(T, E, n).reshape(T, H)
+    sure = spread(clear.double() * n) > 0.5
+
+    def fits(scale):
+        dx, deps = spread(dG) * scale, dG.sum(0) * scale
+        a = (x.grad.double() - dx).abs() <= HALF[dt] * dx.abs() + (1 + HALF[dt]) * spread(tol) * abs(scale)
+        b = (eps.grad.double() - deps).abs() <= abs(scale) * ((tol + torch.where(clear, 0.0, p * (q + m))).sum(0) + (T + 2) * 2.0 ** -24 * dG.abs().sum(0))
+        return bool((a | ~sure).all()), bool(b.all())
+    assert fits(1.0) == (True, True)
+    for scale in (1 / E, T, 1 / alpha, 1 / weight, -1.0, 0.0):
+        assert fits(scale) == (False, False)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("T,K,H,E", [(9, 2, 2560, 32), (33, 3, 777, 21), (50, 8, 1024, 1024), (31, 3, 1236, 6), (7001, 1, 72, 8), (6500, 2, 256, 64)])
 def test_a_group_mean_that_is_no_number_counts_as_zero(X, T, K, H, E, dt):
     """As in the forward pass: the same choices, scores and gradients, bit for bit, as for a group whose ReLU gives nothing."""
