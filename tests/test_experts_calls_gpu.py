@@ -194,3 +194,112 @@ def test_asking_for_a_leafs_stream_leaves_the_leaf_alone(X):
         del kept
     (x * 2.0).sum().backward()
     assert calls == [3.0, 5.0] and x.grad.tolist() == [2.0 + 3.0 + 10.0] * 4
+
+
+MARGIN = 4096
+
+
+class Guarded:
+    """Arrays in the middle of buffers of a fixed pattern: outputs, whose margins have to stay, and inputs, which have to stay."""
+
+    def __init__(self):
+        self.kept = []
+
+    def _place(self, n):
+        buf = torch.empty(n + 2 * MARGIN, dtype=U8, device="cuda")
+        buf.copy_((torch.arange(buf.numel(), device="cuda") * 37 + 11).to(U8))
+        return buf
+
+    def output(self, dtype, *shape):
+        n = torch.empty(0, dtype=dtype).element_size()
+        for s in shape:
+            n *= s
+        buf = self._place(n)
+        self.kept.append((buf, buf.clone(), n))
+        return buf[MARGIN:MARGIN + n].view(dtype).view(shape)
+
+    def input(self, t):
+        n = t.numel() * t.element_size()
+        buf = self._place(n)
+        inner = buf[MARGIN:MARGIN + n].view(t.dtype).view(t.shape)
+        inner.copy_(t)
+        self.kept.append((buf, buf.clone(), 0))
+        return inner
+
+    def check(self):
+        torch.cuda.synchronize()
+        for buf, was, n in self.kept:
+            at = MARGIN if n else buf.numel()
+            assert torch.equal(buf[:at], was[:at]) and torch.equal(buf[at + n:], was[at + n:])
+
+
+OFFSETS = [[0, 1, 2, 3, 4], [0, 0, 5, 6, 7], [1, 2, 2, 5, 6], [0, 90, 20, 2 ** 31 - 1, 70], [-5, -2 ** 31, 30, 10, 500], [70, 70, 0, 0, -1], [2 ** 31 - 1] * 5,
+           [0, 40, 40, 41, 66], [7, 0, 7, 0, 7], [0, 2 ** 31 - 1, 0, 2 ** 31 - 1, 0]]
+
+
+@pytest.mark.parametrize("offsets", OFFSETS)
+@pytest.mark.parametrize("R", [1, 7, 70, 131])
+def test_products_write_their_outputs_and_nothing_else(X, B, R, offsets):
+    """Ordinary offsets, and such as descend or leave the rows, in the form without tiles, with them, and every gradient."""
+    g, E, IN, OUT = gen(R), 4, 72, 264
+    G = Guarded()
+    o = G.input(torch.tensor(offsets, dtype=I32, device="cuda"))
+    x, w, dy, z = (G.input(t) for t in (randn(g, R, IN, dtype=BF), randn(g, E, OUT, IN, dtype=BF), randn(g, R, OUT, dtype=BF), randn(g, R, IN, dtype=BF)))
+    bias, res = G.input(randn(g, E, OUT)), G.input(randn(g, R, OUT, dtype=BF))
+    shape = B.Shape(R, IN, E, 1, 1, B.BF16, 0)
+    ws = G.output(U8, B.locmoe_expert_linear_bytes(shape, OUT))
+    B.locmoe_expert_linear(shape, OUT, x, w, o, G.output(BF, R, OUT), ws, bias, res, G.output(BF, R, OUT), B.ACT_GELU)
+    ws = G.output(U8, B.locmoe_expert_linear_bytes(shape, OUT, True))
+    for dwt in (BF, F32):
+        B.locmoe_expert_linear_grad(shape, OUT, dy, o, x, w, z, G.output(BF, R, IN), G.output(dwt, E, OUT, IN), G.output(F32, E, OUT), B.ACT_SILU, ws)
+    B.locmoe_expert_linear_grad(shape, OUT, dy, o, db=G.output(F32, E, OUT))
+    G.check()
+    assert B.locmoe_device_flags() == 0
+
+
+def test_split_products_write_their_outputs_and_nothing_else(X, B):
+    """Few tiles with a long reduction, in runs that leave sums in the workspace."""
+    g, E, R, IN, OUT = gen(3), 2, 1200, 2048, 136
+    for offsets in ([0, 1100, 1190], [3, 2 ** 31 - 1, 40]):
+        G = Guarded()
+        o = G.input(torch.tensor(offsets, dtype=I32, device="cuda"))
+        x, w, dy = (G.input(t) for t in (randn(g, R, IN, dtype=BF), randn(g, E, OUT, IN, dtype=BF), randn(g, R, OUT, dtype=BF)))
+        shape = B.Shape(R, IN, E, 1, 1, B.BF16, 0)
+        B.locmoe_expert_linear(shape, OUT, x, w, o, G.output(BF, R, OUT), G.output(U8, B.locmoe_expert_linear_bytes(shape, OUT)))
+        B.locmoe_expert_linear_grad(shape, OUT, dy, o, x, w, None, G.output(BF, R, IN), G.output(F32, E, OUT, IN), G.output(F32, E, OUT), B.ACT_NONE,
+                                    G.output(U8, B.locmoe_expert_linear_bytes(shape, OUT, True)))
+        G.check()
+    assert B.locmoe_device_flags() == 0
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,K,H,E", [(5, 2, 72, 4), (33, 3, 777, 7), (1500, 2, 96, 8), (700, 5, 40, 5)])
+def test_rows_are_written_and_nothing_else(X, B, T, K, H, E, dt):
+    """Choices that are no experts, slots that are no rows, offsets that promise more or fewer rows than there are."""
+    g, G = gen(T), Guarded()
+    V, code = K * T, B.F32 if dt is F32 else B.BF16
+    shape = B.Shape(T, H, E, 1, 1, code, 0)
+    wild = torch.tensor([-1, -7, E, 2 ** 31 - 1, -2 ** 31], dtype=I32, device="cuda")
+    idx = torch.randint(0, E, (K, T), generator=g, device="cuda", dtype=I32)
+    idx = G.input(torch.where(torch.rand(K, T, generator=g, device="cuda") < 0.3, wild[torch.randint(0, 5, (K, T), generator=g, device="cuda")], idx))
+    x, y, dout = G.input(randn(g, T, H, dtype=dt)), G.input(randn(g, V, H, dtype=dt)), G.input(randn(g, T, H, dtype=dt))
+    w, eps, dp = G.input(randn(g, K, T)), G.input(randn(g, E)), G.input(randn(g, E))
+    offsets, slot, inv = G.output(I32, E + 1), G.output(I32, K, T), G.output(I32, V)
+    B.locmoe_sort(shape, K, idx, offsets, slot, inv, G.output(I32, E), x, G.output(dt, V, H))
+    B.locmoe_sort(shape, K, idx, offsets, slot, inv, None)
+    bad = torch.where(torch.rand(K, T, generator=g, device="cuda") < 0.2, torch.tensor(2 ** 31 - 1, dtype=I32, device="cuda"), slot)
+    bad = G.input(torch.where(torch.rand(K, T, generator=g, device="cuda") < 0.2, torch.tensor(V, dtype=I32, device="cuda"), bad))
+    for s in (slot, bad):
+        for last in (None, -5, V, 2 ** 31 - 1):
+            o = offsets
+            if last is not None:
+                o = offsets.clone()
+                o[E] = last
+                o = G.input(o)
+            B.locmoe_unsort_grad(shape, K, dout, o, s, y, w, G.output(dt, V, H), G.output(F32, K, T))
+        B.locmoe_unsort(shape, K, y, s, G.output(dt, T, H), w, dout)
+        if H % E == 0:
+            B.locmoe_sort_grad(shape, K, s, G.output(dt, T, H), y, x, eps, idx, w, dp, G.output(F32, E), G.output(U8, B.locmoe_sort_grad_bytes(shape)))
+        B.locmoe_sort_grad(shape, K, s, G.output(dt, T, H), y)
+    G.check()
+    assert B.locmoe_device_flags() == 0
