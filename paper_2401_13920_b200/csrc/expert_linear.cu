@@ -1034,7 +1034,8 @@ __global__ void __launch_bounds__(kBiasThreads) expert_bias_grad_kernel(const in
 // Weights' gradients: up to this many rows an expert on average a tile is stores more than products, and its rows leave as boxes of
 // 128 bytes a row by TMA; a lane's stores of its own row are 32 bytes each, half sectors where rows do not begin on 32 (72
 // rows of 12 experts, weights of 5440 x 8984: 686 against 324 us).  The boxes take the fourth stage of the ring, which long
-// reductions need (65536 rows of 10240 x 2560: 64 % of the tensor cores' cycles with three stages, 80 % with four).
+// reductions need (65536 rows of 10240 x 2560: 64 % of the tensor cores' cycles with three stages, 80 % with four).  Between 128 and
+// 512 rows an expert neither is near the copy rate (2560 x 10240 of 32 experts: 64 rows 313 us, 4096 391, 8192 579; 256 to 288 there).
 constexpr int kBoxRows = 512;
 
 // Rows of a tile.  256 rows share each weight tile's load: 32 instead of 48 KB for 128 x 256 x 64 products come through the SM's
@@ -1045,7 +1046,7 @@ constexpr int kBoxRows = 512;
 // split more dearly: 12332 rows in 8 experts, 2528 x 1784, 3.8 waves, 123 against 166); with whole sectors only for weights'
 // gradients of very many tiles (65536 rows in 32 experts, 2560 x 10240: 3225 against 2957 us; 20893 rows in 8, 2944 x 4672,
 // 12 waves: 495 against 549), and not for products with few rows or an epilogue that costs more (65536 rows forward with
-// GeLU and z: 3137 against 3696).
+// GeLU and z: 3137 against 3696).  Long reductions on whole sectors without such an epilogue were not measured with 256.
 constexpr int kTallRows = 1024, kTallK = 1536;
 int rows_of_tile(Kind kind, long long R, int E, int M, int N, int K) {
     const long long tiles = (kind == kWeights ? (long long)E * ((M + 2 * BM - 1) / (2 * BM)) : R / (2 * BM)) * ((N + BN - 1) / BN);

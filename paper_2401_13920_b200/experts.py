@@ -428,7 +428,8 @@ def moe_layer(x, w_in, w_out, K=1, b_in=None, b_out=None, eps=None, act="gelu", 
     """The MoE layer without a capacity: out[t] = residual[t] + sum over the K best experts of score * FFN_e(x[t]).
 
     x [T][H], w_in [E][F][H], w_out [E][H][F] bf16; b_in [E][F], b_out [E][H] and eps [E] (the router's bias) fp32, or None.
-    Returns ``(out, aux)``, aux the load-balance loss with alpha > 0, else None.  Differentiable in all tensors.
+    Returns ``(out, aux)``, aux the load-balance loss with alpha > 0, else None.  Differentiable in all tensors.  Every token is
+    routed; a padded batch goes through the functions one by one (``sort_rows`` takes -1 for a token that is not).
 
     Forward and backward can be captured into a CUDA graph; no graph of the same leaves that was built on the default stream, by
     whatever operator, may then be alive (the backward pass refuses leaves of its own inputs that are held so)."""
